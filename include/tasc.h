@@ -430,6 +430,107 @@ tasc_status tasc_tok_enrich(const int32_t* tokens, const int64_t* doc_offsets, i
                             int64_t* out_offsets, int32_t* n_merges);
 
 /* ------------------------------------------------------------------------------------------
+ * The operators of a serving step over a cache held in 4 bits: block tables and slots from the requests' lengths, the cache,
+ * attention over it, and the verification of drafts against the target's probabilities.  They take device arrays and enqueue
+ * on `stream` without a host round trip, so a step of them can be recorded into a HIP graph; array contents are bounds-checked
+ * on the device (a length, page or token outside its range is handled as stated, never followed).
+ * Pages hold TASC_PAGE_TOKENS positions.  A slot is page * TASC_PAGE_TOKENS + position in the page.
+ * ---------------------------------------------------------------------------------------- */
+#define TASC_PAGE_TOKENS 16
+
+/*
+ * Grows the requests' block tables to their lengths and lists the slots of the step's rows.
+ *   kv_len     int32[batch]  tokens a sequence holds after this step, its new rows among them
+ *   new_rows   int32[batch], nullable (no rows)  rows it adds, its last positions
+ *   held       int32[batch], nullable (none)  pages its table already lists
+ *   free_pages int32[n_free], nullable (0, 1, ..)  pages to give away, in this order
+ *   table      int32[batch, max_pages]  entries held .. are written where pages are given, all others left as they are
+ *   pages      int32[batch], nullable  pages the table lists afterwards; not the same array as `held`
+ *   row_off    int32[batch + 1], nullable  running sum of new_rows
+ *   slots      int32[slots_cap], nullable  the rows' slots, sequence by sequence, then -1
+ *   summary    int32[3], nullable  rows, pages given away, sequences refused
+ * Pages go to the sequences in order.  A sequence whose pages no longer fit what is left, whose length is beyond max_pages pages, or whose
+ * numbers make no sense (kv_len or new_rows < 0, new_rows > kv_len, held outside [0, max_pages]) is refused: its table stays,
+ * its rows (those of new_rows >= 0) have slot -1.  A sequence that needs fewer pages than it holds keeps them.
+ * Errors: TASC_EINVAL, TASC_EHIP.
+ */
+tasc_status tasc_page_tables(const int32_t* kv_len, const int32_t* new_rows, const int32_t* held, int32_t batch,
+                             const int32_t* free_pages, int32_t n_free, int32_t* table, int32_t max_pages, int32_t* pages,
+                             int32_t* row_off, int32_t* slots, int32_t slots_cap, int32_t* summary, void* stream);
+
+/*
+ * A paged cache of keys and values in 4 bits (one layer): a token's head in groups of min(head_dim, 64) channels, each group with
+ * scale = bf16((hi - lo) * (1 / 15)) and low = bf16(lo) of its least and largest value (the steps in fp32); a value is held as the whole number in [0, 15]
+ * nearest to (value - low) / scale (the even one of two; 0 where scale is 0) and stands for low + scale * number, computed in
+ * fp32.  A group that holds an infinity or a NaN, or whose range is beyond fp32, reads as NaN.
+ *   pool  DEVICE, 256-byte aligned, n_pages * tasc_kv4_page_bytes; what has not been written may hold anything
+ */
+typedef struct {
+    void* pool;
+    int32_t n_pages, n_kv_heads, head_dim; /* head_dim 32, 64 or 128; n_pages < 2^27 */
+} tasc_kv4_cache;
+/* Bytes of a page (keys and values of all heads); 0 for shapes that are not served. */
+size_t tasc_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim);
+/*
+ * Writes the keys and values of `rows` rows: row i is [n_kv_heads, head_dim] at k + i * k_stride (elements of `dtype`, fp32 or bf16), so both may
+ * lie inside the rows of a fused projection.  A row whose slot is negative or outside the pool is skipped.  The slots of a call must
+ * differ: what a slot named twice holds afterwards is unspecified (no other slot is touched).
+ */
+tasc_status tasc_kv4_append(const tasc_kv4_cache* c, const void* k, const void* v, tasc_dtype dtype, int64_t k_stride,
+                            int64_t v_stride, const int32_t* slots, int32_t rows, void* stream);
+/* The values that slots hold: k, v [rows, n_kv_heads, head_dim] of `dtype`, 16-byte aligned; zeros for a slot outside the pool. */
+tasc_status tasc_kv4_read(const tasc_kv4_cache* c, const int32_t* slots, int32_t rows, tasc_dtype dtype, void* k, void* v,
+                          void* stream);
+
+/*
+ * Grouped-query attention of the step's rows over the cache: softmax(scale q . key) value, query head j reads KV head
+ * j * n_kv_heads / n_heads.  Sequence b has the rows row_off[b] .. row_off[b + 1] and kv_len[b] tokens, the rows' own (appended before) the
+ * last of them; row i of n sees positions 0 .. kv_len - n + i.  A row that sees nothing gives zeros; tokens on a page outside
+ * [0, n_pages) are not seen.  Rows at or behind row_off[batch] are left as they are.  max_rows and max_kv are the host's upper bounds
+ * (of rows per sequence: further rows are left out; of kv_len: a hint that sizes the grid).  fp32 scores, sums and products of bf16
+ * weights; a row's bits do not depend on the other rows' contents.
+ */
+typedef struct {
+    const void* q;          /* bf16 [rows, n_heads, head_dim], rows q_stride elements apart (a multiple of 8, 16-byte aligned) */
+    void* out;              /* bf16, rows out_stride elements apart (likewise) */
+    int64_t q_stride, out_stride;
+    const int32_t* table;   /* [batch, max_pages] */
+    const int32_t* row_off; /* [batch + 1] */
+    const int32_t* kv_len;  /* [batch] */
+    int32_t max_pages, batch, rows, n_heads, max_rows, max_kv;
+    float scale;
+} tasc_kv4_attn;
+/* Bytes of scratch for such a call (0: none needed, or a shape that is not served).  Calls that may overlap need their own. */
+size_t tasc_kv4_attention_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
+                                          int32_t max_rows, int32_t max_kv);
+tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv4_attn* a, void* workspace, size_t ws_bytes, void* stream);
+
+/*
+ * Verification of drafted tokens against the target's probabilities, from given random numbers (paper, subsection "Speculative
+ * Decoding": a drafted token is accepted with probability min(1, p / q), the first that is not is replaced by a draw from the
+ * normalised max(0, p - q), and if all are accepted the next token is drawn from p; the emitted tokens are then distributed as if
+ * the target had been sampled token by token).  p is the softmax of logits / temperature; row i of a sequence scores its draft i, the last
+ * row follows them.
+ *   logits       [batch, k + 1, vocab] of `dtype` (fp32 or bf16), rows row_stride elements apart; -infinity masks a token
+ *   drafts       int32[batch, k]; a value outside [0, vocab) ends the sequence's drafts (its row draws from p)
+ *   draft_probs  fp32[batch, k, vocab], nullable: the distributions q that the drafts were drawn from; NULL: they were chosen
+ *                without chance (q is 1 at the draft)
+ *   temperature  fp32[batch], nullable (1); 0: the target is greedy (p is 1 at the largest logit, lowest index among equals)
+ *   u            fp32[batch, k + 1, 2] in [0, 1): [i][0] decides on draft i, [i][1] draws the token at position i
+ *   accept_len   int32[batch]  drafts accepted;  emitted int32[batch, k + 1]  those, then the drawn token, then -1
+ *   logprob      fp32[batch, k + 1], nullable: ln p of the emitted tokens, then 0
+ * A draft is accepted iff u q < p; the drawn token is the lowest one up to which the weights sum to more than u times their total.
+ * Exponentials and sums are taken in 64 bits.  A row that has no distribution (a NaN, +infinity, nothing above -infinity, a
+ * temperature below 0 or NaN) accepts nothing and emits -1 with a NaN as logprob.
+ * Errors: TASC_EINVAL (k outside [0, TASC_MAX_K], vocab outside [2, 2^24]), TASC_ENOMEM (workspace), TASC_EHIP.
+ */
+size_t tasc_accept_sampled_workspace_bytes(int32_t batch, int32_t k, int32_t vocab);
+tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab,
+                                const int32_t* drafts, const float* draft_probs, const float* temperature, const float* u,
+                                int32_t* accept_len, int32_t* emitted, float* logprob, void* workspace, size_t ws_bytes,
+                                void* stream);
+
+/* ------------------------------------------------------------------------------------------
  * Measurement: per-kernel-class device time, taken with HIP event pairs recorded on the stream
  * each kernel is launched on.  Off by default (no events are recorded).  The classes follow the
  * steps of the hot path: table build is timed by tasc_ngram_get_stats, the rest here.

@@ -22,6 +22,8 @@ EXPORTS = [
     "tasc_ngram_unigram", "tasc_ngram_get_stats", "tasc_ngram_entropy", "tasc_ngram_entropy_noalloc", "tasc_model_bigram", "tasc_ngram_from_bigram", "tasc_tok_enrich", "tasc_model_create", "tasc_model_destroy", "tasc_session_kv_bytes",
     "tasc_session_workspace_bytes", "tasc_session_create", "tasc_session_destroy", "tasc_session_prefill", "tasc_draft",
     "tasc_verify_step", "tasc_generate", "tasc_session_get_tokens", "tasc_session_status", "tasc_profile_enable", "tasc_profile_read", "tasc_profile_durations", "tasc_config_set", "tasc_profile_phases", "tasc_calibration_copy", "tasc_calibration_mfma", "tasc_calibration_read", "tasc_calibration_handover", "tasc_calibration_gemm",
+    "tasc_page_tables", "tasc_kv4_page_bytes", "tasc_kv4_append", "tasc_kv4_read", "tasc_kv4_attention_workspace_bytes",
+    "tasc_kv4_attention", "tasc_accept_sampled_workspace_bytes", "tasc_accept_sampled",
 ]
 KERNEL_CLASSES = ["draft", "prepare", "norm", "gemm_qkv", "rope_kv", "attn", "gemm_o", "gemm_gu", "gemm_d", "lmhead", "accept",
                   "verify", "layers"]
@@ -66,6 +68,16 @@ class GenStats(C.Structure):
     _fields_ = [("steps", C.c_int64), ("emitted", C.c_int64), ("accepted", C.c_int64), ("proposed", C.c_int64),
                 ("accept_hist", C.c_int64 * (TASC_MAX_K + 1)), ("prefill_ms", C.c_double), ("decode_ms", C.c_double),
                 ("xcd_local_steps", C.c_int64)]
+
+
+class Kv4CacheDesc(C.Structure):
+    _fields_ = [("pool", C.c_void_p), ("n_pages", C.c_int32), ("n_kv_heads", C.c_int32), ("head_dim", C.c_int32)]
+
+
+class Kv4Attn(C.Structure):
+    _fields_ = [("q", C.c_void_p), ("out", C.c_void_p), ("q_stride", C.c_int64), ("out_stride", C.c_int64), ("table", C.c_void_p),
+                ("row_off", C.c_void_p), ("kv_len", C.c_void_p), ("max_pages", C.c_int32), ("batch", C.c_int32), ("rows", C.c_int32),
+                ("n_heads", C.c_int32), ("max_rows", C.c_int32), ("max_kv", C.c_int32), ("scale", C.c_float)]
 
 
 _lib = None
@@ -121,6 +133,18 @@ def lib():
         L.tasc_profile_enable.argtypes = [C.c_uint32]
         L.tasc_profile_read.argtypes = [C.c_void_p, C.c_void_p]
         L.tasc_profile_durations.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.POINTER(C.c_int64)]
+        L.tasc_page_tables.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p,
+                                       C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
+        for name in ("tasc_kv4_page_bytes", "tasc_kv4_attention_workspace_bytes", "tasc_accept_sampled_workspace_bytes"):
+            getattr(L, name).restype = C.c_size_t
+        L.tasc_kv4_page_bytes.argtypes = [C.c_int32] * 2
+        L.tasc_kv4_append.argtypes = [C.POINTER(Kv4CacheDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p]
+        L.tasc_kv4_read.argtypes = [C.POINTER(Kv4CacheDesc), C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.tasc_kv4_attention_workspace_bytes.argtypes = [C.c_int32] * 7
+        L.tasc_kv4_attention.argtypes = [C.POINTER(Kv4CacheDesc), C.POINTER(Kv4Attn), C.c_void_p, C.c_size_t, C.c_void_p]
+        L.tasc_accept_sampled_workspace_bytes.argtypes = [C.c_int32] * 3
+        L.tasc_accept_sampled.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                          C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         for name in ("tasc_ngram_destroy", "tasc_model_destroy", "tasc_session_destroy"):
             getattr(L, name).argtypes = [C.c_void_p]
             getattr(L, name).restype = None
@@ -451,3 +475,173 @@ def tasc_calibration_handover(n_workgroups, stride, nbytes, with_flags=False, st
 def tasc_calibration_copy(dst, src, stream=None):
     """dst, src: cuda uint8 tensors of equal size (a multiple of 16 bytes)."""
     _check(lib().tasc_calibration_copy(_ptr(dst), _ptr(src), src.numel() * src.element_size(), _stream(stream)))
+
+
+# ---------------------------------------------------------------- the operators of a serving step over a 4-bit cache
+def _refuse(message):
+    raise TascError(TASC_EINVAL, message)
+
+
+def _device_array(who, name, t, dtype, shape, optional=False):
+    """Address of a contiguous tensor of the current device with this dtype and shape (None: any length there)."""
+    if t is None and optional:
+        return None
+    import torch
+    if not torch.is_tensor(t) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.dim() != len(shape) or \
+            any(n is not None and n != m for n, m in zip(shape, t.shape)):
+        _refuse(f"{who}: {name} is not a contiguous {dtype} tensor of shape {tuple(shape)} on the device")
+    if t.device.index != torch.cuda.current_device():
+        _refuse(f"{who}: {name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    return t.data_ptr()
+
+
+def _row_stride(who, name, t, dtypes, width):
+    """Elements from row to row of a tensor [rows, heads, head_dim] or [.., vocab] whose rows are `width` elements side by side."""
+    import torch
+    if not torch.is_tensor(t) or not t.is_cuda or t.dtype not in dtypes:
+        _refuse(f"{who}: {name} is not a device tensor of {' or '.join(str(d) for d in dtypes)}")
+    if t.device.index != torch.cuda.current_device():
+        _refuse(f"{who}: {name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
+    if t.numel() == 0:
+        return width
+    inner = 1
+    for n, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
+        if n != 1 and stride != inner:
+            _refuse(f"{who}: the elements of a row of {name} are not side by side")
+        inner *= n
+    return t.stride(0) if t.shape[0] > 1 else width
+
+
+def _workspace(who, workspace, need, stream):
+    """(tensor kept alive, address, bytes).  A workspace made here belongs to the current stream."""
+    import torch
+    if workspace is None:
+        if need and stream is not None and stream != torch.cuda.current_stream().cuda_stream:
+            _refuse(f"{who}: a call on a stream other than the current one needs a workspace of {need} bytes")
+        workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
+    elif not workspace.is_cuda or not workspace.is_contiguous() or workspace.device.index != torch.cuda.current_device():
+        _refuse(f"{who}: the workspace is not a contiguous tensor of the current device")
+    return workspace, workspace.data_ptr() or None, workspace.numel() * workspace.element_size()
+
+
+def _same_length(who, **lengths):
+    if len(set(lengths.values())) > 1:
+        _refuse(f"{who}: " + ", ".join(f"{k} has {v}" for k, v in lengths.items()))
+
+
+def tasc_page_tables(kv_len, new_rows, held, free_pages, table, pages=None, row_off=None, slots=None, summary=None, n_free=None, stream=None):
+    """int32 cuda tensors: kv_len, new_rows, held, pages [batch], free_pages [n_free] (None: the pages 0 .. n_free - 1), table [batch, max_pages],
+    row_off [batch + 1], slots [any], summary [3]; table, pages, row_off, slots and summary are written in place."""
+    import torch
+    who, i32 = "page_tables", torch.int32
+    B = kv_len.shape[0]
+    max_pages = table.shape[1] if table.dim() == 2 else 0
+    if free_pages is not None and n_free is None:
+        n_free = free_pages.shape[0]
+    if free_pages is not None and n_free > free_pages.shape[0]:
+        _refuse(f"{who}: n_free {n_free} of {free_pages.shape[0]} free pages")
+    a = lambda name, t, shape, optional=True: _device_array(who, name, t, i32, shape, optional)
+    _check(lib().tasc_page_tables(a("kv_len", kv_len, (B,), False), a("new_rows", new_rows, (B,)), a("held", held, (B,)), B,
+                                  a("free_pages", free_pages, (None,)) or None, n_free or 0, a("table", table, (B, max_pages), False), max_pages,
+                                  a("pages", pages, (B,)), a("row_off", row_off, (B + 1,)), a("slots", slots, (None,)) or None,
+                                  0 if slots is None else slots.shape[0], a("summary", summary, (3,)), _stream(stream)))
+
+
+def tasc_kv4_page_bytes(n_kv_heads, head_dim) -> int:
+    return lib().tasc_kv4_page_bytes(n_kv_heads, head_dim)
+
+
+class Kv4Cache:
+    """A paged 4-bit cache of one layer: `pool` (made here unless given, of n_pages * tasc_kv4_page_bytes bytes) and its shape."""
+
+    def __init__(self, n_pages, n_kv_heads, head_dim, pool=None):
+        import torch
+        page = tasc_kv4_page_bytes(n_kv_heads, head_dim)
+        if page == 0 or n_pages < 1:
+            _refuse(f"Kv4Cache: {n_pages} pages of {n_kv_heads} KV heads of {head_dim} channels")
+        if pool is None:
+            pool = torch.empty(n_pages * page, dtype=torch.uint8, device="cuda")
+        elif not pool.is_cuda or not pool.is_contiguous() or pool.numel() * pool.element_size() < n_pages * page:
+            _refuse(f"Kv4Cache: the pool does not hold {n_pages} pages of {page} bytes")
+        self.pool, self.n_pages, self.n_kv_heads, self.head_dim = pool, n_pages, n_kv_heads, head_dim
+        self.desc = Kv4CacheDesc(pool.data_ptr(), n_pages, n_kv_heads, head_dim)
+
+    def _ref(self, who):
+        import torch
+        if self.pool.device.index != torch.cuda.current_device():
+            _refuse(f"{who}: the cache is on {self.pool.device}, the current device is cuda:{torch.cuda.current_device()}")
+        return C.byref(self.desc)
+
+
+def _float_dtype(t):
+    import torch
+    return TASC_F32 if t.dtype == torch.float32 else TASC_BF16
+
+
+def tasc_kv4_append(cache: Kv4Cache, k, v, slots, stream=None):
+    """k, v: cuda tensors [rows, n_kv_heads, head_dim], fp32 or bf16 (both alike), a row's elements side by side; slots: int32 [rows]."""
+    import torch
+    who, shape = "kv4_append", (slots.shape[0], cache.n_kv_heads, cache.head_dim)
+    if tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != v.dtype:
+        _refuse(f"{who}: keys {tuple(k.shape)} {k.dtype}, values {tuple(v.shape)} {v.dtype} for rows of shape {shape}")
+    width = cache.n_kv_heads * cache.head_dim
+    ks, vs = (_row_stride(who, n, t, (torch.float32, torch.bfloat16), width) for n, t in (("k", k), ("v", v)))
+    _check(lib().tasc_kv4_append(cache._ref(who), k.data_ptr(), v.data_ptr(), _float_dtype(k), ks, vs,
+                                 _device_array(who, "slots", slots, torch.int32, (None,)), shape[0], _stream(stream)))
+
+
+def tasc_kv4_read(cache: Kv4Cache, slots, k, v, stream=None):
+    """k, v: cuda tensors [rows, n_kv_heads, head_dim], fp32 or bf16 (both alike), written in place; slots: int32 [rows]."""
+    import torch
+    who, shape = "kv4_read", (slots.shape[0], cache.n_kv_heads, cache.head_dim)
+    if k.dtype not in (torch.float32, torch.bfloat16):
+        _refuse(f"{who}: {k.dtype} is neither float32 nor bfloat16")
+    _check(lib().tasc_kv4_read(cache._ref(who), _device_array(who, "slots", slots, torch.int32, (None,)), shape[0], _float_dtype(k),
+                               _device_array(who, "k", k, k.dtype, shape), _device_array(who, "v", v, k.dtype, shape), _stream(stream)))
+
+
+def tasc_kv4_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, head_dim, max_rows, max_kv) -> int:
+    return lib().tasc_kv4_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, head_dim, max_rows, max_kv)
+
+
+def tasc_kv4_attention(cache: Kv4Cache, q, table, row_off, kv_len, max_rows, max_kv, scale, out, workspace=None, stream=None):
+    """q, out: bf16 cuda tensors [rows, n_heads, head_dim], a row's elements side by side; table int32 [batch, max_pages], row_off int32
+    [batch + 1], kv_len int32 [batch].  out is written in place."""
+    import torch
+    who = "kv4_attention"
+    if q.dim() != 3 or q.shape != out.shape or q.shape[2] != cache.head_dim:
+        _refuse(f"{who}: queries {tuple(q.shape)}, results {tuple(out.shape)} over heads of {cache.head_dim}")
+    rows, H, hd = q.shape
+    B = kv_len.shape[0]
+    max_pages = table.shape[1] if table.dim() == 2 else 0
+    a = Kv4Attn(q.data_ptr(), out.data_ptr(), _row_stride(who, "q", q, (torch.bfloat16,), H * hd), _row_stride(who, "out", out, (torch.bfloat16,), H * hd),
+                _device_array(who, "table", table, torch.int32, (B, max_pages)), _device_array(who, "row_off", row_off, torch.int32, (B + 1,)),
+                _device_array(who, "kv_len", kv_len, torch.int32, (B,)), max_pages, B, rows, H, max_rows, max_kv, scale)
+    need = 0 if workspace is not None else tasc_kv4_attention_workspace_bytes(B, rows, H, cache.n_kv_heads, hd, max_rows, max_kv)
+    keep, ws, n = _workspace(who, workspace, need, stream)
+    _check(lib().tasc_kv4_attention(cache._ref(who), C.byref(a), ws, n, _stream(stream)))
+
+
+def tasc_accept_sampled_workspace_bytes(batch, k, vocab) -> int:
+    return lib().tasc_accept_sampled_workspace_bytes(batch, k, vocab)
+
+
+def tasc_accept_sampled(logits, drafts, draft_probs, temperature, u, accept_len, emitted, logprob=None, workspace=None, stream=None):
+    """logits: fp32 or bf16 cuda tensor [batch, k + 1, vocab], its rows evenly spaced; drafts int32 [batch, k], draft_probs fp32 [batch, k, vocab]
+    or None, temperature fp32 [batch] or None, u fp32 [batch, k + 1, 2]; accept_len int32 [batch], emitted int32 [batch, k + 1] and
+    logprob fp32 [batch, k + 1] (or None) are written in place."""
+    import torch
+    who, f32, i32 = "accept_sampled", torch.float32, torch.int32
+    if not torch.is_tensor(logits) or logits.dim() != 3:
+        _refuse(f"{who}: logits are not [batch, k + 1, vocab]")
+    B, nq, V = logits.shape
+    if B > 1 and nq > 1 and logits.stride(0) != nq * logits.stride(1):
+        _refuse(f"{who}: the rows of logits are not evenly spaced")
+    stride = _row_stride(who, "logits", logits[:, 0] if nq == 1 else logits[0] if B else logits.reshape(-1, V), (f32, torch.bfloat16), V)
+    a = lambda name, t, dtype, shape, optional=False: _device_array(who, name, t, dtype, shape, optional)
+    need = 0 if workspace is not None else tasc_accept_sampled_workspace_bytes(B, nq - 1, V)
+    keep, ws, n = _workspace(who, workspace, need, stream)
+    _check(lib().tasc_accept_sampled(logits.data_ptr(), _float_dtype(logits), stride, B, nq - 1, V, a("drafts", drafts, i32, (B, nq - 1), nq == 1),
+                                     a("draft_probs", draft_probs, f32, (B, nq - 1, V), True), a("temperature", temperature, f32, (B,), True),
+                                     a("u", u, f32, (B, nq, 2)), a("accept_len", accept_len, i32, (B,)), a("emitted", emitted, i32, (B, nq)),
+                                     a("logprob", logprob, f32, (B, nq), True), ws, n, _stream(stream)))

@@ -1,0 +1,143 @@
+// Block tables and slots of a paged cache from the requests' lengths.
+//
+// One launch: every workgroup owns a run of sequences, sums the pages and rows that all sequences ask for (those before its own
+// give its place in the list of free pages and in the list of slots), and a wave writes a sequence's new pages and slots.  A few integers
+// per sequence, page and row: bound by launch latency and two dependent reads.
+#include "tasc_internal.h"
+#include <algorithm>
+
+namespace {
+
+constexpr int kThreads = 512, kWaves = kThreads / 64;
+
+struct PageArgs {
+    const int32_t* kv_len;
+    const int32_t* new_rows;
+    const int32_t* held;
+    const int32_t* free_pages;
+    int32_t *table, *pages, *row_off, *slots, *summary;
+    int32_t batch, n_free, max_pages, slots_cap, per_wg;
+};
+
+struct Ask { int32_t len, rows, held, need, pages; bool fits; };   // rows: those that count in row_off; pages: new ones
+__device__ __forceinline__ Ask ask_of(const PageArgs& a, int b) {
+    Ask q;
+    q.len = a.kv_len[b];
+    const int32_t n = a.new_rows ? a.new_rows[b] : 0;
+    q.held = a.held ? a.held[b] : 0;
+    q.rows = max(n, 0);
+    q.need = q.len > 0 ? (q.len - 1) / TASC_PAGE_TOKENS + 1 : 0;
+    q.fits = n >= 0 && n <= q.len && q.need <= a.max_pages && q.held >= 0 && q.held <= a.max_pages;
+    q.pages = q.fits ? max(q.need - q.held, 0) : 0;
+    return q;
+}
+__device__ __forceinline__ int64_t wave_sum64(int64_t v) {
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+__global__ __launch_bounds__(kThreads) void k_page_tables(PageArgs a) {
+    __shared__ int64_t s_sum[4][kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int b0 = (int)min((int64_t)blockIdx.x * a.per_wg, (int64_t)a.batch), b1 = min(b0 + a.per_wg, a.batch);
+    int64_t pages_before = 0, rows_before = 0, rows_all = 0;
+    for (int b = tid; b < a.batch; b += kThreads) {
+        const Ask q = ask_of(a, b);
+        if (b < b0) {
+            pages_before += q.pages;
+            rows_before += q.rows;
+        }
+        rows_all += q.rows;
+    }
+    pages_before = wave_sum64(pages_before);
+    rows_before = wave_sum64(rows_before);
+    rows_all = wave_sum64(rows_all);
+    if (lane == 0) {
+        s_sum[0][wave] = pages_before;
+        s_sum[1][wave] = rows_before;
+        s_sum[2][wave] = rows_all;
+    }
+    __syncthreads();
+    pages_before = rows_before = rows_all = 0;
+    for (int w = 0; w < kWaves; ++w) {
+        pages_before += s_sum[0][w];
+        rows_before += s_sum[1][w];
+        rows_all += s_sum[2][w];
+    }
+    // the workgroup's sequences in order, a wave each in turn; every wave follows the sums of all of them
+    for (int b = b0; b < b1; ++b) {
+        const Ask q = ask_of(a, b);
+        const int64_t first = pages_before, row = rows_before;
+        pages_before += q.pages;
+        rows_before += q.rows;
+        if ((b - b0) % kWaves != wave) continue;
+        const bool granted = q.fits && (q.pages == 0 || pages_before <= a.n_free);
+        int32_t* const tab = a.table + (size_t)b * a.max_pages;
+        auto given = [&](int j) { return a.free_pages ? a.free_pages[first + j] : (int32_t)(first + j); };      // the sequence's new page j
+        if (granted)
+            for (int j = lane; j < q.pages; j += 64) tab[q.held + j] = given(j);
+        if (lane == 0) {
+            if (a.pages) a.pages[b] = granted ? max(q.need, q.held) : q.held;
+            if (a.row_off) a.row_off[b] = (int32_t)min(row, (int64_t)INT32_MAX);
+        }
+        if (!a.slots) continue;
+        for (int i = lane; i < q.rows && row + i < a.slots_cap; i += 64) {
+            const int pos = q.len - q.rows + i, at = pos / TASC_PAGE_TOKENS;
+            int32_t slot = -1;
+            if (granted) slot = (at < q.held ? tab[at] : given(at - q.held)) * TASC_PAGE_TOKENS + pos % TASC_PAGE_TOKENS;
+            a.slots[row + i] = slot;
+        }
+    }
+    if (a.slots)
+        for (int64_t i = rows_all + (int64_t)blockIdx.x * kThreads + tid; i < a.slots_cap; i += (int64_t)gridDim.x * kThreads) a.slots[i] = -1;
+    if (blockIdx.x != gridDim.x - 1) return;
+    if (tid == 0 && a.row_off) a.row_off[a.batch] = (int32_t)min(rows_all, (int64_t)INT32_MAX);
+    if (!a.summary) return;
+    // pages given away: a sequence that gets pages gets all it asks for, and the sums only grow, so it is the largest sum that fits
+    __syncthreads();
+    if (wave != 0) return;
+    int64_t sum = 0, taken = 0;
+    int refused = 0;
+    for (int b = 0; b < a.batch; b += 64) {
+        Ask q{};
+        q.fits = true;
+        if (b + lane < a.batch) q = ask_of(a, b + lane);
+        int64_t end = q.pages;
+        for (int o = 1; o < 64; o <<= 1) {
+            const int64_t v = __shfl_up(end, o);
+            if (lane >= o) end += v;
+        }
+        end += sum;
+        sum = __shfl(end, 63);
+        if (!q.fits || (q.pages > 0 && end > a.n_free)) ++refused;
+        else if (q.pages > 0 && end > taken) taken = end;
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+        taken = max(taken, (int64_t)__shfl_xor(taken, o));
+        refused += __shfl_xor(refused, o);
+    }
+    if (lane == 0) {
+        a.summary[0] = (int32_t)min(rows_all, (int64_t)INT32_MAX);
+        a.summary[1] = (int32_t)taken;
+        a.summary[2] = refused;
+    }
+}
+
+}  // namespace
+
+extern "C" tasc_status tasc_page_tables(const int32_t* kv_len, const int32_t* new_rows, const int32_t* held, int32_t batch, const int32_t* free_pages, int32_t n_free,
+                                        int32_t* table, int32_t max_pages, int32_t* pages, int32_t* row_off, int32_t* slots, int32_t slots_cap, int32_t* summary,
+                                        void* stream) {
+    TASC_REQUIRE(kv_len && table, "page_tables: null argument");
+    TASC_REQUIRE(batch >= 1 && batch <= 1 << 20, "page_tables: batch %d outside [1, 2^20]", batch);
+    TASC_REQUIRE(max_pages >= 1 && max_pages < 1 << 27, "page_tables: max_pages %d outside [1, 2^27)", max_pages);
+    TASC_REQUIRE(n_free >= 0 && n_free < 1 << 27, "page_tables: n_free %d outside [0, 2^27)", n_free);
+    TASC_REQUIRE(slots_cap >= 0 && (slots || slots_cap == 0), "page_tables: %d slots", slots_cap);
+    TASC_REQUIRE(!pages || pages != held, "page_tables: pages and held are one array");
+    // runs of at least 8 sequences (a wave each), 256 workgroups at most: each reads all lengths
+    const int per_wg = std::max(8, (batch + 255) / 256);
+    const PageArgs a{kv_len, new_rows, held, free_pages, table, pages, row_off, slots, summary, batch, n_free, max_pages, slots_cap, per_wg};
+    k_page_tables<<<dim3((unsigned)((batch + per_wg - 1) / per_wg)), dim3(kThreads), 0, (hipStream_t)stream>>>(a);
+    TASC_LAUNCH_CHECK();
+    return TASC_OK;
+}

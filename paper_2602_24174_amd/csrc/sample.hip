@@ -1,0 +1,373 @@
+// Verification of drafted tokens against the target's probabilities, from given random numbers (paper, subsection "Speculative
+// Decoding").
+//
+// With w(v) = exp((logit(v) - max) / temperature) and Z = sum w, draft d of a row is accepted iff u q(d) Z < w(d); the first row whose draft is
+// not draws from max(0, w / Z - q) (q given) or from w without d (q a point mass), the row behind the last draft from w: the lowest v with
+// sum up to v > u' total.
+//
+// Two passes over a row at most: k_sample_parts reads every logit once and leaves, per segment of 4096 tokens, the maximum, its place and
+// sum w relative to it, without the row's draft (so that what remains after a rejection is a sum, not a difference); k_sample_pick, a workgroup
+// per sequence, joins the segments, decides, finds the segment that the draw falls into and reads that one again.  Given q,
+// k_sample_residual sums max(0, w / Z - q) over the segments of the rejected row in between.  Bound by the bytes of the logits.
+//
+// Exponentials and sums are fp64: the draw compares sums over the whole vocabulary with u' total, and with fp32's 2^-24 on each of 150,000
+// terms a token in a few thousand would come out as its neighbour.  An fp64 fma has the rate of an fp32 one here.
+#include "numeric.h"
+#include <algorithm>
+
+namespace {
+
+constexpr int kSeg = 4096, kPartThreads = 256, kPer = kSeg / kPartThreads, kPickThreads = 1024;
+
+struct __attribute__((aligned(16))) Part { double sum; float top; int32_t at; };   // sum: relative to top, without the row's draft
+
+struct SampleArgs {
+    const void* logits;
+    int64_t row_stride;
+    int32_t k, vocab, n_seg;
+    const int32_t* drafts;           // [B, k]
+    const float* probs;              // nullable [B, k, vocab]
+    const float* temperature;        // nullable [B]
+    const float* u;                  // [B, k + 1, 2]
+    Part* parts;                     // [B (k + 1), n_seg]
+    double* residual;                // [B, n_seg], given probs
+    int32_t *accept_len, *emitted;
+    float* logprob;
+};
+
+// exp(x) for x <= 0 (NaN stays one): x = n ln 2 + r, |r| <= ln 2 / 2, and the Taylor polynomial of degree 11, whose remainder is below
+// (ln 2 / 2)^12 / 12! = 6.3e-15
+__device__ __forceinline__ double exp_neg(double x) {
+    x = x < -1000.0 ? -1000.0 : x;                         // (an underflow either way; -infinity has no n)
+    const double n = rint(x * 1.4426950408889634074);
+    double r = __builtin_fma(n, -0x1.62e42fefa4000p-1, x);            // ln 2 in 40 bits, and the rest
+    r = __builtin_fma(n, 0x1.8432a1b0e2634p-43, r);
+    double p = 1.0 / 39916800.0;
+    p = __builtin_fma(p, r, 1.0 / 3628800.0);
+    p = __builtin_fma(p, r, 1.0 / 362880.0);
+    p = __builtin_fma(p, r, 1.0 / 40320.0);
+    p = __builtin_fma(p, r, 1.0 / 5040.0);
+    p = __builtin_fma(p, r, 1.0 / 720.0);
+    p = __builtin_fma(p, r, 1.0 / 120.0);
+    p = __builtin_fma(p, r, 1.0 / 24.0);
+    p = __builtin_fma(p, r, 1.0 / 6.0);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_fma(p, r, 1.0);
+    return ldexp(p, (int)n);
+}
+// 1 / temperature; 1 for a greedy sequence (its sums only tell whether the row holds a NaN), NaN for a temperature that is none
+__device__ __forceinline__ double inv_temperature(const SampleArgs& a, int b) {
+    const float t = a.temperature ? a.temperature[b] : 1.f;
+    return t > 0.f ? 1.0 / (double)t : t == 0.f ? 1.0 : __builtin_nan("");
+}
+__device__ __forceinline__ bool is_greedy(const SampleArgs& a, int b) { return a.temperature && a.temperature[b] == 0.f; }
+__device__ __forceinline__ int draft_of(const SampleArgs& a, int b, int i) {     // -1: the row scores none
+    const int d = i < a.k ? a.drafts[(int64_t)b * a.k + i] : -1;
+    return d >= 0 && d < a.vocab ? d : -1;
+}
+template <typename T>
+__device__ __forceinline__ const T* row_of(const SampleArgs& a, int b, int i) {
+    return (const T*)a.logits + ((int64_t)b * (a.k + 1) + i) * a.row_stride;
+}
+__device__ __forceinline__ double wave_sum64(double v) {
+    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
+    return v;
+}
+
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void k_sample_parts(SampleArgs a) {
+    __shared__ float s_top[4];
+    __shared__ int32_t s_at[4];
+    __shared__ double s_sum[4];
+    const int r = blockIdx.y, b = r / (a.k + 1), i = r % (a.k + 1), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int v0 = blockIdx.x * kSeg;
+    const T* row = row_of<T>(a, b, i);
+    const double inv = inv_temperature(a, b);
+    const int d = draft_of(a, b, i);
+    float x[kPer];
+    float top = -__builtin_inff();
+    int at = 0x7FFFFFFF;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int v = v0 + e * kPartThreads + tid;
+        x[e] = v < a.vocab ? to_f(row[v]) : -__builtin_inff();
+        if (x[e] > top) { top = x[e]; at = v; }
+    }
+    for (int o = 32; o > 0; o >>= 1) {
+        const float t = __shfl_xor(top, o);
+        const int32_t w = __shfl_xor(at, o);
+        if (t > top || (t == top && w < at)) { top = t; at = w; }
+    }
+    if (lane == 0) { s_top[wave] = top; s_at[wave] = at; }
+    __syncthreads();
+    for (int w = 0; w < 4; ++w)
+        if (s_top[w] > top || (s_top[w] == top && s_at[w] < at)) { top = s_top[w]; at = s_at[w]; }
+    // (nothing above -infinity in the segment: weights relative to 0 are zeros, and a NaN among them shows)
+    const double base = top == -__builtin_inff() ? 0.0 : (double)top;
+    double sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int v = v0 + e * kPartThreads + tid;
+        const double w = exp_neg(((double)x[e] - base) * inv);
+        sum += v == d ? (w != w ? w : 0.0) : w;
+    }
+    sum = wave_sum64(sum);
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    if (tid == 0) a.parts[(int64_t)r * a.n_seg + blockIdx.x] = Part{(s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]), top, at};
+}
+
+// What a row comes to: Z = others + w(draft), log Z, and the decision on its draft
+struct Row { double top, others, z, logz; float draft_logp; int32_t best, draft; bool ok, accept; };
+
+template <typename T>
+__device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int lane) {
+    Row o;
+    const Part* p = a.parts + ((int64_t)b * (a.k + 1) + i) * a.n_seg;
+    float top = -__builtin_inff();
+    int32_t best = 0x7FFFFFFF;
+    for (int s = lane; s < a.n_seg; s += 64) {
+        const Part q = p[s];
+        if (q.top > top || (q.top == top && q.at < best)) { top = q.top; best = q.at; }
+    }
+    for (int f = 32; f > 0; f >>= 1) {
+        const float t = __shfl_xor(top, f);
+        const int32_t w = __shfl_xor(best, f);
+        if (t > top || (t == top && w < best)) { top = t; best = w; }
+    }
+    const double inv = inv_temperature(a, b);
+    double sum = 0.0;
+    for (int s = lane; s < a.n_seg; s += 64) {
+        const Part q = p[s];
+        sum += q.top == -__builtin_inff() ? q.sum : q.sum * exp_neg(((double)q.top - (double)top) * inv);
+    }
+    o.top = top;
+    o.best = best;
+    o.others = wave_sum64(sum);
+    o.draft = draft_of(a, b, i);
+    const double x = o.draft >= 0 ? ((double)to_f(row_of<T>(a, b, i)[o.draft]) - o.top) * inv : 0.0;
+    const double w = o.draft >= 0 ? exp_neg(x) : 0.0;
+    o.z = o.others + w;
+    o.ok = o.z > 0.0 && o.z < __builtin_inf();
+    o.logz = log(o.z);
+    o.draft_logp = (float)(x - o.logz);
+    const double q = o.draft >= 0 && a.probs ? (double)a.probs[((int64_t)b * a.k + i) * a.vocab + o.draft] : 1.0;
+    o.accept = o.ok && o.draft >= 0 && (double)a.u[((int64_t)b * (a.k + 1) + i) * 2] * q * o.z < w;
+    if (is_greedy(a, b)) {
+        o.accept = o.ok && o.draft == o.best && (double)a.u[((int64_t)b * (a.k + 1) + i) * 2] * q < 1.0;
+        o.draft_logp = 0.f;
+        o.logz = 0.0;
+    }
+    return o;
+}
+
+// sum max(0, p - q) over a segment of the row that rejected its draft (others write nothing that is read)
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void k_sample_residual(SampleArgs a) {
+    __shared__ Row s_row[TASC_MAX_K + 1];
+    __shared__ double s_sum[4];
+    const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (is_greedy(a, b)) return;
+    for (int i = wave; i <= a.k; i += 4) {
+        const Row o = join_row<T>(a, b, i, lane);
+        if (lane == 0) s_row[i] = o;
+    }
+    __syncthreads();
+    int m = 0;
+    while (m <= a.k && s_row[m].accept) ++m;
+    if (m >= a.k || s_row[m].draft < 0 || !s_row[m].ok) return;
+    const Row o = s_row[m];
+    const T* row = row_of<T>(a, b, m);
+    const float* q = a.probs + ((int64_t)b * a.k + m) * a.vocab;
+    const double inv = inv_temperature(a, b), inv_z = 1.0 / o.z;
+    double sum = 0.0;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int v = blockIdx.x * kSeg + e * kPartThreads + tid;
+        if (v < a.vocab) sum += fmax(exp_neg(((double)to_f(row[v]) - o.top) * inv) * inv_z - (double)q[v], 0.0);
+    }
+    sum = wave_sum64(sum);
+    if (lane == 0) s_sum[wave] = sum;
+    __syncthreads();
+    if (tid == 0) a.residual[(int64_t)b * a.n_seg + blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+}
+
+template <typename T>
+__global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
+    __shared__ Row s_row[TASC_MAX_K + 1];
+    __shared__ double s_wave[16];
+    __shared__ double s_before, s_target;
+    __shared__ int32_t s_seg, s_first[16], s_last[16];
+    __shared__ double s_x;
+    const int b = blockIdx.x, nq = a.k + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    if (wave < nq) {
+        const Row o = join_row<T>(a, b, wave, lane);
+        if (lane == 0) s_row[wave] = o;
+    }
+    __syncthreads();
+    int m = 0;
+    while (m < a.k && s_row[m].accept) ++m;
+    const Row o = s_row[m];
+    const bool greedy = is_greedy(a, b);
+    int32_t token = -1;
+    float logp = __builtin_nanf("");
+    if (!o.ok) {
+    } else if (greedy) {
+        token = o.best;
+        logp = 0.f;
+    } else {
+        const double inv = inv_temperature(a, b), u = (double)a.u[((int64_t)b * nq + m) * 2 + 1];
+        const Part* p = a.parts + ((int64_t)b * nq + m) * a.n_seg;
+        const double* res = a.residual + (int64_t)b * a.n_seg;
+        // which weights: 0 w, 1 w without the draft, 2 max(0, p - q); what a rejection leaves may round to nothing: then w
+        if (wave == 0) {
+            int kind = o.draft < 0 ? 0 : a.probs ? 2 : 1;
+            auto seg_sum = [&](int s) {
+                if (s >= a.n_seg) return 0.0;
+                if (kind == 2) return res[s];
+                const Part q = p[s];
+                double v = q.top == -__builtin_inff() ? 0.0 : q.sum * exp_neg(((double)q.top - o.top) * inv);
+                if (kind == 0 && o.draft >= 0 && o.draft / kSeg == s) v += o.z - o.others;
+                return v;
+            };
+            double total = 0.0;
+            for (int pass = 0; pass < 2; ++pass) {
+                total = 0.0;
+                for (int s = lane; s < a.n_seg; s += 64) total += seg_sum(s);
+                total = wave_sum64(total);
+                if (total > 0.0) break;
+                kind = 0;
+            }
+            const double target = u * total;
+            double before = 0.0, at_before = 0.0;
+            int seg = -1, last = 0;
+            double last_before = 0.0;
+            for (int s0 = 0; s0 < a.n_seg && seg < 0; s0 += 64) {
+                const double own = seg_sum(s0 + lane);
+                double up = own;
+                for (int f = 1; f < 64; f <<= 1) {
+                    const double t = __shfl_up(up, f);
+                    if (lane >= f) up += t;
+                }
+                const u64 past = __ballot(before + up > target), some = __ballot(own > 0.0);
+                if (some) {
+                    const int l = 63 - __clzll(some);
+                    last = s0 + l;
+                    last_before = before + __shfl(up - own, l);
+                }
+                if (past) {
+                    const int l = __ffsll(past) - 1;
+                    seg = s0 + l;
+                    at_before = before + __shfl(up - own, l);
+                }
+                before += __shfl(up, 63);
+            }
+            if (lane == 0) {
+                s_seg = (seg >= 0 ? seg : last) | kind << 28;
+                s_before = seg >= 0 ? at_before : last_before;
+                s_target = target;
+            }
+        }
+        __syncthreads();
+        const int seg = s_seg & 0xFFFFFFF, kind = s_seg >> 28;
+        const T* row = row_of<T>(a, b, m);
+        const double inv_z = 1.0 / o.z;
+        const float* q = kind == 2 ? a.probs + ((int64_t)b * a.k + m) * a.vocab : nullptr;
+        double w[4], x[4], mine = 0.0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            const int v = seg * kSeg + 4 * tid + e;
+            x[e] = v < a.vocab ? ((double)to_f(row[v]) - o.top) * inv : -1000.0;
+            w[e] = v < a.vocab ? exp_neg(x[e]) : 0.0;
+            if (kind == 1 && v == o.draft) w[e] = 0.0;
+            if (kind == 2 && v < a.vocab) w[e] = fmax(w[e] * inv_z - (double)q[v], 0.0);
+            mine += w[e];
+        }
+        double up = mine;
+        for (int f = 1; f < 64; f <<= 1) {
+            const double t = __shfl_up(up, f);
+            if (lane >= f) up += t;
+        }
+        if (lane == 63) s_wave[wave] = up;
+        __syncthreads();
+        double sum = s_before + (up - mine);
+        for (int i = 0; i < wave; ++i) sum += s_wave[i];
+        int first = 0x7FFFFFFF, last = -1;                  // the first token past the target, the last with any weight
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            sum += w[e];
+            const int v = seg * kSeg + 4 * tid + e;
+            if (w[e] > 0.0) {
+                last = v;
+                if (sum > s_target && first == 0x7FFFFFFF) first = v;
+            }
+        }
+        for (int f = 32; f > 0; f >>= 1) {
+            first = min(first, __shfl_xor(first, f));
+            last = max(last, __shfl_xor(last, f));
+        }
+        if (lane == 0) { s_first[wave] = first; s_last[wave] = last; }
+        __syncthreads();
+        for (int i = 0; i < 16; ++i) {
+            first = min(first, s_first[i]);
+            last = max(last, s_last[i]);
+        }
+        token = first != 0x7FFFFFFF ? first : last;
+        if (token >= 0 && (token - seg * kSeg) / 4 == tid) {
+#pragma unroll
+            for (int e = 0; e < 4; ++e)
+                if (token == seg * kSeg + 4 * tid + e) s_x = x[e];
+        }
+        __syncthreads();
+        if (token >= 0) logp = (float)(s_x - o.logz);
+    }
+    if (tid < nq) {
+        const int64_t at = (int64_t)b * nq + tid;
+        a.emitted[at] = tid < m ? s_row[tid].draft : tid == m ? token : -1;
+        if (a.logprob) a.logprob[at] = tid < m ? s_row[tid].draft_logp : tid == m ? logp : 0.f;
+    }
+    if (tid == 0) a.accept_len[b] = m;
+}
+
+size_t parts_bytes(int batch, int k, int n_seg) { return (size_t)batch * (k + 1) * n_seg * sizeof(Part); }
+int segments(int vocab) { return (vocab + kSeg - 1) / kSeg; }
+
+template <typename T>
+tasc_status enqueue(const SampleArgs& a, int batch, hipStream_t st) {
+    k_sample_parts<T><<<dim3((unsigned)a.n_seg, (unsigned)(batch * (a.k + 1))), dim3(kPartThreads), 0, st>>>(a);
+    if (a.probs && a.k > 0) k_sample_residual<T><<<dim3((unsigned)a.n_seg, (unsigned)batch), dim3(kPartThreads), 0, st>>>(a);
+    k_sample_pick<T><<<dim3((unsigned)batch), dim3(kPickThreads), 0, st>>>(a);
+    TASC_LAUNCH_CHECK();
+    return TASC_OK;
+}
+
+}  // namespace
+
+extern "C" size_t tasc_accept_sampled_workspace_bytes(int32_t batch, int32_t k, int32_t vocab) {
+    if (batch < 1 || k < 0 || k > TASC_MAX_K || vocab < 2 || vocab > 1 << 24) return 0;
+    return parts_bytes(batch, k, segments(vocab)) + (size_t)batch * segments(vocab) * sizeof(double);
+}
+
+extern "C" tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab, const int32_t* drafts,
+                                           const float* draft_probs, const float* temperature, const float* u, int32_t* accept_len, int32_t* emitted, float* logprob,
+                                           void* workspace, size_t ws_bytes, void* stream) {
+    TASC_REQUIRE(k >= 0 && k <= TASC_MAX_K, "accept_sampled: k %d outside [0, %d]", k, TASC_MAX_K);
+    TASC_REQUIRE(vocab >= 2 && vocab <= 1 << 24, "accept_sampled: vocab %d outside [2, 2^24]", vocab);
+    TASC_REQUIRE(batch >= 0 && (int64_t)batch * (k + 1) <= 65535, "accept_sampled: %d sequences of %d rows are not 0 .. 65535 rows", batch, k + 1);
+    if (batch == 0) return TASC_OK;
+    TASC_REQUIRE(logits && u && accept_len && emitted && (drafts || k == 0), "accept_sampled: null argument");
+    TASC_REQUIRE(dtype == TASC_F32 || dtype == TASC_BF16, "accept_sampled: dtype %d", (int)dtype);
+    TASC_REQUIRE(row_stride >= vocab, "accept_sampled: rows of %d logits lie %lld apart", vocab, (long long)row_stride);
+    TASC_REQUIRE((uintptr_t)logits % (dtype == TASC_F32 ? 4 : 2) == 0, "accept_sampled: logits must be aligned to their type");
+    const size_t need = tasc_accept_sampled_workspace_bytes(batch, k, vocab);
+    if (!workspace || ws_bytes < need) {
+        tasc_set_error("accept_sampled: workspace of %zu of %zu bytes", workspace ? ws_bytes : 0, need);
+        return TASC_ENOMEM;
+    }
+    TASC_REQUIRE(((uintptr_t)workspace & 15) == 0, "accept_sampled: the workspace must be 16-byte aligned");
+    const int n_seg = segments(vocab);
+    const SampleArgs a{logits, row_stride, k, vocab, n_seg, drafts, draft_probs, temperature, u, (Part*)workspace,
+                       (double*)((char*)workspace + parts_bytes(batch, k, n_seg)), accept_len, emitted, logprob};
+    return dtype == TASC_F32 ? enqueue<float>(a, batch, (hipStream_t)stream) : enqueue<BF16>(a, batch, (hipStream_t)stream);
+}

@@ -1,0 +1,186 @@
+"""tasc_accept_sampled against its oracle in float64: accepted lengths and tokens equal; ln p is a float64 value rounded to fp32 once
+(2^-24 relative, and 1e-12 for what 64 bits leave of a sum over the vocabulary)."""
+import numpy as np
+import pytest
+
+from oracle import sampled_acceptance as OA
+
+pytestmark = pytest.mark.gpu
+
+
+def inputs(rng, B, k, V, dtype, probs, spread=2.0):
+    import torch
+    logits = rng.normal(size=(B, k + 1, V)).astype(np.float32) * spread
+    for b in range(B):
+        for i in range(k + 1):
+            logits[b, i, rng.integers(0, V, 3)] += 9
+    logits = torch.tensor(logits).to(getattr(torch, dtype))
+    x = logits.float().numpy()
+    drafts = x[:, :k].argmax(-1).astype(np.int32)
+    q = None
+    if probs:
+        noisy = x[:, :k].astype(np.float64) + rng.normal(size=(B, k, V))
+        q = np.exp(noisy - noisy.max(-1, keepdims=True))
+        q = (q / q.sum(-1, keepdims=True)).astype(np.float32)
+        for b in range(B):
+            for i in range(k):
+                drafts[b, i] = rng.choice(V, p=q[b, i] / q[b, i].astype(np.float64).sum())
+    wrong = rng.random((B, k)) < 0.2
+    drafts[wrong] = rng.integers(0, V, int(wrong.sum()))
+    return logits, drafts, q, rng.random((B, k + 1, 2)).astype(np.float32)
+
+
+def run(logits, drafts, q, temperature, u, workspace=None):
+    import torch
+    import paper_2602_24174_amd as T
+    B, nq = logits.shape[:2]
+    dev = lambda x: None if x is None else torch.tensor(np.asarray(x), device="cuda")
+    acc, emitted = torch.full((B,), -9, dtype=torch.int32, device="cuda"), torch.full((B, nq), -9, dtype=torch.int32, device="cuda")
+    logp = torch.full((B, nq), -9, dtype=torch.float32, device="cuda")
+    T.tasc_accept_sampled(logits if logits.is_cuda else logits.cuda(), dev(drafts), dev(q), dev(temperature), dev(u), acc, emitted, logp, workspace)
+    return acc.cpu().numpy(), emitted.cpu().numpy(), logp.cpu().numpy()
+
+
+def check(logits, drafts, q, temperature, u):
+    got = run(logits, drafts, q, temperature, u)
+    x = logits.float().cpu().numpy()
+    seen = set()
+    for b in range(len(x)):
+        m, tokens, logp = OA.accept(x[b], drafts[b], None if q is None else q[b], 1.0 if temperature is None else temperature[b], u[b])
+        nq = x.shape[1]
+        assert got[0][b] == m and got[1][b].tolist() == tokens + [-1] * (nq - len(tokens)), b
+        want = np.array(logp + [0.0] * (nq - len(logp)))
+        assert (np.isnan(want) == np.isnan(got[2][b])).all()
+        assert (np.nan_to_num(np.abs(got[2][b] - want)) <= 2.0 ** -24 * np.abs(np.nan_to_num(want)) + 1e-12).all(), b
+        seen.add(m)
+    return seen
+
+
+@pytest.mark.parametrize("dtype", ["float32", "bfloat16"])
+@pytest.mark.parametrize("probs", [False, True])
+@pytest.mark.parametrize("B, k, V", [(1, 4, 512), (5, 3, 2), (3, 0, 777), (40, 4, 4096), (17, 8, 4097), (9, 15, 12288), (4, 6, 151936)])
+def test_against_the_oracle(B, k, V, probs, dtype):
+    rng = np.random.default_rng(B * 100 + k)
+    logits, drafts, q, u = inputs(rng, B, k, V, dtype, probs and k > 0)
+    temperature = rng.choice([0.0, 0.3, 1.0, 1.7], B).astype(np.float32)
+    print(f"{B} x {k + 1} x {V} {dtype} probs {probs}", flush=True)
+    seen = check(logits, drafts, q, temperature, u)
+    check(logits, drafts, q, None, u)
+    assert B < 40 or len(seen) > 2
+
+
+def test_flat_and_peaked_rows():
+    """All tokens alike (borders 1 / vocab apart), one token with all of the mass, and random numbers at the ends of their range."""
+    import torch
+    V, k = 50000, 2
+    logits = torch.zeros((6, k + 1, V))
+    logits[3:, :, 17] = 200.0
+    drafts = np.array([[5, 6], [49999, 0], [17, 17], [17, 17], [17, 4], [4, 17]], dtype=np.int32)
+    for value in (0.0, 2.0 ** -24, 0.5, 1 - 2.0 ** -24):
+        u = np.full((6, k + 1, 2), value, dtype=np.float32)
+        print(f"u {value}", flush=True)
+        check(logits, drafts, None, None, u)
+        q = np.full((6, k, V), 1.0 / V, dtype=np.float32)
+        check(logits, drafts, q, np.array([1, 0.5, 0, 1, 0.5, 0], dtype=np.float32), u)
+
+
+def test_masks_and_rows_without_a_distribution():
+    import torch
+    rng = np.random.default_rng(11)
+    V, k = 9000, 3
+    logits, drafts, _, u = inputs(rng, 12, k, V, "float32", False)
+    u[..., 0] = 0.0                                          # accept whatever has a weight
+    inf = float("inf")
+    logits[0, 1] = -inf                                      # nothing left
+    logits[1, 2, 100] = float("nan")
+    logits[2, 0, 8999] = inf
+    logits[3, 0, drafts[3, 0]] = float("nan")                # the draft itself
+    logits[4, 1, :8192] = -inf                               # whole segments masked
+    logits[5, 1, 1:] = -inf                                  # one token left, the draft is not it
+    drafts[5, 1] = 7
+    logits[6, 0, drafts[6, 0]] = -inf                        # a masked draft
+    logits[7] = -3.0e38                                      # the type's lowest value everywhere, but for one token
+    logits[7, :, 4500] = 0.0
+    logits[8, 3] = -inf                                      # behind the last draft
+    logits[9, 2, 100] = float("nan")                         # a row that is not reached
+    drafts[9, 0], logits[9, 0, 3] = 3, -inf
+    temperature = np.ones(12, dtype=np.float32)
+    temperature[10], temperature[11] = -1.0, float("nan")
+    check(logits, drafts, None, temperature, u)
+    check(logits, drafts, None, np.where(np.arange(12) < 10, 0, temperature).astype(np.float32), u)
+
+
+def test_fewer_drafts_and_tokens_outside_the_vocabulary():
+    rng = np.random.default_rng(12)
+    logits, drafts, q, u = inputs(rng, 6, 4, 300, "float32", True)
+    drafts[0, 0], drafts[1, 1], drafts[2, 3], drafts[3, 2], drafts[4, 0] = -1, -1, -1, 300, 2147483647
+    u[..., 0] = 0.0
+    check(logits, drafts, None, None, u)
+    check(logits, drafts, q, None, u)
+
+
+def test_probabilities_that_leave_nothing():
+    """q equal to p where the draft is refused all the same (u q rounds past p), q of zeros, q beyond 1, q with NaN."""
+    import torch
+    rng = np.random.default_rng(13)
+    V = 6000
+    logits = torch.tensor(rng.normal(size=(4, 2, V)).astype(np.float32))
+    drafts = np.array([[9], [9], [9], [9]], dtype=np.int32)
+    q = np.zeros((4, 1, V), dtype=np.float32)
+    q[0] = 2.0                                               # max(0, p - q) is zero everywhere: drawn from p
+    q[2, 0, 9] = 1.0
+    q[3, 0, 9], q[3, 0, 100:200] = 1.0, 1.0
+    u = rng.random((4, 2, 2)).astype(np.float32)
+    u[:, :, 0] = 0.9
+    check(logits, drafts, q, None, u)
+
+
+def test_strided_rows_streams_and_graphs():
+    """Logits inside wider rows; a call on another stream; a captured call replayed with new contents, eager calls in between."""
+    import torch
+    import paper_2602_24174_amd as T
+    rng = np.random.default_rng(14)
+    B, k, V = 5, 3, 5000
+    logits, drafts, q, u = inputs(rng, B, k, V, "float32", True)
+    want = run(logits, drafts, q, None, u)
+    wide = torch.full((B, k + 1, V + 77), float("nan"), device="cuda")
+    wide[..., 5:V + 5] = logits.cuda()
+    for g, w in zip(run(wide[..., 5:V + 5], drafts, q, None, u), want):
+        assert np.array_equal(g, w)
+    dev = [torch.tensor(x, device="cuda") for x in (drafts, q, u)]
+    x = logits.cuda()
+    out = [torch.zeros((B,), dtype=torch.int32, device="cuda"), torch.zeros((B, k + 1), dtype=torch.int32, device="cuda"), torch.zeros((B, k + 1), device="cuda")]
+    ws = torch.empty(T.tasc_accept_sampled_workspace_bytes(B, k, V), dtype=torch.uint8, device="cuda")
+    side = torch.cuda.Stream()
+    torch.cuda.synchronize()
+    T.tasc_accept_sampled(x, dev[0], dev[1], None, dev[2], *out, ws, stream=side.cuda_stream)
+    with pytest.raises(T.TascError):
+        T.tasc_accept_sampled(x, dev[0], dev[1], None, dev[2], *out, stream=side.cuda_stream)      # whose would the workspace be
+    torch.cuda.synchronize()
+    for g, w in zip(out, want):
+        assert np.array_equal(g.cpu().numpy(), w)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        T.tasc_accept_sampled(x, dev[0], dev[1], None, dev[2], *out, ws)
+    for seed in range(3):
+        logits2, drafts2, q2, u2 = inputs(np.random.default_rng(seed), B, k, V, "float32", True)
+        for t, n in zip((x, *dev), (logits2, drafts2, q2, u2)):
+            t.copy_(torch.as_tensor(n))
+        graph.replay()
+        eager = run(logits2, drafts2, q2, None, u2)
+        torch.cuda.synchronize()
+        for g, w in zip(out, eager):
+            assert np.array_equal(g.cpu().numpy(), w)
+
+
+def test_refusals_by_the_binding():
+    import torch
+    import paper_2602_24174_amd as T
+    f, i = lambda *n: torch.zeros(n, device="cuda"), lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")
+    good = dict(logits=f(2, 3, 10), drafts=i(2, 2), draft_probs=f(2, 2, 10), temperature=f(2), u=f(2, 3, 2), accept_len=i(2), emitted=i(2, 3), logprob=f(2, 3))
+    T.tasc_accept_sampled(**good)
+    for bad in (dict(logits=f(2, 3, 10).half()), dict(logits=f(2, 30)), dict(logits=f(2, 3, 20)[..., ::2]), dict(logits=f(4, 3, 10)[::2]), dict(drafts=i(2, 3)), dict(drafts=None),
+                dict(draft_probs=f(2, 3, 10)), dict(temperature=f(3)), dict(u=f(2, 3)), dict(accept_len=i(3)), dict(emitted=i(2, 2)), dict(logprob=f(2, 2)),
+                dict(workspace=torch.zeros(8, dtype=torch.uint8, device="cuda"))):
+        with pytest.raises(T.TascError):
+            T.tasc_accept_sampled(**dict(good, **bad))

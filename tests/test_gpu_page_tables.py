@@ -1,0 +1,84 @@
+"""tasc_page_tables against its oracle: every output equal, and what must stay as it was untouched."""
+import numpy as np
+import pytest
+
+from oracle import page_tables as OP
+
+pytestmark = pytest.mark.gpu
+
+
+def run(kv_len, new_rows, held, free, table, cap, n_free=None, guard=7):
+    import torch
+    import paper_2602_24174_amd as T
+    dev = lambda x: torch.tensor(np.asarray(x, dtype=np.int32), device="cuda")
+    B = len(kv_len)
+    tab = dev(table)
+    pages, row_off = torch.full((B + guard,), -9, dtype=torch.int32, device="cuda"), torch.full((B + 1 + guard,), -9, dtype=torch.int32, device="cuda")
+    slots, summary = torch.full((cap + guard,), -9, dtype=torch.int32, device="cuda"), torch.full((3,), -9, dtype=torch.int32, device="cuda")
+    args = dev(kv_len), None if new_rows is None else dev(new_rows), None if held is None else dev(held), None if free is None else dev(free)
+    T.tasc_page_tables(*args, tab, pages[:B], row_off[:B + 1], slots[:cap], summary, n_free=n_free)
+    assert (pages[B:] == -9).all() and (row_off[B + 1:] == -9).all() and (slots[cap:] == -9).all()
+    return tab.cpu().tolist(), pages[:B].tolist(), row_off[:B + 1].tolist(), slots[:cap].tolist(), summary.tolist()
+
+
+def check(kv_len, new_rows, held, free, table, cap):
+    print(f"batch {len(kv_len)}, {len(free)} free pages, {cap} slots", flush=True)
+    want_table = [list(r) for r in table]
+    want = OP.page_tables(kv_len, new_rows, held, free, want_table, cap)
+    got = run(kv_len, new_rows, held, free, table, cap)
+    assert got[0] == want_table
+    for g, w in zip(got[1:], want):
+        assert g == w
+
+
+@pytest.mark.parametrize("batch, most, rows, short", [(1, 1, 1, False), (1, 100, 1, False), (7, 33, 9, False), (8, 16, 16, True), (9, 17, 3, False), (64, 2300, 9, False),
+                                                      (65, 300, 200, True), (513, 70, 40, True), (2100, 50, 3, False)])
+def test_random_lengths(batch, most, rows, short):
+    rng = np.random.default_rng(batch)
+    had = rng.integers(0, most + 1, batch) * (rng.random(batch) < 0.7)
+    new = rng.integers(0, rows + 1, batch)
+    lens, held = had + new, -(-had // 16)
+    held = held + rng.integers(0, 2, batch) * (rng.random(batch) < 0.3)         # some hold a page more than they need
+    cols = int(max(-(-lens.max() // 16), held.max(), 1)) + 1
+    ask = int(np.maximum(-(-lens // 16) - held, 0).sum())
+    order = rng.permutation(int(held.sum()) + ask + 5).tolist()
+    table = np.full((batch, cols), -1)
+    at = 0
+    for b in range(batch):
+        table[b, :held[b]] = order[at:at + held[b]]
+        at += held[b]
+    free = order[at:][:max(0, ask * 2 // 3) if short else None]
+    for cap in (int(new.sum()) + 3, max(0, int(new.sum()) - 2)):
+        check(lens.tolist(), new.tolist(), held.tolist(), free, table.tolist(), cap)
+
+
+def test_lengths_that_make_no_sense():
+    """Negative numbers, more rows than tokens, tables too short, more pages held than a table lists: refused, the others served."""
+    kv_len = [5, -1, 40, 10, 65, 64, 2147483647, 3, 16]
+    new = [5, 0, 3, 11, 1, 4, 2, -2, 16]
+    held = [0, 0, -1, 0, 4, 5, 0, 1, 0]
+    check(kv_len, new, held, list(range(100, 120)), [[b] * 4 for b in range(9)], 48)
+
+
+def test_defaults():
+    """No rows, nothing held, the identity as list of free pages."""
+    got = run([33, 0, 16], None, None, None, [[-1] * 4] * 3, 2, n_free=10)
+    assert got[0] == [[0, 1, 2, -1], [-1] * 4, [3, -1, -1, -1]]
+    assert got[1:] == ([3, 0, 1], [0, 0, 0, 0], [-1, -1], [0, 4, 0])
+    import torch
+    import paper_2602_24174_amd as T
+    table = torch.full((1, 4), -1, dtype=torch.int32, device="cuda")
+    T.tasc_page_tables(torch.tensor([20], dtype=torch.int32, device="cuda"), None, None, torch.tensor([5, 6], dtype=torch.int32, device="cuda"), table)
+    assert table.tolist() == [[5, 6, -1, -1]]
+
+
+def test_refusals_by_the_binding():
+    import torch
+    import paper_2602_24174_amd as T
+    i = lambda *n: torch.zeros(n, dtype=torch.int32, device="cuda")
+    for bad in (dict(pages=i(3)), dict(row_off=i(4)), dict(summary=i(2)), dict(slots=i(8)[::2]), dict(pages=i(4).long()), dict(n_free=9)):
+        with pytest.raises(T.TascError):
+            T.tasc_page_tables(i(4), i(4), i(4), i(8), i(4, 4), **bad)
+    held = i(4)
+    with pytest.raises(T.TascError):
+        T.tasc_page_tables(i(4), i(4), held, i(8), i(4, 4), pages=held)
