@@ -313,6 +313,43 @@ tasc_status tasc_session_get_tokens(const tasc_session* s, int32_t b, int32_t* t
                                     int32_t* n, void* stream);
 
 /* ------------------------------------------------------------------------------------------
+ * Sampled decoding: the same step and loop with the drafts verified against the target's probabilities (tasc_accept_sampled, whose
+ * definitions hold: drafts count as chosen without chance) in place of the greedy acceptance.
+ * ---------------------------------------------------------------------------------------- */
+typedef struct {
+    const float* temperature; /* DEVICE fp32[batch], nullable (1); 0: greedy                                              */
+    const float* u;           /* DEVICE fp32[batch, n_u, 2] in [0, 1): pair e decides on and draws a sequence's generated  */
+    int64_t n_u;              /* token number e (from 0); tokens behind the last pair reuse it                             */
+    void* scratch;            /* DEVICE, 256-byte aligned, tasc_sampled_scratch_bytes: its first batch * (k + 1) * vocab   */
+    size_t scratch_bytes;     /* floats are the step's logits                                                              */
+} tasc_sampling;
+/* 0 for what tasc_accept_sampled does not serve. */
+size_t tasc_sampled_scratch_bytes(const tasc_model* m, int32_t batch, int32_t k);
+/* tasc_verify_step with that acceptance; logprob DEVICE fp32[batch, k + 1], nullable, as in tasc_accept_sampled.  A row without a distribution
+ * commits token 0 (and reports -1).  Which tokens come out depends on the target, the drafts and the random numbers. */
+tasc_status tasc_verify_step_sampled(const tasc_model* m, tasc_session* s, const int32_t* drafts, int32_t k, const tasc_sampling* p,
+                                     int32_t* accept_len, int32_t* emitted, float* logprob, void* stream);
+/* Takes back what the sequences have generated, the token that the prefill committed among it: the prompts stay cached and the next step's
+ * first row is each prompt's last token.  With it the first token is drawn like the others, and one prompt serves several runs. */
+tasc_status tasc_session_rewind(tasc_session* s, void* stream);
+/* tasc_generate with that acceptance, all max_new tokens drawn (prefill, rewind, then draft + verify). */
+tasc_status tasc_generate_sampled(const tasc_model* m, const tasc_ngram* ng, tasc_session* s, const int32_t* prompts,
+                                  const int64_t* prompt_offsets, tasc_mem where, int32_t max_new, const tasc_spec_params* p,
+                                  const tasc_sampling* sampling, int32_t* out_tokens, tasc_gen_stats* stats, void* stream);
+
+/*
+ * A session whose keys and values are held in 4 bits (tasc_kv4_cache below is a layer of it, n_pages pages each, one layer behind the
+ * other): 3.6 times as many tokens per byte, and pages by the requests' lengths: a prefill gives every sequence those of its
+ * prompt + max_new + 2 * max_rows tokens (tasc_page_tables) and fails with TASC_ENOMEM if the pool has fewer.  For bf16 models with d_model,
+ * n_heads * head_dim and d_ffn multiples of 64 and heads of 32, 64 or 128 channels; every forward takes the tiled kernels, whatever
+ * TASC_CFG_SMALL_PATH and TASC_CFG_TILED_PATH say.  Greedy and speculative decoding of such a session agree bit for bit.
+ * kv_pool need not be cleared.  Otherwise as tasc_session_create.
+ */
+size_t tasc_session_kv4_bytes(const tasc_model* m, int32_t n_pages);
+tasc_status tasc_session_create_kv4(const tasc_model* m, int32_t batch, int32_t max_len, int32_t max_rows, int32_t n_pages,
+                                    void* kv_pool, size_t kv_bytes, void* workspace, size_t ws_bytes, tasc_session** out);
+
+/* ------------------------------------------------------------------------------------------
  * Library-wide options (for tests and tuning; the defaults are what the benchmarks run).
  *   TASC_CFG_SMALL_PATH  how a bf16 forward of at most 16 rows runs: 2 (default) = one persistent
  *                        kernel for the whole step, 1 = the same kernel launched once per phase,
@@ -463,7 +500,7 @@ tasc_status tasc_page_tables(const int32_t* kv_len, const int32_t* new_rows, con
  * scale = bf16((hi - lo) * (1 / 15)) and low = bf16(lo) of its least and largest value (the steps in fp32); a value is held as the whole number in [0, 15]
  * nearest to (value - low) / scale (the even one of two; 0 where scale is 0) and stands for low + scale * number, computed in
  * fp32.  A group that holds an infinity or a NaN, or whose range is beyond fp32, reads as NaN.
- *   pool  DEVICE, 256-byte aligned, n_pages * tasc_kv4_page_bytes; what has not been written may hold anything
+ *   pool  DEVICE, 128-byte aligned, n_pages * tasc_kv4_page_bytes; what has not been written may hold anything
  */
 typedef struct {
     void* pool;

@@ -9,5 +9,6 @@ from .binding import (  # noqa: F401
     tasc_ngram_get_stats, tasc_model_bigram, tasc_ngram_from_bigram, tasc_tok_enrich, tasc_ngram_entropy, tasc_ngram_entropy_noalloc, TableEntropy, tasc_ngram_unigram, tasc_session_create, tasc_session_get_tokens, tasc_session_kv_bytes,
     tasc_session_prefill, tasc_session_workspace_bytes, tasc_verify_step,
     Kv4Cache, tasc_page_tables, tasc_kv4_page_bytes, tasc_kv4_append, tasc_kv4_read, tasc_kv4_attention, tasc_kv4_attention_workspace_bytes,
-    tasc_accept_sampled, tasc_accept_sampled_workspace_bytes,
+    tasc_accept_sampled, tasc_accept_sampled_workspace_bytes, Sampling, tasc_sampled_scratch_bytes, tasc_verify_step_sampled, tasc_session_rewind,
+    tasc_generate_sampled, tasc_session_kv4_bytes, tasc_session_create_kv4,
 )

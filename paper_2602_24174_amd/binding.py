@@ -23,7 +23,8 @@ EXPORTS = [
     "tasc_session_workspace_bytes", "tasc_session_create", "tasc_session_destroy", "tasc_session_prefill", "tasc_draft",
     "tasc_verify_step", "tasc_generate", "tasc_session_get_tokens", "tasc_session_status", "tasc_profile_enable", "tasc_profile_read", "tasc_profile_durations", "tasc_config_set", "tasc_profile_phases", "tasc_calibration_copy", "tasc_calibration_mfma", "tasc_calibration_read", "tasc_calibration_handover", "tasc_calibration_gemm",
     "tasc_page_tables", "tasc_kv4_page_bytes", "tasc_kv4_append", "tasc_kv4_read", "tasc_kv4_attention_workspace_bytes",
-    "tasc_kv4_attention", "tasc_accept_sampled_workspace_bytes", "tasc_accept_sampled",
+    "tasc_kv4_attention", "tasc_accept_sampled_workspace_bytes", "tasc_accept_sampled", "tasc_sampled_scratch_bytes",
+    "tasc_verify_step_sampled", "tasc_session_rewind", "tasc_generate_sampled", "tasc_session_kv4_bytes", "tasc_session_create_kv4",
 ]
 KERNEL_CLASSES = ["draft", "prepare", "norm", "gemm_qkv", "rope_kv", "attn", "gemm_o", "gemm_gu", "gemm_d", "lmhead", "accept",
                   "verify", "layers"]
@@ -68,6 +69,10 @@ class GenStats(C.Structure):
     _fields_ = [("steps", C.c_int64), ("emitted", C.c_int64), ("accepted", C.c_int64), ("proposed", C.c_int64),
                 ("accept_hist", C.c_int64 * (TASC_MAX_K + 1)), ("prefill_ms", C.c_double), ("decode_ms", C.c_double),
                 ("xcd_local_steps", C.c_int64)]
+
+
+class Sampling(C.Structure):
+    _fields_ = [("temperature", C.c_void_p), ("u", C.c_void_p), ("n_u", C.c_int64), ("scratch", C.c_void_p), ("scratch_bytes", C.c_size_t)]
 
 
 class Kv4CacheDesc(C.Structure):
@@ -135,7 +140,15 @@ def lib():
         L.tasc_profile_durations.argtypes = [C.c_int32, C.c_void_p, C.c_int64, C.POINTER(C.c_int64)]
         L.tasc_page_tables.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p, C.c_int32, C.c_void_p,
                                        C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
-        for name in ("tasc_kv4_page_bytes", "tasc_kv4_attention_workspace_bytes", "tasc_accept_sampled_workspace_bytes"):
+        L.tasc_sampled_scratch_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
+        L.tasc_verify_step_sampled.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(Sampling), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.tasc_session_rewind.argtypes = [C.c_void_p, C.c_void_p]
+        L.tasc_generate_sampled.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.POINTER(SpecParams),
+                                            C.POINTER(Sampling), C.c_void_p, C.POINTER(GenStats), C.c_void_p]
+        L.tasc_session_kv4_bytes.argtypes = [C.c_void_p, C.c_int32]
+        L.tasc_session_create_kv4.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
+                                              C.POINTER(C.c_void_p)]
+        for name in ("tasc_kv4_page_bytes", "tasc_sampled_scratch_bytes", "tasc_session_kv4_bytes", "tasc_kv4_attention_workspace_bytes", "tasc_accept_sampled_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.tasc_kv4_page_bytes.argtypes = [C.c_int32] * 2
         L.tasc_kv4_append.argtypes = [C.POINTER(Kv4CacheDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p]
@@ -324,6 +337,7 @@ class Session:
     def __init__(self, handle, model, batch, max_len, max_rows, kv_pool, workspace):
         self.handle, self.model, self.batch, self.max_len, self.max_rows = handle, model, batch, max_len, max_rows
         self._kv_pool, self._workspace = kv_pool, workspace     # keep the caller-owned buffers alive
+        self._scratch = {}                                      # of sampled steps, by k
 
     def close(self):
         if self.handle:
@@ -645,3 +659,67 @@ def tasc_accept_sampled(logits, drafts, draft_probs, temperature, u, accept_len,
                                      a("draft_probs", draft_probs, f32, (B, nq - 1, V), True), a("temperature", temperature, f32, (B,), True),
                                      a("u", u, f32, (B, nq, 2)), a("accept_len", accept_len, i32, (B,)), a("emitted", emitted, i32, (B, nq)),
                                      a("logprob", logprob, f32, (B, nq), True), ws, n, _stream(stream)))
+
+
+# ---------------------------------------------------------------- sessions that sample, sessions over a 4-bit cache
+def tasc_session_kv4_bytes(model: Model, n_pages) -> int:
+    return lib().tasc_session_kv4_bytes(model.handle, n_pages)
+
+
+def tasc_session_create_kv4(model: Model, batch, max_len, max_rows, n_pages) -> Session:
+    """A session over a 4-bit cache of n_pages pages a layer; allocates the pool and the workspace through PyTorch."""
+    import torch
+    kvb = tasc_session_kv4_bytes(model, n_pages)
+    wsb = tasc_session_workspace_bytes(model, batch, max_len, max_rows)
+    kv = torch.empty(max(kvb, 1), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(max(wsb, 1), dtype=torch.uint8, device="cuda")
+    out = C.c_void_p()
+    _check(lib().tasc_session_create_kv4(model.handle, batch, max_len, max_rows, n_pages, kv.data_ptr(), kvb, ws.data_ptr(), wsb, C.byref(out)))
+    return Session(out.value, model, batch, max_len, max_rows, kv, ws)
+
+
+def tasc_sampled_scratch_bytes(model: Model, batch, k) -> int:
+    return lib().tasc_sampled_scratch_bytes(model.handle, batch, k)
+
+
+def _sampling(who, model, s, k, u, temperature, scratch):
+    """(what must stay alive, struct).  A scratch made here stays with the session, one for every k, as recorded steps do."""
+    import torch
+    if not torch.is_tensor(u) or u.dim() != 3:
+        _refuse(f"{who}: u is not [batch, pairs, 2]")
+    if scratch is None:
+        if k not in s._scratch:
+            s._scratch[k] = torch.empty(max(tasc_sampled_scratch_bytes(model, s.batch, k), 1), dtype=torch.uint8, device="cuda")
+        scratch = s._scratch[k]
+    return scratch, Sampling(_device_array(who, "temperature", temperature, torch.float32, (s.batch,), True),
+                             _device_array(who, "u", u, torch.float32, (s.batch, None, 2)), u.shape[1], scratch.data_ptr(), scratch.numel() * scratch.element_size())
+
+
+def tasc_verify_step_sampled(model: Model, s: Session, drafts, k, u, temperature=None, accept_len=None, emitted=None, logprob=None, scratch=None, stream=None):
+    """u: fp32 cuda tensor [batch, pairs, 2], pair e for a sequence's generated token e; temperature fp32 [batch] or None; accept_len int32 [batch],
+    emitted int32 [batch, k + 1] and logprob fp32 [batch, k + 1] (or None) are written in place."""
+    import torch
+    who, i32 = "verify_step_sampled", torch.int32
+    keep, p = _sampling(who, model, s, k, u, temperature, scratch)
+    _check(lib().tasc_verify_step_sampled(model.handle, s.handle, _device_array(who, "drafts", drafts, i32, (s.batch, k), k == 0), k, C.byref(p),
+                                          _device_array(who, "accept_len", accept_len, i32, (s.batch,), True),
+                                          _device_array(who, "emitted", emitted, i32, (s.batch, k + 1), True),
+                                          _device_array(who, "logprob", logprob, torch.float32, (s.batch, k + 1), True), _stream(stream)))
+
+
+def tasc_session_rewind(s: Session, stream=None):
+    _check(lib().tasc_session_rewind(s.handle, _stream(stream)))
+
+
+def tasc_generate_sampled(model: Model, ng, s: Session, prompts, prompt_offsets, max_new, params: SpecParams, u, out_tokens, temperature=None, scratch=None,
+                          stream=None) -> GenStats:
+    """As tasc_generate; u: fp32 cuda tensor [batch, pairs, 2] (pairs = max_new gives every token its own)."""
+    import torch
+    who = "generate_sampled"
+    prompt_offsets = np.ascontiguousarray(prompt_offsets, dtype=np.int64)
+    keep, p = _sampling(who, model, s, params.k, u, temperature, scratch)
+    st = GenStats()
+    _check(lib().tasc_generate_sampled(model.handle, ng.handle if ng is not None else None, s.handle, _ptr(prompts), _ptr(prompt_offsets), _where(prompts), max_new,
+                                       C.byref(params), C.byref(p), _device_array(who, "out_tokens", out_tokens, torch.int32, (s.batch, max_new)), C.byref(st),
+                                       _stream(stream)))
+    return st

@@ -96,6 +96,22 @@ __global__ void k_gather_out(int B, int max_len, int max_new, const int32_t* __r
     for (int i = threadIdx.x; i < max_new; i += blockDim.x) out[(size_t)b * max_new + i] = tokens[(size_t)b * max_len + n_prompt[b] + i];
 }
 
+// every sequence's length once it has its tokens, with the rows that a frozen one still writes
+__global__ void k_full_lengths(int B, int more, const int32_t* __restrict__ n_prompt, int32_t* len) {
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b < B) len[b] = n_prompt[b] + more;
+}
+// back to the end of the prompt, whose last token is scored again
+__global__ void k_rewind(int B, const int32_t* __restrict__ n_prompt, int32_t* n_tok, int32_t* cached, int32_t* n_emit, u64* counters) {
+    const int b = blockIdx.x * blockDim.x + threadIdx.x;
+    if (b < B) {
+        n_tok[b] = n_prompt[b];
+        cached[b] = n_prompt[b] - 1;
+        n_emit[b] = 0;
+    }
+    if (b == 0) counters[0] = 0;
+}
+
 __global__ void k_init_block_tab(int B, int max_blocks, int32_t* bt) {
     const int idx = blockIdx.x * blockDim.x + threadIdx.x;
     if (idx >= B * max_blocks) return;
@@ -346,15 +362,22 @@ extern "C" size_t tasc_session_workspace_bytes(const tasc_model* m, int32_t batc
     return ws_layout(m->desc, batch, max_len, max_rows, prompt_rows(m->desc, batch, max_len, max_rows)).total;
 }
 
-extern "C" tasc_status tasc_session_create(const tasc_model* m, int32_t batch, int32_t max_len, int32_t max_rows, void* kv_pool,
-                                           size_t kv_bytes, void* workspace, size_t ws_bytes, tasc_session** out) {
+extern "C" size_t tasc_session_kv4_bytes(const tasc_model* m, int32_t n_pages) {
+    if (!m || n_pages < 1 || n_pages >= 1 << 27 || !tasc_tiled_fits(m->desc)) return 0;
+    return (size_t)m->desc.n_layers * n_pages * tasc_kv4_page_bytes(m->desc.n_kv_heads, m->desc.head_dim);
+}
+
+namespace {
+// kv4_pages: pages of a layer's 4-bit cache, 0: a cache in the model's type
+tasc_status session_create(const tasc_model* m, int32_t batch, int32_t max_len, int32_t max_rows, void* kv_pool, size_t kv_bytes, int32_t kv4_pages,
+                           void* workspace, size_t ws_bytes, tasc_session** out) {
     TASC_REQUIRE(m && kv_pool && workspace && out, "session_create: null argument");
     TASC_REQUIRE(batch >= 1 && max_len >= 1 && max_rows >= 1, "session_create: batch %d, max_len %d, max_rows %d", batch, max_len,
                  max_rows);
     TASC_REQUIRE(max_len <= m->desc.max_pos, "session_create: max_len %d exceeds the model's max_pos %d", max_len, m->desc.max_pos);
     TASC_REQUIRE(((uintptr_t)kv_pool & 255) == 0 && ((uintptr_t)workspace & 255) == 0, "session_create: buffers must be 256-byte "
                  "aligned");
-    const size_t need_kv = tasc_session_kv_bytes(m, batch, max_len);
+    const size_t need_kv = kv4_pages ? tasc_session_kv4_bytes(m, kv4_pages) : tasc_session_kv_bytes(m, batch, max_len);
     // a workspace that does not hold prompt_rows gets as many as it does, batch x max_rows at least
     int64_t lo = (int64_t)batch * max_rows, hi = prompt_rows(m->desc, batch, max_len, max_rows);
     while (lo < hi) {
@@ -380,6 +403,7 @@ extern "C" tasc_status tasc_session_create(const tasc_model* m, int32_t batch, i
     s->prefilled = 0;
     s->kv_pool = kv_pool;
     s->page_elems = 2 * (size_t)m->desc.n_kv_heads * TASC_KV_BLOCK * m->desc.head_dim;
+    s->kv4_pages = kv4_pages;
     s->kv_layer_stride = (size_t)batch * s->max_blocks * s->page_elems;
     s->host_counters = nullptr;
     s->bar_epoch = 0;
@@ -447,16 +471,35 @@ extern "C" tasc_status tasc_session_create(const tasc_model* m, int32_t batch, i
         }
         s->chain_ready = true;
     }
-    const int n = batch * s->max_blocks;
-    k_init_block_tab<<<dim3((n + 255) / 256), dim3(256), 0, 0>>>(batch, s->max_blocks, d.block_tab);
-    TASC_LAUNCH_CHECK();
+    if (!kv4_pages) {
+        const int n = batch * s->max_blocks;
+        k_init_block_tab<<<dim3((n + 255) / 256), dim3(256), 0, 0>>>(batch, s->max_blocks, d.block_tab);
+        TASC_LAUNCH_CHECK();
+    }
     TASC_HIP(hipMemsetAsync(d.counters, 0, TASC_N_COUNTERS * sizeof(u64), 0));
-    // the MFMA attention multiplies masked keys by zero weights: the pool must never hold NaN or Inf patterns
-    TASC_HIP(hipMemsetAsync(kv_pool, 0, need_kv, 0));
+    // the MFMA attention multiplies masked keys by zero weights: the pool must never hold NaN or Inf patterns.  (The one over a 4-bit
+    // cache leaves out what is masked, whatever lies there, and its tables are made by the prefill.)
+    if (!kv4_pages) TASC_HIP(hipMemsetAsync(kv_pool, 0, need_kv, 0));
     TASC_HIP(hipDeviceSynchronize());
     guard.p = nullptr;
     *out = s;
     return TASC_OK;
+}
+}  // namespace
+
+extern "C" tasc_status tasc_session_create(const tasc_model* m, int32_t batch, int32_t max_len, int32_t max_rows, void* kv_pool,
+                                           size_t kv_bytes, void* workspace, size_t ws_bytes, tasc_session** out) {
+    return session_create(m, batch, max_len, max_rows, kv_pool, kv_bytes, 0, workspace, ws_bytes, out);
+}
+
+extern "C" tasc_status tasc_session_create_kv4(const tasc_model* m, int32_t batch, int32_t max_len, int32_t max_rows, int32_t n_pages, void* kv_pool,
+                                               size_t kv_bytes, void* workspace, size_t ws_bytes, tasc_session** out) {
+    TASC_REQUIRE(m, "session_create_kv4: null argument");
+    TASC_REQUIRE(tasc_tiled_fits(m->desc), "session_create_kv4: a 4-bit cache needs a bf16 model with d_model, n_heads * head_dim and d_ffn multiples of 64 and "
+                 "heads of 32, 64 or 128 channels");
+    TASC_REQUIRE(n_pages >= 1 && n_pages < 1 << 27, "session_create_kv4: %d pages outside [1, 2^27)", n_pages);
+    TASC_REQUIRE(batch >= 1 && (int64_t)batch * m->desc.n_kv_heads <= 65535, "session_create_kv4: batch %d x %d KV heads outside [1, 65535]", batch, m->desc.n_kv_heads);
+    return session_create(m, batch, max_len, max_rows, kv_pool, kv_bytes, n_pages, workspace, ws_bytes, out);
 }
 
 extern "C" void tasc_session_destroy(tasc_session* s) {
@@ -484,7 +527,7 @@ extern "C" tasc_status tasc_session_prefill(const tasc_model* m, tasc_session* s
     TASC_REQUIRE(prompt_offsets[0] == 0, "prefill: prompt_offsets[0] != 0");
     hipStream_t st = (hipStream_t)stream;
     const int B = s->batch, C = s->max_rows;
-    int64_t longest = 0;
+    int64_t longest = 0, pages = 0;
     for (int b = 0; b < B; ++b) {
         const int64_t P = prompt_offsets[b + 1] - prompt_offsets[b];
         TASC_REQUIRE(P >= 1, "prefill: prompt %d is empty", b);
@@ -493,6 +536,11 @@ extern "C" tasc_status tasc_session_prefill(const tasc_model* m, tasc_session* s
                      "prefill: prompt %d (%lld tokens) + max_new %d + 2 x max_rows %d exceeds max_len %d", b, (long long)P, max_new,
                      s->max_rows, s->max_len);
         longest = std::max(longest, P);
+        pages += (P + max_new + 2 * (int64_t)s->max_rows + TASC_KV_BLOCK - 1) / TASC_KV_BLOCK;
+    }
+    if (s->kv4_pages && pages > s->kv4_pages) {
+        tasc_set_error("prefill: the sequences need %lld pages of the cache's %d", (long long)pages, s->kv4_pages);
+        return TASC_ENOMEM;
     }
     const int64_t total = prompt_offsets[B];
     s->prefilled = 0;
@@ -510,6 +558,12 @@ extern "C" tasc_status tasc_session_prefill(const tasc_model* m, tasc_session* s
     k_reset<<<dim3(B), dim3(256), 0, st>>>(B, s->max_len, d_prompts, d.off, d.tokens, d.n_tok, d.n_prompt, d.cached, d.n_emit,
                                            max_new, d.counters);
     TASC_LAUNCH_CHECK();
+    if (s->kv4_pages) {
+        k_full_lengths<<<dim3((B + 255) / 256), dim3(256), 0, st>>>(B, max_new + 2 * s->max_rows, d.n_prompt, d.pos0);
+        TASC_LAUNCH_CHECK();
+        tasc_status rc = tasc_page_tables(d.pos0, nullptr, nullptr, B, nullptr, s->kv4_pages, d.block_tab, s->max_blocks, nullptr, nullptr, nullptr, 0, nullptr, st);
+        if (rc != TASC_OK) return rc;
+    }
     s->bar_epoch = 0;  // k_reset cleared the barrier flags and counters (the time-out flag among them) with the other counters
     s->barb_base = 0;
     s->ll_armed = false;   // a step that timed out may have left its hand-over buffers half written: re-armed at the next launch
@@ -569,17 +623,17 @@ extern "C" tasc_status tasc_session_prefill(const tasc_model* m, tasc_session* s
 namespace {
 // the launches of one verify step on `st`: rows, forward, acceptance
 tasc_status verify_step_enqueue(const tasc_model* m, tasc_session* s, const int32_t* drafts, int32_t k, int32_t* accept_len,
-                                int32_t* emitted, float* logits_dbg, int32_t* trace_step, hipStream_t st) {
+                                int32_t* emitted, float* logits_dbg, int32_t* trace_step, const TascSampled* sampled, hipStream_t st) {
     const int B = s->batch, nq = k + 1;
-    const TascVerifyTail tail{k, drafts, accept_len, emitted, trace_step};
-    return tasc_forward_rows(m, s, nq, B * nq, B * nq, logits_dbg, &tail, st);
+    const TascVerifyTail tail{k, drafts, accept_len, emitted, trace_step, sampled};
+    return tasc_forward_rows(m, s, nq, B * nq, B * nq, sampled ? sampled->logits : logits_dbg, &tail, st);
 }
 
 // A verify step outside the persistent kernels is a few dozen to a few hundred launches whose arguments never change from step to step (row
 // counts, positions and tokens live in device memory), so the second step with the same arguments is recorded into a
 // graph, on a stream of the session's own, and every later one is a single graph launch on the caller's stream.
 tasc_status verify_step_impl(const tasc_model* m, tasc_session* s, const int32_t* drafts, int32_t k, int32_t* accept_len,
-                             int32_t* emitted, float* logits_dbg, int32_t* trace_step, hipStream_t st) {
+                             int32_t* emitted, float* logits_dbg, int32_t* trace_step, const TascSampled* sampled, hipStream_t st) {
     TascProfScope whole(TASC_KC_VERIFY, st);
     bool graphable = g_tasc_config.step_graph != 0 && s->chain_ready && !logits_dbg && !trace_step && !tasc_prof_any() &&
                      !tasc_forward_is_small(m, s, k + 1);
@@ -590,25 +644,26 @@ tasc_status verify_step_impl(const tasc_model* m, tasc_session* s, const int32_t
             graphable = false;                // the caller records this step itself
         }
     }
-    if (!graphable) return verify_step_enqueue(m, s, drafts, k, accept_len, emitted, logits_dbg, trace_step, st);
+    if (!graphable) return verify_step_enqueue(m, s, drafts, k, accept_len, emitted, logits_dbg, trace_step, sampled, st);
     const int chains = tasc_forward_chains(m, s, k + 1);
     const bool tiled = tasc_forward_is_tiled(m, s, k + 1);
+    const TascSampled key = sampled ? *sampled : TascSampled{};
     TascStepGraph* g = nullptr;
     for (TascStepGraph& e : s->step_graphs)
-        if (e.k == k && e.chains == chains && e.tiled == tiled && e.drafts == drafts && e.accept_len == accept_len && e.emitted == emitted) g = &e;
+        if (e.k == k && e.chains == chains && e.tiled == tiled && e.drafts == drafts && e.accept_len == accept_len && e.emitted == emitted && e.sampled == key) g = &e;
     if (!g) {
         if (s->step_graphs.size() >= 8) {     // a caller that keeps changing its buffers: forget the oldest
             if (s->step_graphs.front().exec) (void)hipGraphExecDestroy(s->step_graphs.front().exec);
             s->step_graphs.erase(s->step_graphs.begin());
         }
-        s->step_graphs.push_back(TascStepGraph{k, chains, tiled, drafts, accept_len, emitted, 0, nullptr});
+        s->step_graphs.push_back(TascStepGraph{k, chains, key, tiled, drafts, accept_len, emitted, 0, nullptr});
         g = &s->step_graphs.back();
     }
     if (!g->exec && g->seen >= 1) {
         hipGraph_t graph = nullptr;
         bool ok = hipStreamBeginCapture(s->graph_st, hipStreamCaptureModeThreadLocal) == hipSuccess;
         if (ok) {
-            const tasc_status rc = verify_step_enqueue(m, s, drafts, k, accept_len, emitted, nullptr, nullptr, s->graph_st);
+            const tasc_status rc = verify_step_enqueue(m, s, drafts, k, accept_len, emitted, nullptr, nullptr, sampled, s->graph_st);
             ok = hipStreamEndCapture(s->graph_st, &graph) == hipSuccess && rc == TASC_OK && graph != nullptr;
         }
         ok = ok && hipGraphInstantiate(&g->exec, graph, nullptr, nullptr, 0) == hipSuccess;
@@ -624,7 +679,7 @@ tasc_status verify_step_impl(const tasc_model* m, tasc_session* s, const int32_t
         return TASC_OK;
     }
     if (g->seen >= 0) ++g->seen;
-    return verify_step_enqueue(m, s, drafts, k, accept_len, emitted, logits_dbg, trace_step, st);
+    return verify_step_enqueue(m, s, drafts, k, accept_len, emitted, logits_dbg, trace_step, sampled, st);
 }
 }  // namespace
 
@@ -639,30 +694,89 @@ extern "C" tasc_status tasc_verify_step(const tasc_model* m, tasc_session* s, co
         tasc_set_error("verify_step: session has no prompt yet");
         return TASC_ESTATE;
     }
-    return verify_step_impl(m, s, drafts, k, accept_len, emitted, logits_dbg, nullptr, (hipStream_t)stream);
+    return verify_step_impl(m, s, drafts, k, accept_len, emitted, logits_dbg, nullptr, nullptr, (hipStream_t)stream);
 }
 
-extern "C" tasc_status tasc_generate(const tasc_model* m, const tasc_ngram* ng, tasc_session* s, const int32_t* prompts,
-                                     const int64_t* prompt_offsets, tasc_mem where, int32_t max_new, const tasc_spec_params* p,
-                                     int32_t* out_tokens, int32_t* trace, int32_t trace_steps, tasc_gen_stats* stats,
-                                     void* stream) {
+namespace {
+// checks a sampling request and lays out its scratch
+tasc_status sampled_of(const char* who, const tasc_model* m, const tasc_session* s, int32_t k, const tasc_sampling* p, float* logprob, TascSampled* out) {
+    TASC_REQUIRE(p && p->u, "%s: null sampling argument", who);
+    TASC_REQUIRE(p->n_u >= 1, "%s: %lld random pairs per sequence", who, (long long)p->n_u);
+    TASC_REQUIRE((int64_t)s->batch * (k + 1) <= 65535, "%s: %d sequences of %d rows are more than 65535 rows", who, s->batch, k + 1);
+    const size_t need = tasc_sampled_scratch_bytes(m, s->batch, k);
+    TASC_REQUIRE(need > 0, "%s: a vocabulary of %d tokens is beyond 2^24", who, m->desc.vocab);
+    if (!p->scratch || p->scratch_bytes < need) {
+        tasc_set_error("%s: scratch of %zu of %zu bytes", who, p->scratch ? p->scratch_bytes : 0, need);
+        return TASC_ENOMEM;
+    }
+    TASC_REQUIRE(((uintptr_t)p->scratch & 255) == 0, "%s: the scratch must be 256-byte aligned", who);
+    *out = TascSampled{p->temperature, p->u, p->n_u, logprob, (float*)p->scratch, (char*)p->scratch + tasc_sample_logits_bytes(s->batch, k, m->desc.vocab)};
+    return TASC_OK;
+}
+}  // namespace
+
+extern "C" size_t tasc_sampled_scratch_bytes(const tasc_model* m, int32_t batch, int32_t k) {
+    if (!m) return 0;
+    const size_t parts = tasc_accept_sampled_workspace_bytes(batch, k, m->desc.vocab);
+    return parts == 0 ? 0 : tasc_sample_logits_bytes(batch, k, m->desc.vocab) + parts;
+}
+
+extern "C" tasc_status tasc_verify_step_sampled(const tasc_model* m, tasc_session* s, const int32_t* drafts, int32_t k, const tasc_sampling* p, int32_t* accept_len,
+                                                int32_t* emitted, float* logprob, void* stream) {
+    TASC_REQUIRE(m && s, "verify_step_sampled: null argument");
+    TASC_REQUIRE(s->model == m, "verify_step_sampled: session belongs to another model");
+    TASC_REQUIRE(k >= 0 && k <= TASC_MAX_K && k + 1 <= s->max_rows, "verify_step_sampled: k %d outside [0, min(%d, max_rows - 1 = %d)]", k, TASC_MAX_K, s->max_rows - 1);
+    TASC_REQUIRE(k == 0 || drafts, "verify_step_sampled: null drafts");
+    TascSampled sampled;
+    const tasc_status rc = sampled_of("verify_step_sampled", m, s, k, p, logprob, &sampled);
+    if (rc != TASC_OK) return rc;
+    if (!s->prefilled) {
+        tasc_set_error("verify_step_sampled: session has no prompt yet");
+        return TASC_ESTATE;
+    }
+    return verify_step_impl(m, s, drafts, k, accept_len, emitted, nullptr, nullptr, &sampled, (hipStream_t)stream);
+}
+
+extern "C" tasc_status tasc_session_rewind(tasc_session* s, void* stream) {
+    TASC_REQUIRE(s, "session_rewind: null argument");
+    if (!s->prefilled) {
+        tasc_set_error("session_rewind: session has no prompt yet");
+        return TASC_ESTATE;
+    }
+    const TascSessDev& d = s->d;
+    k_rewind<<<dim3((s->batch + 63) / 64), dim3(64), 0, (hipStream_t)stream>>>(s->batch, d.n_prompt, d.n_tok, d.cached, d.n_emit, d.counters);
+    TASC_LAUNCH_CHECK();
+    return TASC_OK;
+}
+
+namespace {
+// the whole loop: greedy, or sampled (`sampling` not null)
+tasc_status generate(const tasc_model* m, const tasc_ngram* ng, tasc_session* s, const int32_t* prompts, const int64_t* prompt_offsets, tasc_mem where, int32_t max_new,
+                     const tasc_spec_params* p, const tasc_sampling* sampling, int32_t* out_tokens, int32_t* trace, int32_t trace_steps, tasc_gen_stats* stats,
+                     void* stream) {
     TASC_REQUIRE(m && s && p && out_tokens, "generate: null argument");
     TASC_REQUIRE(p->k >= 0 && p->k <= TASC_MAX_K && p->k + 1 <= s->max_rows, "generate: k %d outside [0, min(%d, max_rows - 1)]",
                  p->k, TASC_MAX_K);
     TASC_REQUIRE(p->k == 0 || ng, "generate: k > 0 needs the n-gram tables");
     TASC_REQUIRE(!trace || trace_steps >= 0, "generate: negative trace capacity");
+    TascSampled sampled{};
+    if (sampling) {
+        const tasc_status rc = sampled_of("generate_sampled", m, s, p->k, sampling, nullptr, &sampled);
+        if (rc != TASC_OK) return rc;
+    }
     hipStream_t st = (hipStream_t)stream;
     struct Ev { hipEvent_t e[3]; int n = 0; ~Ev() { for (int i = 0; i < n; ++i) (void)hipEventDestroy(e[i]); } } ev;
     for (int i = 0; i < 3; ++i) { TASC_HIP(hipEventCreate(&ev.e[i])); ev.n = i + 1; }
     TASC_HIP(hipEventRecord(ev.e[0], st));
     tasc_status rc = tasc_session_prefill(m, s, prompts, prompt_offsets, where, max_new, st);
+    if (rc == TASC_OK && sampling) rc = tasc_session_rewind(s, st);      // the first token is drawn as the others are
     if (rc != TASC_OK) return rc;
     TASC_HIP(hipEventRecord(ev.e[1], st));
     const int B = s->batch, k = p->k;
     TascSessDev& d = s->d;
     const size_t trace_stride = (size_t)B * (2 * k + 3);
     int64_t steps = 0;
-    int64_t min_emit = 1;
+    int64_t min_emit = sampling ? 0 : 1;
     while (min_emit < max_new) {
         // every step emits at least 1 and at most k + 1 tokens per sequence: this many steps are certainly needed
         const int64_t run = (max_new - min_emit + k) / (k + 1);
@@ -672,7 +786,7 @@ extern "C" tasc_status tasc_generate(const tasc_model* m, const tasc_ngram* ng, 
                 if (rc != TASC_OK) return rc;
             }
             int32_t* tr = (trace && steps < trace_steps) ? trace + steps * trace_stride : nullptr;
-            rc = verify_step_impl(m, s, d.drafts, k, nullptr, nullptr, nullptr, tr, st);
+            rc = verify_step_impl(m, s, d.drafts, k, nullptr, nullptr, nullptr, tr, sampling ? &sampled : nullptr, st);
             if (rc != TASC_OK) return rc;
         }
         k_set_u64<<<dim3(1), dim3(1), 0, st>>>(&d.counters[1], ~0ull);
@@ -711,6 +825,21 @@ extern "C" tasc_status tasc_generate(const tasc_model* m, const tasc_ngram* ng, 
         stats->decode_ms = b;
     }
     return TASC_OK;
+}
+}  // namespace
+
+extern "C" tasc_status tasc_generate(const tasc_model* m, const tasc_ngram* ng, tasc_session* s, const int32_t* prompts,
+                                     const int64_t* prompt_offsets, tasc_mem where, int32_t max_new, const tasc_spec_params* p,
+                                     int32_t* out_tokens, int32_t* trace, int32_t trace_steps, tasc_gen_stats* stats,
+                                     void* stream) {
+    return generate(m, ng, s, prompts, prompt_offsets, where, max_new, p, nullptr, out_tokens, trace, trace_steps, stats, stream);
+}
+
+extern "C" tasc_status tasc_generate_sampled(const tasc_model* m, const tasc_ngram* ng, tasc_session* s, const int32_t* prompts, const int64_t* prompt_offsets,
+                                             tasc_mem where, int32_t max_new, const tasc_spec_params* p, const tasc_sampling* sampling, int32_t* out_tokens,
+                                             tasc_gen_stats* stats, void* stream) {
+    TASC_REQUIRE(sampling, "generate_sampled: null argument");
+    return generate(m, ng, s, prompts, prompt_offsets, where, max_new, p, sampling, out_tokens, nullptr, 0, stats, stream);
 }
 
 extern "C" tasc_status tasc_session_status(tasc_session* s, int32_t* timed_out, void* stream) {

@@ -12,6 +12,7 @@
 #include "kernels_small.h"
 #include "kernels_pipe.h"
 #include "kernels_tiled.h"
+#include "kernels_kv4.h"
 #include <algorithm>
 #include <type_traits>
 #include <utility>
@@ -114,6 +115,7 @@ tasc_status finish_rows(const tasc_session* s, int n_sel, int n_parts, const flo
                         hipStream_t st) {
     const TascSessDev& d = s->d;
     PROF(TASC_KC_ACCEPT);
+    if (tail && tail->sampled) return tasc_sample_step(s, *tail, st);
     if (tail)
         k_argmax_accept<<<dim3(s->batch), dim3(ACCEPT_THREADS(tail->k + 1)), 0, st>>>(
             AcceptArgs{part_val, part_idx, n_parts, tail->k, s->max_len, tail->drafts, d.tokens, d.n_tok, d.cached, d.n_emit, d.counters,
@@ -453,6 +455,8 @@ tasc_status forward_tiled(const tasc_model* m, tasc_session* s, int nq, int M_al
     // 798 | 793), with 146 to 224 of them 0.98 to 1.02 times (4 of 512: 354 | 354, 558 | 564, 811 | 825; 1 of 2048: 423 | 414, 725 | 712, 955 | 932).
     const int prompt_passes = (s->prompt_ref / s->batch * (H / Hkv) + TAP_ROWS - 1) / TAP_ROWS;
     const bool prompt_attn = !decode && att_chunks == 1 && s->batch * Hkv * prompt_passes >= cus;
+    // A 4-bit cache: how its keys are dealt, a session constant for the same reason (the scratch holds 4 partial results of a row)
+    const Kv4Order kv4_ord = kv4_order(s->batch, Hkv, (int64_t)(H / Hkv) * (decode ? 5 : s->prompt_ref / s->batch), s->max_len, 4, decode);
     const BiasCursors bc{BiasCsr{m->bias_rowptr, m->bias_col, m->bias_val, m->bias_base}, d.sel_tok,
                          m->bias_rowptr ? n_sel * (s->n_strips + 1) : 0, s->n_strips, d.bias_ptr, d.bias_first, d.bias_base};
     const unsigned bias_wgs = (unsigned)((bc.n + 255) / 256);
@@ -523,6 +527,7 @@ tasc_status forward_tiled(const tasc_model* m, tasc_session* s, int nq, int M_al
         for (int l = 0; l < c.n_layers; ++l) {
             const TascLayerW& w = m->layers[l];
             BF16* kv_layer = (BF16*)s->kv_pool + (size_t)l * s->kv_layer_stride;
+            uint8_t* const kv4_layer = (uint8_t*)s->kv_pool + (size_t)l * s->kv4_pages * Hkv * kv4_head_bytes(hd);
             if (!h_ready) {
                 PROF(TASC_KC_NORM);
                 if (D <= RRN_MAX_D) k_rmsnorm_row<<<dim3(M), dim3(256), 0, st>>>(x, w.g1, D, c.rms_eps, h);
@@ -532,12 +537,20 @@ tasc_status forward_tiled(const tasc_model* m, tasc_session* s, int nq, int M_al
             {
                 // one slice: rotation and cache append ride in the projection's epilogue
                 PROF(TASC_KC_GEMM_QKV);
-                if (ks_qkv == 1)
+                if (ks_qkv == 1 && s->kv4_pages)
+                    launch_gemm<TEPI_STORE>(h, w.wqkv, M, nqkv, D, part, nullptr, none, 1, st, cus);
+                else if (ks_qkv == 1)
                     launch_gemm<TEPI_ROPE>(h, w.wqkv, M, nqkv, D, nullptr, q, none, 1, st, cus,
                                            RopeEpi{m->rope_cos, m->rope_sin, n_rows, pos0, block_tab, kv_layer, gm, c.max_pos});
                 else launch_gemm<TEPI_PARTIAL>(h, w.wqkv, M, nqkv, D, part, nullptr, none, ks_qkv, st, cus);
             }
-            if (ks_qkv > 1) {
+            if (s->kv4_pages) {
+                PROF(TASC_KC_ROPE_KV);
+                const Kv4RopeArgs ra{part, (size_t)M * nqkv, ks_qkv, m->rope_cos, m->rope_sin, c.max_pos, n_rows, pos0, block_tab, gm, decode ? nq : 0, q, kv4_layer, s->kv4_pages};
+                if (hd == 128) k_rope_kv4<128><<<dim3(M), dim3(256), 0, st>>>(ra);
+                else if (hd == 64) k_rope_kv4<64><<<dim3(M), dim3(256), 0, st>>>(ra);
+                else k_rope_kv4<32><<<dim3(M), dim3(256), 0, st>>>(ra);
+            } else if (ks_qkv > 1) {
                 // the k-slices of a split projection are added inside the rotation kernel (same order as the reduction kernel)
                 PROF(TASC_KC_ROPE_KV);
                 switch (ks_qkv) {
@@ -552,7 +565,19 @@ tasc_status forward_tiled(const tasc_model* m, tasc_session* s, int nq, int M_al
                 PROF(TASC_KC_ATTN);
                 AttnArgs aa{q, att, kv_layer, n_rows, pos0, block_tab, d.row0, b0, (int32_t)r0, M, nq, H, Hkv,
                             s->max_blocks, decode ? 1 : 0, s->page_elems, 1.0f / sqrtf((float)hd)};
-                if (hd == 32 || s->max_blocks > TA_MAX_BLOCKS) {
+                if (s->kv4_pages) {
+                    Kv4Attn ka{};
+                    ka.pool = kv4_layer;
+                    ka.n_pages = s->kv4_pages; ka.max_pages = s->max_blocks; ka.Hkv = Hkv; ka.H = H; ka.batch = nb; ka.rows = M; ka.max_rows = nq;
+                    ka.q = q; ka.out = att; ka.q_stride = ka.out_stride = nqo;
+                    ka.table = block_tab + (size_t)b0 * s->max_blocks;
+                    ka.row0 = d.row0 + b0; ka.n_rows = n_rows + b0; ka.pos0 = pos0 + b0; ka.row_base = (int32_t)r0;
+                    ka.scale = 1.0f / sqrtf((float)hd);
+                    ka.part_o = part;
+                    ka.part_ml = part + (size_t)kv4_ord.chunks * M * nqo;
+                    const tasc_status rc = tasc_kv4_attend(ka, hd, kv4_ord, st);
+                    if (rc != TASC_OK) return rc;
+                } else if (hd == 32 || s->max_blocks > TA_MAX_BLOCKS) {
                     if (hd == 64) k_attn_tiled<2><<<attn_grid, dim3(SMALL_THREADS), 0, st>>>(aa);
                     else if (hd == 128) k_attn_tiled<4><<<attn_grid, dim3(SMALL_THREADS), 0, st>>>(aa);
                     else k_attn_tiled<1><<<attn_grid, dim3(SMALL_THREADS), 0, st>>>(aa);
@@ -698,7 +723,7 @@ tasc_status forward_small(const tasc_model* m, tasc_session* s, int nq, int n_se
         a.act = (BF16*)(d.small_ws + w.act_off); a.act_stride = w.act_stride;
     }
     a.part_val = d.part_val; a.part_idx = d.part_idx; a.amax = d.amax; a.logits_dbg = logits_dbg;
-    a.k = tail ? tail->k : -1;
+    a.k = tail && !tail->sampled ? tail->k : -1;       // (-1: no acceptance)
     a.drafts = tail ? tail->drafts : nullptr;
     a.tokens = d.tokens; a.n_tok = d.n_tok; a.cached = d.cached; a.n_emit = d.n_emit; a.counters = d.counters;
     a.accept_len = tail ? tail->accept_len : nullptr;
@@ -750,7 +775,7 @@ tasc_status forward_small(const tasc_model* m, tasc_session* s, int nq, int n_se
         }
     }
     TASC_LAUNCH_CHECK();
-    return TASC_OK;
+    return tail && tail->sampled ? tasc_sample_step(s, *tail, st) : TASC_OK;
 }
 
 // ---------------------------------------------------------------- the spatial-pipeline kernel
@@ -848,7 +873,7 @@ tasc_status forward_pipe(const tasc_model* m, tasc_session* s, int nq, int n_sel
     pa.kvn = (BF16*)(cur + w.kvn_off); pa.kvn_stride = w.kvn_stride;
     pa.pv = (float*)(cur + w.pv_off); pa.pi = (int32_t*)(cur + w.pi_off);
     a.part_val = d.part_val; a.part_idx = d.part_idx; a.amax = d.amax; a.logits_dbg = logits_dbg;
-    a.k = tail ? tail->k : -1;
+    a.k = tail && !tail->sampled ? tail->k : -1;       // (-1: no acceptance)
     a.drafts = tail ? tail->drafts : nullptr;
     a.tokens = d.tokens; a.n_tok = d.n_tok; a.cached = d.cached; a.n_emit = d.n_emit; a.counters = d.counters;
     a.accept_len = tail ? tail->accept_len : nullptr;
@@ -889,7 +914,7 @@ tasc_status forward_pipe(const tasc_model* m, tasc_session* s, int nq, int n_sel
     }
     TASC_LAUNCH_CHECK();
     s->ll_copy = 1 - s->ll_copy;
-    return TASC_OK;
+    return tail && tail->sampled ? tasc_sample_step(s, *tail, st) : TASC_OK;
 }
 
 }  // namespace
@@ -959,12 +984,12 @@ int tasc_forward_chains(const tasc_model* m, const tasc_session* s, int32_t nq) 
 
 bool tasc_forward_is_small(const tasc_model* m, const tasc_session* s, int32_t nq) {
     const int decode_rows = s->max_rows < SMALL_ROWS ? s->max_rows : SMALL_ROWS;
-    return g_tasc_config.small_path != 0 && nq <= SMALL_ROWS && small_path_fits(m, s->batch, decode_rows, s->max_blocks);
+    return g_tasc_config.small_path != 0 && s->kv4_pages == 0 && nq <= SMALL_ROWS && small_path_fits(m, s->batch, decode_rows, s->max_blocks);
 }
 
 bool tasc_forward_is_tiled(const tasc_model* m, const tasc_session* s, int32_t nq) {
     if (tasc_forward_is_small(m, s, nq)) return false;
-    return g_tasc_config.tiled_path != 0 && tasc_tiled_fits(m->desc);
+    return (g_tasc_config.tiled_path != 0 || s->kv4_pages) && tasc_tiled_fits(m->desc);
 }
 
 tasc_status tasc_forward_rows(const tasc_model* m, tasc_session* s, int32_t nq, int32_t n_rows, int32_t n_sel, float* logits_dbg,
@@ -993,7 +1018,7 @@ tasc_status tasc_forward_rows(const tasc_model* m, tasc_session* s, int32_t nq, 
         }
         return forward_small(m, s, nq, n_sel, logits_dbg, tail, st);
     }
-    if (g_tasc_config.tiled_path != 0 && tasc_tiled_fits(m->desc)) return forward_tiled(m, s, nq, n_rows, n_sel, logits_dbg, tail, st);
+    if (tasc_forward_is_tiled(m, s, nq)) return forward_tiled(m, s, nq, n_rows, n_sel, logits_dbg, tail, st);
     if (m->desc.dtype == TASC_F32) return forward_generic<float>(m, s, nq, n_rows, n_sel, logits_dbg, tail, st);
     return forward_generic<BF16>(m, s, nq, n_rows, n_sel, logits_dbg, tail, st);
 }

@@ -15,6 +15,7 @@
 // A token's bytes are its own (no byte holds two tokens), so rows are written without a look at their neighbours.
 #pragma once
 #include "numeric.h"
+#include <algorithm>
 
 typedef uint32_t kv4_u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t kv4_u32x2 __attribute__((ext_vector_type(2)));
@@ -32,9 +33,22 @@ inline bool kv4_head_dim_ok(int hd) { return hd == 32 || hd == 64 || hd == 128; 
 // ---------------------------------------------------------------- numbers of a group
 // {scale, low} of a group from its least and largest value; not a number for a group that holds an infinity or a NaN (or whose range
 // is beyond fp32), so that every value of it reads as NaN
-__device__ __forceinline__ uint32_t kv4_scale_low(float lo, float hi, bool finite) {
-    const float scale = (hi - lo) * (1.0f / 15.0f);
-    return finite && fabsf(scale) < __builtin_inff() ? f2bf_pair(lo, scale) : 0x7FC07FC0u;
+struct Kv4Range { float lo, hi; int finite; };
+__device__ __forceinline__ Kv4Range kv4_range(const float (&x)[8]) {
+    Kv4Range g{x[0], x[0], 1};
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+        g.lo = fminf(g.lo, x[e]);
+        g.hi = fmaxf(g.hi, x[e]);
+        g.finite &= fabsf(x[e]) < __builtin_inff();
+    }
+    return g;
+}
+__device__ __forceinline__ Kv4Range kv4_join(const Kv4Range& a, const Kv4Range& b) { return {fminf(a.lo, b.lo), fmaxf(a.hi, b.hi), a.finite & b.finite}; }
+__device__ __forceinline__ Kv4Range kv4_from(const Kv4Range& g, int o) { return {__shfl_xor(g.lo, o), __shfl_xor(g.hi, o), __shfl_xor(g.finite, o)}; }   // lane ^ o's
+__device__ __forceinline__ uint32_t kv4_scale_low(const Kv4Range& g) {
+    const float scale = (g.hi - g.lo) * (1.0f / 15.0f);
+    return g.finite && fabsf(scale) < __builtin_inff() ? f2bf_pair(g.lo, scale) : 0x7FC07FC0u;
 }
 __device__ __forceinline__ float kv4_scale(uint32_t sl) { return __uint_as_float(sl & 0xFFFF0000u); }
 __device__ __forceinline__ float kv4_low(uint32_t sl) { return __uint_as_float(sl << 16); }
@@ -121,24 +135,12 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Rows a, const T* __restri
         for (int e = 0; e < 8; ++e) x[e] = to_f(src[e]);
     }
     const int32_t slot = a.slots[row];
-    float lo = x[0], hi = x[0];
-    bool finite = true;
+    Kv4Range g = kv4_range(x);
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-        lo = fminf(lo, x[e]);
-        hi = fmaxf(hi, x[e]);
-        finite &= fabsf(x[e]) < __builtin_inff();
-    }
-    int fin = finite;
-#pragma unroll
-    for (int o = 1; o < SPAN; o *= 2) {
-        lo = fminf(lo, __shfl_xor(lo, o));
-        hi = fmaxf(hi, __shfl_xor(hi, o));
-        fin &= __shfl_xor(fin, o);
-    }
+    for (int o = 1; o < SPAN; o *= 2) g = kv4_join(g, kv4_from(g, o));
     if (unit >= (int64_t)a.rows * a.Hkv || slot < 0 || slot / TASC_KV_BLOCK >= a.n_pages) return;
     uint8_t* const at = a.pool + ((size_t)(slot / TASC_KV_BLOCK) * a.Hkv + head) * Kv4Layout<HD>::HEAD;
-    kv4_put<HD>(at, slot % TASC_KV_BLOCK, blk, value, x, kv4_scale_low(lo, hi, fin != 0));
+    kv4_put<HD>(at, slot % TASC_KV_BLOCK, blk, value, x, kv4_scale_low(g));
 }
 
 // The values that slots hold, zeros for a slot outside the pool.
@@ -199,10 +201,28 @@ struct Kv4Attn {
     const int32_t* n_rows;
     const int32_t* pos0;               //   the position of its first row
     const int32_t* kv_len;             // [batch] with row_off
+    int32_t row_base;                  // first row of the launch in row0's count
     float scale;
     float* part_o;                     // [chunks, rows, H, HD], used if chunks > 1
     float* part_ml;                    // [chunks, rows, H, 2]
 };
+// Which units there are, and so in which order a row's keys are added: waves of a workgroup that share its pairs (1: none), key chunks
+struct Kv4Order { int wk, chunks; };
+// `pairs` (row, head) pairs of a KV head, a bound or what stands for it; split: waves share pairs in any case
+inline Kv4Order kv4_order(int64_t batch, int kv_heads, int64_t pairs, int64_t max_kv, int most_chunks, bool split) {
+    constexpr int64_t kCus = 256;
+    Kv4Order o{4, 1};
+    const int64_t heads = batch * kv_heads;
+    if (!split && pairs >= 256 && (pairs + 255) / 256 * heads >= kCus) o.wk = 1;
+    if (o.wk == 4) {
+        const int64_t wgs = heads * ((pairs + 63) / 64);
+        o.chunks = (int)std::clamp<int64_t>(std::min<int64_t>(2 * kCus / wgs, max_kv / 512), 1, most_chunks);
+    }
+    return o;
+}
+struct Kv4Attn;
+// kv4.hip: enqueues the attention (a.chunks is set from the order)
+tasc_status tasc_kv4_attend(Kv4Attn a, int hd, const Kv4Order& o, hipStream_t st);
 struct Kv4Seq { int first, n, len; };
 __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attn& a, int b) {
     Kv4Seq s;
@@ -211,7 +231,7 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attn& a, int b) {
         s.n = a.row_off[b + 1] - s.first;
         s.len = a.kv_len[b];
     } else {
-        s.first = a.row0[b];
+        s.first = a.row0[b] - a.row_base;
         s.n = a.n_rows[b];
         s.len = a.pos0[b] + s.n;
     }

@@ -12,6 +12,7 @@
 // tile run on the same XCD and find it in that XCD's L2.
 #pragma once
 #include "kernels_gemm.h"
+#include "kernels_kv4.h"
 
 #define TG_LD (TG_BK + 8)                                     // padded LDS row (elements)
 #define TG_LDS_BYTES(BN, BM) (2 * ((BN) + (BM)) * TG_LD * 2)   // 73728 for 128 x 128, 129024 for 256 x 192
@@ -635,6 +636,76 @@ __global__ __launch_bounds__(256) void k_rope_kv(const float* __restrict__ qkv, 
                 vt[(size_t)(half + u) * TASC_KV_BLOCK] = f2bf(c[0][u]);
             }
         }
+    }
+}
+
+// The same into a 4-bit cache: a thread has 8 channels and their partners half a head away; the HD / 16 threads of a head find the ranges of
+// its groups among themselves (of 128 channels the two halves are the two groups, else they are one).
+struct Kv4RopeArgs {
+    const float* qkv;         // [slices][rows][nqkv]
+    size_t slice_stride;
+    int32_t slices;
+    const float *cosT, *sinT;
+    int32_t max_pos;
+    const int32_t *n_rows, *pos0, *block_tab;
+    KvGeom gm;
+    int32_t nq;
+    BF16* q_out;
+    uint8_t* layer;
+    int32_t n_pages;
+};
+template <int HD>
+__global__ __launch_bounds__(256) void k_rope_kv4(Kv4RopeArgs a) {
+    constexpr int PER = HD / 16, HALF = HD / 2;
+    const KvGeom& gm = a.gm;
+    const int r = blockIdx.x, b = a.nq ? (r + gm.first) / a.nq : gm.seq(r), i = a.nq ? (r + gm.first) % a.nq : gm.index(r, b);
+    const int pos = a.pos0[b] + i, tpos = pos < a.max_pos ? pos : a.max_pos - 1;
+    const bool active = a.nq != 0 || i < a.n_rows[b];
+    const int page = active ? a.block_tab[(size_t)b * gm.max_blocks + pos / TASC_KV_BLOCK] : -1;
+    const int nqkv = (gm.H + 2 * gm.Hkv) * HD;
+    for (int idx = threadIdx.x; idx < (gm.H + 2 * gm.Hkv) * PER; idx += 256) {
+        const int head = idx / PER, e = idx % PER;
+        const float* src = a.qkv + (size_t)r * nqkv + head * HD + 8 * e;
+        float x[8], y[8];
+        load8(src, x);
+        load8(src + HALF, y);
+        for (int s = 1; s < a.slices; ++s) {
+            float p[8], q[8];
+            load8(src + s * a.slice_stride, p);
+            load8(src + s * a.slice_stride + HALF, q);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) { x[u] += p[u]; y[u] += q[u]; }
+        }
+        if (head < gm.H + gm.Hkv) {
+            float cs[8], sn[8];
+            load8(a.cosT + (size_t)tpos * HALF + 8 * e, cs);
+            load8(a.sinT + (size_t)tpos * HALF + 8 * e, sn);
+#pragma unroll
+            for (int u = 0; u < 8; ++u) {
+                const float p = x[u], q = y[u];
+                rope_turn(p, q, cs[u], sn[u], x[u], y[u]);
+            }
+        }
+        if (head < gm.H) {
+            BF16* dst = a.q_out + ((size_t)r * gm.H + head) * HD + 8 * e;
+            *reinterpret_cast<u32x4*>(dst) = u32x4{f2bf_pair(x[0], x[1]), f2bf_pair(x[2], x[3]), f2bf_pair(x[4], x[5]), f2bf_pair(x[6], x[7])};
+            *reinterpret_cast<u32x4*>(dst + HALF) = u32x4{f2bf_pair(y[0], y[1]), f2bf_pair(y[2], y[3]), f2bf_pair(y[4], y[5]), f2bf_pair(y[6], y[7])};
+            continue;                                     // (whole heads: the lanes of a later exchange are all there)
+        }
+        Kv4Range gx = kv4_range(x), gy = kv4_range(y);
+        if constexpr (HD != 128) gx = gy = kv4_join(gx, gy);
+#pragma unroll
+        for (int o = 1; o < PER; o *= 2) {
+            gx = kv4_join(gx, kv4_from(gx, o));
+            if constexpr (HD == 128) gy = kv4_join(gy, kv4_from(gy, o));
+            else gy = gx;
+        }
+        if (page < 0 || page >= a.n_pages) continue;
+        const bool value = head >= gm.H + gm.Hkv;
+        const int kvh = head - gm.H - (value ? gm.Hkv : 0);
+        uint8_t* const at = a.layer + ((size_t)page * gm.Hkv + kvh) * Kv4Layout<HD>::HEAD;
+        kv4_put<HD>(at, pos % TASC_KV_BLOCK, e, value, x, kv4_scale_low(gx));
+        kv4_put<HD>(at, pos % TASC_KV_BLOCK, e + PER, value, y, kv4_scale_low(gy));
     }
 }
 

@@ -5,22 +5,6 @@
 
 namespace {
 
-// How a call is cut.  Pairs are (row, query head of the KV head's group).
-struct Kv4Cut { int mt, wk, tiles, chunks; };
-constexpr int kCus = 256;
-Kv4Cut kv4_cut(int64_t batch, int kv_heads, int share, int64_t max_rows, int64_t max_kv) {
-    Kv4Cut c;
-    const int64_t pairs = max_rows * share;
-    c.mt = pairs <= 16 ? 1 : pairs <= 32 ? 2 : 4;
-    const int64_t tiles4 = (pairs + 64 * c.mt - 1) / (64 * c.mt);
-    c.wk = tiles4 * batch * kv_heads >= kCus && pairs >= 256 ? 1 : 4;
-    c.tiles = (int)(c.wk == 1 ? tiles4 : (pairs + 16 * c.mt - 1) / (16 * c.mt));
-    const int64_t wgs = (int64_t)c.tiles * batch * kv_heads;
-    c.chunks = 1;
-    if (c.wk == 4) c.chunks = (int)std::clamp<int64_t>(std::min<int64_t>(2 * kCus / wgs, max_kv / 512), 1, 64);
-    return c;
-}
-
 template <int HD, int MT, int WK>
 tasc_status attend(const Kv4Attn& a, int tiles, hipStream_t st) {
     constexpr int lds = kv4_attention_lds<HD, MT, WK>();
@@ -39,10 +23,12 @@ tasc_status attend(const Kv4Attn& a, int tiles, hipStream_t st) {
     return TASC_OK;
 }
 template <int HD>
-tasc_status attend_hd(const Kv4Attn& a, const Kv4Cut& c, hipStream_t st) {
+tasc_status attend_hd(const Kv4Attn& a, int wk, hipStream_t st) {
+    const int64_t pairs = (int64_t)a.max_rows * (a.H / a.Hkv);
+    auto tiles = [&](int per) { return (int)((pairs + per - 1) / per); };
     tasc_status rc;
-    if (c.wk == 1) rc = attend<HD, 4, 1>(a, c.tiles, st);
-    else rc = c.mt == 1 ? attend<HD, 1, 4>(a, c.tiles, st) : c.mt == 2 ? attend<HD, 2, 4>(a, c.tiles, st) : attend<HD, 4, 4>(a, c.tiles, st);
+    if (wk == 1) rc = attend<HD, 4, 1>(a, tiles(256), st);
+    else rc = pairs <= 16 ? attend<HD, 1, 4>(a, tiles(16), st) : pairs <= 32 ? attend<HD, 2, 4>(a, tiles(32), st) : attend<HD, 4, 4>(a, tiles(64), st);
     if (rc != TASC_OK) return rc;
     if (a.chunks > 1) k_kv4_merge<HD><<<dim3((unsigned)a.max_rows, (unsigned)a.batch), dim3(256), 0, st>>>(a);
     TASC_LAUNCH_CHECK();
@@ -54,7 +40,7 @@ tasc_status check_cache(const char* who, const tasc_kv4_cache* c) {
     TASC_REQUIRE(kv4_head_dim_ok(c->head_dim), "%s: head_dim %d is none of 32, 64, 128", who, c->head_dim);
     TASC_REQUIRE(c->n_kv_heads >= 1 && c->n_kv_heads <= 1024, "%s: %d KV heads outside [1, 1024]", who, c->n_kv_heads);
     TASC_REQUIRE(c->n_pages >= 1 && c->n_pages < 1 << 27, "%s: %d pages outside [1, 2^27)", who, c->n_pages);
-    TASC_REQUIRE(((uintptr_t)c->pool & 255) == 0, "%s: the pool must be 256-byte aligned", who);
+    TASC_REQUIRE(((uintptr_t)c->pool & 127) == 0, "%s: the pool must be 128-byte aligned", who);
     return TASC_OK;
 }
 // f(head_dim as a type)
@@ -65,7 +51,14 @@ void with_hd(int hd, F f) {
     else f(std::integral_constant<int, 32>{});
 }
 
+constexpr int kMostChunks = 64;
+
 }  // namespace
+
+tasc_status tasc_kv4_attend(Kv4Attn a, int hd, const Kv4Order& o, hipStream_t st) {
+    a.chunks = o.chunks;
+    return hd == 128 ? attend_hd<128>(a, o.wk, st) : hd == 64 ? attend_hd<64>(a, o.wk, st) : attend_hd<32>(a, o.wk, st);
+}
 
 extern "C" size_t tasc_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim) {
     if (!kv4_head_dim_ok(head_dim) || n_kv_heads < 1 || n_kv_heads > 1024) return 0;
@@ -123,8 +116,8 @@ extern "C" tasc_status tasc_kv4_read(const tasc_kv4_cache* c, const int32_t* slo
 extern "C" size_t tasc_kv4_attention_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim, int32_t max_rows,
                                                      int32_t max_kv) {
     if (batch < 1 || rows < 1 || n_heads < 1 || n_kv_heads < 1 || n_heads % n_kv_heads || !kv4_head_dim_ok(head_dim) || max_rows < 1 || max_kv < 0) return 0;
-    const Kv4Cut cut = kv4_cut(batch, n_kv_heads, n_heads / n_kv_heads, max_rows, max_kv);
-    return cut.chunks == 1 ? 0 : (size_t)cut.chunks * rows * n_heads * (head_dim + 2) * sizeof(float);
+    const Kv4Order o = kv4_order(batch, n_kv_heads, (int64_t)max_rows * (n_heads / n_kv_heads), max_kv, kMostChunks, false);
+    return o.chunks == 1 ? 0 : (size_t)o.chunks * rows * n_heads * (head_dim + 2) * sizeof(float);
 }
 
 extern "C" tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv4_attn* p, void* workspace, size_t ws_bytes, void* stream) {
@@ -143,8 +136,8 @@ extern "C" tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv
                  (long long)width);
     TASC_REQUIRE(((uintptr_t)p->q & 15) == 0 && ((uintptr_t)p->out & 15) == 0 && p->q_stride % 8 == 0 && p->out_stride % 8 == 0,
                  "kv4_attention: rows of queries and results must be 16-byte aligned");
-    const Kv4Cut cut = kv4_cut(p->batch, c->n_kv_heads, p->n_heads / c->n_kv_heads, p->max_rows, p->max_kv);
-    const size_t n = (size_t)cut.chunks * p->rows * p->n_heads, need = cut.chunks == 1 ? 0 : n * (c->head_dim + 2) * sizeof(float);
+    const Kv4Order order = kv4_order(p->batch, c->n_kv_heads, (int64_t)p->max_rows * (p->n_heads / c->n_kv_heads), p->max_kv, kMostChunks, false);
+    const size_t n = (size_t)order.chunks * p->rows * p->n_heads, need = order.chunks == 1 ? 0 : n * (c->head_dim + 2) * sizeof(float);
     if (need > 0 && (!workspace || ws_bytes < need)) {
         tasc_set_error("kv4_attention: workspace of %zu of %zu bytes", workspace ? ws_bytes : 0, need);
         return TASC_ENOMEM;
@@ -153,13 +146,11 @@ extern "C" tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv
     Kv4Attn a{};
     a.pool = (const uint8_t*)c->pool;
     a.n_pages = c->n_pages; a.max_pages = p->max_pages; a.Hkv = c->n_kv_heads; a.H = p->n_heads; a.batch = p->batch; a.rows = p->rows;
-    a.max_rows = p->max_rows; a.chunks = cut.chunks;
+    a.max_rows = p->max_rows;
     a.q = (const BF16*)p->q; a.out = (BF16*)p->out; a.q_stride = p->q_stride; a.out_stride = p->out_stride;
     a.table = p->table; a.row_off = p->row_off; a.kv_len = p->kv_len;
     a.scale = p->scale;
     a.part_o = (float*)workspace;
-    a.part_ml = cut.chunks == 1 ? nullptr : (float*)workspace + n * c->head_dim;
-    rc = TASC_OK;
-    with_hd(c->head_dim, [&](auto hd) { rc = attend_hd<decltype(hd)::value>(a, cut, (hipStream_t)stream); });
-    return rc;
+    a.part_ml = order.chunks == 1 ? nullptr : (float*)workspace + n * c->head_dim;
+    return tasc_kv4_attend(a, c->head_dim, order, (hipStream_t)stream);
 }

@@ -28,12 +28,20 @@ struct SampleArgs {
     const int32_t* drafts;           // [B, k]
     const float* probs;              // nullable [B, k, vocab]
     const float* temperature;        // nullable [B]
-    const float* u;                  // [B, k + 1, 2]
+    const float* u;                  // [B, n_u, 2]
+    int64_t n_u;
+    const int32_t* n_emit;           // null: row i of a sequence takes pair i; else pair min(n_emit + i, n_u - 1)
     Part* parts;                     // [B (k + 1), n_seg]
     double* residual;                // [B, n_seg], given probs
     int32_t *accept_len, *emitted;
     float* logprob;
+    TascSessDev d;                   // a session's step (n_emit is not null): commits what it emits, as k_argmax_accept does
+    int32_t max_len;
 };
+__device__ __forceinline__ double random_of(const SampleArgs& a, int b, int i, int which) {
+    const int64_t pair = a.n_emit ? min((int64_t)a.n_emit[b] + i, a.n_u - 1) : i;
+    return (double)a.u[2 * (b * a.n_u + pair) + which];
+}
 
 // exp(x) for x <= 0 (NaN stays one): x = n ln 2 + r, |r| <= ln 2 / 2, and the Taylor polynomial of degree 11, whose remainder is below
 // (ln 2 / 2)^12 / 12! = 6.3e-15
@@ -153,9 +161,9 @@ __device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int l
     o.logz = log(o.z);
     o.draft_logp = (float)(x - o.logz);
     const double q = o.draft >= 0 && a.probs ? (double)a.probs[((int64_t)b * a.k + i) * a.vocab + o.draft] : 1.0;
-    o.accept = o.ok && o.draft >= 0 && (double)a.u[((int64_t)b * (a.k + 1) + i) * 2] * q * o.z < w;
+    o.accept = o.ok && o.draft >= 0 && random_of(a, b, i, 0) * q * o.z < w;
     if (is_greedy(a, b)) {
-        o.accept = o.ok && o.draft == o.best && (double)a.u[((int64_t)b * (a.k + 1) + i) * 2] * q < 1.0;
+        o.accept = o.ok && o.draft == o.best && random_of(a, b, i, 0) * q < 1.0;
         o.draft_logp = 0.f;
         o.logz = 0.0;
     }
@@ -201,6 +209,19 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
     __shared__ int32_t s_seg, s_first[16], s_last[16];
     __shared__ double s_x;
     const int b = blockIdx.x, nq = a.k + 1, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    const int n_emit = a.n_emit ? a.n_emit[b] : 0;
+    const bool frozen = a.n_emit && n_emit >= (int)a.d.counters[TASC_CTR_MAX_NEW];
+    if (frozen) {                                          // has its tokens: emits nothing
+        if (tid < nq) {
+            if (a.emitted) a.emitted[(int64_t)b * nq + tid] = -1;
+            if (a.logprob) a.logprob[(int64_t)b * nq + tid] = 0.f;
+        }
+        if (tid == 0) {
+            if (a.accept_len) a.accept_len[b] = 0;
+            if (b == 0) atomicAdd(&a.d.counters[2], 1ull);
+        }
+        return;
+    }
     if (wave < nq) {
         const Row o = join_row<T>(a, b, wave, lane);
         if (lane == 0) s_row[wave] = o;
@@ -217,7 +238,7 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
         token = o.best;
         logp = 0.f;
     } else {
-        const double inv = inv_temperature(a, b), u = (double)a.u[((int64_t)b * nq + m) * 2 + 1];
+        const double inv = inv_temperature(a, b), u = random_of(a, b, m, 1);
         const Part* p = a.parts + ((int64_t)b * nq + m) * a.n_seg;
         const double* res = a.residual + (int64_t)b * a.n_seg;
         // which weights: 0 w, 1 w without the draft, 2 max(0, p - q); what a rejection leaves may round to nothing: then w
@@ -324,10 +345,25 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
     }
     if (tid < nq) {
         const int64_t at = (int64_t)b * nq + tid;
-        a.emitted[at] = tid < m ? s_row[tid].draft : tid == m ? token : -1;
+        if (a.emitted) a.emitted[at] = tid < m ? s_row[tid].draft : tid == m ? token : -1;
         if (a.logprob) a.logprob[at] = tid < m ? s_row[tid].draft_logp : tid == m ? logp : 0.f;
     }
-    if (tid == 0) a.accept_len[b] = m;
+    if (tid == 0 && a.accept_len) a.accept_len[b] = m;
+    if (!a.n_emit) return;
+    __syncthreads();                                       // (every wave has looked at n_emit)
+    const int at = a.d.n_tok[b];
+    // (a row without a distribution commits token 0, as the greedy acceptance does)
+    if (tid <= m) a.d.tokens[(size_t)b * a.max_len + at + tid] = tid < m ? s_row[tid].draft : max(token, 0);
+    __syncthreads();
+    if (tid != 0) return;
+    a.d.n_tok[b] = at + m + 1;
+    a.d.cached[b] += m + 1;
+    a.d.n_emit[b] = n_emit + m + 1;
+    if (n_emit + m + 1 >= (int)a.d.counters[TASC_CTR_MAX_NEW]) atomicAdd(&a.d.counters[0], 1ull);
+    if (b == 0) atomicAdd(&a.d.counters[2], 1ull);
+    atomicAdd(&a.d.counters[3], (u64)m);
+    atomicAdd(&a.d.counters[4], (u64)a.k);
+    atomicAdd(&a.d.counters[8 + m], 1ull);
 }
 
 size_t parts_bytes(int batch, int k, int n_seg) { return (size_t)batch * (k + 1) * n_seg * sizeof(Part); }
@@ -367,7 +403,17 @@ extern "C" tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype,
     }
     TASC_REQUIRE(((uintptr_t)workspace & 15) == 0, "accept_sampled: the workspace must be 16-byte aligned");
     const int n_seg = segments(vocab);
-    const SampleArgs a{logits, row_stride, k, vocab, n_seg, drafts, draft_probs, temperature, u, (Part*)workspace,
-                       (double*)((char*)workspace + parts_bytes(batch, k, n_seg)), accept_len, emitted, logprob};
+    const SampleArgs a{logits, row_stride, k, vocab, n_seg, drafts, draft_probs, temperature, u, k + 1, nullptr, (Part*)workspace,
+                       (double*)((char*)workspace + parts_bytes(batch, k, n_seg)), accept_len, emitted, logprob, TascSessDev{}, 0};
     return dtype == TASC_F32 ? enqueue<float>(a, batch, (hipStream_t)stream) : enqueue<BF16>(a, batch, (hipStream_t)stream);
+}
+
+size_t tasc_sample_logits_bytes(int32_t batch, int32_t k, int32_t vocab) { return ((size_t)batch * (k + 1) * vocab * sizeof(float) + 255) / 256 * 256; }
+
+tasc_status tasc_sample_step(const tasc_session* s, const TascVerifyTail& t, hipStream_t st) {
+    const int vocab = s->model->desc.vocab;
+    const TascSampled& p = *t.sampled;
+    const SampleArgs a{p.logits, vocab, t.k, vocab, segments(vocab), t.drafts, nullptr, p.temperature, p.u, p.n_u, s->d.n_emit, (Part*)p.parts, nullptr,
+                       t.accept_len, t.emitted, p.logprob, s->d, s->max_len};
+    return enqueue<float>(a, s->batch, st);
 }

@@ -280,10 +280,22 @@ struct TascSessDev {
     float* bias_base;    // [M_lm] its bias of unseen successors
 };
 
+// a verify step that samples: the caller's arrays and the scratch of tasc_sampled_scratch_bytes
+struct TascSampled {
+    const float* temperature; // nullable [B]
+    const float* u;           // [B, n_u, 2]
+    int64_t n_u;
+    float* logprob;           // nullable [B, k + 1]
+    float* logits;            // [B, k + 1, vocab]
+    void* parts;
+    bool operator==(const TascSampled&) const = default;
+};
+
 // one verify step outside the persistent kernels, recorded once and replayed: its launches only name buffers of the session and
 // the caller's draft / result pointers, which make the key together with what chooses the launches
 struct TascStepGraph {
     int32_t k, chains;
+    TascSampled sampled;      // all null: greedy
     bool tiled;               // the kernels it was recorded from: tiled, else type-generic
     const int32_t* drafts;
     int32_t* accept_len;
@@ -303,6 +315,7 @@ struct tasc_session {
     void* kv_pool;
     size_t kv_layer_stride;   // elements per layer
     size_t page_elems;        // elements per page (K and V)
+    int32_t kv4_pages;        // pages of a layer's 4-bit cache, 0: keys and values in the model's type, max_blocks pages a sequence
     TascSessDev d;
     u64* host_counters;       // pinned
     u32 bar_epoch;            // barriers the layer group's arrival flags (counters[32..63]) have seen so far
@@ -337,7 +350,11 @@ struct TascVerifyTail {
     int32_t* accept_len;
     int32_t* emitted;
     int32_t* trace_step;
+    const TascSampled* sampled;   // null: greedy acceptance
 };
+// sample.hip: the acceptance of a verify step that samples, from the logits that its forward left
+tasc_status tasc_sample_step(const tasc_session* s, const TascVerifyTail& tail, hipStream_t st);
+size_t tasc_sample_logits_bytes(int32_t batch, int32_t k, int32_t vocab);     // of the scratch: the logits, then the parts
 
 // library-wide options (tasc_config_set)
 // Layout of ONE copy of the small-batch kernels' activation buffers (each written once per launch): byte offsets, strides

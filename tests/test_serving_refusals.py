@@ -35,7 +35,7 @@ def cache(**kw):
     return B.Kv4CacheDesc(**dict(dict(pool=A, n_pages=4, n_kv_heads=2, head_dim=64), **kw))
 
 
-BAD_CACHES = [dict(pool=None), dict(pool=A + 128), dict(n_pages=0), dict(n_pages=1 << 27), dict(n_kv_heads=0), dict(n_kv_heads=1025), dict(head_dim=16),
+BAD_CACHES = [dict(pool=None), dict(pool=A + 64), dict(n_pages=0), dict(n_pages=1 << 27), dict(n_kv_heads=0), dict(n_kv_heads=1025), dict(head_dim=16),
               dict(head_dim=96), dict(head_dim=256)]
 
 
