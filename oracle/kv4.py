@@ -41,7 +41,8 @@ def attention(q, k, v, n_rows, scale):
     0 .. tokens - n_rows + i.  Returns (out float64 [n_rows, heads, head_dim], bound of what a computation in float32 with weights rounded
     to bf16 and a bf16 result may be off).
 
-    The bound.  A weight times its scale is rounded to bf16 (2^-8 relative) and meets the number less 7.5; the result is rounded (2^-8).
+    The bound.  A weight times its scale is rounded to bf16 (2^-8 relative) and meets the number less 7.5, the weight itself is rounded (2^-8)
+    and meets low + 7.5 scale, which is held in two bf16 parts (2^-16 of it); the result is rounded (2^-8).
     In float32 (2^-24 an operation): a score is a sum of head_dim products q (16 + c) scale and of (low - 16 scale) sum q, in at most
     head_dim + 16 operations; an error d of the scores changes each weight by a factor within exp(+-d), so the result by 2 d sum w |v|;
     exponentials are good to 2^-21 with the rounding of their arguments; and the sums over the tokens take at most tokens / 8 + 64 operations on
@@ -50,9 +51,9 @@ def attention(q, k, v, n_rows, scale):
     kv, vv = values(*k), values(*v)
     hd = q.shape[2]
     out, bound = np.zeros(q.shape), np.zeros(q.shape)
-    centred = np.abs(k_centre(v))
-    reach = np.abs(v[1])[..., None] * (39.5 + v[0]) + np.abs(v[2] + 7.5 * v[1])[..., None]
-    reach = reach.reshape(vv.shape)
+    middle = np.abs(v[2] + 7.5 * v[1])[..., None]
+    centred = (np.abs((v[0] - 7.5) * v[1][..., None]) + (1 + 2.0 ** -8) * middle).reshape(vv.shape)
+    reach = (np.abs(v[1])[..., None] * (39.5 + v[0]) + middle).reshape(vv.shape)
     for i in range(n_rows):
         n = tokens - n_rows + i + 1
         if n <= 0:
@@ -70,8 +71,3 @@ def attention(q, k, v, n_rows, scale):
             bound[i, h] *= 1.02                             # products of the above
     return out, bound
 
-
-def k_centre(v):
-    """scale * (number - 7.5), [tokens, kv_heads, head_dim]."""
-    c = (v[0] - 7.5) * v[1][..., None]
-    return c.reshape(c.shape[:-2] + (c.shape[-2] * c.shape[-1],))

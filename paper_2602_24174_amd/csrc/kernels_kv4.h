@@ -187,11 +187,12 @@ __global__ __launch_bounds__(256) void k_kv4_read(Kv4Rows a, T* __restrict__ k, 
 //                                                                                     p scale rounded to bf16 (2^-8 relative at most, like the
 //   output itself), the same rounded weights in the first two sums: a rounding then moves the output by (c - 7.5) scale, about the value's
 //   distance from the middle of its group's range, and not by c scale
-// Maxima, sums and products are fp32.  Tiles of 32 tokens at absolute positions, tile t to unit t % units (a unit: a wave of a key chunk), joined
-// in a fixed order: a row's bits depend on neither the other rows nor the length beyond its own last key.
+// The last two of these sums are rows of a 16 x 16 product of their own, whose first operand holds -23.5 and low + 7.5 scale in two bf16
+// parts.  Maxima, sums and products are fp32.  Tiles of 32 tokens at absolute positions, chunk_tiles of them a key chunk, a chunk's dealt to
+// the waves in turn, all joined in a fixed order: a row's bits depend on neither the other rows nor the length beyond its own last key.
 struct Kv4Attn {
     const uint8_t* pool;
-    int32_t n_pages, max_pages, Hkv, H, batch, rows, max_rows, chunks;
+    int32_t n_pages, max_pages, Hkv, H, batch, rows, max_rows, chunks, chunk_tiles;
     const BF16* q;
     BF16* out;
     int64_t q_stride, out_stride;      // elements from row to row
@@ -206,17 +207,25 @@ struct Kv4Attn {
     float* part_o;                     // [chunks, rows, H, HD], used if chunks > 1
     float* part_ml;                    // [chunks, rows, H, 2]
 };
-// Which units there are, and so in which order a row's keys are added: waves of a workgroup that share its pairs (1: none), key chunks
-struct Kv4Order { int wk, chunks; };
-// `pairs` (row, head) pairs of a KV head, a bound or what stands for it; split: waves share pairs in any case
-inline Kv4Order kv4_order(int64_t batch, int kv_heads, int64_t pairs, int64_t max_kv, int most_chunks, bool split) {
+// In which order a row's keys are added: waves of a workgroup that share its pairs (1: none), key chunks and their length
+struct Kv4Order { int wk, chunks, chunk_tiles; };
+// `pairs` (row, head) pairs of a KV head, a bound or what stands for it; fixed: the order must not depend on the rows of a call, only
+// on these numbers (so that waves share pairs in any case)
+inline Kv4Order kv4_order(int64_t batch, int kv_heads, int64_t pairs, int64_t max_kv, int most_chunks, bool fixed) {
     constexpr int64_t kCus = 256;
-    Kv4Order o{4, 1};
-    const int64_t heads = batch * kv_heads;
-    if (!split && pairs >= 256 && (pairs + 255) / 256 * heads >= kCus) o.wk = 1;
-    if (o.wk == 4) {
-        const int64_t wgs = heads * ((pairs + 63) / 64);
-        o.chunks = (int)std::clamp<int64_t>(std::min<int64_t>(2 * kCus / wgs, max_kv / 512), 1, most_chunks);
+    const int64_t heads = batch * kv_heads, tiles = (max_kv + 31) / 32;
+    Kv4Order o{4, 1, 1 << 26};
+    if (!fixed && pairs >= 256 && (pairs + 255) / 256 * heads >= kCus) {
+        o.wk = 1;
+        return o;
+    }
+    if (!fixed && pairs <= 16) o.wk = 8;
+    const int64_t wgs = heads * ((pairs + 63) / 64);
+    const int64_t want = std::clamp<int64_t>((2 * kCus + wgs - 1) / wgs, 1, most_chunks);
+    const int64_t per = std::max<int64_t>((tiles + want - 1) / want, 4 * o.wk);      // four tiles a wave at least
+    if (tiles > per) {
+        o.chunks = (int)((tiles + per - 1) / per);
+        o.chunk_tiles = (int)per;
     }
     return o;
 }
@@ -240,21 +249,31 @@ __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attn& a, int b) {
     return s;
 }
 
+// A tile's bytes of one lane: 32 tokens, pages p = 0, 1.  The {scale, low} words are dealt over the lanes.
 template <int HD>
-struct Kv4Tile {                       // a tile's bytes of one lane: 32 tokens, pages p = 0, 1
+struct Kv4Tile {
     uint32_t kc[2][HD / 32];
-    kv4_u32x4 ks[2][HD == 128 ? 2 : 1];
     uint32_t vc[2][4];
-    kv4_u32x4 vs[2][HD == 128 ? 2 : 1];
+    uint32_t ks, vs;
 };
+// of two groups lane 32 p + 16 g + t has those of token t, page p; of one group 16 p + t, the upper half of the wave the same again
+template <int HD>
+__device__ __forceinline__ int kv4_scale_word(int lane) { return Kv4Layout<HD>::GROUPS == 2 ? lane & 31 : lane & 15; }
+template <int HD>
+__device__ __forceinline__ int kv4_scale_page(int lane) { return Kv4Layout<HD>::GROUPS == 2 ? lane >> 5 : (lane >> 4) & 1; }
 template <int HD>
 __device__ __forceinline__ void kv4_fetch(Kv4Tile<HD>& t, const uint8_t* __restrict__ head0, const uint8_t* __restrict__ head1, int lane) {
     using L = Kv4Layout<HD>;
-    const int c = lane & 15, r = lane >> 4;
+    const uint32_t c = lane & 15, r = lane >> 4;
+    const uint32_t k_at = L::K + c * L::HALF + r * (L::HALF / 4), v_at = L::V + 4 * r * L::HALF + c * (L::HALF / 16);   // (unsigned: offsets from a scalar base)
+    {
+        const uint8_t* h = (kv4_scale_page<HD>(lane) ? head1 : head0) + 4u * kv4_scale_word<HD>(lane);
+        t.ks = *reinterpret_cast<const uint32_t*>(h + L::KS);
+        t.vs = *reinterpret_cast<const uint32_t*>(h + L::VS);
+    }
 #pragma unroll
     for (int p = 0; p < 2; ++p) {
-        const uint8_t* h = p ? head1 : head0;
-        const uint8_t* kp = h + L::K + c * L::HALF + r * (L::HALF / 4);
+        const uint8_t* kp = (p ? head1 : head0) + k_at;
         if constexpr (HD == 128) {
             const kv4_u32x4 w = *reinterpret_cast<const kv4_u32x4*>(kp);
             t.kc[p][0] = w[0]; t.kc[p][1] = w[1]; t.kc[p][2] = w[2]; t.kc[p][3] = w[3];
@@ -264,24 +283,27 @@ __device__ __forceinline__ void kv4_fetch(Kv4Tile<HD>& t, const uint8_t* __restr
         } else {
             t.kc[p][0] = *reinterpret_cast<const uint32_t*>(kp);
         }
+    }
 #pragma unroll
-        for (int g = 0; g < L::GROUPS; ++g) {
-            t.ks[p][g] = *reinterpret_cast<const kv4_u32x4*>(h + L::KS + 64 * g + 16 * r);
-            t.vs[p][g] = *reinterpret_cast<const kv4_u32x4*>(h + L::VS + 64 * g + 16 * r);
-        }
+    for (int p = 0; p < 2; ++p)
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
-            const uint8_t* vp = h + L::V + (4 * r + i) * L::HALF + c * (L::HALF / 16);
+            const uint8_t* vp = (p ? head1 : head0) + v_at + i * L::HALF;
             if constexpr (HD == 128) t.vc[p][i] = *reinterpret_cast<const uint32_t*>(vp);
             else if constexpr (HD == 64) t.vc[p][i] = *reinterpret_cast<const uint16_t*>(vp);
             else t.vc[p][i] = *vp;
         }
-    }
 }
-// bits 4 j .. 4 j + 3 of both halves of w as the bf16 pair 16 + c
-__device__ __forceinline__ uint32_t kv4_pair(uint32_t w, int j) {
-    return ((j == 0 ? w << 3 : w >> (4 * j - 3)) & 0x00780078u) | 0x41804180u;
+// Bits 4 j .. 4 j + 3 of both halves of w as the bf16 pair 16 + c.  The two constants come out of registers whose contents the compiler
+// does not know: with literals it takes an and and an or, which have room for one each.
+struct Kv4Bits { uint32_t mask, base; };
+__device__ __forceinline__ Kv4Bits kv4_bits() {
+    Kv4Bits k{0x00780078u, 0x41804180u};
+    asm("" : "+s"(k.mask));
+    asm("" : "+v"(k.base));
+    return k;
 }
+__device__ __forceinline__ uint32_t kv4_pair(const Kv4Bits& k, uint32_t w, int j) { return ((j == 0 ? w << 3 : w >> (4 * j - 3)) & k.mask) | k.base; }
 __device__ __forceinline__ float kv4_pair_sum(uint32_t p, float to) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(tasc_bf16x2, p), __builtin_bit_cast(tasc_bf16x2, 0x3F803F80u), to, false);
 }
@@ -294,43 +316,52 @@ __device__ __forceinline__ float kv4_quad_sum(float v) {
     v += __shfl_xor(v, 16);
     return v + __shfl_xor(v, 32);
 }
+// What a tile's {scale, low} words come to, in LDS of the wave's own: every lane works out the tokens that it was dealt, all lanes read
+// those of the products they hold (as each lane's own work it is 130 of 560 instructions a tile of 64 pairs).
+template <int HD>
+struct Kv4Scales {
+    static constexpr int G = Kv4Layout<HD>::GROUPS;
+    float ks[2][G][16], kb[2][G][16], vs[2][G][16];    // by page, group, token
+    uint16_t mid[5][32];                                // rows: low + 7.5 scale of the values' groups as bf16, what that leaves (as bf16), and
+                                                        // zeros; tokens in the order of the second product (4 of page 0, 4 of page 1 for each r)
+};
+constexpr float kKv4Grown = 8.f;                        // a maximum is followed once it grew by more than this power of 2
 
-// MT: tiles of 16 (row, head) pairs a wave holds.  WK: waves of a workgroup that share its pairs and take the key tiles in turn (4), or
-// 1: every wave has pairs of its own and all tiles.
+// MT: tiles of 16 (row, head) pairs a wave holds.  WK: waves of a workgroup that share its pairs and take the key tiles in turn, or 1: four
+// waves that have pairs of their own and all tiles.
 template <int HD, int MT, int WK>
-__global__ __launch_bounds__(256) void k_kv4_attention(Kv4Attn a) {
+__global__ __launch_bounds__(WK == 1 ? 256 : 64 * WK) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv4_attention(Kv4Attn a) {
     using L = Kv4Layout<HD>;
-    constexpr int G = L::GROUPS, KSTEPS = HD / 32, DT = HD / 16;
+    constexpr int G = L::GROUPS, KSTEPS = HD / 32, DT = HD / 16, WAVES = WK == 1 ? 4 : WK;
     extern __shared__ __attribute__((aligned(16))) float lds[];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, col = lane & 15, r = lane >> 4;
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, r = lane >> 4;
+    Kv4Scales<HD>& sc = reinterpret_cast<Kv4Scales<HD>*>(lds)[wave];
     const int b = blockIdx.y / a.Hkv, h = blockIdx.y % a.Hkv, share = a.H / a.Hkv;
     const int tile = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
     const Kv4Seq sq = kv4_seq(a, b);
     const int n_pairs = sq.n * share, pair0 = (WK == 1 ? tile * 4 + wave : tile) * 16 * MT;
-    if (pair0 >= n_pairs) return;                          // (WK 4: the whole workgroup)
+    if (pair0 >= n_pairs) return;                          // (WK > 1: the whole workgroup)
     const int len = min(max(sq.len, 0), a.max_pages * TASC_KV_BLOCK);
     const int pair_last = min(pair0 + 16 * MT, n_pairs) - 1;
     const int first_last = sq.len - sq.n + pair0 / share, last_last = sq.len - sq.n + pair_last / share;   // last keys of the first and the last pair
-    const int n_tiles = (min(last_last + 1, len) + 31) / 32;      // (a negative count: no key at all)
+    // (a negative count: no key at all)
+    const int n_tiles = min((min(last_last + 1, len) + 31) / 32, chunk + 1 < a.chunks ? (chunk + 1) * a.chunk_tiles : INT32_MAX);
 
-    int last[MT], row[MT], head[MT];
+    int last[MT];
     kv4_bf16x8 fq[MT][KSTEPS];
     float qsum[MT][G];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int pair = pair0 + 16 * t + col;
-        row[t] = sq.first + pair / share;
-        head[t] = h * share + pair % share;
-        const bool live = pair < n_pairs && row[t] < a.rows;
+        const int pair = pair0 + 16 * t + col, row = sq.first + pair / share, head = h * share + pair % share;
+        const bool live = pair < n_pairs && row < a.rows;
         last[t] = live ? sq.len - sq.n + pair / share : -1;
-        if (!live) row[t] = -1;
 #pragma unroll
         for (int g = 0; g < G; ++g) qsum[t][g] = 0.f;
 #pragma unroll
         for (int i = 0; i < KSTEPS; ++i) {
             const int d = HD == 128 ? (i / 2) * 64 + 16 * r + 8 * (i & 1) : HD == 64 ? 16 * r + 8 * i : 8 * r;
             kv4_u32x4 w = {0, 0, 0, 0};
-            if (live) w = *reinterpret_cast<const kv4_u32x4*>(a.q + (size_t)row[t] * a.q_stride + head[t] * HD + d);
+            if (live) w = *reinterpret_cast<const kv4_u32x4*>(a.q + (size_t)row * a.q_stride + head * HD + d);
             fq[t][i] = __builtin_bit_cast(kv4_bf16x8, w);
 #pragma unroll
             for (int e = 0; e < 4; ++e) qsum[t][HD == 128 ? i / 2 : 0] = kv4_pair_sum(w[e], qsum[t][HD == 128 ? i / 2 : 0]);
@@ -338,184 +369,208 @@ __global__ __launch_bounds__(256) void k_kv4_attention(Kv4Attn a) {
 #pragma unroll
         for (int g = 0; g < G; ++g) qsum[t][g] = kv4_quad_sum(qsum[t][g]);
     }
+    if (lane < 32) sc.mid[4][lane] = 0;
+    // rows 0 .. G - 1 of the sums' first operand: -23.5 for the group's weights
+    kv4_bf16x8 f235[G];
+#pragma unroll
+    for (int g = 0; g < G; ++g) {
+        const uint32_t w = col == g ? 0xC1BCC1BCu : 0u;     // bf16 -23.5
+        f235[g] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{w, w, w, w});
+    }
 
-    kv4_f32x4 acc[MT][DT];
-    float m[MT], l[MT], ev[MT][G];                          // ev: sum p (low + 7.5 scale) - 23.5 sum (p scale), this lane's tokens
+    kv4_f32x4 acc[MT][DT], ev[MT];                          // ev rows 0 .. G - 1 (+ 2): sum p (low + 7.5 scale) - 23.5 sum (p scale)
+    float m[MT], l[MT], lim[MT];                            // lim: what a score may be above m (nothing yet: -infinity)
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        m[t] = -__builtin_inff();
+        m[t] = 0.f;
         l[t] = 0.f;
-#pragma unroll
-        for (int g = 0; g < G; ++g) ev[t][g] = 0.f;
+        lim[t] = -__builtin_inff();
+        ev[t] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int j = 0; j < DT; ++j) acc[t][j] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
     }
+    const Kv4Bits bits = kv4_bits();
     const float scale2 = a.scale * 1.44269504088896340736f;   // scores in powers of 2
     const int32_t* const tab = a.table + (size_t)b * a.max_pages;
     const size_t page_bytes = (size_t)a.Hkv * L::HEAD;
     const uint8_t* const pool = a.pool + (size_t)h * L::HEAD;
-    const int units = WK * a.chunks, unit = WK == 1 ? chunk : chunk * WK + wave;
+    const int first_tile = chunk * a.chunk_tiles + (WK == 1 ? 0 : wave);
     // a page id outside the pool is not followed: its tokens are masked
-    auto page_of = [&](int t, int p) { const int at = 2 * t + p; return at < a.max_pages ? __builtin_amdgcn_readfirstlane(tab[at]) : -1; };
-    auto where = [&](int page) { return pool + (size_t)(page >= 0 && page < a.n_pages ? page : 0) * page_bytes; };
+    auto page_of = [&](int t, int p) {
+        const int at = 2 * t + p;
+        const int page = t < n_tiles && at < a.max_pages ? __builtin_amdgcn_readfirstlane(tab[at]) : -1;
+        return page < a.n_pages ? page : -1;
+    };
+    auto where = [&](int page) { return pool + (size_t)max(page, 0) * page_bytes; };
 
-    Kv4Tile<HD> cur, nxt;
-    int pg0 = -1, pg1 = -1;
-    if (unit < n_tiles) {
-        pg0 = page_of(unit, 0);
-        pg1 = page_of(unit, 1);
-        kv4_fetch<HD>(cur, where(pg0), where(pg1), lane);
-    }
-    for (int t = unit; t < n_tiles; t += units) {
-        const int ng0 = t + units < n_tiles ? page_of(t + units, 0) : -1, ng1 = t + units < n_tiles ? page_of(t + units, 1) : -1;
-        if (t + units < n_tiles) kv4_fetch<HD>(nxt, where(ng0), where(ng1), lane);
+    Kv4Tile<HD> cur;
+    int pg0 = page_of(first_tile, 0), pg1 = page_of(first_tile, 1);
+    if (first_tile < n_tiles) kv4_fetch<HD>(cur, where(pg0), where(pg1), lane);
+    int ng0 = page_of(first_tile + WK, 0), ng1 = page_of(first_tile + WK, 1);
+    for (int t = first_tile; t < n_tiles; t += WK) {
+        const int nn0 = page_of(t + 2 * WK, 0), nn1 = page_of(t + 2 * WK, 1);
         const int at = 32 * t;
-        const bool ok0 = pg0 >= 0 && pg0 < a.n_pages, ok1 = pg1 >= 0 && pg1 < a.n_pages;
-        const bool whole = ok0 && ok1 && at + 31 <= first_last && at + 32 <= len;
-
-        kv4_bf16x8 fk[2][KSTEPS];
-        float ksc[2][G][4], kb[2][G][4];
+        const bool whole = pg0 >= 0 && pg1 >= 0 && at + 31 <= first_last && at + 32 <= len;
+        {
+            const int p = kv4_scale_page<HD>(lane), w = kv4_scale_word<HD>(lane), tok = lane & 15, g = w / 16;
+            float ks = kv4_scale(cur.ks) * scale2, lo = kv4_low(cur.ks) * scale2, vs = kv4_scale(cur.vs), vl = kv4_low(cur.vs);
+            const bool in = whole || ((p ? pg1 : pg0) >= 0 && at + 16 * p + tok < len);   // (what lies elsewhere may be no number)
+            if (!in) ks = lo = vs = vl = 0.f;
+            float mid = __builtin_fmaf(7.5f, vs, vl);
+            if (!(fabsf(mid) < __builtin_inff())) { ks = __builtin_nanf(""); vs = mid = 0.f; }   // values that are none: who sees the token gets NaN by its score
+            const uint16_t hi = f2bf(mid), rest = f2bf(mid - bf2f(hi));
+            if (G == 2 || lane < 32) {
+                (&sc.ks[0][0][0])[lane] = ks;
+                (&sc.kb[0][0][0])[lane] = __builtin_fmaf(-16.f, ks, lo);
+                (&sc.vs[0][0][0])[lane] = vs;
+                const int slot = (tok / 4) * 8 + 4 * p + tok % 4;
+                sc.mid[g][slot] = hi;
+                sc.mid[2 + g][slot] = rest;
+                if (G == 1 && lane < 32) { sc.mid[1][lane] = 0; sc.mid[3][lane] = 0; }
+            }
+        }
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wave's LDS accesses are in order: the compiler has to keep them so)
+        __builtin_amdgcn_wave_barrier();
+        // scores of 16 tokens at a time, less the maximum so far
+        float s[MT][2][4];
 #pragma unroll
         for (int p = 0; p < 2; ++p) {
+            if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
+            kv4_bf16x8 fk[KSTEPS];
 #pragma unroll
             for (int i = 0; i < KSTEPS; ++i) {
                 const uint32_t w = cur.kc[p][i];
-                fk[p][i] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(w, 0), kv4_pair(w, 1), kv4_pair(w, 2), kv4_pair(w, 3)});
+                fk[i] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(bits, w, 0), kv4_pair(bits, w, 1), kv4_pair(bits, w, 2), kv4_pair(bits, w, 3)});
+            }
+            kv4_f32x4 ks[G], kb[G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                ks[g] = *reinterpret_cast<const kv4_f32x4*>(&sc.ks[p][g][4 * r]);
+                kb[g] = *reinterpret_cast<const kv4_f32x4*>(&sc.kb[p][g][4 * r]);
             }
 #pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    const float sc = kv4_scale(cur.ks[p][g][i]) * scale2, lo = kv4_low(cur.ks[p][g][i]) * scale2;
-                    ksc[p][g][i] = sc;
-                    kb[p][g][i] = __builtin_fmaf(-16.f, sc, lo);
-                }
-        }
-        // value numbers of lane's tokens, channel by channel: pairs of tokens in a register
-        kv4_bf16x8 fv[DT];
-        {
-            uint32_t pr[2][4];                              // [lower, upper half of the words][token pair]
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-                const uint32_t x = cur.vc[s / 2][2 * (s % 2)], y = cur.vc[s / 2][2 * (s % 2) + 1];
-                pr[0][s] = (x & 0xFFFFu) | y << 16;
-                pr[1][s] = x >> 16 | (y & 0xFFFF0000u);
-            }
-#pragma unroll
-            for (int j = 0; j < DT; ++j)
-                fv[j] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(pr[j / 4][0], j % 4), kv4_pair(pr[j / 4][1], j % 4),
-                                                                 kv4_pair(pr[j / 4][2], j % 4), kv4_pair(pr[j / 4][3], j % 4)});
-        }
-        float vsc[2][G][4], vmid[2][G][4];
-#pragma unroll
-        for (int p = 0; p < 2; ++p)
-#pragma unroll
-            for (int g = 0; g < G; ++g)
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    vsc[p][g][i] = kv4_scale(cur.vs[p][g][i]);
-                    vmid[p][g][i] = __builtin_fmaf(7.5f, vsc[p][g][i], kv4_low(cur.vs[p][g][i]));
-                }
-
-#pragma unroll
-        for (int u = 0; u < MT; ++u) {
-            float s[2][4];
-#pragma unroll
-            for (int p = 0; p < 2; ++p) {
+            for (int u = 0; u < MT; ++u) {
                 kv4_f32x4 sg[G];
 #pragma unroll
                 for (int g = 0; g < G; ++g) sg[g] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
                 for (int i = 0; i < KSTEPS; ++i) {
-                    constexpr int per = G == 2 ? KSTEPS / 2 : KSTEPS;
-                    sg[i / per] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fk[p][i], fq[u][i], sg[i / per], 0, 0, 0);
+                    constexpr int per = KSTEPS / G;
+                    sg[i / per] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fk[i], fq[u][i], sg[i / per], 0, 0, 0);
                 }
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    float v = kb[p][0][i] * qsum[u][0];
+                    float v = -m[u];
 #pragma unroll
-                    for (int g = 0; g < G; ++g) {
-                        if (g > 0) v = __builtin_fmaf(kb[p][g][i], qsum[u][g], v);
-                        v = __builtin_fmaf(ksc[p][g][i], sg[g][i], v);
-                    }
-                    s[p][i] = v;
+                    for (int g = 0; g < G; ++g) v = __builtin_fmaf(kb[g][i], qsum[u][g], v);
+#pragma unroll
+                    for (int g = 0; g < G; ++g) v = __builtin_fmaf(ks[g][i], sg[g][i], v);
+                    s[u][p][i] = v;
                 }
             }
-            uint32_t keep = 0xFFu;                          // bit 4 p + i: the token counts
+        }
+        if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
+        // the lane's tokens' value numbers, channel by channel: pairs of tokens in a register
+        kv4_bf16x8 fv[DT];
+        {
+            uint32_t pr[2][4];                              // [lower, upper half of the words][token pair]
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const uint32_t x = cur.vc[e / 2][2 * (e % 2)], y = cur.vc[e / 2][2 * (e % 2) + 1];
+                pr[0][e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+                pr[1][e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+            }
+#pragma unroll
+            for (int j = 0; j < DT; ++j)
+                fv[j] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(bits, pr[j / 4][0], j % 4), kv4_pair(bits, pr[j / 4][1], j % 4),
+                                                                 kv4_pair(bits, pr[j / 4][2], j % 4), kv4_pair(bits, pr[j / 4][3], j % 4)});
+        }
+        kv4_fetch<HD>(cur, where(ng0), where(ng1), lane);      // the next tile, under the second product (behind the last one: page 0, not used)
+        const kv4_bf16x8 fmid = *reinterpret_cast<const kv4_bf16x8*>(&sc.mid[min(col, 4)][8 * r]);
+        kv4_f32x4 vs[2][G];
+#pragma unroll
+        for (int p = 0; p < 2; ++p)
+#pragma unroll
+            for (int g = 0; g < G; ++g) vs[p][g] = *reinterpret_cast<const kv4_f32x4*>(&sc.vs[p][g][4 * r]);
+
+#pragma unroll
+        for (int u = 0; u < MT; ++u) {
+            if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
             if (!whole) {
-                keep = 0;
 #pragma unroll
                 for (int p = 0; p < 2; ++p)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int pos = at + 16 * p + 4 * r + i;
-                        const bool in = (p ? ok1 : ok0) && pos <= last[u] && pos < len;
-                        keep |= (in ? 1u : 0u) << (4 * p + i);
-                        if (!in) s[p][i] = -__builtin_inff();
+                        if ((p ? pg1 : pg0) < 0 || pos > last[u] || pos >= len) s[u][p][i] = -__builtin_inff();
                     }
             }
-            float top = fmaxf(fmaxf(fmaxf(s[0][0], s[0][1]), fmaxf(s[0][2], s[0][3])), fmaxf(fmaxf(s[1][0], s[1][1]), fmaxf(s[1][2], s[1][3])));
-            top = fmaxf(kv4_quad_max(top), m[u]);
-            if (__any(top > m[u])) {
-                const float f = top == m[u] ? 1.f : __builtin_amdgcn_exp2f(m[u] - top);   // (0 at the first key; a pair without one keeps -inf)
-                l[u] *= f;
+            float top = fmaxf(fmaxf(fmaxf(s[u][0][0], s[u][0][1]), fmaxf(s[u][0][2], s[u][0][3])), fmaxf(fmaxf(s[u][1][0], s[u][1][1]), fmaxf(s[u][1][2], s[u][1][3])));
+            if (__any(top > lim[u])) {
+                top = kv4_quad_max(top);
+                if (top > lim[u]) {                         // (the four lanes of a pair alike)
+                    const float f = __builtin_amdgcn_exp2f(-top);
+                    l[u] *= l[u] > 0.f ? f : 1.f;           // (zeros so far: f may be infinite)
+                    if (lim[u] == kKv4Grown) {
+                        ev[u] *= f;
 #pragma unroll
-                for (int g = 0; g < G; ++g) ev[u][g] *= f;
+                        for (int j = 0; j < DT; ++j) acc[u][j] *= f;
+                    }
+                    m[u] += top;
+                    lim[u] = kKv4Grown;
 #pragma unroll
-                for (int j = 0; j < DT; ++j) acc[u][j] *= f;
-                m[u] = top;
+                    for (int p = 0; p < 2; ++p)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) s[u][p][i] -= top;
+                }
             }
-            const float base = m[u] == -__builtin_inff() ? 0.f : m[u];
             float pw[2][4];
 #pragma unroll
             for (int p = 0; p < 2; ++p)
 #pragma unroll
                 for (int i = 0; i < 4; ++i) {
-                    pw[p][i] = __builtin_amdgcn_exp2f(s[p][i] - base);
+                    pw[p][i] = __builtin_amdgcn_exp2f(s[u][p][i]);
                     l[u] += pw[p][i];
                 }
+            const kv4_u32x4 pq = {f2bf_pair(pw[0][0], pw[0][1]), f2bf_pair(pw[0][2], pw[0][3]), f2bf_pair(pw[1][0], pw[1][1]), f2bf_pair(pw[1][2], pw[1][3])};
+            ev[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fmid, __builtin_bit_cast(kv4_bf16x8, pq), ev[u], 0, 0, 0);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float ps[2][4];
 #pragma unroll
                 for (int p = 0; p < 2; ++p)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        ps[p][i] = pw[p][i] * vsc[p][g][i];
-                        float mid = pw[p][i] * vmid[p][g][i];
-                        if (!whole && !(keep >> (4 * p + i) & 1)) { ps[p][i] = 0.f; mid = 0.f; }    // (what lies there may be no number)
-                        ev[u][g] += mid;
-                    }
+                    for (int i = 0; i < 4; ++i) ps[p][i] = pw[p][i] * vs[p][g][i];
                 const kv4_u32x4 w = {f2bf_pair(ps[0][0], ps[0][1]), f2bf_pair(ps[0][2], ps[0][3]), f2bf_pair(ps[1][0], ps[1][1]), f2bf_pair(ps[1][2], ps[1][3])};
-                float rounded = 0.f;
-#pragma unroll
-                for (int e = 0; e < 4; ++e) rounded = kv4_pair_sum(w[e], rounded);
-                ev[u][g] = __builtin_fmaf(-23.5f, rounded, ev[u][g]);
                 const kv4_bf16x8 fp = __builtin_bit_cast(kv4_bf16x8, w);
+                ev[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f235[g], fp, ev[u], 0, 0, 0);
 #pragma unroll
                 for (int j = g * (DT / G); j < (g + 1) * (DT / G); ++j) acc[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv[j], fp, acc[u][j], 0, 0, 0);
             }
         }
-        cur = nxt;
         pg0 = ng0;
         pg1 = ng1;
+        ng0 = nn0;
+        ng1 = nn1;
     }
 
     // the four lanes' sums, and the channels' share of ev
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         l[t] = kv4_quad_sum(l[t]);
+        if (lim[t] != kKv4Grown) m[t] = -__builtin_inff();   // no key
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            const float e = kv4_quad_sum(ev[t][g]);
+            const float e = __shfl(ev[t][g] + ev[t][2 + g], col);
 #pragma unroll
             for (int j = g * (DT / G); j < (g + 1) * (DT / G); ++j) acc[t][j] += e;
         }
     }
     if constexpr (WK > 1) {
-        // the waves' results, (0 + 2) + (1 + 3): maxima first, then sums in units of the common one
-        float* const sm = lds;                              // [4][16 MT]
-        float* const sx = lds + 4 * 16 * MT;                // [2][MT * (DT * 4 + 1)][64]
+        // the waves' results joined pairwise, (0 + 4) + (2 + 6) and so on: maxima first, then sums in units of the common one
+        float* const sm = lds;                              // [WAVES][16 MT]
+        float* const sx = lds + WAVES * 16 * MT;            // [WAVES / 2][MT * (DT * 4 + 1)][64]
+        __syncthreads();                                    // (the scales are read)
         if (r == 0)
 #pragma unroll
             for (int t = 0; t < MT; ++t) sm[wave * 16 * MT + 16 * t + col] = m[t];
@@ -524,7 +579,7 @@ __global__ __launch_bounds__(256) void k_kv4_attention(Kv4Attn a) {
         for (int t = 0; t < MT; ++t) {
             float top = m[t];
 #pragma unroll
-            for (int w = 0; w < 4; ++w) top = fmaxf(top, sm[w * 16 * MT + 16 * t + col]);
+            for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm[w * 16 * MT + 16 * t + col]);
             const float f = m[t] == top ? 1.f : __builtin_amdgcn_exp2f(m[t] - top);
             m[t] = top;
             l[t] *= f;
@@ -533,7 +588,7 @@ __global__ __launch_bounds__(256) void k_kv4_attention(Kv4Attn a) {
         }
         constexpr int SPAN = MT * (DT * 4 + 1);
 #pragma unroll
-        for (int half = 2; half >= 1; half /= 2) {
+        for (int half = WAVES / 2; half >= 1; half /= 2) {
             if (wave >= half && wave < 2 * half) {
                 float* to = sx + (size_t)(wave - half) * SPAN * 64 + lane;
 #pragma unroll
@@ -563,11 +618,12 @@ __global__ __launch_bounds__(256) void k_kv4_attention(Kv4Attn a) {
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        if (row[t] < 0) continue;
+        const int pair = pair0 + 16 * t + col, row = sq.first + pair / share, head = h * share + pair % share;
+        if (pair >= n_pairs || row >= a.rows) continue;
         // lane's channels: of tile j row 4 r + i, channel (HD 128, 64) 64 (j / 4) + 16 r + 4 i + j % 4, (32) 8 r + 2 i + j
         if (a.chunks == 1) {
             const float inv = l[t] > 0.f ? 1.f / l[t] : l[t];          // a pair without keys gives zeros (a NaN stays one)
-            uint16_t* o = reinterpret_cast<uint16_t*>(a.out + (size_t)row[t] * a.out_stride + head[t] * HD);
+            uint16_t* o = reinterpret_cast<uint16_t*>(a.out + (size_t)row * a.out_stride + head * HD);
             if constexpr (HD == 32) {
 #pragma unroll
                 for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(o + 8 * r + 2 * i) = f2bf_pair(acc[t][0][i] * inv, acc[t][1][i] * inv);
@@ -580,7 +636,7 @@ __global__ __launch_bounds__(256) void k_kv4_attention(Kv4Attn a) {
                             kv4_u32x2{f2bf_pair(acc[t][4 * g][i] * inv, acc[t][4 * g + 1][i] * inv), f2bf_pair(acc[t][4 * g + 2][i] * inv, acc[t][4 * g + 3][i] * inv)};
             }
         } else {
-            const size_t at = ((size_t)chunk * a.rows + row[t]) * a.H + head[t];
+            const size_t at = ((size_t)chunk * a.rows + row) * a.H + head;
             float* o = a.part_o + at * HD;
             if constexpr (HD == 32) {
 #pragma unroll
@@ -598,7 +654,10 @@ __global__ __launch_bounds__(256) void k_kv4_attention(Kv4Attn a) {
     }
 }
 template <int HD, int MT, int WK>
-constexpr int kv4_attention_lds() { return WK == 1 ? 0 : (4 * 16 * MT + 2 * MT * (HD / 4 + 1) * 64) * 4; }
+constexpr int kv4_attention_lds() {
+    const int scales = (WK == 1 ? 4 : WK) * (int)sizeof(Kv4Scales<HD>), join = WK == 1 ? 0 : (WK * 16 * MT + WK / 2 * MT * (HD / 4 + 1) * 64) * 4;
+    return scales > join ? scales : join;
+}
 
 // The key chunks' results in chunk order; a workgroup per (sequence, row), a thread per 4 channels of a head at a time.
 template <int HD>

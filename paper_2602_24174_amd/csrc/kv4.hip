@@ -19,16 +19,20 @@ tasc_status attend(const Kv4Attn& a, int tiles, hipStream_t st) {
             ready[dev & 15] = true;
         }
     }
-    k_kv4_attention<HD, MT, WK><<<dim3((unsigned)(tiles * a.chunks), (unsigned)(a.batch * a.Hkv)), dim3(256), lds, st>>>(a);
+    k_kv4_attention<HD, MT, WK><<<dim3((unsigned)(tiles * a.chunks), (unsigned)(a.batch * a.Hkv)), dim3(WK == 1 ? 256 : 64 * WK), lds, st>>>(a);
     return TASC_OK;
 }
 template <int HD>
 tasc_status attend_hd(const Kv4Attn& a, int wk, hipStream_t st) {
     const int64_t pairs = (int64_t)a.max_rows * (a.H / a.Hkv);
+    constexpr int MOST = HD == 128 ? 2 : 4;                // tiles of pairs that fit a wave's registers
     auto tiles = [&](int per) { return (int)((pairs + per - 1) / per); };
     tasc_status rc;
-    if (wk == 1) rc = attend<HD, 4, 1>(a, tiles(256), st);
-    else rc = pairs <= 16 ? attend<HD, 1, 4>(a, tiles(16), st) : pairs <= 32 ? attend<HD, 2, 4>(a, tiles(32), st) : attend<HD, 4, 4>(a, tiles(64), st);
+    if (wk == 1) rc = attend<HD, MOST, 1>(a, tiles(64 * MOST), st);
+    else if (wk == 8) rc = attend<HD, 1, 8>(a, tiles(16), st);
+    else if (pairs <= 16) rc = attend<HD, 1, 4>(a, tiles(16), st);
+    else if (MOST == 2 || pairs <= 32) rc = attend<HD, 2, 4>(a, tiles(32), st);
+    else rc = attend<HD, MOST, 4>(a, tiles(16 * MOST), st);
     if (rc != TASC_OK) return rc;
     if (a.chunks > 1) k_kv4_merge<HD><<<dim3((unsigned)a.max_rows, (unsigned)a.batch), dim3(256), 0, st>>>(a);
     TASC_LAUNCH_CHECK();
@@ -57,6 +61,7 @@ constexpr int kMostChunks = 64;
 
 tasc_status tasc_kv4_attend(Kv4Attn a, int hd, const Kv4Order& o, hipStream_t st) {
     a.chunks = o.chunks;
+    a.chunk_tiles = o.chunk_tiles;
     return hd == 128 ? attend_hd<128>(a, o.wk, st) : hd == 64 ? attend_hd<64>(a, o.wk, st) : attend_hd<32>(a, o.wk, st);
 }
 
