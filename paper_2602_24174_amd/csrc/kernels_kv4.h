@@ -192,7 +192,7 @@ __global__ __launch_bounds__(256) void k_kv4_read(Kv4Rows a, T* __restrict__ k, 
 // the waves in turn, all joined in a fixed order: a row's bits depend on neither the other rows nor the length beyond its own last key.
 struct Kv4Attn {
     const uint8_t* pool;
-    int32_t n_pages, max_pages, Hkv, H, batch, rows, max_rows, chunks, chunk_tiles;
+    int32_t n_pages, max_pages, Hkv, H, batch, rows, max_rows, chunks, chunk_tiles, row_waves;
     const BF16* q;
     BF16* out;
     int64_t q_stride, out_stride;      // elements from row to row
@@ -207,22 +207,22 @@ struct Kv4Attn {
     float* part_o;                     // [chunks, rows, H, HD], used if chunks > 1
     float* part_ml;                    // [chunks, rows, H, 2]
 };
-// In which order a row's keys are added: waves of a workgroup that share its pairs (1: none), key chunks and their length
-struct Kv4Order { int wk, chunks, chunk_tiles; };
+// In which order a row's keys are added: waves that share pairs, key chunks and their length in tiles
+struct Kv4Order { int kw, chunks, chunk_tiles; };
 // `pairs` (row, head) pairs of a KV head, a bound or what stands for it; fixed: the order must not depend on the rows of a call, only
-// on these numbers (so that waves share pairs in any case)
+// on these numbers
 inline Kv4Order kv4_order(int64_t batch, int kv_heads, int64_t pairs, int64_t max_kv, int most_chunks, bool fixed) {
-    constexpr int64_t kCus = 256;
+    constexpr int64_t kWaves = 2048;                        // two a SIMD
     const int64_t heads = batch * kv_heads, tiles = (max_kv + 31) / 32;
-    Kv4Order o{4, 1, 1 << 26};
-    if (!fixed && pairs >= 256 && (pairs + 255) / 256 * heads >= kCus) {
-        o.wk = 1;
+    Kv4Order o{2, 1, 1 << 26};
+    const int64_t row_waves = (pairs + 31) / 32;
+    if (!fixed && row_waves * heads >= kWaves) {
+        o.kw = 1;
         return o;
     }
-    if (!fixed && pairs <= 16) o.wk = 8;
-    const int64_t wgs = heads * ((pairs + 63) / 64);
-    const int64_t want = std::clamp<int64_t>((2 * kCus + wgs - 1) / wgs, 1, most_chunks);
-    const int64_t per = std::max<int64_t>((tiles + want - 1) / want, 4 * o.wk);      // four tiles a wave at least
+    if (!fixed && pairs <= 16) o.kw = heads * 8 <= kWaves ? 8 : 4;
+    const int64_t want = std::clamp<int64_t>((kWaves + heads * row_waves * o.kw - 1) / (heads * row_waves * o.kw), 1, most_chunks);
+    const int64_t per = std::max<int64_t>((tiles + want - 1) / want, 4 * o.kw);      // four tiles a wave at least
     if (tiles > per) {
         o.chunks = (int)((tiles + per - 1) / per);
         o.chunk_tiles = (int)per;
@@ -322,60 +322,92 @@ template <int HD>
 struct Kv4Scales {
     static constexpr int G = Kv4Layout<HD>::GROUPS;
     float ks[2][G][16], kb[2][G][16], vs[2][G][16];    // by page, group, token
-    uint16_t mid[5][32];                                // rows: low + 7.5 scale of the values' groups as bf16, what that leaves (as bf16), and
-                                                        // zeros; tokens in the order of the second product (4 of page 0, 4 of page 1 for each r)
+    uint16_t mid[4][32];                                // low + 7.5 scale of the values' groups as bf16, and what that leaves, as bf16; tokens in
+                                                        // the order of the second product (4 of page 0, 4 of page 1 for each r)
+    uint16_t fixed[2][32];                              // zeros; -23.5
 };
 constexpr float kKv4Grown = 8.f;                        // a maximum is followed once it grew by more than this power of 2
 
-// MT: tiles of 16 (row, head) pairs a wave holds.  WK: waves of a workgroup that share its pairs and take the key tiles in turn, or 1: four
-// waves that have pairs of their own and all tiles.
-template <int HD, int MT, int WK>
-__global__ __launch_bounds__(WK == 1 ? 256 : 64 * WK) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv4_attention(Kv4Attn a) {
+// MT: tiles of 16 (row, head) pairs a wave holds.  KW: waves that share their pairs and take a key chunk's tiles in turn; a workgroup has a.row_waves
+// times as many, each KW of them with pairs of their own (over the same keys, which they so find in the L1 cache).
+template <int HD, int MT, int KW>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv4_attention(Kv4Attn a) {
     using L = Kv4Layout<HD>;
-    constexpr int G = L::GROUPS, KSTEPS = HD / 32, DT = HD / 16, WAVES = WK == 1 ? 4 : WK;
+    constexpr int G = L::GROUPS, KSTEPS = HD / 32, DT = HD / 16;
+    constexpr int AHEAD = MT * HD >= 256 ? 1 : 2;           // tiles under way: as many as the registers of two waves a SIMD hold beside the sums
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, r = lane >> 4;
+    // (the last waves have the fewest pairs; every second workgroup of a compute unit takes them the other way round, or the same SIMDs would
+    // have the full ones every time)
+    const int kw = wave % KW, turned = (blockIdx.y * gridDim.x + blockIdx.x) / 256 % 2, rw = turned ? a.row_waves - 1 - wave / KW : wave / KW;
     Kv4Scales<HD>& sc = reinterpret_cast<Kv4Scales<HD>*>(lds)[wave];
     const int b = blockIdx.y / a.Hkv, h = blockIdx.y % a.Hkv, share = a.H / a.Hkv;
     const int tile = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
     const Kv4Seq sq = kv4_seq(a, b);
-    const int n_pairs = sq.n * share, pair0 = (WK == 1 ? tile * 4 + wave : tile) * 16 * MT;
-    if (pair0 >= n_pairs) return;                          // (WK > 1: the whole workgroup)
+    const int n_pairs = sq.n * share, wg_pair = tile * a.row_waves * 16 * MT, pair0 = wg_pair + rw * 16 * MT;
+    if (wg_pair >= n_pairs) return;                        // (the whole workgroup; a wave without pairs among them goes on without keys)
     const int len = min(max(sq.len, 0), a.max_pages * TASC_KV_BLOCK);
     const int pair_last = min(pair0 + 16 * MT, n_pairs) - 1;
     const int first_last = sq.len - sq.n + pair0 / share, last_last = sq.len - sq.n + pair_last / share;   // last keys of the first and the last pair
     // (a negative count: no key at all)
-    const int n_tiles = min((min(last_last + 1, len) + 31) / 32, chunk + 1 < a.chunks ? (chunk + 1) * a.chunk_tiles : INT32_MAX);
+    int n_tiles = min((min(last_last + 1, len) + 31) / 32, chunk + 1 < a.chunks ? (chunk + 1) * a.chunk_tiles : INT32_MAX);
+    if (pair0 >= n_pairs) n_tiles = 0;
+    const int live = (pair_last - pair0) / 16 + 1;         // tiles of pairs that hold any
+
+    const size_t page_bytes = (size_t)a.Hkv * L::HEAD;
+    const uint8_t* const pool = a.pool + (size_t)h * L::HEAD;
+    const int first_tile = chunk * a.chunk_tiles + kw;
+    // The ids of 32 tiles' pages, two lanes a tile: a look at the table is then no memory access.  -1: behind the last tile, or
+    // outside the pool, where an id is not followed and its tokens are masked.
+    auto page_ids = [&](int from) {
+        const int t = from + (lane >> 1) * KW, at = 2 * t + (lane & 1);
+        int page = -1;
+        if (t < n_tiles && at < a.max_pages) page = a.table[(size_t)b * a.max_pages + at];
+        return page < a.n_pages ? page : -1;
+    };
+    int ids = page_ids(first_tile), ids_next = 0;
+    auto where = [&](int page) { return pool + (size_t)max(page, 0) * page_bytes; };
 
     int last[MT];
+    kv4_u32x4 rq[MT][KSTEPS];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        const int pair = pair0 + 16 * t + col, row = sq.first + pair / share, head = h * share + pair % share;
+        const bool there = pair < n_pairs && row < a.rows;
+        last[t] = there ? sq.len - sq.n + pair / share : -1;
+#pragma unroll
+        for (int i = 0; i < KSTEPS; ++i) {
+            const int d = HD == 128 ? (i / 2) * 64 + 16 * r + 8 * (i & 1) : HD == 64 ? 16 * r + 8 * i : 8 * r;
+            rq[t][i] = kv4_u32x4{0, 0, 0, 0};
+            if (there) rq[t][i] = *reinterpret_cast<const kv4_u32x4*>(a.q + (size_t)row * a.q_stride + head * HD + d);
+        }
+    }
+    // the first two tiles are under way while the queries are looked at
+    Kv4Tile<HD> tile_a, tile_b;
+    int pa0 = __builtin_amdgcn_readlane(ids, 0), pa1 = __builtin_amdgcn_readlane(ids, 1);
+    int pb0 = __builtin_amdgcn_readlane(ids, 2), pb1 = __builtin_amdgcn_readlane(ids, 3);
+    kv4_fetch<HD>(tile_a, where(pa0), where(pa1), lane);   // (without tiles: page 0, not used)
+    if constexpr (AHEAD == 2) kv4_fetch<HD>(tile_b, where(pb0), where(pb1), lane);
     kv4_bf16x8 fq[MT][KSTEPS];
     float qsum[MT][G];
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int pair = pair0 + 16 * t + col, row = sq.first + pair / share, head = h * share + pair % share;
-        const bool live = pair < n_pairs && row < a.rows;
-        last[t] = live ? sq.len - sq.n + pair / share : -1;
 #pragma unroll
         for (int g = 0; g < G; ++g) qsum[t][g] = 0.f;
 #pragma unroll
         for (int i = 0; i < KSTEPS; ++i) {
-            const int d = HD == 128 ? (i / 2) * 64 + 16 * r + 8 * (i & 1) : HD == 64 ? 16 * r + 8 * i : 8 * r;
-            kv4_u32x4 w = {0, 0, 0, 0};
-            if (live) w = *reinterpret_cast<const kv4_u32x4*>(a.q + (size_t)row * a.q_stride + head * HD + d);
-            fq[t][i] = __builtin_bit_cast(kv4_bf16x8, w);
+            fq[t][i] = __builtin_bit_cast(kv4_bf16x8, rq[t][i]);
 #pragma unroll
-            for (int e = 0; e < 4; ++e) qsum[t][HD == 128 ? i / 2 : 0] = kv4_pair_sum(w[e], qsum[t][HD == 128 ? i / 2 : 0]);
+            for (int e = 0; e < 4; ++e) qsum[t][HD == 128 ? i / 2 : 0] = kv4_pair_sum(rq[t][i][e], qsum[t][HD == 128 ? i / 2 : 0]);
         }
 #pragma unroll
         for (int g = 0; g < G; ++g) qsum[t][g] = kv4_quad_sum(qsum[t][g]);
     }
-    if (lane < 32) sc.mid[4][lane] = 0;
-    // rows 0 .. G - 1 of the sums' first operand: -23.5 for the group's weights
-    kv4_bf16x8 f235[G];
-#pragma unroll
-    for (int g = 0; g < G; ++g) {
-        const uint32_t w = col == g ? 0xC1BCC1BCu : 0u;     // bf16 -23.5
-        f235[g] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{w, w, w, w});
+    // rows of the sums' first operands that do not change: zeros, and -23.5 for a group's weights in the group's row
+    if (lane < 32) {
+        sc.fixed[0][lane] = 0;
+        sc.fixed[1][lane] = 0xC1BC;                         // bf16 -23.5
+        if (G == 1) sc.mid[1][lane] = sc.mid[3][lane] = 0;
     }
 
     kv4_f32x4 acc[MT][DT], ev[MT];                          // ev rows 0 .. G - 1 (+ 2): sum p (low + 7.5 scale) - 23.5 sum (p scale)
@@ -391,24 +423,9 @@ __global__ __launch_bounds__(WK == 1 ? 256 : 64 * WK) __attribute__((amdgpu_wave
     }
     const Kv4Bits bits = kv4_bits();
     const float scale2 = a.scale * 1.44269504088896340736f;   // scores in powers of 2
-    const int32_t* const tab = a.table + (size_t)b * a.max_pages;
-    const size_t page_bytes = (size_t)a.Hkv * L::HEAD;
-    const uint8_t* const pool = a.pool + (size_t)h * L::HEAD;
-    const int first_tile = chunk * a.chunk_tiles + (WK == 1 ? 0 : wave);
-    // a page id outside the pool is not followed: its tokens are masked
-    auto page_of = [&](int t, int p) {
-        const int at = 2 * t + p;
-        const int page = t < n_tiles && at < a.max_pages ? __builtin_amdgcn_readfirstlane(tab[at]) : -1;
-        return page < a.n_pages ? page : -1;
-    };
-    auto where = [&](int page) { return pool + (size_t)max(page, 0) * page_bytes; };
 
-    Kv4Tile<HD> cur;
-    int pg0 = page_of(first_tile, 0), pg1 = page_of(first_tile, 1);
-    if (first_tile < n_tiles) kv4_fetch<HD>(cur, where(pg0), where(pg1), lane);
-    int ng0 = page_of(first_tile + WK, 0), ng1 = page_of(first_tile + WK, 1);
-    for (int t = first_tile; t < n_tiles; t += WK) {
-        const int nn0 = page_of(t + 2 * WK, 0), nn1 = page_of(t + 2 * WK, 1);
+    // one tile out of `cur`, whose registers then take the tile of the pages that come next
+    auto work = [&](Kv4Tile<HD>& cur, int t, int pg0, int pg1, int ng0, int ng1) __attribute__((always_inline)) {
         const int at = 32 * t;
         const bool whole = pg0 >= 0 && pg1 >= 0 && at + 31 <= first_last && at + 32 <= len;
         {
@@ -426,7 +443,6 @@ __global__ __launch_bounds__(WK == 1 ? 256 : 64 * WK) __attribute__((amdgpu_wave
                 const int slot = (tok / 4) * 8 + 4 * p + tok % 4;
                 sc.mid[g][slot] = hi;
                 sc.mid[2 + g][slot] = rest;
-                if (G == 1 && lane < 32) { sc.mid[1][lane] = 0; sc.mid[3][lane] = 0; }
             }
         }
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wave's LDS accesses are in order: the compiler has to keep them so)
@@ -450,6 +466,7 @@ __global__ __launch_bounds__(WK == 1 ? 256 : 64 * WK) __attribute__((amdgpu_wave
             }
 #pragma unroll
             for (int u = 0; u < MT; ++u) {
+                if (u >= live) break;
                 kv4_f32x4 sg[G];
 #pragma unroll
                 for (int g = 0; g < G; ++g) sg[g] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -471,30 +488,33 @@ __global__ __launch_bounds__(WK == 1 ? 256 : 64 * WK) __attribute__((amdgpu_wave
         }
         if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
         // the lane's tokens' value numbers, channel by channel: pairs of tokens in a register
-        kv4_bf16x8 fv[DT];
-        {
-            uint32_t pr[2][4];                              // [lower, upper half of the words][token pair]
+        uint32_t pr[HD == 128 ? 2 : 1][4];                  // [lower, upper half of the words][token pair]
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t x = cur.vc[e / 2][2 * (e % 2)], y = cur.vc[e / 2][2 * (e % 2) + 1];
-                pr[0][e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-                pr[1][e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
-            }
-#pragma unroll
-            for (int j = 0; j < DT; ++j)
-                fv[j] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(bits, pr[j / 4][0], j % 4), kv4_pair(bits, pr[j / 4][1], j % 4),
-                                                                 kv4_pair(bits, pr[j / 4][2], j % 4), kv4_pair(bits, pr[j / 4][3], j % 4)});
+        for (int e = 0; e < 4; ++e) {
+            const uint32_t x = cur.vc[e / 2][2 * (e % 2)], y = cur.vc[e / 2][2 * (e % 2) + 1];
+            pr[0][e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+            if constexpr (HD == 128) pr[1][e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
         }
-        kv4_fetch<HD>(cur, where(ng0), where(ng1), lane);      // the next tile, under the second product (behind the last one: page 0, not used)
-        const kv4_bf16x8 fmid = *reinterpret_cast<const kv4_bf16x8*>(&sc.mid[min(col, 4)][8 * r]);
+        if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
+        kv4_fetch<HD>(cur, where(ng0), where(ng1), lane);
+        kv4_bf16x8 fv[DT];
+#pragma unroll
+        for (int j = 0; j < DT; ++j)
+            fv[j] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(bits, pr[j / 4][0], j % 4), kv4_pair(bits, pr[j / 4][1], j % 4),
+                                                             kv4_pair(bits, pr[j / 4][2], j % 4), kv4_pair(bits, pr[j / 4][3], j % 4)});
+        const kv4_bf16x8 fmid = *reinterpret_cast<const kv4_bf16x8*>(col < 4 ? &sc.mid[col][8 * r] : &sc.fixed[0][8 * r]);
+        kv4_bf16x8 fsum[G];
         kv4_f32x4 vs[2][G];
 #pragma unroll
-        for (int p = 0; p < 2; ++p)
+        for (int g = 0; g < G; ++g) {
+            fsum[g] = *reinterpret_cast<const kv4_bf16x8*>(&sc.fixed[col == g][8 * r]);
 #pragma unroll
-            for (int g = 0; g < G; ++g) vs[p][g] = *reinterpret_cast<const kv4_f32x4*>(&sc.vs[p][g][4 * r]);
+            for (int p = 0; p < 2; ++p) vs[p][g] = *reinterpret_cast<const kv4_f32x4*>(&sc.vs[p][g][4 * r]);
+        }
 
 #pragma unroll
         for (int u = 0; u < MT; ++u) {
+            if (u >= live) break;
             if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
             if (!whole) {
 #pragma unroll
@@ -543,15 +563,27 @@ __global__ __launch_bounds__(WK == 1 ? 256 : 64 * WK) __attribute__((amdgpu_wave
                     for (int i = 0; i < 4; ++i) ps[p][i] = pw[p][i] * vs[p][g][i];
                 const kv4_u32x4 w = {f2bf_pair(ps[0][0], ps[0][1]), f2bf_pair(ps[0][2], ps[0][3]), f2bf_pair(ps[1][0], ps[1][1]), f2bf_pair(ps[1][2], ps[1][3])};
                 const kv4_bf16x8 fp = __builtin_bit_cast(kv4_bf16x8, w);
-                ev[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(f235[g], fp, ev[u], 0, 0, 0);
+                ev[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fsum[g], fp, ev[u], 0, 0, 0);
 #pragma unroll
                 for (int j = g * (DT / G); j < (g + 1) * (DT / G); ++j) acc[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv[j], fp, acc[u][j], 0, 0, 0);
             }
         }
-        pg0 = ng0;
-        pg1 = ng1;
-        ng0 = nn0;
-        ng1 = nn1;
+    };
+    int k = 2 * AHEAD;                                      // place of the next tile's ids
+    for (int t = first_tile; t < n_tiles; t += AHEAD * KW) {
+        if (k == 2 * AHEAD) ids_next = page_ids(t + 32 * KW);   // (32 tiles ahead)
+        if (k == 64) { ids = ids_next; k = 0; }
+        const int na0 = __builtin_amdgcn_readlane(ids, k), na1 = __builtin_amdgcn_readlane(ids, k + 1);
+        if constexpr (AHEAD == 2) {
+            const int nb0 = __builtin_amdgcn_readlane(ids, k + 2), nb1 = __builtin_amdgcn_readlane(ids, k + 3);
+            work(tile_a, t, pa0, pa1, na0, na1);
+            if (t + KW < n_tiles) work(tile_b, t + KW, pb0, pb1, nb0, nb1);
+            pb0 = nb0; pb1 = nb1;
+        } else {
+            work(tile_a, t, pa0, pa1, na0, na1);
+        }
+        pa0 = na0; pa1 = na1;
+        k += 2 * AHEAD;
     }
 
     // the four lanes' sums, and the channels' share of ev
@@ -566,119 +598,108 @@ __global__ __launch_bounds__(WK == 1 ? 256 : 64 * WK) __attribute__((amdgpu_wave
             for (int j = g * (DT / G); j < (g + 1) * (DT / G); ++j) acc[t][j] += e;
         }
     }
-    if constexpr (WK > 1) {
-        // the waves' results joined pairwise, (0 + 4) + (2 + 6) and so on: maxima first, then sums in units of the common one
-        float* const sm = lds;                              // [WAVES][16 MT]
-        float* const sx = lds + WAVES * 16 * MT;            // [WAVES / 2][MT * (DT * 4 + 1)][64]
+    // A lane's channels: of tile j row 4 r + i, channel (HD 128, 64) 64 (j / 4) + 16 r + 4 i + j % 4, (32) 8 r + 2 i + j.  With KW > 1 every wave
+    // leaves its sums in LDS and joins a part of the channels, in wave order.
+    constexpr int QUADS = DT / 4 > 0 ? DT / 4 : 1, ITEMS = 4 * QUADS;    // (i, group of four tiles j)
+    constexpr int SPAN = MT * ITEMS;
+    float4* const sx = reinterpret_cast<float4*>(lds) + (size_t)rw * KW * SPAN * 64;                      // [KW][MT][ITEMS][64]
+    float2* const sm = reinterpret_cast<float2*>(reinterpret_cast<float4*>(lds) + (size_t)a.row_waves * KW * SPAN * 64) + rw * KW * MT * 16;   // [KW][MT][16]
+    auto quad = [&](int t, int item) {
+        const int i = item / QUADS, j = 4 * (item % QUADS);
+        return HD == 32 ? make_float4(acc[t][0][i], acc[t][1][i], 0.f, 0.f) : make_float4(acc[t][j][i], acc[t][j + 1][i], acc[t][j + 2][i], acc[t][j + 3][i]);
+    };
+    if constexpr (KW > 1) {
         __syncthreads();                                    // (the scales are read)
-        if (r == 0)
-#pragma unroll
-            for (int t = 0; t < MT; ++t) sm[wave * 16 * MT + 16 * t + col] = m[t];
-        __syncthreads();
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
-            float top = m[t];
 #pragma unroll
-            for (int w = 0; w < WAVES; ++w) top = fmaxf(top, sm[w * 16 * MT + 16 * t + col]);
-            const float f = m[t] == top ? 1.f : __builtin_amdgcn_exp2f(m[t] - top);
-            m[t] = top;
-            l[t] *= f;
-#pragma unroll
-            for (int j = 0; j < DT; ++j) acc[t][j] *= f;
+            for (int item = 0; item < ITEMS; ++item) sx[((kw * MT + t) * ITEMS + item) * 64 + lane] = quad(t, item);
+            if (r == 0) sm[(kw * MT + t) * 16 + col] = make_float2(m[t], l[t]);
         }
-        constexpr int SPAN = MT * (DT * 4 + 1);
-#pragma unroll
-        for (int half = WAVES / 2; half >= 1; half /= 2) {
-            if (wave >= half && wave < 2 * half) {
-                float* to = sx + (size_t)(wave - half) * SPAN * 64 + lane;
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-#pragma unroll
-                    for (int j = 0; j < DT; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) to[(t * (DT * 4 + 1) + 4 * j + e) * 64] = acc[t][j][e];
-                    to[(t * (DT * 4 + 1) + 4 * DT) * 64] = l[t];
-                }
-            }
-            __syncthreads();
-            if (wave < half) {
-                const float* from = sx + (size_t)wave * SPAN * 64 + lane;
-#pragma unroll
-                for (int t = 0; t < MT; ++t) {
-#pragma unroll
-                    for (int j = 0; j < DT; ++j)
-#pragma unroll
-                        for (int e = 0; e < 4; ++e) acc[t][j][e] += from[(t * (DT * 4 + 1) + 4 * j + e) * 64];
-                    l[t] += from[(t * (DT * 4 + 1) + 4 * DT) * 64];
-                }
-            }
-            __syncthreads();
-        }
-        if (wave != 0) return;
+        __syncthreads();
     }
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
         const int pair = pair0 + 16 * t + col, row = sq.first + pair / share, head = h * share + pair % share;
-        if (pair >= n_pairs || row >= a.rows) continue;
-        // lane's channels: of tile j row 4 r + i, channel (HD 128, 64) 64 (j / 4) + 16 r + 4 i + j % 4, (32) 8 r + 2 i + j
-        if (a.chunks == 1) {
-            const float inv = l[t] > 0.f ? 1.f / l[t] : l[t];          // a pair without keys gives zeros (a NaN stays one)
-            uint16_t* o = reinterpret_cast<uint16_t*>(a.out + (size_t)row * a.out_stride + head * HD);
-            if constexpr (HD == 32) {
+        float part[KW];
+        if constexpr (KW > 1) {
+            float top = -__builtin_inff();
 #pragma unroll
-                for (int i = 0; i < 4; ++i) *reinterpret_cast<uint32_t*>(o + 8 * r + 2 * i) = f2bf_pair(acc[t][0][i] * inv, acc[t][1][i] * inv);
-            } else {
+            for (int w = 0; w < KW; ++w) top = fmaxf(top, sm[(w * MT + t) * 16 + col].x);
+            l[t] = 0.f;
 #pragma unroll
-                for (int g = 0; g < DT / 4; ++g)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<kv4_u32x2*>(o + 64 * g + 16 * r + 4 * i) =
-                            kv4_u32x2{f2bf_pair(acc[t][4 * g][i] * inv, acc[t][4 * g + 1][i] * inv), f2bf_pair(acc[t][4 * g + 2][i] * inv, acc[t][4 * g + 3][i] * inv)};
+            for (int w = 0; w < KW; ++w) {
+                const float2 ml = sm[(w * MT + t) * 16 + col];
+                part[w] = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
+                l[t] = __builtin_fmaf(ml.y, part[w], l[t]);
             }
-        } else {
-            const size_t at = ((size_t)chunk * a.rows + row) * a.H + head;
-            float* o = a.part_o + at * HD;
-            if constexpr (HD == 32) {
-#pragma unroll
-                for (int i = 0; i < 4; ++i) *reinterpret_cast<float2*>(o + 8 * r + 2 * i) = make_float2(acc[t][0][i], acc[t][1][i]);
-            } else {
-#pragma unroll
-                for (int g = 0; g < DT / 4; ++g)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i)
-                        *reinterpret_cast<float4*>(o + 64 * g + 16 * r + 4 * i) =
-                            make_float4(acc[t][4 * g][i], acc[t][4 * g + 1][i], acc[t][4 * g + 2][i], acc[t][4 * g + 3][i]);
-            }
-            if (r == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m[t], l[t]);
+            m[t] = top;
         }
+        if (pair >= n_pairs || row >= a.rows) continue;
+        const float inv = a.chunks > 1 ? 1.f : l[t] > 0.f ? 1.f / l[t] : l[t];       // a pair without keys gives zeros (a NaN stays one)
+        const size_t at = ((size_t)chunk * a.rows + row) * a.H + head;
+        constexpr int MINE = ITEMS / KW > 0 ? ITEMS / KW : 1;
+        if (KW <= ITEMS || kw < ITEMS)
+#pragma unroll
+            for (int n = 0; n < MINE; ++n) {
+                float4 o;
+                int item = n;
+                if constexpr (KW == 1) o = quad(t, n);
+                else {
+                    item = kw * MINE + n;
+                    o = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+                    for (int w = 0; w < KW; ++w) {
+                        const float4 x = sx[((w * MT + t) * ITEMS + item) * 64 + lane];
+                        o.x = __builtin_fmaf(x.x, part[w], o.x);
+                        o.y = __builtin_fmaf(x.y, part[w], o.y);
+                        o.z = __builtin_fmaf(x.z, part[w], o.z);
+                        o.w = __builtin_fmaf(x.w, part[w], o.w);
+                    }
+                }
+                const int i = item / QUADS, d = HD == 32 ? 8 * r + 2 * i : 64 * (item % QUADS) + 16 * r + 4 * i;
+                if (a.chunks == 1) {
+                    uint16_t* to = reinterpret_cast<uint16_t*>(a.out + (size_t)row * a.out_stride + head * HD + d);
+                    if constexpr (HD == 32) *reinterpret_cast<uint32_t*>(to) = f2bf_pair(o.x * inv, o.y * inv);
+                    else *reinterpret_cast<kv4_u32x2*>(to) = kv4_u32x2{f2bf_pair(o.x * inv, o.y * inv), f2bf_pair(o.z * inv, o.w * inv)};
+                } else {
+                    float* to = a.part_o + at * HD + d;
+                    if constexpr (HD == 32) *reinterpret_cast<float2*>(to) = make_float2(o.x, o.y);
+                    else *reinterpret_cast<float4*>(to) = o;
+                }
+            }
+        if (a.chunks > 1 && kw == 0 && r == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m[t], l[t]);
     }
 }
-template <int HD, int MT, int WK>
-constexpr int kv4_attention_lds() {
-    const int scales = (WK == 1 ? 4 : WK) * (int)sizeof(Kv4Scales<HD>), join = WK == 1 ? 0 : (WK * 16 * MT + WK / 2 * MT * (HD / 4 + 1) * 64) * 4;
+// LDS of a workgroup of `waves` waves
+template <int HD, int MT, int KW>
+int kv4_attention_lds(int waves) {
+    const int scales = waves * (int)sizeof(Kv4Scales<HD>), join = KW == 1 ? 0 : waves * MT * ((HD >= 64 ? HD / 16 : 4) * 64 * 16 + 16 * 8);
     return scales > join ? scales : join;
 }
 
-// The key chunks' results in chunk order; a workgroup per (sequence, row), a thread per 4 channels of a head at a time.
+// The key chunks' results in chunk order: HD / 4 lanes a (row, head) pair, four channels each; a workgroup per (sequence, row, 1024 / HD heads).
 template <int HD>
 __global__ __launch_bounds__(256) void k_kv4_merge(Kv4Attn a) {
+    constexpr int LANES = HD / 4;
     const Kv4Seq sq = kv4_seq(a, blockIdx.y);
-    const int row = sq.first + blockIdx.x;
-    if ((int)blockIdx.x >= sq.n || row >= a.rows) return;
-    for (int idx = threadIdx.x; idx < a.H * (HD / 4); idx += 256) {
-        const int head = idx / (HD / 4), d = 4 * (idx % (HD / 4));
-        float top = -__builtin_inff();
-        for (int c = 0; c < a.chunks; ++c) top = fmaxf(top, a.part_ml[2 * (((size_t)c * a.rows + row) * a.H + head)]);
-        float l = 0.f;
-        kv4_f32x4 o = {0.f, 0.f, 0.f, 0.f};
-        for (int c = 0; c < a.chunks; ++c) {
-            const size_t at = ((size_t)c * a.rows + row) * a.H + head;
-            const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * at);
-            const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
-            l = __builtin_fmaf(ml.y, f, l);
-            o += *reinterpret_cast<const kv4_f32x4*>(a.part_o + at * HD + d) * f;
-        }
-        const float inv = l > 0.f ? 1.f / l : l;
-        *reinterpret_cast<kv4_u32x2*>(a.out + (size_t)row * a.out_stride + head * HD + d) = kv4_u32x2{f2bf_pair(o[0] * inv, o[1] * inv), f2bf_pair(o[2] * inv, o[3] * inv)};
+    const int i = blockIdx.x % a.max_rows, row = sq.first + i;
+    const int head = blockIdx.x / a.max_rows * (256 / LANES) + threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES);
+    if (i >= sq.n || row >= a.rows || head >= a.H) return;
+    const size_t step = (size_t)a.rows * a.H, at = (size_t)row * a.H + head;
+    float top = -__builtin_inff();
+#pragma unroll 8
+    for (int c = 0; c < a.chunks; ++c) top = fmaxf(top, a.part_ml[2 * (c * step + at)]);
+    float l = 0.f;
+    kv4_f32x4 o = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+    for (int c = 0; c < a.chunks; ++c) {
+        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (c * step + at));
+        const kv4_f32x4 x = *reinterpret_cast<const kv4_f32x4*>(a.part_o + (c * step + at) * HD + d);
+        const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
+        l = __builtin_fmaf(ml.y, f, l);
+        o += x * f;
     }
+    const float inv = l > 0.f ? 1.f / l : l;
+    *reinterpret_cast<kv4_u32x2*>(a.out + (size_t)row * a.out_stride + head * HD + d) = kv4_u32x2{f2bf_pair(o[0] * inv, o[1] * inv), f2bf_pair(o[2] * inv, o[3] * inv)};
 }

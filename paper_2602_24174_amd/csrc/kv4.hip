@@ -5,36 +5,39 @@
 
 namespace {
 
-template <int HD, int MT, int WK>
-tasc_status attend(const Kv4Attn& a, int tiles, hipStream_t st) {
-    constexpr int lds = kv4_attention_lds<HD, MT, WK>();
-    if constexpr (lds > 65536) {
+template <int HD, int MT, int KW>
+tasc_status attend(Kv4Attn a, hipStream_t st) {
+    // four waves a workgroup (KW at least), fewer where the pairs end before
+    const int64_t pairs = (int64_t)a.max_rows * (a.H / a.Hkv), waves = (pairs + 16 * MT - 1) / (16 * MT);
+    constexpr int MOST = KW < 4 ? 4 / KW : 1;
+    a.row_waves = (int)std::min<int64_t>(waves, MOST);
+    const int64_t tiles = (waves + a.row_waves - 1) / a.row_waves;
+    const int lds = kv4_attention_lds<HD, MT, KW>(a.row_waves * KW);
+    if (kv4_attention_lds<HD, MT, KW>(MOST * KW) > 65536) {
         int dev = 0;
         TASC_HIP(hipGetDevice(&dev));
         static std::mutex mu;
         static bool ready[16];
         std::lock_guard<std::mutex> lock(mu);
         if (!ready[dev & 15]) {
-            TASC_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_kv4_attention<HD, MT, WK>), hipFuncAttributeMaxDynamicSharedMemorySize, lds));
+            TASC_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_kv4_attention<HD, MT, KW>), hipFuncAttributeMaxDynamicSharedMemorySize, kv4_attention_lds<HD, MT, KW>(MOST * KW)));
             ready[dev & 15] = true;
         }
     }
-    k_kv4_attention<HD, MT, WK><<<dim3((unsigned)(tiles * a.chunks), (unsigned)(a.batch * a.Hkv)), dim3(WK == 1 ? 256 : 64 * WK), lds, st>>>(a);
+    k_kv4_attention<HD, MT, KW><<<dim3((unsigned)(tiles * a.chunks), (unsigned)(a.batch * a.Hkv)), dim3((unsigned)(64 * a.row_waves * KW)), lds, st>>>(a);
     return TASC_OK;
 }
 template <int HD>
-tasc_status attend_hd(const Kv4Attn& a, int wk, hipStream_t st) {
+tasc_status attend_hd(const Kv4Attn& a, int kw, hipStream_t st) {
     const int64_t pairs = (int64_t)a.max_rows * (a.H / a.Hkv);
-    constexpr int MOST = HD == 128 ? 2 : 4;                // tiles of pairs that fit a wave's registers
-    auto tiles = [&](int per) { return (int)((pairs + per - 1) / per); };
     tasc_status rc;
-    if (wk == 1) rc = attend<HD, MOST, 1>(a, tiles(64 * MOST), st);
-    else if (wk == 8) rc = attend<HD, 1, 8>(a, tiles(16), st);
-    else if (pairs <= 16) rc = attend<HD, 1, 4>(a, tiles(16), st);
-    else if (MOST == 2 || pairs <= 32) rc = attend<HD, 2, 4>(a, tiles(32), st);
-    else rc = attend<HD, MOST, 4>(a, tiles(16 * MOST), st);
+    if (kw == 8) rc = attend<HD, 1, 8>(a, st);
+    else if (kw == 4) rc = attend<HD, 1, 4>(a, st);
+    else if (kw == 1) rc = attend<HD, 2, 1>(a, st);
+    else if (pairs <= 16) rc = attend<HD, 1, 2>(a, st);
+    else rc = attend<HD, 2, 2>(a, st);
     if (rc != TASC_OK) return rc;
-    if (a.chunks > 1) k_kv4_merge<HD><<<dim3((unsigned)a.max_rows, (unsigned)a.batch), dim3(256), 0, st>>>(a);
+    if (a.chunks > 1) k_kv4_merge<HD><<<dim3((unsigned)(a.max_rows * ((a.H + 1024 / HD - 1) / (1024 / HD))), (unsigned)a.batch), dim3(256), 0, st>>>(a);
     TASC_LAUNCH_CHECK();
     return TASC_OK;
 }
@@ -62,7 +65,7 @@ constexpr int kMostChunks = 64;
 tasc_status tasc_kv4_attend(Kv4Attn a, int hd, const Kv4Order& o, hipStream_t st) {
     a.chunks = o.chunks;
     a.chunk_tiles = o.chunk_tiles;
-    return hd == 128 ? attend_hd<128>(a, o.wk, st) : hd == 64 ? attend_hd<64>(a, o.wk, st) : attend_hd<32>(a, o.wk, st);
+    return hd == 128 ? attend_hd<128>(a, o.kw, st) : hd == 64 ? attend_hd<64>(a, o.kw, st) : attend_hd<32>(a, o.kw, st);
 }
 
 extern "C" size_t tasc_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim) {
