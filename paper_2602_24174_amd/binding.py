@@ -492,55 +492,65 @@ def tasc_calibration_copy(dst, src, stream=None):
 
 
 # ---------------------------------------------------------------- the operators of a serving step over a 4-bit cache
+# (A call's checks are a good part of what a small one takes, so they are few and cheap: a device array costs 0.5 us here.)
 def _refuse(message):
     raise TascError(TASC_EINVAL, message)
 
 
-def _device_array(who, name, t, dtype, shape, optional=False):
-    """Address of a contiguous tensor of the current device with this dtype and shape (None: any length there)."""
-    if t is None and optional:
-        return None
+def _array(who, name, t, dtype, shape, dev):
+    """Address of a contiguous tensor of device `dev` with this dtype and shape."""
+    try:
+        if t.dtype is dtype and t.shape == shape and t.get_device() == dev and t.is_contiguous():
+            return t.data_ptr()
+    except AttributeError:
+        pass
+    _refuse(f"{who}: {name} is not a contiguous {dtype} tensor of shape {tuple(shape)} on cuda:{dev}, the current device")
+
+
+def _list(who, name, t, dtype, dev):
+    """(address, length) of a contiguous one-dimensional tensor of any length."""
+    if getattr(t, "ndim", 0) != 1:
+        _refuse(f"{who}: {name} is not a one-dimensional {dtype} tensor on cuda:{dev}")
+    return _array(who, name, t, dtype, t.shape, dev), t.shape[0]
+
+
+def _rows(who, name, t, dtypes, shape, dev):
+    """(address, elements from row to row) of a tensor [rows, heads, head_dim] whose rows are each side by side."""
+    try:
+        if t.dtype in dtypes and t.shape == shape and t.get_device() == dev:
+            if t.is_contiguous():
+                return t.data_ptr(), shape[1] * shape[2]
+            row, head, one = t.stride()
+            if (one == 1 or shape[2] == 1) and (head == shape[2] or shape[1] == 1):
+                return t.data_ptr(), row
+    except AttributeError:
+        pass
+    _refuse(f"{who}: {name} is not a {' or '.join(str(d) for d in dtypes)} tensor of shape {tuple(shape)} on cuda:{dev} whose rows are each side by side")
+
+
+def _here(stream):
+    """(the current device, stream of the call, whether that is the current one)"""
     import torch
-    if not torch.is_tensor(t) or not t.is_cuda or t.dtype != dtype or not t.is_contiguous() or t.dim() != len(shape) or \
-            any(n is not None and n != m for n, m in zip(shape, t.shape)):
-        _refuse(f"{who}: {name} is not a contiguous {dtype} tensor of shape {tuple(shape)} on the device")
-    if t.device.index != torch.cuda.current_device():
-        _refuse(f"{who}: {name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    return t.data_ptr()
+    try:
+        dev = torch.cuda.current_device()
+    except (RuntimeError, AssertionError) as e:
+        raise TascError(TASC_EHIP, f"no device: {e}") from None
+    current = torch.cuda.current_stream(dev).cuda_stream
+    return dev, current if stream is None else stream, stream is None or stream == current
 
 
-def _row_stride(who, name, t, dtypes, width):
-    """Elements from row to row of a tensor [rows, heads, head_dim] or [.., vocab] whose rows are `width` elements side by side."""
-    import torch
-    if not torch.is_tensor(t) or not t.is_cuda or t.dtype not in dtypes:
-        _refuse(f"{who}: {name} is not a device tensor of {' or '.join(str(d) for d in dtypes)}")
-    if t.device.index != torch.cuda.current_device():
-        _refuse(f"{who}: {name} is on {t.device}, the current device is cuda:{torch.cuda.current_device()}")
-    if t.numel() == 0:
-        return width
-    inner = 1
-    for n, stride in zip(reversed(t.shape[1:]), reversed(t.stride()[1:])):
-        if n != 1 and stride != inner:
-            _refuse(f"{who}: the elements of a row of {name} are not side by side")
-        inner *= n
-    return t.stride(0) if t.shape[0] > 1 else width
-
-
-def _workspace(who, workspace, need, stream):
+def _workspace(who, workspace, need, dev, on_current):
     """(tensor kept alive, address, bytes).  A workspace made here belongs to the current stream."""
     import torch
     if workspace is None:
-        if need and stream is not None and stream != torch.cuda.current_stream().cuda_stream:
+        if need == 0:
+            return None, None, 0
+        if not on_current:
             _refuse(f"{who}: a call on a stream other than the current one needs a workspace of {need} bytes")
         workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
-    elif not workspace.is_cuda or not workspace.is_contiguous() or workspace.device.index != torch.cuda.current_device():
+    elif workspace.get_device() != dev or not workspace.is_contiguous():
         _refuse(f"{who}: the workspace is not a contiguous tensor of the current device")
     return workspace, workspace.data_ptr() or None, workspace.numel() * workspace.element_size()
-
-
-def _same_length(who, **lengths):
-    if len(set(lengths.values())) > 1:
-        _refuse(f"{who}: " + ", ".join(f"{k} has {v}" for k, v in lengths.items()))
 
 
 def tasc_page_tables(kv_len, new_rows, held, free_pages, table, pages=None, row_off=None, slots=None, summary=None, n_free=None, stream=None):
@@ -548,17 +558,26 @@ def tasc_page_tables(kv_len, new_rows, held, free_pages, table, pages=None, row_
     row_off [batch + 1], slots [any], summary [3]; table, pages, row_off, slots and summary are written in place."""
     import torch
     who, i32 = "page_tables", torch.int32
-    B = kv_len.shape[0]
-    max_pages = table.shape[1] if table.dim() == 2 else 0
-    if free_pages is not None and n_free is None:
-        n_free = free_pages.shape[0]
-    if free_pages is not None and n_free > free_pages.shape[0]:
-        _refuse(f"{who}: n_free {n_free} of {free_pages.shape[0]} free pages")
-    a = lambda name, t, shape, optional=True: _device_array(who, name, t, i32, shape, optional)
-    _check(lib().tasc_page_tables(a("kv_len", kv_len, (B,), False), a("new_rows", new_rows, (B,)), a("held", held, (B,)), B,
-                                  a("free_pages", free_pages, (None,)) or None, n_free or 0, a("table", table, (B, max_pages), False), max_pages,
-                                  a("pages", pages, (B,)), a("row_off", row_off, (B + 1,)), a("slots", slots, (None,)) or None,
-                                  0 if slots is None else slots.shape[0], a("summary", summary, (3,)), _stream(stream)))
+    dev, st, _ = _here(stream)
+    kv, B = _list(who, "kv_len", kv_len, i32, dev)
+    if getattr(table, "ndim", 0) != 2 or table.shape[0] != B:
+        _refuse(f"{who}: table is not [{B}, max_pages]")
+    per = kv_len.shape
+    free = n = cap = 0
+    if free_pages is not None:
+        free, n = _list(who, "free_pages", free_pages, i32, dev)
+    if n_free is not None:
+        if free_pages is not None and n_free > n:
+            _refuse(f"{who}: n_free {n_free} of {n} free pages")
+        n = n_free
+    at = 0
+    if slots is not None:
+        at, cap = _list(who, "slots", slots, i32, dev)
+    _check(lib().tasc_page_tables(
+        kv, None if new_rows is None else _array(who, "new_rows", new_rows, i32, per, dev), None if held is None else _array(who, "held", held, i32, per, dev), B,
+        free or None, n, _array(who, "table", table, i32, table.shape, dev), table.shape[1], None if pages is None else _array(who, "pages", pages, i32, per, dev),
+        None if row_off is None else _array(who, "row_off", row_off, i32, (B + 1,), dev), at or None, cap,
+        None if summary is None else _array(who, "summary", summary, i32, (3,), dev), st))
 
 
 def tasc_kv4_page_bytes(n_kv_heads, head_dim) -> int:
@@ -578,40 +597,39 @@ class Kv4Cache:
         elif not pool.is_cuda or not pool.is_contiguous() or pool.numel() * pool.element_size() < n_pages * page:
             _refuse(f"Kv4Cache: the pool does not hold {n_pages} pages of {page} bytes")
         self.pool, self.n_pages, self.n_kv_heads, self.head_dim = pool, n_pages, n_kv_heads, head_dim
+        self.device = pool.get_device()
         self.desc = Kv4CacheDesc(pool.data_ptr(), n_pages, n_kv_heads, head_dim)
+        self.ref = C.byref(self.desc)
 
-    def _ref(self, who):
-        import torch
-        if self.pool.device.index != torch.cuda.current_device():
-            _refuse(f"{who}: the cache is on {self.pool.device}, the current device is cuda:{torch.cuda.current_device()}")
-        return C.byref(self.desc)
-
-
-def _float_dtype(t):
-    import torch
-    return TASC_F32 if t.dtype == torch.float32 else TASC_BF16
+    def on(self, who, dev):
+        if self.device != dev:
+            _refuse(f"{who}: the cache is on cuda:{self.device}, the current device is cuda:{dev}")
+        return self.ref
 
 
 def tasc_kv4_append(cache: Kv4Cache, k, v, slots, stream=None):
     """k, v: cuda tensors [rows, n_kv_heads, head_dim], fp32 or bf16 (both alike), a row's elements side by side; slots: int32 [rows]."""
     import torch
-    who, shape = "kv4_append", (slots.shape[0], cache.n_kv_heads, cache.head_dim)
-    if tuple(k.shape) != shape or tuple(v.shape) != shape or k.dtype != v.dtype:
-        _refuse(f"{who}: keys {tuple(k.shape)} {k.dtype}, values {tuple(v.shape)} {v.dtype} for rows of shape {shape}")
-    width = cache.n_kv_heads * cache.head_dim
-    ks, vs = (_row_stride(who, n, t, (torch.float32, torch.bfloat16), width) for n, t in (("k", k), ("v", v)))
-    _check(lib().tasc_kv4_append(cache._ref(who), k.data_ptr(), v.data_ptr(), _float_dtype(k), ks, vs,
-                                 _device_array(who, "slots", slots, torch.int32, (None,)), shape[0], _stream(stream)))
+    who = "kv4_append"
+    dev, st, _ = _here(stream)
+    at, rows = _list(who, "slots", slots, torch.int32, dev)
+    shape, dtype = (rows, cache.n_kv_heads, cache.head_dim), getattr(k, "dtype", None)
+    ka, ks = _rows(who, "k", k, (torch.float32, torch.bfloat16), shape, dev)
+    va, vs = _rows(who, "v", v, (dtype,), shape, dev)
+    _check(lib().tasc_kv4_append(cache.on(who, dev), ka, va, TASC_F32 if dtype is torch.float32 else TASC_BF16, ks, vs, at, rows, st))
 
 
 def tasc_kv4_read(cache: Kv4Cache, slots, k, v, stream=None):
     """k, v: cuda tensors [rows, n_kv_heads, head_dim], fp32 or bf16 (both alike), written in place; slots: int32 [rows]."""
     import torch
-    who, shape = "kv4_read", (slots.shape[0], cache.n_kv_heads, cache.head_dim)
-    if k.dtype not in (torch.float32, torch.bfloat16):
-        _refuse(f"{who}: {k.dtype} is neither float32 nor bfloat16")
-    _check(lib().tasc_kv4_read(cache._ref(who), _device_array(who, "slots", slots, torch.int32, (None,)), shape[0], _float_dtype(k),
-                               _device_array(who, "k", k, k.dtype, shape), _device_array(who, "v", v, k.dtype, shape), _stream(stream)))
+    who, dtype = "kv4_read", getattr(k, "dtype", None)
+    if dtype is not torch.float32 and dtype is not torch.bfloat16:
+        _refuse(f"{who}: {dtype} is neither float32 nor bfloat16")
+    dev, st, _ = _here(stream)
+    at, rows = _list(who, "slots", slots, torch.int32, dev)
+    shape = (rows, cache.n_kv_heads, cache.head_dim)
+    _check(lib().tasc_kv4_read(cache.on(who, dev), at, rows, TASC_F32 if dtype is torch.float32 else TASC_BF16, _array(who, "k", k, dtype, shape, dev),
+                               _array(who, "v", v, dtype, shape, dev), st))
 
 
 def tasc_kv4_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, head_dim, max_rows, max_kv) -> int:
@@ -622,18 +640,22 @@ def tasc_kv4_attention(cache: Kv4Cache, q, table, row_off, kv_len, max_rows, max
     """q, out: bf16 cuda tensors [rows, n_heads, head_dim], a row's elements side by side; table int32 [batch, max_pages], row_off int32
     [batch + 1], kv_len int32 [batch].  out is written in place."""
     import torch
-    who = "kv4_attention"
-    if q.dim() != 3 or q.shape != out.shape or q.shape[2] != cache.head_dim:
-        _refuse(f"{who}: queries {tuple(q.shape)}, results {tuple(out.shape)} over heads of {cache.head_dim}")
-    rows, H, hd = q.shape
-    B = kv_len.shape[0]
-    max_pages = table.shape[1] if table.dim() == 2 else 0
-    a = Kv4Attn(q.data_ptr(), out.data_ptr(), _row_stride(who, "q", q, (torch.bfloat16,), H * hd), _row_stride(who, "out", out, (torch.bfloat16,), H * hd),
-                _device_array(who, "table", table, torch.int32, (B, max_pages)), _device_array(who, "row_off", row_off, torch.int32, (B + 1,)),
-                _device_array(who, "kv_len", kv_len, torch.int32, (B,)), max_pages, B, rows, H, max_rows, max_kv, scale)
+    who, i32 = "kv4_attention", torch.int32
+    dev, st, on_current = _here(stream)
+    if getattr(q, "ndim", 0) != 3 or q.shape[2] != cache.head_dim:
+        _refuse(f"{who}: queries are not [rows, n_heads, {cache.head_dim}]")
+    shape = q.shape
+    rows, H, hd = shape
+    qa, qs = _rows(who, "q", q, (torch.bfloat16,), shape, dev)
+    oa, os = _rows(who, "out", out, (torch.bfloat16,), shape, dev)
+    kv, B = _list(who, "kv_len", kv_len, i32, dev)
+    if getattr(table, "ndim", 0) != 2 or table.shape[0] != B:
+        _refuse(f"{who}: table is not [{B}, max_pages]")
+    a = Kv4Attn(qa, oa, qs, os, _array(who, "table", table, i32, table.shape, dev), _array(who, "row_off", row_off, i32, (B + 1,), dev), kv, table.shape[1], B, rows, H,
+                max_rows, max_kv, scale)
     need = 0 if workspace is not None else tasc_kv4_attention_workspace_bytes(B, rows, H, cache.n_kv_heads, hd, max_rows, max_kv)
-    keep, ws, n = _workspace(who, workspace, need, stream)
-    _check(lib().tasc_kv4_attention(cache._ref(who), C.byref(a), ws, n, _stream(stream)))
+    keep, ws, n = _workspace(who, workspace, need, dev, on_current)
+    _check(lib().tasc_kv4_attention(cache.on(who, dev), a, ws, n, st))
 
 
 def tasc_accept_sampled_workspace_bytes(batch, k, vocab) -> int:
@@ -646,19 +668,27 @@ def tasc_accept_sampled(logits, drafts, draft_probs, temperature, u, accept_len,
     logprob fp32 [batch, k + 1] (or None) are written in place."""
     import torch
     who, f32, i32 = "accept_sampled", torch.float32, torch.int32
-    if not torch.is_tensor(logits) or logits.dim() != 3:
-        _refuse(f"{who}: logits are not [batch, k + 1, vocab]")
+    dev, st, on_current = _here(stream)
+    dtype = getattr(logits, "dtype", None)
+    if (dtype is not f32 and dtype is not torch.bfloat16) or logits.ndim != 3 or logits.get_device() != dev:
+        _refuse(f"{who}: logits are not a float32 or bfloat16 tensor [batch, k + 1, vocab] on cuda:{dev}, the current device")
     B, nq, V = logits.shape
-    if B > 1 and nq > 1 and logits.stride(0) != nq * logits.stride(1):
-        _refuse(f"{who}: the rows of logits are not evenly spaced")
-    stride = _row_stride(who, "logits", logits[:, 0] if nq == 1 else logits[0] if B else logits.reshape(-1, V), (f32, torch.bfloat16), V)
-    a = lambda name, t, dtype, shape, optional=False: _device_array(who, name, t, dtype, shape, optional)
+    stride = V
+    if not logits.is_contiguous():
+        far, near, one = logits.stride()
+        stride = near if nq > 1 else far if B > 1 else V
+        if one != 1 or (B > 1 and far != nq * stride):
+            _refuse(f"{who}: the rows of logits are not evenly spaced")
+    per_row = (B, nq)
     need = 0 if workspace is not None else tasc_accept_sampled_workspace_bytes(B, nq - 1, V)
-    keep, ws, n = _workspace(who, workspace, need, stream)
-    _check(lib().tasc_accept_sampled(logits.data_ptr(), _float_dtype(logits), stride, B, nq - 1, V, a("drafts", drafts, i32, (B, nq - 1), nq == 1),
-                                     a("draft_probs", draft_probs, f32, (B, nq - 1, V), True), a("temperature", temperature, f32, (B,), True),
-                                     a("u", u, f32, (B, nq, 2)), a("accept_len", accept_len, i32, (B,)), a("emitted", emitted, i32, (B, nq)),
-                                     a("logprob", logprob, f32, (B, nq), True), ws, n, _stream(stream)))
+    keep, ws, n = _workspace(who, workspace, need, dev, on_current)
+    _check(lib().tasc_accept_sampled(
+        logits.data_ptr(), TASC_F32 if dtype is f32 else TASC_BF16, stride, B, nq - 1, V,
+        None if drafts is None and nq == 1 else _array(who, "drafts", drafts, i32, (B, nq - 1), dev),
+        None if draft_probs is None else _array(who, "draft_probs", draft_probs, f32, (B, nq - 1, V), dev),
+        None if temperature is None else _array(who, "temperature", temperature, f32, (B,), dev), _array(who, "u", u, f32, (B, nq, 2), dev),
+        _array(who, "accept_len", accept_len, i32, (B,), dev), _array(who, "emitted", emitted, i32, per_row, dev),
+        None if logprob is None else _array(who, "logprob", logprob, f32, per_row, dev), ws, n, st))
 
 
 # ---------------------------------------------------------------- sessions that sample, sessions over a 4-bit cache
@@ -682,17 +712,18 @@ def tasc_sampled_scratch_bytes(model: Model, batch, k) -> int:
     return lib().tasc_sampled_scratch_bytes(model.handle, batch, k)
 
 
-def _sampling(who, model, s, k, u, temperature, scratch):
+def _sampling(who, model, s, k, u, temperature, scratch, dev):
     """(what must stay alive, struct).  A scratch made here stays with the session, one for every k, as recorded steps do."""
     import torch
-    if not torch.is_tensor(u) or u.dim() != 3:
+    if getattr(u, "ndim", 0) != 3:
         _refuse(f"{who}: u is not [batch, pairs, 2]")
     if scratch is None:
         if k not in s._scratch:
             s._scratch[k] = torch.empty(max(tasc_sampled_scratch_bytes(model, s.batch, k), 1), dtype=torch.uint8, device="cuda")
         scratch = s._scratch[k]
-    return scratch, Sampling(_device_array(who, "temperature", temperature, torch.float32, (s.batch,), True),
-                             _device_array(who, "u", u, torch.float32, (s.batch, None, 2)), u.shape[1], scratch.data_ptr(), scratch.numel() * scratch.element_size())
+    return scratch, Sampling(None if temperature is None else _array(who, "temperature", temperature, torch.float32, (s.batch,), dev),
+                             _array(who, "u", u, torch.float32, (s.batch, u.shape[1], 2), dev), u.shape[1], scratch.data_ptr(),
+                             scratch.numel() * scratch.element_size())
 
 
 def tasc_verify_step_sampled(model: Model, s: Session, drafts, k, u, temperature=None, accept_len=None, emitted=None, logprob=None, scratch=None, stream=None):
@@ -700,11 +731,13 @@ def tasc_verify_step_sampled(model: Model, s: Session, drafts, k, u, temperature
     emitted int32 [batch, k + 1] and logprob fp32 [batch, k + 1] (or None) are written in place."""
     import torch
     who, i32 = "verify_step_sampled", torch.int32
-    keep, p = _sampling(who, model, s, k, u, temperature, scratch)
-    _check(lib().tasc_verify_step_sampled(model.handle, s.handle, _device_array(who, "drafts", drafts, i32, (s.batch, k), k == 0), k, C.byref(p),
-                                          _device_array(who, "accept_len", accept_len, i32, (s.batch,), True),
-                                          _device_array(who, "emitted", emitted, i32, (s.batch, k + 1), True),
-                                          _device_array(who, "logprob", logprob, torch.float32, (s.batch, k + 1), True), _stream(stream)))
+    dev, st, _ = _here(stream)
+    keep, p = _sampling(who, model, s, k, u, temperature, scratch, dev)
+    per_row = (s.batch, k + 1)
+    _check(lib().tasc_verify_step_sampled(model.handle, s.handle, None if drafts is None and k == 0 else _array(who, "drafts", drafts, i32, (s.batch, k), dev), k, C.byref(p),
+                                          None if accept_len is None else _array(who, "accept_len", accept_len, i32, (s.batch,), dev),
+                                          None if emitted is None else _array(who, "emitted", emitted, i32, per_row, dev),
+                                          None if logprob is None else _array(who, "logprob", logprob, torch.float32, per_row, dev), st))
 
 
 def tasc_session_rewind(s: Session, stream=None):
@@ -716,10 +749,10 @@ def tasc_generate_sampled(model: Model, ng, s: Session, prompts, prompt_offsets,
     """As tasc_generate; u: fp32 cuda tensor [batch, pairs, 2] (pairs = max_new gives every token its own)."""
     import torch
     who = "generate_sampled"
+    dev, st, _ = _here(stream)
     prompt_offsets = np.ascontiguousarray(prompt_offsets, dtype=np.int64)
-    keep, p = _sampling(who, model, s, params.k, u, temperature, scratch)
-    st = GenStats()
+    keep, p = _sampling(who, model, s, params.k, u, temperature, scratch, dev)
+    stats = GenStats()
     _check(lib().tasc_generate_sampled(model.handle, ng.handle if ng is not None else None, s.handle, _ptr(prompts), _ptr(prompt_offsets), _where(prompts), max_new,
-                                       C.byref(params), C.byref(p), _device_array(who, "out_tokens", out_tokens, torch.int32, (s.batch, max_new)), C.byref(st),
-                                       _stream(stream)))
-    return st
+                                       C.byref(params), C.byref(p), _array(who, "out_tokens", out_tokens, torch.int32, (s.batch, max_new), dev), C.byref(stats), st))
+    return stats
