@@ -5,10 +5,10 @@
 // not draws from max(0, w / Z - q) (q given) or from w without d (q a point mass), the row behind the last draft from w: the lowest v with
 // sum up to v > u' total.
 //
-// Two passes over a row at most: k_sample_parts reads every logit once and leaves, per segment of 4096 tokens, the maximum, its place and
-// sum w relative to it, without the row's draft (so that what remains after a rejection is a sum, not a difference); k_sample_pick, a workgroup
-// per sequence, joins the segments, decides, finds the segment that the draw falls into and reads that one again.  Given q,
-// k_sample_residual sums max(0, w / Z - q) over the segments of the rejected row in between.  Bound by the bytes of the logits.
+// Two passes over a row at most: k_sample_parts reads every logit once and leaves, per segment of 4096 tokens, the maximum (of a greedy
+// sequence its place, too) and sum w relative to it, without the row's draft (so that what remains after a rejection is a sum, not a difference); k_sample_pick, a workgroup
+// per sequence, joins the segments, decides, finds the segment that the draw falls into and reads that one again.  Given q, k_sample_decide
+// joins and decides, and k_sample_residual sums max(0, w / Z - q) over the segments of the rejected row in between.
 //
 // Exponentials and sums are fp64: the draw compares sums over the whole vocabulary with u' total, and with fp32's 2^-24 on each of 150,000
 // terms a token in a few thousand would come out as its neighbour.  An fp64 fma has the rate of an fp32 one here.
@@ -21,6 +21,7 @@ constexpr int kSeg = 4096, kPartThreads = 256, kPer = kSeg / kPartThreads, kPick
 
 struct __attribute__((aligned(16))) Part { double sum; float top; int32_t at; };   // sum: relative to top, without the row's draft
 
+struct Row;
 struct SampleArgs {
     const void* logits;
     int64_t row_stride;
@@ -32,6 +33,7 @@ struct SampleArgs {
     int64_t n_u;
     const int32_t* n_emit;           // null: row i of a sequence takes pair i; else pair min(n_emit + i, n_u - 1)
     Part* parts;                     // [B (k + 1), n_seg]
+    Row* decided;             // [B (k + 1)], given probs
     double* residual;                // [B, n_seg], given probs
     int32_t *accept_len, *emitted;
     float* logprob;
@@ -83,60 +85,114 @@ __device__ __forceinline__ double wave_sum64(double v) {
     return v;
 }
 
-template <typename T>
+// 16 logits of a segment: VEC, 16 bytes side by side at a time (rows start at multiples of 16 bytes), else thread by thread
+template <typename T, bool VEC>
+struct Segment {
+    static constexpr int SIDE = VEC ? 16 / (int)sizeof(T) : 1;
+    static __device__ __forceinline__ int place(int e, int tid) { return (e / SIDE * kPartThreads + tid) * SIDE + e % SIDE; }
+    static __device__ __forceinline__ void load(const T* __restrict__ row, int v0, int vocab, int tid, float (&x)[kPer]) {
+        if (VEC && v0 + kSeg <= vocab) {
+#pragma unroll
+            for (int e = 0; e < kPer; e += SIDE) load_n<SIDE == 1 ? 4 : SIDE>(row + v0 + place(e, tid), x + e);
+        } else {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const int v = v0 + place(e, tid);
+                x[e] = v < vocab ? to_f(row[v]) : -__builtin_inff();
+            }
+        }
+    }
+};
+
+// What bounds it is the exponentials, 16 a thread: exp(y) = 2^(i / 64) exp(f ln 2 / 64) with i = rint(64 y / ln 2), the first factor out of a table
+// of 64 in LDS and a shift of the exponent, the second by the polynomial of degree 4 (|f| <= 1/2: its remainder is below (ln 2 / 128)^5 / 120
+// = 4e-14).  15 instructions of 64 bits an element beside 3 of 32; with exp_neg, and the place of the maximum followed as it went, 34
+// (1280 rows of 151936 fp32 logits 250 us).
+template <typename T, bool VEC>
 __global__ __launch_bounds__(kPartThreads) void k_sample_parts(SampleArgs a) {
+    __shared__ double s_pow[64];
     __shared__ float s_top[4];
-    __shared__ int32_t s_at[4];
+    __shared__ int32_t s_at[4], s_bad[4];
     __shared__ double s_sum[4];
     const int r = blockIdx.y, b = r / (a.k + 1), i = r % (a.k + 1), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     const int v0 = blockIdx.x * kSeg;
-    const T* row = row_of<T>(a, b, i);
+    float x[kPer];
+    Segment<T, VEC>::load(row_of<T>(a, b, i), v0, a.vocab, tid, x);
     const double inv = inv_temperature(a, b);
     const int d = draft_of(a, b, i);
-    float x[kPer];
+    const bool greedy = is_greedy(a, b);
+    if (tid < 64) s_pow[tid] = exp_neg((tid - 64) * 1.0830424696249145e-02) * 2.0;      // 2^(tid / 64)
     float top = -__builtin_inff();
-    int at = 0x7FFFFFFF;
+    bool nan = inv != inv;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const int v = v0 + e * kPartThreads + tid;
-        x[e] = v < a.vocab ? to_f(row[v]) : -__builtin_inff();
-        if (x[e] > top) { top = x[e]; at = v; }
+    for (int e = 0; e < kPer; e += 2) {
+        top = fmaxf(top, fmaxf(x[e], x[e + 1]));
+        nan |= __builtin_isunordered(x[e], x[e + 1]);
     }
-    for (int o = 32; o > 0; o >>= 1) {
-        const float t = __shfl_xor(top, o);
-        const int32_t w = __shfl_xor(at, o);
-        if (t > top || (t == top && w < at)) { top = t; at = w; }
-    }
-    if (lane == 0) { s_top[wave] = top; s_at[wave] = at; }
+    top = wave_max(top);
+    const int32_t bad = __any(nan) ? 1 : 0;
+    if (lane == 0) { s_top[wave] = top; s_bad[wave] = bad; }
     __syncthreads();
-    for (int w = 0; w < 4; ++w)
-        if (s_top[w] > top || (s_top[w] == top && s_at[w] < at)) { top = s_top[w]; at = s_at[w]; }
-    // (nothing above -infinity in the segment: weights relative to 0 are zeros, and a NaN among them shows)
-    const double base = top == -__builtin_inff() ? 0.0 : (double)top;
+    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    const bool any_bad = (s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]) != 0 || top == __builtin_inff();
+    int32_t at = 0x7FFFFFFF;
+    if (greedy) {                                          // the lowest place of the maximum
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (x[e] == top) at = min(at, v0 + Segment<T, VEC>::place(e, tid));
+        for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o));
+        if (lane == 0) s_at[wave] = at;
+    }
+    if (d >= v0 && d < v0 + kSeg) {
+#pragma unroll
+        for (int e = 0; e < kPer; ++e)
+            if (v0 + Segment<T, VEC>::place(e, tid) == d) x[e] = -__builtin_inff();
+    }
+    const double base = top == -__builtin_inff() ? 0.0 : (double)top, unit = inv * 92.332482616893656877;    // 64 / ln 2
     double sum = 0.0;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-        const int v = v0 + e * kPartThreads + tid;
-        const double w = exp_neg(((double)x[e] - base) * inv);
-        sum += v == d ? (w != w ? w : 0.0) : w;
+        const double t = fmax(((double)x[e] - base) * unit, -64000.0), n = rint(t), f = t - n;     // (2^-1000: nothing either way)
+        const int m = (int)n;
+        double p = 0x1.3b2ab6fba4e77p-31;
+        p = __builtin_fma(p, f, 0x1.c6b08d704a0c0p-23);
+        p = __builtin_fma(p, f, 0x1.ebfbdff82c58fp-15);
+        p = __builtin_fma(p, f, 0x1.62e42fefa39efp-7);
+        p = __builtin_fma(p, f, 1.0);
+        sum += ldexp(p * s_pow[m & 63], m >> 6);
     }
     sum = wave_sum64(sum);
     if (lane == 0) s_sum[wave] = sum;
     __syncthreads();
-    if (tid == 0) a.parts[(int64_t)r * a.n_seg + blockIdx.x] = Part{(s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]), top, at};
+    if (tid == 0) {
+        sum = any_bad ? __builtin_nan("") : (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+        if (greedy) at = min(min(s_at[0], s_at[1]), min(s_at[2], s_at[3]));
+        a.parts[(int64_t)r * a.n_seg + blockIdx.x] = Part{sum, top, at};
+    }
 }
 
 // What a row comes to: Z = others + w(draft), log Z, and the decision on its draft
-struct Row { double top, others, z, logz; float draft_logp; int32_t best, draft; bool ok, accept; };
+struct Row { double top, others, z, logz; float draft_logp; int32_t best, draft; int32_t ok, accept; };
+// weight of a segment relative to the row's maximum
+__device__ __forceinline__ double scaled(const Part& q, double top, double inv) {
+    return q.top == -__builtin_inff() ? q.sum : q.sum * exp_neg(((double)q.top - top) * inv);
+}
 
 template <typename T>
-__device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int lane) {
+// own: the lane's segment (number `lane`) as `scaled` gives it
+__device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int lane, double& own) {
     Row o;
+    o.draft = draft_of(a, b, i);
+    const double inv = inv_temperature(a, b), chance = random_of(a, b, i, 0);
+    const float logit = o.draft >= 0 ? to_f(row_of<T>(a, b, i)[o.draft]) : 0.f;      // (on their way while the segments are joined)
+    const float prob = o.draft >= 0 && a.probs ? a.probs[((int64_t)b * a.k + i) * a.vocab + o.draft] : 1.f;
     const Part* p = a.parts + ((int64_t)b * (a.k + 1) + i) * a.n_seg;
     float top = -__builtin_inff();
     int32_t best = 0x7FFFFFFF;
+    Part mine{0.0, -__builtin_inff(), 0x7FFFFFFF};
+    if (lane < a.n_seg) mine = p[lane];
     for (int s = lane; s < a.n_seg; s += 64) {
-        const Part q = p[s];
+        const Part q = s == lane ? mine : p[s];
         if (q.top > top || (q.top == top && q.at < best)) { top = q.top; best = q.at; }
     }
     for (int f = 32; f > 0; f >>= 1) {
@@ -144,48 +200,47 @@ __device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int l
         const int32_t w = __shfl_xor(best, f);
         if (t > top || (t == top && w < best)) { top = t; best = w; }
     }
-    const double inv = inv_temperature(a, b);
-    double sum = 0.0;
-    for (int s = lane; s < a.n_seg; s += 64) {
-        const Part q = p[s];
-        sum += q.top == -__builtin_inff() ? q.sum : q.sum * exp_neg(((double)q.top - (double)top) * inv);
-    }
     o.top = top;
     o.best = best;
+    double sum = own = lane < a.n_seg ? scaled(mine, o.top, inv) : 0.0;
+    for (int s = lane + 64; s < a.n_seg; s += 64) sum += scaled(p[s], o.top, inv);
     o.others = wave_sum64(sum);
-    o.draft = draft_of(a, b, i);
-    const double x = o.draft >= 0 ? ((double)to_f(row_of<T>(a, b, i)[o.draft]) - o.top) * inv : 0.0;
-    const double w = o.draft >= 0 ? exp_neg(x) : 0.0;
+    const double x = o.draft >= 0 ? ((double)logit - o.top) * inv : 0.0, w = o.draft >= 0 ? exp_neg(x) : 0.0;
     o.z = o.others + w;
     o.ok = o.z > 0.0 && o.z < __builtin_inf();
-    o.logz = log(o.z);
-    o.draft_logp = (float)(x - o.logz);
-    const double q = o.draft >= 0 && a.probs ? (double)a.probs[((int64_t)b * a.k + i) * a.vocab + o.draft] : 1.0;
-    o.accept = o.ok && o.draft >= 0 && random_of(a, b, i, 0) * q * o.z < w;
-    if (is_greedy(a, b)) {
-        o.accept = o.ok && o.draft == o.best && random_of(a, b, i, 0) * q < 1.0;
+    const bool greedy = is_greedy(a, b);
+    if (greedy) {
+        o.accept = o.ok && o.draft == o.best && chance * (double)prob < 1.0;
         o.draft_logp = 0.f;
         o.logz = 0.0;
+    } else {
+        o.accept = o.ok && o.draft >= 0 && chance * (double)prob * o.z < w;
+        o.logz = log(o.z);
+        o.draft_logp = (float)(x - o.logz);
     }
     return o;
+}
+
+// Given q: every row's decision, which the two kernels behind it look up
+template <typename T>
+__global__ __launch_bounds__(64) void k_sample_decide(SampleArgs a) {
+    const int r = blockIdx.x;
+    double own;
+    const Row o = join_row<T>(a, r / (a.k + 1), r % (a.k + 1), threadIdx.x, own);
+    if (threadIdx.x == 0) a.decided[r] = o;
 }
 
 // sum max(0, p - q) over a segment of the row that rejected its draft (others write nothing that is read)
 template <typename T>
 __global__ __launch_bounds__(kPartThreads) void k_sample_residual(SampleArgs a) {
-    __shared__ Row s_row[TASC_MAX_K + 1];
     __shared__ double s_sum[4];
     const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (is_greedy(a, b)) return;
-    for (int i = wave; i <= a.k; i += 4) {
-        const Row o = join_row<T>(a, b, i, lane);
-        if (lane == 0) s_row[i] = o;
-    }
-    __syncthreads();
+    const Row* rows = a.decided + (int64_t)b * (a.k + 1);
     int m = 0;
-    while (m <= a.k && s_row[m].accept) ++m;
-    if (m >= a.k || s_row[m].draft < 0 || !s_row[m].ok) return;
-    const Row o = s_row[m];
+    while (m < a.k && rows[m].accept) ++m;
+    const Row o = rows[m];
+    if (m >= a.k || o.draft < 0 || !o.ok) return;
     const T* row = row_of<T>(a, b, m);
     const float* q = a.probs + ((int64_t)b * a.k + m) * a.vocab;
     const double inv = inv_temperature(a, b), inv_z = 1.0 / o.z;
@@ -222,8 +277,11 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
         }
         return;
     }
+    double own = 0.0;                                       // of the wave's row: the lane's segment
     if (wave < nq) {
-        const Row o = join_row<T>(a, b, wave, lane);
+        Row o;
+        if (a.probs) o = a.decided[(int64_t)b * nq + wave];
+        else o = join_row<T>(a, b, wave, lane, own);
         if (lane == 0) s_row[wave] = o;
     }
     __syncthreads();
@@ -242,13 +300,12 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
         const Part* p = a.parts + ((int64_t)b * nq + m) * a.n_seg;
         const double* res = a.residual + (int64_t)b * a.n_seg;
         // which weights: 0 w, 1 w without the draft, 2 max(0, p - q); what a rejection leaves may round to nothing: then w
-        if (wave == 0) {
+        if (wave == m) {
             int kind = o.draft < 0 ? 0 : a.probs ? 2 : 1;
             auto seg_sum = [&](int s) {
                 if (s >= a.n_seg) return 0.0;
                 if (kind == 2) return res[s];
-                const Part q = p[s];
-                double v = q.top == -__builtin_inff() ? 0.0 : q.sum * exp_neg(((double)q.top - o.top) * inv);
+                double v = s == lane && !a.probs ? own : scaled(p[s], o.top, inv);
                 if (kind == 0 && o.draft >= 0 && o.draft / kSeg == s) v += o.z - o.others;
                 return v;
             };
@@ -366,13 +423,21 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
     atomicAdd(&a.d.counters[8 + m], 1ull);
 }
 
+// the workspace: parts, decisions, residual sums
 size_t parts_bytes(int batch, int k, int n_seg) { return (size_t)batch * (k + 1) * n_seg * sizeof(Part); }
+size_t decided_bytes(int batch, int k) { return (size_t)batch * (k + 1) * sizeof(Row); }
 int segments(int vocab) { return (vocab + kSeg - 1) / kSeg; }
 
 template <typename T>
 tasc_status enqueue(const SampleArgs& a, int batch, hipStream_t st) {
-    k_sample_parts<T><<<dim3((unsigned)a.n_seg, (unsigned)(batch * (a.k + 1))), dim3(kPartThreads), 0, st>>>(a);
-    if (a.probs && a.k > 0) k_sample_residual<T><<<dim3((unsigned)a.n_seg, (unsigned)batch), dim3(kPartThreads), 0, st>>>(a);
+    const bool vec = (((uintptr_t)a.logits | (uintptr_t)(a.row_stride * (int64_t)sizeof(T))) & 15) == 0;
+    const dim3 grid((unsigned)a.n_seg, (unsigned)(batch * (a.k + 1)));
+    if (vec) k_sample_parts<T, true><<<grid, dim3(kPartThreads), 0, st>>>(a);
+    else k_sample_parts<T, false><<<grid, dim3(kPartThreads), 0, st>>>(a);
+    if (a.probs) {
+        k_sample_decide<T><<<dim3((unsigned)(batch * (a.k + 1))), dim3(64), 0, st>>>(a);
+        k_sample_residual<T><<<dim3((unsigned)a.n_seg, (unsigned)batch), dim3(kPartThreads), 0, st>>>(a);
+    }
     k_sample_pick<T><<<dim3((unsigned)batch), dim3(kPickThreads), 0, st>>>(a);
     TASC_LAUNCH_CHECK();
     return TASC_OK;
@@ -382,7 +447,7 @@ tasc_status enqueue(const SampleArgs& a, int batch, hipStream_t st) {
 
 extern "C" size_t tasc_accept_sampled_workspace_bytes(int32_t batch, int32_t k, int32_t vocab) {
     if (batch < 1 || k < 0 || k > TASC_MAX_K || vocab < 2 || vocab > 1 << 24) return 0;
-    return parts_bytes(batch, k, segments(vocab)) + (size_t)batch * segments(vocab) * sizeof(double);
+    return parts_bytes(batch, k, segments(vocab)) + decided_bytes(batch, k) + (size_t)batch * segments(vocab) * sizeof(double);
 }
 
 extern "C" tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab, const int32_t* drafts,
@@ -403,8 +468,9 @@ extern "C" tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype,
     }
     TASC_REQUIRE(((uintptr_t)workspace & 15) == 0, "accept_sampled: the workspace must be 16-byte aligned");
     const int n_seg = segments(vocab);
-    const SampleArgs a{logits, row_stride, k, vocab, n_seg, drafts, draft_probs, temperature, u, k + 1, nullptr, (Part*)workspace,
-                       (double*)((char*)workspace + parts_bytes(batch, k, n_seg)), accept_len, emitted, logprob, TascSessDev{}, 0};
+    const SampleArgs a{logits, row_stride, k, vocab, n_seg, drafts, k > 0 ? draft_probs : nullptr, temperature, u, k + 1, nullptr, (Part*)workspace,
+                       (Row*)((char*)workspace + parts_bytes(batch, k, n_seg)),
+                       (double*)((char*)workspace + parts_bytes(batch, k, n_seg) + decided_bytes(batch, k)), accept_len, emitted, logprob, TascSessDev{}, 0};
     return dtype == TASC_F32 ? enqueue<float>(a, batch, (hipStream_t)stream) : enqueue<BF16>(a, batch, (hipStream_t)stream);
 }
 
@@ -413,7 +479,7 @@ size_t tasc_sample_logits_bytes(int32_t batch, int32_t k, int32_t vocab) { retur
 tasc_status tasc_sample_step(const tasc_session* s, const TascVerifyTail& t, hipStream_t st) {
     const int vocab = s->model->desc.vocab;
     const TascSampled& p = *t.sampled;
-    const SampleArgs a{p.logits, vocab, t.k, vocab, segments(vocab), t.drafts, nullptr, p.temperature, p.u, p.n_u, s->d.n_emit, (Part*)p.parts, nullptr,
+    const SampleArgs a{p.logits, vocab, t.k, vocab, segments(vocab), t.drafts, nullptr, p.temperature, p.u, p.n_u, s->d.n_emit, (Part*)p.parts, nullptr, nullptr,
                        t.accept_len, t.emitted, p.logprob, s->d, s->max_len};
     return enqueue<float>(a, s->batch, st);
 }
