@@ -1,6 +1,7 @@
 // Storage types, vector loads and wave sums that the kernels share.
 #pragma once
 #include "tasc_internal.h"
+#include <type_traits>
 
 struct BF16 { uint16_t v; };
 
@@ -65,4 +66,29 @@ __device__ __forceinline__ float wave_sum_dpp(float v) {
     const float r2 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 32));
     const float r3 = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), 48));
     return (r0 + r1) + (r2 + r3);
+}
+// The same for a maximum, and for a sum of 64 bits
+__device__ __forceinline__ float wave_max_dpp(float v) {
+    auto up = [](float x, auto ctrl) { return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false))); };
+    v = up(v, std::integral_constant<int, 0xB1>{});
+    v = up(v, std::integral_constant<int, 0x4E>{});
+    v = up(v, std::integral_constant<int, 0x141>{});
+    v = up(v, std::integral_constant<int, 0x140>{});
+    auto row = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); };
+    return fmaxf(fmaxf(row(0), row(16)), fmaxf(row(32), row(48)));
+}
+__device__ __forceinline__ double wave_sum64_dpp(double v) {
+    auto up = [](double x, auto ctrl) {
+        const u64 b = __builtin_bit_cast(u64, x);
+        const u32 lo = __builtin_amdgcn_update_dpp(0, (int)(u32)b, decltype(ctrl)::value, 0xF, 0xF, false);
+        const u32 hi = __builtin_amdgcn_update_dpp(0, (int)(u32)(b >> 32), decltype(ctrl)::value, 0xF, 0xF, false);
+        return x + __builtin_bit_cast(double, (u64)hi << 32 | lo);
+    };
+    v = up(v, std::integral_constant<int, 0xB1>{});
+    v = up(v, std::integral_constant<int, 0x4E>{});
+    v = up(v, std::integral_constant<int, 0x141>{});
+    v = up(v, std::integral_constant<int, 0x140>{});
+    const u64 b = __builtin_bit_cast(u64, v);
+    auto row = [&](int l) { return __builtin_bit_cast(double, (u64)(u32)__builtin_amdgcn_readlane((int)(u32)(b >> 32), l) << 32 | (u32)__builtin_amdgcn_readlane((int)(u32)b, l)); };
+    return (row(0) + row(16)) + (row(32) + row(48));
 }

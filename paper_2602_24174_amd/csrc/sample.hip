@@ -17,9 +17,12 @@
 
 namespace {
 
-constexpr int kSeg = 4096, kPartThreads = 256, kPer = kSeg / kPartThreads, kPickThreads = 1024;
+typedef uint32_t word2 __attribute__((ext_vector_type(2)));
+constexpr int kSeg = 4096, kPartThreads = 256, kPer = kSeg / kPartThreads, kPickThreads = 1024, kMostSegs = 8;
 
-struct __attribute__((aligned(16))) Part { double sum; float top; int32_t at; };   // sum: relative to top, without the row's draft
+// A segment: sum of its weights, without the row's draft, in units of exp(scale) (-infinity: nothing above -infinity in it), its largest logit
+// and, of a greedy sequence, that one's lowest place
+struct __attribute__((aligned(16))) Part { double sum, scale; float top; int32_t at; };
 
 struct Row;
 struct SampleArgs {
@@ -45,7 +48,7 @@ __device__ __forceinline__ double random_of(const SampleArgs& a, int b, int i, i
     return (double)a.u[2 * (b * a.n_u + pair) + which];
 }
 
-// exp(x) for x <= 0 (NaN stays one): x = n ln 2 + r, |r| <= ln 2 / 2, and the Taylor polynomial of degree 11, whose remainder is below
+// exp(x) for x <= 1 (NaN stays one): x = n ln 2 + r, |r| <= ln 2 / 2, and the Taylor polynomial of degree 11, whose remainder is below
 // (ln 2 / 2)^12 / 12! = 6.3e-15
 __device__ __forceinline__ double exp_neg(double x) {
     x = x < -1000.0 ? -1000.0 : x;                         // (an underflow either way; -infinity has no n)
@@ -76,16 +79,18 @@ __device__ __forceinline__ int draft_of(const SampleArgs& a, int b, int i) {    
     const int d = i < a.k ? a.drafts[(int64_t)b * a.k + i] : -1;
     return d >= 0 && d < a.vocab ? d : -1;
 }
+// a logit over the temperature, in the units of a row's weights; the product is rounded as the scale's own was, so that equal logits
+// come out equal however large they are
+__device__ __forceinline__ double exponent(float logit, double inv, double scale) {
+#pragma clang fp contract(off)
+    const double y = (double)logit * inv;
+    return y - scale;
+}
 template <typename T>
 __device__ __forceinline__ const T* row_of(const SampleArgs& a, int b, int i) {
     return (const T*)a.logits + ((int64_t)b * (a.k + 1) + i) * a.row_stride;
 }
-__device__ __forceinline__ double wave_sum64(double v) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-
-// 16 logits of a segment: VEC, 16 bytes side by side at a time (rows start at multiples of 16 bytes), else thread by thread
+// A thread's 16 logits of a segment: VEC, 16 bytes side by side at a time (rows start at multiples of 16 bytes), else thread by thread
 template <typename T, bool VEC>
 struct Segment {
     static constexpr int SIDE = VEC ? 16 / (int)sizeof(T) : 1;
@@ -104,79 +109,140 @@ struct Segment {
     }
 };
 
-// What bounds it is the exponentials, 16 a thread: exp(y) = 2^(i / 64) exp(f ln 2 / 64) with i = rint(64 y / ln 2), the first factor out of a table
-// of 64 in LDS and a shift of the exponent, the second by the polynomial of degree 4 (|f| <= 1/2: its remainder is below (ln 2 / 128)^5 / 120
-// = 4e-14).  15 instructions of 64 bits an element beside 3 of 32; with exp_neg, and the place of the maximum followed as it went, 34
-// (1280 rows of 151936 fp32 logits 250 us).
-template <typename T, bool VEC>
-__global__ __launch_bounds__(kPartThreads) void k_sample_parts(SampleArgs a) {
-    __shared__ double s_pow[64];
-    __shared__ float s_top[4];
-    __shared__ int32_t s_at[4], s_bad[4];
-    __shared__ double s_sum[4];
+// What bounds it is the exponentials, 16 a thread and segment: exp(y) = 2^(i / 256) exp(f ln 2 / 256) with i = rint(256 y / ln 2), the first factor out of a
+// table of 256 in LDS with i / 256 added to its exponent, the second by the polynomial of degree 3 (|f| <= 1/2: its remainder is below
+// (ln 2 / 512)^4 / 24 = 1.4e-13).  A wave's weights are relative to the power of 2^(1/256) next to its largest, so that y = x / temperature - i' ln 2 / 256
+// takes one fma, the rounding is the addition of 1.5 2^52 in another, which leaves i in the lower word, and the table has i's lower bits
+// taken out of its exponents before: 10 instructions an element (rint, conversion and ldexp have a quarter of the rate of a product).
+// Waves that hold logits too far from their largest for that (masked ones, say), or so large that 2^-53 of them counts, take the loop behind it.
+// us of 1280 rows of 151936 fp32 logits: exp_neg, with the place of the maximum followed as it went, 250; a table of 64, rint, a
+// conversion and ldexp 169; the second loop for all waves 151.
+// 2^(i / 256), by the series of the exponential
+constexpr double pow2_256(int i) {
+    const double x = i * (0.69314718055994530942 / 256);
+    double sum = 1.0, term = 1.0;
+    for (int k = 1; k < 30; ++k) sum += term *= x / k;
+    return sum;
+}
+struct PowTable { word2 at[256]; };                   // lower word, upper word less i << 12 (what i adds there beside i / 256 << 20)
+constexpr PowTable pow_table() {
+    PowTable t{};
+    for (int i = 0; i < 256; ++i) {
+        const u64 b = __builtin_bit_cast(u64, pow2_256(i));
+        t.at[i] = word2{(u32)b, (u32)(b >> 32) - ((u32)i << 12)};
+    }
+    return t;
+}
+__device__ const PowTable kPow = pow_table();
+// p 2^(m / 256)
+__device__ __forceinline__ double times_power(const word2* pow, double p, u32 m, double plus) {
+    const word2 w = pow[m & 255];
+    return __builtin_fma(p, __builtin_bit_cast(double, word2{w[0], w[1] + (m << 12)}), plus);
+}
+__device__ __forceinline__ double small_power(double f) {  // 2^(f / 256)
+    double p = 0x1.c6b08d704a0c0p-29;
+    p = __builtin_fma(p, f, 0x1.ebfbdff82c58fp-19);
+    p = __builtin_fma(p, f, 0x1.62e42fefa39efp-9);
+    return __builtin_fma(p, f, 1.0);
+}
+
+// SEVERAL: a workgroup takes kMostSegs segments side by side, the next one's logits under way while one's exponentials are computed, and its
+// waves do not wait for each other before the last; the registers for it cost three of seven waves a SIMD.
+template <typename T, bool VEC, bool SEVERAL>
+__global__ __launch_bounds__(kPartThreads) __attribute__((amdgpu_waves_per_eu(SEVERAL ? 4 : 6))) void k_sample_parts(SampleArgs a) {
+    using S = Segment<T, VEC>;
+    constexpr int kWaves = kPartThreads / 64, kMost = SEVERAL ? kMostSegs : 1;
+    __shared__ word2 s_pow[256];
+    __shared__ float s_top[kMost * kWaves];
+    __shared__ int32_t s_at[kMost * kWaves];
+    __shared__ double s_sum[kMost * kWaves], s_scale[kMost * kWaves];
     const int r = blockIdx.y, b = r / (a.k + 1), i = r % (a.k + 1), tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
-    const int v0 = blockIdx.x * kSeg;
-    float x[kPer];
-    Segment<T, VEC>::load(row_of<T>(a, b, i), v0, a.vocab, tid, x);
-    const double inv = inv_temperature(a, b);
+    const int s0 = blockIdx.x * kMost, n = SEVERAL ? min(kMost, a.n_seg - s0) : 1;
+    const T* const row = row_of<T>(a, b, i);
+    float next[kPer];
+    S::load(row, s0 * kSeg, a.vocab, tid, next);
+    static_assert(kPartThreads == 256, "a thread an entry");
+    s_pow[tid] = kPow.at[tid];
+    const double inv = inv_temperature(a, b), unit = inv * 369.3299304675746;     // 256 / ln 2
     const int d = draft_of(a, b, i);
     const bool greedy = is_greedy(a, b);
-    if (tid < 64) s_pow[tid] = exp_neg((tid - 64) * 1.0830424696249145e-02) * 2.0;      // 2^(tid / 64)
-    float top = -__builtin_inff();
-    bool nan = inv != inv;
-#pragma unroll
-    for (int e = 0; e < kPer; e += 2) {
-        top = fmaxf(top, fmaxf(x[e], x[e + 1]));
-        nan |= __builtin_isunordered(x[e], x[e + 1]);
-    }
-    top = wave_max(top);
-    const int32_t bad = __any(nan) ? 1 : 0;
-    if (lane == 0) { s_top[wave] = top; s_bad[wave] = bad; }
     __syncthreads();
-    top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
-    const bool any_bad = (s_bad[0] | s_bad[1] | s_bad[2] | s_bad[3]) != 0 || top == __builtin_inff();
-    int32_t at = 0x7FFFFFFF;
-    if (greedy) {                                          // the lowest place of the maximum
+    for (int g = 0; g < n; ++g) {
+        const int v0 = (s0 + g) * kSeg;
+        float x[kPer];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (x[e] == top) at = min(at, v0 + Segment<T, VEC>::place(e, tid));
-        for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o));
-        if (lane == 0) s_at[wave] = at;
-    }
-    if (d >= v0 && d < v0 + kSeg) {
+        for (int e = 0; e < kPer; ++e) x[e] = next[e];
+        if (SEVERAL && g + 1 < n) S::load(row, v0 + kSeg, a.vocab, tid, next);
+        float top = x[0], least = x[0];
 #pragma unroll
-        for (int e = 0; e < kPer; ++e)
-            if (v0 + Segment<T, VEC>::place(e, tid) == d) x[e] = -__builtin_inff();
-    }
-    const double base = top == -__builtin_inff() ? 0.0 : (double)top, unit = inv * 92.332482616893656877;    // 64 / ln 2
-    double sum = 0.0;
+        for (int e = 0; e < kPer; e += 2) {                 // (fmaxf would quiet its operands first; a NaN is left out by either)
+            asm("v_max3_f32 %0, %1, %2, %3" : "=v"(top) : "v"(top), "v"(x[e]), "v"(x[e + 1]));
+            asm("v_min3_f32 %0, %1, %2, %3" : "=v"(least) : "v"(least), "v"(x[e]), "v"(x[e + 1]));
+        }
+        top = wave_max_dpp(top);
+        const int place = g * kWaves + wave;
+        if (greedy) {                                       // the lowest place of the maximum
+            int32_t at = 0x7FFFFFFF;
 #pragma unroll
-    for (int e = 0; e < kPer; ++e) {
-        const double t = fmax(((double)x[e] - base) * unit, -64000.0), n = rint(t), f = t - n;     // (2^-1000: nothing either way)
-        const int m = (int)n;
-        double p = 0x1.3b2ab6fba4e77p-31;
-        p = __builtin_fma(p, f, 0x1.c6b08d704a0c0p-23);
-        p = __builtin_fma(p, f, 0x1.ebfbdff82c58fp-15);
-        p = __builtin_fma(p, f, 0x1.62e42fefa39efp-7);
-        p = __builtin_fma(p, f, 1.0);
-        sum += ldexp(p * s_pow[m & 63], m >> 6);
+            for (int e = 0; e < kPer; ++e)
+                if (x[e] == top) at = min(at, v0 + S::place(e, tid));
+            for (int o = 32; o > 0; o >>= 1) at = min(at, __shfl_xor(at, o));
+            if (lane == 0) s_at[place] = at;
+        }
+        const double whole = rint((double)top * unit);
+        double sum = 0.0, scale;
+        // (conditions that a NaN fails: such a wave takes the second loop, and so do those of the draft's segment)
+        if (!__any(!((double)least * unit > whole - 600.0 * 369.0)) && fabs(whole) < 0x1p24 && (d < v0 || d >= v0 + kSeg)) {
+            const double start = 0x1.8p52 - whole;
+            scale = whole * (0.69314718055994530942 / 256);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const double y = (double)x[e], big = __builtin_fma(y, unit, start);
+                sum = times_power(s_pow, small_power(__builtin_fma(y, unit, start - big)), (u32)__builtin_bit_cast(u64, big), sum);
+            }
+        } else {
+            // y is no less than -1023 ln 2, where an entry's exponent and mantissa come out as zero: a masked token weighs exactly nothing
+            const double base = top == -__builtin_inff() ? 0.0 : (double)top;
+            scale = top == -__builtin_inff() ? -__builtin_inf() : base * inv;
+            bool nan = inv != inv || top == __builtin_inff();
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                nan |= x[e] != x[e];
+                const double t = fmax(((double)x[e] - base) * unit, -1023.0 * 256.0), big = t + 0x1.8p52;
+                const bool none = v0 + S::place(e, tid) == d || x[e] == -__builtin_inff();
+                sum += none ? 0.0 : times_power(s_pow, small_power(t - (big - 0x1.8p52)), (u32)__builtin_bit_cast(u64, big), 0.0);
+            }
+            if (nan) sum = __builtin_nan("");
+        }
+        sum = wave_sum64_dpp(sum);
+        if (lane == 0) {
+            s_top[place] = top;
+            s_sum[place] = sum;
+            s_scale[place] = scale;
+        }
     }
-    sum = wave_sum64(sum);
-    if (lane == 0) s_sum[wave] = sum;
     __syncthreads();
-    if (tid == 0) {
-        sum = any_bad ? __builtin_nan("") : (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
-        if (greedy) at = min(min(s_at[0], s_at[1]), min(s_at[2], s_at[3]));
-        a.parts[(int64_t)r * a.n_seg + blockIdx.x] = Part{sum, top, at};
-    }
+    // a segment's four waves joined by four lanes
+    if (tid >= n * kWaves) return;
+    float top = s_top[tid];
+    double scale = s_scale[tid], sum = s_sum[tid];
+    top = fmaxf(top, __shfl_xor(top, 1));
+    top = fmaxf(top, __shfl_xor(top, 2));
+    double most = fmax(scale, __shfl_xor(scale, 1));
+    most = fmax(most, __shfl_xor(most, 2));
+    if (scale != -__builtin_inf()) sum *= exp_neg(scale - most);
+    sum += __shfl_xor(sum, 2);
+    sum += __shfl_xor(sum, 1);
+    int32_t at = greedy && s_top[tid] == top ? s_at[tid] : 0x7FFFFFFF;
+    at = min(at, __shfl_xor(at, 1));
+    at = min(at, __shfl_xor(at, 2));
+    if (tid % kWaves == 0) a.parts[(int64_t)r * a.n_seg + s0 + tid / kWaves] = Part{sum, most, top, at};
 }
 
 // What a row comes to: Z = others + w(draft), log Z, and the decision on its draft
-struct Row { double top, others, z, logz; float draft_logp; int32_t best, draft; int32_t ok, accept; };
-// weight of a segment relative to the row's maximum
-__device__ __forceinline__ double scaled(const Part& q, double top, double inv) {
-    return q.top == -__builtin_inff() ? q.sum : q.sum * exp_neg(((double)q.top - top) * inv);
-}
+struct Row { double scale, others, z, logz; float draft_logp; int32_t best, draft; int32_t ok, accept; };
+// weight of a segment in units of exp(scale)
+__device__ __forceinline__ double scaled(const Part& q, double scale) { return q.scale == -__builtin_inf() ? q.sum : q.sum * exp_neg(q.scale - scale); }
 
 template <typename T>
 // own: the lane's segment (number `lane`) as `scaled` gives it
@@ -189,10 +255,12 @@ __device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int l
     const Part* p = a.parts + ((int64_t)b * (a.k + 1) + i) * a.n_seg;
     float top = -__builtin_inff();
     int32_t best = 0x7FFFFFFF;
-    Part mine{0.0, -__builtin_inff(), 0x7FFFFFFF};
+    double scale = -__builtin_inf();
+    Part mine{0.0, -__builtin_inf(), -__builtin_inff(), 0x7FFFFFFF};
     if (lane < a.n_seg) mine = p[lane];
     for (int s = lane; s < a.n_seg; s += 64) {
         const Part q = s == lane ? mine : p[s];
+        scale = fmax(scale, q.scale);
         if (q.top > top || (q.top == top && q.at < best)) { top = q.top; best = q.at; }
     }
     for (int f = 32; f > 0; f >>= 1) {
@@ -200,12 +268,13 @@ __device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int l
         const int32_t w = __shfl_xor(best, f);
         if (t > top || (t == top && w < best)) { top = t; best = w; }
     }
-    o.top = top;
+    for (int f = 32; f > 0; f >>= 1) scale = fmax(scale, __shfl_xor(scale, f));
+    o.scale = scale;
     o.best = best;
-    double sum = own = lane < a.n_seg ? scaled(mine, o.top, inv) : 0.0;
-    for (int s = lane + 64; s < a.n_seg; s += 64) sum += scaled(p[s], o.top, inv);
-    o.others = wave_sum64(sum);
-    const double x = o.draft >= 0 ? ((double)logit - o.top) * inv : 0.0, w = o.draft >= 0 ? exp_neg(x) : 0.0;
+    double sum = own = lane < a.n_seg ? scaled(mine, scale) : 0.0;
+    for (int s = lane + 64; s < a.n_seg; s += 64) sum += scaled(p[s], scale);
+    o.others = wave_sum64_dpp(sum);
+    const double x = o.draft >= 0 ? exponent(logit, inv, scale) : 0.0, w = o.draft >= 0 ? exp_neg(x) : 0.0;
     o.z = o.others + w;
     o.ok = o.z > 0.0 && o.z < __builtin_inf();
     const bool greedy = is_greedy(a, b);
@@ -231,32 +300,43 @@ __global__ __launch_bounds__(64) void k_sample_decide(SampleArgs a) {
 }
 
 // sum max(0, p - q) over a segment of the row that rejected its draft (others write nothing that is read)
-template <typename T>
+template <typename T, bool VEC>
 __global__ __launch_bounds__(kPartThreads) void k_sample_residual(SampleArgs a) {
-    __shared__ double s_sum[4];
+    using S = Segment<T, VEC>;
+    __shared__ word2 s_pow[256];
+    __shared__ double s_sum[kPartThreads / 64];
     const int b = blockIdx.y, tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if (is_greedy(a, b)) return;
     const Row* rows = a.decided + (int64_t)b * (a.k + 1);
-    int m = 0;
-    while (m < a.k && rows[m].accept) ++m;
+    const u64 stops = __ballot(lane >= a.k || !rows[min(lane, a.k)].accept);
+    const int m = __builtin_amdgcn_readfirstlane(__ffsll((unsigned long long)stops) - 1);
     const Row o = rows[m];
     if (m >= a.k || o.draft < 0 || !o.ok) return;
-    const T* row = row_of<T>(a, b, m);
-    const float* q = a.probs + ((int64_t)b * a.k + m) * a.vocab;
+    float x[kPer], q[kPer];
+    S::load(row_of<T>(a, b, m), blockIdx.x * kSeg, a.vocab, tid, x);
+    const float* probs = a.probs + ((int64_t)b * a.k + m) * a.vocab;
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) {
+        const int v = blockIdx.x * kSeg + S::place(e, tid);
+        q[e] = v < a.vocab ? probs[v] : 0.f;
+    }
+    s_pow[tid] = kPow.at[tid];
+    __syncthreads();
     const double inv = inv_temperature(a, b), inv_z = 1.0 / o.z;
     double sum = 0.0;
 #pragma unroll
     for (int e = 0; e < kPer; ++e) {
-        const int v = blockIdx.x * kSeg + e * kPartThreads + tid;
-        if (v < a.vocab) sum += fmax(exp_neg(((double)to_f(row[v]) - o.top) * inv) * inv_z - (double)q[v], 0.0);
+        const double t = fmax(exponent(x[e], inv, o.scale) * 369.3299304675746, -1023.0 * 256.0), big = t + 0x1.8p52;      // (as in k_sample_parts' second loop)
+        const double w = times_power(s_pow, small_power(t - (big - 0x1.8p52)), (u32)__builtin_bit_cast(u64, big), 0.0);
+        sum += fmax(w * inv_z - (double)q[e], 0.0);
     }
-    sum = wave_sum64(sum);
+    sum = wave_sum64_dpp(sum);
     if (lane == 0) s_sum[wave] = sum;
     __syncthreads();
     if (tid == 0) a.residual[(int64_t)b * a.n_seg + blockIdx.x] = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
 }
 
-template <typename T>
+template <typename T, bool VEC>
 __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
     __shared__ Row s_row[TASC_MAX_K + 1];
     __shared__ double s_wave[16];
@@ -305,7 +385,7 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
             auto seg_sum = [&](int s) {
                 if (s >= a.n_seg) return 0.0;
                 if (kind == 2) return res[s];
-                double v = s == lane && !a.probs ? own : scaled(p[s], o.top, inv);
+                double v = s == lane && !a.probs ? own : scaled(p[s], o.scale);
                 if (kind == 0 && o.draft >= 0 && o.draft / kSeg == s) v += o.z - o.others;
                 return v;
             };
@@ -313,7 +393,7 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
             for (int pass = 0; pass < 2; ++pass) {
                 total = 0.0;
                 for (int s = lane; s < a.n_seg; s += 64) total += seg_sum(s);
-                total = wave_sum64(total);
+                total = wave_sum64_dpp(total);
                 if (total > 0.0) break;
                 kind = 0;
             }
@@ -352,14 +432,24 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
         const T* row = row_of<T>(a, b, m);
         const double inv_z = 1.0 / o.z;
         const float* q = kind == 2 ? a.probs + ((int64_t)b * a.k + m) * a.vocab : nullptr;
-        double w[4], x[4], mine = 0.0;
+        constexpr int SPAN = kSeg / kPickThreads;
+        const int v0 = seg * kSeg + SPAN * tid;
+        float logit[SPAN];
+        if (VEC && v0 + SPAN <= a.vocab) {
+            load_n<SPAN>(row + v0, logit);
+        } else {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const int v = seg * kSeg + 4 * tid + e;
-            x[e] = v < a.vocab ? ((double)to_f(row[v]) - o.top) * inv : -1000.0;
-            w[e] = v < a.vocab ? exp_neg(x[e]) : 0.0;
+            for (int e = 0; e < SPAN; ++e) logit[e] = v0 + e < a.vocab ? to_f(row[v0 + e]) : -__builtin_inff();
+        }
+        double w[SPAN], x[SPAN], mine = 0.0;
+#pragma unroll
+        for (int e = 0; e < SPAN; ++e) {
+            const int v = v0 + e;
+            const bool in = v < a.vocab;
+            x[e] = exponent(logit[e], inv, o.scale);
+            w[e] = logit[e] == -__builtin_inff() ? 0.0 : exp_neg(x[e]);
             if (kind == 1 && v == o.draft) w[e] = 0.0;
-            if (kind == 2 && v < a.vocab) w[e] = fmax(w[e] * inv_z - (double)q[v], 0.0);
+            if (kind == 2 && in) w[e] = fmax(w[e] * inv_z - (double)q[v], 0.0);
             mine += w[e];
         }
         double up = mine;
@@ -373,9 +463,9 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
         for (int i = 0; i < wave; ++i) sum += s_wave[i];
         int first = 0x7FFFFFFF, last = -1;                  // the first token past the target, the last with any weight
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
+        for (int e = 0; e < SPAN; ++e) {
             sum += w[e];
-            const int v = seg * kSeg + 4 * tid + e;
+            const int v = v0 + e;
             if (w[e] > 0.0) {
                 last = v;
                 if (sum > s_target && first == 0x7FFFFFFF) first = v;
@@ -392,11 +482,9 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
             last = max(last, s_last[i]);
         }
         token = first != 0x7FFFFFFF ? first : last;
-        if (token >= 0 && (token - seg * kSeg) / 4 == tid) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-                if (token == seg * kSeg + 4 * tid + e) s_x = x[e];
-        }
+        for (int e = 0; e < SPAN; ++e)
+            if (token == v0 + e) s_x = x[e];
         __syncthreads();
         if (token >= 0) logp = (float)(s_x - o.logz);
     }
@@ -426,19 +514,26 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
 // the workspace: parts, decisions, residual sums
 size_t parts_bytes(int batch, int k, int n_seg) { return (size_t)batch * (k + 1) * n_seg * sizeof(Part); }
 size_t decided_bytes(int batch, int k) { return (size_t)batch * (k + 1) * sizeof(Row); }
-int segments(int vocab) { return (vocab + kSeg - 1) / kSeg; }
+int segments(int vocab) { return (vocab - 1) / kSeg + 1; }
+// Several segments a workgroup from four rounds of them on (us of a call, one | several a workgroup: 1280 rows of 151936 fp32 logits 163 | 154,
+// 640 84 | 85, 224 of bf16, with draft probabilities, 51 | 55).
+bool several_segments(int64_t rows, int n_seg) { return rows * n_seg >= 24576; }
 
 template <typename T>
 tasc_status enqueue(const SampleArgs& a, int batch, hipStream_t st) {
     const bool vec = (((uintptr_t)a.logits | (uintptr_t)(a.row_stride * (int64_t)sizeof(T))) & 15) == 0;
-    const dim3 grid((unsigned)a.n_seg, (unsigned)(batch * (a.k + 1)));
-    if (vec) k_sample_parts<T, true><<<grid, dim3(kPartThreads), 0, st>>>(a);
-    else k_sample_parts<T, false><<<grid, dim3(kPartThreads), 0, st>>>(a);
+    const bool several = several_segments((int64_t)batch * (a.k + 1), a.n_seg);
+    const int per = several ? kMostSegs : 1;
+    const dim3 grid((unsigned)((a.n_seg + per - 1) / per), (unsigned)(batch * (a.k + 1))), threads(kPartThreads);
+    auto parts = several ? (vec ? &k_sample_parts<T, true, true> : &k_sample_parts<T, false, true>) : (vec ? &k_sample_parts<T, true, false> : &k_sample_parts<T, false, false>);
+    parts<<<grid, threads, 0, st>>>(a);
     if (a.probs) {
+        const dim3 of((unsigned)a.n_seg, (unsigned)batch);
         k_sample_decide<T><<<dim3((unsigned)(batch * (a.k + 1))), dim3(64), 0, st>>>(a);
-        k_sample_residual<T><<<dim3((unsigned)a.n_seg, (unsigned)batch), dim3(kPartThreads), 0, st>>>(a);
+        vec ? k_sample_residual<T, true><<<of, threads, 0, st>>>(a) : k_sample_residual<T, false><<<of, threads, 0, st>>>(a);
     }
-    k_sample_pick<T><<<dim3((unsigned)batch), dim3(kPickThreads), 0, st>>>(a);
+    const dim3 seqs((unsigned)batch), many(kPickThreads);
+    vec ? k_sample_pick<T, true><<<seqs, many, 0, st>>>(a) : k_sample_pick<T, false><<<seqs, many, 0, st>>>(a);
     TASC_LAUNCH_CHECK();
     return TASC_OK;
 }
@@ -447,7 +542,8 @@ tasc_status enqueue(const SampleArgs& a, int batch, hipStream_t st) {
 
 extern "C" size_t tasc_accept_sampled_workspace_bytes(int32_t batch, int32_t k, int32_t vocab) {
     if (batch < 1 || k < 0 || k > TASC_MAX_K || vocab < 2 || vocab > 1 << 24) return 0;
-    return parts_bytes(batch, k, segments(vocab)) + decided_bytes(batch, k) + (size_t)batch * segments(vocab) * sizeof(double);
+    const int n_seg = segments(vocab);
+    return parts_bytes(batch, k, n_seg) + decided_bytes(batch, k) + (size_t)batch * n_seg * sizeof(double);
 }
 
 extern "C" tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab, const int32_t* drafts,
@@ -477,9 +573,9 @@ extern "C" tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype,
 size_t tasc_sample_logits_bytes(int32_t batch, int32_t k, int32_t vocab) { return ((size_t)batch * (k + 1) * vocab * sizeof(float) + 255) / 256 * 256; }
 
 tasc_status tasc_sample_step(const tasc_session* s, const TascVerifyTail& t, hipStream_t st) {
-    const int vocab = s->model->desc.vocab;
+    const int vocab = s->model->desc.vocab, n_seg = segments(vocab);
     const TascSampled& p = *t.sampled;
-    const SampleArgs a{p.logits, vocab, t.k, vocab, segments(vocab), t.drafts, nullptr, p.temperature, p.u, p.n_u, s->d.n_emit, (Part*)p.parts, nullptr, nullptr,
+    const SampleArgs a{p.logits, vocab, t.k, vocab, n_seg, t.drafts, nullptr, p.temperature, p.u, p.n_u, s->d.n_emit, (Part*)p.parts, nullptr, nullptr,
                        t.accept_len, t.emitted, p.logprob, s->d, s->max_len};
     return enqueue<float>(a, s->batch, st);
 }

@@ -110,6 +110,23 @@ def test_masks_and_rows_without_a_distribution():
     check(logits, drafts, None, np.where(np.arange(12) < 10, 0, temperature).astype(np.float32), u)
 
 
+@pytest.mark.parametrize("size", [1e4, 1e7, 3e38])
+def test_logits_of_any_size(size):
+    """Rows whose logits are far from zero or far apart, several equal largest ones among them, at temperatures whose products are not exact."""
+    import torch
+    rng = np.random.default_rng(15)
+    V, k = 9001, 2
+    logits = torch.tensor((rng.normal(size=(5, k + 1, V)) * 2 if size < 1e6 else np.zeros((5, k + 1, V))) + size, dtype=torch.float64).clamp(max=3.4e38).float()
+    logits[1] = -size
+    logits[2, :, ::3] = -size                                # equal ones a third apart
+    logits[3, :, 1::2] = -size
+    drafts = rng.integers(0, V, (5, k)).astype(np.int32)
+    u = rng.random((5, k + 1, 2)).astype(np.float32)
+    for temperature in (0.7, 1.0, 3.3):
+        check(logits, drafts, None, np.full(5, temperature, dtype=np.float32), u)
+        check(logits, drafts, np.full((5, k, V), 1.5 / V, dtype=np.float32), np.full(5, temperature, dtype=np.float32), u)
+
+
 def test_fewer_drafts_and_tokens_outside_the_vocabulary():
     rng = np.random.default_rng(12)
     logits, drafts, q, u = inputs(rng, 6, 4, 300, "float32", True)
