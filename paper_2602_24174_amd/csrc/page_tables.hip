@@ -1,8 +1,9 @@
 // Block tables and slots of a paged cache from the requests' lengths.
 //
-// One launch: every workgroup owns a run of sequences, sums the pages and rows that all sequences ask for (those before its own
-// give its place in the list of free pages and in the list of slots), and a wave writes a sequence's new pages and slots.  A few integers
-// per sequence, page and row: bound by launch latency and two dependent reads.
+// One launch: every workgroup owns 8 sequences (more of a batch beyond 2048, so that 256 workgroups read all lengths), sums the pages and rows
+// that all sequences ask for (those before its own give its place in the list of free pages and in the list of slots), and a wave
+// writes a sequence's new pages and slots.  A few integers per sequence, page and row: bound by launch latency and three dependent
+// reads.  The last workgroup adds up what was given and refused.
 #include "tasc_internal.h"
 #include <algorithm>
 
@@ -35,18 +36,28 @@ __device__ __forceinline__ int64_t wave_sum64(int64_t v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
     return v;
 }
+__device__ __forceinline__ int64_t wave_scan64(int64_t v, int lane) {      // inclusive
+    for (int o = 1; o < 64; o <<= 1) {
+        const int64_t up = __shfl_up(v, o);
+        if (lane >= o) v += up;
+    }
+    return v;
+}
+__device__ __forceinline__ int64_t from_lane(int64_t v, int lane) {        // a uniform lane
+    return (int64_t)(u32)__builtin_amdgcn_readlane((int)(v >> 32), lane) << 32 | (u32)__builtin_amdgcn_readlane((int)v, lane);
+}
 
 __global__ __launch_bounds__(kThreads) void k_page_tables(PageArgs a) {
-    __shared__ int64_t s_sum[4][kWaves];
-    const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+    __shared__ int64_t s_sum[3][kWaves];
+    __shared__ int32_t s_refused[kWaves];
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int b0 = (int)min((int64_t)blockIdx.x * a.per_wg, (int64_t)a.batch), b1 = min(b0 + a.per_wg, a.batch);
     int64_t pages_before = 0, rows_before = 0, rows_all = 0;
+#pragma unroll 4
     for (int b = tid; b < a.batch; b += kThreads) {
         const Ask q = ask_of(a, b);
-        if (b < b0) {
-            pages_before += q.pages;
-            rows_before += q.rows;
-        }
+        pages_before += b < b0 ? q.pages : 0;
+        rows_before += b < b0 ? q.rows : 0;
         rows_all += q.rows;
     }
     pages_before = wave_sum64(pages_before);
@@ -64,28 +75,36 @@ __global__ __launch_bounds__(kThreads) void k_page_tables(PageArgs a) {
         rows_before += s_sum[1][w];
         rows_all += s_sum[2][w];
     }
-    // the workgroup's sequences in order, a wave each in turn; every wave follows the sums of all of them
-    for (int b = b0; b < b1; ++b) {
-        const Ask q = ask_of(a, b);
-        const int64_t first = pages_before, row = rows_before;
-        pages_before += q.pages;
-        rows_before += q.rows;
-        if ((b - b0) % kWaves != wave) continue;
-        const bool granted = q.fits && (q.pages == 0 || pages_before <= a.n_free);
-        int32_t* const tab = a.table + (size_t)b * a.max_pages;
-        auto given = [&](int j) { return a.free_pages ? a.free_pages[first + j] : (int32_t)(first + j); };      // the sequence's new page j
-        if (granted)
-            for (int j = lane; j < q.pages; j += 64) tab[q.held + j] = given(j);
-        if (lane == 0) {
-            if (a.pages) a.pages[b] = granted ? max(q.need, q.held) : q.held;
-            if (a.row_off) a.row_off[b] = (int32_t)min(row, (int64_t)INT32_MAX);
-        }
-        if (!a.slots) continue;
-        for (int i = lane; i < q.rows && row + i < a.slots_cap; i += 64) {
-            const int pos = q.len - q.rows + i, at = pos / TASC_PAGE_TOKENS;
-            int32_t slot = -1;
-            if (granted) slot = (at < q.held ? tab[at] : given(at - q.held)) * TASC_PAGE_TOKENS + pos % TASC_PAGE_TOKENS;
-            a.slots[row + i] = slot;
+    // the workgroup's sequences, 64 at a time: a lane each for the sums, then a wave each in turn
+    for (int c = b0; c < b1; c += 64) {
+        Ask mine{};
+        if (c + lane < b1) mine = ask_of(a, c + lane);
+        const int64_t pages_to = wave_scan64(mine.pages, lane) + pages_before, rows_to = wave_scan64(mine.rows, lane) + rows_before;
+        pages_before = from_lane(pages_to, 63);
+        rows_before = from_lane(rows_to, 63);
+        for (int n = wave; n < min(64, b1 - c); n += kWaves) {
+            const int b = c + n;
+            auto of = [&](int v) { return __builtin_amdgcn_readlane(v, n); };
+            const int held = of(mine.held), need = of(mine.need), pages = of(mine.pages), rows = of(mine.rows), len = of(mine.len);
+            const int64_t end = from_lane(pages_to, n), first = end - pages, row = from_lane(rows_to, n) - rows;
+            const bool granted = of(mine.fits) && (pages == 0 || end <= a.n_free);
+            int32_t* const tab = a.table + (size_t)b * a.max_pages;
+            auto given = [&](int j) { return a.free_pages ? a.free_pages[first + j] : (int32_t)(first + j); };      // the sequence's new page j
+            if (granted)
+                for (int j = lane; j < pages; j += 64) tab[held + j] = given(j);
+            if (lane == 0) {
+                if (a.pages) a.pages[b] = granted ? max(need, held) : held;
+                if (a.row_off) a.row_off[b] = (int32_t)min(row, (int64_t)INT32_MAX);
+            }
+            if (!a.slots) continue;
+            const int count = (int)min((int64_t)rows, max((int64_t)a.slots_cap - row, (int64_t)0));
+#pragma unroll 4
+            for (int i = lane; i < count; i += 64) {
+                const int pos = len - rows + i, at = pos / TASC_PAGE_TOKENS;
+                int32_t slot = -1;
+                if (granted) slot = (at < held ? tab[at] : given(at - held)) * TASC_PAGE_TOKENS + pos % TASC_PAGE_TOKENS;
+                a.slots[row + i] = slot;
+            }
         }
     }
     if (a.slots)
@@ -93,34 +112,41 @@ __global__ __launch_bounds__(kThreads) void k_page_tables(PageArgs a) {
     if (blockIdx.x != gridDim.x - 1) return;
     if (tid == 0 && a.row_off) a.row_off[a.batch] = (int32_t)min(rows_all, (int64_t)INT32_MAX);
     if (!a.summary) return;
-    // pages given away: a sequence that gets pages gets all it asks for, and the sums only grow, so it is the largest sum that fits
-    __syncthreads();
-    if (wave != 0) return;
+    // pages given away: a sequence that gets pages gets all it asks for, and the sums only grow, so it is the largest sum that fits.  A
+    // thread adds up a run of sequences, then knows where its run begins.
+    const int run = (a.batch + kThreads - 1) / kThreads, from = min(tid * run, a.batch), to = min(from + run, a.batch);
     int64_t sum = 0, taken = 0;
+    for (int b = from; b < to; ++b) sum += ask_of(a, b).pages;
+    const int64_t upto = wave_scan64(sum, lane);
+    __syncthreads();
+    if (lane == 63) s_sum[0][wave] = upto;
+    __syncthreads();
+    int64_t end = upto - sum;
+    for (int w = 0; w < wave; ++w) end += s_sum[0][w];
     int refused = 0;
-    for (int b = 0; b < a.batch; b += 64) {
-        Ask q{};
-        q.fits = true;
-        if (b + lane < a.batch) q = ask_of(a, b + lane);
-        int64_t end = q.pages;
-        for (int o = 1; o < 64; o <<= 1) {
-            const int64_t v = __shfl_up(end, o);
-            if (lane >= o) end += v;
-        }
-        end += sum;
-        sum = __shfl(end, 63);
+    for (int b = from; b < to; ++b) {
+        const Ask q = ask_of(a, b);
+        end += q.pages;
         if (!q.fits || (q.pages > 0 && end > a.n_free)) ++refused;
-        else if (q.pages > 0 && end > taken) taken = end;
+        else if (q.pages > 0) taken = max(taken, end);
     }
     for (int o = 32; o > 0; o >>= 1) {
         taken = max(taken, (int64_t)__shfl_xor(taken, o));
         refused += __shfl_xor(refused, o);
     }
     if (lane == 0) {
-        a.summary[0] = (int32_t)min(rows_all, (int64_t)INT32_MAX);
-        a.summary[1] = (int32_t)taken;
-        a.summary[2] = refused;
+        s_sum[1][wave] = taken;
+        s_refused[wave] = refused;
     }
+    __syncthreads();
+    if (tid != 0) return;
+    for (int w = 1; w < kWaves; ++w) {
+        taken = max(taken, s_sum[1][w]);
+        refused += s_refused[w];
+    }
+    a.summary[0] = (int32_t)min(rows_all, (int64_t)INT32_MAX);
+    a.summary[1] = (int32_t)taken;
+    a.summary[2] = refused;
 }
 
 }  // namespace
