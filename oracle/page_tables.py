@@ -3,7 +3,7 @@
 
 def page_tables(kv_len, new_rows, held, free_pages, table, slots_cap, page=16):
     """table: list of lists, grown in place.  Returns (pages, row_off, slots, summary)."""
-    cols, asked, taken, refused = len(table[0]), 0, 0, 0
+    cols, asked, reach, refused = len(table[0]), 0, 0, 0
     pages, row_off, slots = [], [0], []
     for b, (n, new, has) in enumerate(zip(kv_len, new_rows, held)):
         need = -(-max(n, 0) // page)
@@ -13,7 +13,7 @@ def page_tables(kv_len, new_rows, held, free_pages, table, slots_cap, page=16):
         granted = fits and (ask == 0 or asked <= len(free_pages))
         if granted:
             table[b][has:has + ask] = free_pages[first:first + ask]
-            taken = max(taken, asked if ask else 0)
+            reach = asked
         refused += not granted
         pages.append(max(need, has) if granted else has)
         for i in range(max(new, 0)):
@@ -21,4 +21,4 @@ def page_tables(kv_len, new_rows, held, free_pages, table, slots_cap, page=16):
             slots.append(table[b][pos // page] * page + pos % page if granted else -1)
         row_off.append(len(slots))
     rows = len(slots)
-    return pages, row_off, (slots + [-1] * slots_cap)[:slots_cap], [rows, taken, refused]
+    return pages, row_off, (slots + [-1] * slots_cap)[:slots_cap], [rows, reach, refused]

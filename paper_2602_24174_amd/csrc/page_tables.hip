@@ -112,10 +112,10 @@ __global__ __launch_bounds__(kThreads) void k_page_tables(PageArgs a) {
     if (blockIdx.x != gridDim.x - 1) return;
     if (tid == 0 && a.row_off) a.row_off[a.batch] = (int32_t)min(rows_all, (int64_t)INT32_MAX);
     if (!a.summary) return;
-    // pages given away: a sequence that gets pages gets all it asks for, and the sums only grow, so it is the largest sum that fits.  A
-    // thread adds up a run of sequences, then knows where its run begins.
+    // pages asked for up to the last sequence that is granted: the sums only grow, so it is the largest of a granted one's.  A thread adds up
+    // a run of sequences, then knows where its run begins.
     const int run = (a.batch + kThreads - 1) / kThreads, from = min(tid * run, a.batch), to = min(from + run, a.batch);
-    int64_t sum = 0, taken = 0;
+    int64_t sum = 0, reach = 0;
     for (int b = from; b < to; ++b) sum += ask_of(a, b).pages;
     const int64_t upto = wave_scan64(sum, lane);
     __syncthreads();
@@ -128,24 +128,24 @@ __global__ __launch_bounds__(kThreads) void k_page_tables(PageArgs a) {
         const Ask q = ask_of(a, b);
         end += q.pages;
         if (!q.fits || (q.pages > 0 && end > a.n_free)) ++refused;
-        else if (q.pages > 0) taken = max(taken, end);
+        else reach = end;
     }
     for (int o = 32; o > 0; o >>= 1) {
-        taken = max(taken, (int64_t)__shfl_xor(taken, o));
+        reach = max(reach, (int64_t)__shfl_xor(reach, o));
         refused += __shfl_xor(refused, o);
     }
     if (lane == 0) {
-        s_sum[1][wave] = taken;
+        s_sum[1][wave] = reach;
         s_refused[wave] = refused;
     }
     __syncthreads();
     if (tid != 0) return;
     for (int w = 1; w < kWaves; ++w) {
-        taken = max(taken, s_sum[1][w]);
+        reach = max(reach, s_sum[1][w]);
         refused += s_refused[w];
     }
     a.summary[0] = (int32_t)min(rows_all, (int64_t)INT32_MAX);
-    a.summary[1] = (int32_t)taken;
+    a.summary[1] = (int32_t)min(reach, (int64_t)INT32_MAX);
     a.summary[2] = refused;
 }
 

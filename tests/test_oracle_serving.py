@@ -21,7 +21,7 @@ def test_page_tables_refuse_in_order():
     table[2][0] = 9
     got = OP.page_tables([16, 20, 16, 1], [1, 1, 1, 1], [0, 0, 1, 0], [5, 6], table, 4)
     assert table == [[5, -1, -1], [-1] * 3, [9, -1, -1], [-1] * 3]
-    assert got[0] == [1, 0, 1, 0] and got[2] == [5 * 16 + 15, -1, 9 * 16 + 15, -1] and got[3] == [4, 1, 2]
+    assert got[0] == [1, 0, 1, 0] and got[2] == [5 * 16 + 15, -1, 9 * 16 + 15, -1] and got[3] == [4, 3, 2]
 
 
 def test_numbers_are_the_nearest():
