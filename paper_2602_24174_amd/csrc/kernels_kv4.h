@@ -330,202 +330,150 @@ __device__ __forceinline__ float kv4_quad_sum(float v) {
     v += __shfl_xor(v, 16);
     return v + __shfl_xor(v, 32);
 }
-// What a tile's {scale, low} words come to, in LDS of the wave's own: every lane works out the tokens that it was dealt, all lanes read
-// those of the products they hold (as each lane's own work it is 130 of 560 instructions a tile of 64 pairs).
+// What a tile's {scale, low} words come to, in LDS: every lane works out the tokens that it was dealt, all lanes read those of the products
+// they hold (as each lane's own work it is a quarter of a tile's instructions).  A value low + scale c is scale (c + z), z = low / scale:
+// the weights of the second product are p scale, rounded to bf16 once, and meet 16 + c in one matrix instruction and z - 16, as three bf16
+// terms, in another, so that what the rounding takes from a weight it takes from the whole value.  (With p (low + 7.5 scale) as a product
+// of its own, the two roundings of a weight differ, and the error against 64 bits is twice as large.)
 template <int HD>
-struct Kv4Scales {
+struct __attribute__((aligned(16))) Kv4Scales {
     static constexpr int G = Kv4Layout<HD>::GROUPS;
     float ks[2][G][16], kb[2][G][16], vs[2][G][16];    // by page, group, token
-    uint16_t mid[4][32];                                // low + 7.5 scale of the values' groups as bf16, and what that leaves, as bf16; tokens in
-                                                        // the order of the second product (4 of page 0, 4 of page 1 for each r)
-    uint16_t fixed[2][32];                              // zeros; -23.5
+    uint16_t z[G][3][32];                               // tokens in the order of the second product (4 of page 0, 4 of page 1 for each r)
 };
+// z - 16 in three terms, and the scale to go with it: where z is too large for them (its value is low then, to fp32's last place) or
+// there is no scale, another pair with the same values
+struct Kv4Z { float scale; uint16_t z[3]; };
+__device__ __forceinline__ Kv4Z kv4_z(float scale, float low) {
+    float z = low * __builtin_amdgcn_rcpf(scale);
+    if (scale < 1.17549435e-38f && scale != 0.f) z = low / scale;               // (below the reciprocal's range)
+    if (!(fabsf(z) <= 1073741824.f)) {                      // 2^30
+        z = scale == 0.f ? 1.f : 1073741824.f;             // (numbers are 0 where the scale is)
+        scale = scale == 0.f ? low : low * (1.f / 1073741824.f);
+    }
+    Kv4Z o;
+    o.scale = scale;
+    z -= 16.f;
+#pragma unroll
+    for (int i = 0; i < 3; ++i) {
+        o.z[i] = f2bf(z);
+        z -= bf2f(o.z[i]);
+    }
+    return o;
+}
 constexpr float kKv4Grown = 8.f;                        // a maximum is followed once it grew by more than this power of 2
 
-// MT: tiles of 16 (row, head) pairs a wave holds.  KW: waves that share their pairs and take a key chunk's tiles in turn; a workgroup has a.row_waves
-// times as many, each KW of them with pairs of their own (over the same keys, which they so find in the L1 cache).
-template <int HD, int MT, int KW>
-__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv4_attention(Kv4Attn a) {
-    using L = Kv4Layout<HD>;
-    constexpr int G = L::GROUPS, KSTEPS = HD / 32, DT = HD / 16;
-    constexpr int AHEAD = MT * HD >= 256 ? 1 : 2;           // tiles under way: as many as the registers of two waves a SIMD hold beside the sums
-    extern __shared__ __attribute__((aligned(16))) float lds[];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, r = lane >> 4;
-    // (the last waves have the fewest pairs; every second workgroup of a compute unit takes them the other way round, or the same SIMDs would
-    // have the full ones every time)
-    const int kw = wave % KW, turned = (blockIdx.y * gridDim.x + blockIdx.x) / 256 % 2, rw = turned ? a.row_waves - 1 - wave / KW : wave / KW;
-    Kv4Scales<HD>& sc = reinterpret_cast<Kv4Scales<HD>*>(lds)[wave];
-    const int b = blockIdx.y / a.Hkv, h = blockIdx.y % a.Hkv, share = a.H / a.Hkv;
-    const int tile = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
-    const Kv4Seq sq = kv4_seq(a, b);
-    const int n_pairs = sq.n * share, wg_pair = tile * a.row_waves * 16 * MT, pair0 = wg_pair + rw * 16 * MT;
-    if (wg_pair >= n_pairs) return;                        // (the whole workgroup; a wave without pairs among them goes on without keys)
-    const int len = min(max(sq.len, 0), a.max_pages * TASC_KV_BLOCK);
-    const int pair_last = min(pair0 + 16 * MT, n_pairs) - 1;
-    const int first_last = sq.len - sq.n + pair0 / share, last_last = sq.len - sq.n + pair_last / share;   // last keys of the first and the last pair
-    // (a negative count: no key at all)
-    int n_tiles = min((min(last_last + 1, len) + 31) / 32, chunk + 1 < a.chunks ? (chunk + 1) * a.chunk_tiles : INT32_MAX);
-    if (pair0 >= n_pairs) n_tiles = 0;
-    const int live = (pair_last - pair0) / 16 + 1;         // tiles of pairs that hold any
-
-    const size_t page_bytes = (size_t)a.Hkv * L::HEAD;
-    const uint8_t* const pool = a.pool + (size_t)h * L::HEAD;
-    const int first_tile = chunk * a.chunk_tiles + kw;
-    // The ids of 32 tiles' pages, two lanes a tile: a look at the table is then no memory access.  -1: behind the last tile, or
-    // outside the pool, where an id is not followed and its tokens are masked.
-    auto page_ids = [&](int from) {
-        const int t = from + (lane >> 1) * KW, at = 2 * t + (lane & 1);
-        int page = -1;
-        if (t < n_tiles && at < a.max_pages) page = a.table[(size_t)b * a.max_pages + at];
-        return page < a.n_pages ? page : -1;
-    };
-    int ids = page_ids(first_tile), ids_next = 0;
-    auto where = [&](int page) { return pool + (size_t)max(page, 0) * page_bytes; };
-
-    int last[MT];
-    kv4_u32x4 rq[MT][KSTEPS];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        const int pair = pair0 + 16 * t + col, row = sq.first + pair / share, head = h * share + pair % share;
-        const bool there = pair < n_pairs && row < a.rows;
-        last[t] = there ? sq.len - sq.n + pair / share : -1;
-#pragma unroll
-        for (int i = 0; i < KSTEPS; ++i) {
-            const int d = HD == 128 ? (i / 2) * 64 + 16 * r + 8 * (i & 1) : HD == 64 ? 16 * r + 8 * i : 8 * r;
-            rq[t][i] = kv4_u32x4{0, 0, 0, 0};
-            if (there) rq[t][i] = *reinterpret_cast<const kv4_u32x4*>(a.q + (size_t)row * a.q_stride + head * HD + d);
-        }
-    }
-    // the first two tiles are under way while the queries are looked at
-    Kv4Tile<HD> tile_a, tile_b;
-    int pa0 = __builtin_amdgcn_readlane(ids, 0), pa1 = __builtin_amdgcn_readlane(ids, 1);
-    int pb0 = __builtin_amdgcn_readlane(ids, 2), pb1 = __builtin_amdgcn_readlane(ids, 3);
-    kv4_fetch<HD>(tile_a, where(pa0), where(pa1), lane);   // (without tiles: page 0, not used)
-    if constexpr (AHEAD == 2) kv4_fetch<HD>(tile_b, where(pb0), where(pb1), lane);
+// What a wave holds: MT tiles of 16 (row, head) pairs of a KV head, with their queries and sums.
+template <int HD, int MT>
+struct Kv4Wave {
+    static constexpr int G = Kv4Layout<HD>::GROUPS, KSTEPS = HD / 32, DT = HD / 16;
     kv4_bf16x8 fq[MT][KSTEPS];
     float qsum[MT][G];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-#pragma unroll
-        for (int g = 0; g < G; ++g) qsum[t][g] = 0.f;
-#pragma unroll
-        for (int i = 0; i < KSTEPS; ++i) {
-            fq[t][i] = __builtin_bit_cast(kv4_bf16x8, rq[t][i]);
-#pragma unroll
-            for (int e = 0; e < 4; ++e) qsum[t][HD == 128 ? i / 2 : 0] = kv4_pair_sum(rq[t][i][e], qsum[t][HD == 128 ? i / 2 : 0]);
-        }
-#pragma unroll
-        for (int g = 0; g < G; ++g) qsum[t][g] = kv4_quad_sum(qsum[t][g]);
-    }
-    // rows of the sums' first operands that do not change: zeros, and -23.5 for a group's weights in the group's row
-    if (lane < 32) {
-        sc.fixed[0][lane] = 0;
-        sc.fixed[1][lane] = 0xC1BC;                         // bf16 -23.5
-        if (G == 1) sc.mid[1][lane] = sc.mid[3][lane] = 0;
-    }
-
-    kv4_f32x4 acc[MT][DT], ev[MT];                          // ev rows 0 .. G - 1 (+ 2): sum p (low + 7.5 scale) - 23.5 sum (p scale)
+    kv4_f32x4 acc[MT][DT], ev[MT];                          // ev rows 4 g .. 4 g + 2: sums of p scale (z - 16)'s terms
     float m[MT], l[MT], lim[MT];                            // lim: what a score may be above m (nothing yet: -infinity)
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        m[t] = 0.f;
-        l[t] = 0.f;
-        lim[t] = -__builtin_inff();
-        ev[t] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-        for (int j = 0; j < DT; ++j) acc[t][j] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
-    }
-    const Kv4Bits bits = kv4_bits();
-    const float scale2 = a.scale * 1.44269504088896340736f;   // scores in powers of 2
+    float s[MT][2][4];                                      // a tile's scores, less m
+    int last[MT];                                           // last key that the lane's pair sees
+    int pair0, live, first_last;                            // first pair, tiles of pairs that hold any, last key of the first pair
+    const Kv4Seq& sq;
+    int h, share, n_pairs, lane, col, r;
 
-    // one tile out of `cur`, whose registers then take the tile of the pages that come next
-    auto work = [&](Kv4Tile<HD>& cur, int t, int pg0, int pg1, int ng0, int ng1) __attribute__((always_inline)) {
-        const int at = 32 * t;
-        const bool whole = pg0 >= 0 && pg1 >= 0 && at + 31 <= first_last && at + 32 <= len;
-        {
-            const int p = kv4_scale_page<HD>(lane), w = kv4_scale_word<HD>(lane), tok = lane & 15, g = w / 16;
-            float ks = kv4_scale(cur.ks) * scale2, lo = kv4_low(cur.ks) * scale2, vs = kv4_scale(cur.vs), vl = kv4_low(cur.vs);
-            const bool in = whole || ((p ? pg1 : pg0) >= 0 && at + 16 * p + tok < len);   // (what lies elsewhere may be no number)
-            if (!in) ks = lo = vs = vl = 0.f;
-            float mid = __builtin_fmaf(7.5f, vs, vl);
-            if (!(fabsf(mid) < __builtin_inff())) { ks = __builtin_nanf(""); vs = mid = 0.f; }   // values that are none: who sees the token gets NaN by its score
-            const uint16_t hi = f2bf(mid), rest = f2bf(mid - bf2f(hi));
-            if (G == 2 || lane < 32) {
-                (&sc.ks[0][0][0])[lane] = ks;
-                (&sc.kb[0][0][0])[lane] = __builtin_fmaf(-16.f, ks, lo);
-                (&sc.vs[0][0][0])[lane] = vs;
-                const int slot = (tok / 4) * 8 + 4 * p + tok % 4;
-                sc.mid[g][slot] = hi;
-                sc.mid[2 + g][slot] = rest;
-            }
-        }
-        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wave's LDS accesses are in order: the compiler has to keep them so)
-        __builtin_amdgcn_wave_barrier();
-        // scores of 16 tokens at a time, less the maximum so far
-        float s[MT][2][4];
+    __device__ __forceinline__ Kv4Wave(const Kv4Seq& sequence, int kv_head, int heads_share, int first_pair, int lane_)
+        : pair0(first_pair), sq(sequence), h(kv_head), share(heads_share), lane(lane_), col(lane_ & 15), r(lane_ >> 4) {
+        n_pairs = sq.n * share;
+        live = pair0 < n_pairs ? (min(pair0 + 16 * MT, n_pairs) - 1 - pair0) / 16 + 1 : 0;
+        first_last = sq.len - sq.n + pair0 / share;
+    }
+    // tiles of 32 tokens with a key that any of the pairs sees (a negative count: none)
+    __device__ __forceinline__ int tiles(int len) const {
+        if (pair0 >= n_pairs) return 0;
+        const int last_last = sq.len - sq.n + (min(pair0 + 16 * MT, n_pairs) - 1) / share;
+        return (min(last_last + 1, len) + 31) / 32;
+    }
+    __device__ __forceinline__ bool pair(int t, int rows, int& row, int& head) const {
+        const int pr = pair0 + 16 * t + col;
+        row = sq.first + pr / share;
+        head = h * share + pr % share;
+        return pr < n_pairs && row < rows;
+    }
+    // the queries are asked for ..
+    __device__ __forceinline__ void ask(const Kv4Attn& a) {
 #pragma unroll
-        for (int p = 0; p < 2; ++p) {
-            if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
-            kv4_bf16x8 fk[KSTEPS];
+        for (int t = 0; t < MT; ++t) {
+            int row, head;
+            const bool there = pair(t, a.rows, row, head);
+            last[t] = there ? sq.len - sq.n + (pair0 + 16 * t + col) / share : -1;
 #pragma unroll
             for (int i = 0; i < KSTEPS; ++i) {
-                const uint32_t w = cur.kc[p][i];
-                fk[i] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(bits, w, 0), kv4_pair(bits, w, 1), kv4_pair(bits, w, 2), kv4_pair(bits, w, 3)});
-            }
-            kv4_f32x4 ks[G], kb[G];
-#pragma unroll
-            for (int g = 0; g < G; ++g) {
-                ks[g] = *reinterpret_cast<const kv4_f32x4*>(&sc.ks[p][g][4 * r]);
-                kb[g] = *reinterpret_cast<const kv4_f32x4*>(&sc.kb[p][g][4 * r]);
-            }
-#pragma unroll
-            for (int u = 0; u < MT; ++u) {
-                if (u >= live) break;
-                kv4_f32x4 sg[G];
-#pragma unroll
-                for (int g = 0; g < G; ++g) sg[g] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-                for (int i = 0; i < KSTEPS; ++i) {
-                    constexpr int per = KSTEPS / G;
-                    sg[i / per] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fk[i], fq[u][i], sg[i / per], 0, 0, 0);
-                }
-#pragma unroll
-                for (int i = 0; i < 4; ++i) {
-                    float v = -m[u];
-#pragma unroll
-                    for (int g = 0; g < G; ++g) v = __builtin_fmaf(kb[g][i], qsum[u][g], v);
-#pragma unroll
-                    for (int g = 0; g < G; ++g) v = __builtin_fmaf(ks[g][i], sg[g][i], v);
-                    s[u][p][i] = v;
-                }
+                const int d = HD == 128 ? (i / 2) * 64 + 16 * r + 8 * (i & 1) : HD == 64 ? 16 * r + 8 * i : 8 * r;
+                kv4_u32x4 w = {0, 0, 0, 0};
+                if (there) w = *reinterpret_cast<const kv4_u32x4*>(a.q + (size_t)row * a.q_stride + head * HD + d);
+                fq[t][i] = __builtin_bit_cast(kv4_bf16x8, w);
             }
         }
-        if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
-        // the lane's tokens' value numbers, channel by channel: pairs of tokens in a register
-        uint32_t pr[HD == 128 ? 2 : 1][4];                  // [lower, upper half of the words][token pair]
+    }
+    // .. and looked at
+    __device__ __forceinline__ void begin() {
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const uint32_t x = cur.vc[e / 2][2 * (e % 2)], y = cur.vc[e / 2][2 * (e % 2) + 1];
-            pr[0][e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
-            if constexpr (HD == 128) pr[1][e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+        for (int t = 0; t < MT; ++t) {
+#pragma unroll
+            for (int g = 0; g < G; ++g) qsum[t][g] = 0.f;
+#pragma unroll
+            for (int i = 0; i < KSTEPS; ++i) {
+                const kv4_u32x4 w = __builtin_bit_cast(kv4_u32x4, fq[t][i]);
+#pragma unroll
+                for (int e = 0; e < 4; ++e) qsum[t][HD == 128 ? i / 2 : 0] = kv4_pair_sum(w[e], qsum[t][HD == 128 ? i / 2 : 0]);
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g) qsum[t][g] = kv4_quad_sum(qsum[t][g]);
+            m[t] = 0.f;
+            l[t] = 0.f;
+            lim[t] = -__builtin_inff();
+            ev[t] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int j = 0; j < DT; ++j) acc[t][j] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
         }
-        if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
-        kv4_fetch<HD>(cur, where(ng0), where(ng1), lane);
-        kv4_bf16x8 fv[DT];
+    }
+    // scores of page p's 16 tokens
+    __device__ __forceinline__ void scores(int p, const kv4_bf16x8 (&fk)[KSTEPS], const Kv4Scales<HD>& sc) {
+        kv4_f32x4 ks[G], kb[G];
 #pragma unroll
-        for (int j = 0; j < DT; ++j)
-            fv[j] = __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(bits, pr[j / 4][0], j % 4), kv4_pair(bits, pr[j / 4][1], j % 4),
-                                                             kv4_pair(bits, pr[j / 4][2], j % 4), kv4_pair(bits, pr[j / 4][3], j % 4)});
-        const kv4_bf16x8 fmid = *reinterpret_cast<const kv4_bf16x8*>(col < 4 ? &sc.mid[col][8 * r] : &sc.fixed[0][8 * r]);
-        kv4_bf16x8 fsum[G];
+        for (int g = 0; g < G; ++g) {
+            ks[g] = *reinterpret_cast<const kv4_f32x4*>(&sc.ks[p][g][4 * r]);
+            kb[g] = *reinterpret_cast<const kv4_f32x4*>(&sc.kb[p][g][4 * r]);
+        }
+#pragma unroll
+        for (int u = 0; u < MT; ++u) {
+            if (u >= live) break;
+            kv4_f32x4 sg[G];
+#pragma unroll
+            for (int g = 0; g < G; ++g) sg[g] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+            for (int i = 0; i < KSTEPS; ++i) {
+                constexpr int per = KSTEPS / G;
+                sg[i / per] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fk[i], fq[u][i], sg[i / per], 0, 0, 0);
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                float v = -m[u];
+#pragma unroll
+                for (int g = 0; g < G; ++g) v = __builtin_fmaf(kb[g][i], qsum[u][g], v);
+#pragma unroll
+                for (int g = 0; g < G; ++g) v = __builtin_fmaf(ks[g][i], sg[g][i], v);
+                s[u][p][i] = v;
+            }
+        }
+    }
+    // the tile's weights and their sums; at: its first position, whole: every pair sees all of it, ok0, ok1: its pages are in the pool
+    __device__ __forceinline__ void sums(const kv4_bf16x8 (&fv)[DT], const Kv4Scales<HD>& sc, int at, bool whole, bool ok0, bool ok1, int len) {
+        kv4_bf16x8 fz[G];
         kv4_f32x4 vs[2][G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            fsum[g] = *reinterpret_cast<const kv4_bf16x8*>(&sc.fixed[col == g][8 * r]);
+            fz[g] = *reinterpret_cast<const kv4_bf16x8*>(&sc.z[g][min(col & 3, 2)][8 * r]);
+            if (col < 4 * g || col >= 4 * g + 3) fz[g] = kv4_bf16x8{};
 #pragma unroll
             for (int p = 0; p < 2; ++p) vs[p][g] = *reinterpret_cast<const kv4_f32x4*>(&sc.vs[p][g][4 * r]);
         }
-
 #pragma unroll
         for (int u = 0; u < MT; ++u) {
             if (u >= live) break;
@@ -536,7 +484,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
 #pragma unroll
                     for (int i = 0; i < 4; ++i) {
                         const int pos = at + 16 * p + 4 * r + i;
-                        if ((p ? pg1 : pg0) < 0 || pos > last[u] || pos >= len) s[u][p][i] = -__builtin_inff();
+                        if (!(p ? ok1 : ok0) || pos > last[u] || pos >= len) s[u][p][i] = -__builtin_inff();
                     }
             }
             float top = fmaxf(fmaxf(fmaxf(s[u][0][0], s[u][0][1]), fmaxf(s[u][0][2], s[u][0][3])), fmaxf(fmaxf(s[u][1][0], s[u][1][1]), fmaxf(s[u][1][2], s[u][1][3])));
@@ -566,8 +514,6 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     pw[p][i] = __builtin_amdgcn_exp2f(s[u][p][i]);
                     l[u] += pw[p][i];
                 }
-            const kv4_u32x4 pq = {f2bf_pair(pw[0][0], pw[0][1]), f2bf_pair(pw[0][2], pw[0][3]), f2bf_pair(pw[1][0], pw[1][1]), f2bf_pair(pw[1][2], pw[1][3])};
-            ev[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fmid, __builtin_bit_cast(kv4_bf16x8, pq), ev[u], 0, 0, 0);
 #pragma unroll
             for (int g = 0; g < G; ++g) {
                 float ps[2][4];
@@ -577,15 +523,158 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
                     for (int i = 0; i < 4; ++i) ps[p][i] = pw[p][i] * vs[p][g][i];
                 const kv4_u32x4 w = {f2bf_pair(ps[0][0], ps[0][1]), f2bf_pair(ps[0][2], ps[0][3]), f2bf_pair(ps[1][0], ps[1][1]), f2bf_pair(ps[1][2], ps[1][3])};
                 const kv4_bf16x8 fp = __builtin_bit_cast(kv4_bf16x8, w);
-                ev[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fsum[g], fp, ev[u], 0, 0, 0);
+                ev[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fz[g], fp, ev[u], 0, 0, 0);
 #pragma unroll
                 for (int j = g * (DT / G); j < (g + 1) * (DT / G); ++j) acc[u][j] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(fv[j], fp, acc[u][j], 0, 0, 0);
             }
         }
+    }
+    // the four lanes' sums, and the channels' share of ev
+    __device__ __forceinline__ void end() {
+#pragma unroll
+        for (int t = 0; t < MT; ++t) {
+            l[t] = kv4_quad_sum(l[t]);
+            if (lim[t] != kKv4Grown) m[t] = -__builtin_inff();   // no key
+#pragma unroll
+            for (int g = 0; g < G; ++g) {
+                const float e = __shfl((ev[t][0] + ev[t][1]) + ev[t][2], 16 * g + col);
+#pragma unroll
+                for (int j = g * (DT / G); j < (g + 1) * (DT / G); ++j) acc[t][j] += e;
+            }
+        }
+    }
+    // A lane's channels: of tile j row 4 r + i, channel (HD 128, 64) 64 (j / 4) + 16 r + 4 i + j % 4, (32) 8 r + 2 i + j: in items (i, group of
+    // four tiles j) of as many neighbours
+    static constexpr int QUADS = DT / 4 > 0 ? DT / 4 : 1, ITEMS = 4 * QUADS;
+    __device__ __forceinline__ float4 quad(int t, int item) const {
+        const int i = item / QUADS, j = 4 * (item % QUADS);
+        return HD == 32 ? make_float4(acc[t][0][i], acc[t][1][i], 0.f, 0.f) : make_float4(acc[t][j][i], acc[t][j + 1][i], acc[t][j + 2][i], acc[t][j + 3][i]);
+    }
+    __device__ __forceinline__ int channel(int item) const { return HD == 32 ? 8 * r + 2 * (item / QUADS) : 64 * (item % QUADS) + 16 * r + 4 * (item / QUADS); }
+    static __device__ __forceinline__ void store(const Kv4Attn& a, int row, int head, int d, const float4& o, float inv) {
+        uint16_t* to = reinterpret_cast<uint16_t*>(a.out + (size_t)row * a.out_stride + head * HD + d);
+        if constexpr (HD == 32) *reinterpret_cast<uint32_t*>(to) = f2bf_pair(o.x * inv, o.y * inv);
+        else *reinterpret_cast<kv4_u32x2*>(to) = kv4_u32x2{f2bf_pair(o.x * inv, o.y * inv), f2bf_pair(o.z * inv, o.w * inv)};
+    }
+};
+// a pair without keys gives zeros (a NaN stays one)
+__device__ __forceinline__ float kv4_inverse(float l) { return l > 0.f ? 1.f / l : l; }
+
+// the tile's {scale, low} words, which the lanes were dealt, into LDS
+template <int HD>
+__device__ __forceinline__ void kv4_work_scales(Kv4Scales<HD>& sc, uint32_t k_word, uint32_t v_word, float scale2, int at, bool whole, bool ok0, bool ok1, int len, int lane) {
+    constexpr int G = Kv4Layout<HD>::GROUPS;
+    const int p = kv4_scale_page<HD>(lane), g = kv4_scale_word<HD>(lane) / 16, tok = lane & 15;
+    float ks = kv4_scale(k_word) * scale2, lo = kv4_low(k_word) * scale2, vs = kv4_scale(v_word), vl = kv4_low(v_word);
+    const bool in = whole || ((p ? ok1 : ok0) && at + 16 * p + tok < len);      // (what lies elsewhere may be no number)
+    if (!in) ks = lo = vs = vl = 0.f;
+    if (!(fabsf(__builtin_fmaf(7.5f, vs, vl)) < __builtin_inff())) { ks = __builtin_nanf(""); vs = vl = 0.f; }   // values that are none: who sees the token gets NaN by its score
+    const Kv4Z z = kv4_z(vs, vl);
+    if (G == 2 || lane < 32) {
+        (&sc.ks[0][0][0])[lane] = ks;
+        (&sc.kb[0][0][0])[lane] = __builtin_fmaf(-16.f, ks, lo);
+        (&sc.vs[0][0][0])[lane] = z.scale;
+#pragma unroll
+        for (int i = 0; i < 3; ++i) sc.z[g][i][(tok / 4) * 8 + 4 * p + tok % 4] = z.z[i];
+    }
+}
+template <int HD>
+__device__ __forceinline__ kv4_bf16x8 kv4_key_part(const Kv4Bits& bits, const Kv4Tile<HD>& t, int p, int i) {
+    const uint32_t w = t.kc[p][i];
+    return __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(bits, w, 0), kv4_pair(bits, w, 1), kv4_pair(bits, w, 2), kv4_pair(bits, w, 3)});
+}
+// the lane's tokens' value numbers, pairs of tokens in a register: [lower, upper half of the words][token pair]
+template <int HD>
+struct Kv4Values { uint32_t pr[HD == 128 ? 2 : 1][4]; };
+template <int HD>
+__device__ __forceinline__ Kv4Values<HD> kv4_values(const Kv4Tile<HD>& t) {
+    Kv4Values<HD> v;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        const uint32_t x = t.vc[e / 2][2 * (e % 2)], y = t.vc[e / 2][2 * (e % 2) + 1];
+        v.pr[0][e] = __builtin_amdgcn_perm(y, x, 0x05040100u);
+        if constexpr (HD == 128) v.pr[1][e] = __builtin_amdgcn_perm(y, x, 0x07060302u);
+    }
+    return v;
+}
+template <int HD>
+__device__ __forceinline__ kv4_bf16x8 kv4_value_part(const Kv4Bits& bits, const Kv4Values<HD>& v, int j) {
+    const uint32_t(&w)[4] = v.pr[j / 4];
+    return __builtin_bit_cast(kv4_bf16x8, kv4_u32x4{kv4_pair(bits, w[0], j % 4), kv4_pair(bits, w[1], j % 4), kv4_pair(bits, w[2], j % 4), kv4_pair(bits, w[3], j % 4)});
+}
+// The ids of 32 tiles' pages, two lanes a tile, tile `from` and every `step`-th behind it: a look at the table is then no memory access.
+// -1: behind the last tile, or outside the pool, where an id is not followed and its tokens are masked.
+__device__ __forceinline__ int kv4_page_ids(const Kv4Attn& a, int b, int from, int step, int n_tiles, int lane) {
+    const int t = from + (lane >> 1) * step, at = 2 * t + (lane & 1);
+    int page = -1;
+    if (t < n_tiles && at < a.max_pages) page = a.table[(size_t)b * a.max_pages + at];
+    return page < a.n_pages ? page : -1;
+}
+
+// A step's rows: few pairs.  KW waves share their pairs and take a key chunk's tiles in turn; a workgroup has a.row_waves times as
+// many, each KW of them with pairs of their own (over the same keys, which they so find in the L1 cache).
+template <int HD, int MT, int KW>
+__global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv4_attention(Kv4Attn a) {
+    using W = Kv4Wave<HD, MT>;
+    using L = Kv4Layout<HD>;
+    constexpr int AHEAD = MT * HD >= 256 ? 1 : 2;           // tiles under way: as many as the registers of two waves a SIMD hold beside the sums
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), col = lane & 15, r = lane >> 4;
+    // (the last waves have the fewest pairs; every second workgroup of a compute unit takes them the other way round, or the same SIMDs would
+    // have the full ones every time)
+    const int kw = wave % KW, turned = (blockIdx.y * gridDim.x + blockIdx.x) / 256 % 2, rw = turned ? a.row_waves - 1 - wave / KW : wave / KW;
+    Kv4Scales<HD>& sc = reinterpret_cast<Kv4Scales<HD>*>(lds)[wave];
+    const int b = blockIdx.y / a.Hkv, h = blockIdx.y % a.Hkv, share = a.H / a.Hkv;
+    const int tile = blockIdx.x / a.chunks, chunk = blockIdx.x % a.chunks;
+    const Kv4Seq sq = kv4_seq(a, b);
+    const int wg_pair = tile * a.row_waves * 16 * MT;
+    if (wg_pair >= sq.n * share) return;                   // (the whole workgroup; a wave without pairs among them goes on without keys)
+    W w(sq, h, share, wg_pair + rw * 16 * MT, lane);
+    const int len = min(max(sq.len, 0), a.max_pages * TASC_KV_BLOCK);
+    const int n_tiles = min(w.tiles(len), chunk + 1 < a.chunks ? (chunk + 1) * a.chunk_tiles : INT32_MAX);
+    const size_t page_bytes = (size_t)a.Hkv * L::HEAD;
+    const uint8_t* const pool = a.pool + (size_t)h * L::HEAD;
+    const int first_tile = chunk * a.chunk_tiles + kw;
+    int ids = kv4_page_ids(a, b, first_tile, KW, n_tiles, lane), ids_next = 0;
+    auto where = [&](int page) { return pool + (size_t)max(page, 0) * page_bytes; };
+    w.ask(a);
+    // the first tiles are under way while the queries are looked at
+    Kv4Tile<HD> tile_a, tile_b;
+    int pa0 = __builtin_amdgcn_readlane(ids, 0), pa1 = __builtin_amdgcn_readlane(ids, 1);
+    int pb0 = __builtin_amdgcn_readlane(ids, 2), pb1 = __builtin_amdgcn_readlane(ids, 3);
+    kv4_fetch<HD>(tile_a, where(pa0), where(pa1), lane);   // (without tiles: page 0, not used)
+    if constexpr (AHEAD == 2) kv4_fetch<HD>(tile_b, where(pb0), where(pb1), lane);
+    w.begin();
+    const Kv4Bits bits = kv4_bits();
+    const float scale2 = a.scale * 1.44269504088896340736f;   // scores in powers of 2
+
+    // one tile out of `cur`, whose registers then take the tile of the pages that come next
+    auto work = [&](Kv4Tile<HD>& cur, int t, int pg0, int pg1, int ng0, int ng1) __attribute__((always_inline)) {
+        const int at = 32 * t;
+        const bool whole = pg0 >= 0 && pg1 >= 0 && at + 31 <= w.first_last && at + 32 <= len;
+        kv4_work_scales<HD>(sc, cur.ks, cur.vs, scale2, at, whole, pg0 >= 0, pg1 >= 0, len, lane);
+        __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wave's LDS accesses are in order: the compiler has to keep them so)
+        __builtin_amdgcn_wave_barrier();
+#pragma unroll
+        for (int p = 0; p < 2; ++p) {
+            if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
+            kv4_bf16x8 fk[W::KSTEPS];
+#pragma unroll
+            for (int i = 0; i < W::KSTEPS; ++i) fk[i] = kv4_key_part<HD>(bits, cur, p, i);
+            w.scores(p, fk, sc);
+        }
+        if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
+        const Kv4Values<HD> values = kv4_values<HD>(cur);
+        if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
+        kv4_fetch<HD>(cur, where(ng0), where(ng1), lane);
+        kv4_bf16x8 fv[W::DT];
+#pragma unroll
+        for (int j = 0; j < W::DT; ++j) fv[j] = kv4_value_part<HD>(bits, values, j);
+        w.sums(fv, sc, at, whole, pg0 >= 0, pg1 >= 0, len);
     };
     int k = 2 * AHEAD;                                      // place of the next tile's ids
     for (int t = first_tile; t < n_tiles; t += AHEAD * KW) {
-        if (k == 2 * AHEAD) ids_next = page_ids(t + 32 * KW);   // (32 tiles ahead)
+        if (k == 2 * AHEAD) ids_next = kv4_page_ids(a, b, t + 32 * KW, KW, n_tiles, lane);   // (32 tiles ahead)
         if (k == 64) { ids = ids_next; k = 0; }
         const int na0 = __builtin_amdgcn_readlane(ids, k), na1 = __builtin_amdgcn_readlane(ids, k + 1);
         if constexpr (AHEAD == 2) {
@@ -600,97 +689,157 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         k += 2 * AHEAD;
     }
 
-    // the four lanes' sums, and the channels' share of ev
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
-        l[t] = kv4_quad_sum(l[t]);
-        if (lim[t] != kKv4Grown) m[t] = -__builtin_inff();   // no key
-#pragma unroll
-        for (int g = 0; g < G; ++g) {
-            const float e = __shfl(ev[t][g] + ev[t][2 + g], col);
-#pragma unroll
-            for (int j = g * (DT / G); j < (g + 1) * (DT / G); ++j) acc[t][j] += e;
-        }
-    }
-    // A lane's channels: of tile j row 4 r + i, channel (HD 128, 64) 64 (j / 4) + 16 r + 4 i + j % 4, (32) 8 r + 2 i + j.  With KW > 1 every wave
-    // leaves its sums in LDS and joins a part of the channels, in wave order.
-    constexpr int QUADS = DT / 4 > 0 ? DT / 4 : 1, ITEMS = 4 * QUADS;    // (i, group of four tiles j)
-    constexpr int SPAN = MT * ITEMS;
+    // every wave leaves its sums in LDS and joins a part of the channels, in wave order
+    w.end();
+    constexpr int ITEMS = W::ITEMS, SPAN = MT * ITEMS;
     float4* const sx = reinterpret_cast<float4*>(lds) + (size_t)rw * KW * SPAN * 64;                      // [KW][MT][ITEMS][64]
     float2* const sm = reinterpret_cast<float2*>(reinterpret_cast<float4*>(lds) + (size_t)a.row_waves * KW * SPAN * 64) + rw * KW * MT * 16;   // [KW][MT][16]
-    auto quad = [&](int t, int item) {
-        const int i = item / QUADS, j = 4 * (item % QUADS);
-        return HD == 32 ? make_float4(acc[t][0][i], acc[t][1][i], 0.f, 0.f) : make_float4(acc[t][j][i], acc[t][j + 1][i], acc[t][j + 2][i], acc[t][j + 3][i]);
-    };
-    if constexpr (KW > 1) {
-        __syncthreads();                                    // (the scales are read)
-#pragma unroll
-        for (int t = 0; t < MT; ++t) {
-#pragma unroll
-            for (int item = 0; item < ITEMS; ++item) sx[((kw * MT + t) * ITEMS + item) * 64 + lane] = quad(t, item);
-            if (r == 0) sm[(kw * MT + t) * 16 + col] = make_float2(m[t], l[t]);
-        }
-        __syncthreads();
-    }
+    __syncthreads();                                        // (the scales are read)
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        const int pair = pair0 + 16 * t + col, row = sq.first + pair / share, head = h * share + pair % share;
-        float part[KW];
-        if constexpr (KW > 1) {
-            float top = -__builtin_inff();
 #pragma unroll
-            for (int w = 0; w < KW; ++w) top = fmaxf(top, sm[(w * MT + t) * 16 + col].x);
-            l[t] = 0.f;
+        for (int item = 0; item < ITEMS; ++item) sx[((kw * MT + t) * ITEMS + item) * 64 + lane] = w.quad(t, item);
+        if (r == 0) sm[(kw * MT + t) * 16 + col] = make_float2(w.m[t], w.l[t]);
+    }
+    __syncthreads();
 #pragma unroll
-            for (int w = 0; w < KW; ++w) {
-                const float2 ml = sm[(w * MT + t) * 16 + col];
-                part[w] = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
-                l[t] = __builtin_fmaf(ml.y, part[w], l[t]);
-            }
-            m[t] = top;
+    for (int t = 0; t < MT; ++t) {
+        float part[KW], top = -__builtin_inff(), l = 0.f;
+#pragma unroll
+        for (int x = 0; x < KW; ++x) top = fmaxf(top, sm[(x * MT + t) * 16 + col].x);
+#pragma unroll
+        for (int x = 0; x < KW; ++x) {
+            const float2 ml = sm[(x * MT + t) * 16 + col];
+            part[x] = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
+            l = __builtin_fmaf(ml.y, part[x], l);
         }
-        if (pair >= n_pairs || row >= a.rows) continue;
-        const float inv = a.chunks > 1 ? 1.f : l[t] > 0.f ? 1.f / l[t] : l[t];       // a pair without keys gives zeros (a NaN stays one)
+        int row, head;
+        if (!w.pair(t, a.rows, row, head)) continue;
+        const float inv = kv4_inverse(l);
         const size_t at = ((size_t)chunk * a.rows + row) * a.H + head;
         constexpr int MINE = ITEMS / KW > 0 ? ITEMS / KW : 1;
         if (KW <= ITEMS || kw < ITEMS)
 #pragma unroll
             for (int n = 0; n < MINE; ++n) {
-                float4 o;
-                int item = n;
-                if constexpr (KW == 1) o = quad(t, n);
-                else {
-                    item = kw * MINE + n;
-                    o = make_float4(0.f, 0.f, 0.f, 0.f);
+                const int item = kw * MINE + n, d = w.channel(item);
+                float4 o = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
-                    for (int w = 0; w < KW; ++w) {
-                        const float4 x = sx[((w * MT + t) * ITEMS + item) * 64 + lane];
-                        o.x = __builtin_fmaf(x.x, part[w], o.x);
-                        o.y = __builtin_fmaf(x.y, part[w], o.y);
-                        o.z = __builtin_fmaf(x.z, part[w], o.z);
-                        o.w = __builtin_fmaf(x.w, part[w], o.w);
-                    }
+                for (int x = 0; x < KW; ++x) {
+                    const float4 v = sx[((x * MT + t) * ITEMS + item) * 64 + lane];
+                    o.x = __builtin_fmaf(v.x, part[x], o.x);
+                    o.y = __builtin_fmaf(v.y, part[x], o.y);
+                    o.z = __builtin_fmaf(v.z, part[x], o.z);
+                    o.w = __builtin_fmaf(v.w, part[x], o.w);
                 }
-                const int i = item / QUADS, d = HD == 32 ? 8 * r + 2 * i : 64 * (item % QUADS) + 16 * r + 4 * i;
                 if (a.chunks == 1) {
-                    uint16_t* to = reinterpret_cast<uint16_t*>(a.out + (size_t)row * a.out_stride + head * HD + d);
-                    if constexpr (HD == 32) *reinterpret_cast<uint32_t*>(to) = f2bf_pair(o.x * inv, o.y * inv);
-                    else *reinterpret_cast<kv4_u32x2*>(to) = kv4_u32x2{f2bf_pair(o.x * inv, o.y * inv), f2bf_pair(o.z * inv, o.w * inv)};
+                    W::store(a, row, head, d, o, inv);
                 } else {
                     float* to = a.part_o + at * HD + d;
                     if constexpr (HD == 32) *reinterpret_cast<float2*>(to) = make_float2(o.x, o.y);
                     else *reinterpret_cast<float4*>(to) = o;
                 }
             }
-        if (a.chunks > 1 && kw == 0 && r == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(m[t], l[t]);
+        if (a.chunks > 1 && kw == 0 && r == 0) *reinterpret_cast<float2*>(a.part_ml + 2 * at) = make_float2(top, l);
     }
 }
 // LDS of a workgroup of `waves` waves
 template <int HD, int MT, int KW>
 int kv4_attention_lds(int waves) {
-    const int scales = waves * (int)sizeof(Kv4Scales<HD>), join = KW == 1 ? 0 : waves * MT * ((HD >= 64 ? HD / 16 : 4) * 64 * 16 + 16 * 8);
+    const int scales = waves * (int)sizeof(Kv4Scales<HD>), join = waves * MT * ((HD >= 64 ? HD / 16 : 4) * 64 * 16 + 16 * 8);
     return scales > join ? scales : join;
 }
+
+// A prompt's rows: enough pairs that every wave has 32 of its own and sees all of their keys.  What a tile comes to before it meets
+// a query (numbers as bf16, scales) is a third of a wave's instructions, so the four waves of a workgroup work out a tile each, a
+// fragment of a product's operand a KB of LDS, and all of them take the four.
+template <int HD>
+struct Kv4Staged {
+    kv4_u32x4 key[2][HD / 32][64], value[HD / 16][64];
+    Kv4Scales<HD> scales;
+};
+constexpr int kKv4RowWaves = 4;
+template <int HD>
+__global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv4_attention_rows(Kv4Attn a) {
+    constexpr int MT = 2, WAVES = kKv4RowWaves;
+    using W = Kv4Wave<HD, MT>;
+    using L = Kv4Layout<HD>;
+    extern __shared__ __attribute__((aligned(16))) float lds[];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    Kv4Staged<HD>* const staged = reinterpret_cast<Kv4Staged<HD>*>(lds);                 // [WAVES]
+    const int b = blockIdx.y / a.Hkv, h = blockIdx.y % a.Hkv, share = a.H / a.Hkv;
+    const Kv4Seq sq = kv4_seq(a, b);
+    // the last pairs see the most keys: they begin first
+    const int n_pairs = sq.n * share, n_wgs = (n_pairs + 16 * MT * WAVES - 1) / (16 * MT * WAVES), turn = n_wgs - 1 - (int)blockIdx.x;
+    if (turn < 0) return;
+    W w(sq, h, share, (turn * WAVES + wave) * 16 * MT, lane);
+    const int len = min(max(sq.len, 0), a.max_pages * TASC_KV_BLOCK);
+    const int mine = w.tiles(len);
+    const int n_tiles = (min(sq.len - sq.n + (min((turn + 1) * WAVES * 16 * MT, n_pairs) - 1) / share + 1, len) + 31) / 32;    // of the workgroup
+    const size_t page_bytes = (size_t)a.Hkv * L::HEAD;
+    const uint8_t* const pool = a.pool + (size_t)h * L::HEAD;
+    auto where = [&](int page) { return pool + (size_t)max(page, 0) * page_bytes; };
+    int ids = kv4_page_ids(a, b, wave, WAVES, n_tiles, lane), ids_next = 0, k = 0;
+    w.ask(a);
+    Kv4Tile<HD> tile;
+    int pg0 = __builtin_amdgcn_readlane(ids, 0), pg1 = __builtin_amdgcn_readlane(ids, 1);
+    kv4_fetch<HD>(tile, where(pg0), where(pg1), lane);
+    w.begin();
+    const Kv4Bits bits = kv4_bits();
+    const float scale2 = a.scale * 1.44269504088896340736f;
+    __shared__ int s_ok[WAVES];                             // pages of a tile that are in the pool: bits 0, 1
+    for (int t0 = 0; t0 < n_tiles; t0 += WAVES) {
+        {
+            Kv4Staged<HD>& to = staged[wave];
+            const int t = t0 + wave;
+            const bool inside = pg0 >= 0 && pg1 >= 0 && 32 * t + 32 <= len;
+            kv4_work_scales<HD>(to.scales, tile.ks, tile.vs, scale2, 32 * t, inside, pg0 >= 0, pg1 >= 0, len, lane);
+#pragma unroll
+            for (int p = 0; p < 2; ++p)
+#pragma unroll
+                for (int i = 0; i < W::KSTEPS; ++i) to.key[p][i][lane] = __builtin_bit_cast(kv4_u32x4, kv4_key_part<HD>(bits, tile, p, i));
+            const Kv4Values<HD> values = kv4_values<HD>(tile);
+#pragma unroll
+            for (int j = 0; j < W::DT; ++j) to.value[j][lane] = __builtin_bit_cast(kv4_u32x4, kv4_value_part<HD>(bits, values, j));
+            if (lane == 0) s_ok[wave] = (pg0 >= 0 ? 1 : 0) | (pg1 >= 0 ? 2 : 0);
+        }
+        // the next four tiles are under way while these are worked on
+        k += 2;
+        if (k == 2) ids_next = kv4_page_ids(a, b, t0 + wave + 32 * WAVES, WAVES, n_tiles, lane);
+        if (k == 64) { ids = ids_next; k = 0; }
+        pg0 = __builtin_amdgcn_readlane(ids, k);
+        pg1 = __builtin_amdgcn_readlane(ids, k + 1);
+        kv4_fetch<HD>(tile, where(pg0), where(pg1), lane);
+        __syncthreads();
+        for (int n = 0; n < WAVES && t0 + n < mine; ++n) {
+            const Kv4Staged<HD>& from = staged[n];
+            const int at = 32 * (t0 + n), ok = __builtin_amdgcn_readfirstlane(s_ok[n]);
+            const bool whole = ok == 3 && at + 31 <= w.first_last && at + 32 <= len;
+#pragma unroll
+            for (int p = 0; p < 2; ++p) {
+                kv4_bf16x8 fk[W::KSTEPS];
+#pragma unroll
+                for (int i = 0; i < W::KSTEPS; ++i) fk[i] = __builtin_bit_cast(kv4_bf16x8, from.key[p][i][lane]);
+                w.scores(p, fk, from.scales);
+            }
+            kv4_bf16x8 fv[W::DT];
+#pragma unroll
+            for (int j = 0; j < W::DT; ++j) fv[j] = __builtin_bit_cast(kv4_bf16x8, from.value[j][lane]);
+            w.sums(fv, from.scales, at, whole, ok & 1, (ok >> 1) & 1, len);
+        }
+        __syncthreads();
+    }
+    w.end();
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+        int row, head;
+        if (!w.pair(t, a.rows, row, head)) continue;
+        const float inv = kv4_inverse(w.l[t]);
+#pragma unroll
+        for (int item = 0; item < W::ITEMS; ++item) W::store(a, row, head, w.channel(item), w.quad(t, item), inv);
+    }
+}
+template <int HD>
+int kv4_attention_rows_lds() { return kKv4RowWaves * (int)sizeof(Kv4Staged<HD>); }
 
 // The key chunks' results in chunk order: HD / 4 lanes a (row, head) pair, four channels each; a workgroup per (sequence, row, 1024 / HD heads).
 template <int HD>

@@ -5,6 +5,32 @@
 
 namespace {
 
+// A kernel's largest dynamic LDS, set once per device where it is beyond the default
+struct LdsRoom {
+    std::mutex mu;
+    bool ready[16] = {};
+    tasc_status for_kernel(const void* kernel, int bytes) {
+        if (bytes <= 65536) return TASC_OK;
+        int dev = 0;
+        TASC_HIP(hipGetDevice(&dev));
+        std::lock_guard<std::mutex> lock(mu);
+        if (ready[dev & 15]) return TASC_OK;
+        TASC_HIP(hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, bytes));
+        ready[dev & 15] = true;
+        return TASC_OK;
+    }
+};
+
+template <int HD>
+tasc_status attend_rows(const Kv4Attn& a, hipStream_t st) {
+    const int64_t pairs = (int64_t)a.max_rows * (a.H / a.Hkv), per = 32 * kKv4RowWaves;
+    const int lds = kv4_attention_rows_lds<HD>();
+    static LdsRoom room;
+    const tasc_status rc = room.for_kernel(reinterpret_cast<const void*>(&k_kv4_attention_rows<HD>), lds);
+    if (rc != TASC_OK) return rc;
+    k_kv4_attention_rows<HD><<<dim3((unsigned)((pairs + per - 1) / per), (unsigned)(a.batch * a.Hkv)), dim3(64 * kKv4RowWaves), lds, st>>>(a);
+    return TASC_OK;
+}
 template <int HD, int MT, int KW>
 tasc_status attend(Kv4Attn a, hipStream_t st) {
     // four waves a workgroup (KW at least), fewer where the pairs end before
@@ -13,17 +39,9 @@ tasc_status attend(Kv4Attn a, hipStream_t st) {
     a.row_waves = (int)std::min<int64_t>(waves, MOST);
     const int64_t tiles = (waves + a.row_waves - 1) / a.row_waves;
     const int lds = kv4_attention_lds<HD, MT, KW>(a.row_waves * KW);
-    if (kv4_attention_lds<HD, MT, KW>(MOST * KW) > 65536) {
-        int dev = 0;
-        TASC_HIP(hipGetDevice(&dev));
-        static std::mutex mu;
-        static bool ready[16];
-        std::lock_guard<std::mutex> lock(mu);
-        if (!ready[dev & 15]) {
-            TASC_HIP(hipFuncSetAttribute(reinterpret_cast<const void*>(&k_kv4_attention<HD, MT, KW>), hipFuncAttributeMaxDynamicSharedMemorySize, kv4_attention_lds<HD, MT, KW>(MOST * KW)));
-            ready[dev & 15] = true;
-        }
-    }
+    static LdsRoom room;
+    const tasc_status rc = room.for_kernel(reinterpret_cast<const void*>(&k_kv4_attention<HD, MT, KW>), kv4_attention_lds<HD, MT, KW>(MOST * KW));
+    if (rc != TASC_OK) return rc;
     k_kv4_attention<HD, MT, KW><<<dim3((unsigned)(tiles * a.chunks), (unsigned)(a.batch * a.Hkv)), dim3((unsigned)(64 * a.row_waves * KW)), lds, st>>>(a);
     return TASC_OK;
 }
@@ -33,7 +51,7 @@ tasc_status attend_hd(const Kv4Attn& a, int kw, hipStream_t st) {
     tasc_status rc;
     if (kw == 8) rc = attend<HD, 1, 8>(a, st);
     else if (kw == 4) rc = attend<HD, 1, 4>(a, st);
-    else if (kw == 1) rc = attend<HD, 2, 1>(a, st);
+    else if (kw == 1) rc = attend_rows<HD>(a, st);
     else if (pairs <= 16) rc = attend<HD, 1, 2>(a, st);
     else rc = attend<HD, 2, 2>(a, st);
     if (rc != TASC_OK) return rc;
