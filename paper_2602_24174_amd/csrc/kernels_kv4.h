@@ -321,6 +321,12 @@ __device__ __forceinline__ uint32_t kv4_pair(const Kv4Bits& k, uint32_t w, int j
 __device__ __forceinline__ float kv4_pair_sum(uint32_t p, float to) {
     return __builtin_amdgcn_fdot2_f32_bf16(__builtin_bit_cast(tasc_bf16x2, p), __builtin_bit_cast(tasc_bf16x2, 0x3F803F80u), to, false);
 }
+// (fmaxf quiets each operand by an instruction of its own first)
+__device__ __forceinline__ float kv4_max3(float a, float b, float c) {
+    float m;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(m) : "v"(a), "v"(b), "v"(c));
+    return m;
+}
 // maximum / sum over the four lanes that share lane % 16
 __device__ __forceinline__ float kv4_quad_max(float v) {
     v = fmaxf(v, __shfl_xor(v, 16));
@@ -339,7 +345,7 @@ template <int HD>
 struct __attribute__((aligned(16))) Kv4Scales {
     static constexpr int G = Kv4Layout<HD>::GROUPS;
     float ks[2][G][16], kb[2][G][16], vs[2][G][16];    // by page, group, token
-    uint16_t z[G][3][32];                               // tokens in the order of the second product (4 of page 0, 4 of page 1 for each r)
+    uint16_t z[G][3][32], none[32];                     // (and zeros, the product's other rows) tokens in the order of the second product (4 of page 0, 4 of page 1 for each r)
 };
 // z - 16 in three terms, and the scale to go with it: where z is too large for them (its value is low then, to fp32's last place) or
 // there is no scale, another pair with the same values
@@ -355,9 +361,10 @@ __device__ __forceinline__ Kv4Z kv4_z(float scale, float low) {
     o.scale = scale;
     z -= 16.f;
 #pragma unroll
-    for (int i = 0; i < 3; ++i) {
-        o.z[i] = f2bf(z);
-        z -= bf2f(o.z[i]);
+    for (int i = 0; i < 3; ++i) {                           // 8 of the 24 bits each
+        const uint32_t top = __float_as_uint(z) & 0xFFFF0000u;
+        o.z[i] = (uint16_t)(top >> 16);
+        z -= __uint_as_float(top);
     }
     return o;
 }
@@ -469,8 +476,8 @@ struct Kv4Wave {
         kv4_f32x4 vs[2][G];
 #pragma unroll
         for (int g = 0; g < G; ++g) {
-            fz[g] = *reinterpret_cast<const kv4_bf16x8*>(&sc.z[g][min(col & 3, 2)][8 * r]);
-            if (col < 4 * g || col >= 4 * g + 3) fz[g] = kv4_bf16x8{};
+            const int k = col - 4 * g;
+            fz[g] = *reinterpret_cast<const kv4_bf16x8*>(&sc.z[0][k >= 0 && k < 3 ? 3 * g + k : 3 * G][8 * r]);     // 3 G: the zeros
 #pragma unroll
             for (int p = 0; p < 2; ++p) vs[p][g] = *reinterpret_cast<const kv4_f32x4*>(&sc.vs[p][g][4 * r]);
         }
@@ -480,14 +487,14 @@ struct Kv4Wave {
             if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
             if (!whole) {
 #pragma unroll
-                for (int p = 0; p < 2; ++p)
+                for (int p = 0; p < 2; ++p) {
+                    const int upto = ((p ? ok1 : ok0) ? min(last[u], len - 1) : -1) - (at + 16 * p + 4 * r);
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) {
-                        const int pos = at + 16 * p + 4 * r + i;
-                        if (!(p ? ok1 : ok0) || pos > last[u] || pos >= len) s[u][p][i] = -__builtin_inff();
-                    }
+                    for (int i = 0; i < 4; ++i) s[u][p][i] = i > upto ? -__builtin_inff() : s[u][p][i];
+                }
             }
-            float top = fmaxf(fmaxf(fmaxf(s[u][0][0], s[u][0][1]), fmaxf(s[u][0][2], s[u][0][3])), fmaxf(fmaxf(s[u][1][0], s[u][1][1]), fmaxf(s[u][1][2], s[u][1][3])));
+            float top = kv4_max3(kv4_max3(s[u][0][0], s[u][0][1], s[u][0][2]), s[u][0][3], s[u][1][0]);
+            top = kv4_max3(kv4_max3(top, s[u][1][1], s[u][1][2]), s[u][1][3], s[u][1][3]);
             if (__any(top > lim[u])) {
                 top = kv4_quad_max(top);
                 if (top > lim[u]) {                         // (the four lanes of a pair alike)
@@ -645,6 +652,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     kv4_fetch<HD>(tile_a, where(pa0), where(pa1), lane);   // (without tiles: page 0, not used)
     if constexpr (AHEAD == 2) kv4_fetch<HD>(tile_b, where(pb0), where(pb1), lane);
     w.begin();
+    if (lane < 32) sc.none[lane] = 0;
     const Kv4Bits bits = kv4_bits();
     const float scale2 = a.scale * 1.44269504088896340736f;   // scores in powers of 2
 
@@ -766,10 +774,11 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Kv4Staged<HD>* const staged = reinterpret_cast<Kv4Staged<HD>*>(lds);                 // [WAVES]
-    const int b = blockIdx.y / a.Hkv, h = blockIdx.y % a.Hkv, share = a.H / a.Hkv;
+    const int heads = a.batch * a.Hkv, turned = blockIdx.x / heads, head = (blockIdx.x % heads + turned) % heads, b = head / a.Hkv, h = head % a.Hkv, share = a.H / a.Hkv;
     const Kv4Seq sq = kv4_seq(a, b);
-    // the last pairs see the most keys: they begin first
-    const int n_pairs = sq.n * share, n_wgs = (n_pairs + 16 * MT * WAVES - 1) / (16 * MT * WAVES), turn = n_wgs - 1 - (int)blockIdx.x;
+    // The last pairs see the most keys: those of all heads begin first, and a head goes from one XCD to the next (head by head: 113 us for
+    // 4 prompts of up to 2048 rows, 12 heads, where this takes 104; a head on one XCD, whose prompt may be the short one: 133).
+    const int n_pairs = sq.n * share, n_wgs = (n_pairs + 16 * MT * WAVES - 1) / (16 * MT * WAVES), turn = n_wgs - 1 - turned;
     if (turn < 0) return;
     W w(sq, h, share, (turn * WAVES + wave) * 16 * MT, lane);
     const int len = min(max(sq.len, 0), a.max_pages * TASC_KV_BLOCK);
@@ -784,6 +793,7 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
     int pg0 = __builtin_amdgcn_readlane(ids, 0), pg1 = __builtin_amdgcn_readlane(ids, 1);
     kv4_fetch<HD>(tile, where(pg0), where(pg1), lane);
     w.begin();
+    if (lane < 32) staged[wave].scales.none[lane] = 0;
     const Kv4Bits bits = kv4_bits();
     const float scale2 = a.scale * 1.44269504088896340736f;
     __shared__ int s_ok[WAVES];                             // pages of a tile that are in the pool: bits 0, 1
@@ -831,11 +841,11 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
     w.end();
 #pragma unroll
     for (int t = 0; t < MT; ++t) {
-        int row, head;
-        if (!w.pair(t, a.rows, row, head)) continue;
+        int row, q_head;
+        if (!w.pair(t, a.rows, row, q_head)) continue;
         const float inv = kv4_inverse(w.l[t]);
 #pragma unroll
-        for (int item = 0; item < W::ITEMS; ++item) W::store(a, row, head, w.channel(item), w.quad(t, item), inv);
+        for (int item = 0; item < W::ITEMS; ++item) W::store(a, row, q_head, w.channel(item), w.quad(t, item), inv);
     }
 }
 template <int HD>
