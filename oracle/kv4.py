@@ -41,19 +41,17 @@ def attention(q, k, v, n_rows, scale):
     0 .. tokens - n_rows + i.  Returns (out float64 [n_rows, heads, head_dim], bound of what a computation in float32 with weights rounded
     to bf16 and a bf16 result may be off).
 
-    The bound.  A weight times its scale is rounded to bf16 (2^-8 relative) and meets the number less 7.5, the weight itself is rounded (2^-8)
-    and meets low + 7.5 scale, which is held in two bf16 parts (2^-16 of it); the result is rounded (2^-8).
+    The bound.  A weight times its scale is rounded to bf16 (2^-8 relative) and meets the whole value, number and low; the result is
+    rounded (2^-8).
     In float32 (2^-24 an operation): a score is a sum of head_dim products q (16 + c) scale and of (low - 16 scale) sum q, in at most
     head_dim + 16 operations; an error d of the scores changes each weight by a factor within exp(+-d), so the result by 2 d sum w |v|;
     exponentials are good to 2^-21 with the rounding of their arguments; and the sums over the tokens take at most tokens / 8 + 64 operations on
-    terms (16 + c) scale, 23.5 scale and |low + 7.5 scale|."""
+    terms (16 + c) scale and low - 16 scale."""
     tokens, heads, share = k[0].shape[0], q.shape[1], q.shape[1] // k[0].shape[1]
     kv, vv = values(*k), values(*v)
     hd = q.shape[2]
     out, bound = np.zeros(q.shape), np.zeros(q.shape)
-    middle = np.abs(v[2] + 7.5 * v[1])[..., None]
-    centred = (np.abs((v[0] - 7.5) * v[1][..., None]) + (1 + 2.0 ** -8) * middle).reshape(vv.shape)
-    reach = (np.abs(v[1])[..., None] * (39.5 + v[0]) + middle).reshape(vv.shape)
+    reach = (np.abs(v[1])[..., None] * (32 + v[0]) + np.abs(v[2])[..., None]).reshape(vv.shape)
     for i in range(n_rows):
         n = tokens - n_rows + i + 1
         if n <= 0:
@@ -66,7 +64,7 @@ def attention(q, k, v, n_rows, scale):
             w = np.exp(x - x.max())
             w /= w.sum()
             out[i, h] = w @ vv[:n, g]
-            bound[i, h] = 2.0 ** -8 * np.abs(out[i, h]) + 2.0 ** -8 * (w @ centred[:n, g]) + 2 * d * (w @ np.abs(vv[:n, g])) + \
+            bound[i, h] = 2.0 ** -8 * np.abs(out[i, h]) + 2.0 ** -8 * (w @ np.abs(vv[:n, g])) + 2 * d * (w @ np.abs(vv[:n, g])) + \
                 (tokens / 8 + 64) * 2.0 ** -24 * (w @ reach[:n, g])
             bound[i, h] *= 1.02                             # products of the above
     return out, bound

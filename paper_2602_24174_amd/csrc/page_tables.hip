@@ -159,7 +159,7 @@ extern "C" tasc_status tasc_page_tables(const int32_t* kv_len, const int32_t* ne
     TASC_REQUIRE(max_pages >= 1 && max_pages < 1 << 27, "page_tables: max_pages %d outside [1, 2^27)", max_pages);
     TASC_REQUIRE(n_free >= 0 && n_free < 1 << 27, "page_tables: n_free %d outside [0, 2^27)", n_free);
     TASC_REQUIRE(slots_cap >= 0 && (slots || slots_cap == 0), "page_tables: %d slots", slots_cap);
-    TASC_REQUIRE(!pages || pages != held, "page_tables: pages and held are one array");
+    TASC_REQUIRE(!pages || !held || pages + batch <= held || held + batch <= pages, "page_tables: pages and held overlap");
     // runs of at least 8 sequences (a wave each), 256 workgroups at most: each reads all lengths
     const int per_wg = std::max(8, (batch + 255) / 256);
     const PageArgs a{kv_len, new_rows, held, free_pages, table, pages, row_off, slots, summary, batch, n_free, max_pages, slots_cap, per_wg};

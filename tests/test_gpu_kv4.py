@@ -255,6 +255,51 @@ def test_large_scores_and_far_maxima():
     batch.check(batch.run())
 
 
+@pytest.mark.parametrize("hd", [32, 64, 128])
+def test_values_of_any_range(hd):
+    """Groups without a range, narrow ones far from zero, wide ones, ones beside the smallest and the largest numbers, in both roles."""
+    import torch
+    import paper_2602_24174_amd as T
+    rng = np.random.default_rng(hd)
+    n = 70
+    x = rng.normal(size=(2, n, 2, hd)).astype(np.float32)
+    kinds = [lambda v: v * 0, lambda v: v * 0 + 5, lambda v: v * 0 - 0.3, lambda v: 1e4 + v * 1e-3, lambda v: -300 + v * 1e-9, lambda v: v * 1e-30, lambda v: v * 1e-39,
+             lambda v: 1e-20 + v * 1e-39, lambda v: v * 1e-41, lambda v: v * 40 + 1000]
+    for t in range(n):
+        x[1, t] = kinds[t % len(kinds)](x[1, t].astype(np.float64)).astype(np.float32)
+    x[0, 3::7] = x[0, 3::7] * 0 + 0.25
+    x[0, 5::7] = 1 + x[0, 5::7] * 1e-6
+    slots = torch.arange(n, dtype=torch.int32, device="cuda")
+    one = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    for first, last in ((0, 10), (0, n), (8, 9), (6, 7), (1, 2), (4, 5), (9, 10)):
+        some = x[:, first:last]
+        cache = dirty_cache(6, 2, hd)
+        T.tasc_kv4_append(cache, *(torch.tensor(some[i]).cuda() for i in (0, 1)), slots[:last - first])
+        q = torch.tensor(rng.normal(size=(2, 6, hd)).astype(np.float32)).bfloat16().cuda()
+        out = torch.zeros_like(q)
+        T.tasc_kv4_attention(cache, q, torch.arange(6, dtype=torch.int32, device="cuda")[None], one([0, 2]), one([last - first]), 2, n, hd ** -0.5, out)
+        want, bound = OK.attention(q.float().cpu().numpy().astype(np.float64), OK.quantise(some[0]), OK.quantise(some[1]), 2, hd ** -0.5)
+        # (bf16's smallest number is 2^-133: half of it more, and the weights' products end there)
+        assert (np.abs(out.float().cpu().numpy() - want) <= bound + 2.0 ** -133 * 33).all(), (first, last)
+
+
+def test_values_of_the_largest_numbers():
+    import torch
+    import paper_2602_24174_amd as T
+    rng = np.random.default_rng(8)
+    x = rng.normal(size=(2, 20, 2, 64)).astype(np.float32)
+    x[1, 4:9] = 1e36 * x[1, 4:9]
+    x[1, 9:12] = -3e37 * (1 + 1e-3 * x[1, 9:12])
+    cache, slots = dirty_cache(2, 2, 64), torch.arange(20, dtype=torch.int32, device="cuda")
+    T.tasc_kv4_append(cache, *(torch.tensor(t).cuda() for t in x), slots)
+    q = torch.tensor(rng.normal(size=(16, 4, 64)).astype(np.float32)).bfloat16().cuda()
+    out = torch.zeros_like(q)
+    one = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    T.tasc_kv4_attention(cache, q, one([[0, 1]]), one([0, 16]), one([20]), 16, 20, 0.125, out)
+    want, bound = OK.attention(q.float().cpu().numpy().astype(np.float64), OK.quantise(x[0]), OK.quantise(x[1]), 16, 0.125)
+    assert (np.abs(out.float().cpu().numpy() - want) <= bound).all()
+
+
 def test_offsets_beyond_32_bits():
     """A pool of more than 4 GiB whose last pages are used."""
     import torch
