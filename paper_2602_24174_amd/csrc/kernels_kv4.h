@@ -851,28 +851,42 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
 template <int HD>
 int kv4_attention_rows_lds() { return kKv4RowWaves * (int)sizeof(Kv4Staged<HD>); }
 
-// The key chunks' results in chunk order: HD / 4 lanes a (row, head) pair, four channels each; a workgroup per (sequence, row, 1024 / HD heads).
-template <int HD>
+// The key chunks' results joined: HD / 4 lanes a (row, head) pair, four channels each.  A workgroup has 1024 / HD pairs of a sequence's row,
+// or, of many chunks (SPLIT), one, whose chunks its 1024 / HD parts take in turn (64 chunks of 64 pairs: 9.6 -> 4.8 us).
+template <int HD, bool SPLIT>
 __global__ __launch_bounds__(256) void k_kv4_merge(Kv4Attn a) {
-    constexpr int LANES = HD / 4;
+    constexpr int LANES = HD / 4, PARTS = 256 / LANES;
+    __shared__ kv4_f32x4 s_o[SPLIT ? PARTS : 1][LANES];
+    __shared__ float2 s_ml[SPLIT ? PARTS : 1];
     const Kv4Seq sq = kv4_seq(a, blockIdx.y);
-    const int i = blockIdx.x % a.max_rows, row = sq.first + i;
-    const int head = blockIdx.x / a.max_rows * (256 / LANES) + threadIdx.x / LANES, d = 4 * (threadIdx.x % LANES);
-    if (i >= sq.n || row >= a.rows || head >= a.H) return;
+    const int i = blockIdx.x % a.max_rows, row = sq.first + i, part = threadIdx.x / LANES, lane = threadIdx.x % LANES;
+    const int head = SPLIT ? blockIdx.x / a.max_rows : blockIdx.x / a.max_rows * PARTS + part;
+    if (i >= sq.n || row >= a.rows || head >= a.H) return;  // (of SPLIT the whole workgroup)
     const size_t step = (size_t)a.rows * a.H, at = (size_t)row * a.H + head;
-    float top = -__builtin_inff();
+    const int c0 = SPLIT ? part : 0, by = SPLIT ? PARTS : 1;
+    float top = -__builtin_inff(), l = 0.f;
 #pragma unroll 8
-    for (int c = 0; c < a.chunks; ++c) top = fmaxf(top, a.part_ml[2 * (c * step + at)]);
-    float l = 0.f;
+    for (int c = c0; c < a.chunks; c += by) top = fmaxf(top, a.part_ml[2 * (c * step + at)]);
     kv4_f32x4 o = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll 8
-    for (int c = 0; c < a.chunks; ++c) {
-        const float2 ml = *reinterpret_cast<const float2*>(a.part_ml + 2 * (c * step + at));
-        const kv4_f32x4 x = *reinterpret_cast<const kv4_f32x4*>(a.part_o + (c * step + at) * HD + d);
+    auto join = [&](const float2& ml, const kv4_f32x4& x) {
         const float f = ml.x == top ? 1.f : __builtin_amdgcn_exp2f(ml.x - top);
         l = __builtin_fmaf(ml.y, f, l);
         o += x * f;
+    };
+#pragma unroll 8
+    for (int c = c0; c < a.chunks; c += by)
+        join(*reinterpret_cast<const float2*>(a.part_ml + 2 * (c * step + at)), *reinterpret_cast<const kv4_f32x4*>(a.part_o + (c * step + at) * HD + 4 * lane));
+    if constexpr (SPLIT) {
+        s_o[part][lane] = o;
+        if (lane == 0) s_ml[part] = make_float2(top, l);
+        __syncthreads();
+        if (part > 0) return;
+        for (int n = 0; n < PARTS; ++n) top = fmaxf(top, s_ml[n].x);
+        l = 0.f;
+        o = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int n = 0; n < PARTS; ++n) join(s_ml[n], s_o[n][lane]);
     }
-    const float inv = l > 0.f ? 1.f / l : l;
-    *reinterpret_cast<kv4_u32x2*>(a.out + (size_t)row * a.out_stride + head * HD + d) = kv4_u32x2{f2bf_pair(o[0] * inv, o[1] * inv), f2bf_pair(o[2] * inv, o[3] * inv)};
+    const float inv = kv4_inverse(l);
+    *reinterpret_cast<kv4_u32x2*>(a.out + (size_t)row * a.out_stride + head * HD + 4 * lane) = kv4_u32x2{f2bf_pair(o[0] * inv, o[1] * inv), f2bf_pair(o[2] * inv, o[3] * inv)};
 }

@@ -55,7 +55,8 @@ tasc_status attend_hd(const Kv4Attn& a, int kw, hipStream_t st) {
     else if (pairs <= 16) rc = attend<HD, 1, 2>(a, st);
     else rc = attend<HD, 2, 2>(a, st);
     if (rc != TASC_OK) return rc;
-    if (a.chunks > 1) k_kv4_merge<HD><<<dim3((unsigned)(a.max_rows * ((a.H + 1024 / HD - 1) / (1024 / HD))), (unsigned)a.batch), dim3(256), 0, st>>>(a);
+    if (a.chunks > 8) k_kv4_merge<HD, true><<<dim3((unsigned)(a.max_rows * a.H), (unsigned)a.batch), dim3(256), 0, st>>>(a);
+    else if (a.chunks > 1) k_kv4_merge<HD, false><<<dim3((unsigned)(a.max_rows * ((a.H + 1024 / HD - 1) / (1024 / HD))), (unsigned)a.batch), dim3(256), 0, st>>>(a);
     TASC_LAUNCH_CHECK();
     return TASC_OK;
 }
