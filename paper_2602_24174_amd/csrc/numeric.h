@@ -77,18 +77,32 @@ __device__ __forceinline__ float wave_max_dpp(float v) {
     auto row = [&](int l) { return __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), l)); };
     return fmaxf(fmaxf(row(0), row(16)), fmaxf(row(32), row(48)));
 }
-__device__ __forceinline__ double wave_sum64_dpp(double v) {
-    auto up = [](double x, auto ctrl) {
-        const u64 b = __builtin_bit_cast(u64, x);
-        const u32 lo = __builtin_amdgcn_update_dpp(0, (int)(u32)b, decltype(ctrl)::value, 0xF, 0xF, false);
-        const u32 hi = __builtin_amdgcn_update_dpp(0, (int)(u32)(b >> 32), decltype(ctrl)::value, 0xF, 0xF, false);
-        return x + __builtin_bit_cast(double, (u64)hi << 32 | lo);
-    };
-    v = up(v, std::integral_constant<int, 0xB1>{});
-    v = up(v, std::integral_constant<int, 0x4E>{});
-    v = up(v, std::integral_constant<int, 0x141>{});
-    v = up(v, std::integral_constant<int, 0x140>{});
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ double lane64_dpp(double v) {   // 0 where the lane has no source
     const u64 b = __builtin_bit_cast(u64, v);
-    auto row = [&](int l) { return __builtin_bit_cast(double, (u64)(u32)__builtin_amdgcn_readlane((int)(u32)(b >> 32), l) << 32 | (u32)__builtin_amdgcn_readlane((int)(u32)b, l)); };
-    return (row(0) + row(16)) + (row(32) + row(48));
+    const u32 lo = __builtin_amdgcn_update_dpp(0, (int)(u32)b, CTRL, ROWS, 0xF, false), hi = __builtin_amdgcn_update_dpp(0, (int)(u32)(b >> 32), CTRL, ROWS, 0xF, false);
+    return __builtin_bit_cast(double, (u64)hi << 32 | lo);
+}
+__device__ __forceinline__ double lane64(double v, int l) {  // l: the same in all lanes
+    const u64 b = __builtin_bit_cast(u64, v);
+    return __builtin_bit_cast(double, (u64)(u32)__builtin_amdgcn_readlane((int)(u32)(b >> 32), l) << 32 | (u32)__builtin_amdgcn_readlane((int)(u32)b, l));
+}
+template <typename Op>
+__device__ __forceinline__ double wave_all64_dpp(double v, Op op) {
+    v = op(v, lane64_dpp<0xB1>(v));
+    v = op(v, lane64_dpp<0x4E>(v));
+    v = op(v, lane64_dpp<0x141>(v));
+    v = op(v, lane64_dpp<0x140>(v));
+    return op(op(lane64(v, 0), lane64(v, 16)), op(lane64(v, 32), lane64(v, 48)));
+}
+__device__ __forceinline__ double wave_sum64_dpp(double v) { return wave_all64_dpp(v, [](double x, double y) { return x + y; }); }
+__device__ __forceinline__ double wave_max64_dpp(double v) { return wave_all64_dpp(v, [](double x, double y) { return fmax(x, y); }); }
+__device__ __forceinline__ double wave_scan64_dpp(double v) {   // sums of the lanes up to each
+    v += lane64_dpp<0x111>(v);                              // row_shr 1, 2, 4, 8
+    v += lane64_dpp<0x112>(v);
+    v += lane64_dpp<0x114>(v);
+    v += lane64_dpp<0x118>(v);
+    v += lane64_dpp<0x142, 0xA>(v);                         // lane 15 of the row before, into rows 1 and 3
+    v += lane64_dpp<0x143, 0xC>(v);                         // lane 31, into rows 2 and 3
+    return v;
 }

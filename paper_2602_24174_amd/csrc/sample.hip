@@ -115,8 +115,8 @@ struct Segment {
 // takes one fma, the rounding is the addition of 1.5 2^52 in another, which leaves i in the lower word, and the table has i's lower bits
 // taken out of its exponents before: 10 instructions an element (rint, conversion and ldexp have a quarter of the rate of a product).
 // Waves that hold logits too far from their largest for that (masked ones, say), or so large that 2^-53 of them counts, take the loop behind it.
-// us of 1280 rows of 151936 fp32 logits: exp_neg, with the place of the maximum followed as it went, 250; a table of 64, rint, a
-// conversion and ldexp 169; the second loop for all waves 151.
+// us of this kernel, 1280 rows of 151936 fp32 logits: exp_neg, with the place of the maximum followed as it went, 250; a table of 64, rint, a
+// conversion and ldexp 169; the second loop for all waves 151; as it is 138 (5.6 TB/s).
 // 2^(i / 256), by the series of the exponential
 constexpr double pow2_256(int i) {
     const double x = i * (0.69314718055994530942 / 256);
@@ -263,12 +263,12 @@ __device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int l
         scale = fmax(scale, q.scale);
         if (q.top > top || (q.top == top && q.at < best)) { top = q.top; best = q.at; }
     }
-    for (int f = 32; f > 0; f >>= 1) {
-        const float t = __shfl_xor(top, f);
-        const int32_t w = __shfl_xor(best, f);
-        if (t > top || (t == top && w < best)) { top = t; best = w; }
+    const bool greedy = is_greedy(a, b);
+    if (greedy) {                                           // the lowest place among the lanes that hold the maximum
+        if (top != wave_max_dpp(top)) best = 0x7FFFFFFF;
+        for (int f = 32; f > 0; f >>= 1) best = min(best, __shfl_xor(best, f));
     }
-    for (int f = 32; f > 0; f >>= 1) scale = fmax(scale, __shfl_xor(scale, f));
+    scale = wave_max64_dpp(scale);
     o.scale = scale;
     o.best = best;
     double sum = own = lane < a.n_seg ? scaled(mine, scale) : 0.0;
@@ -277,7 +277,6 @@ __device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int l
     const double x = o.draft >= 0 ? exponent(logit, inv, scale) : 0.0, w = o.draft >= 0 ? exp_neg(x) : 0.0;
     o.z = o.others + w;
     o.ok = o.z > 0.0 && o.z < __builtin_inf();
-    const bool greedy = is_greedy(a, b);
     if (greedy) {
         o.accept = o.ok && o.draft == o.best && chance * (double)prob < 1.0;
         o.draft_logp = 0.f;
@@ -403,23 +402,19 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
             double last_before = 0.0;
             for (int s0 = 0; s0 < a.n_seg && seg < 0; s0 += 64) {
                 const double own = seg_sum(s0 + lane);
-                double up = own;
-                for (int f = 1; f < 64; f <<= 1) {
-                    const double t = __shfl_up(up, f);
-                    if (lane >= f) up += t;
-                }
+                const double up = wave_scan64_dpp(own);
                 const u64 past = __ballot(before + up > target), some = __ballot(own > 0.0);
                 if (some) {
                     const int l = 63 - __clzll(some);
                     last = s0 + l;
-                    last_before = before + __shfl(up - own, l);
+                    last_before = before + lane64(up - own, l);
                 }
                 if (past) {
                     const int l = __ffsll(past) - 1;
                     seg = s0 + l;
-                    at_before = before + __shfl(up - own, l);
+                    at_before = before + lane64(up - own, l);
                 }
-                before += __shfl(up, 63);
+                before += lane64(up, 63);
             }
             if (lane == 0) {
                 s_seg = (seg >= 0 ? seg : last) | kind << 28;
@@ -452,11 +447,7 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
             if (kind == 2 && in) w[e] = fmax(w[e] * inv_z - (double)q[v], 0.0);
             mine += w[e];
         }
-        double up = mine;
-        for (int f = 1; f < 64; f <<= 1) {
-            const double t = __shfl_up(up, f);
-            if (lane >= f) up += t;
-        }
+        const double up = wave_scan64_dpp(mine);
         if (lane == 63) s_wave[wave] = up;
         __syncthreads();
         double sum = s_before + (up - mine);
@@ -471,16 +462,16 @@ __global__ __launch_bounds__(kPickThreads) void k_sample_pick(SampleArgs a) {
                 if (sum > s_target && first == 0x7FFFFFFF) first = v;
             }
         }
-        for (int f = 32; f > 0; f >>= 1) {
-            first = min(first, __shfl_xor(first, f));
-            last = max(last, __shfl_xor(last, f));
-        }
+        const u64 hits = __ballot(first != 0x7FFFFFFF), any = __ballot(last >= 0);      // (the tokens go up with the lanes and the waves)
+        first = hits ? __builtin_amdgcn_readlane(first, __ffsll((unsigned long long)hits) - 1) : 0x7FFFFFFF;
+        last = any ? __builtin_amdgcn_readlane(last, 63 - __clzll(any)) : -1;
         if (lane == 0) { s_first[wave] = first; s_last[wave] = last; }
         __syncthreads();
-        for (int i = 0; i < 16; ++i) {
-            first = min(first, s_first[i]);
-            last = max(last, s_last[i]);
-        }
+        first = s_first[lane & 15];
+        last = s_last[lane & 15];
+        const u32 hit = (u32)__ballot(first != 0x7FFFFFFF) & 0xFFFF, some = (u32)__ballot(last >= 0) & 0xFFFF;
+        first = hit ? __builtin_amdgcn_readlane(first, __ffs(hit) - 1) : 0x7FFFFFFF;
+        last = some ? __builtin_amdgcn_readlane(last, 31 - __clz(some)) : -1;
         token = first != 0x7FFFFFFF ? first : last;
 #pragma unroll
         for (int e = 0; e < SPAN; ++e)
