@@ -450,7 +450,7 @@ struct Kv4Wave {
         }
 #pragma unroll
         for (int u = 0; u < MT; ++u) {
-            if (u >= live) break;
+            if (MT > 1 && u >= live) break;                 // (a wave without pairs sees no tile)
             kv4_f32x4 sg[G];
 #pragma unroll
             for (int g = 0; g < G; ++g) sg[g] = kv4_f32x4{0.f, 0.f, 0.f, 0.f};
@@ -483,7 +483,7 @@ struct Kv4Wave {
         }
 #pragma unroll
         for (int u = 0; u < MT; ++u) {
-            if (u >= live) break;
+            if (MT > 1 && u >= live) break;                 // (a wave without pairs sees no tile)
             if constexpr (MT > 1) __builtin_amdgcn_sched_barrier(0);
             if (!whole) {
 #pragma unroll
@@ -774,10 +774,13 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
     extern __shared__ __attribute__((aligned(16))) float lds[];
     const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     Kv4Staged<HD>* const staged = reinterpret_cast<Kv4Staged<HD>*>(lds);                 // [WAVES]
-    const int heads = a.batch * a.Hkv, turned = blockIdx.x / heads, head = (blockIdx.x % heads + turned) % heads, b = head / a.Hkv, h = head % a.Hkv, share = a.H / a.Hkv;
-    const Kv4Seq sq = kv4_seq(a, b);
     // The last pairs see the most keys: those of all heads begin first, and a head goes from one XCD to the next (head by head: 113 us for
-    // 4 prompts of up to 2048 rows, 12 heads, where this takes 104; a head on one XCD, whose prompt may be the short one: 133).
+    // 4 prompts of up to 2048 rows, 12 heads, where this takes 104; a head on one XCD, whose prompt may be the short one: 133).  Every second
+    // 256 workgroups, one a compute unit, come the other way round, so that long ones share theirs with short ones (8 prompts of up to 1024
+    // rows 69 -> 65 us, 16 of 400 24.9 -> 23.9, the 4 of 2048 alike).
+    const int layer = blockIdx.x / 256, id = layer % 2 == 1 && (layer + 1) * 256 <= (int)gridDim.x ? (2 * layer + 1) * 256 - 1 - (int)blockIdx.x : (int)blockIdx.x;
+    const int heads = a.batch * a.Hkv, turned = id / heads, head = (id % heads + turned) % heads, b = head / a.Hkv, h = head % a.Hkv, share = a.H / a.Hkv;
+    const Kv4Seq sq = kv4_seq(a, b);
     const int n_pairs = sq.n * share, n_wgs = (n_pairs + 16 * MT * WAVES - 1) / (16 * MT * WAVES), turn = n_wgs - 1 - turned;
     if (turn < 0) return;
     W w(sq, h, share, (turn * WAVES + wave) * 16 * MT, lane);
