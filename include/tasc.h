@@ -490,7 +490,7 @@ tasc_status tasc_tok_enrich(const int32_t* tokens, const int64_t* doc_offsets, i
  * Pages go to the sequences in order.  A sequence whose pages no longer fit what is left, whose length is beyond max_pages pages, or whose
  * numbers make no sense (kv_len or new_rows < 0, new_rows > kv_len, held outside [0, max_pages]) is refused: its table stays,
  * its rows (those of new_rows >= 0) have slot -1.  A sequence that needs fewer pages than it holds keeps them.
- * Errors: TASC_EINVAL, TASC_EHIP.
+ * Limits: batch in [1, 2^20], max_pages and n_free below 2^27.  Errors: TASC_EINVAL, TASC_EHIP.
  */
 tasc_status tasc_page_tables(const int32_t* kv_len, const int32_t* new_rows, const int32_t* held, int32_t batch,
                              const int32_t* free_pages, int32_t n_free, int32_t* table, int32_t max_pages, int32_t* pages,
@@ -525,8 +525,8 @@ tasc_status tasc_kv4_read(const tasc_kv4_cache* c, const int32_t* slots, int32_t
  * j * n_kv_heads / n_heads.  Sequence b has the rows row_off[b] .. row_off[b + 1] and kv_len[b] tokens, the rows' own (appended before) the
  * last of them; row i of n sees positions 0 .. kv_len - n + i.  A row that sees nothing gives zeros; tokens on a page outside
  * [0, n_pages) are not seen.  Rows at or behind row_off[batch] are left as they are.  max_rows and max_kv are the host's upper bounds
- * (of rows per sequence: further rows are left out; of kv_len: a hint that sizes the grid).  fp32 scores, sums and products of bf16
- * weights; a row's bits do not depend on the other rows' contents.
+ * (of rows per sequence: further rows are left out; of kv_len: a hint that sizes the grid).  fp32 scores, sums and products; a weight is
+ * rounded to bf16 once, before it meets the values; a row's bits do not depend on the other rows' contents.
  */
 typedef struct {
     const void* q;          /* bf16 [rows, n_heads, head_dim], rows q_stride elements apart (a multiple of 8, 16-byte aligned) */
@@ -538,7 +538,8 @@ typedef struct {
     int32_t max_pages, batch, rows, n_heads, max_rows, max_kv;
     float scale;
 } tasc_kv4_attn;
-/* Bytes of scratch for such a call (0: none needed, or a shape that is not served).  Calls that may overlap need their own. */
+/* Bytes of scratch for such a call (0: none needed, or a shape that is not served).  Calls that may overlap need their own.
+ * Limits: batch * n_kv_heads <= 65535, max_pages < 2^27, max_rows * n_heads < 2^30.  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP. */
 size_t tasc_kv4_attention_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                           int32_t max_rows, int32_t max_kv);
 tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv4_attn* a, void* workspace, size_t ws_bytes, void* stream);
@@ -560,7 +561,7 @@ tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv4_attn* a, 
  * A draft is accepted iff u q < p; the drawn token is the lowest one up to which the weights sum to more than u times their total.
  * Exponentials and sums are taken in 64 bits.  A row that has no distribution (a NaN, +infinity, nothing above -infinity, a
  * temperature below 0 or NaN) accepts nothing and emits -1 with a NaN as logprob.
- * Errors: TASC_EINVAL (k outside [0, TASC_MAX_K], vocab outside [2, 2^24]), TASC_ENOMEM (workspace), TASC_EHIP.
+ * Errors: TASC_EINVAL (k outside [0, TASC_MAX_K], vocab outside [2, 2^24], more than 65535 rows), TASC_ENOMEM (workspace), TASC_EHIP.
  */
 size_t tasc_accept_sampled_workspace_bytes(int32_t batch, int32_t k, int32_t vocab);
 tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab,

@@ -131,7 +131,8 @@ struct Kv4Rows {
 };
 
 // One thread per 8 channels of a row's key or value head; the HD / 8 (8 at most) threads of a group find its range among themselves.
-// Bound by bytes: 2 or 4 read and 1/2 written per value.  VEC: rows start at multiples of 16 bytes.
+// Bound by bytes: 2 or 4 read and 1/2 written per value (16384 rows of 8 x 128 fp32: 153 MB in 31 us, 4.9 TB/s, the rate of a copy).  VEC: rows start
+// at multiples of 16 bytes.
 template <int HD, typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_kv4_append(Kv4Rows a, const T* __restrict__ k, const T* __restrict__ v, int64_t k_stride, int64_t v_stride) {
     constexpr int BLKS = HD / 8, SPAN = BLKS < 8 ? BLKS : 8;
@@ -157,7 +158,7 @@ __global__ __launch_bounds__(256) void k_kv4_append(Kv4Rows a, const T* __restri
     kv4_put<HD>(at, slot % TASC_KV_BLOCK, blk, value, x, kv4_scale_low(g));
 }
 
-// The values that slots hold, zeros for a slot outside the pool.
+// The values that slots hold, zeros for a slot outside the pool.  Bound by the bytes it writes (the same rows: 31 us).
 template <int HD, typename T>
 __global__ __launch_bounds__(256) void k_kv4_read(Kv4Rows a, T* __restrict__ k, T* __restrict__ v) {
     using L = Kv4Layout<HD>;
@@ -197,13 +198,14 @@ __global__ __launch_bounds__(256) void k_kv4_read(Kv4Rows a, T* __restrict__ k, 
 // exchanged between lanes but the maximum of a pair's four lanes.
 //   A number c enters the products as the bf16 value 16 + c, which is a shift and a mask away from its 4 bits (0x4180 | c << 3), and exact.
 //   q . key = sum over groups of scale (q . (16 + c)) + (low - 16 scale) sum q        scales applied to the fp32 products
-//   sum p value = sum (p scale) (16 + c) - 23.5 sum (p scale) + sum p (low + 7.5 scale)
-//                                                                                     p scale rounded to bf16 (2^-8 relative at most, like the
-//   output itself), the same rounded weights in the first two sums: a rounding then moves the output by (c - 7.5) scale, about the value's
-//   distance from the middle of its group's range, and not by c scale
-// The last two of these sums are rows of a 16 x 16 product of their own, whose first operand holds -23.5 and low + 7.5 scale in two bf16
-// parts.  Maxima, sums and products are fp32.  Tiles of 32 tokens at absolute positions, chunk_tiles of them a key chunk, a chunk's dealt to
+//   sum p value = sum (p scale) (16 + c) + sum (p scale) (z - 16),  z = low / scale        p scale rounded to bf16 (2^-8 relative at most, like
+//                                                                                     the output itself)
+// The last of these sums is three rows of a 16 x 16 product of its own, z - 16 in three bf16 terms.  Maxima, sums and products are
+// fp32.  Tiles of 32 tokens at absolute positions, chunk_tiles of them a key chunk, a chunk's dealt to
 // the waves in turn, all joined in a fixed order: a row's bits depend on neither the other rows nor the length beyond its own last key.
+// What bounds it: of long contexts with few pairs the read of the cache (2 sequences of up to 131072 tokens, 8 x 128: 227 MB in 55 us, 4.1 TB/s), else
+// the vector instructions around the products (exponentials, scales, numbers to bf16; 56 to 60 % of the busy time) and, with ragged
+// lengths, compute units that are done before others.
 struct Kv4Attn {
     const uint8_t* pool;
     int32_t n_pages, max_pages, Hkv, H, batch, rows, max_rows, chunks, chunk_tiles, row_waves;
@@ -224,7 +226,12 @@ struct Kv4Attn {
 // In which order a row's keys are added: waves that share pairs, key chunks and their length in tiles
 struct Kv4Order { int kw, chunks, chunk_tiles; };
 // `pairs` (row, head) pairs of a KV head, a bound or what stands for it; fixed: the order must not depend on the rows of a call, only
-// on these numbers
+// on these numbers.  A compute unit holds eight waves, two a SIMD, of these registers:
+//   waves with 32 pairs of their own for all of them: nothing is shared (kw 1; us of 4 prompts of up to 2048 rows, 12 heads, 108, with kw 2 119; of
+//     16 of 400 25 | 35)
+//   up to 16 pairs: eight waves a workgroup where that is not more than fill the chip (one sequence of 700 tokens, 9 / 3 heads: 6.9, with four
+//     8.5; 64 of 2300, 12 / 2: 15.3 | 17.6), else four (256 of 700, 16 / 2: 14.1, with eight 18.4, with two 18.1)
+//   else two, and key chunks until the waves fill the chip
 inline Kv4Order kv4_order(int64_t batch, int kv_heads, int64_t pairs, int64_t max_kv, int most_chunks, bool fixed) {
     constexpr int64_t kWaves = 2048;                        // two a SIMD
     const int64_t heads = batch * kv_heads, tiles = (max_kv + 31) / 32;
@@ -618,7 +625,9 @@ __device__ __forceinline__ int kv4_page_ids(const Kv4Attn& a, int b, int from, i
     return page < a.n_pages ? page : -1;
 }
 
-// A step's rows: few pairs.  KW waves share their pairs and take a key chunk's tiles in turn; a workgroup has a.row_waves times as
+// A step's rows: few pairs (up to 16 MT a wave).  (To work a tile out once for the two waves of 17 to 64 pairs, as k_kv4_attention_rows does, is
+// no faster: 256 sequences of 5 rows, 16 / 2 heads, 29.7 | 29.6 us, 64 of 9 rows 34.3 | 33.9, and with 20 pairs 24.8 | 36.3: the barriers cost
+// what the instructions save.)  KW waves share their pairs and take a key chunk's tiles in turn; a workgroup has a.row_waves times as
 // many, each KW of them with pairs of their own (over the same keys, which they so find in the L1 cache).
 template <int HD, int MT, int KW>
 __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) void k_kv4_attention(Kv4Attn a) {
