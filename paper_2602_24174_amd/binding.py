@@ -535,7 +535,7 @@ def _here(stream):
         dev = torch.cuda.current_device()
     except (RuntimeError, AssertionError) as e:
         raise TascError(TASC_EHIP, f"no device: {e}") from None
-    current = torch.cuda.current_stream(dev).cuda_stream
+    current = torch._C._cuda_getCurrentRawStream(dev)      # (what torch.cuda.current_stream(dev).cuda_stream is, without an object for it)
     return dev, current if stream is None else stream, stream is None or stream == current
 
 
