@@ -484,7 +484,7 @@ tasc_status tasc_tok_enrich(const int32_t* tokens, const int64_t* doc_offsets, i
  *   table      int32[batch, max_pages]  entries held .. are written where pages are given, all others left as they are
  *   pages      int32[batch], nullable  pages the table lists afterwards; not the same array as `held`
  *   row_off    int32[batch + 1], nullable  running sum of new_rows
- *   slots      int32[slots_cap], nullable  the rows' slots, sequence by sequence, then -1
+ *   slots      int32[slots_cap], nullable  the rows' slots, sequence by sequence (-1 for a page outside [0, 2^27)), then -1
  *   summary    int32[3], nullable  rows; free pages asked for by the sequences up to the last one granted (those given away if none was refused
  *              for want of pages; after a refusal they are the sum of pages - held); sequences refused
  * Pages go to the sequences in order.  A sequence whose pages no longer fit what is left, whose length is beyond max_pages pages, or whose

@@ -18,7 +18,8 @@ def page_tables(kv_len, new_rows, held, free_pages, table, slots_cap, page=16):
         pages.append(max(need, has) if granted else has)
         for i in range(max(new, 0)):
             pos = n - new + i
-            slots.append(table[b][pos // page] * page + pos % page if granted else -1)
+            at = table[b][pos // page] if granted else -1
+            slots.append(at * page + pos % page if 0 <= at < 1 << 27 else -1)
         row_off.append(len(slots))
     rows = len(slots)
     return pages, row_off, (slots + [-1] * slots_cap)[:slots_cap], [rows, reach, refused]

@@ -163,7 +163,10 @@ __global__ __launch_bounds__(kThreads) void k_page_tables(PageArgs a) {
             for (int i = lane; i < count; i += 64) {
                 const int pos = len - rows + i, at = pos / TASC_PAGE_TOKENS;
                 int32_t slot = -1;
-                if (granted) slot = (at < held ? tab[at] : given(at - held)) * TASC_PAGE_TOKENS + pos % TASC_PAGE_TOKENS;
+                if (granted) {
+                    const int page = at < held ? tab[at] : given(at - held);
+                    if (page >= 0 && page < 1 << 27) slot = page * TASC_PAGE_TOKENS + pos % TASC_PAGE_TOKENS;      // (no cache has more pages)
+                }
                 a.slots[row + i] = slot;
             }
         }

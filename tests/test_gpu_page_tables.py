@@ -60,6 +60,11 @@ def test_lengths_that_make_no_sense():
     check(kv_len, new, held, list(range(100, 120)), [[b] * 4 for b in range(9)], 48)
 
 
+def test_pages_that_are_none():
+    """Held or free pages outside [0, 2^27): listed as they are, their rows have no slot (2^28 + 1 times 16 would come out as 16)."""
+    check([20, 30, 33], [3, 20, 33], [2, 1, 0], [5, -1, (1 << 28) + 1, 7], [[3, -7, 9, 9], [(1 << 27), 9, 9, 9], [9] * 4], 60)
+
+
 def test_defaults():
     """No rows, nothing held, the identity as list of free pages."""
     got = run([33, 0, 16], None, None, None, [[-1] * 4] * 3, 2, n_free=10)
