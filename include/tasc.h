@@ -524,8 +524,8 @@ tasc_status tasc_kv4_read(const tasc_kv4_cache* c, const int32_t* slots, int32_t
  * Grouped-query attention of the step's rows over the cache: softmax(scale q . key) value, query head j reads KV head
  * j * n_kv_heads / n_heads.  Sequence b has the rows row_off[b] .. row_off[b + 1] and kv_len[b] tokens, the rows' own (appended before) the
  * last of them; row i of n sees positions 0 .. kv_len - n + i.  A row that sees nothing gives zeros; tokens on a page outside
- * [0, n_pages) are not seen.  Rows at or behind row_off[batch] are left as they are.  max_rows and max_kv are the host's upper bounds
- * (of rows per sequence: further rows are left out; of kv_len: a hint that sizes the grid).  fp32 scores, sums and products; a weight is
+ * [0, n_pages) are not seen.  Rows at or behind row_off[batch] are left as they are; a sequence whose row_off is below 0, falls or begins
+ * beyond `rows` has none.  max_rows and max_kv are the host's upper bounds (of rows per sequence: further rows are left as they are; of kv_len: a hint that sizes the grid).  fp32 scores, sums and products; a weight is
  * rounded to bf16 once, before it meets the values; a row's bits do not depend on the other rows' contents.
  */
 typedef struct {
@@ -539,7 +539,7 @@ typedef struct {
     float scale;
 } tasc_kv4_attn;
 /* Bytes of scratch for such a call (0: none needed, or a shape that is not served).  Calls that may overlap need their own.
- * Limits: batch * n_kv_heads <= 65535, max_pages < 2^27, max_rows * n_heads < 2^30.  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP. */
+ * Limits: batch * n_kv_heads <= 65535, max_pages <= 2^26, max_rows * n_heads < 2^30.  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP. */
 size_t tasc_kv4_attention_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                           int32_t max_rows, int32_t max_kv);
 tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv4_attn* a, void* workspace, size_t ws_bytes, void* stream);

@@ -255,18 +255,15 @@ struct Kv4Attn;
 tasc_status tasc_kv4_attend(Kv4Attn a, int hd, const Kv4Order& o, hipStream_t st);
 struct Kv4Seq { int first, n, len; };
 __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attn& a, int b) {
+    // in 64 bits, since the arrays may hold anything: rows that are not among the call's, or beyond max_rows, are left out; the last ones, whose
+    // tokens are no other row's
+    const int64_t first = a.row_off ? a.row_off[b] : a.row0[b] - a.row_base, n = a.row_off ? a.row_off[b + 1] - first : a.n_rows[b];
+    const int64_t len = a.row_off ? a.kv_len[b] : (int64_t)a.pos0[b] + n;
+    const int64_t kept = first < 0 || n < 0 ? 0 : max(min(min(n, (int64_t)a.max_rows), (int64_t)a.rows - first), (int64_t)0);
     Kv4Seq s;
-    if (a.row_off) {
-        s.first = a.row_off[b];
-        s.n = a.row_off[b + 1] - s.first;
-        s.len = a.kv_len[b];
-    } else {
-        s.first = a.row0[b] - a.row_base;
-        s.n = a.n_rows[b];
-        s.len = a.pos0[b] + s.n;
-    }
-    s.n = min(s.n, a.max_rows);
-    if (s.first < 0) s.n = 0;
+    s.first = kept > 0 ? (int)first : 0;
+    s.n = (int)kept;
+    s.len = kept > 0 ? (int)max(len - (n - kept), (int64_t)0) : 0;        // (below 0 as 0: the rows see nothing)
     return s;
 }
 

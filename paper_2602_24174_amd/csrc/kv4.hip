@@ -157,7 +157,7 @@ extern "C" tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv
     TASC_REQUIRE(p->q && p->out && p->table && p->row_off && p->kv_len, "kv4_attention: null argument");
     TASC_REQUIRE(p->n_heads >= 1 && p->n_heads % c->n_kv_heads == 0, "kv4_attention: %d query heads over %d KV heads", p->n_heads, c->n_kv_heads);
     TASC_REQUIRE((int64_t)p->batch * c->n_kv_heads <= 65535, "kv4_attention: batch %d x %d KV heads is beyond 65535", p->batch, c->n_kv_heads);
-    TASC_REQUIRE(p->max_pages < (1 << 27) && (int64_t)p->max_rows * p->n_heads < (int64_t)1 << 30 && (int64_t)p->max_rows * p->n_heads / 128 * p->batch < (int64_t)1 << 30, "kv4_attention: max_pages %d, max_rows %d", p->max_pages, p->max_rows);
+    TASC_REQUIRE(p->max_pages <= (1 << 26) && (int64_t)p->max_rows * p->n_heads < (int64_t)1 << 30 && (int64_t)p->max_rows * p->n_heads / 128 * p->batch < (int64_t)1 << 30, "kv4_attention: max_pages %d, max_rows %d", p->max_pages, p->max_rows);
     const int64_t width = (int64_t)p->n_heads * c->head_dim;
     TASC_REQUIRE(p->q_stride >= 0 && p->out_stride >= width, "kv4_attention: row strides %lld, %lld of rows of %lld", (long long)p->q_stride, (long long)p->out_stride,
                  (long long)width);

@@ -192,6 +192,35 @@ def test_rows_that_see_nothing():
         assert (out[:2] == 0).all() and (out[5:7] == 0).all() and (out[7:17] == 0).all()
 
 
+def test_rows_beyond_the_bound_are_left_out():
+    """max_rows below a sequence's rows: its first ones are as they are without the bound, the others stay as they were."""
+    import torch
+    for lens, rows, most, heads in (([40, 9], [7, 3], 4, 4), ([300], [200], 70, 12), ([5, 64], [9, 2], 3, 4)):
+        batch = Batch(lens, rows, heads, 2, 64)
+        all_of, some = batch.run().float().cpu().numpy(), batch.run(max_rows=most).float().cpu().numpy()
+        q = batch.q.float().cpu().numpy().astype(np.float64)
+        for b, n in enumerate(rows):
+            first, kept = batch.off[b], min(n, most)
+            want, bound = OK.attention(q[first:first + n], batch.k[b], batch.v[b], n, batch.scale)
+            assert (np.abs(some[first:first + kept] - want[:kept]) <= bound[:kept]).all() and (np.abs(all_of[first:first + n] - want) <= bound).all()
+            assert (some[first + kept:first + n] == 7).all()
+
+
+def test_lengths_and_rows_that_make_no_sense():
+    """Negative lengths: rows that see nothing.  Offsets that fall or begin below 0: no rows.  Offsets beyond the rows: those that exist."""
+    import torch
+    batch = Batch([40, 40, 40, 40], [2, 3, 2, 2], 4, 2, 64)
+    clean = batch.run()
+    one = lambda v: torch.tensor(v, dtype=torch.int32, device="cuda")
+    batch.kv_len = one([40, -2147483648, -1, 40])
+    out = batch.run()
+    assert torch.equal(out[:2], clean[:2]) and (out[2:7] == 0).all() and torch.equal(out[7:], clean[7:])
+    batch.kv_len, batch.row_off = one([40] * 4), one([-2147483648, 5, 2, 2147483647, -3])
+    out = batch.run(max_rows=3)
+    assert (out[:2] == 7).all() and (out[5:] == 7).all()        # the third sequence has rows 2, 3, 4 of very many, which see nothing
+    assert (out[2:5] == 0).all()
+
+
 def test_pages_outside_the_pool():
     """Their tokens are not seen, and nothing is read there."""
     import torch

@@ -72,7 +72,7 @@ def test_attention():
         assert call(cache(**bad)) == B.TASC_EINVAL, bad
     for bad in (dict(q=None), dict(out=None), dict(table=None), dict(row_off=None), dict(kv_len=None), dict(max_pages=0), dict(batch=-1), dict(rows=-1), dict(n_heads=3),
                 dict(n_heads=0), dict(max_rows=-1), dict(max_kv=-1), dict(q=A + 8), dict(out=A + 2), dict(q_stride=260), dict(out_stride=250), dict(out_stride=252),
-                dict(q_stride=-256), dict(max_pages=(1 << 27) + 1), dict(max_pages=1 << 27), dict(max_rows=1 << 30)):
+                dict(q_stride=-256), dict(max_pages=(1 << 27) + 1), dict(max_pages=(1 << 26) + 1), dict(max_rows=1 << 30)):
         assert call(**bad) == B.TASC_EINVAL, bad
     for none in (dict(batch=0), dict(rows=0), dict(max_rows=0)):
         assert call(**none) == 0, none
