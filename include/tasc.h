@@ -525,8 +525,9 @@ tasc_status tasc_kv4_read(const tasc_kv4_cache* c, const int32_t* slots, int32_t
  * j * n_kv_heads / n_heads.  Sequence b has the rows row_off[b] .. row_off[b + 1] and kv_len[b] tokens, the rows' own (appended before) the
  * last of them; row i of n sees positions 0 .. kv_len - n + i.  A row that sees nothing gives zeros; tokens on a page outside
  * [0, n_pages) are not seen.  Rows at or behind row_off[batch] are left as they are; a sequence whose row_off is below 0, falls or begins
- * beyond `rows` has none.  max_rows and max_kv are the host's upper bounds (of rows per sequence: further rows are left as they are; of kv_len: a hint that sizes the grid).  fp32 scores, sums and products; a weight is
- * rounded to bf16 once, before it meets the values; a row's bits do not depend on the other rows' contents.
+ * beyond `rows` has none.  max_rows and max_kv are the host's upper bounds (of rows per sequence: further rows are left as they are; of
+ * kv_len: a hint that sizes the grid).  fp32 scores, sums and products; a weight is rounded to bf16 once, before it meets the values; a
+ * row's bits do not depend on the other rows' contents.
  */
 typedef struct {
     const void* q;          /* bf16 [rows, n_heads, head_dim], rows q_stride elements apart (a multiple of 8, 16-byte aligned) */

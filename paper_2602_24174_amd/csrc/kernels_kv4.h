@@ -255,15 +255,16 @@ struct Kv4Attn;
 tasc_status tasc_kv4_attend(Kv4Attn a, int hd, const Kv4Order& o, hipStream_t st);
 struct Kv4Seq { int first, n, len; };
 __device__ __forceinline__ Kv4Seq kv4_seq(const Kv4Attn& a, int b) {
-    // in 64 bits, since the arrays may hold anything: rows that are not among the call's, or beyond max_rows, are left out; the last ones, whose
-    // tokens are no other row's
-    const int64_t first = a.row_off ? a.row_off[b] : a.row0[b] - a.row_base, n = a.row_off ? a.row_off[b + 1] - first : a.n_rows[b];
-    const int64_t len = a.row_off ? a.kv_len[b] : (int64_t)a.pos0[b] + n;
-    const int64_t kept = first < 0 || n < 0 ? 0 : max(min(min(n, (int64_t)a.max_rows), (int64_t)a.rows - first), (int64_t)0);
-    Kv4Seq s;
-    s.first = kept > 0 ? (int)first : 0;
-    s.n = (int)kept;
-    s.len = kept > 0 ? (int)max(len - (n - kept), (int64_t)0) : 0;        // (below 0 as 0: the rows see nothing)
+    // The arrays may hold anything: rows that are not among the call's, or beyond max_rows, are left out; the last ones, whose tokens are no
+    // other row's.  (Differences of numbers from 0 on: none overflows.)
+    const int first = a.row_off ? a.row_off[b] : a.row0[b] - a.row_base, next = a.row_off ? a.row_off[b + 1] : first + a.n_rows[b];
+    Kv4Seq s{0, 0, 0};
+    if (first >= 0 && next > first && first < a.rows) {
+        const int n = next - first, len = a.row_off ? max(a.kv_len[b], 0) : a.pos0[b] + n;
+        s.first = first;
+        s.n = min(min(n, a.max_rows), a.rows - first);
+        s.len = max(len - (n - s.n), 0);                    // (below 0 as 0: the rows see nothing)
+    }
     return s;
 }
 
