@@ -337,7 +337,7 @@ class Session:
     def __init__(self, handle, model, batch, max_len, max_rows, kv_pool, workspace):
         self.handle, self.model, self.batch, self.max_len, self.max_rows = handle, model, batch, max_len, max_rows
         self._kv_pool, self._workspace = kv_pool, workspace     # keep the caller-owned buffers alive
-        self._scratch = {}                                      # of sampled steps, by k
+        self._scratch = {}                                      # of sampled steps, by k and stream
 
     def close(self):
         if self.handle:
@@ -712,15 +712,21 @@ def tasc_sampled_scratch_bytes(model: Model, batch, k) -> int:
     return lib().tasc_sampled_scratch_bytes(model.handle, batch, k)
 
 
-def _sampling(who, model, s, k, u, temperature, scratch, dev):
-    """(what must stay alive, struct).  A scratch made here stays with the session, one for every k, as recorded steps do."""
+def _sampling(who, model, s, k, u, temperature, scratch, dev, st):
+    """(what must stay alive, struct).  A scratch made here comes from the memory of the call's stream, where nothing that is still to run can
+    write to it, and stays with the session, one for every k and stream, as recorded steps do."""
     import torch
+    if s._kv_pool.get_device() != dev:
+        _refuse(f"{who}: the session is on cuda:{s._kv_pool.get_device()}, the current device is cuda:{dev}")
     if getattr(u, "ndim", 0) != 3:
         _refuse(f"{who}: u is not [batch, pairs, 2]")
     if scratch is None:
-        if k not in s._scratch:
-            s._scratch[k] = torch.empty(max(tasc_sampled_scratch_bytes(model, s.batch, k), 1), dtype=torch.uint8, device="cuda")
-        scratch = s._scratch[k]
+        if (k, st) not in s._scratch:
+            with torch.cuda.stream(torch.cuda.ExternalStream(st, device=dev) if st else torch.cuda.default_stream(dev)):
+                s._scratch[k, st] = torch.empty(max(tasc_sampled_scratch_bytes(model, s.batch, k), 1), dtype=torch.uint8, device="cuda")
+        scratch = s._scratch[k, st]
+    elif not isinstance(scratch, torch.Tensor) or scratch.get_device() != dev or not scratch.is_contiguous():
+        _refuse(f"{who}: the scratch is not a contiguous tensor of the current device")
     return scratch, Sampling(None if temperature is None else _array(who, "temperature", temperature, torch.float32, (s.batch,), dev),
                              _array(who, "u", u, torch.float32, (s.batch, u.shape[1], 2), dev), u.shape[1], scratch.data_ptr(),
                              scratch.numel() * scratch.element_size())
@@ -732,7 +738,7 @@ def tasc_verify_step_sampled(model: Model, s: Session, drafts, k, u, temperature
     import torch
     who, i32 = "verify_step_sampled", torch.int32
     dev, st, _ = _here(stream)
-    keep, p = _sampling(who, model, s, k, u, temperature, scratch, dev)
+    keep, p = _sampling(who, model, s, k, u, temperature, scratch, dev, st)
     per_row = (s.batch, k + 1)
     _check(lib().tasc_verify_step_sampled(model.handle, s.handle, None if drafts is None and k == 0 else _array(who, "drafts", drafts, i32, (s.batch, k), dev), k, C.byref(p),
                                           None if accept_len is None else _array(who, "accept_len", accept_len, i32, (s.batch,), dev),
@@ -751,7 +757,7 @@ def tasc_generate_sampled(model: Model, ng, s: Session, prompts, prompt_offsets,
     who = "generate_sampled"
     dev, st, _ = _here(stream)
     prompt_offsets = np.ascontiguousarray(prompt_offsets, dtype=np.int64)
-    keep, p = _sampling(who, model, s, params.k, u, temperature, scratch, dev)
+    keep, p = _sampling(who, model, s, params.k, u, temperature, scratch, dev, st)
     stats = GenStats()
     _check(lib().tasc_generate_sampled(model.handle, ng.handle if ng is not None else None, s.handle, _ptr(prompts), _ptr(prompt_offsets), _where(prompts), max_new,
                                        C.byref(params), C.byref(p), _array(who, "out_tokens", out_tokens, torch.int32, (s.batch, max_new), dev), C.byref(stats), st))
