@@ -555,7 +555,8 @@ tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv4_attn* a, 
  *   drafts       int32[batch, k]; a value outside [0, vocab) ends the sequence's drafts (its row draws from p)
  *   draft_probs  fp32[batch, k, vocab], nullable: the distributions q that the drafts were drawn from; NULL: they were chosen
  *                without chance (q is 1 at the draft)
- *   temperature  fp32[batch], nullable (1); 0: the target is greedy (p is 1 at the largest logit, lowest index among equals)
+ *   temperature  fp32[batch], nullable (1); 0: the target is greedy (p is 1 at the largest logit, lowest index among equals); infinite: all
+ *                tokens that are not masked are alike
  *   u            fp32[batch, k + 1, 2] in [0, 1): [i][0] decides on draft i, [i][1] draws the token at position i
  *   accept_len   int32[batch]  drafts accepted;  emitted int32[batch, k + 1]  those, then the drawn token, then -1
  *   logprob      fp32[batch, k + 1], nullable: ln p of the emitted tokens, then 0

@@ -274,7 +274,8 @@ __device__ __forceinline__ Row join_row(const SampleArgs& a, int b, int i, int l
     double sum = own = lane < a.n_seg ? scaled(mine, scale) : 0.0;
     for (int s = lane + 64; s < a.n_seg; s += 64) sum += scaled(p[s], scale);
     o.others = wave_sum64_dpp(sum);
-    const double x = o.draft >= 0 ? exponent(logit, inv, scale) : 0.0, w = o.draft >= 0 ? exp_neg(x) : 0.0;
+    // (a masked draft weighs nothing at any temperature: over an infinite one -infinity is no number)
+    const double x = o.draft >= 0 ? exponent(logit, inv, scale) : 0.0, w = o.draft >= 0 && logit != -__builtin_inff() ? exp_neg(x) : 0.0;
     o.z = o.others + w;
     o.ok = o.z > 0.0 && o.z < __builtin_inf();
     if (greedy) {
