@@ -527,7 +527,8 @@ tasc_status tasc_kv4_read(const tasc_kv4_cache* c, const int32_t* slots, int32_t
  * [0, n_pages) are not seen.  Rows at or behind row_off[batch] are left as they are; a sequence whose row_off is below 0, falls or begins
  * beyond `rows` has none.  max_rows and max_kv are the host's upper bounds (of rows per sequence: further rows are left as they are; of
  * kv_len: a hint that sizes the grid).  fp32 scores, sums and products; a weight is rounded to bf16 once, before it meets the values; a
- * row's bits do not depend on the other rows' contents.
+ * row's bits do not depend on the other rows' contents.  Values may be as large as fp32 holds (a token whose least value rounds to a bf16 infinity
+ * counts as NaN); of queries and keys sum |q| (31 scale + |low|) over the channels has to stay within fp32, or the scores may be NaN.
  */
 typedef struct {
     const void* q;          /* bf16 [rows, n_heads, head_dim], rows q_stride elements apart (a multiple of 8, 16-byte aligned) */

@@ -359,8 +359,10 @@ __device__ __forceinline__ Kv4Z kv4_z(float scale, float low) {
     float z = low * __builtin_amdgcn_rcpf(scale);
     if (scale < 1.17549435e-38f && scale != 0.f) z = low / scale;               // (below the reciprocal's range)
     if (!(fabsf(z) <= 1073741824.f)) {                      // 2^30
-        z = scale == 0.f ? 1.f : 1073741824.f;             // (numbers are 0 where the scale is)
-        scale = scale == 0.f ? low : low * (1.f / 1073741824.f);
+        // (numbers are 0 where the scale is: 16 + c times low / 16 is the value, and z - 16 nothing)
+        const bool none = scale == 0.f;
+        z = none ? 16.f : 1073741824.f;
+        scale = low * (none ? 1.f / 16.f : 1.f / 1073741824.f);
     }
     Kv4Z o;
     o.scale = scale;
@@ -374,6 +376,10 @@ __device__ __forceinline__ Kv4Z kv4_z(float scale, float low) {
     return o;
 }
 constexpr float kKv4Grown = 8.f;                        // a maximum is followed once it grew by more than this power of 2
+// Sums are taken of 2^-40 times the values from the first tile on that holds large ones (kKv4Large), for these have no room beside the weights
+// (up to 2^8 each, of up to 2^30 tokens) and 16 + c: below that a sum is at most 2^38 (31 scale + |low - 16 scale|) < 2^111, and with the factor, of
+// the largest values, 2^38 2^129.1 2^-40 < 2^128.  A power of 2: what ordinary tiles give is the same bits either way.
+constexpr float kKv4Large = 0x1p70f, kKv4Less = 0x1p-40f, kKv4Room = 0x1p118f;
 
 // What a wave holds: MT tiles of 16 (row, head) pairs of a KV head, with their queries and sums.
 template <int HD, int MT>
@@ -386,6 +392,7 @@ struct Kv4Wave {
     float s[MT][2][4];                                      // a tile's scores, less m
     int last[MT];                                           // last key that the lane's pair sees
     int pair0, live, first_last;                            // first pair, tiles of pairs that hold any, last key of the first pair
+    bool less;                                              // acc and ev are of 2^-40 times the values
     const Kv4Seq& sq;
     int h, share, n_pairs, lane, col, r;
 
@@ -425,6 +432,7 @@ struct Kv4Wave {
     }
     // .. and looked at
     __device__ __forceinline__ void begin() {
+        less = false;
 #pragma unroll
         for (int t = 0; t < MT; ++t) {
 #pragma unroll
@@ -475,8 +483,9 @@ struct Kv4Wave {
             }
         }
     }
-    // the tile's weights and their sums; at: its first position, whole: every pair sees all of it, ok0, ok1: its pages are in the pool
-    __device__ __forceinline__ void sums(const kv4_bf16x8 (&fv)[DT], const Kv4Scales<HD>& sc, int at, bool whole, bool ok0, bool ok1, int len) {
+    // the tile's weights and their sums; at: its first position, whole: every pair sees all of it, ok0, ok1: its pages are in the pool, large:
+    // some of its values are
+    __device__ __forceinline__ void sums(const kv4_bf16x8 (&fv)[DT], const Kv4Scales<HD>& sc, int at, bool whole, bool ok0, bool ok1, bool large, int len) {
         kv4_bf16x8 fz[G];
         kv4_f32x4 vs[2][G];
 #pragma unroll
@@ -485,6 +494,21 @@ struct Kv4Wave {
             fz[g] = *reinterpret_cast<const kv4_bf16x8*>(&sc.z[0][k >= 0 && k < 3 ? 3 * g + k : 3 * G][8 * r]);     // 3 G: the zeros
 #pragma unroll
             for (int p = 0; p < 2; ++p) vs[p][g] = *reinterpret_cast<const kv4_f32x4*>(&sc.vs[p][g][4 * r]);
+        }
+        if (large || less) {
+            if (!less) {
+                less = true;
+#pragma unroll
+                for (int u = 0; u < MT; ++u) {
+                    ev[u] *= kKv4Less;
+#pragma unroll
+                    for (int j = 0; j < DT; ++j) acc[u][j] *= kKv4Less;
+                }
+            }
+#pragma unroll
+            for (int g = 0; g < G; ++g)
+#pragma unroll
+                for (int p = 0; p < 2; ++p) vs[p][g] *= kKv4Less;
         }
 #pragma unroll
         for (int u = 0; u < MT; ++u) {
@@ -553,6 +577,23 @@ struct Kv4Wave {
 #pragma unroll
                 for (int j = g * (DT / G); j < (g + 1) * (DT / G); ++j) acc[t][j] += e;
             }
+            // Back to the values themselves; a pair whose sums have no room for that (there are up to 512 to join) has the same mean with 2^-16 as
+            // its weights' sum, and a maximum to go with it.  (What a pair does not see decides nothing here.)
+            if (less) {
+                float top = 0.f;
+#pragma unroll
+                for (int j = 0; j < DT; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) top = fmaxf(top, fabsf(acc[t][j][i]));
+                const bool room = !(kv4_quad_max(top) > kKv4Room * kKv4Less);
+                const float f = room ? 1.f / kKv4Less : (0x1p-16f / kKv4Less) / l[t];
+#pragma unroll
+                for (int j = 0; j < DT; ++j) acc[t][j] *= f;
+                if (!room) {
+                    m[t] += __builtin_amdgcn_logf(l[t]) + 16.f;
+                    l[t] = 0x1p-16f;
+                }
+            }
         }
     }
     // A lane's channels: of tile j row 4 r + i, channel (HD 128, 64) 64 (j / 4) + 16 r + 4 i + j % 4, (32) 8 r + 2 i + j: in items (i, group of
@@ -572,9 +613,9 @@ struct Kv4Wave {
 // a pair without keys gives zeros (a NaN stays one)
 __device__ __forceinline__ float kv4_inverse(float l) { return l > 0.f ? 1.f / l : l; }
 
-// the tile's {scale, low} words, which the lanes were dealt, into LDS
+// the tile's {scale, low} words, which the lanes were dealt, into LDS; whether any of the values is large
 template <int HD>
-__device__ __forceinline__ void kv4_work_scales(Kv4Scales<HD>& sc, uint32_t k_word, uint32_t v_word, float scale2, int at, bool whole, bool ok0, bool ok1, int len, int lane) {
+__device__ __forceinline__ bool kv4_work_scales(Kv4Scales<HD>& sc, uint32_t k_word, uint32_t v_word, float scale2, int at, bool whole, bool ok0, bool ok1, int len, int lane) {
     constexpr int G = Kv4Layout<HD>::GROUPS;
     const int p = kv4_scale_page<HD>(lane), g = kv4_scale_word<HD>(lane) / 16, tok = lane & 15;
     float ks = kv4_scale(k_word) * scale2, lo = kv4_low(k_word) * scale2, vs = kv4_scale(v_word), vl = kv4_low(v_word);
@@ -589,6 +630,7 @@ __device__ __forceinline__ void kv4_work_scales(Kv4Scales<HD>& sc, uint32_t k_wo
 #pragma unroll
         for (int i = 0; i < 3; ++i) sc.z[g][i][(tok / 4) * 8 + 4 * p + tok % 4] = z.z[i];
     }
+    return __any(__builtin_fmaf(16.f, vs, fabsf(vl)) > kKv4Large);
 }
 template <int HD>
 __device__ __forceinline__ kv4_bf16x8 kv4_key_part(const Kv4Bits& bits, const Kv4Tile<HD>& t, int p, int i) {
@@ -667,7 +709,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
     auto work = [&](Kv4Tile<HD>& cur, int t, int pg0, int pg1, int ng0, int ng1) __attribute__((always_inline)) {
         const int at = 32 * t;
         const bool whole = pg0 >= 0 && pg1 >= 0 && at + 31 <= w.first_last && at + 32 <= len;
-        kv4_work_scales<HD>(sc, cur.ks, cur.vs, scale2, at, whole, pg0 >= 0, pg1 >= 0, len, lane);
+        const bool large = kv4_work_scales<HD>(sc, cur.ks, cur.vs, scale2, at, whole, pg0 >= 0, pg1 >= 0, len, lane);
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");   // (a wave's LDS accesses are in order: the compiler has to keep them so)
         __builtin_amdgcn_wave_barrier();
 #pragma unroll
@@ -685,7 +727,7 @@ __global__ __launch_bounds__(512) __attribute__((amdgpu_waves_per_eu(2, 2))) voi
         kv4_bf16x8 fv[W::DT];
 #pragma unroll
         for (int j = 0; j < W::DT; ++j) fv[j] = kv4_value_part<HD>(bits, values, j);
-        w.sums(fv, sc, at, whole, pg0 >= 0, pg1 >= 0, len);
+        w.sums(fv, sc, at, whole, pg0 >= 0, pg1 >= 0, large, len);
     };
     int k = 2 * AHEAD;                                      // place of the next tile's ids
     for (int t = first_tile; t < n_tiles; t += AHEAD * KW) {
@@ -806,13 +848,13 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
     if (lane < 32) staged[wave].scales.none[lane] = 0;
     const Kv4Bits bits = kv4_bits();
     const float scale2 = a.scale * 1.44269504088896340736f;
-    __shared__ int s_ok[WAVES];                             // pages of a tile that are in the pool: bits 0, 1
+    __shared__ int s_ok[WAVES];                             // pages of a tile that are in the pool: bits 0, 1; large values: bit 2
     for (int t0 = 0; t0 < n_tiles; t0 += WAVES) {
         {
             Kv4Staged<HD>& to = staged[wave];
             const int t = t0 + wave;
             const bool inside = pg0 >= 0 && pg1 >= 0 && 32 * t + 32 <= len;
-            kv4_work_scales<HD>(to.scales, tile.ks, tile.vs, scale2, 32 * t, inside, pg0 >= 0, pg1 >= 0, len, lane);
+            const bool large = kv4_work_scales<HD>(to.scales, tile.ks, tile.vs, scale2, 32 * t, inside, pg0 >= 0, pg1 >= 0, len, lane);
 #pragma unroll
             for (int p = 0; p < 2; ++p)
 #pragma unroll
@@ -820,7 +862,7 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
             const Kv4Values<HD> values = kv4_values<HD>(tile);
 #pragma unroll
             for (int j = 0; j < W::DT; ++j) to.value[j][lane] = __builtin_bit_cast(kv4_u32x4, kv4_value_part<HD>(bits, values, j));
-            if (lane == 0) s_ok[wave] = (pg0 >= 0 ? 1 : 0) | (pg1 >= 0 ? 2 : 0);
+            if (lane == 0) s_ok[wave] = (pg0 >= 0 ? 1 : 0) | (pg1 >= 0 ? 2 : 0) | (large ? 4 : 0);
         }
         // the next four tiles are under way while these are worked on
         k += 2;
@@ -833,7 +875,7 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
         for (int n = 0; n < WAVES && t0 + n < mine; ++n) {
             const Kv4Staged<HD>& from = staged[n];
             const int at = 32 * (t0 + n), ok = __builtin_amdgcn_readfirstlane(s_ok[n]);
-            const bool whole = ok == 3 && at + 31 <= w.first_last && at + 32 <= len;
+            const bool whole = (ok & 3) == 3 && at + 31 <= w.first_last && at + 32 <= len;
 #pragma unroll
             for (int p = 0; p < 2; ++p) {
                 kv4_bf16x8 fk[W::KSTEPS];
@@ -844,7 +886,7 @@ __global__ __launch_bounds__(64 * kKv4RowWaves) __attribute__((amdgpu_waves_per_
             kv4_bf16x8 fv[W::DT];
 #pragma unroll
             for (int j = 0; j < W::DT; ++j) fv[j] = __builtin_bit_cast(kv4_bf16x8, from.value[j][lane]);
-            w.sums(fv, from.scales, at, whole, ok & 1, (ok >> 1) & 1, len);
+            w.sums(fv, from.scales, at, whole, ok & 1, (ok >> 1) & 1, (ok >> 2) & 1, len);
         }
         __syncthreads();
     }
