@@ -15,7 +15,7 @@
 // A token's bytes are its own (no byte holds two tokens), so rows are written without a look at their neighbours.
 #pragma once
 #include "numeric.h"
-#include <algorithm>
+#include "kv4_order.h"
 
 typedef uint32_t kv4_u32x4 __attribute__((ext_vector_type(4)));
 typedef uint32_t kv4_u32x2 __attribute__((ext_vector_type(2)));
@@ -223,34 +223,6 @@ struct Kv4Attn {
     float* part_o;                     // [chunks, rows, H, HD], used if chunks > 1
     float* part_ml;                    // [chunks, rows, H, 2]
 };
-// In which order a row's keys are added: waves that share pairs, key chunks and their length in tiles
-struct Kv4Order { int kw, chunks, chunk_tiles; };
-// `pairs` (row, head) pairs of a KV head, a bound or what stands for it; fixed: the order must not depend on the rows of a call, only
-// on these numbers.  A compute unit holds eight waves, two a SIMD, of these registers:
-//   waves with 32 pairs of their own for all of them: nothing is shared (kw 1; us of 4 prompts of up to 2048 rows, 12 heads, 108, with kw 2 119; of
-//     16 of 400 25 | 35)
-//   up to 16 pairs: eight waves a workgroup where that is not more than fill the chip (one sequence of 700 tokens, 9 / 3 heads: 6.9, with four
-//     8.5; 64 of 2300, 12 / 2: 15.3 | 17.6), else four (256 of 700, 16 / 2: 14.1, with eight 18.4, with two 18.1)
-//   else two, and key chunks until the waves fill the chip
-inline Kv4Order kv4_order(int64_t batch, int kv_heads, int64_t pairs, int64_t max_kv, int most_chunks, bool fixed) {
-    constexpr int64_t kWaves = 2048;                        // two a SIMD
-    const int64_t heads = batch * kv_heads, tiles = (max_kv + 31) / 32;
-    Kv4Order o{2, 1, 1 << 26};
-    const int64_t row_waves = (pairs + 31) / 32;
-    if (!fixed && row_waves * heads >= kWaves) {
-        o.kw = 1;
-        return o;
-    }
-    if (!fixed && pairs <= 16) o.kw = heads * 8 <= kWaves ? 8 : 4;
-    const int64_t want = std::clamp<int64_t>((kWaves + heads * row_waves * o.kw - 1) / (heads * row_waves * o.kw), 1, most_chunks);
-    const int64_t per = std::max<int64_t>((tiles + want - 1) / want, 4 * o.kw);      // four tiles a wave at least
-    if (tiles > per) {
-        o.chunks = (int)((tiles + per - 1) / per);
-        o.chunk_tiles = (int)per;
-    }
-    return o;
-}
-struct Kv4Attn;
 // kv4.hip: enqueues the attention (a.chunks is set from the order)
 tasc_status tasc_kv4_attend(Kv4Attn a, int hd, const Kv4Order& o, hipStream_t st);
 struct Kv4Seq { int first, n, len; };
