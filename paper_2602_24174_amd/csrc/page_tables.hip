@@ -158,10 +158,10 @@ __global__ __launch_bounds__(kThreads) void k_page_tables(PageArgs a) {
                 if (a.row_off) a.row_off[b] = (int32_t)min(row, (int64_t)INT32_MAX);
             }
             if (!a.slots) continue;
-            const int count = (int)min((int64_t)rows, max((int64_t)a.slots_cap - row, (int64_t)0));
+            const u32 count = (u32)min((int64_t)rows, max((int64_t)a.slots_cap - row, (int64_t)0));
 #pragma unroll 4
-            for (int i = lane; i < count; i += 64) {
-                const int pos = len - rows + i, at = pos / TASC_PAGE_TOKENS;
+            for (u32 i = lane; i < count; i += 64) {        // (the step behind 2^31 - 1 slots is past 31 bits)
+                const int pos = len - rows + (int)i, at = pos / TASC_PAGE_TOKENS;
                 int32_t slot = -1;
                 if (granted) {
                     const int page = at < held ? tab[at] : given(at - held);
