@@ -513,6 +513,7 @@ size_t tasc_kv4_page_bytes(int32_t n_kv_heads, int32_t head_dim);
  * Writes the keys and values of `rows` rows: row i is [n_kv_heads, head_dim] at k + i * k_stride (elements of `dtype`, fp32 or bf16), so both may
  * lie inside the rows of a fused projection.  A row whose slot is negative or outside the pool is skipped.  The slots of a call must
  * differ: what a slot named twice holds afterwards is unspecified (no other slot is touched).
+ * Limit, of this call and the next: rows * n_kv_heads * head_dim < 2^35.  Errors: TASC_EINVAL, TASC_EHIP.
  */
 tasc_status tasc_kv4_append(const tasc_kv4_cache* c, const void* k, const void* v, tasc_dtype dtype, int64_t k_stride,
                             int64_t v_stride, const int32_t* slots, int32_t rows, void* stream);
@@ -541,7 +542,8 @@ typedef struct {
     float scale;
 } tasc_kv4_attn;
 /* Bytes of scratch for such a call (0: none needed, or a shape that is not served).  Calls that may overlap need their own.
- * Limits: batch * n_kv_heads <= 65535, max_pages <= 2^26, max_rows * n_heads < 2^30.  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP. */
+ * Limits: batch * n_kv_heads <= 65535, max_pages <= 2^26, max_rows * n_heads < 2^30, batch * max_rows * n_heads < 2^31 (max_rows * n_heads /
+ * n_kv_heads counted in whole 128s).  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP. */
 size_t tasc_kv4_attention_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
                                           int32_t max_rows, int32_t max_kv);
 tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv4_attn* a, void* workspace, size_t ws_bytes, void* stream);

@@ -78,6 +78,7 @@ void with_hd(int hd, F f) {
 }
 
 constexpr int kMostChunks = 64;
+constexpr int64_t kMostBlocks = 1 << 24;                    // workgroups of 256 threads: a launch has less than 2^32 threads a dimension
 
 }  // namespace
 
@@ -106,8 +107,9 @@ extern "C" tasc_status tasc_kv4_append(const tasc_kv4_cache* c, const void* k, c
     TASC_REQUIRE((uintptr_t)k % es == 0 && (uintptr_t)v % es == 0, "kv4_append: keys and values must be aligned to their type");
     const bool vec = (((uintptr_t)k | (uintptr_t)v | (uintptr_t)(k_stride * es) | (uintptr_t)(v_stride * es)) & 15) == 0;
     const Kv4Rows a{(uint8_t*)c->pool, c->n_pages, c->n_kv_heads, rows, slots};
-    const int64_t threads = (int64_t)rows * (width / 8);
-    const dim3 grid((unsigned)((threads + 255) / 256), 2);
+    const int64_t blocks = ((int64_t)rows * (width / 8) + 255) / 256;
+    TASC_REQUIRE(blocks < kMostBlocks, "kv4_append: %d rows of %d x %d channels are 2^35 and more", rows, c->n_kv_heads, c->head_dim);
+    const dim3 grid((unsigned)blocks, 2);
     hipStream_t st = (hipStream_t)stream;
     with_hd(c->head_dim, [&](auto hd) {
         constexpr int HD = decltype(hd)::value;
@@ -128,8 +130,9 @@ extern "C" tasc_status tasc_kv4_read(const tasc_kv4_cache* c, const int32_t* slo
     TASC_REQUIRE(dtype == TASC_F32 || dtype == TASC_BF16, "kv4_read: dtype %d", (int)dtype);
     TASC_REQUIRE((((uintptr_t)k | (uintptr_t)v) & 15) == 0, "kv4_read: outputs must be 16-byte aligned");
     const Kv4Rows a{(uint8_t*)c->pool, c->n_pages, c->n_kv_heads, rows, slots};
-    const int64_t threads = (int64_t)rows * c->n_kv_heads * (c->head_dim / 8);
-    const dim3 grid((unsigned)((threads + 255) / 256), 2);
+    const int64_t blocks = ((int64_t)rows * c->n_kv_heads * (c->head_dim / 8) + 255) / 256;
+    TASC_REQUIRE(blocks < kMostBlocks, "kv4_read: %d rows of %d x %d channels are 2^35 and more", rows, c->n_kv_heads, c->head_dim);
+    const dim3 grid((unsigned)blocks, 2);
     hipStream_t st = (hipStream_t)stream;
     with_hd(c->head_dim, [&](auto hd) {
         constexpr int HD = decltype(hd)::value;
@@ -157,7 +160,9 @@ extern "C" tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv
     TASC_REQUIRE(p->q && p->out && p->table && p->row_off && p->kv_len, "kv4_attention: null argument");
     TASC_REQUIRE(p->n_heads >= 1 && p->n_heads % c->n_kv_heads == 0, "kv4_attention: %d query heads over %d KV heads", p->n_heads, c->n_kv_heads);
     TASC_REQUIRE((int64_t)p->batch * c->n_kv_heads <= 65535, "kv4_attention: batch %d x %d KV heads is beyond 65535", p->batch, c->n_kv_heads);
-    TASC_REQUIRE(p->max_pages <= (1 << 26) && (int64_t)p->max_rows * p->n_heads < (int64_t)1 << 30 && (int64_t)p->max_rows * p->n_heads / 128 * p->batch < (int64_t)1 << 30, "kv4_attention: max_pages %d, max_rows %d", p->max_pages, p->max_rows);
+    TASC_REQUIRE(p->max_pages <= (1 << 26) && (int64_t)p->max_rows * p->n_heads < (int64_t)1 << 30, "kv4_attention: max_pages %d, max_rows %d", p->max_pages, p->max_rows);
+    TASC_REQUIRE(((int64_t)p->max_rows * (p->n_heads / c->n_kv_heads) + 127) / 128 * p->batch * c->n_kv_heads < kMostBlocks,
+                 "kv4_attention: batch %d of up to %d rows of %d heads is beyond 2^31", p->batch, p->max_rows, p->n_heads);
     const int64_t width = (int64_t)p->n_heads * c->head_dim;
     TASC_REQUIRE(p->q_stride >= 0 && p->out_stride >= width, "kv4_attention: row strides %lld, %lld of rows of %lld", (long long)p->q_stride, (long long)p->out_stride,
                  (long long)width);
