@@ -470,7 +470,8 @@ tasc_status tasc_tok_enrich(const int32_t* tokens, const int64_t* doc_offsets, i
  * The operators of a serving step over a cache held in 4 bits: block tables and slots from the requests' lengths, the cache,
  * attention over it, and the verification of drafts against the target's probabilities.  They take device arrays and enqueue
  * on `stream` without a host round trip, so a step of them can be recorded into a HIP graph; array contents are bounds-checked
- * on the device (a length, page or token outside its range is handled as stated, never followed).
+ * on the device (a length, page or token outside its range is handled as stated, never followed).  What a call writes may overlap nothing else that
+ * it names (tasc_page_tables refuses such calls).
  * Pages hold TASC_PAGE_TOKENS positions.  A slot is page * TASC_PAGE_TOKENS + position in the page.
  * ---------------------------------------------------------------------------------------- */
 #define TASC_PAGE_TOKENS 16
@@ -482,7 +483,7 @@ tasc_status tasc_tok_enrich(const int32_t* tokens, const int64_t* doc_offsets, i
  *   held       int32[batch], nullable (none)  pages its table already lists
  *   free_pages int32[n_free], nullable (0, 1, ..)  pages to give away, in this order
  *   table      int32[batch, max_pages]  entries held .. are written where pages are given, all others left as they are
- *   pages      int32[batch], nullable  pages the table lists afterwards; not the same array as `held`
+ *   pages      int32[batch], nullable  pages the table lists afterwards
  *   row_off    int32[batch + 1], nullable  running sum of new_rows
  *   slots      int32[slots_cap], nullable  the rows' slots, sequence by sequence (-1 for a page outside [0, 2^27)), then -1
  *   summary    int32[3], nullable  rows; free pages asked for by the sequences up to the last one granted (those given away if none was refused

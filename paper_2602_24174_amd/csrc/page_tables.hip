@@ -186,7 +186,15 @@ extern "C" tasc_status tasc_page_tables(const int32_t* kv_len, const int32_t* ne
     TASC_REQUIRE(max_pages >= 1 && max_pages < 1 << 27, "page_tables: max_pages %d outside [1, 2^27)", max_pages);
     TASC_REQUIRE(n_free >= 0 && n_free < 1 << 27, "page_tables: n_free %d outside [0, 2^27)", n_free);
     TASC_REQUIRE(slots_cap >= 0 && (slots || slots_cap == 0), "page_tables: %d slots", slots_cap);
-    TASC_REQUIRE(!pages || !held || pages + batch <= held || held + batch <= pages, "page_tables: pages and held overlap");
+    // (workgroups read the lengths of all sequences while others write)
+    struct Array { const char* name; const int32_t* at; int64_t n; };
+    const Array written[] = {{"table", table, (int64_t)batch * max_pages}, {"pages", pages, batch}, {"row_off", row_off, batch + 1}, {"slots", slots, slots_cap}, {"summary", summary, 3}};
+    const Array read[] = {{"kv_len", kv_len, batch}, {"new_rows", new_rows, batch}, {"held", held, batch}, {"free_pages", free_pages, n_free}};
+    auto apart = [](const Array& x, const Array& y) { return !x.at || !y.at || x.n == 0 || y.n == 0 || (uintptr_t)(x.at + x.n) <= (uintptr_t)y.at || (uintptr_t)(y.at + y.n) <= (uintptr_t)x.at; };
+    for (const Array& w : written) {
+        for (const Array& r : read) TASC_REQUIRE(apart(w, r), "page_tables: %s and %s overlap", w.name, r.name);
+        for (const Array* v = written; v != &w; ++v) TASC_REQUIRE(apart(w, *v), "page_tables: %s and %s overlap", w.name, v->name);
+    }
     // runs of at least 8 sequences (a wave each), 256 workgroups at most: each reads all lengths
     const int per_wg = std::max(8, (batch + 255) / 256);
     const int n_wgs = (batch + per_wg - 1) / per_wg;
