@@ -758,24 +758,28 @@ tasc_status forward_small(const tasc_model* m, tasc_session* s, int nq, int n_se
     a.bar_epoch = s->bar_epoch;
     a.barb_base = s->barb_base;
     s->ll_armed = false;       // this kernel writes the first copy of the buffers the pipeline kernel expects untouched
-    PROF(TASC_KC_LAYERS);
     auto launch = [&](int p0, int p1) {
         if (c.head_dim == 32) k_small_step<1><<<dim3(grid), dim3(SMALL_THREADS), SMALL_LDS_BYTES, st>>>(a, p0, p1);
         else if (c.head_dim == 64) k_small_step<2><<<dim3(grid), dim3(SMALL_THREADS), SMALL_LDS_BYTES, st>>>(a, p0, p1);
         else k_small_step<4><<<dim3(grid), dim3(SMALL_THREADS), SMALL_LDS_BYTES, st>>>(a, p0, p1);
     };
-    if (g_tasc_config.small_path == 2) {
-        launch(0, last);
-        s->bar_epoch += (u32)(n_lg_phases - 1);
-        s->barb_base += (u64)(last - n_lg_phases) * grid;
-    } else {
-        for (int ph = 0; ph < last; ++ph) {
-            // a launch of one phase crosses no barrier
-            launch(ph, ph + 1);
+    {
+        PROF(TASC_KC_LAYERS);
+        if (g_tasc_config.small_path == 2) {
+            launch(0, last);
+            s->bar_epoch += (u32)(n_lg_phases - 1);
+            s->barb_base += (u64)(last - n_lg_phases) * grid;
+        } else {
+            for (int ph = 0; ph < last; ++ph) {
+                // a launch of one phase crosses no barrier
+                launch(ph, ph + 1);
+            }
         }
     }
     TASC_LAUNCH_CHECK();
-    return tail && tail->sampled ? tasc_sample_step(s, *tail, st) : TASC_OK;
+    if (!tail || !tail->sampled) return TASC_OK;
+    PROF(TASC_KC_ACCEPT);
+    return tasc_sample_step(s, *tail, st);
 }
 
 // ---------------------------------------------------------------- the spatial-pipeline kernel
@@ -894,7 +898,6 @@ tasc_status forward_pipe(const tasc_model* m, tasc_session* s, int nq, int n_sel
         return TASC_EINVAL;
     }
     const int last = n_sel > 0 ? n_phases : n_lg_phases;
-    PROF(TASC_KC_LAYERS);
     auto launch = [&](int p0, int p1) {
         pa.rearm = p0 == 0 ? (u64*)other : nullptr;
         pa.rearm_units = p0 == 0 ? w.bytes / 16 : 0;
@@ -907,14 +910,19 @@ tasc_status forward_pipe(const tasc_model* m, tasc_session* s, int nq, int n_sel
         else { PIPE_LAUNCH(4); }
 #undef PIPE_LAUNCH
     };
-    if (g_tasc_config.small_path == 2) {
-        launch(0, last);
-    } else {
-        for (int ph = 0; ph < last; ++ph) launch(ph, ph + 1);
+    {
+        PROF(TASC_KC_LAYERS);
+        if (g_tasc_config.small_path == 2) {
+            launch(0, last);
+        } else {
+            for (int ph = 0; ph < last; ++ph) launch(ph, ph + 1);
+        }
     }
     TASC_LAUNCH_CHECK();
     s->ll_copy = 1 - s->ll_copy;
-    return tail && tail->sampled ? tasc_sample_step(s, *tail, st) : TASC_OK;
+    if (!tail || !tail->sampled) return TASC_OK;
+    PROF(TASC_KC_ACCEPT);
+    return tasc_sample_step(s, *tail, st);
 }
 
 }  // namespace
