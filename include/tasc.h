@@ -542,7 +542,9 @@ typedef struct {
     int32_t max_pages, batch, rows, n_heads, max_rows, max_kv;
     float scale;
 } tasc_kv4_attn;
-/* Bytes of scratch for such a call (0: none needed, or a shape that is not served).  Calls that may overlap need their own.
+/* Bytes of scratch for such a call (0: none needed, or a shape that is not served).  Calls that may overlap need their own.  Fewer sequences or rows may need
+ * more (their keys are cut into more chunks): a workspace for several calls is the most that any of them needs, and 2^18 * (head_dim + 2) bytes
+ * are enough for every call with rows <= batch * max_rows.
  * Limits: batch * n_kv_heads <= 65535, max_pages <= 2^26, max_rows * n_heads < 2^30, batch * max_rows * n_heads < 2^31 (max_rows * n_heads /
  * n_kv_heads counted in whole 128s).  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP. */
 size_t tasc_kv4_attention_workspace_bytes(int32_t batch, int32_t rows, int32_t n_heads, int32_t n_kv_heads, int32_t head_dim,
@@ -565,7 +567,7 @@ tasc_status tasc_kv4_attention(const tasc_kv4_cache* c, const tasc_kv4_attn* a, 
  *   accept_len   int32[batch]  drafts accepted;  emitted int32[batch, k + 1]  those, then the drawn token, then -1
  *   logprob      fp32[batch, k + 1], nullable: ln p of the emitted tokens, then 0
  * A draft is accepted iff u q < p; the drawn token is the lowest one up to which the weights sum to more than u times their total.
- * Exponentials and sums are taken in 64 bits.  A row that has no distribution (a NaN, +infinity, nothing above -infinity, a
+ * Sums are of 64 bits, and so are exponentials, each within 2e-13 of itself (and 3e-16 |logit / temperature|).  A row that has no distribution (a NaN, +infinity, nothing above -infinity, a
  * temperature below 0 or NaN) accepts nothing and emits -1 with a NaN as logprob.
  * Errors: TASC_EINVAL (k outside [0, TASC_MAX_K], vocab outside [2, 2^24], more than 65535 rows), TASC_ENOMEM (workspace), TASC_EHIP.
  */

@@ -548,7 +548,7 @@ def _workspace(who, workspace, need, dev, on_current):
         if not on_current:
             _refuse(f"{who}: a call on a stream other than the current one needs a workspace of {need} bytes")
         workspace = torch.empty(need, dtype=torch.uint8, device="cuda")
-    elif workspace.get_device() != dev or not workspace.is_contiguous():
+    elif not isinstance(workspace, torch.Tensor) or workspace.get_device() != dev or not workspace.is_contiguous():
         _refuse(f"{who}: the workspace is not a contiguous tensor of the current device")
     return workspace, workspace.data_ptr() or None, workspace.numel() * workspace.element_size()
 
@@ -633,6 +633,7 @@ def tasc_kv4_read(cache: Kv4Cache, slots, k, v, stream=None):
 
 
 def tasc_kv4_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, head_dim, max_rows, max_kv) -> int:
+    """Of this call: a smaller one may need more.  2^18 * (head_dim + 2) bytes are enough for all with rows <= batch * max_rows."""
     return lib().tasc_kv4_attention_workspace_bytes(batch, rows, n_heads, n_kv_heads, head_dim, max_rows, max_kv)
 
 
