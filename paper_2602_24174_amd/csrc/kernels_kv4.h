@@ -131,8 +131,8 @@ struct Kv4Rows {
 };
 
 // One thread per 8 channels of a row's key or value head; the HD / 8 (8 at most) threads of a group find its range among themselves.
-// Bound by bytes: 2 or 4 read and 1/2 written per value (16384 rows of 8 x 128 fp32: 153 MB in 31 us, 4.9 TB/s, the rate of a copy).  VEC: rows start
-// at multiples of 16 bytes.
+// fp32 values: bound by bytes, 4 read and 1/2 written per value (16384 rows of 8 x 128: 153 MB in 31 us, 4.9 TB/s, the rate of a copy); bf16 ones
+// by the quotients in 64 bits that 62 % of the waves take (fp32 2 %): 39 us.  VEC: rows start at multiples of 16 bytes.
 template <int HD, typename T, bool VEC>
 __global__ __launch_bounds__(256) void k_kv4_append(Kv4Rows a, const T* __restrict__ k, const T* __restrict__ v, int64_t k_stride, int64_t v_stride) {
     constexpr int BLKS = HD / 8, SPAN = BLKS < 8 ? BLKS : 8;
@@ -203,8 +203,8 @@ __global__ __launch_bounds__(256) void k_kv4_read(Kv4Rows a, T* __restrict__ k, 
 // The last of these sums is three rows of a 16 x 16 product of its own, z - 16 in three bf16 terms.  Maxima, sums and products are
 // fp32.  Tiles of 32 tokens at absolute positions, chunk_tiles of them a key chunk, a chunk's dealt to
 // the waves in turn, all joined in a fixed order: a row's bits depend on neither the other rows nor the length beyond its own last key.
-// What bounds it: of long contexts with few pairs the read of the cache (2 sequences of up to 131072 tokens, 8 x 128: 227 MB in 55 us, 4.1 TB/s), else
-// the vector instructions around the products (exponentials, scales, numbers to bf16; 56 to 60 % of the busy time) and, with ragged
+// What bounds it: of long contexts with few pairs the read of the cache (2 sequences of up to 131072 tokens, 8 x 128: 227 MB in 54 us, 4.2 TB/s, where a stream of reads alone has 6.4), else
+// the vector instructions around the products (exponentials, scales, numbers to bf16; 55 to 60 % of the busy time) and, with ragged
 // lengths, compute units that are done before others.
 struct Kv4Attn {
     const uint8_t* pool;
