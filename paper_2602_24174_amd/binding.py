@@ -715,7 +715,7 @@ def tasc_sampled_scratch_bytes(model: Model, batch, k) -> int:
 
 def _sampling(who, model, s, k, u, temperature, scratch, dev, st):
     """(what must stay alive, struct).  A scratch made here comes from the memory of the call's stream, where nothing that is still to run can
-    write to it, and stays with the session, one for every k and stream, as recorded steps do."""
+    write to it, and stays with the session, one for every k and stream, as recorded steps do (a program that steps on many streams gives its own)."""
     import torch
     if s._kv_pool.get_device() != dev:
         _refuse(f"{who}: the session is on cuda:{s._kv_pool.get_device()}, the current device is cuda:{dev}")

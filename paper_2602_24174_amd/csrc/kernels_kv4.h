@@ -203,9 +203,9 @@ __global__ __launch_bounds__(256) void k_kv4_read(Kv4Rows a, T* __restrict__ k, 
 // The last of these sums is three rows of a 16 x 16 product of its own, z - 16 in three bf16 terms.  Maxima, sums and products are
 // fp32.  Tiles of 32 tokens at absolute positions, chunk_tiles of them a key chunk, a chunk's dealt to
 // the waves in turn, all joined in a fixed order: a row's bits depend on neither the other rows nor the length beyond its own last key.
-// What bounds it: of long contexts with few pairs the read of the cache (2 sequences of up to 131072 tokens, 8 x 128: 227 MB in 54 us, 4.2 TB/s, where a stream of reads alone has 6.4), else
-// the vector instructions around the products (exponentials, scales, numbers to bf16; 55 to 60 % of the busy time) and, with ragged
-// lengths, compute units that are done before others.
+// What bounds it: of long contexts with few pairs the read of the cache (2 sequences of up to 131072 tokens, 8 x 128: 227 MB in 54 us, 4.2 TB/s,
+// where a stream of reads alone has 6.4), else the vector instructions around the products (exponentials, scales, numbers to bf16; 55 to 60 % of the
+// busy time) and, with ragged lengths, compute units that are done before others.
 struct Kv4Attn {
     const uint8_t* pool;
     int32_t n_pages, max_pages, Hkv, H, batch, rows, max_rows, chunks, chunk_tiles, row_waves;
@@ -350,7 +350,8 @@ __device__ __forceinline__ Kv4Z kv4_z(float scale, float low) {
 constexpr float kKv4Grown = 8.f;                        // a maximum is followed once it grew by more than this power of 2
 // Sums are taken of 2^-40 times the values from the first tile on that holds large ones (kKv4Large), for these have no room beside the weights
 // (up to 2^8 each, of up to 2^30 tokens) and 16 + c: below that a sum is at most 2^38 (31 scale + |low - 16 scale|) < 2^111, and with the factor, of
-// the largest values, 2^38 2^129.1 2^-40 < 2^128.  A power of 2: what ordinary tiles give is the same bits either way.
+// the largest values, 2^38 2^129.1 2^-40 < 2^128.  A power of 2: what ordinary tiles give is the same bits either way (products of a weight and
+// a scale from 2^-86 on).
 constexpr float kKv4Large = 0x1p70f, kKv4Less = 0x1p-40f, kKv4Room = 0x1p118f;
 
 // What a wave holds: MT tiles of 16 (row, head) pairs of a KV head, with their queries and sums.
