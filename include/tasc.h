@@ -343,8 +343,8 @@ tasc_status tasc_generate_sampled(const tasc_model* m, const tasc_ngram* ng, tas
  * prompt + max_new + 2 * max_rows tokens (tasc_page_tables) and fails with TASC_ENOMEM if the pool has fewer.  For bf16 models with d_model,
  * n_heads * head_dim and d_ffn multiples of 64 and heads of 32, 64 or 128 channels; every forward takes the tiled kernels, whatever
  * TASC_CFG_SMALL_PATH and TASC_CFG_TILED_PATH say, so steps of at most 16 rows are slower than on a bf16 session's persistent kernels (a 0.1B model, one sequence:
- * 1375 us a step instead of 560); many sequences' steps take as long as a bf16 session's, long contexts' less (a 1.5B model, one sequence of
- * 32768 tokens: 6.6 ms instead of 19).  Greedy and speculative decoding of such a session agree bit for bit.
+ * 1460 us a step instead of 560); many sequences' steps take as long as a bf16 session's, long contexts' less (a 1.5B model, one sequence of
+ * 32768 tokens: 6.7 ms instead of 19).  Greedy and speculative decoding of such a session agree bit for bit.
  * kv_pool need not be cleared.  Otherwise as tasc_session_create.
  */
 size_t tasc_session_kv4_bytes(const tasc_model* m, int32_t n_pages);
