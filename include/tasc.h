@@ -579,6 +579,56 @@ tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t ro
                                 int32_t* accept_len, int32_t* emitted, float* logprob, void* workspace, size_t ws_bytes,
                                 void* stream);
 
+/*
+ * Sequences that continue others (several samples of one prompt): for each pair i, sequence dst[i] gets sequence src[i]'s tokens.  Its table lists the
+ * same pages, but a last page that is partly filled is replaced by new_pages[i], since both go on writing there; the copy that this asks for is copy_from[i] ->
+ * copy_to[i] (tasc_pages_copy makes it), -1 for none.  kv_len[dst[i]] = kv_len[src[i]], pages[dst[i]] = its pages; table entries behind them stay.
+ *   src, dst   int32[n];  new_pages int32[n], nullable (none): pages that no table lists, all different; one that is not needed stays free
+ *   kv_len, pages  int32[batch]; table int32[batch, max_pages]; copy_from, copy_to int32[n]
+ *   summary    int32[3], nullable: pairs granted, new pages taken, pairs refused
+ * The pages that dst listed before are given up (tasc_pages_free finds those that no table lists any more).  A pair is refused, changes nothing and asks for no copy,
+ * if src or dst is outside [0, batch), if they are one, if a pair before it has the same dst, if any pair's src is its dst, if src's table does not list its
+ * tokens (kv_len < 0, or more pages than pages[src], or pages[src] > max_pages) or if it needs a page and new_pages[i] is outside [0, 2^27).
+ * A sequence that shares pages may not be cut back into them and written again: its rows would show in the others.
+ * Limits: n <= 2^14, batch in [1, 2^20], max_pages < 2^27.  Errors: TASC_EINVAL, TASC_EHIP.
+ */
+tasc_status tasc_pages_fork(const int32_t* src, const int32_t* dst, int32_t n, const int32_t* new_pages, int32_t* kv_len, int32_t* table,
+                            int32_t* pages, int32_t batch, int32_t max_pages, int32_t* copy_from, int32_t* copy_to, int32_t* summary,
+                            void* stream);
+/*
+ * Copies page copy_from[i] to page copy_to[i], i < n, in each of n_layers layers of a pool: layer j holds n_pages pages of page_bytes bytes from
+ * pool + j * layer_stride on (a 4-bit cache: tasc_kv4_page_bytes).  A pair with a page outside [0, n_pages), or with one page twice, copies nothing.  The pages
+ * copied to must differ from each other and from all that are copied from: what such a page holds afterwards is unspecified (no other page is touched).
+ *   pool  DEVICE, 16-byte aligned; page_bytes a multiple of 16 up to 2^30; layer_stride a multiple of 16, >= n_pages * page_bytes
+ * Errors: TASC_EINVAL, TASC_EHIP.
+ */
+tasc_status tasc_pages_copy(void* pool, size_t page_bytes, int32_t n_pages, int32_t n_layers, size_t layer_stride,
+                            const int32_t* copy_from, const int32_t* copy_to, int32_t n, void* stream);
+/*
+ * The pages of a pool that no sequence lists: what requests that ended, were cut back or were forked over have left, ready for
+ * tasc_page_tables.  Sequence b lists the first pages[b] entries of its row (cut to [0, max_pages]; a request that has ended has 0), several
+ * sequences may list one page; entries outside [0, n_pages) list none.
+ *   free_pages  int32[n_pages]: the free pages, ascending, then -1
+ *   summary     int32[3], nullable: free pages, listed pages, entries that list one
+ *   workspace   of tasc_pages_workspace_bytes, 16-byte aligned; calls that may overlap need their own
+ * Limits: batch in [1, 2^20], max_pages and n_pages in [1, 2^27).  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP.
+ */
+size_t tasc_pages_workspace_bytes(int32_t n_pages);
+tasc_status tasc_pages_free(const int32_t* table, const int32_t* pages, int32_t batch, int32_t max_pages, int32_t n_pages,
+                            int32_t* free_pages, int32_t* summary, void* workspace, size_t ws_bytes, void* stream);
+/*
+ * Moves the listed pages to the front of their pool: with L of them (a shared one counts once), the highest page at or above L goes to the lowest
+ * free page below L, and so on; copy_from and copy_to are those moves, then -1, for tasc_pages_copy, which must follow before anything else uses table_out.
+ * table_out[b][j] is where entry j < pages[b] lies afterwards (an entry outside [0, n_pages) stays as it is); other entries of table_out are left as they
+ * are; it may be table.  Only the first max_moves moves are made, if there are more.
+ *   copy_from, copy_to  int32[max_moves] (n_pages / 2 are enough for all)
+ *   summary   int32[3], nullable: L, moves made, pages that the pool needs afterwards (behind the last listed one)
+ * Otherwise as tasc_pages_free.
+ */
+tasc_status tasc_pages_compact(const int32_t* table, const int32_t* pages, int32_t batch, int32_t max_pages, int32_t n_pages,
+                               int32_t* table_out, int32_t* copy_from, int32_t* copy_to, int32_t max_moves, int32_t* summary,
+                               void* workspace, size_t ws_bytes, void* stream);
+
 /* ------------------------------------------------------------------------------------------
  * Measurement: per-kernel-class device time, taken with HIP event pairs recorded on the stream
  * each kernel is launched on.  Off by default (no events are recorded).  The classes follow the

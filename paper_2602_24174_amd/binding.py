@@ -25,6 +25,7 @@ EXPORTS = [
     "tasc_page_tables", "tasc_kv4_page_bytes", "tasc_kv4_append", "tasc_kv4_read", "tasc_kv4_attention_workspace_bytes",
     "tasc_kv4_attention", "tasc_accept_sampled_workspace_bytes", "tasc_accept_sampled", "tasc_sampled_scratch_bytes",
     "tasc_verify_step_sampled", "tasc_session_rewind", "tasc_generate_sampled", "tasc_session_kv4_bytes", "tasc_session_create_kv4",
+    "tasc_pages_fork", "tasc_pages_copy", "tasc_pages_workspace_bytes", "tasc_pages_free", "tasc_pages_compact",
 ]
 KERNEL_CLASSES = ["draft", "prepare", "norm", "gemm_qkv", "rope_kv", "attn", "gemm_o", "gemm_gu", "gemm_d", "lmhead", "accept",
                   "verify", "layers"]
@@ -148,9 +149,17 @@ def lib():
         L.tasc_session_kv4_bytes.argtypes = [C.c_void_p, C.c_int32]
         L.tasc_session_create_kv4.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
                                               C.POINTER(C.c_void_p)]
-        for name in ("tasc_kv4_page_bytes", "tasc_sampled_scratch_bytes", "tasc_session_kv4_bytes", "tasc_kv4_attention_workspace_bytes", "tasc_accept_sampled_workspace_bytes"):
+        for name in ("tasc_kv4_page_bytes", "tasc_sampled_scratch_bytes", "tasc_session_kv4_bytes", "tasc_kv4_attention_workspace_bytes", "tasc_accept_sampled_workspace_bytes",
+                     "tasc_pages_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.tasc_kv4_page_bytes.argtypes = [C.c_int32] * 2
+        L.tasc_pages_workspace_bytes.argtypes = [C.c_int32]
+        L.tasc_pages_fork.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
+                                      C.c_void_p, C.c_void_p, C.c_void_p]
+        L.tasc_pages_copy.argtypes = [C.c_void_p, C.c_size_t, C.c_int32, C.c_int32, C.c_size_t, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p]
+        L.tasc_pages_free.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.tasc_pages_compact.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p,
+                                         C.c_void_p, C.c_size_t, C.c_void_p]
         L.tasc_kv4_append.argtypes = [C.POINTER(Kv4CacheDesc), C.c_void_p, C.c_void_p, C.c_int32, C.c_int64, C.c_int64, C.c_void_p, C.c_int32, C.c_void_p]
         L.tasc_kv4_read.argtypes = [C.POINTER(Kv4CacheDesc), C.c_void_p, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p]
         L.tasc_kv4_attention_workspace_bytes.argtypes = [C.c_int32] * 7
@@ -578,6 +587,73 @@ def tasc_page_tables(kv_len, new_rows, held, free_pages, table, pages=None, row_
         free or None, n, _array(who, "table", table, i32, table.shape, dev), table.shape[1], None if pages is None else _array(who, "pages", pages, i32, per, dev),
         None if row_off is None else _array(who, "row_off", row_off, i32, (B + 1,), dev), at or None, cap,
         None if summary is None else _array(who, "summary", summary, i32, (3,), dev), st))
+
+
+def _tables(who, table, pages, dev):
+    """(address of the table, of pages, batch, max_pages)"""
+    import torch
+    at, B = _list(who, "pages", pages, torch.int32, dev)
+    if getattr(table, "ndim", 0) != 2 or table.shape[0] != B:
+        _refuse(f"{who}: table is not [{B}, max_pages]")
+    return _array(who, "table", table, torch.int32, table.shape, dev), at, B, table.shape[1]
+
+
+def tasc_pages_fork(src, dst, kv_len, table, pages, new_pages, copy_from, copy_to, summary=None, stream=None):
+    """int32 cuda tensors: src, dst, new_pages (or None), copy_from, copy_to [pairs], kv_len, pages [batch], table [batch, max_pages], summary [3]; kv_len, table,
+    pages, copy_from, copy_to and summary are written in place."""
+    import torch
+    who, i32 = "pages_fork", torch.int32
+    dev, st, _ = _here(stream)
+    s, n = _list(who, "src", src, i32, dev)
+    tab, at, B, cols = _tables(who, table, pages, dev)
+    per = src.shape
+    _check(lib().tasc_pages_fork(s or None, _array(who, "dst", dst, i32, per, dev) or None, n, None if new_pages is None else _array(who, "new_pages", new_pages, i32, per, dev) or None,
+                                 _array(who, "kv_len", kv_len, i32, pages.shape, dev), tab, at, B, cols, _array(who, "copy_from", copy_from, i32, per, dev) or None,
+                                 _array(who, "copy_to", copy_to, i32, per, dev) or None, None if summary is None else _array(who, "summary", summary, i32, (3,), dev), st))
+
+
+def tasc_pages_copy(pool, page_bytes, n_pages, n_layers, copy_from, copy_to, layer_stride=None, stream=None):
+    """pool: contiguous cuda tensor that holds n_layers layers of n_pages pages of page_bytes bytes, layer_stride bytes from one to the next (None: one behind the
+    other); copy_from, copy_to int32 [any]."""
+    import torch
+    who, i32 = "pages_copy", torch.int32
+    dev, st, _ = _here(stream)
+    at, n = _list(who, "copy_from", copy_from, i32, dev)
+    stride = n_pages * page_bytes if layer_stride is None else layer_stride
+    if not isinstance(pool, torch.Tensor) or pool.get_device() != dev or not pool.is_contiguous():
+        _refuse(f"{who}: the pool is not a contiguous tensor on cuda:{dev}, the current device")
+    if min(page_bytes, n_pages, n_layers, stride) < 0 or (n_layers > 0 and (n_layers - 1) * stride + n_pages * page_bytes > pool.numel() * pool.element_size()):
+        _refuse(f"{who}: the pool does not hold {n_layers} layers of {n_pages} pages of {page_bytes} bytes")
+    _check(lib().tasc_pages_copy(pool.data_ptr(), page_bytes, n_pages, n_layers, stride, at or None, _array(who, "copy_to", copy_to, i32, copy_from.shape, dev) or None, n, st))
+
+
+def tasc_pages_workspace_bytes(n_pages) -> int:
+    return lib().tasc_pages_workspace_bytes(n_pages)
+
+
+def tasc_pages_free(table, pages, n_pages, free_pages, summary=None, workspace=None, stream=None):
+    """int32 cuda tensors: table [batch, max_pages], pages [batch]; free_pages [n_pages] and summary [3] are written in place."""
+    import torch
+    who, i32 = "pages_free", torch.int32
+    dev, st, on_current = _here(stream)
+    tab, at, B, cols = _tables(who, table, pages, dev)
+    keep, ws, n = _workspace(who, workspace, 0 if workspace is not None else tasc_pages_workspace_bytes(n_pages), dev, on_current)
+    _check(lib().tasc_pages_free(tab, at, B, cols, n_pages, _array(who, "free_pages", free_pages, i32, (n_pages,), dev),
+                                 None if summary is None else _array(who, "summary", summary, i32, (3,), dev), ws, n, st))
+
+
+def tasc_pages_compact(table, pages, n_pages, table_out, copy_from, copy_to, summary=None, workspace=None, stream=None):
+    """int32 cuda tensors: table [batch, max_pages], pages [batch]; table_out [batch, max_pages] (it may be table), copy_from, copy_to [most moves] and
+    summary [3] are written in place."""
+    import torch
+    who, i32 = "pages_compact", torch.int32
+    dev, st, on_current = _here(stream)
+    tab, at, B, cols = _tables(who, table, pages, dev)
+    frm, cap = _list(who, "copy_from", copy_from, i32, dev)
+    keep, ws, n = _workspace(who, workspace, 0 if workspace is not None else tasc_pages_workspace_bytes(n_pages), dev, on_current)
+    _check(lib().tasc_pages_compact(tab, at, B, cols, n_pages, _array(who, "table_out", table_out, i32, table.shape, dev), frm or None,
+                                    _array(who, "copy_to", copy_to, i32, copy_from.shape, dev) or None, cap,
+                                    None if summary is None else _array(who, "summary", summary, i32, (3,), dev), ws, n, st))
 
 
 def tasc_kv4_page_bytes(n_kv_heads, head_dim) -> int:
