@@ -582,7 +582,7 @@ tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t ro
 /*
  * Sequences that continue others (several samples of one prompt): for each pair i, sequence dst[i] gets sequence src[i]'s tokens.  Its table lists the
  * same pages, but a last page that is partly filled is replaced by new_pages[i], since both go on writing there; the copy that this asks for is copy_from[i] ->
- * copy_to[i] (tasc_pages_copy makes it), -1 for none.  kv_len[dst[i]] = kv_len[src[i]], pages[dst[i]] = its pages; table entries behind them stay.
+ * copy_to[i] (tasc_pages_copy makes it), -1 for none and -2 where the pair is refused.  kv_len[dst[i]] = kv_len[src[i]], pages[dst[i]] = its pages; table entries behind them stay.
  *   src, dst   int32[n];  new_pages int32[n], nullable (none): pages that no table lists, all different; one that is not needed stays free
  *   kv_len, pages  int32[batch]; table int32[batch, max_pages]; copy_from, copy_to int32[n]
  *   summary    int32[3], nullable: pairs granted, new pages taken, pairs refused

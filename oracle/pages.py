@@ -4,7 +4,7 @@
 def fork(src, dst, new_pages, kv_len, table, pages, page=16):
     """kv_len, table (list of lists) and pages are changed in place.  Returns (copy_from, copy_to, summary)."""
     batch, cols = len(kv_len), len(table[0])
-    copy_from, copy_to, done = [-1] * len(src), [-1] * len(src), []
+    copy_from, copy_to, done = [-2] * len(src), [-2] * len(src), []
     for i, (s, d) in enumerate(zip(src, dst)):
         if not (0 <= s < batch and 0 <= d < batch) or s == d or d in dst[:i] or d in src:
             continue
@@ -15,6 +15,7 @@ def fork(src, dst, new_pages, kv_len, table, pages, page=16):
         done.append((i, s, d, need, part))
     for i, s, d, need, part in done:
         kv_len[d], pages[d] = kv_len[s], need
+        copy_from[i] = copy_to[i] = -1
         table[d][:need] = table[s][:need]
         if part:
             copy_from[i], copy_to[i] = table[s][need - 1], new_pages[i]

@@ -1,7 +1,7 @@
 // Pages of a cache behind their tables: sequences that continue others, pages copied through all layers, the pages that no table lists, and the
 // pages in use moved to the front of their pool.
 //
-// Which pages are in use follows from the tables alone (a bitmap of the pages that any table lists), so sequences may share pages without
+// Which pages are in use follows from the tables alone (a map of the pages that any table lists), so sequences may share pages without
 // counts that have to be kept beside them.
 #include "tasc_internal.h"
 #include <algorithm>
@@ -39,37 +39,37 @@ __device__ __forceinline__ Fork fork_of(const ForkArgs& a, int i) {
 }
 
 // A workgroup a pair, which looks through all pairs for one that takes the same place or continues it (nothing that a granted pair reads is
-// then written by another); one more workgroup adds up, a lane a pair.  A few integers per page of a prompt: bound by launch and three dependent reads.
+// then written by another).  A few integers per page of a prompt: bound by launch and three dependent reads.  Up to kForkThreads pairs are added up by
+// one more workgroup of the same launch, a lane a pair with the others' numbers out of LDS; more by a launch of its own, since that
+// workgroup's look at all pairs of all pairs would take longer than the copies (480 pairs, one at a time through the scalar cache: 130 us).
 constexpr int kForkThreads = 256;
+__device__ __forceinline__ void sum_forks(int done, int taken, int refused, int32_t* summary, int (&s_sum)[3][kForkThreads / 64], int tid) {
+    done = wave_sum32(done);
+    taken = wave_sum32(taken);
+    refused = wave_sum32(refused);
+    if ((tid & 63) == 0) {
+        s_sum[0][tid >> 6] = done;
+        s_sum[1][tid >> 6] = taken;
+        s_sum[2][tid >> 6] = refused;
+    }
+    __syncthreads();
+    if (tid < 3) summary[tid] = s_sum[tid][0] + s_sum[tid][1] + s_sum[tid][2] + s_sum[tid][3];
+}
 __global__ __launch_bounds__(kForkThreads) void k_pages_fork(ForkArgs a) {
     __shared__ int s_clash[kForkThreads / 64], s_sum[3][kForkThreads / 64];
+    __shared__ int2 s_pair[kForkThreads];
     const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
     if ((int)blockIdx.x == a.n) {
-        int done = 0, taken = 0, refused = 0;
-        for (int i0 = 0; i0 < a.n; i0 += kForkThreads) {
-            const int i = i0 + tid;
-            Fork f{-1, -1, 0, 0, false, false};
-            if (i < a.n) f = fork_of(a, i);
-            for (int j = 0; j < a.n; ++j) {
-                const int s = a.src[j], d = a.dst[j];      // (the same in all lanes)
-                if (s == f.dst || (j < i && d == f.dst)) f.ok = false;
-            }
-            if (i >= a.n) continue;
-            done += f.ok;
-            taken += f.ok && f.part;
-            refused += !f.ok;
-        }
-        done = wave_sum32(done);
-        taken = wave_sum32(taken);
-        refused = wave_sum32(refused);
-        if (lane == 0) {
-            s_sum[0][wave] = done;
-            s_sum[1][wave] = taken;
-            s_sum[2][wave] = refused;
-        }
+        Fork f{-1, -1, 0, 0, false, false};
+        if (tid < a.n) f = fork_of(a, tid);
+        s_pair[tid] = int2{f.src, f.dst};
         __syncthreads();
-        if (tid < 3) a.summary[tid] = s_sum[tid][0] + s_sum[tid][1] + s_sum[tid][2] + s_sum[tid][3];
-        return;
+        for (int j = 0; j < a.n; ++j) {
+            const int2 p = s_pair[j];
+            if (p.x == f.dst || (j < tid && p.y == f.dst)) f.ok = false;
+        }
+        const bool real = tid < a.n;
+        return sum_forks(real && f.ok, real && f.ok && f.part, real && !f.ok, a.summary, s_sum, tid);
     }
     const int i = blockIdx.x;
     const Fork f = fork_of(a, i);
@@ -79,7 +79,7 @@ __global__ __launch_bounds__(kForkThreads) void k_pages_fork(ForkArgs a) {
     if (lane == 0) s_clash[wave] = any;
     __syncthreads();
     const bool granted = f.ok && !(s_clash[0] | s_clash[1] | s_clash[2] | s_clash[3]);
-    const int fresh = granted && f.part ? a.new_pages[i] : -1;
+    const int fresh = !granted ? -2 : f.part ? a.new_pages[i] : -1;
     if (granted) {
         const int32_t* const from = a.table + (size_t)f.src * a.max_pages;
         int32_t* const to = a.table + (size_t)f.dst * a.max_pages;
@@ -90,9 +90,20 @@ __global__ __launch_bounds__(kForkThreads) void k_pages_fork(ForkArgs a) {
         }
     }
     if (tid == 0) {
-        a.copy_from[i] = fresh >= 0 ? a.table[(size_t)f.src * a.max_pages + f.need - 1] : -1;
+        a.copy_from[i] = fresh >= 0 ? a.table[(size_t)f.src * a.max_pages + f.need - 1] : fresh;
         a.copy_to[i] = fresh;
     }
+}
+__global__ __launch_bounds__(kForkThreads) void k_pages_fork_sum(const int32_t* copy_to, int n, int32_t* summary) {
+    __shared__ int s_sum[3][kForkThreads / 64];
+    int done = 0, taken = 0, refused = 0;
+    for (int i = threadIdx.x; i < n; i += kForkThreads) {
+        const int to = copy_to[i];
+        done += to != -2;
+        taken += to >= 0;
+        refused += to == -2;
+    }
+    sum_forks(done, taken, refused, summary, s_sum, threadIdx.x);
 }
 
 // ---------------------------------------------------------------- copies
@@ -131,10 +142,12 @@ __global__ __launch_bounds__(kCopyThreads) void k_pages_copy(CopyArgs a) {
 struct UseArgs {
     const int32_t *table, *pages;
     int32_t batch, max_pages, n_pages, n_words;
-    u32* bits;                         // a bit a page: some table lists it
+    uint8_t* marks;                    // [32 n_words, to a whole 64] a byte a page: some table lists it
+    u32* bits;                         // the same as bits
     u32* before;                       // [n_words] listed pages in the words before (compacting)
     u32* sums;                         // [n_blocks] listed pages of a block of words
-    u64* entries;                      // table entries that list a page of the pool
+    u64* entries;                      // [n_marking] table entries that list a page of the pool, by workgroup
+    int32_t n_marking;
     int32_t* free_pages;               // freeing
     int32_t *table_out, *copy_from, *copy_to;   // compacting
     int32_t cap;                       // moves
@@ -145,42 +158,38 @@ constexpr int kBlockWords = 1024, kUseThreads = 256, kSmallThreads = 1024;
 __device__ __forceinline__ int row_pages(const UseArgs& a, int b) { return min(max(a.pages[b], 0), a.max_pages); }
 
 __global__ __launch_bounds__(kUseThreads) void k_use_clear(UseArgs a) {
-    const int i = blockIdx.x * kUseThreads + threadIdx.x;
-    if (i < a.n_words) a.bits[i] = 0;
-    if (i == 0) *a.entries = 0;
+    quad* const to = (quad*)a.marks;                       // (two words' pages)
+    const int n = (a.n_words + 1) / 2 * 4;
+    for (int i = blockIdx.x * kUseThreads + threadIdx.x; i < n; i += gridDim.x * kUseThreads) to[i] = quad{0, 0, 0, 0};
 }
-// A wave a sequence; a bit that is there already is not set again, so shared pages cost no atomics of their own.
-constexpr int kMarkCols = 4096;
-__global__ __launch_bounds__(kUseThreads) void k_use_mark(UseArgs a) {
-    __shared__ int s_n[kUseThreads / 64];
-    const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.x * (kUseThreads / 64) + wave;
-    int n = 0;
-    if (b < a.batch) {
-        const int to = min(row_pages(a, b), (int)min((int64_t)(blockIdx.y + 1) * kMarkCols, (int64_t)a.max_pages));
+// A wave a sequence (of a run of columns).  A page's mark is a byte, written by whoever lists it: bits set by atomics, which cross the chip's dies one by
+// one, took 230 of 248 us for 2.5 million entries of a pool of 3.7 million pages.
+constexpr int kMarkCols = 4096, kMarkBlocks = 2048;
+__global__ __launch_bounds__(kUseThreads) void k_use_mark(UseArgs a, int col_runs, int64_t n_items) {
+    __shared__ u64 s_n[kUseThreads / 64];
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    u64 n = 0;
+    for (int64_t item = (int64_t)blockIdx.x * (kUseThreads / 64) + wave; item < n_items; item += (int64_t)gridDim.x * (kUseThreads / 64)) {
+        const int b = (int)(item / col_runs), run = (int)(item % col_runs);
+        const int to = min(row_pages(a, b), (int)min((int64_t)(run + 1) * kMarkCols, (int64_t)a.max_pages));
         const int32_t* const row = a.table + (size_t)b * a.max_pages;
-        constexpr int AHEAD = 4;
-        for (int c = blockIdx.y * kMarkCols + lane; c < to; c += 64 * AHEAD) {
+        constexpr int AHEAD = 8;
+        for (int c = run * kMarkCols + lane; c < to; c += 64 * AHEAD) {
             int p[AHEAD];
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) p[j] = c + 64 * j < to ? row[c + 64 * j] : -1;
-            u32 had[AHEAD];
-#pragma unroll
-            for (int j = 0; j < AHEAD; ++j) had[j] = p[j] >= 0 && p[j] < a.n_pages ? a.bits[p[j] >> 5] : 0;
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
                 if (p[j] < 0 || p[j] >= a.n_pages) continue;
                 ++n;
-                if (!(had[j] >> (p[j] & 31) & 1)) atomicOr(&a.bits[p[j] >> 5], 1u << (p[j] & 31));
+                a.marks[p[j]] = 1;
             }
         }
     }
-    n = wave_sum32(n);
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
     if (lane == 0) s_n[wave] = n;
     __syncthreads();
-    if (threadIdx.x == 0) {
-        n = s_n[0] + s_n[1] + s_n[2] + s_n[3];
-        if (n) atomicAdd(a.entries, (u64)n);
-    }
+    if (threadIdx.x == 0) a.entries[blockIdx.x] = s_n[0] + s_n[1] + s_n[2] + s_n[3];
 }
 __device__ __forceinline__ int block_sum(int v, int* s, int tid) {       // of 256 threads
     v = wave_sum32(v);
@@ -194,7 +203,15 @@ __global__ __launch_bounds__(kUseThreads) void k_use_count(UseArgs a) {
     __shared__ int s[kUseThreads / 64];
     const int tid = threadIdx.x, w0 = blockIdx.x * kBlockWords;
     int n = 0;
-    for (int w = w0 + tid; w < min(w0 + kBlockWords, a.n_words); w += kUseThreads) n += __popc(a.bits[w]);
+    for (int w = w0 + tid; w < min(w0 + kBlockWords, a.n_words); w += kUseThreads) {
+        const quad* const p = (const quad*)(a.marks + 32 * (size_t)w);
+        const quad lo = p[0], hi = p[1];
+        // four marks to four bits: byte i's bit 0 goes to bit 21 + i of the product
+        auto four = [](u32 m) { return m * 0x00204081u >> 21 & 15; };
+        const u32 bits = four(lo[0]) | four(lo[1]) << 4 | four(lo[2]) << 8 | four(lo[3]) << 12 | four(hi[0]) << 16 | four(hi[1]) << 20 | four(hi[2]) << 24 | four(hi[3]) << 28;
+        a.bits[w] = bits;
+        n += __popc(bits);
+    }
     n = block_sum(n, s, tid);
     if (tid == 0) a.sums[blockIdx.x] = n;
 }
@@ -301,7 +318,16 @@ __global__ __launch_bounds__(kUseThreads) void k_use_list(UseArgs a) {
         }
     }
     pad<COMPACT>(a, t, (int64_t)blk * kUseThreads + tid, (int64_t)n_blocks * kUseThreads);
-    if (blk == 0 && tid == 0) sum_use<COMPACT>(a, t, *a.entries);
+    if (blk == 0) {
+        __shared__ u64 s_entries[kUseThreads / 64];
+        u64 n = 0;
+        if (!COMPACT)
+            for (int i = tid; i < a.n_marking; i += kUseThreads) n += a.entries[i];
+        for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+        if (lane == 0) s_entries[wave] = n;
+        __syncthreads();
+        if (tid == 0) sum_use<COMPACT>(a, t, s_entries[0] + s_entries[1] + s_entries[2] + s_entries[3]);
+    }
     if (COMPACT && blk == 0 && tid == 0) a.sums[n_blocks] = t.listed;
 }
 // the page that holds page p's contents after the moves
@@ -403,8 +429,9 @@ __global__ __launch_bounds__(kSmallThreads) void k_use_small(UseArgs a) {
     }
 }
 
-// the workspace: bits, running sums, sums of blocks and how many are listed, entries
+// the workspace: entries, marks, bits, running sums, sums of blocks and how many are listed
 int words_of(int n_pages) { return (n_pages - 1) / 32 + 1; }
+size_t mark_bytes(int n_words) { return (size_t)((n_words + 1) / 2) * 64; }
 int blocks_of(int n_words) { return (n_words - 1) / kBlockWords + 1; }
 constexpr int kSmallWords = 2048, kSmallBatch = 64, kSmallEntries = 1 << 16;
 
@@ -429,12 +456,16 @@ tasc_status enqueue_use(const char* who, UseArgs a, void* workspace, size_t ws_b
         return TASC_OK;
     }
     a.entries = (u64*)workspace;
-    a.bits = (u32*)workspace + 4;
+    a.marks = (uint8_t*)(a.entries + kMarkBlocks);
+    a.bits = (u32*)(a.marks + mark_bytes(a.n_words));
     a.before = a.bits + a.n_words;
     a.sums = a.before + a.n_words;
-    const dim3 threads(kUseThreads), rows((unsigned)((a.batch + kUseThreads / 64 - 1) / (kUseThreads / 64)), (unsigned)((a.max_pages - 1) / kMarkCols + 1));
-    k_use_clear<<<dim3((unsigned)((a.n_words + kUseThreads - 1) / kUseThreads)), threads, 0, st>>>(a);
-    k_use_mark<<<rows, threads, 0, st>>>(a);
+    const int col_runs = (a.max_pages - 1) / kMarkCols + 1;
+    const int64_t items = (int64_t)a.batch * col_runs;
+    a.n_marking = (int)std::min<int64_t>((items + kUseThreads / 64 - 1) / (kUseThreads / 64), kMarkBlocks);
+    const dim3 threads(kUseThreads), rows((unsigned)((a.batch + kUseThreads / 64 - 1) / (kUseThreads / 64)), (unsigned)col_runs);
+    k_use_clear<<<dim3((unsigned)std::min((a.n_words / 2 * 4 + kUseThreads) / kUseThreads, 4096)), threads, 0, st>>>(a);
+    k_use_mark<<<dim3((unsigned)a.n_marking), threads, 0, st>>>(a, col_runs, items);
     k_use_count<<<dim3((unsigned)n_blocks), threads, 0, st>>>(a);
     k_use_list<COMPACT><<<dim3((unsigned)n_blocks), threads, 0, st>>>(a);
     if (COMPACT) k_use_rewrite<<<rows, threads, 0, st>>>(a, n_blocks);
@@ -467,7 +498,9 @@ extern "C" tasc_status tasc_pages_fork(const int32_t* src, const int32_t* dst, i
     }
     if (n == 0 && !summary) return TASC_OK;
     const ForkArgs a{src, dst, new_pages, kv_len, table, pages, copy_from, copy_to, summary, n, batch, max_pages};
-    k_pages_fork<<<dim3((unsigned)(n + (summary ? 1 : 0))), dim3(kForkThreads), 0, (hipStream_t)stream>>>(a);
+    const bool at_once = n <= kForkThreads;
+    k_pages_fork<<<dim3((unsigned)(n + (summary && at_once ? 1 : 0))), dim3(kForkThreads), 0, (hipStream_t)stream>>>(a);
+    if (summary && !at_once) k_pages_fork_sum<<<dim3(1), dim3(kForkThreads), 0, (hipStream_t)stream>>>(copy_to, n, summary);
     TASC_LAUNCH_CHECK();
     return TASC_OK;
 }
@@ -494,7 +527,7 @@ extern "C" tasc_status tasc_pages_copy(void* pool, size_t page_bytes, int32_t n_
 extern "C" size_t tasc_pages_workspace_bytes(int32_t n_pages) {
     if (n_pages < 1 || n_pages >= kPageLimit) return 0;
     const int words = words_of(n_pages);
-    return 16 + ((size_t)words * 2 + blocks_of(words) + 1) * 4;
+    return kMarkBlocks * sizeof(u64) + mark_bytes(words) + ((size_t)words * 2 + blocks_of(words) + 1) * 4;
 }
 
 extern "C" tasc_status tasc_pages_free(const int32_t* table, const int32_t* pages, int32_t batch, int32_t max_pages, int32_t n_pages, int32_t* free_pages,

@@ -15,7 +15,7 @@ def test_a_fork_shares_full_pages_and_copies_the_last():
 def test_pairs_that_are_refused():
     kv_len, pages, table = [20, 20, -1, 33, 5], [2, 1, 1, 4, 1], [[0, 1, -1]] * 5
     for src, dst, new in ((0, 0, 9), (0, 5, 9), (-1, 1, 9), (1, 4, 9), (2, 4, 9), (3, 4, 9), (0, 4, -1), (0, 4, 1 << 27)):
-        assert OP.fork([src], [dst], [new], kv_len, table, pages) == ([-1], [-1], [0, 0, 1])
+        assert OP.fork([src], [dst], [new], kv_len, table, pages) == ([-2], [-2], [0, 0, 1])
     assert OP.fork([0], [4], None, kv_len, table, pages)[2] == [0, 0, 1]
     # one place twice: the first; a place that another pair continues: not at all
     table = [[b, b + 10, -1] for b in range(5)]
