@@ -580,6 +580,35 @@ tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t ro
                                 void* stream);
 
 /*
+ * A token of each row under top-k, top-p and min-p, from given random numbers.  A row's tokens are taken by their logits, the largest first,
+ * the lowest index first among equal ones; a token weighs w = exp((logit - largest) / temperature) (temperature 0: 1 at the first token alone;
+ * infinite: all that are not masked weigh 1; -infinity masks a token).  With K = top_k and C the sum of w over the places before a token's, it is kept
+ * if its place is below K and, unless it is the first, C < top_p * (sum of w over the places below K) and w >= min_p.  The token drawn is the
+ * lowest one up to which the kept weights sum to more than u times their total.
+ *   logits       [rows, vocab] of `dtype` (fp32 or bf16), rows row_stride elements apart
+ *   temperature  fp32[rows], nullable (1);  top_k int32[rows], nullable; 0 and less, and more than there are, keep all
+ *   top_p        fp32[rows], nullable; 1 and more keep all, 0 and less the first;  min_p fp32[rows], nullable; 0 and less keep all
+ *   u            fp32[rows] in [0, 1)
+ *   token        int32[rows];  logprob fp32[rows], nullable: ln of its share of the kept weights;  kept int32[rows], nullable: tokens kept
+ * Weights are sums of whole numbers of 2^-39 to 2^-60 (by vocab), a bin of weights alike at a time, so a row's outputs depend neither on the order of the work nor on other
+ * rows' contents.  A row without a distribution (a NaN, +infinity, nothing above -infinity, a temperature below 0 or a NaN as one of its parameters) gives
+ * token -1 with a NaN as logprob, 0 kept.
+ * Limits: rows <= 65535, vocab in [2, 2^24].  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP.
+ */
+size_t tasc_sample_workspace_bytes(int32_t rows, int32_t vocab);   /* for tasc_filter_logits, too, with rows = batch * (k + 1) */
+tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature,
+                        const int32_t* top_k, const float* top_p, const float* min_p, const float* u, int32_t* token, float* logprob,
+                        int32_t* kept, void* workspace, size_t ws_bytes, void* stream);
+/*
+ * The same filters as masked logits: out [batch, k + 1, vocab] is logits where a token is kept, else -infinity, so tasc_accept_sampled over it, with the same
+ * temperature, verifies drafts under them.  Parameters are a sequence's ([batch]); out may be logits, with the same stride; kept
+ * int32[batch, k + 1], nullable.  A row without a distribution is passed on as it is (0 kept).  vocab, rows and errors as for tasc_sample, k in [0, TASC_MAX_K].
+ */
+tasc_status tasc_filter_logits(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab,
+                               const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, void* out,
+                               int64_t out_stride, int32_t* kept, void* workspace, size_t ws_bytes, void* stream);
+
+/*
  * Sequences that continue others (several samples of one prompt): for each pair i, sequence dst[i] gets sequence src[i]'s tokens.  Its table lists the
  * same pages, but a last page that is partly filled is replaced by new_pages[i], since both go on writing there; the copy that this asks for is copy_from[i] ->
  * copy_to[i] (tasc_pages_copy makes it), -1 for none and -2 where the pair is refused.  kv_len[dst[i]] = kv_len[src[i]], pages[dst[i]] = its pages; table entries behind them stay.

@@ -25,6 +25,7 @@ EXPORTS = [
     "tasc_page_tables", "tasc_kv4_page_bytes", "tasc_kv4_append", "tasc_kv4_read", "tasc_kv4_attention_workspace_bytes",
     "tasc_kv4_attention", "tasc_accept_sampled_workspace_bytes", "tasc_accept_sampled", "tasc_sampled_scratch_bytes",
     "tasc_verify_step_sampled", "tasc_session_rewind", "tasc_generate_sampled", "tasc_session_kv4_bytes", "tasc_session_create_kv4",
+    "tasc_sample_workspace_bytes", "tasc_sample", "tasc_filter_logits",
     "tasc_pages_fork", "tasc_pages_copy", "tasc_pages_workspace_bytes", "tasc_pages_free", "tasc_pages_compact",
 ]
 KERNEL_CLASSES = ["draft", "prepare", "norm", "gemm_qkv", "rope_kv", "attn", "gemm_o", "gemm_gu", "gemm_d", "lmhead", "accept",
@@ -150,9 +151,14 @@ def lib():
         L.tasc_session_create_kv4.argtypes = [C.c_void_p, C.c_int32, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_size_t, C.c_void_p, C.c_size_t,
                                               C.POINTER(C.c_void_p)]
         for name in ("tasc_kv4_page_bytes", "tasc_sampled_scratch_bytes", "tasc_session_kv4_bytes", "tasc_kv4_attention_workspace_bytes", "tasc_accept_sampled_workspace_bytes",
-                     "tasc_pages_workspace_bytes"):
+                     "tasc_pages_workspace_bytes", "tasc_sample_workspace_bytes"):
             getattr(L, name).restype = C.c_size_t
         L.tasc_kv4_page_bytes.argtypes = [C.c_int32] * 2
+        L.tasc_sample_workspace_bytes.argtypes = [C.c_int32] * 2
+        L.tasc_sample.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                  C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
+        L.tasc_filter_logits.argtypes = [C.c_void_p, C.c_int32, C.c_int64, C.c_int32, C.c_int32, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p,
+                                         C.c_int64, C.c_void_p, C.c_void_p, C.c_size_t, C.c_void_p]
         L.tasc_pages_workspace_bytes.argtypes = [C.c_int32]
         L.tasc_pages_fork.argtypes = [C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.c_void_p,
                                       C.c_void_p, C.c_void_p, C.c_void_p]
@@ -766,6 +772,75 @@ def tasc_accept_sampled(logits, drafts, draft_probs, temperature, u, accept_len,
         None if temperature is None else _array(who, "temperature", temperature, f32, (B,), dev), _array(who, "u", u, f32, (B, nq, 2), dev),
         _array(who, "accept_len", accept_len, i32, (B,), dev), _array(who, "emitted", emitted, i32, per_row, dev),
         None if logprob is None else _array(who, "logprob", logprob, f32, per_row, dev), ws, n, st))
+
+
+def tasc_sample_workspace_bytes(rows, vocab) -> int:
+    """For tasc_filter_logits, too, with rows = batch * (k + 1)."""
+    return lib().tasc_sample_workspace_bytes(rows, vocab)
+
+
+def _filters(who, temperature, top_k, top_p, min_p, shape, dev):
+    import torch
+    f32 = torch.float32
+    return (None if temperature is None else _array(who, "temperature", temperature, f32, shape, dev),
+            None if top_k is None else _array(who, "top_k", top_k, torch.int32, shape, dev),
+            None if top_p is None else _array(who, "top_p", top_p, f32, shape, dev),
+            None if min_p is None else _array(who, "min_p", min_p, f32, shape, dev))
+
+
+def tasc_sample(logits, u, token, temperature=None, top_k=None, top_p=None, min_p=None, logprob=None, kept=None, workspace=None, stream=None):
+    """logits: fp32 or bf16 cuda tensor [rows, vocab], a row's side by side; u fp32 [rows]; temperature, top_p, min_p fp32 and top_k int32 [rows], or None;
+    token int32, logprob fp32 and kept int32 [rows] (the last two may be None) are written in place."""
+    import torch
+    who, f32, i32 = "sample", torch.float32, torch.int32
+    dev, st, on_current = _here(stream)
+    dtype = getattr(logits, "dtype", None)
+    if (dtype is not f32 and dtype is not torch.bfloat16) or logits.ndim != 2 or logits.get_device() != dev:
+        _refuse(f"{who}: logits are not a float32 or bfloat16 tensor [rows, vocab] on cuda:{dev}, the current device")
+    rows, V = logits.shape
+    stride = V
+    if not logits.is_contiguous():
+        far, one = logits.stride()
+        stride = far if rows > 1 else V
+        if one != 1:
+            _refuse(f"{who}: the rows of logits are not side by side")
+    per = (rows,)
+    keep, ws, n = _workspace(who, workspace, 0 if workspace is not None else tasc_sample_workspace_bytes(rows, V), dev, on_current)
+    _check(lib().tasc_sample(logits.data_ptr(), TASC_F32 if dtype is f32 else TASC_BF16, stride, rows, V, *_filters(who, temperature, top_k, top_p, min_p, per, dev),
+                             _array(who, "u", u, f32, per, dev), _array(who, "token", token, i32, per, dev),
+                             None if logprob is None else _array(who, "logprob", logprob, f32, per, dev),
+                             None if kept is None else _array(who, "kept", kept, i32, per, dev), ws, n, st))
+
+
+def _evenly(who, name, t, dtype, shape, dev):
+    """(address, elements from row to row) of a tensor [batch, k + 1, vocab] whose rows are evenly spaced"""
+    if getattr(t, "dtype", None) is not dtype or t.shape != shape or t.get_device() != dev:
+        _refuse(f"{who}: {name} is not a {dtype} tensor [batch, k + 1, vocab] on cuda:{dev}, the current device")
+    B, nq, V = shape
+    if t.is_contiguous():
+        return t.data_ptr(), V
+    far, near, one = t.stride()
+    stride = near if nq > 1 else far if B > 1 else V
+    if one != 1 or (B > 1 and far != nq * stride):
+        _refuse(f"{who}: the rows of {name} are not evenly spaced")
+    return t.data_ptr(), stride
+
+
+def tasc_filter_logits(logits, out, temperature=None, top_k=None, top_p=None, min_p=None, kept=None, workspace=None, stream=None):
+    """logits, out: fp32 or bf16 cuda tensors [batch, k + 1, vocab] (both alike; they may be one), their rows evenly spaced; temperature, top_p, min_p fp32
+    and top_k int32 [batch], or None; kept int32 [batch, k + 1] or None; out and kept are written in place."""
+    import torch
+    who, f32 = "filter_logits", torch.float32
+    dev, st, on_current = _here(stream)
+    dtype = getattr(logits, "dtype", None)
+    if (dtype is not f32 and dtype is not torch.bfloat16) or logits.ndim != 3:
+        _refuse(f"{who}: logits are not a float32 or bfloat16 tensor [batch, k + 1, vocab]")
+    B, nq, V = shape = logits.shape
+    at, stride = _evenly(who, "logits", logits, dtype, shape, dev)
+    to, out_stride = _evenly(who, "out", out, dtype, shape, dev)
+    keep, ws, n = _workspace(who, workspace, 0 if workspace is not None else tasc_sample_workspace_bytes(B * nq, V), dev, on_current)
+    _check(lib().tasc_filter_logits(at, TASC_F32 if dtype is f32 else TASC_BF16, stride, B, nq - 1, V, *_filters(who, temperature, top_k, top_p, min_p, (B,), dev),
+                                    to, out_stride, None if kept is None else _array(who, "kept", kept, torch.int32, (B, nq), dev), ws, n, st))
 
 
 # ---------------------------------------------------------------- sessions that sample, sessions over a 4-bit cache

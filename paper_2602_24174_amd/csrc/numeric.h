@@ -106,3 +106,25 @@ __device__ __forceinline__ double wave_scan64_dpp(double v) {   // sums of the l
     v += lane64_dpp<0x143, 0xC>(v);                         // lane 31, into rows 2 and 3
     return v;
 }
+
+// exp(x) for x <= 1 (NaN stays one): x = n ln 2 + r, |r| <= ln 2 / 2, and the Taylor polynomial of degree 11, whose remainder is below
+// (ln 2 / 2)^12 / 12! = 6.3e-15
+__device__ __forceinline__ double exp_neg(double x) {
+    x = x < -1000.0 ? -1000.0 : x;                         // (an underflow either way; -infinity has no n)
+    const double n = rint(x * 1.4426950408889634074);
+    double r = __builtin_fma(n, -0x1.62e42fefa4000p-1, x);            // ln 2 in 40 bits, and the rest
+    r = __builtin_fma(n, 0x1.8432a1b0e2634p-43, r);
+    double p = 1.0 / 39916800.0;
+    p = __builtin_fma(p, r, 1.0 / 3628800.0);
+    p = __builtin_fma(p, r, 1.0 / 362880.0);
+    p = __builtin_fma(p, r, 1.0 / 40320.0);
+    p = __builtin_fma(p, r, 1.0 / 5040.0);
+    p = __builtin_fma(p, r, 1.0 / 720.0);
+    p = __builtin_fma(p, r, 1.0 / 120.0);
+    p = __builtin_fma(p, r, 1.0 / 24.0);
+    p = __builtin_fma(p, r, 1.0 / 6.0);
+    p = __builtin_fma(p, r, 0.5);
+    p = __builtin_fma(p, r, 1.0);
+    p = __builtin_fma(p, r, 1.0);
+    return ldexp(p, (int)n);
+}

@@ -1,0 +1,250 @@
+"""tasc_sample and tasc_filter_logits against their oracle in 64 bits: tokens and counts equal, probabilities within what their type and weights hold."""
+import numpy as np
+import pytest
+
+from oracle import filtered_sampling as OF
+
+pytestmark = pytest.mark.gpu
+
+
+def logits_of(rng, rows, vocab, kind):
+    x = rng.standard_normal((rows, vocab)) * 1.5
+    if kind == "peaked":
+        x[np.arange(rows)[:, None], rng.integers(0, vocab, (rows, min(8, vocab)))] += rng.uniform(5, 14, (rows, min(8, vocab)))
+    elif kind == "masked":
+        x[rng.random((rows, vocab)) < 0.9] = -np.inf
+        x[:, vocab // 2] = 0.0
+    elif kind == "ties":
+        x = np.round(x * 2) / 2
+    elif kind == "equal":
+        x[:] = -3.25
+    elif kind == "wide":
+        x *= 100
+    elif kind == "zeros":
+        x = np.where(rng.random((rows, vocab)) < 0.5, -0.0, 0.0)
+    return x
+
+
+def tolerance(want, vocab):
+    """fp32's half step, 64-bit functions, and the weights: each is off by half of 2^-F of the largest, F at least 61 less the vocabulary's bits"""
+    return 2.0 ** -24 * abs(want) + 1e-12 + vocab * 2.0 ** -(62 - int(vocab).bit_length())
+
+
+def settings(rng, rows):
+    """a row each with temperature, top_k, top_p and min_p"""
+    t = rng.uniform(0.3, 2.0, rows).astype(np.float32)
+    k = rng.integers(1, 100, rows).astype(np.int32)
+    p = rng.uniform(0.3, 0.98, rows).astype(np.float32)
+    m = rng.uniform(0.005, 0.3, rows).astype(np.float32)
+    i = np.arange(rows)
+    k[(i >> 0) % 2 == 1] = 0
+    p[(i >> 1) % 2 == 1] = 1.0
+    m[(i >> 2) % 2 == 1] = 0.0
+    t[i % 11 == 9] = 0.0
+    return t, k, p, m
+
+
+def dev(x):
+    import torch
+    return None if x is None else torch.tensor(x, device="cuda")
+
+
+def placed(x, dtype, pad, offset):
+    """x as a device tensor whose rows lie `pad` beyond their length apart and begin `offset` elements behind an aligned address"""
+    import torch
+    rows, vocab = x.shape
+    whole = torch.full((rows * (vocab + pad) + offset + 8,), 99.0, dtype=dtype, device="cuda")
+    view = whole[offset:offset + rows * (vocab + pad)].view(rows, vocab + pad)[:, :vocab]
+    view.copy_(torch.tensor(x, dtype=torch.float64))
+    return view, view.double().cpu().numpy()
+
+
+def check(x, u, t=None, k=None, p=None, m=None, dtype=None, pad=0, offset=0, mask=True):
+    import torch
+    import paper_2602_24174_amd as T
+    rows, vocab = x.shape
+    print(f"{rows} rows of {vocab}", flush=True)
+    logits, seen = placed(x, dtype or torch.float32, pad, offset)
+    token, kept = (torch.full((rows + 3,), -9, dtype=torch.int32, device="cuda") for _ in range(2))
+    logp = torch.full((rows + 3,), -9.0, device="cuda")
+    T.tasc_sample(logits, dev(u), token[:rows], dev(t), dev(k), dev(p), dev(m), logp[:rows], kept[:rows])
+    assert (token[rows:] == -9).all() and (kept[rows:] == -9).all() and (logp[rows:] == -9).all()
+    per = [(1.0 if t is None else t[r], 0 if k is None else k[r], 1.0 if p is None else p[r], 0.0 if m is None else m[r]) for r in range(rows)]
+    for r in range(rows):
+        want = OF.sample(seen[r], u[r], *per[r])
+        got = int(token[r]), float(logp[r]), int(kept[r])
+        assert got[0] == want[0] and got[2] == want[2], (r, got, want, per[r])
+        assert (np.isnan(want[1]) and np.isnan(got[1])) or abs(got[1] - want[1]) <= tolerance(want[1], vocab), (r, got, want, per[r])
+    if not mask:
+        return
+    out, before = torch.full((rows, 1, vocab + 5), 77.0, dtype=logits.dtype, device="cuda"), logits.clone()
+    T.tasc_filter_logits(logits[:, None], out[:, :, :vocab], dev(t), dev(k), dev(p), dev(m), kept[:rows, None].contiguous())
+    assert (out[:, :, vocab:] == 77.0).all() and torch.equal(logits.nan_to_num(5.0), before.nan_to_num(5.0))
+    left = [OF.masked(seen[r], *per[r]) for r in range(rows)]
+    for r in range(rows):
+        assert np.array_equal(out[r, 0, :vocab].double().cpu().numpy(), left[r][0], equal_nan=True), (r, per[r])
+    counts = torch.full((rows, 1), -9, dtype=torch.int32, device="cuda")
+    T.tasc_filter_logits(logits[:, None], logits[:, None], dev(t), dev(k), dev(p), dev(m), counts)        # in place
+    assert torch.equal(logits.nan_to_num(5.0), out[:, 0, :vocab].nan_to_num(5.0))
+    assert counts[:, 0].tolist() == [n for _, n in left]
+
+
+@pytest.mark.parametrize("kind", ["peaked", "flat", "masked", "ties", "equal", "wide", "zeros"])
+@pytest.mark.parametrize("rows, vocab, dtype, pad, offset", [(16, 500, "f32", 0, 0), (24, 2, "f32", 0, 0), (24, 3, "bf16", 1, 1), (16, 4096, "bf16", 0, 0), (16, 4097, "f32", 3, 0),
+                                                             (16, 9999, "bf16", 1, 3), (16, 32000, "f32", 0, 0), (16, 50257, "f32", 0, 2), (8, 151936, "bf16", 0, 0),
+                                                             (8, 151936, "f32", 0, 0)])
+def test_settings(rows, vocab, dtype, pad, offset, kind):
+    import torch
+    rng = np.random.default_rng(vocab + len(kind))
+    x = logits_of(rng, rows, vocab, kind)
+    check(x, rng.random(rows).astype(np.float32), *settings(rng, rows), dtype=torch.bfloat16 if dtype == "bf16" else torch.float32, pad=pad, offset=offset)
+
+
+def test_defaults_and_one_at_a_time():
+    rng = np.random.default_rng(3)
+    x = logits_of(rng, 12, 7001, "peaked")
+    u = rng.random(12).astype(np.float32)
+    t, k, p, m = (a.copy() for a in settings(rng, 12))
+    k[:], p[:], m[:] = rng.integers(1, 3000, 12), rng.uniform(0.1, 0.999, 12), rng.uniform(1e-4, 1, 12)
+    check(x, u)
+    for kw in (dict(t=t), dict(k=k), dict(p=p), dict(m=m), dict(k=k, p=p), dict(k=k, m=m), dict(p=p, m=m), dict(k=k, p=p, m=m)):
+        check(x, u, **kw)
+
+
+def test_parameters_at_the_ends():
+    inf, nan = np.inf, np.nan
+    f = lambda *v: np.array(v, dtype=np.float32)
+    rng = np.random.default_rng(4)
+    x = logits_of(rng, 8, 6000, "peaked")
+    u = f(0, 0.25, 0.5, 1 - 2 ** -24, 0, 0.75, 1 - 2 ** -24, 0.1)
+    check(x, u, t=f(0, inf, 1e-6, 1e6, -1, nan, -0.0, 1e-45))
+    check(x, u, t=f(inf, inf, 1e30, 1e-30, 1, 1, 0.01, 100), k=np.array([5, 0, 7, 9, 6000, 5999, 6001, -1], dtype=np.int32))
+    check(x, u, p=f(0, -1, 1, 2, nan, 1e-30, 1 - 2 ** -24, inf))
+    check(x, u, m=f(0, -1, 1, 2, nan, 1e-30, 1 - 2 ** -24, inf))
+    check(x, u, t=f(inf, inf, inf, inf, 0, 0, 0, 0), p=f(0.5, 0.25, 1, 0, 0.5, 1, 0, 0.9), m=f(0, 0.5, 1, 1, 0.1, 0, 1, 0.5), k=np.array([0, 9, 100, 3, 9, 0, 2, 1], dtype=np.int32))
+    check(x, u, k=np.array([2 ** 31 - 1, -2 ** 31, 1, 2, 3, 2047, 2048, 2049], dtype=np.int32))
+    check(x, u, k=np.array([4100, 3000, 5000, 2500, 5990, 4096, 4095, 4097], dtype=np.int32), p=f(0.9, 0.99, 0.5, 0.7, 0.95, 1, 0.8, 0.6), t=f(9, 8, 7, 6, 5, 4, 3, 2))
+
+
+def test_rows_without_a_distribution():
+    inf, nan = np.inf, np.nan
+    x = np.zeros((7, 5000))
+    x[0, 4999], x[1, 17], x[2, :], x[4, :], x[5, 3], x[5, 4] = nan, inf, -inf, -inf, inf, nan
+    x[4, 77] = 3e38
+    x[6, 0], x[6, 1] = 3.4e38, -3.4e38
+    for kw in (dict(), dict(k=np.full(7, 3, dtype=np.int32), p=np.full(7, 0.5, dtype=np.float32), m=np.full(7, 0.5, dtype=np.float32))):
+        check(x, np.full(7, 0.6, dtype=np.float32), **kw)
+
+
+def test_the_largest_vocabulary():
+    """2^24 tokens, ties of thousands in a bin: found token by token, and by halves of their indices where they are one logit"""
+    import torch
+    rng = np.random.default_rng(6)
+    vocab = 1 << 24
+    x = rng.standard_normal((4, vocab)).astype(np.float32) * 2
+    x[3] = 1.5
+    x[3, 5::7] = 1.25
+    x[2] = np.round(x[2])
+    f = lambda *v: np.array(v, dtype=np.float32)
+    check(x, f(0.3, 0.9, 0.5, 0.77), t=f(1, 0.7, 1.3, 1), p=f(0.6, 0.9, 0.4, 0.5), mask=False)
+    check(x, f(0.3, 0.9, 0.5, 0.77), k=np.array([50, 100000, 3000000, 14380000], dtype=np.int32), p=f(1, 0.5, 0.3, 0.7))
+    check(x[:2], f(0.1, 0.99), m=f(0.0001, 0.5), dtype=torch.bfloat16, mask=False)
+
+
+def test_a_row_is_its_own():
+    """A row's bits depend on neither the other rows nor their number"""
+    import torch
+    import paper_2602_24174_amd as T
+    rng = np.random.default_rng(8)
+    rows, vocab = 300, 40000
+    x, u = dev(logits_of(rng, rows, vocab, "peaked").astype(np.float32)), dev(rng.random(rows).astype(np.float32))
+    t, k, p, m = (dev(a) for a in settings(rng, rows))
+
+    def run(at):
+        n = len(at)
+        token, kept, logp = torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, dtype=torch.int32, device="cuda"), torch.zeros(n, device="cuda")
+        T.tasc_sample(x[at], u[at], token, t[at], k[at], p[at], m[at], logp, kept)
+        return torch.stack([token, kept, logp.view(torch.int32)])
+
+    whole = run(torch.arange(rows, device="cuda"))
+    assert torch.equal(whole, run(torch.arange(rows, device="cuda")))
+    for at in ([7], [299, 3], list(range(17, 90))):
+        assert torch.equal(run(torch.tensor(at, device="cuda")), whole[:, at])
+
+
+def test_drafts_verified_under_the_filters():
+    """tasc_filter_logits, then tasc_accept_sampled over what it leaves, for sequences of nine rows: as the oracles have it"""
+    import torch
+    import paper_2602_24174_amd as T
+    from oracle import sampled_acceptance as OS
+    rng = np.random.default_rng(9)
+    B, k, V = 6, 8, 5003
+    x = logits_of(rng, B * (k + 1), V, "peaked").astype(np.float32)
+    t, tk, p, m = settings(rng, B)
+    t[0] = 0.7
+    drafts = x.reshape(B, k + 1, V)[:, :k].argmax(-1).astype(np.int32)
+    drafts[2, 3], drafts[4, 1] = 11, -1
+    u = rng.random((B, k + 1, 2)).astype(np.float32)
+    logits, out = dev(x.reshape(B, k + 1, V)), torch.empty((B, k + 1, V), device="cuda")
+    kept, n, emitted = torch.zeros((B, k + 1), dtype=torch.int32, device="cuda"), torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros((B, k + 1), dtype=torch.int32, device="cuda")
+    T.tasc_filter_logits(logits, out, dev(t), dev(tk), dev(p), dev(m), kept)
+    T.tasc_accept_sampled(out, dev(drafts), None, dev(t), dev(u), n, emitted)
+    want = np.empty_like(x)
+    for r in range(B * (k + 1)):
+        b = r // (k + 1)
+        want[r], count = OF.masked(x[r], t[b], tk[b], p[b], m[b])
+        assert int(kept.view(-1)[r]) == count
+    want = want.reshape(B, k + 1, V)
+    assert np.array_equal(out.cpu().numpy(), want)
+    for b in range(B):
+        got = OS.accept(want[b], drafts[b], None, t[b], u[b])
+        assert int(n[b]) == got[0] and emitted[b].tolist() == list(got[1]) + [-1] * (k + 1 - len(got[1]))
+
+
+def test_replayed_and_on_another_stream():
+    import torch
+    import paper_2602_24174_amd as T
+    rng = np.random.default_rng(10)
+    rows, vocab = 6, 20001
+    x, u = torch.zeros((rows, vocab), device="cuda"), torch.zeros(rows, device="cuda")
+    t, k, p, m = settings(rng, rows)
+    params = dev(t), dev(k), dev(p), dev(m)
+    token, kept, logp = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, device="cuda")
+    out = torch.zeros((rows, 1, vocab), device="cuda")
+    ws = [torch.empty(T.tasc_sample_workspace_bytes(rows, vocab), dtype=torch.uint8, device="cuda") for _ in range(2)]
+
+    def step():
+        T.tasc_sample(x, u, token, *params, logp, kept, ws[0])
+        T.tasc_filter_logits(x[:, None], out, *params, None, ws[1])
+
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for kind in ("peaked", "flat", "ties", "peaked"):
+        new = logits_of(rng, rows, vocab, kind).astype(np.float32)
+        x.copy_(dev(new))
+        u.copy_(dev(rng.random(rows).astype(np.float32)))
+        graph.replay()
+        torch.cuda.synchronize()
+        replayed = token.tolist(), kept.tolist(), logp.tolist()
+        for r in range(rows):
+            want = OF.sample(new[r], float(u[r]), t[r], k[r], p[r], m[r])
+            assert (replayed[0][r], replayed[1][r]) == (want[0], want[2])
+            assert np.array_equal(out[r, 0].cpu().numpy(), OF.masked(new[r], t[r], k[r], p[r], m[r])[0])
+        token.zero_()
+        step()
+        torch.cuda.synchronize()
+        assert (token.tolist(), kept.tolist(), logp.tolist()) == replayed
+
+
+def test_no_rows():
+    import torch
+    import paper_2602_24174_amd as T
+    none = torch.zeros(0, dtype=torch.int32, device="cuda")
+    T.tasc_sample(torch.zeros((0, 50), device="cuda"), torch.zeros(0, device="cuda"), none)
+    T.tasc_filter_logits(torch.zeros((0, 3, 50), device="cuda"), torch.zeros((0, 3, 50), device="cuda"))
