@@ -3,19 +3,39 @@
 // A row's tokens in the order of their logits (equal ones by index) are whole numbers of 56 bits, `comp`: the logit's bits, turned so that
 // the largest comes first, over the index.  Every filter keeps a prefix of that order, so all of them together come to one last comp, `cut`.
 //
-// A prefix is found by a histogram over the values, 4096 bins between the largest logit and the least: of counts for top-k, of weights for
-// top-p.  The bin in which the prefix ends then has few tokens, which are gathered, sorted and summed one by one.  A bin of more than fits
-// (ties of thousands, a vocabulary of millions) is cut into 4096 again, by comp, until one token is left.
+// Three kernels.  k_filter_parts reads every logit once, a workgroup 16384 of them: the largest, the sum of the weights where it is wanted, and a list of
+// those above a bound that it takes from a sample, about 1500 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always
+// the cut lies in them.  Where it does not (flat distributions, ties of thousands, a top-k of thousands) k_filter_wide, a larger workgroup a row, finds it
+// from the row itself: a histogram over the values, 4096 bins between the largest logit and the least, of counts for top-k and of weights for
+// top-p; the bin in which the prefix ends has few tokens, which are gathered, sorted and summed one by one, or is cut into 4096 again, by comp, until
+// one token is left.  Rows of up to kList tokens are their own list and need one launch.
 //
 // Weights are sums of whole numbers, which no order of the work changes: a bin's of 2^-F of the weight at its middle, so that a bin far from the
-// largest is as exact as one next to it, a list's and the draw's of 2^-F of the largest.
+// largest is as exact as one next to it, a list's and the draw's of 2^-F of the largest.  Sums over whole rows are fp64 in a fixed order.
 #include "numeric.h"
 #include <algorithm>
+#include <math.h>
 
 namespace {
 
-constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096, kList = 2048;
-constexpr int kListBits = 50;                              // a list's weights: 2^11 of them stay below 2^62
+constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096, kWideList = 2048;
+constexpr int kListBits = 50;                              // a list's weights: 2^12 of them stay below 2^62
+// a workgroup of k_filter_parts, its waves' shares; lists of a row together, and entries that k_filter_finish takes
+constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPer = 16, kStep = 64 * kPer;
+constexpr int kPart = 16384, kMostParts = 64, kList = 4096, kGroups = 64;
+constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64;
+
+// What a part of a row comes to
+struct __attribute__((aligned(16))) Part {
+    double sum, scale;               // sum of the weights in units of exp(scale), if has_sum
+    float top, bound;                // the largest logit; the lists hold all logits from bound on (infinity: they are not whole)
+    int32_t live, bad;               // tokens that are not masked; a NaN or an infinity among the logits
+    int32_t listed[kPartWaves];
+    int32_t has_sum, pad[3];
+};
+// and a row: kept are the tokens up to `cut`
+enum { ROW_DONE = 0, ROW_WIDE = 1, ROW_BAD = 2 };
+struct RowOut { u64 cut; int32_t state, pad; };
 
 struct FilterArgs {
     const void* logits;
@@ -31,6 +51,13 @@ struct FilterArgs {
     int32_t* kept;
     void* out;                       // filtering
     int64_t out_stride;
+    Part* parts;                     // [rows, n_parts]
+    u64* lists;                      // [rows, n_parts, kPartWaves, list_len]
+    RowOut* rows;                    // [rows]
+    int32_t n_parts, part_len, list_len;
+    int32_t sample_len, sample_rank; // the bound: of 64 groups' largest logits, 16 * sample_len each, the one with so many of them above or at it
+    int32_t direct;                  // rows are their own lists
+    int32_t in_place, out_aligned;   // out_aligned: rows to write begin at multiples of 16 bytes
 };
 
 __device__ __forceinline__ u32 key_of(float x) {           // grows with x; -0 is 0
@@ -41,6 +68,23 @@ __device__ __forceinline__ float from_key(u32 s) { return __uint_as_float(s & 0x
 __device__ __forceinline__ u64 comp_of(float x, int v) { return (u64)~key_of(x) << 24 | (u32)v; }
 __device__ __forceinline__ float logit_of(u64 comp) { return from_key(~(u32)(comp >> 24)); }
 __device__ __forceinline__ int token_of(u64 comp) { return (int)(comp & 0xFFFFFF); }
+
+// A row's parameters: the first alone; by count; by mass; by the largest's share
+struct Params { double inv; float p, m; int k; bool good, one, by_count, by_mass, by_share; };
+__device__ __forceinline__ Params params_of(const FilterArgs& a, int b) {
+    const float t = a.temperature ? a.temperature[b] : 1.f;
+    Params o;
+    o.p = a.top_p ? a.top_p[b] : 1.f;
+    o.m = a.min_p ? a.min_p[b] : 0.f;
+    o.k = a.top_k ? a.top_k[b] : 0;
+    o.good = t >= 0.f && o.p == o.p && o.m == o.m;
+    o.inv = t > 0.f ? 1.0 / (double)t : 1.0;
+    o.one = t == 0.f || o.p <= 0.f || o.m > 1.f || o.k == 1;
+    o.by_count = !o.one && o.k > 0 && o.k < a.vocab;
+    o.by_mass = !o.one && o.p < 1.f;
+    o.by_share = !o.one && o.m > 0.f;
+    return o;
+}
 
 __device__ __forceinline__ u64 wave_sum_u64(u64 v) {
     for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
@@ -83,7 +127,7 @@ struct RowLoop {
 };
 
 struct __attribute__((aligned(16))) Shared {
-    u64 big[kBins];                  // a histogram; lists of kList; segments of the draw
+    u64 big[kBins];                  // a histogram; lists of kWideList; segments of the draw
     double sum[kWaves];
     u64 whole[kWaves];
     int32_t num[4][kWaves];
@@ -131,8 +175,8 @@ __device__ __forceinline__ u64 weight_of(const RowState& r, float x, int bits) {
 }
 // The least key for which a condition holds that holds from some key up to the largest logit's: 64 of them at a time
 template <typename F>
-__device__ __forceinline__ u32 first_key(const RowState& r, int lane, F holds) {
-    const u32 most = key_of(r.top), none = key_of(-__builtin_inff());
+__device__ __forceinline__ u32 first_key(float top, int lane, F holds) {
+    const u32 most = key_of(top), none = key_of(-__builtin_inff());
     u32 base = 0;
     for (int shift = 30; shift >= 0; shift -= 6) {
         const u64 at = (u64)base + ((u64)lane << shift);
@@ -310,10 +354,10 @@ struct Row {
         const int b = last_below(s, tid, [&](int i) { return UNIT ? (double)s.big[i] : (double)s.big[i] * unit * exp_neg(-i * r.bin_width); },
                                  [&](double total) { return end = limit(total); }, before);
         // the bin's tokens, and all up to them
-        const u32 lo = first_key(r, lane, [&](float x) { return bin_of(r, x).at <= b; });
-        const u32 hi = b == 0 ? key_of(__builtin_inff()) : first_key(r, lane, [&](float x) { return bin_of(r, x).at < b; });
+        const u32 lo = first_key(r.top, lane, [&](float x) { return bin_of(r, x).at <= b; });
+        const u32 hi = b == 0 ? key_of(__builtin_inff()) : first_key(r.top, lane, [&](float x) { return bin_of(r, x).at < b; });
         const float x_lo = from_key(lo), x_hi = from_key(hi);
-        u64 *const all = s.big, *const own = s.big + kList;
+        u64 *const all = s.big, *const own = s.big + kWideList;
         if (tid < 2) s.count[tid] = 0;
         __syncthreads();
         int above = 0;
@@ -323,7 +367,7 @@ struct Row {
             int at = 0;
             if (lane == 0) at = atomicAdd(&s.count[which], __popcll(m));
             at = __builtin_amdgcn_readfirstlane(at) + __popcll(m & ((1ull << lane) - 1));
-            if (in && at < kList) list[at] = comp_of(x, v);
+            if (in && at < kWideList) list[at] = comp_of(x, v);
         };
         Loop::run(row, vocab, tid, [&](const float* x, int v) {
 #pragma unroll
@@ -337,14 +381,14 @@ struct Row {
         above = block_count(s, above, tid);
         const int n_all = s.count[0], n_own = s.count[1];
         __syncthreads();
-        if (n_all <= kList) {
+        if (n_all <= kWideList) {
             sort_list(all, n_all, tid);
             r.listed = n_all;
             const double scale = 0x1p50;
             static_assert(kListBits == 50);
             r.kept = UNIT ? (int)fmin(end, (double)n_all) : list_below(s, r, all, n_all, tid, [&](double) { return end * scale; });
             r.cut = all[r.kept - 1];
-        } else if (n_own <= kList) {
+        } else if (n_own <= kWideList) {
             sort_list(own, n_own, tid);
             const int n = UNIT ? (int)fmin(end - before, (double)n_own) : list_below(s, r, own, n_own, tid, [&](double) { return (end - before) * 0x1p50; });
             r.kept = above + n;
@@ -401,7 +445,7 @@ struct Row {
 
     // the token that u falls on, and ln of its share
     __device__ int draw(float u, float& logp) {
-        u64* const seg = s.big + kList;
+        u64* const seg = s.big + kWideList;
         const bool from_list = r.listed >= 0;
         const int bits = from_list ? kListBits : r.bits;
         const float cut_x = logit_of(r.cut);
@@ -471,56 +515,52 @@ struct Row {
 };
 
 template <typename T, bool VEC, bool MASK>
-__global__ __launch_bounds__(kThreads) void k_filter_rows(FilterArgs a) {
+__global__ __launch_bounds__(kThreads) void k_filter_wide(FilterArgs a) {
     __shared__ Shared s;
     const int i = blockIdx.x, b = i / a.per, tid = threadIdx.x;
+    if (a.rows[i].state != ROW_WIDE) return;
+    const Params q = params_of(a, b);
     Row<T, VEC> row{(const T*)a.logits + (int64_t)i * a.row_stride, a.vocab, tid, tid & 63, tid >> 6, s, RowState{}};
     RowState& r = row.r;
-    const float t = a.temperature ? a.temperature[b] : 1.f, p = a.top_p ? a.top_p[b] : 1.f, m = a.min_p ? a.min_p[b] : 0.f;
-    int k = a.top_k ? a.top_k[b] : 0;
-    bool good = row.look();
-    good = good && t >= 0.f && p == p && m == m;
-    int token = -1;
-    float logp = __builtin_nanf("");
-    r.kept = 0;
-    if (good) {
-        if (t == 0.f || p <= 0.f || m > 1.f) k = 1;         // the first alone
-        r.inv = t > 0.f ? 1.0 / (double)t : 1.0;
-        const double range = (double)r.top - (double)r.least;
-        r.per_unit = fmax(64.0 * r.inv, range > 0.0 ? (kBins - 1.5) / range : 1.0);
-        r.bin_width = r.inv / r.per_unit;
-        r.bits = min(50, 61 - (32 - __clz(a.vocab)));
-        r.cut = (u64)~key_of(r.least) << 24 | 0xFFFFFF;
-        r.kept = r.live;
-        r.listed = -1;
-        const bool by_mass = p > 0.f && p < 1.f && k != 1;
-        if (k > 0 && k < r.live) row.template select<true>([&](double) { return (double)k; });
-        if (by_mass) {
-            if (r.listed >= 0) {
-                r.kept = list_below(s, r, s.big, r.kept, tid, [&](double total) { return (double)p * total; });
-                r.cut = s.big[r.kept - 1];
-            } else {
-                row.template select<false>([&](double total) { return (double)p * total; });
-            }
+    row.look();
+    r.inv = q.inv;
+    const double range = (double)r.top - (double)r.least;
+    r.per_unit = fmax(64.0 * r.inv, range > 0.0 ? (kBins - 1.5) / range : 1.0);
+    r.bin_width = r.inv / r.per_unit;
+    r.bits = min(50, 61 - (32 - __clz(a.vocab)));
+    r.cut = (u64)~key_of(r.least) << 24 | 0xFFFFFF;
+    r.kept = r.live;
+    r.listed = -1;
+    const int k = q.one ? 1 : q.by_count ? q.k : r.live;
+    if (k < r.live) row.template select<true>([&](double) { return (double)k; });
+    if (q.by_mass) {
+        if (r.listed >= 0) {
+            r.kept = list_below(s, r, s.big, r.kept, tid, [&](double total) { return (double)q.p * total; });
+            r.cut = s.big[r.kept - 1];
+        } else {
+            row.template select<false>([&](double total) { return (double)q.p * total; });
         }
-        if (m > 0.f && m <= 1.f && k != 1) {
-            const double most = -log((double)m);
-            row.at_least(first_key(r, tid & 63, [&](float x) { return ((double)r.top - (double)x) * r.inv <= most; }));
-        }
-        if (!MASK) token = row.draw(a.u[i], logp);
     }
+    if (q.by_share) {
+        const double most = -log((double)q.m);
+        row.at_least(first_key(r.top, tid & 63, [&](float x) { return ((double)r.top - (double)x) * r.inv <= most; }));
+    }
+    int token = -1;
+    float logp = 0.f;
     if (MASK) {
-        const float cut_x = good ? logit_of(r.cut) : 0.f;
-        const int cut_v = good ? token_of(r.cut) : 0;
+        const float cut_x = logit_of(r.cut);
+        const int cut_v = token_of(r.cut);
         int kept = 0;
         T* const out = (T*)a.out + (int64_t)i * a.out_stride;
         for (int v = tid; v < a.vocab; v += kThreads) {
             const T x = row.row[v];
-            const bool in = good && row.is_kept(to_f(x), v, cut_x, cut_v);
+            const bool in = row.is_kept(to_f(x), v, cut_x, cut_v);
             kept += in;
-            out[v] = in || !good ? x : from_f<T>(-__builtin_inff());
+            out[v] = in ? x : from_f<T>(-__builtin_inff());
         }
         if (r.kept < 0) r.kept = block_count(s, kept, tid);
+    } else {
+        token = row.draw(a.u[i], logp);
     }
     if (tid != 0) return;
     if (a.kept) a.kept[i] = r.kept;
@@ -529,10 +569,514 @@ __global__ __launch_bounds__(kThreads) void k_filter_rows(FilterArgs a) {
     if (a.logprob) a.logprob[i] = logp;
 }
 
+// ---------------------------------------------------------------- one read of every logit
+// A wave has a run of its own, 16 logits a lane at a time.  The first of them are the sample: of groups of 16 to 64 logits the largest, and of these 64 one
+// by its rank, which about 1500 / vocab of all logits exceed; the sum's units come from the sample's largest, too.
+template <typename T, bool VEC>
+struct Run {
+    static constexpr int SIDE = VEC ? 16 / (int)sizeof(T) : 1;
+    static __device__ __forceinline__ int place(int e, int lane) { return (e / SIDE * 64 + lane) * SIDE + e % SIDE; }
+    static __device__ __forceinline__ void load(const T* __restrict__ row, int v0, int end, int lane, float (&x)[kPer]) {
+#pragma unroll
+        for (int e = 0; e < kPer; e += SIDE) {
+            const int v = v0 + place(e, lane);
+            if (VEC && v + SIDE <= end) {
+                load_n<SIDE == 1 ? 4 : SIDE>(row + v, x + e);
+            } else {
+#pragma unroll
+                for (int f = 0; f < SIDE; ++f) x[e + f] = v + f < end ? to_f(row[v + f]) : -__builtin_inff();
+            }
+        }
+    }
+};
+__device__ __forceinline__ float row16_max(float v) {      // of 16 lanes side by side, in all of them
+    auto up = [](float x, auto ctrl) { return fmaxf(x, __builtin_bit_cast(float, __builtin_amdgcn_update_dpp(0, __builtin_bit_cast(int, x), decltype(ctrl)::value, 0xF, 0xF, false))); };
+    v = up(v, std::integral_constant<int, 0xB1>{});
+    v = up(v, std::integral_constant<int, 0x4E>{});
+    v = up(v, std::integral_constant<int, 0x141>{});
+    return up(v, std::integral_constant<int, 0x140>{});
+}
+
+template <typename T, bool VEC, bool FILL>
+__global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
+    using R = Run<T, VEC>;
+    __shared__ word2 s_pow[256];
+    __shared__ float s_group[kGroups];
+    __shared__ float s_bound;
+    __shared__ double s_sum[kPartWaves];
+    __shared__ float s_top[kPartWaves];
+    __shared__ int32_t s_live[kPartWaves], s_bad[kPartWaves], s_listed[kPartWaves];
+    const int i = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
+    const int p0 = part * a.part_len, run = a.part_len / kPartWaves, v_begin = min(p0 + wave * run, a.vocab), v_end = min(v_begin + run, a.vocab);
+    float next[kPer];
+    R::load(row, v_begin, v_end, lane, next);
+    s_pow[tid] = kPow.at[tid];
+    const Params q = params_of(a, i / a.per);
+    const bool all = !FILL && !a.in_place && !q.one && !q.by_count && !q.by_mass && !q.by_share;      // nothing is dropped: no list
+    const bool want_sum = all || (q.by_mass && !q.by_count);
+    // the sample
+    static_assert(kPer == 16 && kGroups == 4 * 4 * kPartWaves);
+#pragma unroll
+    for (int g = 0; g < 4; ++g) {
+        float m = next[4 * g];
+        if (a.sample_len > 1) m = fmaxf(m, next[4 * g + 1]);
+        if (a.sample_len > 2) m = fmaxf(fmaxf(m, next[4 * g + 2]), next[4 * g + 3]);
+        m = row16_max(m);
+        if ((lane & 15) == 0) s_group[wave * 16 + g * 4 + lane / 16] = m;
+    }
+    __syncthreads();
+    const float group = s_group[lane];
+    const float anchor = wave_max_dpp(group);
+    if (wave == 0) {
+        int above = 0;                                      // groups before this one in descending order
+#pragma unroll 16
+        for (int g = 0; g < kGroups; ++g) {
+            const float x = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, group), g));
+            above += x > group || (x == group && g < lane);
+        }
+        if (above == (q.one ? 0 : a.sample_rank - 1)) s_bound = group;
+    }
+    __syncthreads();
+    // (a NaN among the sample leaves the bound to chance; the row is refused all the same)
+    const float bound = all ? __builtin_inff() : s_bound;
+    const double unit = q.inv * 369.3299304675746;          // 256 / ln 2
+    const double whole = anchor > -__builtin_inff() && anchor < __builtin_inff() ? rint((double)anchor * unit) : 0.0, start = 0x1.8p52 - whole;
+    const bool sums = want_sum && q.good && q.inv > 1e-20 && fabs(whole) < 0x1p24;
+    const float lowest = sums ? (float)((whole - 200000.0) / unit) : 0.f;       // 2^-781: a masked logit's weight is none
+    const int64_t list = (((int64_t)i * a.n_parts + part) * kPartWaves + wave) * a.list_len;
+    T* const out = FILL ? (T*)a.out + (int64_t)i * a.out_stride : nullptr;
+    float top = -__builtin_inff();
+    double sum = 0.0;
+    int listed = 0, live = 0;
+    bool bad = false;
+    for (int v0 = v_begin; v0 < v_end; v0 += kStep) {
+        float x[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) x[e] = next[e];
+        if (v0 + kStep < v_end) R::load(row, v0 + kStep, v_end, lane, next);
+        if (FILL) {
+#pragma unroll
+            for (int e = 0; e < kPer; e += R::SIDE) {
+                const int v = v0 + R::place(e, lane);
+                constexpr u32 none = sizeof(T) == 4 ? 0xFF800000u : 0xFF80FF80u;
+                if (VEC && a.out_aligned && v + R::SIDE <= v_end) *(uint4*)(out + v) = uint4{none, none, none, none};
+                else
+#pragma unroll
+                    for (int f = 0; f < R::SIDE; ++f)
+                        if (v + f < v_end) out[v + f] = from_f<T>(-__builtin_inff());
+            }
+        }
+        float most = x[0];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            bad |= !(x[e] < __builtin_inff());
+            live += __popcll(__ballot(x[e] > -__builtin_inff()));
+            most = fmaxf(most, x[e]);
+        }
+        top = fmaxf(top, most);
+        if (sums) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                const double y = (double)fmaxf(x[e], lowest), big = __builtin_fma(y, unit, start);
+                sum = times_power(s_pow, small_power(__builtin_fma(y, unit, start - big)), (u32)__builtin_bit_cast(u64, big), sum);
+            }
+        }
+        if (!__any(most >= bound)) continue;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) {
+            const bool in = x[e] >= bound && x[e] > -__builtin_inff();
+            const u64 m = __ballot(in);
+            if (!m) continue;
+            const int at = listed + __builtin_amdgcn_mbcnt_hi((u32)(m >> 32), __builtin_amdgcn_mbcnt_lo((u32)m, 0));
+            if (in && at < a.list_len) a.lists[list + at] = comp_of(x[e], v0 + R::place(e, lane));
+            listed += __popcll(m);
+        }
+    }
+    sum = wave_sum64_dpp(sum);
+    top = wave_max_dpp(top);
+    if (lane == 0) {
+        s_sum[wave] = sum;
+        s_top[wave] = top;
+        s_live[wave] = live;
+        s_listed[wave] = listed;
+    }
+    const bool any_bad = __any(bad);
+    if (lane == 0) s_bad[wave] = any_bad;
+    __syncthreads();
+    if (tid != 0) return;
+    Part o{};
+    o.top = fmaxf(fmaxf(s_top[0], s_top[1]), fmaxf(s_top[2], s_top[3]));
+    o.sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
+    o.scale = whole * (0.69314718055994530942 / 256);
+    o.bound = bound;
+    for (int w = 0; w < kPartWaves; ++w) {
+        o.live += s_live[w];
+        o.bad |= s_bad[w];
+        o.listed[w] = min(s_listed[w], a.list_len);
+        if (s_listed[w] > a.list_len) o.bound = __builtin_inff();
+    }
+    // (weights up to 2^781 of the sample's largest: beyond that the sum says nothing)
+    o.has_sum = sums && ((double)o.top - (double)anchor) * unit < 200000.0;
+    if (o.live == 0) o.has_sum = 1, o.sum = 0.0, o.scale = -__builtin_inf();
+    a.parts[(int64_t)i * a.n_parts + part] = o;
+}
+
+// ---------------------------------------------------------------- a row from its lists
+struct __attribute__((aligned(16))) FinishShared {
+    u64 list[kList];
+    u64 bins[kFinishBins];
+    u64 few_key[kFew], few_q[kFew];
+    u64 red[kFinishWaves];
+    int32_t num[kFinishWaves], few, n, bad;
+};
+struct Found { u64 key, sum; };      // sum: up to it and with it
+
+// Of n items with weights q (0: not there), in the order of their keys within [lo, hi]: the last whose sum of those before it is below `limit`
+template <typename Key, typename Weight>
+__device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 hi, u64 limit, int tid, Key key, Weight weight) {
+    const int lane = tid & 63;
+    u64 sum = 0;
+    for (;;) {
+        int shift = 0;
+        while ((hi - lo) >> shift >= kFinishBins) ++shift;
+        __syncthreads();                                    // (bins and few are still looked at)
+        for (int i = tid; i < kFinishBins; i += kFinishThreads) s.bins[i] = 0;
+        if (tid == 0) s.few = 0;
+        __syncthreads();
+        for (int i = tid; i < n; i += kFinishThreads) {
+            const u64 c = key(i);
+            if (c < lo || c > hi) continue;
+            const u64 q = weight(i);
+            if (q) atomicAdd(&s.bins[(c - lo) >> shift], q);
+        }
+        __syncthreads();
+        // every wave for itself, 8 bins a lane
+        constexpr int PER = kFinishBins / 64;
+        u64 v[PER], mine = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) mine += v[e] = s.bins[PER * lane + e];
+        const u64 up = wave_scan_u64(mine, lane);
+        u64 at = up - mine, before = 0, own = 0;
+        int last = -1;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if (v[e] && at < limit) {
+                last = PER * lane + e;
+                before = at;
+                own = v[e];
+            }
+            at += v[e];
+        }
+        const u64 have = __ballot(last >= 0);               // (the first item's bin has nothing before it: none only where there are no items)
+        if (!have) return Found{lo, sum};
+        const int from = 63 - __clzll(have);
+        const int b = __builtin_amdgcn_readlane(last, from);
+        before = of_lane(before, from);
+        own = of_lane(own, from);
+        sum += before;
+        limit -= before;
+        lo += (u64)b << shift;
+        hi = min(hi, lo + ((1ull << shift) - 1));
+        if (shift == 0) return Found{lo, sum + own};
+        for (int i = tid; i < n; i += kFinishThreads) {
+            const u64 c = key(i);
+            if (c < lo || c > hi) continue;
+            const u64 q = weight(i);
+            if (!q) continue;
+            const int place = atomicAdd(&s.few, 1);
+            if (place < kFew) {
+                s.few_key[place] = c;
+                s.few_q[place] = q;
+            }
+        }
+        __syncthreads();
+        const int few = s.few;
+        if (few > kFew) continue;
+        const u64 c = lane < few ? s.few_key[lane] : ~0ull, q = lane < few ? s.few_q[lane] : 0;
+        u64 below = 0;
+        for (int j = 0; j < few; ++j) below += of_lane(c, j) < c ? of_lane(q, j) : 0;
+        // the largest key among those that are kept
+        u64 best = lane < few && below < limit ? c : 0;
+        for (int o = 32; o > 0; o >>= 1) best = max(best, (u64)__shfl_xor(best, o));
+        const int l = __ffsll((unsigned long long)__ballot(lane < few && c == best)) - 1;
+        return Found{best, sum + of_lane(below, l) + of_lane(q, l)};
+    }
+}
+struct Sum { u64 q; int n; };
+__device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid) {
+    q = wave_sum_u64(q);
+    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+    __syncthreads();
+    if ((tid & 63) == 0) {
+        s.red[tid >> 6] = q;
+        s.num[tid >> 6] = n;
+    }
+    __syncthreads();
+    return Sum{s.red[0] + s.red[1] + s.red[2] + s.red[3], s.num[0] + s.num[1] + s.num[2] + s.num[3]};
+}
+
 template <typename T, bool MASK>
-tasc_status enqueue(const FilterArgs& a, int rows, hipStream_t st) {
+__global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) {
+    __shared__ FinishShared s;
+    const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
+    const Params p = params_of(a, i / a.per);
+    if (tid == 0) s.n = s.bad = 0;
+    __syncthreads();
+    // the list, and what is known of the row
+    int live = 0;
+    bool bad = !p.good, whole = true, has_sum = true;       // whole: the list holds all that are not masked
+    float top = -__builtin_inff(), bound = -__builtin_inff();
+    double part_sum = 0.0, part_scale = -__builtin_inf();   // the lane's part
+    auto append = [&](bool in, u64 c) {
+        const u64 m = __ballot(in);
+        if (!m) return;
+        int at = 0;
+        if (lane == 0) at = atomicAdd(&s.n, __popcll(m));
+        at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi((u32)(m >> 32), __builtin_amdgcn_mbcnt_lo((u32)m, 0));
+        if (in && at < kList) s.list[at] = c;
+    };
+    if (a.direct) {
+        bool nan = false;
+        for (int v0 = 0; v0 < a.vocab; v0 += kFinishThreads) {
+            const float x = v0 + tid < a.vocab ? to_f(row[v0 + tid]) : -__builtin_inff();
+            nan |= !(x < __builtin_inff());
+            top = fmaxf(top, x);
+            append(x > -__builtin_inff(), comp_of(x, v0 + tid));
+        }
+        if (__any(nan) && lane == 0) s.bad = 1;
+        top = wave_max_dpp(top);
+        if (lane == 0) s.num[wave] = __builtin_bit_cast(int, top);
+        __syncthreads();
+        for (int w = 0; w < kFinishWaves; ++w) top = fmaxf(top, __builtin_bit_cast(float, s.num[w]));
+        bad |= s.bad != 0;
+        live = s.n;
+    } else {
+        static_assert(kMostParts == 64);
+        const Part* const parts = a.parts + (int64_t)i * a.n_parts;
+        bool no_sum = false, wrong = false;
+        if (lane < a.n_parts) {
+            const Part o = parts[lane];
+            top = o.top;
+            bound = o.bound;
+            live = o.live;
+            wrong = o.bad;
+            no_sum = !o.has_sum;
+            part_sum = o.sum;
+            part_scale = o.scale;
+        }
+        bad |= __any(wrong) != 0;
+        has_sum = !__any(no_sum);
+        top = wave_max_dpp(top);
+        bound = wave_max_dpp(bound);
+        for (int o = 32; o > 0; o >>= 1) live += __shfl_xor(live, o);
+        // a wave every fourth list, the first 64 of 8 lists at a time
+        const int n_lists = a.n_parts * kPartWaves;
+        const u64* const lists = a.lists + (int64_t)i * n_lists * a.list_len;
+        const u64 last = (u64)~key_of(bound) << 24 | 0xFFFFFF;
+        for (int l0 = wave; l0 < n_lists && bound < __builtin_inff(); l0 += 8 * kFinishWaves) {
+            u64 c[8];
+            int n[8];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const int l = l0 + j * kFinishWaves;
+                n[j] = l < n_lists ? parts[l / kPartWaves].listed[l % kPartWaves] : 0;
+            }
+#pragma unroll
+            for (int j = 0; j < 8; ++j) c[j] = lane < n[j] ? lists[(int64_t)(l0 + j * kFinishWaves) * a.list_len + lane] : ~0ull;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                append(c[j] <= last, c[j]);
+                for (int e = 64; e < n[j]; e += 64) {
+                    const u64 more = e + lane < n[j] ? lists[(int64_t)(l0 + j * kFinishWaves) * a.list_len + e + lane] : ~0ull;
+                    append(more <= last, more);
+                }
+            }
+        }
+        __syncthreads();
+        whole = bound == -__builtin_inff();
+    }
+    const int n = min(s.n, kList);
+    bool wide = !a.direct && s.n > kList;
+    bool nothing_listed = !a.direct && bound == __builtin_inff();
+    bad |= live == 0;
+    wide = wide && !bad;
+    RowState r{};
+    r.top = top + 0.f;
+    r.inv = p.inv;
+    int token = -1, kept = 0;
+    float logp = __builtin_nanf("");
+    u64 cut = ~0ull;
+    if (!bad) {
+        const bool by_count = p.by_count && p.k < live, any = p.one || by_count || p.by_mass || p.by_share;
+        const u64 lo = (u64)~key_of(r.top) << 24, hi = a.direct || whole ? ((1ull << 56) - 1) : (u64)~key_of(bound) << 24 | 0xFFFFFF;
+        auto comp = [&](int e) { return s.list[e]; };
+        auto weight = [&](int e) { return weight_of(r, logit_of(s.list[e]), kListBits); };
+        auto cut_weight = [&](int e) { return s.list[e] <= cut ? weight(e) : 0; };
+        bool held = whole;                                  // the list holds all that the filters so far keep
+        if (nothing_listed) {
+            wide = any || MASK || !has_sum;
+        } else if (!wide) {
+            if (p.one) {
+                u64 first = ~0ull;
+                for (int e = tid; e < n; e += kFinishThreads) first = min(first, s.list[e]);
+                for (int o = 32; o > 0; o >>= 1) first = min(first, (u64)__shfl_xor(first, o));
+                __syncthreads();
+                if (lane == 0) s.red[wave] = first;
+                __syncthreads();
+                cut = min(min(s.red[0], s.red[1]), min(s.red[2], s.red[3]));
+                held = true;
+            }
+            if (by_count) {
+                if (p.k <= n) {
+                    cut = last_item(s, n, lo, hi, (u64)p.k, tid, comp, [](int) { return 1ull; }).key;
+                    held = true;
+                } else if (!held) {
+                    wide = true;
+                }
+            }
+            if (p.by_mass && !wide) {
+                u64 mine = 0;
+                for (int e = tid; e < n; e += kFinishThreads) mine += cut_weight(e);
+                const u64 listed = block_sum(s, mine, 0, tid).q;
+                double limit = 0.0;
+                if (held) {
+                    limit = ceil((double)p.p * (double)listed);
+                } else if (has_sum) {
+                    const double total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0);
+                    limit = ceil((double)p.p * total * 0x1p50);
+                    static_assert(kListBits == 50);
+                    wide = !((double)listed >= limit);
+                } else {
+                    wide = true;
+                }
+                if (!wide) {
+                    cut = last_item(s, n, lo, min(hi, cut), (u64)fmax(limit, 1.0), tid, comp, weight).key;
+                    held = true;
+                }
+            }
+            if (p.by_share && !wide) {
+                const double most = -log((double)p.m);
+                const u32 key = first_key(r.top, lane, [&](float x) { return ((double)r.top - (double)x) * r.inv <= most; });
+                if (from_key(key) >= bound) held = true;
+                cut = min(cut, (u64)~key << 24 | 0xFFFFFF);
+            }
+            wide = wide || !held;
+        }
+        if (wide) {
+        } else if (nothing_listed) {                        // nothing is dropped: the part that the draw falls into, read again
+            const double own = part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0, up = wave_scan64_dpp(own);
+            const double total = lane64(up, 63), target = fmin(fmax((double)a.u[i], 0.0), 1.0) * total;
+            const u64 past = __ballot(up > target), some = __ballot(own > 0.0);
+            const int part = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(some);
+            const int p0 = part * a.part_len, len = min(a.part_len, a.vocab - p0), bits = min(50, 62 - (32 - __clz(a.part_len)));
+            const u64 limit = (u64)(fmax(target - lane64(up - own, part), 0.0) * ldexp(1.0, bits)) + 1;
+            const Found f = last_item(s, len, 0, (u64)len - 1, limit, tid, [&](int e) { return (u64)e; },
+                                      [&](int e) { const float x = to_f(row[p0 + e]); return x > -__builtin_inff() ? max(weight_of(r, x, bits), (u64)1) : 0; });
+            token = p0 + (int)f.key;
+            logp = (float)(((double)to_f(row[token]) - (double)r.top) * r.inv - log(total));
+            kept = live;
+        } else {
+            u64 q = 0;
+            int c = 0;
+            for (int e = tid; e < n; e += kFinishThreads) {
+                const bool in = s.list[e] <= cut;
+                c += in;
+                if (!MASK && in) q += weight(e);
+            }
+            const Sum all = block_sum(s, q, c, tid);
+            kept = all.n;
+            if (!MASK) {
+                const float u = a.u[i];
+                const u64 limit = u > 0.f ? min((u64)((double)u * (double)all.q), all.q - 1) + 1 : 1;
+                token = (int)last_item(s, n, 0, (u64)a.vocab - 1, limit, tid, [&](int e) { return (u64)token_of(s.list[e]); }, cut_weight).key;
+                logp = p.one ? 0.f : (float)(((double)to_f(row[token]) - (double)r.top) * r.inv - log((double)all.q * 0x1p-50));
+            }
+        }
+    }
+    if (MASK) {
+        T* const out = (T*)a.out + (int64_t)i * a.out_stride;
+        const T none = from_f<T>(-__builtin_inff());
+        if (bad || a.direct) {                              // (a row without a distribution is passed on)
+            if (!bad || !a.in_place)
+                for (int v = tid; v < a.vocab; v += kFinishThreads) {
+                    const T x = row[v];
+                    out[v] = bad || (to_f(x) > -__builtin_inff() && comp_of(to_f(x), v) <= cut) ? x : none;
+                }
+        } else if (!wide && !a.in_place) {
+            for (int e = tid; e < n; e += kFinishThreads)
+                if (s.list[e] <= cut) out[token_of(s.list[e])] = row[token_of(s.list[e])];
+        }
+    }
+    if (tid != 0) return;
+    if (!a.direct) a.rows[i] = RowOut{cut, bad ? ROW_BAD : wide ? ROW_WIDE : ROW_DONE, 0};
+    if (wide) return;
+    if (a.kept) a.kept[i] = kept;
+    if (MASK) return;
+    a.token[i] = token;
+    if (a.logprob) a.logprob[i] = logp;
+}
+
+// In place: what is dropped
+template <typename T>
+__global__ __launch_bounds__(kPartThreads) void k_filter_apply(FilterArgs a) {
+    const int i = blockIdx.y;
+    const RowOut o = a.rows[i];
+    if (o.state != ROW_DONE) return;
+    const float cut_x = logit_of(o.cut);
+    const int cut_v = token_of(o.cut), end = min((int)(blockIdx.x + 1) * a.part_len, a.vocab);
+    const bool all = o.cut == ~0ull;
+    T* const row = (T*)a.out + (int64_t)i * a.out_stride;
+    for (int v = blockIdx.x * a.part_len + threadIdx.x; v < end; v += kPartThreads) {
+        const float x = to_f(row[v]);
+        if (!all && !(x > cut_x || (x == cut_x && v <= cut_v))) row[v] = from_f<T>(-__builtin_inff());
+    }
+}
+
+// How a call is cut: parts of kPart logits, up to kMostParts; lists that hold three times what the sample should let through
+struct Plan { int direct, n_parts, part_len, list_len, sample_len, sample_rank; };
+Plan plan_of(int vocab) {
+    Plan p{};
+    p.direct = vocab <= kList;
+    if (p.direct) return p;
+    p.n_parts = std::min((vocab - 1) / kPart + 1, kMostParts);
+    p.part_len = ((vocab - 1) / (p.n_parts * kPartWaves) / 16 + 1) * 16 * kPartWaves;    // (waves' runs alike, as whole vectors)
+    // 1500 of the row, a share f of its logits: a group's largest lies among them with probability 1 - (1 - f)^n
+    const double f = 1500.0 / vocab;
+    p.sample_len = f < 0.015 ? 4 : f < 0.03 ? 2 : 1;
+    p.sample_rank = std::min(kGroups, std::max(1, (int)(kGroups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
+    p.list_len = std::max(192, kList / (p.n_parts * kPartWaves));
+    return p;
+}
+size_t lists_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * kPartWaves * p.list_len * sizeof(u64); }
+size_t parts_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * sizeof(Part); }
+
+template <typename T, bool MASK>
+tasc_status enqueue(FilterArgs a, int rows, void* workspace, hipStream_t st) {
     const bool vec = (((uintptr_t)a.logits | (uintptr_t)(a.row_stride * (int64_t)sizeof(T))) & 15) == 0;
-    vec ? k_filter_rows<T, true, MASK><<<dim3((unsigned)rows), dim3(kThreads), 0, st>>>(a) : k_filter_rows<T, false, MASK><<<dim3((unsigned)rows), dim3(kThreads), 0, st>>>(a);
+    const Plan p = plan_of(a.vocab);
+    a.direct = p.direct;
+    a.in_place = MASK && a.out == a.logits;
+    const dim3 all((unsigned)rows), threads(kPartThreads), parts((unsigned)p.n_parts, (unsigned)rows);
+    if (!p.direct) {
+        a.parts = (Part*)workspace;
+        a.rows = (RowOut*)((char*)workspace + parts_bytes(p, rows));
+        a.lists = (u64*)((char*)a.rows + (size_t)rows * sizeof(RowOut));
+        a.n_parts = p.n_parts;
+        a.part_len = p.part_len;
+        a.list_len = p.list_len;
+        a.sample_len = p.sample_len;
+        a.sample_rank = p.sample_rank;
+        a.out_aligned = (((uintptr_t)a.out | (uintptr_t)(a.out_stride * (int64_t)sizeof(T))) & 15) == 0;
+        if (MASK && !a.in_place) vec ? k_filter_parts<T, true, true><<<parts, threads, 0, st>>>(a) : k_filter_parts<T, false, true><<<parts, threads, 0, st>>>(a);
+        else vec ? k_filter_parts<T, true, false><<<parts, threads, 0, st>>>(a) : k_filter_parts<T, false, false><<<parts, threads, 0, st>>>(a);
+    }
+    k_filter_finish<T, MASK><<<all, dim3(kFinishThreads), 0, st>>>(a);
+    if (!p.direct) {
+        if (a.in_place) k_filter_apply<T><<<parts, threads, 0, st>>>(a);
+        vec ? k_filter_wide<T, true, MASK><<<all, dim3(kThreads), 0, st>>>(a) : k_filter_wide<T, false, MASK><<<all, dim3(kThreads), 0, st>>>(a);
+    }
     TASC_LAUNCH_CHECK();
     return TASC_OK;
 }
@@ -562,7 +1106,8 @@ tasc_status check_workspace(const char* who, void* workspace, size_t ws_bytes, i
 
 extern "C" size_t tasc_sample_workspace_bytes(int32_t rows, int32_t vocab) {
     if (rows < 1 || rows > 65535 || vocab < 2 || vocab > 1 << 24) return 0;
-    return 16;
+    const Plan p = plan_of(vocab);
+    return p.direct ? 0 : parts_bytes(p, rows) + (size_t)rows * sizeof(RowOut) + lists_bytes(p, rows);
 }
 
 extern "C" tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature, const int32_t* top_k,
@@ -573,8 +1118,8 @@ extern "C" tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t
     TASC_REQUIRE(u && token, "sample: null argument");
     rc = check_workspace("sample", workspace, ws_bytes, rows, vocab);
     if (rc != TASC_OK) return rc;
-    const FilterArgs a{logits, row_stride, 1, vocab, temperature, top_k, top_p, min_p, u, token, logprob, kept, nullptr, 0};
-    return dtype == TASC_F32 ? enqueue<float, false>(a, rows, (hipStream_t)stream) : enqueue<BF16, false>(a, rows, (hipStream_t)stream);
+    const FilterArgs a{logits, row_stride, 1, vocab, temperature, top_k, top_p, min_p, u, token, logprob, kept};
+    return dtype == TASC_F32 ? enqueue<float, false>(a, rows, workspace, (hipStream_t)stream) : enqueue<BF16, false>(a, rows, workspace, (hipStream_t)stream);
 }
 
 extern "C" tasc_status tasc_filter_logits(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab, const float* temperature,
@@ -593,5 +1138,5 @@ extern "C" tasc_status tasc_filter_logits(const void* logits, tasc_dtype dtype, 
     rc = check_workspace("filter_logits", workspace, ws_bytes, (int32_t)rows, vocab);
     if (rc != TASC_OK) return rc;
     const FilterArgs a{logits, row_stride, k + 1, vocab, temperature, top_k, top_p, min_p, nullptr, nullptr, nullptr, kept, out, out_stride};
-    return dtype == TASC_F32 ? enqueue<float, true>(a, (int)rows, (hipStream_t)stream) : enqueue<BF16, true>(a, (int)rows, (hipStream_t)stream);
+    return dtype == TASC_F32 ? enqueue<float, true>(a, (int)rows, workspace, (hipStream_t)stream) : enqueue<BF16, true>(a, (int)rows, workspace, (hipStream_t)stream);
 }

@@ -128,3 +128,34 @@ __device__ __forceinline__ double exp_neg(double x) {
     p = __builtin_fma(p, r, 1.0);
     return ldexp(p, (int)n);
 }
+
+// Exponentials by a table: 2^(n / 256) p, n in the low word of a double
+typedef uint32_t word2 __attribute__((ext_vector_type(2)));
+// 2^(i / 256), by the series of the exponential
+constexpr double pow2_256(int i) {
+    const double x = i * (0.69314718055994530942 / 256);
+    double sum = 1.0, term = 1.0;
+    for (int k = 1; k < 30; ++k) sum += term *= x / k;
+    return sum;
+}
+struct PowTable { word2 at[256]; };                   // lower word, upper word less i << 12 (what i adds there beside i / 256 << 20)
+constexpr PowTable pow_table() {
+    PowTable t{};
+    for (int i = 0; i < 256; ++i) {
+        const u64 b = __builtin_bit_cast(u64, pow2_256(i));
+        t.at[i] = word2{(u32)b, (u32)(b >> 32) - ((u32)i << 12)};
+    }
+    return t;
+}
+static __device__ const PowTable kPow = pow_table();
+// p 2^(m / 256)
+__device__ __forceinline__ double times_power(const word2* pow, double p, u32 m, double plus) {
+    const word2 w = pow[m & 255];
+    return __builtin_fma(p, __builtin_bit_cast(double, word2{w[0], w[1] + (m << 12)}), plus);
+}
+__device__ __forceinline__ double small_power(double f) {  // 2^(f / 256)
+    double p = 0x1.c6b08d704a0c0p-29;
+    p = __builtin_fma(p, f, 0x1.ebfbdff82c58fp-19);
+    p = __builtin_fma(p, f, 0x1.62e42fefa39efp-9);
+    return __builtin_fma(p, f, 1.0);
+}

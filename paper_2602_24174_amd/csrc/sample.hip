@@ -17,7 +17,6 @@
 
 namespace {
 
-typedef uint32_t word2 __attribute__((ext_vector_type(2)));
 constexpr int kSeg = 4096, kPartThreads = 256, kPer = kSeg / kPartThreads, kPickThreads = 1024, kMostSegs = 8;
 
 // A segment: sum of its weights, without the row's draft, in units of exp(scale) (-infinity: nothing above -infinity in it), its largest logit
@@ -96,35 +95,6 @@ struct Segment {
 // Waves that hold logits too far from their largest for that (masked ones, say), or so large that 2^-53 of them counts, take the loop behind it.
 // us of this kernel, 1280 rows of 151936 fp32 logits: exp_neg, with the place of the maximum followed as it went, 250; a table of 64, rint, a
 // conversion and ldexp 169; the second loop for all waves 151; as it is 138 (5.6 TB/s).
-// 2^(i / 256), by the series of the exponential
-constexpr double pow2_256(int i) {
-    const double x = i * (0.69314718055994530942 / 256);
-    double sum = 1.0, term = 1.0;
-    for (int k = 1; k < 30; ++k) sum += term *= x / k;
-    return sum;
-}
-struct PowTable { word2 at[256]; };                   // lower word, upper word less i << 12 (what i adds there beside i / 256 << 20)
-constexpr PowTable pow_table() {
-    PowTable t{};
-    for (int i = 0; i < 256; ++i) {
-        const u64 b = __builtin_bit_cast(u64, pow2_256(i));
-        t.at[i] = word2{(u32)b, (u32)(b >> 32) - ((u32)i << 12)};
-    }
-    return t;
-}
-__device__ const PowTable kPow = pow_table();
-// p 2^(m / 256)
-__device__ __forceinline__ double times_power(const word2* pow, double p, u32 m, double plus) {
-    const word2 w = pow[m & 255];
-    return __builtin_fma(p, __builtin_bit_cast(double, word2{w[0], w[1] + (m << 12)}), plus);
-}
-__device__ __forceinline__ double small_power(double f) {  // 2^(f / 256)
-    double p = 0x1.c6b08d704a0c0p-29;
-    p = __builtin_fma(p, f, 0x1.ebfbdff82c58fp-19);
-    p = __builtin_fma(p, f, 0x1.62e42fefa39efp-9);
-    return __builtin_fma(p, f, 1.0);
-}
-
 // SEVERAL: a workgroup takes kMostSegs segments side by side, the next one's logits under way while one's exponentials are computed, and its
 // waves do not wait for each other before the last; the registers for it cost three of seven waves a SIMD.
 template <typename T, bool VEC, bool SEVERAL>

@@ -18,29 +18,30 @@ def status(name, *args):
 
 
 def test_sample():
-    need = T.tasc_sample_workspace_bytes(3, 100)
-    good = dict(logits=A, dtype=0, stride=100, rows=3, vocab=100, t=2 * A, k=3 * A, p=4 * A, m=5 * A, u=6 * A, token=7 * A, logprob=8 * A, kept=9 * A, ws=10 * A, n=need)
+    need = T.tasc_sample_workspace_bytes(3, 5000)
+    good = dict(logits=A, dtype=0, stride=5000, rows=3, vocab=5000, t=2 * A, k=3 * A, p=4 * A, m=5 * A, u=6 * A, token=7 * A, logprob=8 * A, kept=9 * A, ws=10 * A, n=need)
 
     def call(**kw):
         return status("tasc_sample", *dict(good, **kw).values(), None)
 
-    for bad in (dict(logits=None), dict(u=None), dict(token=None), dict(dtype=2), dict(dtype=-1), dict(stride=99), dict(rows=-1), dict(rows=65536), dict(vocab=1), dict(vocab=(1 << 24) + 1, stride=1 << 25),
+    for bad in (dict(logits=None), dict(u=None), dict(token=None), dict(dtype=2), dict(dtype=-1), dict(stride=4999), dict(rows=-1), dict(rows=65536), dict(vocab=1), dict(vocab=(1 << 24) + 1, stride=1 << 25),
                 dict(logits=A + 2), dict(logits=A + 1, dtype=1), dict(ws=10 * A + 8)):
         assert call(**bad) == B.TASC_EINVAL, bad
     assert call(n=need - 1) == B.TASC_ENOMEM and call(ws=None) == B.TASC_ENOMEM
+    assert T.tasc_sample_workspace_bytes(3, 4096) == 0 and call(vocab=4096, ws=None, n=0, dtype=7) == B.TASC_EINVAL
     assert call(rows=0, logits=None, u=None, token=None) == 0
     assert [T.tasc_sample_workspace_bytes(*s) for s in ((0, 100), (65536, 100), (3, 1), (3, (1 << 24) + 1))] == [0] * 4
 
 
 def test_filter_logits():
-    need = T.tasc_sample_workspace_bytes(9, 100)
-    good = dict(logits=A, dtype=1, stride=100, batch=3, k=2, vocab=100, t=2 * A, tk=3 * A, p=4 * A, m=5 * A, out=6 * A, out_stride=100, kept=9 * A, ws=10 * A, n=need)
+    need = T.tasc_sample_workspace_bytes(9, 5000)
+    good = dict(logits=A, dtype=1, stride=5000, batch=3, k=2, vocab=5000, t=2 * A, tk=3 * A, p=4 * A, m=5 * A, out=6 * A, out_stride=5000, kept=9 * A, ws=10 * A, n=need)
 
     def call(**kw):
         return status("tasc_filter_logits", *dict(good, **kw).values(), None)
 
-    for bad in (dict(logits=None), dict(out=None), dict(dtype=3), dict(stride=99), dict(out_stride=99), dict(batch=-1), dict(batch=30000), dict(k=-1), dict(k=16), dict(vocab=1),
-                dict(vocab=(1 << 24) + 1, stride=1 << 25, out_stride=1 << 25), dict(out=6 * A + 1), dict(out=A + 2), dict(out=A, out_stride=104), dict(out=A + 1600), dict(out=A - 1700),
+    for bad in (dict(logits=None), dict(out=None), dict(dtype=3), dict(stride=4999), dict(out_stride=4999), dict(batch=-1), dict(batch=30000), dict(k=-1), dict(k=16), dict(vocab=1),
+                dict(vocab=(1 << 24) + 1, stride=1 << 25, out_stride=1 << 25), dict(out=6 * A + 1), dict(out=A + 2), dict(out=A, out_stride=5008), dict(out=A + 80000), dict(out=A - 80000),
                 dict(ws=10 * A + 4)):
         assert call(**bad) == B.TASC_EINVAL, bad
     assert call(n=need - 1) == B.TASC_ENOMEM and call(ws=None) == B.TASC_ENOMEM
