@@ -3,12 +3,13 @@
 // A row's tokens in the order of their logits (equal ones by index) are whole numbers of 56 bits, `comp`: the logit's bits, turned so that
 // the largest comes first, over the index.  Every filter keeps a prefix of that order, so all of them together come to one last comp, `cut`.
 //
-// Three kernels.  k_filter_parts reads every logit once, a workgroup 16384 of them: the largest, the sum of the weights where it is wanted, and a list of
-// those above a bound that it takes from a sample, about 1500 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always
-// the cut lies in them.  Where it does not (flat distributions, ties of thousands, a top-k of thousands) k_filter_wide, a larger workgroup a row, finds it
-// from the row itself: a histogram over the values, 4096 bins between the largest logit and the least, of counts for top-k and of weights for
-// top-p; the bin in which the prefix ends has few tokens, which are gathered, sorted and summed one by one, or is cut into 4096 again, by comp, until
-// one token is left.  Rows of up to kList tokens are their own list and need one launch.
+// k_filter_parts reads every logit once, a workgroup up to 16384 of them: the largest, the sum of the weights where it is wanted, and a list of those
+// above a bound that it takes from a sample, about 1500 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always the
+// cut lies in them.  Rows whose cut does not (flat distributions: thousands of tokens kept) are listed for two kernels that read them again, parts side by
+// side: k_filter_bins sums the weights (or counts) of 512 ranges of values, its last workgroup of a row finds the range in which the cut lies; k_filter_gather
+// lists that range's tokens and sums what is above it, its last workgroup finds the cut and draws.  k_filter_slow, a workgroup a row, serves what is left (ties of
+// thousands at the cut, a top-k of thousands and a top-p together): 4096 ranges, of which the one with the cut is sorted if it fits, or cut into 4096 again, by
+// comp, until one token is left.  Rows of up to kList tokens are their own list and need one launch.
 //
 // Weights are sums of whole numbers, which no order of the work changes: a bin's of 2^-F of the weight at its middle, so that a bin far from the
 // largest is as exact as one next to it, a list's and the draw's of 2^-F of the largest.  Sums over whole rows are fp64 in a fixed order.
@@ -23,7 +24,7 @@ constexpr int kListBits = 50;                              // a list's weights: 
 // a workgroup of k_filter_parts, its waves' shares; lists of a row together, and entries that k_filter_finish takes
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPer = 16, kStep = 64 * kPer;
 constexpr int kPart = 16384, kMostParts = 64, kList = 4096, kGroups = 64;
-constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64;
+constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64, kWideGrid = 1024;
 
 // What a part of a row comes to
 struct __attribute__((aligned(16))) Part {
@@ -31,11 +32,28 @@ struct __attribute__((aligned(16))) Part {
     float top, bound;                // the largest logit; the lists hold all logits from bound on (infinity: they are not whole)
     int32_t live, bad;               // tokens that are not masked; a NaN or an infinity among the logits
     int32_t listed[kPartWaves];
-    int32_t has_sum, pad[3];
+    int32_t has_sum;
+    float least;                     // the sample's least logit
+    int32_t above;                   // k_filter_gather's: the logits above the range, and their weights
+    int32_t pad;
+    u64 above_q;
 };
 // and a row: kept are the tokens up to `cut`
-enum { ROW_DONE = 0, ROW_WIDE = 1, ROW_BAD = 2 };
-struct RowOut { u64 cut; int32_t state, pad; };
+enum { ROW_DONE = 0, ROW_CUT = 1, ROW_BAD = 2, ROW_WIDE = 3, ROW_SLOW = 4 };     // CUT: what is kept is not in the lists
+enum { BY_MASS = 0, BY_COUNT = 1, BY_SHARE = 2 };
+struct __attribute__((aligned(16))) RowOut {
+    u64 cut;
+    int32_t state, type;
+    float top, ref;                  // largest logit; the logits below `ref` are not listed (infinity: none is)
+    float least;                     // roughly
+    int32_t listed;                  // logits from ref on, and their weights in 2^-kListBits
+    u64 listed_q;
+    float x_lo, x_hi;                // the range that the cut lies in
+    u64 left;                        // what of it is kept, in its units
+    int32_t tickets[2];
+    float x_m;                       // min-p's least logit (-infinity: none)
+    int32_t pad[3];
+};
 
 struct FilterArgs {
     const void* logits;
@@ -54,6 +72,7 @@ struct FilterArgs {
     Part* parts;                     // [rows, n_parts]
     u64* lists;                      // [rows, n_parts, kPartWaves, list_len]
     RowOut* rows;                    // [rows]
+    int32_t* wide;                   // how many rows are listed here, and which
     int32_t n_parts, part_len, list_len;
     int32_t sample_len, sample_rank; // the bound: of 64 groups' largest logits, 16 * sample_len each, the one with so many of them above or at it
     int32_t direct;                  // rows are their own lists
@@ -443,6 +462,17 @@ struct Row {
         }
     }
 
+    __device__ void count() {
+        const float cut_x = logit_of(r.cut);
+        const int cut_v = token_of(r.cut);
+        int n = 0;
+        Loop::run(row, vocab, tid, [&](const float* x, int v) {
+#pragma unroll
+            for (int e = 0; e < SIDE; ++e) n += is_kept(x[e], v + e, cut_x, cut_v);
+        });
+        r.kept = block_count(s, n, tid);
+    }
+
     // the token that u falls on, and ln of its share
     __device__ int draw(float u, float& logp) {
         u64* const seg = s.big + kWideList;
@@ -515,10 +545,10 @@ struct Row {
 };
 
 template <typename T, bool VEC, bool MASK>
-__global__ __launch_bounds__(kThreads) void k_filter_wide(FilterArgs a) {
+__global__ __launch_bounds__(kThreads) void k_filter_slow(FilterArgs a) {
     __shared__ Shared s;
     const int i = blockIdx.x, b = i / a.per, tid = threadIdx.x;
-    if (a.rows[i].state != ROW_WIDE) return;
+    if (a.rows[i].state != ROW_SLOW) return;
     const Params q = params_of(a, b);
     Row<T, VEC> row{(const T*)a.logits + (int64_t)i * a.row_stride, a.vocab, tid, tid & 63, tid >> 6, s, RowState{}};
     RowState& r = row.r;
@@ -547,24 +577,15 @@ __global__ __launch_bounds__(kThreads) void k_filter_wide(FilterArgs a) {
     }
     int token = -1;
     float logp = 0.f;
-    if (MASK) {
-        const float cut_x = logit_of(r.cut);
-        const int cut_v = token_of(r.cut);
-        int kept = 0;
-        T* const out = (T*)a.out + (int64_t)i * a.out_stride;
-        for (int v = tid; v < a.vocab; v += kThreads) {
-            const T x = row.row[v];
-            const bool in = row.is_kept(to_f(x), v, cut_x, cut_v);
-            kept += in;
-            out[v] = in ? x : from_f<T>(-__builtin_inff());
-        }
-        if (r.kept < 0) r.kept = block_count(s, kept, tid);
-    } else {
-        token = row.draw(a.u[i], logp);
-    }
+    if (!MASK) token = row.draw(a.u[i], logp);
+    else if (r.kept < 0) row.count();
     if (tid != 0) return;
     if (a.kept) a.kept[i] = r.kept;
-    if (MASK) return;
+    if (MASK) {
+        a.rows[i].cut = r.cut;
+        a.rows[i].state = ROW_CUT;
+        return;
+    }
     a.token[i] = token;
     if (a.logprob) a.logprob[i] = logp;
 }
@@ -604,7 +625,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
     __shared__ float s_group[kGroups];
     __shared__ float s_bound;
     __shared__ double s_sum[kPartWaves];
-    __shared__ float s_top[kPartWaves];
+    __shared__ float s_top[kPartWaves], s_least[kPartWaves];
     __shared__ int32_t s_live[kPartWaves], s_bad[kPartWaves], s_listed[kPartWaves];
     const int i = blockIdx.y, part = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
@@ -625,6 +646,12 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
         m = row16_max(m);
         if ((lane & 15) == 0) s_group[wave * 16 + g * 4 + lane / 16] = m;
     }
+    float least = __builtin_inff();
+#pragma unroll
+    for (int e = 0; e < kPer; ++e) least = fminf(least, next[e] > -__builtin_inff() ? next[e] : __builtin_inff());
+    least = -wave_max_dpp(-least);
+    if (lane == 0) s_least[wave] = least;
+    if (tid == 0 && part == 0 && i == 0) *a.wide = 0;
     __syncthreads();
     const float group = s_group[lane];
     const float anchor = wave_max_dpp(group);
@@ -710,6 +737,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
     o.sum = (s_sum[0] + s_sum[1]) + (s_sum[2] + s_sum[3]);
     o.scale = whole * (0.69314718055994530942 / 256);
     o.bound = bound;
+    o.least = fminf(fminf(s_least[0], s_least[1]), fminf(s_least[2], s_least[3]));
     for (int w = 0; w < kPartWaves; ++w) {
         o.live += s_live[w];
         o.bad |= s_bad[w];
@@ -828,6 +856,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
     int live = 0;
     bool bad = !p.good, whole = true, has_sum = true;       // whole: the list holds all that are not masked
     float top = -__builtin_inff(), bound = -__builtin_inff();
+    float least = __builtin_inff();
     double part_sum = 0.0, part_scale = -__builtin_inf();   // the lane's part
     auto append = [&](bool in, u64 c) {
         const u64 m = __ballot(in);
@@ -865,11 +894,13 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             no_sum = !o.has_sum;
             part_sum = o.sum;
             part_scale = o.scale;
+            least = o.least;
         }
         bad |= __any(wrong) != 0;
         has_sum = !__any(no_sum);
         top = wave_max_dpp(top);
         bound = wave_max_dpp(bound);
+        least = -wave_max_dpp(-least);
         for (int o = 32; o > 0; o >>= 1) live += __shfl_xor(live, o);
         // a wave every fourth list, the first 64 of 8 lists at a time
         const int n_lists = a.n_parts * kPartWaves;
@@ -907,7 +938,9 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
     r.inv = p.inv;
     int token = -1, kept = 0;
     float logp = __builtin_nanf("");
-    u64 cut = ~0ull;
+    u64 cut = ~0ull, listed_q = 0;
+    float x_m = -__builtin_inff();
+    int type = -1;                                          // of a wide row that the kernels behind this one serve
     if (!bad) {
         const bool by_count = p.by_count && p.k < live, any = p.one || by_count || p.by_mass || p.by_share;
         const u64 lo = (u64)~key_of(r.top) << 24, hi = a.direct || whole ? ((1ull << 56) - 1) : (u64)~key_of(bound) << 24 | 0xFFFFFF;
@@ -915,6 +948,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         auto weight = [&](int e) { return weight_of(r, logit_of(s.list[e]), kListBits); };
         auto cut_weight = [&](int e) { return s.list[e] <= cut ? weight(e) : 0; };
         bool held = whole;                                  // the list holds all that the filters so far keep
+        if (p.by_share) x_m = from_key(first_key(r.top, lane, [&, most = -log((double)p.m)](float x) { return ((double)r.top - (double)x) * r.inv <= most; }));
         if (nothing_listed) {
             wide = any || MASK || !has_sum;
         } else if (!wide) {
@@ -939,7 +973,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             if (p.by_mass && !wide) {
                 u64 mine = 0;
                 for (int e = tid; e < n; e += kFinishThreads) mine += cut_weight(e);
-                const u64 listed = block_sum(s, mine, 0, tid).q;
+                const u64 listed = listed_q = block_sum(s, mine, 0, tid).q;
                 double limit = 0.0;
                 if (held) {
                     limit = ceil((double)p.p * (double)listed);
@@ -957,14 +991,15 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
                 }
             }
             if (p.by_share && !wide) {
-                const double most = -log((double)p.m);
-                const u32 key = first_key(r.top, lane, [&](float x) { return ((double)r.top - (double)x) * r.inv <= most; });
-                if (from_key(key) >= bound) held = true;
-                cut = min(cut, (u64)~key << 24 | 0xFFFFFF);
+                if (x_m >= bound) held = true;
+                cut = min(cut, (u64)~key_of(x_m) << 24 | 0xFFFFFF);
             }
             wide = wide || !held;
         }
         if (wide) {
+            type = !any ? -1 : by_count ? (p.by_mass ? -1 : BY_COUNT) : p.by_mass ? BY_MASS : p.by_share ? BY_SHARE : -1;
+            if (nothing_listed || s.n > kList) bound = __builtin_inff();
+            if (bound == __builtin_inff()) listed_q = 0;
         } else if (nothing_listed) {                        // nothing is dropped: the part that the draw falls into, read again
             const double own = part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0, up = wave_scan64_dpp(own);
             const double total = lane64(up, 63), target = fmin(fmax((double)a.u[i], 0.0), 1.0) * total;
@@ -995,6 +1030,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             }
         }
     }
+    const bool keep_all = MASK && !bad && !a.direct && !p.one && !(p.by_count && p.k < live) && !p.by_mass && !p.by_share;
     if (MASK) {
         T* const out = (T*)a.out + (int64_t)i * a.out_stride;
         const T none = from_f<T>(-__builtin_inff());
@@ -1004,33 +1040,312 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
                     const T x = row[v];
                     out[v] = bad || (to_f(x) > -__builtin_inff() && comp_of(to_f(x), v) <= cut) ? x : none;
                 }
-        } else if (!wide && !a.in_place) {
+        } else if (!wide && !keep_all && !a.in_place) {
             for (int e = tid; e < n; e += kFinishThreads)
                 if (s.list[e] <= cut) out[token_of(s.list[e])] = row[token_of(s.list[e])];
         }
     }
     if (tid != 0) return;
-    if (!a.direct) a.rows[i] = RowOut{cut, bad ? ROW_BAD : wide ? ROW_WIDE : ROW_DONE, 0};
-    if (wide) return;
+    if (!a.direct) {
+        RowOut o{};
+        o.cut = keep_all ? (1ull << 56) - 1 : cut;
+        o.state = bad ? ROW_BAD : keep_all ? ROW_CUT : !wide ? ROW_DONE : type < 0 ? ROW_SLOW : ROW_WIDE;
+        o.type = type;
+        o.top = r.top;
+        o.ref = bound;
+        o.least = least;
+        o.listed = bound == __builtin_inff() ? 0 : n;
+        o.listed_q = listed_q;
+        o.x_lo = o.x_hi = o.x_m = x_m;
+        a.rows[i] = o;
+        if (o.state == ROW_WIDE) a.wide[1 + atomicAdd(a.wide, 1)] = i;
+    }
+    if (keep_all) kept = live;
+    else if (wide) return;
     if (a.kept) a.kept[i] = kept;
     if (MASK) return;
     a.token[i] = token;
     if (a.logprob) a.logprob[i] = logp;
 }
 
-// In place: what is dropped
-template <typename T>
+// ---------------------------------------------------------------- rows whose cut is beyond their lists
+// 2^bits exp((x - ref) / temperature) to a whole number, x at most ref or little above it
+struct TableWeight {
+    const word2* pow;
+    double ref, unit;
+    u32 up;
+    __device__ TableWeight(const word2* table, float of, double inv, int bits) : pow(table), ref((double)of), unit(inv * 369.3299304675746), up(256u * (u32)bits) {}
+    __device__ __forceinline__ u64 operator()(float x) const {
+        const double t = fmax(((double)x - ref) * unit, -900.0 * 256.0), big = t + 0x1.8p52;
+        return __builtin_bit_cast(u64, times_power(pow, small_power(t - (big - 0x1.8p52)), (u32)__builtin_bit_cast(u64, big) + up, 0x1p52)) & 0xFFFFFFFFFFFFFull;
+    }
+};
+// the range of a logit at or below `ref`
+struct Ranges {
+    double ref, per_unit;
+    __device__ Ranges(const RowOut& o) : ref((double)(o.ref < __builtin_inff() ? o.ref : o.top)) {
+        const double range = ref - (double)o.least;
+        per_unit = range > 0.0 ? (kFinishBins - 1.5) / range : 1.0;
+    }
+    __device__ __forceinline__ int operator()(float x) const {
+        const double big = fmin((ref - (double)x) * per_unit, (double)(kFinishBins - 1)) + 0x1.8p52;
+        return (int)(u32)__builtin_bit_cast(u64, big);
+    }
+};
+__device__ __forceinline__ int sum_bits(int n) { return min(kListBits, 61 - (32 - __clz(n))); }      // n weights stay below 2^62
+// whether this workgroup is the last of n to come here with a row; what the others wrote before is then seen
+__device__ __forceinline__ bool last_of(int32_t* ticket, int n, int tid, int32_t* s_last) {
+    __threadfence();
+    __syncthreads();
+    if (tid == 0) *s_last = atomicAdd(ticket, 1) == n - 1;
+    __syncthreads();
+    const bool last = *s_last;
+    __threadfence();
+    return last;
+}
+
+// Ranges' sums, in 2^-F of the weight at ref; the last workgroup of a row finds the range with the cut.
+// LDS atomics bound it (a wave's 64 take about 100 cycles).
+template <typename T, bool VEC>
+__global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
+    using R = Run<T, VEC>;
+    __shared__ word2 s_pow[256];
+    __shared__ u64 s_bins[kFinishBins];
+    __shared__ int32_t s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int items = *a.wide * a.n_parts;
+    if ((int)blockIdx.x >= items) return;
+    s_pow[tid] = kPow.at[tid];
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int i = a.wide[1 + item / a.n_parts], part = item % a.n_parts;
+        RowOut& o = a.rows[i];
+        if (o.type == BY_SHARE) continue;
+        const Params q = params_of(a, i / a.per);
+        const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
+        const int p0 = part * a.part_len, run = a.part_len / kPartWaves, v_begin = min(p0 + wave * run, a.vocab), v_end = min(v_begin + run, a.vocab);
+        const Ranges range_of(o);
+        const TableWeight weight(s_pow, (float)range_of.ref, q.inv, sum_bits(a.vocab));
+        const bool count = o.type == BY_COUNT;
+        const float below = o.ref;
+        __syncthreads();
+        for (int e = tid; e < kFinishBins; e += kPartThreads) s_bins[e] = 0;
+        __syncthreads();
+        float next[kPer];
+        R::load(row, v_begin, v_end, lane, next);
+        for (int v0 = v_begin; v0 < v_end; v0 += kStep) {
+            float x[kPer];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) x[e] = next[e];
+            if (v0 + kStep < v_end) R::load(row, v0 + kStep, v_end, lane, next);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e)
+                if (x[e] < below && x[e] > -__builtin_inff()) atomicAdd(&s_bins[range_of(x[e])], count ? 1ull : weight(x[e]));
+        }
+        __syncthreads();
+        u64* const slices = a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len;
+        for (int e = tid; e < kFinishBins; e += kPartThreads) slices[part * kFinishBins + e] = s_bins[e];
+        if (!last_of(&o.tickets[0], a.n_parts, tid, &s_last)) continue;
+        for (int e = tid; e < kFinishBins; e += kPartThreads) {
+            u64 sum = 0;
+            for (int j = 0; j < a.n_parts; ++j) sum += slices[j * kFinishBins + e];
+            s_bins[e] = sum;
+        }
+        __syncthreads();
+        // every wave for itself, 8 ranges a lane
+        constexpr int PER = kFinishBins / 64;
+        u64 v[PER], mine = 0;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) mine += v[e] = s_bins[PER * lane + e];
+        const u64 up = wave_scan_u64(mine, lane), all = of_lane(up, 63);
+        u64 left;
+        bool good = all > 0;
+        if (count) {
+            good = good && q.k > o.listed;
+            left = (u64)max(q.k - o.listed, 1);
+        } else {
+            const double at_ref = exp_neg((range_of.ref - (double)o.top) * q.inv), unit = ldexp(1.0, -sum_bits(a.vocab)) * at_ref, known = (double)o.listed_q * 0x1p-50;
+            const double rest = (double)q.p * (known + (double)all * unit) - known;
+            good = good && rest > 0.0;
+            left = (u64)fmax(ceil(rest / unit), 1.0);
+        }
+        u64 at = up - mine, before = 0;
+        int last = -1;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if (v[e] && at < left) {
+                last = PER * lane + e;
+                before = at;
+            }
+            at += v[e];
+        }
+        const u64 have = __ballot(last >= 0);
+        if (!good || !have) {
+            if (tid == 0) o.state = ROW_SLOW;
+            continue;
+        }
+        const int from = 63 - __clzll(have), b = __builtin_amdgcn_readlane(last, from);
+        before = of_lane(before, from);
+        const float ref = (float)range_of.ref;
+        const u32 lo = first_key(ref, lane, [&](float x) { return range_of(x) <= b; });
+        const float x_hi = b == 0 ? below : from_key(first_key(ref, lane, [&](float x) { return range_of(x) < b; }));
+        if (tid == 0) {
+            if (o.x_m >= x_hi) {                            // min-p keeps less
+                o.type = BY_SHARE;
+            } else {
+                o.x_lo = from_key(lo);
+                o.x_hi = x_hi;
+                o.left = left - before;
+            }
+        }
+    }
+}
+
+// The range's tokens and what lies above it; the last workgroup of a row finds the cut, and draws
+template <typename T, bool VEC, bool MASK>
+__global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
+    using R = Run<T, VEC>;
+    static_assert(kPartThreads == kFinishThreads && kPartWaves == kFinishWaves);
+    __shared__ word2 s_pow[256];
+    __shared__ FinishShared s;
+    __shared__ u64 s_part[kMostParts];
+    __shared__ u64 s_q[kPartWaves];
+    __shared__ int32_t s_above[kPartWaves], s_listed[kPartWaves], s_last;
+    const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const int items = *a.wide * a.n_parts;
+    if ((int)blockIdx.x >= items) return;
+    s_pow[tid] = kPow.at[tid];
+    for (int item = blockIdx.x; item < items; item += gridDim.x) {
+        const int i = a.wide[1 + item / a.n_parts], part = item % a.n_parts;
+        RowOut& o = a.rows[i];
+        if (o.state == ROW_SLOW) continue;
+        const Params q = params_of(a, i / a.per);
+        const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
+        const int p0 = part * a.part_len, run = a.part_len / kPartWaves, v_begin = min(p0 + wave * run, a.vocab), v_end = min(v_begin + run, a.vocab);
+        const int bits = sum_bits(a.vocab);
+        const TableWeight weight(s_pow, o.top, q.inv, bits);
+        const float x_lo = o.x_lo, x_hi = o.x_hi;
+        u64* const lists = a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len;
+        u64* const list = lists + (part * kPartWaves + wave) * (int64_t)a.list_len;
+        u64 sum = 0;
+        int above = 0, listed = 0;
+        float next[kPer];
+        R::load(row, v_begin, v_end, lane, next);
+        __syncthreads();
+        for (int v0 = v_begin; v0 < v_end; v0 += kStep) {
+            float x[kPer];
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) x[e] = next[e];
+            if (v0 + kStep < v_end) R::load(row, v0 + kStep, v_end, lane, next);
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) {
+                if (x[e] >= x_hi) {
+                    ++above;
+                    if (!MASK) sum += weight(x[e]);
+                }
+                const bool in = x[e] >= x_lo && x[e] < x_hi;
+                const u64 m = __ballot(in);
+                if (!m) continue;
+                const int at = listed + __builtin_amdgcn_mbcnt_hi((u32)(m >> 32), __builtin_amdgcn_mbcnt_lo((u32)m, 0));
+                if (in && at < a.list_len) list[at] = comp_of(x[e], v0 + R::place(e, lane));
+                listed += __popcll(m);
+            }
+        }
+        sum = wave_sum_u64(sum);
+        for (int f = 32; f > 0; f >>= 1) above += __shfl_xor(above, f);
+        if (lane == 0) {
+            s_q[wave] = sum;
+            s_above[wave] = above;
+            s_listed[wave] = listed;
+        }
+        __syncthreads();
+        if (tid == 0) {
+            Part& to = a.parts[(int64_t)i * a.n_parts + part];
+            to.above = s_above[0] + s_above[1] + s_above[2] + s_above[3];
+            to.above_q = s_q[0] + s_q[1] + s_q[2] + s_q[3];
+            for (int w = 0; w < kPartWaves; ++w) to.listed[w] = s_listed[w];
+        }
+        if (!last_of(&o.tickets[1], a.n_parts, tid, &s_last)) continue;
+        // the row from its parts
+        if (tid == 0) s.n = 0;
+        if (tid < kMostParts) s_part[tid] = tid < a.n_parts ? a.parts[(int64_t)i * a.n_parts + tid].above_q : 0;
+        __syncthreads();
+        int n_above = lane < a.n_parts ? a.parts[(int64_t)i * a.n_parts + lane].above : 0;
+        for (int f = 32; f > 0; f >>= 1) n_above += __shfl_xor(n_above, f);
+        bool over = false;
+        for (int l = wave; l < a.n_parts * kPartWaves; l += kPartWaves) {
+            const int n = a.parts[(int64_t)i * a.n_parts + l / kPartWaves].listed[l % kPartWaves];
+            over |= n > a.list_len;
+            int at = 0;
+            if (lane == 0) at = atomicAdd(&s.n, n);
+            at = __builtin_amdgcn_readfirstlane(at);
+            for (int e = lane; e < min(n, a.list_len); e += 64)
+                if (at + e < kList) s.list[at + e] = lists[(int64_t)l * a.list_len + e];
+        }
+        if (over && lane == 0) atomicAdd(&s.n, kList);
+        __syncthreads();
+        const int n = s.n;
+        if (n > kList) {
+            if (tid == 0) o.state = ROW_SLOW;
+            continue;
+        }
+        const TableWeight at_ref(s_pow, o.ref < __builtin_inff() ? o.ref : o.top, q.inv, bits);      // (k_filter_bins' numbers)
+        u64 cut = (u64)~key_of(x_hi) << 24 | 0xFFFFFF;      // (x_hi itself is above)
+        if (o.type != BY_SHARE) {
+            const bool count = o.type == BY_COUNT;
+            cut = last_item(s, n, (u64)~(key_of(x_hi) - 1) << 24, (u64)~key_of(x_lo) << 24 | 0xFFFFFF, o.left, tid, [&](int e) { return s.list[e]; },
+                            [&](int e) { return count ? 1ull : at_ref(logit_of(s.list[e])); }).key;
+            if (q.by_share) cut = min(cut, (u64)~key_of(o.x_m) << 24 | 0xFFFFFF);
+        }
+        int kept = 0;
+        for (int e = tid; e < n; e += kFinishThreads) {
+            const u64 c = s.list[e];
+            if (c > cut) continue;
+            ++kept;
+            if (!MASK) atomicAdd(&s_part[token_of(c) / a.part_len], weight(logit_of(c)));
+        }
+        kept = block_sum(s, 0, kept, tid).n + n_above;
+        int token = -1;
+        float logp = 0.f;
+        if (!MASK) {
+            const float u = a.u[i];
+            const u64 own = s_part[lane], up = wave_scan_u64(own, lane), total = of_lane(up, 63);
+            const u64 target = u > 0.f ? min((u64)((double)u * (double)total), total - 1) : 0;
+            const int of = __ffsll((unsigned long long)__ballot(up > target)) - 1, first = of * a.part_len, len = min(a.part_len, a.vocab - first);
+            const float cut_x = logit_of(cut);
+            const int cut_v = token_of(cut);
+            token = first + (int)last_item(s, len, 0, (u64)len - 1, target - of_lane(up - own, of) + 1, tid, [](int e) { return (u64)e; }, [&](int e) {
+                const float x = to_f(row[first + e]);
+                return x > cut_x || (x == cut_x && first + e <= cut_v) ? weight(x) : 0;
+            }).key;
+            logp = (float)(((double)to_f(row[token]) - (double)o.top) * q.inv - log((double)total * ldexp(1.0, -bits)));
+        }
+        if (tid == 0) {
+            o.cut = cut;
+            o.state = ROW_CUT;
+            if (a.kept) a.kept[i] = kept;
+            if (!MASK) {
+                a.token[i] = token;
+                if (a.logprob) a.logprob[i] = logp;
+            }
+        }
+        __syncthreads();
+    }
+}
+
+// In place: what is dropped.  Else, of the rows that were not written from their lists, what is kept.
+template <typename T, bool IN_PLACE>
 __global__ __launch_bounds__(kPartThreads) void k_filter_apply(FilterArgs a) {
-    const int i = blockIdx.y;
-    const RowOut o = a.rows[i];
-    if (o.state != ROW_DONE) return;
-    const float cut_x = logit_of(o.cut);
-    const int cut_v = token_of(o.cut), end = min((int)(blockIdx.x + 1) * a.part_len, a.vocab);
-    const bool all = o.cut == ~0ull;
-    T* const row = (T*)a.out + (int64_t)i * a.out_stride;
+    const int i = blockIdx.y, state = a.rows[i].state;
+    if (state != ROW_CUT && !(IN_PLACE && state == ROW_DONE)) return;
+    const u64 cut = a.rows[i].cut;
+    const int end = min((int)(blockIdx.x + 1) * a.part_len, a.vocab);
+    const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
+    T* const out = (T*)a.out + (int64_t)i * a.out_stride;
     for (int v = blockIdx.x * a.part_len + threadIdx.x; v < end; v += kPartThreads) {
-        const float x = to_f(row[v]);
-        if (!all && !(x > cut_x || (x == cut_x && v <= cut_v))) row[v] = from_f<T>(-__builtin_inff());
+        const T x = IN_PLACE ? out[v] : row[v];
+        const bool in = to_f(x) > -__builtin_inff() && comp_of(to_f(x), v) <= cut;
+        if (IN_PLACE && !in) out[v] = from_f<T>(-__builtin_inff());
+        if (!IN_PLACE && in) out[v] = x;
     }
 }
 
@@ -1063,6 +1378,7 @@ tasc_status enqueue(FilterArgs a, int rows, void* workspace, hipStream_t st) {
         a.parts = (Part*)workspace;
         a.rows = (RowOut*)((char*)workspace + parts_bytes(p, rows));
         a.lists = (u64*)((char*)a.rows + (size_t)rows * sizeof(RowOut));
+        a.wide = (int32_t*)((char*)a.lists + lists_bytes(p, rows));
         a.n_parts = p.n_parts;
         a.part_len = p.part_len;
         a.list_len = p.list_len;
@@ -1074,8 +1390,13 @@ tasc_status enqueue(FilterArgs a, int rows, void* workspace, hipStream_t st) {
     }
     k_filter_finish<T, MASK><<<all, dim3(kFinishThreads), 0, st>>>(a);
     if (!p.direct) {
-        if (a.in_place) k_filter_apply<T><<<parts, threads, 0, st>>>(a);
-        vec ? k_filter_wide<T, true, MASK><<<all, dim3(kThreads), 0, st>>>(a) : k_filter_wide<T, false, MASK><<<all, dim3(kThreads), 0, st>>>(a);
+        if (a.top_k || a.top_p || a.min_p) {
+            const dim3 some((unsigned)std::min<int64_t>((int64_t)rows * p.n_parts, kWideGrid));
+            vec ? k_filter_bins<T, true><<<some, threads, 0, st>>>(a) : k_filter_bins<T, false><<<some, threads, 0, st>>>(a);
+            vec ? k_filter_gather<T, true, MASK><<<some, threads, 0, st>>>(a) : k_filter_gather<T, false, MASK><<<some, threads, 0, st>>>(a);
+        }
+        vec ? k_filter_slow<T, true, MASK><<<all, dim3(kThreads), 0, st>>>(a) : k_filter_slow<T, false, MASK><<<all, dim3(kThreads), 0, st>>>(a);
+        if (MASK) a.in_place ? k_filter_apply<T, true><<<parts, threads, 0, st>>>(a) : k_filter_apply<T, false><<<parts, threads, 0, st>>>(a);
     }
     TASC_LAUNCH_CHECK();
     return TASC_OK;
@@ -1107,7 +1428,7 @@ tasc_status check_workspace(const char* who, void* workspace, size_t ws_bytes, i
 extern "C" size_t tasc_sample_workspace_bytes(int32_t rows, int32_t vocab) {
     if (rows < 1 || rows > 65535 || vocab < 2 || vocab > 1 << 24) return 0;
     const Plan p = plan_of(vocab);
-    return p.direct ? 0 : parts_bytes(p, rows) + (size_t)rows * sizeof(RowOut) + lists_bytes(p, rows);
+    return p.direct ? 0 : parts_bytes(p, rows) + (size_t)rows * sizeof(RowOut) + lists_bytes(p, rows) + ((size_t)rows + 1) * sizeof(int32_t);
 }
 
 extern "C" tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature, const int32_t* top_k,
