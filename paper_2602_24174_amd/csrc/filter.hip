@@ -4,7 +4,7 @@
 // the largest comes first, over the index.  Every filter keeps a prefix of that order, so all of them together come to one last comp, `cut`.
 //
 // k_filter_parts reads every logit once, a workgroup up to 16384 of them: the largest, the sum of the weights where it is wanted, and a list of those
-// above a bound that it takes from a sample, about 1500 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always the
+// above a bound that it takes from a sample, about 700 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always the
 // cut lies in them.  Rows whose cut does not (flat distributions: thousands of tokens kept) are listed for two kernels that read them again, parts side by
 // side: k_filter_bins sums the weights (or counts) of 512 ranges of values, its last workgroup of a row finds the range in which the cut lies; k_filter_gather
 // lists that range's tokens and sums what is above it, its last workgroup finds the cut and draws.  k_filter_slow, a workgroup a row, serves what is left (ties of
@@ -23,8 +23,8 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096, kWideList =
 constexpr int kListBits = 50;                              // a list's weights: 2^12 of them stay below 2^62
 // a workgroup of k_filter_parts, its waves' shares; lists of a row together, and entries that k_filter_finish takes
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPer = 16, kStep = 64 * kPer;
-constexpr int kPart = 16384, kMostParts = 64, kList = 4096, kGroups = 64;
-constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64, kWideGrid = 1024;
+constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 2048, kMostParts = 64, kList = 4096, kGroups = 64, kWanted = 768;
+constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64, kRanges = 1024, kWideGrid = 1024;
 
 // What a part of a row comes to
 struct __attribute__((aligned(16))) Part {
@@ -49,7 +49,7 @@ struct __attribute__((aligned(16))) RowOut {
     int32_t listed;                  // logits from ref on, and their weights in 2^-kListBits
     u64 listed_q;
     float x_lo, x_hi;                // the range that the cut lies in
-    u64 left;                        // what of it is kept, in its units
+    double total;                    // sum of all weights, in the largest's
     int32_t tickets[2];
     float x_m;                       // min-p's least logit (-infinity: none)
     int32_t pad[3];
@@ -105,19 +105,26 @@ __device__ __forceinline__ Params params_of(const FilterArgs& a, int b) {
     return o;
 }
 
-__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
-    for (int o = 32; o > 0; o >>= 1) v += __shfl_xor(v, o);
-    return v;
-}
-__device__ __forceinline__ u64 wave_scan_u64(u64 v, int lane) {          // inclusive
-    for (int o = 1; o < 64; o <<= 1) {
-        const u64 up = __shfl_up(v, o);
-        if (lane >= o) v += up;
-    }
-    return v;
-}
-__device__ __forceinline__ u64 of_lane(u64 v, int l) {
+template <int CTRL, int ROWS = 0xF>
+__device__ __forceinline__ u64 dpp_u64(u64 v) { return __builtin_bit_cast(u64, lane64_dpp<CTRL, ROWS>(__builtin_bit_cast(double, v))); }
+__device__ __forceinline__ u64 of_lane(u64 v, int l) {     // l: the same in all lanes
     return (u64)(u32)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 | (u32)__builtin_amdgcn_readlane((int)(u32)v, l);
+}
+__device__ __forceinline__ u64 wave_sum_u64(u64 v) {
+    v += dpp_u64<0xB1>(v);                                  // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
+    v += dpp_u64<0x4E>(v);
+    v += dpp_u64<0x141>(v);
+    v += dpp_u64<0x140>(v);
+    return of_lane(v, 0) + of_lane(v, 16) + of_lane(v, 32) + of_lane(v, 48);
+}
+__device__ __forceinline__ u64 wave_scan_u64(u64 v) {      // inclusive
+    v += dpp_u64<0x111>(v);                                 // row_shr 1, 2, 4, 8
+    v += dpp_u64<0x112>(v);
+    v += dpp_u64<0x114>(v);
+    v += dpp_u64<0x118>(v);
+    v += dpp_u64<0x142, 0xA>(v);                            // lane 15 of the row before, into rows 1 and 3
+    v += dpp_u64<0x143, 0xC>(v);                            // lane 31, into rows 2 and 3
+    return v;
 }
 
 // The logits of a row, thread by thread: f(x, first index) over SIDE side by side, those behind the vocabulary as masked
@@ -283,7 +290,7 @@ __device__ __forceinline__ int list_below(Shared& s, const RowState& r, const u6
     u64 q[2], mine = 0;
 #pragma unroll
     for (int e = 0; e < 2; ++e) mine += q[e] = 2 * tid + e < n ? weight_of(r, logit_of(list[2 * tid + e]), kListBits) : 0;
-    const u64 up = wave_scan_u64(mine, lane);
+    const u64 up = wave_scan_u64(mine);
     if (lane == 63) s.whole[wave] = up;
     __syncthreads();
     u64 at = up - mine, total = 0;
@@ -514,7 +521,7 @@ struct Row {
                 }
             }
             __syncthreads();
-            const u64 mine = seg[tid], up = wave_scan_u64(mine, lane);
+            const u64 mine = seg[tid], up = wave_scan_u64(mine);
             if (lane == 63) s.whole[wave] = up;
             __syncthreads();
             u64 before = up - mine, all = 0;
@@ -592,7 +599,7 @@ __global__ __launch_bounds__(kThreads) void k_filter_slow(FilterArgs a) {
 
 // ---------------------------------------------------------------- one read of every logit
 // A wave has a run of its own, 16 logits a lane at a time.  The first of them are the sample: of groups of 16 to 64 logits the largest, and of these 64 one
-// by its rank, which about 1500 / vocab of all logits exceed; the sum's units come from the sample's largest, too.
+// by its rank, which about kWanted / vocab of all logits exceed; the sum's units come from the sample's largest, too.
 template <typename T, bool VEC>
 struct Run {
     static constexpr int SIDE = VEC ? 16 / (int)sizeof(T) : 1;
@@ -758,6 +765,14 @@ struct __attribute__((aligned(16))) FinishShared {
     u64 red[kFinishWaves];
     int32_t num[kFinishWaves], few, n, bad;
 };
+__device__ __forceinline__ void append_to(FinishShared& s, bool in, u64 c, int lane) {
+    const u64 m = __ballot(in);
+    if (!m) return;
+    int at = 0;
+    if (lane == 0) at = atomicAdd(&s.n, __popcll(m));
+    at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi((u32)(m >> 32), __builtin_amdgcn_mbcnt_lo((u32)m, 0));
+    if (in && at < kList) s.list[at] = c;
+}
 struct Found { u64 key, sum; };      // sum: up to it and with it
 
 // Of n items with weights q (0: not there), in the order of their keys within [lo, hi]: the last whose sum of those before it is below `limit`
@@ -766,8 +781,8 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
     const int lane = tid & 63;
     u64 sum = 0;
     for (;;) {
-        int shift = 0;
-        while ((hi - lo) >> shift >= kFinishBins) ++shift;
+        const int shift = max(0, 64 - 9 - __clzll((long long)(hi - lo)));
+        static_assert(kFinishBins == 1 << 9);
         __syncthreads();                                    // (bins and few are still looked at)
         for (int i = tid; i < kFinishBins; i += kFinishThreads) s.bins[i] = 0;
         if (tid == 0) s.few = 0;
@@ -784,7 +799,7 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
         u64 v[PER], mine = 0;
 #pragma unroll
         for (int e = 0; e < PER; ++e) mine += v[e] = s.bins[PER * lane + e];
-        const u64 up = wave_scan_u64(mine, lane);
+        const u64 up = wave_scan_u64(mine);
         u64 at = up - mine, before = 0, own = 0;
         int last = -1;
 #pragma unroll
@@ -844,7 +859,103 @@ __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid)
     return Sum{s.red[0] + s.red[1] + s.red[2] + s.red[3], s.num[0] + s.num[1] + s.num[2] + s.num[3]};
 }
 
-template <typename T, bool MASK>
+// The entries up to `last` of a row's lists, a wave every fourth list, the first 64 of 8 lists at a time: append(whether there is one, it)
+template <typename Append>
+__device__ __forceinline__ void read_lists(const FilterArgs& a, int i, int wave, int lane, u64 last, Append append) {
+    const Part* const parts = a.parts + (int64_t)i * a.n_parts;
+    const int n_lists = a.n_parts * kPartWaves;
+    const u64* const lists = a.lists + (int64_t)i * n_lists * a.list_len;
+    for (int l0 = wave; l0 < n_lists; l0 += 8 * kFinishWaves) {
+        u64 c[8];
+        int n[8];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int l = l0 + j * kFinishWaves;
+            n[j] = l < n_lists ? min(parts[l / kPartWaves].listed[l % kPartWaves], a.list_len) : 0;
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) c[j] = lane < n[j] ? lists[(int64_t)(l0 + j * kFinishWaves) * a.list_len + lane] : ~0ull;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            append(c[j] <= last, c[j]);
+            for (int e = 64; e < n[j]; e += 64) {
+                const u64 more = e + lane < n[j] ? lists[(int64_t)(l0 + j * kFinishWaves) * a.list_len + e + lane] : ~0ull;
+                append(more <= last, more);
+            }
+        }
+    }
+}
+
+// The first of the logits [p0, end) whose weights up to it sum to more than `target` (the last with any if none does): the sums of the waves' steps, then the
+// logits of one step.  weight(x, v) is 0 where a token is not kept.
+template <typename T, bool VEC, typename Weight>
+__device__ __forceinline__ int draw_part(FinishShared& s, const T* row, int p0, int run, int end, u64 target, int tid, Weight weight) {
+    using R = Run<T, VEC>;
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), v_begin = min(p0 + wave * run, end), v_end = min(v_begin + run, end);
+    const int steps = (run + kStep - 1) / kStep;            // of a wave
+    __syncthreads();
+    for (int i = tid; i < kFinishBins; i += kFinishThreads) s.bins[i] = 0;
+    __syncthreads();
+    float next[kPer];
+    R::load(row, v_begin, v_end, lane, next);
+    for (int st = 0; st < steps; ++st) {
+        const int v0 = v_begin + st * kStep;
+        float x[kPer];
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) x[e] = next[e];
+        if (v0 + kStep < v_end) R::load(row, v0 + kStep, v_end, lane, next);
+        if (v0 >= v_end) break;
+        u64 q = 0;
+#pragma unroll
+        for (int e = 0; e < kPer; ++e) q += weight(x[e], v0 + R::place(e, lane));
+        q = wave_sum_u64(q);
+        if (lane == 0) s.bins[wave * steps + st] = q;
+    }
+    __syncthreads();
+    constexpr int PER = kFinishBins / 64;
+    u64 v[PER], mine = 0;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) mine += v[e] = s.bins[PER * lane + e];
+    const u64 up = wave_scan_u64(mine);
+    u64 at = up - mine, before = 0;
+    int last = -1;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        if (v[e] && at <= target) {
+            last = PER * lane + e;
+            before = at;
+        }
+        at += v[e];
+    }
+    const u64 have = __ballot(last >= 0);
+    if (!have) return p0;
+    const int from = 63 - __clzll(have), step = __builtin_amdgcn_readlane(last, from);
+    target -= of_lane(before, from);
+    // four logits a thread
+    static_assert(kStep == 4 * kFinishThreads);
+    const int w = step / steps, first = p0 + w * run + step % steps * kStep, stop = min(min(p0 + (w + 1) * run, end), first + kStep), v0 = first + 4 * tid;
+    u64 q[4], own = 0;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) own += q[e] = v0 + e < stop ? weight(to_f(row[v0 + e]), v0 + e) : 0;
+    const u64 sum = wave_scan_u64(own);
+    __syncthreads();
+    if (lane == 63) s.red[wave] = sum;
+    __syncthreads();
+    at = sum - own;
+    for (int i = 0; i < wave; ++i) at += s.red[i];
+    int token = -1;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+        if (q[e] && at <= target) token = v0 + e;
+        at += q[e];
+    }
+    for (int o = 32; o > 0; o >>= 1) token = max(token, __shfl_xor(token, o));
+    if (lane == 0) s.num[wave] = token;
+    __syncthreads();
+    return max(max(s.num[0], s.num[1]), max(s.num[2], s.num[3]));
+}
+
+template <typename T, bool VEC, bool MASK>
 __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) {
     __shared__ FinishShared s;
     const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -858,14 +969,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
     float top = -__builtin_inff(), bound = -__builtin_inff();
     float least = __builtin_inff();
     double part_sum = 0.0, part_scale = -__builtin_inf();   // the lane's part
-    auto append = [&](bool in, u64 c) {
-        const u64 m = __ballot(in);
-        if (!m) return;
-        int at = 0;
-        if (lane == 0) at = atomicAdd(&s.n, __popcll(m));
-        at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi((u32)(m >> 32), __builtin_amdgcn_mbcnt_lo((u32)m, 0));
-        if (in && at < kList) s.list[at] = c;
-    };
+    auto append = [&](bool in, u64 c) { append_to(s, in, c, lane); };
     if (a.direct) {
         bool nan = false;
         for (int v0 = 0; v0 < a.vocab; v0 += kFinishThreads) {
@@ -902,29 +1006,8 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         bound = wave_max_dpp(bound);
         least = -wave_max_dpp(-least);
         for (int o = 32; o > 0; o >>= 1) live += __shfl_xor(live, o);
-        // a wave every fourth list, the first 64 of 8 lists at a time
-        const int n_lists = a.n_parts * kPartWaves;
-        const u64* const lists = a.lists + (int64_t)i * n_lists * a.list_len;
-        const u64 last = (u64)~key_of(bound) << 24 | 0xFFFFFF;
-        for (int l0 = wave; l0 < n_lists && bound < __builtin_inff(); l0 += 8 * kFinishWaves) {
-            u64 c[8];
-            int n[8];
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const int l = l0 + j * kFinishWaves;
-                n[j] = l < n_lists ? parts[l / kPartWaves].listed[l % kPartWaves] : 0;
-            }
-#pragma unroll
-            for (int j = 0; j < 8; ++j) c[j] = lane < n[j] ? lists[(int64_t)(l0 + j * kFinishWaves) * a.list_len + lane] : ~0ull;
-#pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                append(c[j] <= last, c[j]);
-                for (int e = 64; e < n[j]; e += 64) {
-                    const u64 more = e + lane < n[j] ? lists[(int64_t)(l0 + j * kFinishWaves) * a.list_len + e + lane] : ~0ull;
-                    append(more <= last, more);
-                }
-            }
-        }
+        if (bound < __builtin_inff())
+            read_lists(a, i, wave, lane, (u64)~key_of(bound) << 24 | 0xFFFFFF, append);
         __syncthreads();
         whole = bound == -__builtin_inff();
     }
@@ -940,6 +1023,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
     float logp = __builtin_nanf("");
     u64 cut = ~0ull, listed_q = 0;
     float x_m = -__builtin_inff();
+    double total = 0.0;                                     // of all weights
     int type = -1;                                          // of a wide row that the kernels behind this one serve
     if (!bad) {
         const bool by_count = p.by_count && p.k < live, any = p.one || by_count || p.by_mass || p.by_share;
@@ -978,7 +1062,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
                 if (held) {
                     limit = ceil((double)p.p * (double)listed);
                 } else if (has_sum) {
-                    const double total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0);
+                    total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0);
                     limit = ceil((double)p.p * total * 0x1p50);
                     static_assert(kListBits == 50);
                     wide = !((double)listed >= limit);
@@ -997,7 +1081,8 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             wide = wide || !held;
         }
         if (wide) {
-            type = !any ? -1 : by_count ? (p.by_mass ? -1 : BY_COUNT) : p.by_mass ? BY_MASS : p.by_share ? BY_SHARE : -1;
+            type = !any ? -1 : by_count ? (p.by_mass ? -1 : BY_COUNT) : p.by_mass ? (has_sum ? BY_MASS : -1) : p.by_share ? BY_SHARE : -1;
+            if (type == BY_MASS) total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0);
             if (nothing_listed || s.n > kList) bound = __builtin_inff();
             if (bound == __builtin_inff()) listed_q = 0;
         } else if (nothing_listed) {                        // nothing is dropped: the part that the draw falls into, read again
@@ -1006,10 +1091,8 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             const u64 past = __ballot(up > target), some = __ballot(own > 0.0);
             const int part = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(some);
             const int p0 = part * a.part_len, len = min(a.part_len, a.vocab - p0), bits = min(50, 62 - (32 - __clz(a.part_len)));
-            const u64 limit = (u64)(fmax(target - lane64(up - own, part), 0.0) * ldexp(1.0, bits)) + 1;
-            const Found f = last_item(s, len, 0, (u64)len - 1, limit, tid, [&](int e) { return (u64)e; },
-                                      [&](int e) { const float x = to_f(row[p0 + e]); return x > -__builtin_inff() ? max(weight_of(r, x, bits), (u64)1) : 0; });
-            token = p0 + (int)f.key;
+            const u64 within = (u64)(fmax(target - lane64(up - own, part), 0.0) * ldexp(1.0, bits));
+            token = draw_part<T, VEC>(s, row, p0, a.part_len / kPartWaves, p0 + len, within, tid, [&](float x, int) { return x > -__builtin_inff() ? max(weight_of(r, x, bits), (u64)1) : 0; });
             logp = (float)(((double)to_f(row[token]) - (double)r.top) * r.inv - log(total));
             kept = live;
         } else {
@@ -1056,6 +1139,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         o.least = least;
         o.listed = bound == __builtin_inff() ? 0 : n;
         o.listed_q = listed_q;
+        o.total = total;
         o.x_lo = o.x_hi = o.x_m = x_m;
         a.rows[i] = o;
         if (o.state == ROW_WIDE) a.wide[1 + atomicAdd(a.wide, 1)] = i;
@@ -1080,55 +1164,52 @@ struct TableWeight {
         return __builtin_bit_cast(u64, times_power(pow, small_power(t - (big - 0x1.8p52)), (u32)__builtin_bit_cast(u64, big) + up, 0x1p52)) & 0xFFFFFFFFFFFFFull;
     }
 };
-// the range of a logit at or below `ref`
+// the range of a logit below `ref`, the first next to it
 struct Ranges {
-    double ref, per_unit;
-    __device__ Ranges(const RowOut& o) : ref((double)(o.ref < __builtin_inff() ? o.ref : o.top)) {
-        const double range = ref - (double)o.least;
-        per_unit = range > 0.0 ? (kFinishBins - 1.5) / range : 1.0;
+    float ref, per_unit;
+    __device__ Ranges(const RowOut& o) : ref(o.ref < __builtin_inff() ? o.ref : o.top) {
+        const float width = ref - o.least;
+        per_unit = width > 0.f && width < __builtin_inff() ? (float)fmin((kRanges - 1) / (double)width, 1e38) : 1.f;
     }
-    __device__ __forceinline__ int operator()(float x) const {
-        const double big = fmin((ref - (double)x) * per_unit, (double)(kFinishBins - 1)) + 0x1.8p52;
-        return (int)(u32)__builtin_bit_cast(u64, big);
-    }
+    __device__ __forceinline__ int operator()(float x) const { return (int)fminf((ref - x) * per_unit, (float)(kRanges - 1)); }
 };
 __device__ __forceinline__ int sum_bits(int n) { return min(kListBits, 61 - (32 - __clz(n))); }      // n weights stay below 2^62
-// whether this workgroup is the last of n to come here with a row; what the others wrote before is then seen
+// Whether this workgroup is the last of n to come here with a row; what the others wrote before is then seen.  One thread's fences serve its
+// workgroup, the barriers around them order the others' accesses: an agent's fence writes a whole L2 back and takes thousands of cycles.
 __device__ __forceinline__ bool last_of(int32_t* ticket, int n, int tid, int32_t* s_last) {
-    __threadfence();
     __syncthreads();
-    if (tid == 0) *s_last = atomicAdd(ticket, 1) == n - 1;
+    if (tid == 0) {
+        __threadfence();
+        const bool last = atomicAdd(ticket, 1) == n - 1;
+        if (last) __threadfence();
+        *s_last = last;
+    }
     __syncthreads();
-    const bool last = *s_last;
-    __threadfence();
-    return last;
+    return *s_last != 0;
 }
 
-// Ranges' sums, in 2^-F of the weight at ref; the last workgroup of a row finds the range with the cut.
-// LDS atomics bound it (a wave's 64 take about 100 cycles).
+// Counts of the ranges; the last workgroup of a row finds the one with the cut, by the counts times the weight at each range's middle.  Ranges are so narrow
+// (0.01 of a logit, 400 tokens, for 150,000 tokens over 10) that this is off by a token or so: that range and its neighbours go to k_filter_gather, which
+// has exact sums and sees whether the cut lies in them.  Bound by the LDS atomics.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
     using R = Run<T, VEC>;
-    __shared__ word2 s_pow[256];
-    __shared__ u64 s_bins[kFinishBins];
+    __shared__ u32 s_bins[kRanges];
     __shared__ int32_t s_last;
+    __shared__ double s_sum[kPartWaves];
+    __shared__ int32_t s_at[kPartWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int items = *a.wide * a.n_parts;
-    if ((int)blockIdx.x >= items) return;
-    s_pow[tid] = kPow.at[tid];
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
         const int i = a.wide[1 + item / a.n_parts], part = item % a.n_parts;
         RowOut& o = a.rows[i];
         if (o.type == BY_SHARE) continue;
-        const Params q = params_of(a, i / a.per);
         const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
         const int p0 = part * a.part_len, run = a.part_len / kPartWaves, v_begin = min(p0 + wave * run, a.vocab), v_end = min(v_begin + run, a.vocab);
         const Ranges range_of(o);
-        const TableWeight weight(s_pow, (float)range_of.ref, q.inv, sum_bits(a.vocab));
-        const bool count = o.type == BY_COUNT;
         const float below = o.ref;
         __syncthreads();
-        for (int e = tid; e < kFinishBins; e += kPartThreads) s_bins[e] = 0;
+        for (int e = tid; e < kRanges; e += kPartThreads) s_bins[e] = 0;
         __syncthreads();
         float next[kPer];
         R::load(row, v_begin, v_end, lane, next);
@@ -1139,68 +1220,65 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
             if (v0 + kStep < v_end) R::load(row, v0 + kStep, v_end, lane, next);
 #pragma unroll
             for (int e = 0; e < kPer; ++e)
-                if (x[e] < below && x[e] > -__builtin_inff()) atomicAdd(&s_bins[range_of(x[e])], count ? 1ull : weight(x[e]));
+                if (x[e] < below && x[e] > -__builtin_inff()) atomicAdd(&s_bins[range_of(x[e])], 1u);
         }
         __syncthreads();
-        u64* const slices = a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len;
-        for (int e = tid; e < kFinishBins; e += kPartThreads) slices[part * kFinishBins + e] = s_bins[e];
+        u32* const slices = (u32*)(a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len);
+        for (int e = tid; e < kRanges; e += kPartThreads) slices[part * kRanges + e] = s_bins[e];
         if (!last_of(&o.tickets[0], a.n_parts, tid, &s_last)) continue;
-        for (int e = tid; e < kFinishBins; e += kPartThreads) {
-            u64 sum = 0;
-            for (int j = 0; j < a.n_parts; ++j) sum += slices[j * kFinishBins + e];
-            s_bins[e] = sum;
+        const Params q = params_of(a, i / a.per);
+        const bool count = o.type == BY_COUNT;
+        // what the ranges hold, four a thread, and where the limit falls
+        static_assert(kRanges == 4 * kPartThreads);
+        uint4 n = {0, 0, 0, 0};
+#pragma unroll 8
+        for (int j = 0; j < a.n_parts; ++j) {
+            const uint4 m = *(const uint4*)(slices + j * kRanges + 4 * tid);
+            n.x += m.x;
+            n.y += m.y;
+            n.z += m.z;
+            n.w += m.w;
         }
-        __syncthreads();
-        // every wave for itself, 8 ranges a lane
-        constexpr int PER = kFinishBins / 64;
-        u64 v[PER], mine = 0;
+        const u32 each[4] = {n.x, n.y, n.z, n.w};
+        double v[4], mine = 0.0;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) mine += v[e] = s_bins[PER * lane + e];
-        const u64 up = wave_scan_u64(mine, lane), all = of_lane(up, 63);
-        u64 left;
-        bool good = all > 0;
-        if (count) {
-            good = good && q.k > o.listed;
-            left = (u64)max(q.k - o.listed, 1);
-        } else {
-            const double at_ref = exp_neg((range_of.ref - (double)o.top) * q.inv), unit = ldexp(1.0, -sum_bits(a.vocab)) * at_ref, known = (double)o.listed_q * 0x1p-50;
-            const double rest = (double)q.p * (known + (double)all * unit) - known;
-            good = good && rest > 0.0;
-            left = (u64)fmax(ceil(rest / unit), 1.0);
+        for (int e = 0; e < 4; ++e) {
+            const double middle = (double)range_of.ref - (4 * tid + e + 0.5) / (double)range_of.per_unit;
+            mine += v[e] = (double)each[e] * (count ? 1.0 : exp_neg(fmin((middle - (double)o.top) * q.inv, 0.0)));
         }
-        u64 at = up - mine, before = 0;
+        const double limit = count ? (double)(q.k - o.listed) : (double)q.p * o.total - (double)o.listed_q * 0x1p-50, up = wave_scan64_dpp(mine);
+        if (lane == 63) s_sum[wave] = up;
+        __syncthreads();
+        double at = up - mine;
+        for (int w = 0; w < wave; ++w) at += s_sum[w];
         int last = -1;
 #pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            if (v[e] && at < left) {
-                last = PER * lane + e;
-                before = at;
-            }
+        for (int e = 0; e < 4; ++e) {
+            if (v[e] > 0.0 && at < limit) last = 4 * tid + e;
             at += v[e];
         }
-        const u64 have = __ballot(last >= 0);
-        if (!good || !have) {
-            if (tid == 0) o.state = ROW_SLOW;
-            continue;
-        }
-        const int from = 63 - __clzll(have), b = __builtin_amdgcn_readlane(last, from);
-        before = of_lane(before, from);
-        const float ref = (float)range_of.ref;
-        const u32 lo = first_key(ref, lane, [&](float x) { return range_of(x) <= b; });
-        const float x_hi = b == 0 ? below : from_key(first_key(ref, lane, [&](float x) { return range_of(x) < b; }));
+        for (int f = 32; f > 0; f >>= 1) last = max(last, __shfl_xor(last, f));
+        if (lane == 0) s_at[wave] = last;
+        __syncthreads();
+        const int b = max(max(s_at[0], s_at[1]), max(s_at[2], s_at[3]));
+        const bool good = b >= 0 && limit > 0.0;
+        const u32 lo = first_key(range_of.ref, lane, [&](float x) { return range_of(x) <= b + 1; });
+        const float x_hi = b <= 1 ? below : from_key(first_key(range_of.ref, lane, [&](float x) { return range_of(x) < b - 1; }));
         if (tid == 0) {
-            if (o.x_m >= x_hi) {                            // min-p keeps less
+            if (!good) {
+                o.state = ROW_SLOW;
+            } else if (o.x_m >= x_hi) {                     // min-p keeps less
                 o.type = BY_SHARE;
             } else {
                 o.x_lo = from_key(lo);
                 o.x_hi = x_hi;
-                o.left = left - before;
             }
         }
     }
 }
 
 // The range's tokens and what lies above it; the last workgroup of a row finds the cut, and draws
+// A workgroup a part, then a row: bound by the exponentials of what is kept, and the last workgroups' chains of reads.
 template <typename T, bool VEC, bool MASK>
 __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
     using R = Run<T, VEC>;
@@ -1240,7 +1318,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
             for (int e = 0; e < kPer; ++e) {
                 if (x[e] >= x_hi) {
                     ++above;
-                    if (!MASK) sum += weight(x[e]);
+                    sum += weight(x[e]);
                 }
                 const bool in = x[e] >= x_lo && x[e] < x_hi;
                 const u64 m = __ballot(in);
@@ -1272,15 +1350,9 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         int n_above = lane < a.n_parts ? a.parts[(int64_t)i * a.n_parts + lane].above : 0;
         for (int f = 32; f > 0; f >>= 1) n_above += __shfl_xor(n_above, f);
         bool over = false;
-        for (int l = wave; l < a.n_parts * kPartWaves; l += kPartWaves) {
-            const int n = a.parts[(int64_t)i * a.n_parts + l / kPartWaves].listed[l % kPartWaves];
-            over |= n > a.list_len;
-            int at = 0;
-            if (lane == 0) at = atomicAdd(&s.n, n);
-            at = __builtin_amdgcn_readfirstlane(at);
-            for (int e = lane; e < min(n, a.list_len); e += 64)
-                if (at + e < kList) s.list[at + e] = lists[(int64_t)l * a.list_len + e];
-        }
+        for (int l = tid; l < a.n_parts * kPartWaves; l += kFinishThreads) over |= a.parts[(int64_t)i * a.n_parts + l / kPartWaves].listed[l % kPartWaves] > a.list_len;
+        over = __any(over);
+        read_lists(a, i, wave, lane, (1ull << 56) - 1, [&](bool in, u64 c) { append_to(s, in, c, lane); });
         if (over && lane == 0) atomicAdd(&s.n, kList);
         __syncthreads();
         const int n = s.n;
@@ -1288,13 +1360,25 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
             if (tid == 0) o.state = ROW_SLOW;
             continue;
         }
-        const TableWeight at_ref(s_pow, o.ref < __builtin_inff() ? o.ref : o.top, q.inv, bits);      // (k_filter_bins' numbers)
         u64 cut = (u64)~key_of(x_hi) << 24 | 0xFFFFFF;      // (x_hi itself is above)
+        bool good = true;
         if (o.type != BY_SHARE) {
             const bool count = o.type == BY_COUNT;
-            cut = last_item(s, n, (u64)~(key_of(x_hi) - 1) << 24, (u64)~key_of(x_lo) << 24 | 0xFFFFFF, o.left, tid, [&](int e) { return s.list[e]; },
-                            [&](int e) { return count ? 1ull : at_ref(logit_of(s.list[e])); }).key;
+            const u64 over_q = wave_sum_u64(s_part[lane]);
+            u64 mine = 0;
+            for (int e = tid; e < n; e += kFinishThreads) mine += count ? 1 : weight(logit_of(s.list[e]));
+            const u64 listed = block_sum(s, mine, 0, tid).q;
+            // what the range may still keep; the cut lies in it if something, and no more than it has
+            const double left = count ? (double)(q.k - n_above) : ceil((double)q.p * o.total * ldexp(1.0, bits)) - (double)over_q;
+            good = n > 0 && left >= 1.0 && left <= (double)listed;
+            if (good)
+                cut = last_item(s, n, (u64)~(key_of(x_hi) - 1) << 24, (u64)~key_of(x_lo) << 24 | 0xFFFFFF, (u64)left, tid, [&](int e) { return s.list[e]; },
+                                [&](int e) { return count ? 1ull : weight(logit_of(s.list[e])); }).key;
             if (q.by_share) cut = min(cut, (u64)~key_of(o.x_m) << 24 | 0xFFFFFF);
+        }
+        if (!good) {
+            if (tid == 0) o.state = ROW_SLOW;
+            continue;
         }
         int kept = 0;
         for (int e = tid; e < n; e += kFinishThreads) {
@@ -1308,15 +1392,13 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         float logp = 0.f;
         if (!MASK) {
             const float u = a.u[i];
-            const u64 own = s_part[lane], up = wave_scan_u64(own, lane), total = of_lane(up, 63);
+            const u64 own = s_part[lane], up = wave_scan_u64(own), total = of_lane(up, 63);
             const u64 target = u > 0.f ? min((u64)((double)u * (double)total), total - 1) : 0;
             const int of = __ffsll((unsigned long long)__ballot(up > target)) - 1, first = of * a.part_len, len = min(a.part_len, a.vocab - first);
             const float cut_x = logit_of(cut);
             const int cut_v = token_of(cut);
-            token = first + (int)last_item(s, len, 0, (u64)len - 1, target - of_lane(up - own, of) + 1, tid, [](int e) { return (u64)e; }, [&](int e) {
-                const float x = to_f(row[first + e]);
-                return x > cut_x || (x == cut_x && first + e <= cut_v) ? weight(x) : 0;
-            }).key;
+            token = draw_part<T, VEC>(s, row, first, run, first + len, target - of_lane(up - own, of), tid,
+                                      [&](float x, int v) { return x > cut_x || (x == cut_x && v <= cut_v) ? weight(x) : 0; });
             logp = (float)(((double)to_f(row[token]) - (double)o.top) * q.inv - log((double)total * ldexp(1.0, -bits)));
         }
         if (tid == 0) {
@@ -1341,27 +1423,39 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_apply(FilterArgs a) {
     const int end = min((int)(blockIdx.x + 1) * a.part_len, a.vocab);
     const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
     T* const out = (T*)a.out + (int64_t)i * a.out_stride;
-    for (int v = blockIdx.x * a.part_len + threadIdx.x; v < end; v += kPartThreads) {
-        const T x = IN_PLACE ? out[v] : row[v];
-        const bool in = to_f(x) > -__builtin_inff() && comp_of(to_f(x), v) <= cut;
-        if (IN_PLACE && !in) out[v] = from_f<T>(-__builtin_inff());
-        if (!IN_PLACE && in) out[v] = x;
+    constexpr int AHEAD = 8;
+    for (int v0 = blockIdx.x * a.part_len + threadIdx.x; v0 < end; v0 += AHEAD * kPartThreads) {
+        T x[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j)
+            if (v0 + j * kPartThreads < end) x[j] = row[v0 + j * kPartThreads];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int v = v0 + j * kPartThreads;
+            if (v >= end) continue;
+            const bool in = to_f(x[j]) > -__builtin_inff() && comp_of(to_f(x[j]), v) <= cut;
+            if (IN_PLACE && !in) out[v] = from_f<T>(-__builtin_inff());
+            if (!IN_PLACE && in) out[v] = x[j];
+        }
     }
 }
 
 // How a call is cut: parts of kPart logits, up to kMostParts; lists that hold three times what the sample should let through
 struct Plan { int direct, n_parts, part_len, list_len, sample_len, sample_rank; };
-Plan plan_of(int vocab) {
+Plan plan_of(int rows, int vocab) {
     Plan p{};
     p.direct = vocab <= kList;
     if (p.direct) return p;
-    p.n_parts = std::min((vocab - 1) / kPart + 1, kMostParts);
+    // parts of up to kPart logits; smaller ones, down to kLeastPart, where the rows alone do not fill the chip
+    const int most = std::min((vocab - 1) / kLeastPart + 1, kMostParts), least = std::min((vocab - 1) / kPart + 1, kMostParts);
+    p.n_parts = std::max(least, std::min(most, kFillParts / rows));
     p.part_len = ((vocab - 1) / (p.n_parts * kPartWaves) / 16 + 1) * 16 * kPartWaves;    // (waves' runs alike, as whole vectors)
-    // 1500 of the row, a share f of its logits: a group's largest lies among them with probability 1 - (1 - f)^n
-    const double f = 1500.0 / vocab;
+    // kWanted of the row, a share f of its logits: a group's largest lies among them with probability 1 - (1 - f)^n
+    const double f = (double)kWanted / vocab;
     p.sample_len = f < 0.015 ? 4 : f < 0.03 ? 2 : 1;
     p.sample_rank = std::min(kGroups, std::max(1, (int)(kGroups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
-    p.list_len = std::max(192, kList / (p.n_parts * kPartWaves));
+    // eight times what a wave should find, room for k_filter_bins' counts, and no more than there is
+    p.list_len = std::max(kRanges / 2 / kPartWaves, (8 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16);
     return p;
 }
 size_t lists_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * kPartWaves * p.list_len * sizeof(u64); }
@@ -1370,7 +1464,7 @@ size_t parts_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * 
 template <typename T, bool MASK>
 tasc_status enqueue(FilterArgs a, int rows, void* workspace, hipStream_t st) {
     const bool vec = (((uintptr_t)a.logits | (uintptr_t)(a.row_stride * (int64_t)sizeof(T))) & 15) == 0;
-    const Plan p = plan_of(a.vocab);
+    const Plan p = plan_of(rows, a.vocab);
     a.direct = p.direct;
     a.in_place = MASK && a.out == a.logits;
     const dim3 all((unsigned)rows), threads(kPartThreads), parts((unsigned)p.n_parts, (unsigned)rows);
@@ -1388,7 +1482,7 @@ tasc_status enqueue(FilterArgs a, int rows, void* workspace, hipStream_t st) {
         if (MASK && !a.in_place) vec ? k_filter_parts<T, true, true><<<parts, threads, 0, st>>>(a) : k_filter_parts<T, false, true><<<parts, threads, 0, st>>>(a);
         else vec ? k_filter_parts<T, true, false><<<parts, threads, 0, st>>>(a) : k_filter_parts<T, false, false><<<parts, threads, 0, st>>>(a);
     }
-    k_filter_finish<T, MASK><<<all, dim3(kFinishThreads), 0, st>>>(a);
+    vec ? k_filter_finish<T, true, MASK><<<all, dim3(kFinishThreads), 0, st>>>(a) : k_filter_finish<T, false, MASK><<<all, dim3(kFinishThreads), 0, st>>>(a);
     if (!p.direct) {
         if (a.top_k || a.top_p || a.min_p) {
             const dim3 some((unsigned)std::min<int64_t>((int64_t)rows * p.n_parts, kWideGrid));
@@ -1427,7 +1521,7 @@ tasc_status check_workspace(const char* who, void* workspace, size_t ws_bytes, i
 
 extern "C" size_t tasc_sample_workspace_bytes(int32_t rows, int32_t vocab) {
     if (rows < 1 || rows > 65535 || vocab < 2 || vocab > 1 << 24) return 0;
-    const Plan p = plan_of(vocab);
+    const Plan p = plan_of(rows, vocab);
     return p.direct ? 0 : parts_bytes(p, rows) + (size_t)rows * sizeof(RowOut) + lists_bytes(p, rows) + ((size_t)rows + 1) * sizeof(int32_t);
 }
 
