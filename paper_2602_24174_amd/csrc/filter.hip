@@ -4,7 +4,7 @@
 // the largest comes first, over the index.  Every filter keeps a prefix of that order, so all of them together come to one last comp, `cut`.
 //
 // k_filter_parts reads every logit once, a workgroup up to 16384 of them: the largest, the sum of the weights where it is wanted, and a list of those
-// above a bound that it takes from a sample, about 700 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always the
+// above a bound that it takes from a sample, about 900 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always the
 // cut lies in them.  Rows whose cut does not (flat distributions: thousands of tokens kept) are listed for two kernels that read them again, parts side by
 // side: k_filter_bins sums the weights (or counts) of 512 ranges of values, its last workgroup of a row finds the range in which the cut lies; k_filter_gather
 // lists that range's tokens and sums what is above it, its last workgroup finds the cut and draws.  k_filter_slow, a workgroup a row, serves what is left (ties of
@@ -20,11 +20,11 @@
 namespace {
 
 constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096, kWideList = 2048;
-constexpr int kListBits = 50;                              // a list's weights: 2^12 of them stay below 2^62
+constexpr int kListBits = 50;                              // a list's weights: 2^11 of them stay below 2^62
 // a workgroup of k_filter_parts, its waves' shares; lists of a row together, and entries that k_filter_finish takes
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPer = 16, kStep = 64 * kPer;
-constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 2048, kMostParts = 64, kList = 4096, kGroups = 64, kWanted = 768;
-constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64, kRanges = 1024, kWideGrid = 1024;
+constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 1024, kMostParts = 64, kList = 2048, kGroups = 64, kWanted = 1024;
+constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64, kRanges = 2048, kWideGrid = 2048;
 
 // What a part of a row comes to
 struct __attribute__((aligned(16))) Part {
@@ -36,7 +36,7 @@ struct __attribute__((aligned(16))) Part {
     float least;                     // the sample's least logit
     int32_t above;                   // k_filter_gather's: the logits above the range, and their weights
     int32_t pad;
-    u64 above_q;
+    u64 above_q[kPartWaves];
 };
 // and a row: kept are the tokens up to `cut`
 enum { ROW_DONE = 0, ROW_CUT = 1, ROW_BAD = 2, ROW_WIDE = 3, ROW_SLOW = 4 };     // CUT: what is kept is not in the lists
@@ -109,6 +109,13 @@ template <int CTRL, int ROWS = 0xF>
 __device__ __forceinline__ u64 dpp_u64(u64 v) { return __builtin_bit_cast(u64, lane64_dpp<CTRL, ROWS>(__builtin_bit_cast(double, v))); }
 __device__ __forceinline__ u64 of_lane(u64 v, int l) {     // l: the same in all lanes
     return (u64)(u32)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 | (u32)__builtin_amdgcn_readlane((int)(u32)v, l);
+}
+__device__ __forceinline__ int wave_sum_int(int v) {
+    v += __builtin_amdgcn_update_dpp(0, v, 0xB1, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x4E, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x141, 0xF, 0xF, false);
+    v += __builtin_amdgcn_update_dpp(0, v, 0x140, 0xF, 0xF, false);
+    return __builtin_amdgcn_readlane(v, 0) + __builtin_amdgcn_readlane(v, 16) + __builtin_amdgcn_readlane(v, 32) + __builtin_amdgcn_readlane(v, 48);
 }
 __device__ __forceinline__ u64 wave_sum_u64(u64 v) {
     v += dpp_u64<0xB1>(v);                                  // quad_perm [1,0,3,2], [2,3,0,1], row_half_mirror, row_mirror
@@ -663,17 +670,17 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
     const float group = s_group[lane];
     const float anchor = wave_max_dpp(group);
     if (wave == 0) {
-        int above = 0;                                      // groups before this one in descending order
-#pragma unroll 16
-        for (int g = 0; g < kGroups; ++g) {
-            const float x = __builtin_bit_cast(float, __builtin_amdgcn_readlane(__builtin_bit_cast(int, group), g));
-            above += x > group || (x == group && g < lane);
-        }
-        if (above == (q.one ? 0 : a.sample_rank - 1)) s_bound = group;
+        // the largest bound that so many groups reach, by the upper half of its bits
+        const u32 key = key_of(group);
+        const int rank = q.one ? 1 : a.sample_rank;
+        u32 at = 0;
+        for (u32 bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
+            if (__popcll(__ballot(key >= (at | bit))) >= rank) at |= bit;
+        if (lane == 0) s_bound = at > key_of(-__builtin_inff()) ? from_key(at) : -__builtin_inff();
     }
     __syncthreads();
     // (a NaN among the sample leaves the bound to chance; the row is refused all the same)
-    const float bound = all ? __builtin_inff() : s_bound;
+    const float bound = all ? __builtin_inff() : s_bound, reach = fmaxf(bound, -3.4028234663852886e38f);      // (-infinity is not listed)
     const double unit = q.inv * 369.3299304675746;          // 256 / ln 2
     const double whole = anchor > -__builtin_inff() && anchor < __builtin_inff() ? rint((double)anchor * unit) : 0.0, start = 0x1.8p52 - whole;
     const bool sums = want_sum && q.good && q.inv > 1e-20 && fabs(whole) < 0x1p24;
@@ -701,14 +708,20 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
                         if (v + f < v_end) out[v + f] = from_f<T>(-__builtin_inff());
             }
         }
-        float most = x[0];
+        float most = x[0], low = x[0];                      // (a NaN stays one)
 #pragma unroll
-        for (int e = 0; e < kPer; ++e) {
-            bad |= !(x[e] < __builtin_inff());
-            live += __popcll(__ballot(x[e] > -__builtin_inff()));
-            most = fmaxf(most, x[e]);
+        for (int e = 0; e < kPer; e += 2) {
+            asm("v_maximum3_f32 %0, %1, %2, %3" : "=v"(most) : "v"(most), "v"(x[e]), "v"(x[e + 1]));
+            asm("v_minimum3_f32 %0, %1, %2, %3" : "=v"(low) : "v"(low), "v"(x[e]), "v"(x[e + 1]));
         }
+        bad |= !(most < __builtin_inff());
         top = fmaxf(top, most);
+        if (__any(!(low > -__builtin_inff()))) {
+#pragma unroll
+            for (int e = 0; e < kPer; ++e) live += __popcll(__ballot(x[e] > -__builtin_inff()));
+        } else {
+            live += kStep;
+        }
         if (sums) {
 #pragma unroll
             for (int e = 0; e < kPer; ++e) {
@@ -716,10 +729,10 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
                 sum = times_power(s_pow, small_power(__builtin_fma(y, unit, start - big)), (u32)__builtin_bit_cast(u64, big), sum);
             }
         }
-        if (!__any(most >= bound)) continue;
+        if (!__any(most >= reach)) continue;
 #pragma unroll
         for (int e = 0; e < kPer; ++e) {
-            const bool in = x[e] >= bound && x[e] > -__builtin_inff();
+            const bool in = x[e] >= reach;
             const u64 m = __ballot(in);
             if (!m) continue;
             const int at = listed + __builtin_amdgcn_mbcnt_hi((u32)(m >> 32), __builtin_amdgcn_mbcnt_lo((u32)m, 0));
@@ -748,7 +761,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
     for (int w = 0; w < kPartWaves; ++w) {
         o.live += s_live[w];
         o.bad |= s_bad[w];
-        o.listed[w] = min(s_listed[w], a.list_len);
+        o.listed[w] = s_listed[w];
         if (s_listed[w] > a.list_len) o.bound = __builtin_inff();
     }
     // (weights up to 2^781 of the sample's largest: beyond that the sum says nothing)
@@ -759,7 +772,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
 
 // ---------------------------------------------------------------- a row from its lists
 struct __attribute__((aligned(16))) FinishShared {
-    u64 list[kList];
+    u64 list[kList], weight[kList];
     u64 bins[kFinishBins];
     u64 few_key[kFew], few_q[kFew];
     u64 red[kFinishWaves];
@@ -776,11 +789,18 @@ __device__ __forceinline__ void append_to(FinishShared& s, bool in, u64 c, int l
 struct Found { u64 key, sum; };      // sum: up to it and with it
 
 // Of n items with weights q (0: not there), in the order of their keys within [lo, hi]: the last whose sum of those before it is below `limit`
-template <typename Key, typename Weight>
+// (FEW: there are no more than kFew of them).
+template <bool FEW, typename Key, typename Weight>
 __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 hi, u64 limit, int tid, Key key, Weight weight) {
     const int lane = tid & 63;
     u64 sum = 0;
+    if (FEW) {
+        __syncthreads();
+        if (tid == 0) s.few = 0;
+        __syncthreads();
+    }
     for (;;) {
+        if (!FEW) {
         const int shift = max(0, 64 - 9 - __clzll((long long)(hi - lo)));
         static_assert(kFinishBins == 1 << 9);
         __syncthreads();                                    // (bins and few are still looked at)
@@ -822,6 +842,7 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
         lo += (u64)b << shift;
         hi = min(hi, lo + ((1ull << shift) - 1));
         if (shift == 0) return Found{lo, sum + own};
+        }
         for (int i = tid; i < n; i += kFinishThreads) {
             const u64 c = key(i);
             if (c < lo || c > hi) continue;
@@ -835,21 +856,26 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
         }
         __syncthreads();
         const int few = s.few;
-        if (few > kFew) continue;
+        if (!FEW && few > kFew) continue;
         const u64 c = lane < few ? s.few_key[lane] : ~0ull, q = lane < few ? s.few_q[lane] : 0;
         u64 below = 0;
-        for (int j = 0; j < few; ++j) below += of_lane(c, j) < c ? of_lane(q, j) : 0;
-        // the largest key among those that are kept
-        u64 best = lane < few && below < limit ? c : 0;
-        for (int o = 32; o > 0; o >>= 1) best = max(best, (u64)__shfl_xor(best, o));
-        const int l = __ffsll((unsigned long long)__ballot(lane < few && c == best)) - 1;
-        return Found{best, sum + of_lane(below, l) + of_lane(q, l)};
+        int rank = 0;
+        for (int j = 0; j < few; ++j) {
+            const bool less = of_lane(c, j) < c;
+            below += less ? of_lane(q, j) : 0;
+            rank += less;
+        }
+        // the last of those that are kept
+        const bool kept = lane < few && below < limit;
+        const int l = __ffsll((unsigned long long)__ballot(kept && rank == __popcll(__ballot(kept)) - 1)) - 1;
+        if (l < 0) return Found{lo, sum};                   // (no items)
+        return Found{of_lane(c, l), sum + of_lane(below, l) + of_lane(q, l)};
     }
 }
 struct Sum { u64 q; int n; };
 __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid) {
     q = wave_sum_u64(q);
-    for (int o = 32; o > 0; o >>= 1) n += __shfl_xor(n, o);
+    n = wave_sum_int(n);
     __syncthreads();
     if ((tid & 63) == 0) {
         s.red[tid >> 6] = q;
@@ -859,31 +885,56 @@ __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid)
     return Sum{s.red[0] + s.red[1] + s.red[2] + s.red[3], s.num[0] + s.num[1] + s.num[2] + s.num[3]};
 }
 
-// The entries up to `last` of a row's lists, a wave every fourth list, the first 64 of 8 lists at a time: append(whether there is one, it)
-template <typename Append>
-__device__ __forceinline__ void read_lists(const FilterArgs& a, int i, int wave, int lane, u64 last, Append append) {
+// A row's lists one behind the other in s.list, entries beyond `last` as none (~0): how many places, or -1 if they do not fit or one of them is not whole;
+// s.n counts the others.  A thread a list for their lengths, then a thread an entry.
+__device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, int i, int tid, u64 last) {
+    static_assert(kMostParts * kPartWaves <= kFinishThreads && kFinishThreads <= kFinishBins);
     const Part* const parts = a.parts + (int64_t)i * a.n_parts;
-    const int n_lists = a.n_parts * kPartWaves;
+    const int n_lists = a.n_parts * kPartWaves, lane = tid & 63, wave = tid >> 6;
     const u64* const lists = a.lists + (int64_t)i * n_lists * a.list_len;
-    for (int l0 = wave; l0 < n_lists; l0 += 8 * kFinishWaves) {
-        u64 c[8];
-        int n[8];
+    const int own = tid < n_lists ? parts[tid / kPartWaves].listed[tid % kPartWaves] : 0;
+    // the sums of the lengths; bit 32 of a sum: a list that is not whole
+    const u64 up = wave_scan_u64((u64)(u32)own | (own > a.list_len ? 1ull << 32 : 0));
+    if (lane == 63) s.red[wave] = up;
+    if (tid == 0) s.n = 0;
+    __syncthreads();
+    u64 before = 0, all = 0;
+    for (int w = 0; w < kFinishWaves; ++w) {
+        if (w == wave) before = all;
+        all += s.red[w];
+    }
+    const int n = (int)(u32)all;
+    if (all >> 32 || n > kList) return -1;
+    u32* const ends = (u32*)s.bins;
+    ends[tid] = (u32)(before + up);
+    __syncthreads();
+    int valid = 0;
+    constexpr int AHEAD = 4;
+    for (int e0 = tid; e0 < n; e0 += AHEAD * kFinishThreads) {
+        int l[AHEAD] = {};                                  // lists that end at or before the entry
 #pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            const int l = l0 + j * kFinishWaves;
-            n[j] = l < n_lists ? min(parts[l / kPartWaves].listed[l % kPartWaves], a.list_len) : 0;
+        for (int step = kFinishThreads / 2; step > 0; step /= 2)
+#pragma unroll
+            for (int j = 0; j < AHEAD; ++j)
+                if (ends[l[j] + step - 1] <= (u32)(e0 + j * kFinishThreads)) l[j] += step;
+        u64 c[AHEAD];
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const int e = e0 + j * kFinishThreads;
+            c[j] = e < n ? lists[(int64_t)l[j] * a.list_len + (e - (l[j] > 0 ? (int)ends[l[j] - 1] : 0))] : ~0ull;
         }
 #pragma unroll
-        for (int j = 0; j < 8; ++j) c[j] = lane < n[j] ? lists[(int64_t)(l0 + j * kFinishWaves) * a.list_len + lane] : ~0ull;
-#pragma unroll
-        for (int j = 0; j < 8; ++j) {
-            append(c[j] <= last, c[j]);
-            for (int e = 64; e < n[j]; e += 64) {
-                const u64 more = e + lane < n[j] ? lists[(int64_t)(l0 + j * kFinishWaves) * a.list_len + e + lane] : ~0ull;
-                append(more <= last, more);
-            }
+        for (int j = 0; j < AHEAD; ++j) {
+            const int e = e0 + j * kFinishThreads;
+            if (e >= n) continue;
+            s.list[e] = c[j] <= last ? c[j] : ~0ull;
+            valid += c[j] <= last;
         }
     }
+    valid = wave_sum_int(valid);
+    if (lane == 0) atomicAdd(&s.n, valid);
+    __syncthreads();
+    return n;
 }
 
 // The first of the logits [p0, end) whose weights up to it sum to more than `target` (the last with any if none does): the sums of the waves' steps, then the
@@ -964,7 +1015,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
     if (tid == 0) s.n = s.bad = 0;
     __syncthreads();
     // the list, and what is known of the row
-    int live = 0;
+    int live = 0, n = 0;
     bool bad = !p.good, whole = true, has_sum = true;       // whole: the list holds all that are not masked
     float top = -__builtin_inff(), bound = -__builtin_inff();
     float least = __builtin_inff();
@@ -1005,23 +1056,23 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         top = wave_max_dpp(top);
         bound = wave_max_dpp(bound);
         least = -wave_max_dpp(-least);
-        for (int o = 32; o > 0; o >>= 1) live += __shfl_xor(live, o);
-        if (bound < __builtin_inff())
-            read_lists(a, i, wave, lane, (u64)~key_of(bound) << 24 | 0xFFFFFF, append);
-        __syncthreads();
+        live = wave_sum_int(live);
+        if (bound < __builtin_inff()) n = read_lists(s, a, i, tid, (u64)~key_of(bound) << 24 | 0xFFFFFF);
+        if (n < 0) bound = __builtin_inff();
         whole = bound == -__builtin_inff();
     }
-    const int n = min(s.n, kList);
-    bool wide = !a.direct && s.n > kList;
-    bool nothing_listed = !a.direct && bound == __builtin_inff();
+    // places of the list, some of them empty
+    if (a.direct) n = s.n;
+    const int valid = bound < __builtin_inff() ? s.n : 0;
+    const bool nothing_listed = bound == __builtin_inff();
+    bool wide = false;
     bad |= live == 0;
-    wide = wide && !bad;
     RowState r{};
     r.top = top + 0.f;
     r.inv = p.inv;
     int token = -1, kept = 0;
     float logp = __builtin_nanf("");
-    u64 cut = ~0ull, listed_q = 0;
+    u64 cut = (1ull << 56) - 1, listed_q = 0;
     float x_m = -__builtin_inff();
     double total = 0.0;                                     // of all weights
     int type = -1;                                          // of a wide row that the kernels behind this one serve
@@ -1029,10 +1080,14 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         const bool by_count = p.by_count && p.k < live, any = p.one || by_count || p.by_mass || p.by_share;
         const u64 lo = (u64)~key_of(r.top) << 24, hi = a.direct || whole ? ((1ull << 56) - 1) : (u64)~key_of(bound) << 24 | 0xFFFFFF;
         auto comp = [&](int e) { return s.list[e]; };
-        auto weight = [&](int e) { return weight_of(r, logit_of(s.list[e]), kListBits); };
-        auto cut_weight = [&](int e) { return s.list[e] <= cut ? weight(e) : 0; };
+        auto weight = [&](int e) { return s.weight[e]; };
         bool held = whole;                                  // the list holds all that the filters so far keep
         if (p.by_share) x_m = from_key(first_key(r.top, lane, [&, most = -log((double)p.m)](float x) { return ((double)r.top - (double)x) * r.inv <= most; }));
+        // the weights, 0 for an empty place; each is looked at by the thread that sets it, up to last_item's barriers
+        if (!nothing_listed && (p.by_mass || !MASK)) {
+#pragma unroll 4
+            for (int e = tid; e < n; e += kFinishThreads) s.weight[e] = s.list[e] <= hi ? weight_of(r, logit_of(s.list[e]), kListBits) : 0;
+        }
         if (nothing_listed) {
             wide = any || MASK || !has_sum;
         } else if (!wide) {
@@ -1047,8 +1102,8 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
                 held = true;
             }
             if (by_count) {
-                if (p.k <= n) {
-                    cut = last_item(s, n, lo, hi, (u64)p.k, tid, comp, [](int) { return 1ull; }).key;
+                if (p.k <= valid) {
+                    cut = last_item<false>(s, n, lo, hi, (u64)p.k, tid, comp, [](int) { return 1ull; }).key;
                     held = true;
                 } else if (!held) {
                     wide = true;
@@ -1056,13 +1111,13 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             }
             if (p.by_mass && !wide) {
                 u64 mine = 0;
-                for (int e = tid; e < n; e += kFinishThreads) mine += cut_weight(e);
+                for (int e = tid; e < n; e += kFinishThreads) mine += s.list[e] <= cut ? weight(e) : 0;
                 const u64 listed = listed_q = block_sum(s, mine, 0, tid).q;
                 double limit = 0.0;
                 if (held) {
                     limit = ceil((double)p.p * (double)listed);
                 } else if (has_sum) {
-                    total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0);
+                    total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp_neg(part_scale - (double)r.top * r.inv) : 0.0);
                     limit = ceil((double)p.p * total * 0x1p50);
                     static_assert(kListBits == 50);
                     wide = !((double)listed >= limit);
@@ -1070,7 +1125,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
                     wide = true;
                 }
                 if (!wide) {
-                    cut = last_item(s, n, lo, min(hi, cut), (u64)fmax(limit, 1.0), tid, comp, weight).key;
+                    cut = last_item<false>(s, n, lo, min(hi, cut), (u64)fmax(limit, 1.0), tid, comp, weight).key;
                     held = true;
                 }
             }
@@ -1082,11 +1137,10 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         }
         if (wide) {
             type = !any ? -1 : by_count ? (p.by_mass ? -1 : BY_COUNT) : p.by_mass ? (has_sum ? BY_MASS : -1) : p.by_share ? BY_SHARE : -1;
-            if (type == BY_MASS) total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0);
-            if (nothing_listed || s.n > kList) bound = __builtin_inff();
-            if (bound == __builtin_inff()) listed_q = 0;
+            if (type == BY_MASS) total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp_neg(part_scale - (double)r.top * r.inv) : 0.0);
+            if (nothing_listed) listed_q = 0;
         } else if (nothing_listed) {                        // nothing is dropped: the part that the draw falls into, read again
-            const double own = part_sum > 0.0 ? part_sum * exp(part_scale - (double)r.top * r.inv) : 0.0, up = wave_scan64_dpp(own);
+            const double own = part_sum > 0.0 ? part_sum * exp_neg(part_scale - (double)r.top * r.inv) : 0.0, up = wave_scan64_dpp(own);
             const double total = lane64(up, 63), target = fmin(fmax((double)a.u[i], 0.0), 1.0) * total;
             const u64 past = __ballot(up > target), some = __ballot(own > 0.0);
             const int part = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(some);
@@ -1108,8 +1162,12 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             if (!MASK) {
                 const float u = a.u[i];
                 const u64 limit = u > 0.f ? min((u64)((double)u * (double)all.q), all.q - 1) + 1 : 1;
-                token = (int)last_item(s, n, 0, (u64)a.vocab - 1, limit, tid, [&](int e) { return (u64)token_of(s.list[e]); }, cut_weight).key;
-                logp = p.one ? 0.f : (float)(((double)to_f(row[token]) - (double)r.top) * r.inv - log((double)all.q * 0x1p-50));
+                auto token_at = [&](int e) { return s.list[e] <= cut ? (u64)token_of(s.list[e]) << 32 | (u32)e : ~0ull; };
+                const Found f = kept <= kFew ? last_item<true>(s, n, 0, ~0ull - 1, limit, tid, token_at, weight)
+                                             : last_item<false>(s, n, 0, (u64)a.vocab << 32, limit, tid, token_at, weight);
+                token = (int)(f.key >> 32);
+                const float x = logit_of(s.list[(u32)f.key]);
+                logp = p.one ? 0.f : (float)(((double)x - (double)r.top) * r.inv - log((double)all.q * 0x1p-50));
             }
         }
     }
@@ -1131,13 +1189,13 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
     if (tid != 0) return;
     if (!a.direct) {
         RowOut o{};
-        o.cut = keep_all ? (1ull << 56) - 1 : cut;
+        o.cut = cut;
         o.state = bad ? ROW_BAD : keep_all ? ROW_CUT : !wide ? ROW_DONE : type < 0 ? ROW_SLOW : ROW_WIDE;
         o.type = type;
         o.top = r.top;
         o.ref = bound;
         o.least = least;
-        o.listed = bound == __builtin_inff() ? 0 : n;
+        o.listed = valid;
         o.listed_q = listed_q;
         o.total = total;
         o.x_lo = o.x_hi = o.x_m = x_m;
@@ -1188,16 +1246,15 @@ __device__ __forceinline__ bool last_of(int32_t* ticket, int n, int tid, int32_t
     return *s_last != 0;
 }
 
-// Counts of the ranges; the last workgroup of a row finds the one with the cut, by the counts times the weight at each range's middle.  Ranges are so narrow
-// (0.01 of a logit, 400 tokens, for 150,000 tokens over 10) that this is off by a token or so: that range and its neighbours go to k_filter_gather, which
-// has exact sums and sees whether the cut lies in them.  Bound by the LDS atomics.
+// Counts of the ranges; the last workgroup of a row finds those in which the cut may lie, by the counts times the weights at a range's ends: ranges are narrow
+// (0.005 of a logit, 200 tokens, for 150,000 tokens over 10), so that a few are left for k_filter_gather, which has exact sums.  Bound by the LDS atomics.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
     using R = Run<T, VEC>;
     __shared__ u32 s_bins[kRanges];
     __shared__ int32_t s_last;
-    __shared__ double s_sum[kPartWaves];
-    __shared__ int32_t s_at[kPartWaves];
+    __shared__ double s_sum[2][kPartWaves];
+    __shared__ int32_t s_at[2][kPartWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int items = *a.wide * a.n_parts;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
@@ -1223,47 +1280,73 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
                 if (x[e] < below && x[e] > -__builtin_inff()) atomicAdd(&s_bins[range_of(x[e])], 1u);
         }
         __syncthreads();
+        // (16 bits a count: one that does not fit only makes the ranges miss the cut)
         u32* const slices = (u32*)(a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len);
-        for (int e = tid; e < kRanges; e += kPartThreads) slices[part * kRanges + e] = s_bins[e];
+        for (int e = tid; e < kRanges / 2; e += kPartThreads) slices[part * (kRanges / 2) + e] = min(s_bins[2 * e], 65535u) | min(s_bins[2 * e + 1], 65535u) << 16;
         if (!last_of(&o.tickets[0], a.n_parts, tid, &s_last)) continue;
         const Params q = params_of(a, i / a.per);
         const bool count = o.type == BY_COUNT;
-        // what the ranges hold, four a thread, and where the limit falls
-        static_assert(kRanges == 4 * kPartThreads);
-        uint4 n = {0, 0, 0, 0};
+        // what the ranges hold, eight a thread, and where the limit falls
+        constexpr int PER = kRanges / kPartThreads;
+        static_assert(PER == 8);
+        u32 each[PER] = {};
 #pragma unroll 8
         for (int j = 0; j < a.n_parts; ++j) {
-            const uint4 m = *(const uint4*)(slices + j * kRanges + 4 * tid);
-            n.x += m.x;
-            n.y += m.y;
-            n.z += m.z;
-            n.w += m.w;
-        }
-        const u32 each[4] = {n.x, n.y, n.z, n.w};
-        double v[4], mine = 0.0;
+            const uint4 m = *(const uint4*)(slices + j * (kRanges / 2) + 4 * tid);
+            const u32 two[4] = {m.x, m.y, m.z, m.w};
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            const double middle = (double)range_of.ref - (4 * tid + e + 0.5) / (double)range_of.per_unit;
-            mine += v[e] = (double)each[e] * (count ? 1.0 : exp_neg(fmin((middle - (double)o.top) * q.inv, 0.0)));
+            for (int e = 0; e < 4; ++e) {
+                each[2 * e] += two[e] & 0xFFFF;
+                each[2 * e + 1] += two[e] >> 16;
+            }
         }
-        const double limit = count ? (double)(q.k - o.listed) : (double)q.p * o.total - (double)o.listed_q * 0x1p-50, up = wave_scan64_dpp(mine);
-        if (lane == 63) s_sum[wave] = up;
-        __syncthreads();
-        double at = up - mine;
-        for (int w = 0; w < wave; ++w) at += s_sum[w];
-        int last = -1;
+        // a range's weight is about its count times the weight at its middle; an eighth of a range to either side for all of them together (values that lie on a
+        // grid of their own, as bf16's, are off by half a range in one and by less on average: 0.02 of one over a hundred of them)
+        const double limit = count ? (double)(q.k - o.listed) : (double)q.p * o.total - (double)o.listed_q * 0x1p-50;
+        const double width = count ? 0.0 : q.inv / (double)range_of.per_unit, step = exp_neg(-width), spare = exp_neg(-0.125 * width);
+        double middle = count ? 1.0 : exp_neg(fmin(((double)range_of.ref - (double)o.top) * q.inv - (PER * tid + 0.5) * width, 0.0));
+        double least = 0.0, most = 0.0, v_least[PER], v_most[PER];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            if (v[e] > 0.0 && at < limit) last = 4 * tid + e;
-            at += v[e];
+        for (int e = 0; e < PER; ++e) {
+            const bool rest = !count && PER * tid + e == kRanges - 1;          // (all that is below the others)
+            least += v_least[e] = rest ? 0.0 : each[e] * middle * spare;
+            most += v_most[e] = each[e] * middle / spare;
+            middle *= step;
         }
-        for (int f = 32; f > 0; f >>= 1) last = max(last, __shfl_xor(last, f));
-        if (lane == 0) s_at[wave] = last;
+        const double up_least = wave_scan64_dpp(least), up_most = wave_scan64_dpp(most);
+        if (lane == 63) {
+            s_sum[0][wave] = up_least;
+            s_sum[1][wave] = up_most;
+        }
         __syncthreads();
-        const int b = max(max(s_at[0], s_at[1]), max(s_at[2], s_at[3]));
-        const bool good = b >= 0 && limit > 0.0;
-        const u32 lo = first_key(range_of.ref, lane, [&](float x) { return range_of(x) <= b + 1; });
-        const float x_hi = b <= 1 ? below : from_key(first_key(range_of.ref, lane, [&](float x) { return range_of(x) < b - 1; }));
+        double at_least = up_least - least, at_most = up_most - most;
+        for (int w = 0; w < wave; ++w) {
+            at_least += s_sum[0][w];
+            at_most += s_sum[1][w];
+        }
+        // the first range that may, and the first that must, reach the limit
+        int b0 = kRanges, b1 = kRanges;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            at_least += v_least[e];
+            at_most += v_most[e];
+            if (at_most >= limit) b0 = min(b0, PER * tid + e);
+            if (at_least >= limit) b1 = min(b1, PER * tid + e);
+        }
+        for (int f = 32; f > 0; f >>= 1) {
+            b0 = min(b0, __shfl_xor(b0, f));
+            b1 = min(b1, __shfl_xor(b1, f));
+        }
+        if (lane == 0) {
+            s_at[0][wave] = b0;
+            s_at[1][wave] = b1;
+        }
+        __syncthreads();
+        b0 = min(min(s_at[0][0], s_at[0][1]), min(s_at[0][2], s_at[0][3]));
+        b1 = min(min(min(s_at[1][0], s_at[1][1]), min(s_at[1][2], s_at[1][3])), kRanges - 1);
+        const bool good = b0 < kRanges && limit > 0.0;
+        const u32 lo = first_key(range_of.ref, lane, [&](float x) { return range_of(x) <= b1; });
+        const float x_hi = b0 == 0 ? below : from_key(first_key(range_of.ref, lane, [&](float x) { return range_of(x) < b0; }));
         if (tid == 0) {
             if (!good) {
                 o.state = ROW_SLOW;
@@ -1285,7 +1368,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
     static_assert(kPartThreads == kFinishThreads && kPartWaves == kFinishWaves);
     __shared__ word2 s_pow[256];
     __shared__ FinishShared s;
-    __shared__ u64 s_part[kMostParts];
+    __shared__ u64 s_part[kMostParts * kPartWaves];
     __shared__ u64 s_q[kPartWaves];
     __shared__ int32_t s_above[kPartWaves], s_listed[kPartWaves], s_last;
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
@@ -1329,7 +1412,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
             }
         }
         sum = wave_sum_u64(sum);
-        for (int f = 32; f > 0; f >>= 1) above += __shfl_xor(above, f);
+        above = wave_sum_int(above);
         if (lane == 0) {
             s_q[wave] = sum;
             s_above[wave] = above;
@@ -1339,24 +1422,20 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         if (tid == 0) {
             Part& to = a.parts[(int64_t)i * a.n_parts + part];
             to.above = s_above[0] + s_above[1] + s_above[2] + s_above[3];
-            to.above_q = s_q[0] + s_q[1] + s_q[2] + s_q[3];
-            for (int w = 0; w < kPartWaves; ++w) to.listed[w] = s_listed[w];
+            for (int w = 0; w < kPartWaves; ++w) {
+                to.above_q[w] = s_q[w];
+                to.listed[w] = s_listed[w];
+            }
         }
         if (!last_of(&o.tickets[1], a.n_parts, tid, &s_last)) continue;
         // the row from its parts
-        if (tid == 0) s.n = 0;
-        if (tid < kMostParts) s_part[tid] = tid < a.n_parts ? a.parts[(int64_t)i * a.n_parts + tid].above_q : 0;
+        static_assert(kMostParts * kPartWaves == kPartThreads);
+        s_part[tid] = tid < a.n_parts * kPartWaves ? a.parts[(int64_t)i * a.n_parts + tid / kPartWaves].above_q[tid % kPartWaves] : 0;
         __syncthreads();
         int n_above = lane < a.n_parts ? a.parts[(int64_t)i * a.n_parts + lane].above : 0;
-        for (int f = 32; f > 0; f >>= 1) n_above += __shfl_xor(n_above, f);
-        bool over = false;
-        for (int l = tid; l < a.n_parts * kPartWaves; l += kFinishThreads) over |= a.parts[(int64_t)i * a.n_parts + l / kPartWaves].listed[l % kPartWaves] > a.list_len;
-        over = __any(over);
-        read_lists(a, i, wave, lane, (1ull << 56) - 1, [&](bool in, u64 c) { append_to(s, in, c, lane); });
-        if (over && lane == 0) atomicAdd(&s.n, kList);
-        __syncthreads();
-        const int n = s.n;
-        if (n > kList) {
+        n_above = wave_sum_int(n_above);
+        const int n = read_lists(s, a, i, tid, (1ull << 56) - 1);
+        if (n < 0) {
             if (tid == 0) o.state = ROW_SLOW;
             continue;
         }
@@ -1364,16 +1443,16 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         bool good = true;
         if (o.type != BY_SHARE) {
             const bool count = o.type == BY_COUNT;
-            const u64 over_q = wave_sum_u64(s_part[lane]);
+            const u64 over_q = wave_sum_u64(s_part[lane] + s_part[lane + 64] + s_part[lane + 128] + s_part[lane + 192]);
             u64 mine = 0;
-            for (int e = tid; e < n; e += kFinishThreads) mine += count ? 1 : weight(logit_of(s.list[e]));
+            for (int e = tid; e < n; e += kFinishThreads) mine += s.weight[e] = count ? 1 : weight(logit_of(s.list[e]));
             const u64 listed = block_sum(s, mine, 0, tid).q;
             // what the range may still keep; the cut lies in it if something, and no more than it has
             const double left = count ? (double)(q.k - n_above) : ceil((double)q.p * o.total * ldexp(1.0, bits)) - (double)over_q;
             good = n > 0 && left >= 1.0 && left <= (double)listed;
             if (good)
-                cut = last_item(s, n, (u64)~(key_of(x_hi) - 1) << 24, (u64)~key_of(x_lo) << 24 | 0xFFFFFF, (u64)left, tid, [&](int e) { return s.list[e]; },
-                                [&](int e) { return count ? 1ull : weight(logit_of(s.list[e])); }).key;
+                cut = last_item<false>(s, n, (u64)~(key_of(x_hi) - 1) << 24, (u64)~key_of(x_lo) << 24 | 0xFFFFFF, (u64)left, tid, [&](int e) { return s.list[e]; },
+                                [&](int e) { return s.weight[e]; }).key;
             if (q.by_share) cut = min(cut, (u64)~key_of(o.x_m) << 24 | 0xFFFFFF);
         }
         if (!good) {
@@ -1385,19 +1464,34 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
             const u64 c = s.list[e];
             if (c > cut) continue;
             ++kept;
-            if (!MASK) atomicAdd(&s_part[token_of(c) / a.part_len], weight(logit_of(c)));
+            if (!MASK) atomicAdd(&s_part[token_of(c) / run], weight(logit_of(c)));
         }
         kept = block_sum(s, 0, kept, tid).n + n_above;
         int token = -1;
         float logp = 0.f;
         if (!MASK) {
             const float u = a.u[i];
-            const u64 own = s_part[lane], up = wave_scan_u64(own), total = of_lane(up, 63);
-            const u64 target = u > 0.f ? min((u64)((double)u * (double)total), total - 1) : 0;
-            const int of = __ffsll((unsigned long long)__ballot(up > target)) - 1, first = of * a.part_len, len = min(a.part_len, a.vocab - first);
+            // a lane four waves' runs
+            u64 each[4], own = 0;
+#pragma unroll
+            for (int e = 0; e < 4; ++e) own += each[e] = s_part[4 * lane + e];
+            const u64 up = wave_scan_u64(own), total = of_lane(up, 63);
+            u64 target = u > 0.f ? min((u64)((double)u * (double)total), total - 1) : 0;
+            const int of = __ffsll((unsigned long long)__ballot(up > target)) - 1;
+            target -= of_lane(up - own, of);
+            int w = 0;
+#pragma unroll
+            for (int e = 0; e < 3; ++e) {
+                const u64 q_e = of_lane(each[e], of);
+                if (w == e && target >= q_e) {
+                    target -= q_e;
+                    ++w;
+                }
+            }
+            const int first = (4 * of + w) * run, end = min(first + run, a.vocab), quarter = (run / 16 + kPartWaves - 1) / kPartWaves * 16;
             const float cut_x = logit_of(cut);
             const int cut_v = token_of(cut);
-            token = draw_part<T, VEC>(s, row, first, run, first + len, target - of_lane(up - own, of), tid,
+            token = draw_part<T, VEC>(s, row, first, quarter, end, target, tid,
                                       [&](float x, int v) { return x > cut_x || (x == cut_x && v <= cut_v) ? weight(x) : 0; });
             logp = (float)(((double)to_f(row[token]) - (double)o.top) * q.inv - log((double)total * ldexp(1.0, -bits)));
         }
@@ -1453,9 +1547,10 @@ Plan plan_of(int rows, int vocab) {
     // kWanted of the row, a share f of its logits: a group's largest lies among them with probability 1 - (1 - f)^n
     const double f = (double)kWanted / vocab;
     p.sample_len = f < 0.015 ? 4 : f < 0.03 ? 2 : 1;
-    p.sample_rank = std::min(kGroups, std::max(1, (int)(kGroups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
-    // eight times what a wave should find, room for k_filter_bins' counts, and no more than there is
-    p.list_len = std::max(kRanges / 2 / kPartWaves, (8 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16);
+    const int groups = kGroups / 4 * std::min(4, std::max(1, p.part_len / kPartWaves / 256));      // (a short run fills a part of a step)
+    p.sample_rank = std::min(groups, std::max(1, (int)(groups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
+    // six times what a wave should find, room for k_filter_bins' counts, and no more than there is
+    p.list_len = std::max(kRanges / 4 / kPartWaves, (6 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16);
     return p;
 }
 size_t lists_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * kPartWaves * p.list_len * sizeof(u64); }

@@ -90,7 +90,7 @@ def check(x, u, t=None, k=None, p=None, m=None, dtype=None, pad=0, offset=0, mas
 
 
 @pytest.mark.parametrize("kind", ["peaked", "flat", "masked", "ties", "equal", "wide", "zeros"])
-@pytest.mark.parametrize("rows, vocab, dtype, pad, offset", [(16, 500, "f32", 0, 0), (24, 2, "f32", 0, 0), (24, 3, "bf16", 1, 1), (16, 4096, "bf16", 0, 0), (16, 4097, "f32", 3, 0),
+@pytest.mark.parametrize("rows, vocab, dtype, pad, offset", [(16, 500, "f32", 0, 0), (24, 2, "f32", 0, 0), (24, 3, "bf16", 1, 1), (16, 2048, "bf16", 0, 0), (16, 2049, "f32", 3, 0), (16, 3001, "bf16", 7, 8), (16, 4097, "f32", 3, 0),
                                                              (16, 9999, "bf16", 1, 3), (16, 32000, "f32", 0, 0), (16, 50257, "f32", 0, 2), (8, 151936, "bf16", 0, 0),
                                                              (8, 151936, "f32", 0, 0)])
 def test_settings(rows, vocab, dtype, pad, offset, kind):
