@@ -329,6 +329,12 @@ size_t tasc_sampled_scratch_bytes(const tasc_model* m, int32_t batch, int32_t k)
  * commits token 0 (and reports -1).  Which tokens come out depends on the target, the drafts and the random numbers. */
 tasc_status tasc_verify_step_sampled(const tasc_model* m, tasc_session* s, const int32_t* drafts, int32_t k, const tasc_sampling* p,
                                      int32_t* accept_len, int32_t* emitted, float* logprob, void* stream);
+/* From the next sampled step (of any of the calls here) on, the session's sequences draw under top-k, top-p and min-p: every row's logits go through
+ * tasc_filter_logits, whose definitions hold, before the acceptance, and logprob is ln of a token's share of what is kept.  All three NULL: no filter.
+ *   top_k  DEVICE int32[batch], top_p, min_p DEVICE fp32[batch], each nullable; their contents may change from step to step
+ *   workspace  DEVICE, 16-byte aligned, tasc_sample_workspace_bytes(batch * (k + 1), vocab) for the largest k of the steps (less: TASC_ENOMEM from the step)
+ * The arrays and the workspace must outlive the steps that use them.  Enqueues nothing. */
+tasc_status tasc_session_filter(tasc_session* s, const int32_t* top_k, const float* top_p, const float* min_p, void* workspace, size_t ws_bytes);
 /* Takes back what the sequences have generated, the token that the prefill committed among it: the prompts stay cached and the next step's
  * first row is each prompt's last token.  With it the first token is drawn like the others, and one prompt serves several runs. */
 tasc_status tasc_session_rewind(tasc_session* s, void* stream);

@@ -11,6 +11,6 @@ from .binding import (  # noqa: F401
     Kv4Cache, tasc_page_tables, tasc_kv4_page_bytes, tasc_kv4_append, tasc_kv4_read, tasc_kv4_attention, tasc_kv4_attention_workspace_bytes,
     tasc_accept_sampled, tasc_accept_sampled_workspace_bytes, Sampling, tasc_sampled_scratch_bytes, tasc_verify_step_sampled, tasc_session_rewind,
     tasc_generate_sampled, tasc_session_kv4_bytes, tasc_session_create_kv4,
-    tasc_sample, tasc_sample_workspace_bytes, tasc_filter_logits,
+    tasc_sample, tasc_sample_workspace_bytes, tasc_filter_logits, tasc_session_filter,
     tasc_pages_fork, tasc_pages_copy, tasc_pages_workspace_bytes, tasc_pages_free, tasc_pages_compact,
 )

@@ -26,7 +26,7 @@ EXPORTS = [
     "tasc_kv4_attention", "tasc_accept_sampled_workspace_bytes", "tasc_accept_sampled", "tasc_sampled_scratch_bytes",
     "tasc_verify_step_sampled", "tasc_session_rewind", "tasc_generate_sampled", "tasc_session_kv4_bytes", "tasc_session_create_kv4",
     "tasc_sample_workspace_bytes", "tasc_sample", "tasc_filter_logits",
-    "tasc_pages_fork", "tasc_pages_copy", "tasc_pages_workspace_bytes", "tasc_pages_free", "tasc_pages_compact",
+    "tasc_session_filter", "tasc_pages_fork", "tasc_pages_copy", "tasc_pages_workspace_bytes", "tasc_pages_free", "tasc_pages_compact",
 ]
 KERNEL_CLASSES = ["draft", "prepare", "norm", "gemm_qkv", "rope_kv", "attn", "gemm_o", "gemm_gu", "gemm_d", "lmhead", "accept",
                   "verify", "layers"]
@@ -144,6 +144,7 @@ def lib():
                                        C.c_void_p, C.c_void_p, C.c_int32, C.c_void_p, C.c_void_p]
         L.tasc_sampled_scratch_bytes.argtypes = [C.c_void_p, C.c_int32, C.c_int32]
         L.tasc_verify_step_sampled.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.POINTER(Sampling), C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p]
+        L.tasc_session_filter.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_size_t]
         L.tasc_session_rewind.argtypes = [C.c_void_p, C.c_void_p]
         L.tasc_generate_sampled.argtypes = [C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_void_p, C.c_int32, C.c_int32, C.POINTER(SpecParams),
                                             C.POINTER(Sampling), C.c_void_p, C.POINTER(GenStats), C.c_void_p]
@@ -352,6 +353,7 @@ class Session:
     def __init__(self, handle, model, batch, max_len, max_rows, kv_pool, workspace):
         self.handle, self.model, self.batch, self.max_len, self.max_rows = handle, model, batch, max_len, max_rows
         self._kv_pool, self._workspace = kv_pool, workspace     # keep the caller-owned buffers alive
+        self._filters = self._filter_workspace = None           # what tasc_session_filter was given, and a workspace made there
         self._scratch = {}                                      # of sampled steps, by k and stream
 
     def close(self):
@@ -896,6 +898,25 @@ def tasc_verify_step_sampled(model: Model, s: Session, drafts, k, u, temperature
                                           None if accept_len is None else _array(who, "accept_len", accept_len, i32, (s.batch,), dev),
                                           None if emitted is None else _array(who, "emitted", emitted, i32, per_row, dev),
                                           None if logprob is None else _array(who, "logprob", logprob, torch.float32, per_row, dev), st))
+
+
+def tasc_session_filter(s: Session, top_k=None, top_p=None, min_p=None, workspace=None):
+    """From the next sampled step on: top_k int32, top_p and min_p fp32 cuda tensors [batch] or None (all None: no filters); the session keeps them.  A workspace
+    made here serves steps of every k and stays with the session (what was in its place may be in use on any stream: it is waited for, once)."""
+    import torch
+    who = "session_filter"
+    dev, _, _ = _here(None)
+    if s._kv_pool.get_device() != dev:
+        _refuse(f"{who}: the session is on cuda:{s._kv_pool.get_device()}, the current device is cuda:{dev}")
+    _, k, p, m = _filters(who, None, top_k, top_p, min_p, (s.batch,), dev)
+    if workspace is None and (k or p or m):
+        if s._filter_workspace is None:
+            s._filter_workspace = torch.empty(tasc_sample_workspace_bytes(s.batch * min(s.max_rows, TASC_MAX_K + 1), s.model.desc.vocab), dtype=torch.uint8, device="cuda")
+            torch.cuda.synchronize()
+        workspace = s._filter_workspace
+    keep, ws, n = _workspace(who, workspace, 0, dev, True)
+    _check(lib().tasc_session_filter(s.handle, k, p, m, ws, n))
+    s._filters = top_k, top_p, min_p, workspace
 
 
 def tasc_session_rewind(s: Session, stream=None):

@@ -710,7 +710,15 @@ tasc_status sampled_of(const char* who, const tasc_model* m, const tasc_session*
         return TASC_ENOMEM;
     }
     TASC_REQUIRE(((uintptr_t)p->scratch & 255) == 0, "%s: the scratch must be 256-byte aligned", who);
-    *out = TascSampled{p->temperature, p->u, p->n_u, logprob, (float*)p->scratch, (char*)p->scratch + tasc_sample_logits_bytes(s->batch, k, m->desc.vocab)};
+    const TascFilters& f = s->filters;
+    if (f.top_k || f.top_p || f.min_p) {
+        const size_t room = tasc_sample_workspace_bytes(s->batch * (k + 1), m->desc.vocab);
+        if (f.ws_bytes < room) {
+            tasc_set_error("%s: the filters' workspace holds %zu of %zu bytes", who, f.ws_bytes, room);
+            return TASC_ENOMEM;
+        }
+    }
+    *out = TascSampled{p->temperature, p->u, p->n_u, logprob, (float*)p->scratch, (char*)p->scratch + tasc_sample_logits_bytes(s->batch, k, m->desc.vocab), f};
     return TASC_OK;
 }
 }  // namespace
@@ -735,6 +743,13 @@ extern "C" tasc_status tasc_verify_step_sampled(const tasc_model* m, tasc_sessio
         return TASC_ESTATE;
     }
     return verify_step_impl(m, s, drafts, k, accept_len, emitted, nullptr, nullptr, &sampled, (hipStream_t)stream);
+}
+
+extern "C" tasc_status tasc_session_filter(tasc_session* s, const int32_t* top_k, const float* top_p, const float* min_p, void* workspace, size_t ws_bytes) {
+    TASC_REQUIRE(s, "session_filter: null argument");
+    TASC_REQUIRE(((uintptr_t)workspace & 15) == 0, "session_filter: the workspace must be 16-byte aligned");
+    s->filters = TascFilters{top_k, top_p, min_p, workspace, workspace ? ws_bytes : 0};
+    return TASC_OK;
 }
 
 extern "C" tasc_status tasc_session_rewind(tasc_session* s, void* stream) {

@@ -516,6 +516,12 @@ size_t tasc_sample_logits_bytes(int32_t batch, int32_t k, int32_t vocab) { retur
 tasc_status tasc_sample_step(const tasc_session* s, const TascVerifyTail& t, hipStream_t st) {
     const int vocab = s->model->desc.vocab, n_seg = segments(vocab);
     const TascSampled& p = *t.sampled;
+    const TascFilters& f = p.filters;
+    if (f.top_k || f.top_p || f.min_p) {
+        const tasc_status rc = tasc_filter_logits(p.logits, TASC_F32, vocab, s->batch, t.k, vocab, p.temperature, f.top_k, f.top_p, f.min_p, p.logits, vocab, nullptr,
+                                                  f.workspace, f.ws_bytes, st);
+        if (rc != TASC_OK) return rc;
+    }
     const SampleArgs a{p.logits, vocab, t.k, vocab, n_seg, t.drafts, nullptr, p.temperature, p.u, p.n_u, s->d.n_emit, (Part*)p.parts, nullptr, nullptr,
                        t.accept_len, t.emitted, p.logprob, s->d, s->max_len};
     return enqueue<float>(a, s->batch, st);

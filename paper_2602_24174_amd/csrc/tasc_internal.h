@@ -280,6 +280,15 @@ struct TascSessDev {
     float* bias_base;    // [M_lm] its bias of unseen successors
 };
 
+// top-k, top-p and min-p of a session's sampled steps, and the workspace of tasc_filter_logits (all null: none)
+struct TascFilters {
+    const int32_t* top_k;
+    const float* top_p;
+    const float* min_p;
+    void* workspace;
+    size_t ws_bytes;
+    bool operator==(const TascFilters&) const = default;
+};
 // a verify step that samples: the caller's arrays and the scratch of tasc_sampled_scratch_bytes
 struct TascSampled {
     const float* temperature; // nullable [B]
@@ -288,6 +297,7 @@ struct TascSampled {
     float* logprob;           // nullable [B, k + 1]
     float* logits;            // [B, k + 1, vocab]
     void* parts;
+    TascFilters filters;
     bool operator==(const TascSampled&) const = default;
 };
 
@@ -327,6 +337,7 @@ struct tasc_session {
     std::vector<TascStepGraph> step_graphs;   // instantiated verify steps, by their arguments
     int ll_copy;              // which copy of the small-batch activation buffers the next pipeline launch uses
     bool ll_armed;            // both copies hold the "not written yet" pattern wherever the next launch expects it
+    TascFilters filters{};    // of the sampled steps
 };
 
 // counters[] slots used beyond the statistics
