@@ -807,11 +807,10 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
         for (int i = tid; i < kFinishBins; i += kFinishThreads) s.bins[i] = 0;
         if (tid == 0) s.few = 0;
         __syncthreads();
+#pragma unroll 4
         for (int i = tid; i < n; i += kFinishThreads) {
-            const u64 c = key(i);
-            if (c < lo || c > hi) continue;
-            const u64 q = weight(i);
-            if (q) atomicAdd(&s.bins[(c - lo) >> shift], q);
+            const u64 c = key(i), q = weight(i);
+            if (c >= lo && c <= hi && q) atomicAdd(&s.bins[(c - lo) >> shift], q);
         }
         __syncthreads();
         // every wave for itself, 8 bins a lane
@@ -843,11 +842,10 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
         hi = min(hi, lo + ((1ull << shift) - 1));
         if (shift == 0) return Found{lo, sum + own};
         }
+#pragma unroll 4
         for (int i = tid; i < n; i += kFinishThreads) {
-            const u64 c = key(i);
-            if (c < lo || c > hi) continue;
-            const u64 q = weight(i);
-            if (!q) continue;
+            const u64 c = key(i), q = weight(i);
+            if (c < lo || c > hi || !q) continue;
             const int place = atomicAdd(&s.few, 1);
             if (place < kFew) {
                 s.few_key[place] = c;
@@ -887,12 +885,13 @@ __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid)
 
 // A row's lists one behind the other in s.list, entries beyond `last` as none (~0): how many places, or -1 if they do not fit or one of them is not whole;
 // s.n counts the others.  A thread a list for their lengths, then a thread an entry.
-__device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, int i, int tid, u64 last) {
+__device__ __forceinline__ int list_length(const FilterArgs& a, int i, int tid) {      // of the thread's list
+    return tid < a.n_parts * kPartWaves ? a.parts[(int64_t)i * a.n_parts + tid / kPartWaves].listed[tid % kPartWaves] : 0;
+}
+__device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, int i, int own, int tid, u64 last) {
     static_assert(kMostParts * kPartWaves <= kFinishThreads && kFinishThreads <= kFinishBins);
-    const Part* const parts = a.parts + (int64_t)i * a.n_parts;
-    const int n_lists = a.n_parts * kPartWaves, lane = tid & 63, wave = tid >> 6;
-    const u64* const lists = a.lists + (int64_t)i * n_lists * a.list_len;
-    const int own = tid < n_lists ? parts[tid / kPartWaves].listed[tid % kPartWaves] : 0;
+    const int lane = tid & 63, wave = tid >> 6;
+    const u64* const lists = a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len;
     // the sums of the lengths; bit 32 of a sum: a list that is not whole
     const u64 up = wave_scan_u64((u64)(u32)own | (own > a.list_len ? 1ull << 32 : 0));
     if (lane == 63) s.red[wave] = up;
@@ -1011,6 +1010,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
     __shared__ FinishShared s;
     const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
+    const int length = a.direct ? 0 : list_length(a, i, tid);
     const Params p = params_of(a, i / a.per);
     if (tid == 0) s.n = s.bad = 0;
     __syncthreads();
@@ -1057,7 +1057,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         bound = wave_max_dpp(bound);
         least = -wave_max_dpp(-least);
         live = wave_sum_int(live);
-        if (bound < __builtin_inff()) n = read_lists(s, a, i, tid, (u64)~key_of(bound) << 24 | 0xFFFFFF);
+        if (bound < __builtin_inff()) n = read_lists(s, a, i, length, tid, (u64)~key_of(bound) << 24 | 0xFFFFFF);
         if (n < 0) bound = __builtin_inff();
         whole = bound == -__builtin_inff();
     }
@@ -1434,7 +1434,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         __syncthreads();
         int n_above = lane < a.n_parts ? a.parts[(int64_t)i * a.n_parts + lane].above : 0;
         n_above = wave_sum_int(n_above);
-        const int n = read_lists(s, a, i, tid, (1ull << 56) - 1);
+        const int n = read_lists(s, a, i, list_length(a, i, tid), tid, (1ull << 56) - 1);
         if (n < 0) {
             if (tid == 0) o.state = ROW_SLOW;
             continue;

@@ -153,7 +153,7 @@ struct UseArgs {
     int32_t cap;                       // moves
     int32_t* summary;
 };
-constexpr int kBlockWords = 1024, kUseThreads = 256, kSmallThreads = 1024;
+constexpr int kBlockWords = 256, kUseThreads = 256, kSmallThreads = 1024;
 
 __device__ __forceinline__ int row_pages(const UseArgs& a, int b) { return min(max(a.pages[b], 0), a.max_pages); }
 
@@ -162,14 +162,19 @@ __global__ __launch_bounds__(kUseThreads) void k_use_clear(UseArgs a) {
     const int n = (a.n_words + 1) / 2 * 4;
     for (int i = blockIdx.x * kUseThreads + threadIdx.x; i < n; i += gridDim.x * kUseThreads) to[i] = quad{0, 0, 0, 0};
 }
-// A wave a sequence (of a run of columns).  A page's mark is a byte, written by whoever lists it: bits set by atomics, which cross the chip's dies one by
-// one, took 230 of 248 us for 2.5 million entries of a pool of 3.7 million pages.
-constexpr int kMarkCols = 4096, kMarkBlocks = 2048;
+// A wave a sequence (of a run of columns).  A page's mark is a byte, written by whoever lists it: with bits set by atomics, which all meet behind the dies'
+// caches, a whole call over 2.5 million entries of a pool of 3.7 million pages took 248 us, with bytes 56.  Workgroups in turn take the lower and the upper half of the
+// pages (the dispatcher deals them to the dies in turn, so a die's cache then holds half of the marks): 26 us of this kernel without that, 19 with two or four
+// shares, 24 with eight, since every share reads all entries.
+constexpr int kMarkCols = 4096, kMarkBlocks = 2048, kMarkShares = 2;
 __global__ __launch_bounds__(kUseThreads) void k_use_mark(UseArgs a, int col_runs, int64_t n_items) {
+    constexpr int shares = kMarkShares;
     __shared__ u64 s_n[kUseThreads / 64];
-    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), share = blockIdx.x % shares;
+    const int per = (a.n_pages - 1) / shares + 1;
+    const u32 from = share * (u32)per, count = min((u32)per, (u32)a.n_pages - min(from, (u32)a.n_pages));
     u64 n = 0;
-    for (int64_t item = (int64_t)blockIdx.x * (kUseThreads / 64) + wave; item < n_items; item += (int64_t)gridDim.x * (kUseThreads / 64)) {
+    for (int64_t item = (int64_t)(blockIdx.x / shares) * (kUseThreads / 64) + wave; item < n_items; item += (int64_t)(gridDim.x / shares) * (kUseThreads / 64)) {
         const int b = (int)(item / col_runs), run = (int)(item % col_runs);
         const int to = min(row_pages(a, b), (int)min((int64_t)(run + 1) * kMarkCols, (int64_t)a.max_pages));
         const int32_t* const row = a.table + (size_t)b * a.max_pages;
@@ -180,7 +185,7 @@ __global__ __launch_bounds__(kUseThreads) void k_use_mark(UseArgs a, int col_run
             for (int j = 0; j < AHEAD; ++j) p[j] = c + 64 * j < to ? row[c + 64 * j] : -1;
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j) {
-                if (p[j] < 0 || p[j] >= a.n_pages) continue;
+                if ((u32)p[j] - from >= count) continue;   // (also what is no page of the pool)
                 ++n;
                 a.marks[p[j]] = 1;
             }
@@ -462,7 +467,7 @@ tasc_status enqueue_use(const char* who, UseArgs a, void* workspace, size_t ws_b
     a.sums = a.before + a.n_words;
     const int col_runs = (a.max_pages - 1) / kMarkCols + 1;
     const int64_t items = (int64_t)a.batch * col_runs;
-    a.n_marking = (int)std::min<int64_t>((items + kUseThreads / 64 - 1) / (kUseThreads / 64), kMarkBlocks);
+    a.n_marking = (int)std::min<int64_t>((items + kUseThreads / 64 - 1) / (kUseThreads / 64), kMarkBlocks / kMarkShares) * kMarkShares;
     const dim3 threads(kUseThreads), rows((unsigned)((a.batch + kUseThreads / 64 - 1) / (kUseThreads / 64)), (unsigned)col_runs);
     k_use_clear<<<dim3((unsigned)std::min((a.n_words / 2 * 4 + kUseThreads) / kUseThreads, 4096)), threads, 0, st>>>(a);
     k_use_mark<<<dim3((unsigned)a.n_marking), threads, 0, st>>>(a, col_runs, items);
