@@ -7,7 +7,7 @@
 // above a bound that it takes from a sample, about 900 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always the
 // cut lies in them.  Rows whose cut does not (flat distributions: thousands of tokens kept) are listed for two kernels that read them again, parts side by
 // side: k_filter_bins sums the weights (or counts) of 512 ranges of values, its last workgroup of a row finds the range in which the cut lies; k_filter_gather
-// lists that range's tokens and sums what is above it, its last workgroup finds the cut and draws.  k_filter_slow, a workgroup a row, serves what is left (ties of
+// lists that range's tokens and sums what is above it, its last workgroup finds the cut and draws.  k_filter_close, a workgroup a row, serves what is left (ties of
 // thousands at the cut, a top-k of thousands and a top-p together): 4096 ranges, of which the one with the cut is sorted if it fits, or cut into 4096 again, by
 // comp, until one token is left.  Rows of up to kList tokens are their own list and need one launch.
 //
@@ -48,11 +48,11 @@ struct __attribute__((aligned(16))) RowOut {
     float least;                     // roughly
     int32_t listed;                  // logits from ref on, and their weights in 2^-kListBits
     u64 listed_q;
-    float x_lo, x_hi;                // the range that the cut lies in
+    float x_lo, x_hi;                // k_filter_gather's: the range that the cut lies in
     double total;                    // sum of all weights, in the largest's
-    int32_t tickets[2];
     float x_m;                       // min-p's least logit (-infinity: none)
-    int32_t pad[3];
+    int32_t found;                   // k_filter_gather's: what decides on the cut, or -1
+    int32_t pad[2];
 };
 
 struct FilterArgs {
@@ -71,6 +71,7 @@ struct FilterArgs {
     int64_t out_stride;
     Part* parts;                     // [rows, n_parts]
     u64* lists;                      // [rows, n_parts, kPartWaves, list_len]
+    u32* slices;                     // [rows, n_parts, kRanges / 2] counts of ranges, of the rows in `wide`
     RowOut* rows;                    // [rows]
     int32_t* wide;                   // how many rows are listed here, and which
     int32_t n_parts, part_len, list_len;
@@ -558,52 +559,6 @@ struct Row {
     }
 };
 
-template <typename T, bool VEC, bool MASK>
-__global__ __launch_bounds__(kThreads) void k_filter_slow(FilterArgs a) {
-    __shared__ Shared s;
-    const int i = blockIdx.x, b = i / a.per, tid = threadIdx.x;
-    if (a.rows[i].state != ROW_SLOW) return;
-    const Params q = params_of(a, b);
-    Row<T, VEC> row{(const T*)a.logits + (int64_t)i * a.row_stride, a.vocab, tid, tid & 63, tid >> 6, s, RowState{}};
-    RowState& r = row.r;
-    row.look();
-    r.inv = q.inv;
-    const double range = (double)r.top - (double)r.least;
-    r.per_unit = fmax(64.0 * r.inv, range > 0.0 ? (kBins - 1.5) / range : 1.0);
-    r.bin_width = r.inv / r.per_unit;
-    r.bits = min(50, 61 - (32 - __clz(a.vocab)));
-    r.cut = (u64)~key_of(r.least) << 24 | 0xFFFFFF;
-    r.kept = r.live;
-    r.listed = -1;
-    const int k = q.one ? 1 : q.by_count ? q.k : r.live;
-    if (k < r.live) row.template select<true>([&](double) { return (double)k; });
-    if (q.by_mass) {
-        if (r.listed >= 0) {
-            r.kept = list_below(s, r, s.big, r.kept, tid, [&](double total) { return (double)q.p * total; });
-            r.cut = s.big[r.kept - 1];
-        } else {
-            row.template select<false>([&](double total) { return (double)q.p * total; });
-        }
-    }
-    if (q.by_share) {
-        const double most = -log((double)q.m);
-        row.at_least(first_key(r.top, tid & 63, [&](float x) { return ((double)r.top - (double)x) * r.inv <= most; }));
-    }
-    int token = -1;
-    float logp = 0.f;
-    if (!MASK) token = row.draw(a.u[i], logp);
-    else if (r.kept < 0) row.count();
-    if (tid != 0) return;
-    if (a.kept) a.kept[i] = r.kept;
-    if (MASK) {
-        a.rows[i].cut = r.cut;
-        a.rows[i].state = ROW_CUT;
-        return;
-    }
-    a.token[i] = token;
-    if (a.logprob) a.logprob[i] = logp;
-}
-
 // ---------------------------------------------------------------- one read of every logit
 // A wave has a run of its own, 16 logits a lane at a time.  The first of them are the sample: of groups of 16 to 64 logits the largest, and of these 64 one
 // by its rank, which about kWanted / vocab of all logits exceed; the sum's units come from the sample's largest, too.
@@ -775,8 +730,8 @@ struct __attribute__((aligned(16))) FinishShared {
     u64 list[kList], weight[kList];
     u64 bins[kFinishBins];
     u64 few_key[kFew], few_q[kFew];
-    u64 red[kFinishWaves];
-    int32_t num[kFinishWaves], few, n, bad;
+    u64 red[kWaves];
+    int32_t num[kWaves], few, n, bad;
 };
 __device__ __forceinline__ void append_to(FinishShared& s, bool in, u64 c, int lane) {
     const u64 m = __ballot(in);
@@ -790,7 +745,7 @@ struct Found { u64 key, sum; };      // sum: up to it and with it
 
 // Of n items with weights q (0: not there), in the order of their keys within [lo, hi]: the last whose sum of those before it is below `limit`
 // (FEW: there are no more than kFew of them).
-template <bool FEW, typename Key, typename Weight>
+template <bool FEW, int NT, typename Key, typename Weight>
 __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 hi, u64 limit, int tid, Key key, Weight weight) {
     const int lane = tid & 63;
     u64 sum = 0;
@@ -804,11 +759,11 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
         const int shift = max(0, 64 - 9 - __clzll((long long)(hi - lo)));
         static_assert(kFinishBins == 1 << 9);
         __syncthreads();                                    // (bins and few are still looked at)
-        for (int i = tid; i < kFinishBins; i += kFinishThreads) s.bins[i] = 0;
+        for (int i = tid; i < kFinishBins; i += NT) s.bins[i] = 0;
         if (tid == 0) s.few = 0;
         __syncthreads();
 #pragma unroll 4
-        for (int i = tid; i < n; i += kFinishThreads) {
+        for (int i = tid; i < n; i += NT) {
             const u64 c = key(i), q = weight(i);
             if (c >= lo && c <= hi && q) atomicAdd(&s.bins[(c - lo) >> shift], q);
         }
@@ -843,7 +798,7 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
         if (shift == 0) return Found{lo, sum + own};
         }
 #pragma unroll 4
-        for (int i = tid; i < n; i += kFinishThreads) {
+        for (int i = tid; i < n; i += NT) {
             const u64 c = key(i), q = weight(i);
             if (c < lo || c > hi || !q) continue;
             const int place = atomicAdd(&s.few, 1);
@@ -871,6 +826,7 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
     }
 }
 struct Sum { u64 q; int n; };
+template <int NT>
 __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid) {
     q = wave_sum_u64(q);
     n = wave_sum_int(n);
@@ -880,7 +836,13 @@ __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid)
         s.num[tid >> 6] = n;
     }
     __syncthreads();
-    return Sum{s.red[0] + s.red[1] + s.red[2] + s.red[3], s.num[0] + s.num[1] + s.num[2] + s.num[3]};
+    Sum all{0, 0};
+#pragma unroll
+    for (int w = 0; w < NT / 64; ++w) {
+        all.q += s.red[w];
+        all.n += s.num[w];
+    }
+    return all;
 }
 
 // A row's lists one behind the other in s.list, entries beyond `last` as none (~0): how many places, or -1 if they do not fit or one of them is not whole;
@@ -888,8 +850,9 @@ __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid)
 __device__ __forceinline__ int list_length(const FilterArgs& a, int i, int tid) {      // of the thread's list
     return tid < a.n_parts * kPartWaves ? a.parts[(int64_t)i * a.n_parts + tid / kPartWaves].listed[tid % kPartWaves] : 0;
 }
+template <int NT>
 __device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, int i, int own, int tid, u64 last) {
-    static_assert(kMostParts * kPartWaves <= kFinishThreads && kFinishThreads <= kFinishBins);
+    static_assert(kMostParts * kPartWaves <= NT && NT <= 2 * kFinishBins);
     const int lane = tid & 63, wave = tid >> 6;
     const u64* const lists = a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len;
     // the sums of the lengths; bit 32 of a sum: a list that is not whole
@@ -898,7 +861,7 @@ __device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, 
     if (tid == 0) s.n = 0;
     __syncthreads();
     u64 before = 0, all = 0;
-    for (int w = 0; w < kFinishWaves; ++w) {
+    for (int w = 0; w < NT / 64; ++w) {
         if (w == wave) before = all;
         all += s.red[w];
     }
@@ -909,22 +872,22 @@ __device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, 
     __syncthreads();
     int valid = 0;
     constexpr int AHEAD = 4;
-    for (int e0 = tid; e0 < n; e0 += AHEAD * kFinishThreads) {
+    for (int e0 = tid; e0 < n; e0 += AHEAD * NT) {
         int l[AHEAD] = {};                                  // lists that end at or before the entry
 #pragma unroll
-        for (int step = kFinishThreads / 2; step > 0; step /= 2)
+        for (int step = NT / 2; step > 0; step /= 2)
 #pragma unroll
             for (int j = 0; j < AHEAD; ++j)
-                if (ends[l[j] + step - 1] <= (u32)(e0 + j * kFinishThreads)) l[j] += step;
+                if (ends[l[j] + step - 1] <= (u32)(e0 + j * NT)) l[j] += step;
         u64 c[AHEAD];
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int e = e0 + j * kFinishThreads;
+            const int e = e0 + j * NT;
             c[j] = e < n ? lists[(int64_t)l[j] * a.list_len + (e - (l[j] > 0 ? (int)ends[l[j] - 1] : 0))] : ~0ull;
         }
 #pragma unroll
         for (int j = 0; j < AHEAD; ++j) {
-            const int e = e0 + j * kFinishThreads;
+            const int e = e0 + j * NT;
             if (e >= n) continue;
             s.list[e] = c[j] <= last ? c[j] : ~0ull;
             valid += c[j] <= last;
@@ -938,13 +901,13 @@ __device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, 
 
 // The first of the logits [p0, end) whose weights up to it sum to more than `target` (the last with any if none does): the sums of the waves' steps, then the
 // logits of one step.  weight(x, v) is 0 where a token is not kept.
-template <typename T, bool VEC, typename Weight>
+template <typename T, bool VEC, int NT, typename Weight>
 __device__ __forceinline__ int draw_part(FinishShared& s, const T* row, int p0, int run, int end, u64 target, int tid, Weight weight) {
     using R = Run<T, VEC>;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), v_begin = min(p0 + wave * run, end), v_end = min(v_begin + run, end);
     const int steps = (run + kStep - 1) / kStep;            // of a wave
     __syncthreads();
-    for (int i = tid; i < kFinishBins; i += kFinishThreads) s.bins[i] = 0;
+    for (int i = tid; i < kFinishBins; i += NT) s.bins[i] = 0;
     __syncthreads();
     float next[kPer];
     R::load(row, v_begin, v_end, lane, next);
@@ -981,12 +944,12 @@ __device__ __forceinline__ int draw_part(FinishShared& s, const T* row, int p0, 
     if (!have) return p0;
     const int from = 63 - __clzll(have), step = __builtin_amdgcn_readlane(last, from);
     target -= of_lane(before, from);
-    // four logits a thread
-    static_assert(kStep == 4 * kFinishThreads);
-    const int w = step / steps, first = p0 + w * run + step % steps * kStep, stop = min(min(p0 + (w + 1) * run, end), first + kStep), v0 = first + 4 * tid;
-    u64 q[4], own = 0;
+    // a few logits a thread
+    constexpr int SPAN = kStep / NT;
+    const int w = step / steps, first = p0 + w * run + step % steps * kStep, stop = min(min(p0 + (w + 1) * run, end), first + kStep), v0 = first + SPAN * tid;
+    u64 q[SPAN], own = 0;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) own += q[e] = v0 + e < stop ? weight(to_f(row[v0 + e]), v0 + e) : 0;
+    for (int e = 0; e < SPAN; ++e) own += q[e] = v0 + e < stop ? weight(to_f(row[v0 + e]), v0 + e) : 0;
     const u64 sum = wave_scan_u64(own);
     __syncthreads();
     if (lane == 63) s.red[wave] = sum;
@@ -995,14 +958,15 @@ __device__ __forceinline__ int draw_part(FinishShared& s, const T* row, int p0, 
     for (int i = 0; i < wave; ++i) at += s.red[i];
     int token = -1;
 #pragma unroll
-    for (int e = 0; e < 4; ++e) {
+    for (int e = 0; e < SPAN; ++e) {
         if (q[e] && at <= target) token = v0 + e;
         at += q[e];
     }
     for (int o = 32; o > 0; o >>= 1) token = max(token, __shfl_xor(token, o));
     if (lane == 0) s.num[wave] = token;
     __syncthreads();
-    return max(max(s.num[0], s.num[1]), max(s.num[2], s.num[3]));
+    for (int i = 0; i < NT / 64; ++i) token = max(token, s.num[i]);
+    return token;
 }
 
 template <typename T, bool VEC, bool MASK>
@@ -1057,7 +1021,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         bound = wave_max_dpp(bound);
         least = -wave_max_dpp(-least);
         live = wave_sum_int(live);
-        if (bound < __builtin_inff()) n = read_lists(s, a, i, length, tid, (u64)~key_of(bound) << 24 | 0xFFFFFF);
+        if (bound < __builtin_inff()) n = read_lists<kFinishThreads>(s, a, i, length, tid, (u64)~key_of(bound) << 24 | 0xFFFFFF);
         if (n < 0) bound = __builtin_inff();
         whole = bound == -__builtin_inff();
     }
@@ -1103,7 +1067,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             }
             if (by_count) {
                 if (p.k <= valid) {
-                    cut = last_item<false>(s, n, lo, hi, (u64)p.k, tid, comp, [](int) { return 1ull; }).key;
+                    cut = last_item<false, kFinishThreads>(s, n, lo, hi, (u64)p.k, tid, comp, [](int) { return 1ull; }).key;
                     held = true;
                 } else if (!held) {
                     wide = true;
@@ -1112,7 +1076,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             if (p.by_mass && !wide) {
                 u64 mine = 0;
                 for (int e = tid; e < n; e += kFinishThreads) mine += s.list[e] <= cut ? weight(e) : 0;
-                const u64 listed = listed_q = block_sum(s, mine, 0, tid).q;
+                const u64 listed = listed_q = block_sum<kFinishThreads>(s, mine, 0, tid).q;
                 double limit = 0.0;
                 if (held) {
                     limit = ceil((double)p.p * (double)listed);
@@ -1125,7 +1089,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
                     wide = true;
                 }
                 if (!wide) {
-                    cut = last_item<false>(s, n, lo, min(hi, cut), (u64)fmax(limit, 1.0), tid, comp, weight).key;
+                    cut = last_item<false, kFinishThreads>(s, n, lo, min(hi, cut), (u64)fmax(limit, 1.0), tid, comp, weight).key;
                     held = true;
                 }
             }
@@ -1146,7 +1110,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             const int part = past ? __ffsll((unsigned long long)past) - 1 : 63 - __clzll(some);
             const int p0 = part * a.part_len, len = min(a.part_len, a.vocab - p0), bits = min(50, 62 - (32 - __clz(a.part_len)));
             const u64 within = (u64)(fmax(target - lane64(up - own, part), 0.0) * ldexp(1.0, bits));
-            token = draw_part<T, VEC>(s, row, p0, a.part_len / kPartWaves, p0 + len, within, tid, [&](float x, int) { return x > -__builtin_inff() ? max(weight_of(r, x, bits), (u64)1) : 0; });
+            token = draw_part<T, VEC, kFinishThreads>(s, row, p0, a.part_len / kFinishWaves, p0 + len, within, tid, [&](float x, int) { return x > -__builtin_inff() ? max(weight_of(r, x, bits), (u64)1) : 0; });
             logp = (float)(((double)to_f(row[token]) - (double)r.top) * r.inv - log(total));
             kept = live;
         } else {
@@ -1157,14 +1121,14 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
                 c += in;
                 if (!MASK && in) q += weight(e);
             }
-            const Sum all = block_sum(s, q, c, tid);
+            const Sum all = block_sum<kFinishThreads>(s, q, c, tid);
             kept = all.n;
             if (!MASK) {
                 const float u = a.u[i];
                 const u64 limit = u > 0.f ? min((u64)((double)u * (double)all.q), all.q - 1) + 1 : 1;
                 auto token_at = [&](int e) { return s.list[e] <= cut ? (u64)token_of(s.list[e]) << 32 | (u32)e : ~0ull; };
-                const Found f = kept <= kFew ? last_item<true>(s, n, 0, ~0ull - 1, limit, tid, token_at, weight)
-                                             : last_item<false>(s, n, 0, (u64)a.vocab << 32, limit, tid, token_at, weight);
+                const Found f = kept <= kFew ? last_item<true, kFinishThreads>(s, n, 0, ~0ull - 1, limit, tid, token_at, weight)
+                                             : last_item<false, kFinishThreads>(s, n, 0, (u64)a.vocab << 32, limit, tid, token_at, weight);
                 token = (int)(f.key >> 32);
                 const float x = logit_of(s.list[(u32)f.key]);
                 logp = p.one ? 0.f : (float)(((double)x - (double)r.top) * r.inv - log((double)all.q * 0x1p-50));
@@ -1198,7 +1162,7 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         o.listed = valid;
         o.listed_q = listed_q;
         o.total = total;
-        o.x_lo = o.x_hi = o.x_m = x_m;
+        o.x_m = x_m;
         a.rows[i] = o;
         if (o.state == ROW_WIDE) a.wide[1 + atomicAdd(a.wide, 1)] = i;
     }
@@ -1232,29 +1196,11 @@ struct Ranges {
     __device__ __forceinline__ int operator()(float x) const { return (int)fminf((ref - x) * per_unit, (float)(kRanges - 1)); }
 };
 __device__ __forceinline__ int sum_bits(int n) { return min(kListBits, 61 - (32 - __clz(n))); }      // n weights stay below 2^62
-// Whether this workgroup is the last of n to come here with a row; what the others wrote before is then seen.  One thread's fences serve its
-// workgroup, the barriers around them order the others' accesses: an agent's fence writes a whole L2 back and takes thousands of cycles.
-__device__ __forceinline__ bool last_of(int32_t* ticket, int n, int tid, int32_t* s_last) {
-    __syncthreads();
-    if (tid == 0) {
-        __threadfence();
-        const bool last = atomicAdd(ticket, 1) == n - 1;
-        if (last) __threadfence();
-        *s_last = last;
-    }
-    __syncthreads();
-    return *s_last != 0;
-}
-
-// Counts of the ranges; the last workgroup of a row finds those in which the cut may lie, by the counts times the weights at a range's ends: ranges are narrow
-// (0.005 of a logit, 200 tokens, for 150,000 tokens over 10), so that a few are left for k_filter_gather, which has exact sums.  Bound by the LDS atomics.
+// Counts of the ranges by part.  Bound by the LDS atomics.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
     using R = Run<T, VEC>;
     __shared__ u32 s_bins[kRanges];
-    __shared__ int32_t s_last;
-    __shared__ double s_sum[2][kPartWaves];
-    __shared__ int32_t s_at[2][kPartWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int items = *a.wide * a.n_parts;
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
@@ -1281,96 +1227,93 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
         }
         __syncthreads();
         // (16 bits a count: one that does not fit only makes the ranges miss the cut)
-        u32* const slices = (u32*)(a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len);
+        u32* const slices = a.slices + (int64_t)i * a.n_parts * (kRanges / 2);
         for (int e = tid; e < kRanges / 2; e += kPartThreads) slices[part * (kRanges / 2) + e] = min(s_bins[2 * e], 65535u) | min(s_bins[2 * e + 1], 65535u) << 16;
-        if (!last_of(&o.tickets[0], a.n_parts, tid, &s_last)) continue;
-        const Params q = params_of(a, i / a.per);
-        const bool count = o.type == BY_COUNT;
-        // what the ranges hold, eight a thread, and where the limit falls
-        constexpr int PER = kRanges / kPartThreads;
-        static_assert(PER == 8);
-        u32 each[PER] = {};
-#pragma unroll 8
-        for (int j = 0; j < a.n_parts; ++j) {
-            const uint4 m = *(const uint4*)(slices + j * (kRanges / 2) + 4 * tid);
-            const u32 two[4] = {m.x, m.y, m.z, m.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                each[2 * e] += two[e] & 0xFFFF;
-                each[2 * e + 1] += two[e] >> 16;
-            }
-        }
-        // a range's weight is about its count times the weight at its middle; an eighth of a range to either side for all of them together (values that lie on a
-        // grid of their own, as bf16's, are off by half a range in one and by less on average: 0.02 of one over a hundred of them)
-        const double limit = count ? (double)(q.k - o.listed) : (double)q.p * o.total - (double)o.listed_q * 0x1p-50;
-        const double width = count ? 0.0 : q.inv / (double)range_of.per_unit, step = exp_neg(-width), spare = exp_neg(-0.125 * width);
-        double middle = count ? 1.0 : exp_neg(fmin(((double)range_of.ref - (double)o.top) * q.inv - (PER * tid + 0.5) * width, 0.0));
-        double least = 0.0, most = 0.0, v_least[PER], v_most[PER];
-#pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            const bool rest = !count && PER * tid + e == kRanges - 1;          // (all that is below the others)
-            least += v_least[e] = rest ? 0.0 : each[e] * middle * spare;
-            most += v_most[e] = each[e] * middle / spare;
-            middle *= step;
-        }
-        const double up_least = wave_scan64_dpp(least), up_most = wave_scan64_dpp(most);
-        if (lane == 63) {
-            s_sum[0][wave] = up_least;
-            s_sum[1][wave] = up_most;
-        }
-        __syncthreads();
-        double at_least = up_least - least, at_most = up_most - most;
-        for (int w = 0; w < wave; ++w) {
-            at_least += s_sum[0][w];
-            at_most += s_sum[1][w];
-        }
-        // the first range that may, and the first that must, reach the limit
-        int b0 = kRanges, b1 = kRanges;
-#pragma unroll
-        for (int e = 0; e < PER; ++e) {
-            at_least += v_least[e];
-            at_most += v_most[e];
-            if (at_most >= limit) b0 = min(b0, PER * tid + e);
-            if (at_least >= limit) b1 = min(b1, PER * tid + e);
-        }
-        for (int f = 32; f > 0; f >>= 1) {
-            b0 = min(b0, __shfl_xor(b0, f));
-            b1 = min(b1, __shfl_xor(b1, f));
-        }
-        if (lane == 0) {
-            s_at[0][wave] = b0;
-            s_at[1][wave] = b1;
-        }
-        __syncthreads();
-        b0 = min(min(s_at[0][0], s_at[0][1]), min(s_at[0][2], s_at[0][3]));
-        b1 = min(min(min(s_at[1][0], s_at[1][1]), min(s_at[1][2], s_at[1][3])), kRanges - 1);
-        const bool good = b0 < kRanges && limit > 0.0;
-        const u32 lo = first_key(range_of.ref, lane, [&](float x) { return range_of(x) <= b1; });
-        const float x_hi = b0 == 0 ? below : from_key(first_key(range_of.ref, lane, [&](float x) { return range_of(x) < b0; }));
-        if (tid == 0) {
-            if (!good) {
-                o.state = ROW_SLOW;
-            } else if (o.x_m >= x_hi) {                     // min-p keeps less
-                o.type = BY_SHARE;
-            } else {
-                o.x_lo = from_key(lo);
-                o.x_hi = x_hi;
-            }
-        }
     }
 }
 
-// The range's tokens and what lies above it; the last workgroup of a row finds the cut, and draws
-// A workgroup a part, then a row: bound by the exponentials of what is kept, and the last workgroups' chains of reads.
-template <typename T, bool VEC, bool MASK>
+// The ranges in which the cut may lie, by the counts times the weights at their middles: ranges are narrow (0.005 of a logit, 200 tokens, for 150,000 tokens
+// over 10), so that a few are left for k_filter_gather, which has exact sums.  false: nothing is found.
+struct RangeShared { double sum[2][kPartWaves]; int32_t at[2][kPartWaves]; };
+__device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a, const RowOut& o, const Params& q, const u32* slices, int tid, float& x_lo, float& x_hi) {
+    const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+    const Ranges range_of(o);
+    const float below = o.ref;
+    const bool count = o.type == BY_COUNT;
+    // what the ranges hold, eight a thread, and where the limit falls
+    constexpr int PER = kRanges / kPartThreads;
+    static_assert(PER == 8);
+    u32 each[PER] = {};
+#pragma unroll 8
+    for (int j = 0; j < a.n_parts; ++j) {
+        const uint4 m = *(const uint4*)(slices + j * (kRanges / 2) + 4 * tid);
+        const u32 two[4] = {m.x, m.y, m.z, m.w};
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            each[2 * e] += two[e] & 0xFFFF;
+            each[2 * e + 1] += two[e] >> 16;
+        }
+    }
+    // a range's weight is about its count times the weight at its middle; an eighth of a range to either side for all of them together (values that lie on a
+    // grid of their own, as bf16's, are off by half a range in one and by less on average: 0.02 of one over a hundred of them)
+    const double limit = count ? (double)(q.k - o.listed) : (double)q.p * o.total - (double)o.listed_q * 0x1p-50;
+    const double width = count ? 0.0 : q.inv / (double)range_of.per_unit, step = exp_neg(-width), spare = exp_neg(-0.125 * width);
+    double middle = count ? 1.0 : exp_neg(fmin(((double)range_of.ref - (double)o.top) * q.inv - (PER * tid + 0.5) * width, 0.0));
+    double least = 0.0, most = 0.0, v_least[PER], v_most[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        const bool rest = !count && PER * tid + e == kRanges - 1;          // (all that is below the others)
+        least += v_least[e] = rest ? 0.0 : each[e] * middle * spare;
+        most += v_most[e] = each[e] * middle / spare;
+        middle *= step;
+    }
+    const double up_least = wave_scan64_dpp(least), up_most = wave_scan64_dpp(most);
+    if (lane == 63) {
+        s.sum[0][wave] = up_least;
+        s.sum[1][wave] = up_most;
+    }
+    __syncthreads();
+    double at_least = up_least - least, at_most = up_most - most;
+    for (int w = 0; w < wave; ++w) {
+        at_least += s.sum[0][w];
+        at_most += s.sum[1][w];
+    }
+    // the first range that may, and the first that must, reach the limit
+    int b0 = kRanges, b1 = kRanges;
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        at_least += v_least[e];
+        at_most += v_most[e];
+        if (at_most >= limit) b0 = min(b0, PER * tid + e);
+        if (at_least >= limit) b1 = min(b1, PER * tid + e);
+    }
+    for (int f = 32; f > 0; f >>= 1) {
+        b0 = min(b0, __shfl_xor(b0, f));
+        b1 = min(b1, __shfl_xor(b1, f));
+    }
+    if (lane == 0) {
+        s.at[0][wave] = b0;
+        s.at[1][wave] = b1;
+    }
+    __syncthreads();
+    b0 = min(min(s.at[0][0], s.at[0][1]), min(s.at[0][2], s.at[0][3]));
+    b1 = min(min(min(s.at[1][0], s.at[1][1]), min(s.at[1][2], s.at[1][3])), kRanges - 1);
+    const bool good = b0 < kRanges && limit > 0.0;
+    x_lo = from_key(first_key(range_of.ref, lane, [&](float x) { return range_of(x) <= b1; }));
+    x_hi = b0 == 0 ? below : from_key(first_key(range_of.ref, lane, [&](float x) { return range_of(x) < b0; }));
+    return good;
+}
+
+// The tokens of the ranges in which the cut may lie, and what lies above them, by part; every workgroup finds the ranges for itself.  Bound by the exponentials of
+// what is kept.  (With a row's last workgroup finding them, and the cut, the fences around that took longer than either kernel's own work: 1280 rows, 140 of
+// them here, 95 + 87 us.)
+template <typename T, bool VEC>
 __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
     using R = Run<T, VEC>;
-    static_assert(kPartThreads == kFinishThreads && kPartWaves == kFinishWaves);
     __shared__ word2 s_pow[256];
-    __shared__ FinishShared s;
-    __shared__ u64 s_part[kMostParts * kPartWaves];
+    __shared__ RangeShared s;
     __shared__ u64 s_q[kPartWaves];
-    __shared__ int32_t s_above[kPartWaves], s_listed[kPartWaves], s_last;
+    __shared__ int32_t s_above[kPartWaves], s_listed[kPartWaves];
     const int tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const int items = *a.wide * a.n_parts;
     if ((int)blockIdx.x >= items) return;
@@ -1378,20 +1321,30 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
         const int i = a.wide[1 + item / a.n_parts], part = item % a.n_parts;
         RowOut& o = a.rows[i];
-        if (o.state == ROW_SLOW) continue;
         const Params q = params_of(a, i / a.per);
+        float x_lo = o.x_m, x_hi = o.x_m;
+        int type = o.type;
+        __syncthreads();
+        if (type != BY_SHARE) {
+            if (!find_ranges(s, a, o, q, a.slices + (int64_t)i * a.n_parts * (kRanges / 2), tid, x_lo, x_hi)) type = -1;
+            else if (o.x_m >= x_hi) type = BY_SHARE, x_lo = x_hi = o.x_m;          // min-p keeps less
+        }
+        if (part == 0 && tid == 0) {
+            o.found = type;
+            o.x_lo = x_lo;
+            o.x_hi = x_hi;
+        }
+        if (type < 0) continue;
         const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
         const int p0 = part * a.part_len, run = a.part_len / kPartWaves, v_begin = min(p0 + wave * run, a.vocab), v_end = min(v_begin + run, a.vocab);
         const int bits = sum_bits(a.vocab);
         const TableWeight weight(s_pow, o.top, q.inv, bits);
-        const float x_lo = o.x_lo, x_hi = o.x_hi;
         u64* const lists = a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len;
         u64* const list = lists + (part * kPartWaves + wave) * (int64_t)a.list_len;
         u64 sum = 0;
         int above = 0, listed = 0;
         float next[kPer];
         R::load(row, v_begin, v_end, lane, next);
-        __syncthreads();
         for (int v0 = v_begin; v0 < v_end; v0 += kStep) {
             float x[kPer];
 #pragma unroll
@@ -1427,85 +1380,142 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
                 to.listed[w] = s_listed[w];
             }
         }
-        if (!last_of(&o.tickets[1], a.n_parts, tid, &s_last)) continue;
-        // the row from its parts
-        static_assert(kMostParts * kPartWaves == kPartThreads);
-        s_part[tid] = tid < a.n_parts * kPartWaves ? a.parts[(int64_t)i * a.n_parts + tid / kPartWaves].above_q[tid % kPartWaves] : 0;
-        __syncthreads();
-        int n_above = lane < a.n_parts ? a.parts[(int64_t)i * a.n_parts + lane].above : 0;
-        n_above = wave_sum_int(n_above);
-        const int n = read_lists(s, a, i, list_length(a, i, tid), tid, (1ull << 56) - 1);
-        if (n < 0) {
-            if (tid == 0) o.state = ROW_SLOW;
-            continue;
+    }
+}
+
+// The cut of a row from what k_filter_gather left, and the draw; false: it does not lie there
+struct CloseShared { FinishShared f; u64 part[kMostParts * kPartWaves]; word2 pow[256]; };
+template <typename T, bool VEC, bool MASK>
+__device__ __forceinline__ bool close_row(CloseShared& c_s, const FilterArgs& a, int i, RowOut& o, const Params& q, int tid) {
+    FinishShared& s = c_s.f;
+    u64* const s_part = c_s.part;
+    const int lane = tid & 63, run = a.part_len / kPartWaves, bits = sum_bits(a.vocab);
+    const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
+    const float x_lo = o.x_lo, x_hi = o.x_hi;
+    if (tid < 256) c_s.pow[tid] = kPow.at[tid];
+    const TableWeight weight(c_s.pow, o.top, q.inv, bits);
+    // the row from its parts
+    if (tid < kMostParts * kPartWaves) s_part[tid] = tid < a.n_parts * kPartWaves ? a.parts[(int64_t)i * a.n_parts + tid / kPartWaves].above_q[tid % kPartWaves] : 0;
+    __syncthreads();
+    int n_above = lane < a.n_parts ? a.parts[(int64_t)i * a.n_parts + lane].above : 0;
+    n_above = wave_sum_int(n_above);
+    const int n = read_lists<kThreads>(s, a, i, list_length(a, i, tid), tid, (1ull << 56) - 1);
+    if (n < 0) return false;
+    u64 cut = (u64)~key_of(x_hi) << 24 | 0xFFFFFF;      // (x_hi itself is above)
+    bool good = true;
+    if (o.found != BY_SHARE) {
+        const bool count = o.found == BY_COUNT;
+        const u64 over_q = wave_sum_u64(s_part[lane] + s_part[lane + 64] + s_part[lane + 128] + s_part[lane + 192]);
+        u64 mine = 0;
+        for (int e = tid; e < n; e += kThreads) mine += s.weight[e] = count ? 1 : weight(logit_of(s.list[e]));
+        const u64 listed = block_sum<kThreads>(s, mine, 0, tid).q;
+        // what the range may still keep; the cut lies in it if something, and no more than it has
+        const double left = count ? (double)(q.k - n_above) : ceil((double)q.p * o.total * ldexp(1.0, bits)) - (double)over_q;
+        good = n > 0 && left >= 1.0 && left <= (double)listed;
+        if (good)
+            cut = last_item<false, kThreads>(s, n, (u64)~(key_of(x_hi) - 1) << 24, (u64)~key_of(x_lo) << 24 | 0xFFFFFF, (u64)left, tid,
+                                             [&](int e) { return s.list[e]; }, [&](int e) { return s.weight[e]; }).key;
+        if (q.by_share) cut = min(cut, (u64)~key_of(o.x_m) << 24 | 0xFFFFFF);
+    }
+    if (!good) return false;
+    int kept = 0;
+    for (int e = tid; e < n; e += kThreads) {
+        const u64 c = s.list[e];
+        if (c > cut) continue;
+        ++kept;
+        if (!MASK) atomicAdd(&s_part[token_of(c) / run], weight(logit_of(c)));
+    }
+    kept = block_sum<kThreads>(s, 0, kept, tid).n + n_above;
+    int token = -1;
+    float logp = 0.f;
+    if (!MASK) {
+        const float u = a.u[i];
+        // a lane four waves' runs
+        u64 each[4], own = 0;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) own += each[e] = s_part[4 * lane + e];
+        const u64 up = wave_scan_u64(own), total = of_lane(up, 63);
+        u64 target = u > 0.f ? min((u64)((double)u * (double)total), total - 1) : 0;
+        const int of = __ffsll((unsigned long long)__ballot(up > target)) - 1;
+        target -= of_lane(up - own, of);
+        int w = 0;
+#pragma unroll
+        for (int e = 0; e < 3; ++e) {
+            const u64 q_e = of_lane(each[e], of);
+            if (w == e && target >= q_e) {
+                target -= q_e;
+                ++w;
+            }
         }
-        u64 cut = (u64)~key_of(x_hi) << 24 | 0xFFFFFF;      // (x_hi itself is above)
-        bool good = true;
-        if (o.type != BY_SHARE) {
-            const bool count = o.type == BY_COUNT;
-            const u64 over_q = wave_sum_u64(s_part[lane] + s_part[lane + 64] + s_part[lane + 128] + s_part[lane + 192]);
-            u64 mine = 0;
-            for (int e = tid; e < n; e += kFinishThreads) mine += s.weight[e] = count ? 1 : weight(logit_of(s.list[e]));
-            const u64 listed = block_sum(s, mine, 0, tid).q;
-            // what the range may still keep; the cut lies in it if something, and no more than it has
-            const double left = count ? (double)(q.k - n_above) : ceil((double)q.p * o.total * ldexp(1.0, bits)) - (double)over_q;
-            good = n > 0 && left >= 1.0 && left <= (double)listed;
-            if (good)
-                cut = last_item<false>(s, n, (u64)~(key_of(x_hi) - 1) << 24, (u64)~key_of(x_lo) << 24 | 0xFFFFFF, (u64)left, tid, [&](int e) { return s.list[e]; },
-                                [&](int e) { return s.weight[e]; }).key;
-            if (q.by_share) cut = min(cut, (u64)~key_of(o.x_m) << 24 | 0xFFFFFF);
-        }
-        if (!good) {
-            if (tid == 0) o.state = ROW_SLOW;
-            continue;
-        }
-        int kept = 0;
-        for (int e = tid; e < n; e += kFinishThreads) {
-            const u64 c = s.list[e];
-            if (c > cut) continue;
-            ++kept;
-            if (!MASK) atomicAdd(&s_part[token_of(c) / run], weight(logit_of(c)));
-        }
-        kept = block_sum(s, 0, kept, tid).n + n_above;
-        int token = -1;
-        float logp = 0.f;
+        const int first = (4 * of + w) * run, end = min(first + run, a.vocab), share = (run / 16 + kWaves - 1) / kWaves * 16;
+        const float cut_x = logit_of(cut);
+        const int cut_v = token_of(cut);
+        token = draw_part<T, VEC, kThreads>(s, row, first, share, end, target, tid,
+                                            [&](float x, int v) { return x > cut_x || (x == cut_x && v <= cut_v) ? weight(x) : 0; });
+        logp = (float)(((double)to_f(row[token]) - (double)o.top) * q.inv - log((double)total * ldexp(1.0, -bits)));
+    }
+    if (tid == 0) {
+        o.cut = cut;
+        o.state = ROW_CUT;
+        if (a.kept) a.kept[i] = kept;
         if (!MASK) {
-            const float u = a.u[i];
-            // a lane four waves' runs
-            u64 each[4], own = 0;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) own += each[e] = s_part[4 * lane + e];
-            const u64 up = wave_scan_u64(own), total = of_lane(up, 63);
-            u64 target = u > 0.f ? min((u64)((double)u * (double)total), total - 1) : 0;
-            const int of = __ffsll((unsigned long long)__ballot(up > target)) - 1;
-            target -= of_lane(up - own, of);
-            int w = 0;
-#pragma unroll
-            for (int e = 0; e < 3; ++e) {
-                const u64 q_e = of_lane(each[e], of);
-                if (w == e && target >= q_e) {
-                    target -= q_e;
-                    ++w;
-                }
-            }
-            const int first = (4 * of + w) * run, end = min(first + run, a.vocab), quarter = (run / 16 + kPartWaves - 1) / kPartWaves * 16;
-            const float cut_x = logit_of(cut);
-            const int cut_v = token_of(cut);
-            token = draw_part<T, VEC>(s, row, first, quarter, end, target, tid,
-                                      [&](float x, int v) { return x > cut_x || (x == cut_x && v <= cut_v) ? weight(x) : 0; });
-            logp = (float)(((double)to_f(row[token]) - (double)o.top) * q.inv - log((double)total * ldexp(1.0, -bits)));
+            a.token[i] = token;
+            if (a.logprob) a.logprob[i] = logp;
         }
-        if (tid == 0) {
-            o.cut = cut;
-            o.state = ROW_CUT;
-            if (a.kept) a.kept[i] = kept;
-            if (!MASK) {
-                a.token[i] = token;
-                if (a.logprob) a.logprob[i] = logp;
-            }
-        }
+    }
+    return true;
+}
+
+// The rows that k_filter_gather has read, and those that are left: a workgroup a row
+template <typename T, bool VEC, bool MASK>
+__global__ __launch_bounds__(kThreads) void k_filter_close(FilterArgs a) {
+    __shared__ union { Shared slow; CloseShared close; } shared;
+    const int i = blockIdx.x, b = i / a.per, tid = threadIdx.x, state = a.rows[i].state;
+    if (state != ROW_WIDE && state != ROW_SLOW) return;
+    const Params q = params_of(a, b);
+    if (state == ROW_WIDE && a.rows[i].found >= 0) {
+        if (close_row<T, VEC, MASK>(shared.close, a, i, a.rows[i], q, tid)) return;
         __syncthreads();
     }
+    Shared& s = shared.slow;
+    Row<T, VEC> row{(const T*)a.logits + (int64_t)i * a.row_stride, a.vocab, tid, tid & 63, tid >> 6, s, RowState{}};
+    RowState& r = row.r;
+    row.look();
+    r.inv = q.inv;
+    const double range = (double)r.top - (double)r.least;
+    r.per_unit = fmax(64.0 * r.inv, range > 0.0 ? (kBins - 1.5) / range : 1.0);
+    r.bin_width = r.inv / r.per_unit;
+    r.bits = min(50, 61 - (32 - __clz(a.vocab)));
+    r.cut = (u64)~key_of(r.least) << 24 | 0xFFFFFF;
+    r.kept = r.live;
+    r.listed = -1;
+    const int k = q.one ? 1 : q.by_count ? q.k : r.live;
+    if (k < r.live) row.template select<true>([&](double) { return (double)k; });
+    if (q.by_mass) {
+        if (r.listed >= 0) {
+            r.kept = list_below(s, r, s.big, r.kept, tid, [&](double total) { return (double)q.p * total; });
+            r.cut = s.big[r.kept - 1];
+        } else {
+            row.template select<false>([&](double total) { return (double)q.p * total; });
+        }
+    }
+    if (q.by_share) {
+        const double most = -log((double)q.m);
+        row.at_least(first_key(r.top, tid & 63, [&](float x) { return ((double)r.top - (double)x) * r.inv <= most; }));
+    }
+    int token = -1;
+    float logp = 0.f;
+    if (!MASK) token = row.draw(a.u[i], logp);
+    else if (r.kept < 0) row.count();
+    if (tid != 0) return;
+    if (a.kept) a.kept[i] = r.kept;
+    if (MASK) {
+        a.rows[i].cut = r.cut;
+        a.rows[i].state = ROW_CUT;
+        return;
+    }
+    a.token[i] = token;
+    if (a.logprob) a.logprob[i] = logp;
 }
 
 // In place: what is dropped.  Else, of the rows that were not written from their lists, what is kept.
@@ -1549,11 +1559,12 @@ Plan plan_of(int rows, int vocab) {
     p.sample_len = f < 0.015 ? 4 : f < 0.03 ? 2 : 1;
     const int groups = kGroups / 4 * std::min(4, std::max(1, p.part_len / kPartWaves / 256));      // (a short run fills a part of a step)
     p.sample_rank = std::min(groups, std::max(1, (int)(groups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
-    // six times what a wave should find, room for k_filter_bins' counts, and no more than there is
-    p.list_len = std::max(kRanges / 4 / kPartWaves, (6 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16);
+    // six times what a wave should find
+    p.list_len = std::max(64, (6 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16);
     return p;
 }
 size_t lists_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * kPartWaves * p.list_len * sizeof(u64); }
+size_t slices_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * (kRanges / 2) * sizeof(u32); }
 size_t parts_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * sizeof(Part); }
 
 template <typename T, bool MASK>
@@ -1567,7 +1578,8 @@ tasc_status enqueue(FilterArgs a, int rows, void* workspace, hipStream_t st) {
         a.parts = (Part*)workspace;
         a.rows = (RowOut*)((char*)workspace + parts_bytes(p, rows));
         a.lists = (u64*)((char*)a.rows + (size_t)rows * sizeof(RowOut));
-        a.wide = (int32_t*)((char*)a.lists + lists_bytes(p, rows));
+        a.slices = (u32*)((char*)a.lists + lists_bytes(p, rows));
+        a.wide = (int32_t*)((char*)a.slices + slices_bytes(p, rows));
         a.n_parts = p.n_parts;
         a.part_len = p.part_len;
         a.list_len = p.list_len;
@@ -1582,9 +1594,9 @@ tasc_status enqueue(FilterArgs a, int rows, void* workspace, hipStream_t st) {
         if (a.top_k || a.top_p || a.min_p) {
             const dim3 some((unsigned)std::min<int64_t>((int64_t)rows * p.n_parts, kWideGrid));
             vec ? k_filter_bins<T, true><<<some, threads, 0, st>>>(a) : k_filter_bins<T, false><<<some, threads, 0, st>>>(a);
-            vec ? k_filter_gather<T, true, MASK><<<some, threads, 0, st>>>(a) : k_filter_gather<T, false, MASK><<<some, threads, 0, st>>>(a);
+            vec ? k_filter_gather<T, true><<<some, threads, 0, st>>>(a) : k_filter_gather<T, false><<<some, threads, 0, st>>>(a);
         }
-        vec ? k_filter_slow<T, true, MASK><<<all, dim3(kThreads), 0, st>>>(a) : k_filter_slow<T, false, MASK><<<all, dim3(kThreads), 0, st>>>(a);
+        vec ? k_filter_close<T, true, MASK><<<all, dim3(kThreads), 0, st>>>(a) : k_filter_close<T, false, MASK><<<all, dim3(kThreads), 0, st>>>(a);
         if (MASK) a.in_place ? k_filter_apply<T, true><<<parts, threads, 0, st>>>(a) : k_filter_apply<T, false><<<parts, threads, 0, st>>>(a);
     }
     TASC_LAUNCH_CHECK();
@@ -1617,7 +1629,7 @@ tasc_status check_workspace(const char* who, void* workspace, size_t ws_bytes, i
 extern "C" size_t tasc_sample_workspace_bytes(int32_t rows, int32_t vocab) {
     if (rows < 1 || rows > 65535 || vocab < 2 || vocab > 1 << 24) return 0;
     const Plan p = plan_of(rows, vocab);
-    return p.direct ? 0 : parts_bytes(p, rows) + (size_t)rows * sizeof(RowOut) + lists_bytes(p, rows) + ((size_t)rows + 1) * sizeof(int32_t);
+    return p.direct ? 0 : parts_bytes(p, rows) + (size_t)rows * sizeof(RowOut) + lists_bytes(p, rows) + slices_bytes(p, rows) + ((size_t)rows + 1) * sizeof(int32_t);
 }
 
 extern "C" tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature, const int32_t* top_k,
