@@ -729,6 +729,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
 struct __attribute__((aligned(16))) FinishShared {
     u64 list[kList], weight[kList];
     u64 bins[kFinishBins];
+    u32 counts[kFinishBins];
     u64 few_key[kFew], few_q[kFew];
     u64 red[kWaves];
     int32_t num[kWaves], few, n, bad;
@@ -843,6 +844,113 @@ __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid)
         all.n += s.num[w];
     }
     return all;
+}
+
+// The cut of the n places of s.list (weights beside them) by count (k > 0), then by mass (p < 1) of what is left, or of `total` (in the weights' units; below 0: of
+// what is left): one histogram of counts and weights for both, then the tokens of the bins that the two fall into.
+enum { CUT_DONE, CUT_MANY, CUT_BEYOND };                    // MANY: a bin holds more than kFew; BEYOND: the list's mass does not reach the limit
+struct ListCut { u64 cut, total; int kept, state; u64 listed; };     // total: weights of the kept ones; listed: of all
+template <int NT>
+__device__ __forceinline__ ListCut list_cut(FinishShared& s, int n, u64 lo, u64 hi, int k, double p, double total, int tid) {
+    const int lane = tid & 63, shift = max(0, 64 - 9 - __clzll((long long)(hi - lo)));
+    static_assert(kFinishBins == 1 << 9);
+    __syncthreads();
+    for (int i = tid; i < kFinishBins; i += NT) {
+        s.bins[i] = 0;
+        s.counts[i] = 0;
+    }
+    if (tid == 0) s.few = 0;
+    __syncthreads();
+#pragma unroll 4
+    for (int i = tid; i < n; i += NT) {
+        const u64 c = s.list[i], q = s.weight[i];
+        if (c > hi) continue;
+        atomicAdd(&s.bins[(c - lo) >> shift], q);
+        atomicAdd(&s.counts[(c - lo) >> shift], 1u);
+    }
+    __syncthreads();
+    // every wave for itself, 8 bins a lane
+    constexpr int PER = kFinishBins / 64;
+    u64 w[PER], w_own = 0, c_own = 0;
+    u32 c[PER];
+#pragma unroll
+    for (int e = 0; e < PER; ++e) {
+        w_own += w[e] = s.bins[PER * lane + e];
+        c_own += c[e] = s.counts[PER * lane + e];
+    }
+    const u64 w_up = wave_scan_u64(w_own), c_up = wave_scan_u64(c_own);
+    ListCut out{hi, of_lane(w_up, 63), (int)of_lane(c_up, 63), CUT_DONE, of_lane(w_up, 63)};
+    int held = -1, few = 0;                                 // the bin whose tokens lie in few_*
+    u64 key = 0, q = 0, below = 0;
+    int rank = 0;
+    // the last bin whose count (weight) before it is below the limit, its tokens, and the last of those
+    auto narrow = [&](bool by_count, u64 limit) {
+        u64 w_at = w_up - w_own, c_at = c_up - c_own, w_before = 0, c_before = 0;
+        int last = -1;
+#pragma unroll
+        for (int e = 0; e < PER; ++e) {
+            if (c[e] && (by_count ? c_at : w_at) < limit) {
+                last = PER * lane + e;
+                w_before = w_at;
+                c_before = c_at;
+            }
+            w_at += w[e];
+            c_at += c[e];
+        }
+        const u64 have = __ballot(last >= 0);
+        if (!have) {
+            out.state = CUT_MANY;
+            return;
+        }
+        const int from = 63 - __clzll(have), b = __builtin_amdgcn_readlane(last, from);
+        w_before = of_lane(w_before, from);
+        c_before = of_lane(c_before, from);
+        if (b != held) {
+            if (held >= 0) {
+                __syncthreads();
+                if (tid == 0) s.few = 0;
+                __syncthreads();
+            }
+            held = b;
+#pragma unroll 4
+            for (int i = tid; i < n; i += NT) {
+                const u64 at = s.list[i];
+                if (at > hi || (int)((at - lo) >> shift) != b) continue;
+                const int place = atomicAdd(&s.few, 1);
+                if (place < kFew) {
+                    s.few_key[place] = at;
+                    s.few_q[place] = s.weight[i];
+                }
+            }
+            __syncthreads();
+            few = s.few;
+            if (few > kFew) {
+                out.state = CUT_MANY;
+                return;
+            }
+            key = lane < few ? s.few_key[lane] : ~0ull;
+            q = lane < few ? s.few_q[lane] : 0;
+            below = 0;
+            rank = 0;
+            for (int j = 0; j < few; ++j) {
+                const bool less = of_lane(key, j) < key;
+                below += less ? of_lane(q, j) : 0;
+                rank += less;
+            }
+        }
+        const bool kept = lane < few && (by_count ? c_before + rank : w_before + below) < limit;
+        const int l = __ffsll((unsigned long long)__ballot(kept && rank == __popcll(__ballot(kept)) - 1)) - 1;
+        out.cut = of_lane(key, l & 63);
+        out.kept = (int)c_before + __builtin_amdgcn_readlane(rank, l & 63) + 1;
+        out.total = w_before + of_lane(below, l & 63) + of_lane(q, l & 63);
+    };
+    if (k > 0) narrow(true, (u64)k);
+    if (p < 1.0 && out.state == CUT_DONE) {
+        const double limit = ceil(p * (total < 0.0 ? (double)out.total : total));
+        if (!((double)out.total >= limit)) out.state = CUT_BEYOND;
+        else narrow(false, (u64)fmax(limit, 1.0));
+    }
+    return out;
 }
 
 // A row's lists one behind the other in s.list, entries beyond `last` as none (~0): how many places, or -1 if they do not fit or one of them is not whole;
@@ -969,6 +1077,11 @@ __device__ __forceinline__ int draw_part(FinishShared& s, const T* row, int p0, 
     return token;
 }
 
+// The sum of a row's weights in the largest's, from the lanes' parts
+__device__ __forceinline__ double part_total(double sum, double scale, const RowState& r) {
+    return wave_sum64_dpp(sum > 0.0 ? sum * exp_neg(scale - (double)r.top * r.inv) : 0.0);
+}
+
 template <typename T, bool VEC, bool MASK>
 __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) {
     __shared__ FinishShared s;
@@ -1045,10 +1158,11 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         const u64 lo = (u64)~key_of(r.top) << 24, hi = a.direct || whole ? ((1ull << 56) - 1) : (u64)~key_of(bound) << 24 | 0xFFFFFF;
         auto comp = [&](int e) { return s.list[e]; };
         auto weight = [&](int e) { return s.weight[e]; };
-        bool held = whole;                                  // the list holds all that the filters so far keep
+        bool held = whole, counted = false;                 // the list holds all that the filters so far keep; `by` counts them
+        u64 counted_q = 0;
         if (p.by_share) x_m = from_key(first_key(r.top, lane, [&, most = -log((double)p.m)](float x) { return ((double)r.top - (double)x) * r.inv <= most; }));
         // the weights, 0 for an empty place; each is looked at by the thread that sets it, up to last_item's barriers
-        if (!nothing_listed && (p.by_mass || !MASK)) {
+        if (!nothing_listed && (by_count || p.by_mass || !MASK)) {
 #pragma unroll 4
             for (int e = tid; e < n; e += kFinishThreads) s.weight[e] = s.list[e] <= hi ? weight_of(r, logit_of(s.list[e]), kListBits) : 0;
         }
@@ -1065,43 +1179,66 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
                 cut = min(min(s.red[0], s.red[1]), min(s.red[2], s.red[3]));
                 held = true;
             }
-            if (by_count) {
-                if (p.k <= valid) {
-                    cut = last_item<false, kFinishThreads>(s, n, lo, hi, (u64)p.k, tid, comp, [](int) { return 1ull; }).key;
-                    held = true;
-                } else if (!held) {
+            ListCut by{0, 0, 0, CUT_MANY, 0};
+            const bool from_parts = p.by_mass && !by_count && !held;          // the mass is the whole row's
+            if (from_parts && has_sum) total = part_total(part_sum, part_scale, r);
+            if ((by_count && p.k <= valid) || (!by_count && p.by_mass && (held || has_sum))) {
+                by = list_cut<kFinishThreads>(s, n, lo, hi, by_count ? p.k : 0, p.by_mass ? (double)p.p : 1.0, from_parts ? total * 0x1p50 : -1.0, tid);
+                static_assert(kListBits == 50);
+                if (by.state == CUT_DONE) {
+                    cut = by.cut;
+                    held = counted = true;
+                } else if (by.state == CUT_BEYOND) {
                     wide = true;
+                    listed_q = by.listed;
                 }
             }
-            if (p.by_mass && !wide) {
-                u64 mine = 0;
-                for (int e = tid; e < n; e += kFinishThreads) mine += s.list[e] <= cut ? weight(e) : 0;
-                const u64 listed = listed_q = block_sum<kFinishThreads>(s, mine, 0, tid).q;
-                double limit = 0.0;
-                if (held) {
-                    limit = ceil((double)p.p * (double)listed);
-                } else if (has_sum) {
-                    total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp_neg(part_scale - (double)r.top * r.inv) : 0.0);
-                    limit = ceil((double)p.p * total * 0x1p50);
-                    static_assert(kListBits == 50);
-                    wide = !((double)listed >= limit);
-                } else {
-                    wide = true;
+            if (by.state == CUT_MANY) {                     // (ties of thousands: the same one after the other)
+                if (by_count) {
+                    if (p.k <= valid) {
+                        cut = last_item<false, kFinishThreads>(s, n, lo, hi, (u64)p.k, tid, comp, [](int) { return 1ull; }).key;
+                        held = true;
+                    } else if (!held) {
+                        wide = true;
+                    }
                 }
-                if (!wide) {
-                    cut = last_item<false, kFinishThreads>(s, n, lo, min(hi, cut), (u64)fmax(limit, 1.0), tid, comp, weight).key;
-                    held = true;
+                if (p.by_mass && !wide) {
+                    u64 mine = 0;
+                    for (int e = tid; e < n; e += kFinishThreads) mine += s.list[e] <= cut ? weight(e) : 0;
+                    const u64 listed = listed_q = block_sum<kFinishThreads>(s, mine, 0, tid).q;
+                    double limit = 0.0;
+                    if (held) {
+                        limit = ceil((double)p.p * (double)listed);
+                    } else if (has_sum) {
+                        limit = ceil((double)p.p * total * 0x1p50);
+                        static_assert(kListBits == 50);
+                        wide = !((double)listed >= limit);
+                    } else {
+                        wide = true;
+                    }
+                    if (!wide) {
+                        cut = last_item<false, kFinishThreads>(s, n, lo, min(hi, cut), (u64)fmax(limit, 1.0), tid, comp, weight).key;
+                        held = true;
+                    }
                 }
+            }
+            if (counted) {
+                kept = by.kept;
+                counted_q = by.total;
             }
             if (p.by_share && !wide) {
                 if (x_m >= bound) held = true;
-                cut = min(cut, (u64)~key_of(x_m) << 24 | 0xFFFFFF);
+                const u64 least_kept = (u64)~key_of(x_m) << 24 | 0xFFFFFF;
+                if (least_kept < cut) {
+                    cut = least_kept;
+                    counted = false;
+                }
             }
             wide = wide || !held;
         }
         if (wide) {
             type = !any ? -1 : by_count ? (p.by_mass ? -1 : BY_COUNT) : p.by_mass ? (has_sum ? BY_MASS : -1) : p.by_share ? BY_SHARE : -1;
-            if (type == BY_MASS) total = wave_sum64_dpp(part_sum > 0.0 ? part_sum * exp_neg(part_scale - (double)r.top * r.inv) : 0.0);
+            if (type == BY_MASS) total = part_total(part_sum, part_scale, r);
             if (nothing_listed) listed_q = 0;
         } else if (nothing_listed) {                        // nothing is dropped: the part that the draw falls into, read again
             const double own = part_sum > 0.0 ? part_sum * exp_neg(part_scale - (double)r.top * r.inv) : 0.0, up = wave_scan64_dpp(own);
@@ -1114,24 +1251,27 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
             logp = (float)(((double)to_f(row[token]) - (double)r.top) * r.inv - log(total));
             kept = live;
         } else {
-            u64 q = 0;
-            int c = 0;
-            for (int e = tid; e < n; e += kFinishThreads) {
-                const bool in = s.list[e] <= cut;
-                c += in;
-                if (!MASK && in) q += weight(e);
+            if (!counted) {
+                u64 q = 0;
+                int c = 0;
+                for (int e = tid; e < n; e += kFinishThreads) {
+                    const bool in = s.list[e] <= cut;
+                    c += in;
+                    if (!MASK && in) q += weight(e);
+                }
+                const Sum all = block_sum<kFinishThreads>(s, q, c, tid);
+                kept = all.n;
+                counted_q = all.q;
             }
-            const Sum all = block_sum<kFinishThreads>(s, q, c, tid);
-            kept = all.n;
             if (!MASK) {
                 const float u = a.u[i];
-                const u64 limit = u > 0.f ? min((u64)((double)u * (double)all.q), all.q - 1) + 1 : 1;
+                const u64 limit = u > 0.f ? min((u64)((double)u * (double)counted_q), counted_q - 1) + 1 : 1;
                 auto token_at = [&](int e) { return s.list[e] <= cut ? (u64)token_of(s.list[e]) << 32 | (u32)e : ~0ull; };
                 const Found f = kept <= kFew ? last_item<true, kFinishThreads>(s, n, 0, ~0ull - 1, limit, tid, token_at, weight)
                                              : last_item<false, kFinishThreads>(s, n, 0, (u64)a.vocab << 32, limit, tid, token_at, weight);
                 token = (int)(f.key >> 32);
                 const float x = logit_of(s.list[(u32)f.key]);
-                logp = p.one ? 0.f : (float)(((double)x - (double)r.top) * r.inv - log((double)all.q * 0x1p-50));
+                logp = p.one ? 0.f : (float)(((double)x - (double)r.top) * r.inv - log((double)counted_q * 0x1p-50));
             }
         }
     }
@@ -1163,8 +1303,9 @@ __global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) 
         o.listed_q = listed_q;
         o.total = total;
         o.x_m = x_m;
+        o.found = -1;
         a.rows[i] = o;
-        if (o.state == ROW_WIDE) a.wide[1 + atomicAdd(a.wide, 1)] = i;
+        if (o.state == ROW_WIDE || o.state == ROW_SLOW) a.wide[1 + atomicAdd(a.wide, 1)] = i;
     }
     if (keep_all) kept = live;
     else if (wide) return;
@@ -1206,7 +1347,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
     for (int item = blockIdx.x; item < items; item += gridDim.x) {
         const int i = a.wide[1 + item / a.n_parts], part = item % a.n_parts;
         RowOut& o = a.rows[i];
-        if (o.type == BY_SHARE) continue;
+        if (o.type != BY_MASS && o.type != BY_COUNT) continue;
         const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
         const int p0 = part * a.part_len, run = a.part_len / kPartWaves, v_begin = min(p0 + wave * run, a.vocab), v_end = min(v_begin + run, a.vocab);
         const Ranges range_of(o);
@@ -1325,7 +1466,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         float x_lo = o.x_m, x_hi = o.x_m;
         int type = o.type;
         __syncthreads();
-        if (type != BY_SHARE) {
+        if (type >= 0 && type != BY_SHARE) {
             if (!find_ranges(s, a, o, q, a.slices + (int64_t)i * a.n_parts * (kRanges / 2), tid, x_lo, x_hi)) type = -1;
             else if (o.x_m >= x_hi) type = BY_SHARE, x_lo = x_hi = o.x_m;          // min-p keeps less
         }
@@ -1466,18 +1607,9 @@ __device__ __forceinline__ bool close_row(CloseShared& c_s, const FilterArgs& a,
     return true;
 }
 
-// The rows that k_filter_gather has read, and those that are left: a workgroup a row
+// The cut of a row whatever it is, from the row itself
 template <typename T, bool VEC, bool MASK>
-__global__ __launch_bounds__(kThreads) void k_filter_close(FilterArgs a) {
-    __shared__ union { Shared slow; CloseShared close; } shared;
-    const int i = blockIdx.x, b = i / a.per, tid = threadIdx.x, state = a.rows[i].state;
-    if (state != ROW_WIDE && state != ROW_SLOW) return;
-    const Params q = params_of(a, b);
-    if (state == ROW_WIDE && a.rows[i].found >= 0) {
-        if (close_row<T, VEC, MASK>(shared.close, a, i, a.rows[i], q, tid)) return;
-        __syncthreads();
-    }
-    Shared& s = shared.slow;
+__device__ __forceinline__ void slow_row(Shared& s, const FilterArgs& a, int i, const Params& q, int tid) {
     Row<T, VEC> row{(const T*)a.logits + (int64_t)i * a.row_stride, a.vocab, tid, tid & 63, tid >> 6, s, RowState{}};
     RowState& r = row.r;
     row.look();
@@ -1516,6 +1648,22 @@ __global__ __launch_bounds__(kThreads) void k_filter_close(FilterArgs a) {
     }
     a.token[i] = token;
     if (a.logprob) a.logprob[i] = logp;
+}
+
+// The rows that k_filter_gather has read, and those that are left: a workgroup a row
+template <typename T, bool VEC, bool MASK>
+__global__ __launch_bounds__(kThreads) void k_filter_close(FilterArgs a) {
+    __shared__ union { Shared slow; CloseShared close; } shared;
+    const int tid = threadIdx.x;
+    if ((int)blockIdx.x >= *a.wide) return;
+    const int i = a.wide[1 + blockIdx.x];
+    RowOut& o = a.rows[i];
+    const Params q = params_of(a, i / a.per);
+    if (o.found >= 0) {
+        if (close_row<T, VEC, MASK>(shared.close, a, i, o, q, tid)) return;
+        __syncthreads();
+    }
+    slow_row<T, VEC, MASK>(shared.slow, a, i, q, tid);
 }
 
 // In place: what is dropped.  Else, of the rows that were not written from their lists, what is kept.
