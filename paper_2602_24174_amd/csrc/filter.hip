@@ -23,7 +23,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096, kWideList =
 constexpr int kListBits = 50;                              // a list's weights: 2^11 of them stay below 2^62
 // a workgroup of k_filter_parts, its waves' shares; lists of a row together, and entries that k_filter_finish takes
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPer = 16, kStep = 64 * kPer;
-constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 1024, kMostParts = 64, kList = 2048, kGroups = 64, kWanted = 1024;
+constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 1024, kMostParts = 64, kList = 2048, kCloseList = 4096, kGroups = 64, kWanted = 1024;
 constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64, kRanges = 2048, kWideGrid = 2048;
 
 // What a part of a row comes to
@@ -726,28 +726,32 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
 }
 
 // ---------------------------------------------------------------- a row from its lists
-struct __attribute__((aligned(16))) FinishShared {
-    u64 list[kList], weight[kList];
+template <int ROOM>
+struct __attribute__((aligned(16))) ListShared {
+    static constexpr int room = ROOM;
+    u64 list[ROOM], weight[ROOM];
     u64 bins[kFinishBins];
     u32 counts[kFinishBins];
     u64 few_key[kFew], few_q[kFew];
     u64 red[kWaves];
     int32_t num[kWaves], few, n, bad;
 };
-__device__ __forceinline__ void append_to(FinishShared& s, bool in, u64 c, int lane) {
+template <typename S>
+__device__ __forceinline__ void append_to(S& s, bool in, u64 c, int lane) {
     const u64 m = __ballot(in);
     if (!m) return;
     int at = 0;
     if (lane == 0) at = atomicAdd(&s.n, __popcll(m));
     at = __builtin_amdgcn_readfirstlane(at) + __builtin_amdgcn_mbcnt_hi((u32)(m >> 32), __builtin_amdgcn_mbcnt_lo((u32)m, 0));
-    if (in && at < kList) s.list[at] = c;
+    if (in && at < S::room) s.list[at] = c;
 }
+using FinishShared = ListShared<kList>;
 struct Found { u64 key, sum; };      // sum: up to it and with it
 
 // Of n items with weights q (0: not there), in the order of their keys within [lo, hi]: the last whose sum of those before it is below `limit`
 // (FEW: there are no more than kFew of them).
-template <bool FEW, int NT, typename Key, typename Weight>
-__device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 hi, u64 limit, int tid, Key key, Weight weight) {
+template <bool FEW, int NT, typename S, typename Key, typename Weight>
+__device__ __forceinline__ Found last_item(S& s, int n, u64 lo, u64 hi, u64 limit, int tid, Key key, Weight weight) {
     const int lane = tid & 63;
     u64 sum = 0;
     if (FEW) {
@@ -827,8 +831,8 @@ __device__ __forceinline__ Found last_item(FinishShared& s, int n, u64 lo, u64 h
     }
 }
 struct Sum { u64 q; int n; };
-template <int NT>
-__device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid) {
+template <int NT, typename S>
+__device__ __forceinline__ Sum block_sum(S& s, u64 q, int n, int tid) {
     q = wave_sum_u64(q);
     n = wave_sum_int(n);
     __syncthreads();
@@ -850,8 +854,8 @@ __device__ __forceinline__ Sum block_sum(FinishShared& s, u64 q, int n, int tid)
 // what is left): one histogram of counts and weights for both, then the tokens of the bins that the two fall into.
 enum { CUT_DONE, CUT_MANY, CUT_BEYOND };                    // MANY: a bin holds more than kFew; BEYOND: the list's mass does not reach the limit
 struct ListCut { u64 cut, total; int kept, state; u64 listed; };     // total: weights of the kept ones; listed: of all
-template <int NT>
-__device__ __forceinline__ ListCut list_cut(FinishShared& s, int n, u64 lo, u64 hi, int k, double p, double total, int tid) {
+template <int NT, typename S>
+__device__ __forceinline__ ListCut list_cut(S& s, int n, u64 lo, u64 hi, int k, double p, double total, int tid) {
     const int lane = tid & 63, shift = max(0, 64 - 9 - __clzll((long long)(hi - lo)));
     static_assert(kFinishBins == 1 << 9);
     __syncthreads();
@@ -953,13 +957,13 @@ __device__ __forceinline__ ListCut list_cut(FinishShared& s, int n, u64 lo, u64 
     return out;
 }
 
-// A row's lists one behind the other in s.list, entries beyond `last` as none (~0): how many places, or -1 if they do not fit or one of them is not whole;
-// s.n counts the others.  A thread a list for their lengths, then a thread an entry.
 __device__ __forceinline__ int list_length(const FilterArgs& a, int i, int tid) {      // of the thread's list
     return tid < a.n_parts * kPartWaves ? a.parts[(int64_t)i * a.n_parts + tid / kPartWaves].listed[tid % kPartWaves] : 0;
 }
-template <int NT>
-__device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, int i, int own, int tid, u64 last) {
+// A row's lists one behind the other in s.list, entries beyond `last` as none (~0): how many places, or -1 if they do not fit or one of them is not whole;
+// s.n counts the others.  A thread a list (`own`: its length), then a thread an entry.
+template <int NT, typename S>
+__device__ __forceinline__ int read_lists(S& s, const FilterArgs& a, int i, int own, int tid, u64 last) {
     static_assert(kMostParts * kPartWaves <= NT && NT <= 2 * kFinishBins);
     const int lane = tid & 63, wave = tid >> 6;
     const u64* const lists = a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len;
@@ -974,7 +978,7 @@ __device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, 
         all += s.red[w];
     }
     const int n = (int)(u32)all;
-    if (all >> 32 || n > kList) return -1;
+    if (all >> 32 || n > S::room) return -1;
     u32* const ends = (u32*)s.bins;
     ends[tid] = (u32)(before + up);
     __syncthreads();
@@ -1009,8 +1013,8 @@ __device__ __forceinline__ int read_lists(FinishShared& s, const FilterArgs& a, 
 
 // The first of the logits [p0, end) whose weights up to it sum to more than `target` (the last with any if none does): the sums of the waves' steps, then the
 // logits of one step.  weight(x, v) is 0 where a token is not kept.
-template <typename T, bool VEC, int NT, typename Weight>
-__device__ __forceinline__ int draw_part(FinishShared& s, const T* row, int p0, int run, int end, u64 target, int tid, Weight weight) {
+template <typename T, bool VEC, int NT, typename S, typename Weight>
+__device__ __forceinline__ int draw_part(S& s, const T* row, int p0, int run, int end, u64 target, int tid, Weight weight) {
     using R = Run<T, VEC>;
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6), v_begin = min(p0 + wave * run, end), v_end = min(v_begin + run, end);
     const int steps = (run + kStep - 1) / kStep;            // of a wave
@@ -1376,7 +1380,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
 // The ranges in which the cut may lie, by the counts times the weights at their middles: ranges are narrow (0.005 of a logit, 200 tokens, for 150,000 tokens
 // over 10), so that a few are left for k_filter_gather, which has exact sums.  false: nothing is found.
 struct RangeShared { double sum[2][kPartWaves]; int32_t at[2][kPartWaves]; };
-__device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a, const RowOut& o, const Params& q, const u32* slices, int tid, float& x_lo, float& x_hi) {
+__device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a, const RowOut& o, const Params& q, const u32* slices, double aside, int tid, float& x_lo, float& x_hi) {
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Ranges range_of(o);
     const float below = o.ref;
@@ -1395,10 +1399,10 @@ __device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a,
             each[2 * e + 1] += two[e] >> 16;
         }
     }
-    // a range's weight is about its count times the weight at its middle; an eighth of a range to either side for all of them together (values that lie on a
-    // grid of their own, as bf16's, are off by half a range in one and by less on average: 0.02 of one over a hundred of them)
+    // a range's weight is about its count times the weight at its middle, and for all of them together the logits lie within an eighth of a range of the middles;
+    // bf16's, which lie on a grid of their own, within 0.3 of one (with an eighth there, 2 of 600 flat rows of 151936 bf16 logits missed their cut)
     const double limit = count ? (double)(q.k - o.listed) : (double)q.p * o.total - (double)o.listed_q * 0x1p-50;
-    const double width = count ? 0.0 : q.inv / (double)range_of.per_unit, step = exp_neg(-width), spare = exp_neg(-0.125 * width);
+    const double width = count ? 0.0 : q.inv / (double)range_of.per_unit, step = exp_neg(-width), spare = exp_neg(-aside * width);
     double middle = count ? 1.0 : exp_neg(fmin(((double)range_of.ref - (double)o.top) * q.inv - (PER * tid + 0.5) * width, 0.0));
     double least = 0.0, most = 0.0, v_least[PER], v_most[PER];
 #pragma unroll
@@ -1467,7 +1471,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         int type = o.type;
         __syncthreads();
         if (type >= 0 && type != BY_SHARE) {
-            if (!find_ranges(s, a, o, q, a.slices + (int64_t)i * a.n_parts * (kRanges / 2), tid, x_lo, x_hi)) type = -1;
+            if (!find_ranges(s, a, o, q, a.slices + (int64_t)i * a.n_parts * (kRanges / 2), sizeof(T) == 2 ? 0.3 : 0.125, tid, x_lo, x_hi)) type = -1;
             else if (o.x_m >= x_hi) type = BY_SHARE, x_lo = x_hi = o.x_m;          // min-p keeps less
         }
         if (part == 0 && tid == 0) {
@@ -1525,10 +1529,10 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
 }
 
 // The cut of a row from what k_filter_gather left, and the draw; false: it does not lie there
-struct CloseShared { FinishShared f; u64 part[kMostParts * kPartWaves]; word2 pow[256]; };
+struct CloseShared { ListShared<kCloseList> f; u64 part[kMostParts * kPartWaves]; word2 pow[256]; };
 template <typename T, bool VEC, bool MASK>
 __device__ __forceinline__ bool close_row(CloseShared& c_s, const FilterArgs& a, int i, RowOut& o, const Params& q, int tid) {
-    FinishShared& s = c_s.f;
+    auto& s = c_s.f;
     u64* const s_part = c_s.part;
     const int lane = tid & 63, run = a.part_len / kPartWaves, bits = sum_bits(a.vocab);
     const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
@@ -1707,8 +1711,8 @@ Plan plan_of(int rows, int vocab) {
     p.sample_len = f < 0.015 ? 4 : f < 0.03 ? 2 : 1;
     const int groups = kGroups / 4 * std::min(4, std::max(1, p.part_len / kPartWaves / 256));      // (a short run fills a part of a step)
     p.sample_rank = std::min(groups, std::max(1, (int)(groups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
-    // six times what a wave should find
-    p.list_len = std::max(64, (6 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16);
+    // eight times what a wave should find
+    p.list_len = std::max(64, (8 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16);
     return p;
 }
 size_t lists_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * kPartWaves * p.list_len * sizeof(u64); }
