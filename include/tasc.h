@@ -596,9 +596,12 @@ tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t ro
  *   top_p        fp32[rows], nullable; 1 and more keep all, 0 and less the first;  min_p fp32[rows], nullable; 0 and less keep all
  *   u            fp32[rows] in [0, 1)
  *   token        int32[rows];  logprob fp32[rows], nullable: ln of its share of the kept weights;  kept int32[rows], nullable: tokens kept
- * Weights are sums of whole numbers of 2^-39 to 2^-60 (by vocab), a bin of weights alike at a time, so a row's outputs depend neither on the order of the work nor on other
- * rows' contents.  A row without a distribution (a NaN, +infinity, nothing above -infinity, a temperature below 0 or a NaN as one of its parameters) gives
+ * Sums are of 64 bits, of whole numbers of 2^-36 of the largest weight (vocabularies of 2^24 tokens) to 2^-50 or finer or of fp64 in a fixed order, so a row's outputs depend neither on
+ * the order of the work nor on other rows' contents; exponentials are within 2e-13 of themselves.  A row without a distribution (a NaN, +infinity, nothing above -infinity, a temperature below 0 or a NaN as one of its parameters) gives
  * token -1 with a NaN as logprob, 0 kept.
+ * The workspace is 16-byte aligned; calls that may overlap need their own.  Rows that keep up to about 500 tokens (of vocabularies beyond 1536) are served from one read of
+ * their logits; those that keep more are read three times, and a few (a top-k beyond 500 together with a top-p, thousands of equal logits at the border) take
+ * a row's workgroup 100 us and more.
  * Limits: rows <= 65535, vocab in [2, 2^24].  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP.
  */
 size_t tasc_sample_workspace_bytes(int32_t rows, int32_t vocab);   /* for tasc_filter_logits, too, with rows = batch * (k + 1) */

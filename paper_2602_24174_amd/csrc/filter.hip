@@ -23,7 +23,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096, kWideList =
 constexpr int kListBits = 50;                              // a list's weights: 2^11 of them stay below 2^62
 // a workgroup of k_filter_parts, its waves' shares; lists of a row together, and entries that k_filter_finish takes
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPer = 16, kStep = 64 * kPer;
-constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 1024, kMostParts = 64, kList = 2048, kCloseList = 4096, kGroups = 64, kWanted = 1024;
+constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 1024, kMostParts = 64, kList = 1536, kCloseList = 6144, kGroups = 64, kWanted = 768;
 constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64, kRanges = 2048, kWideGrid = 2048;
 
 // What a part of a row comes to
@@ -1087,7 +1087,7 @@ __device__ __forceinline__ double part_total(double sum, double scale, const Row
 }
 
 template <typename T, bool VEC, bool MASK>
-__global__ __launch_bounds__(kFinishThreads) void k_filter_finish(FilterArgs a) {
+__global__ __launch_bounds__(kFinishThreads) __attribute__((amdgpu_waves_per_eu(5))) void k_filter_finish(FilterArgs a) {
     __shared__ FinishShared s;
     const int i = blockIdx.x, tid = threadIdx.x, lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
@@ -1380,7 +1380,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
 // The ranges in which the cut may lie, by the counts times the weights at their middles: ranges are narrow (0.005 of a logit, 200 tokens, for 150,000 tokens
 // over 10), so that a few are left for k_filter_gather, which has exact sums.  false: nothing is found.
 struct RangeShared { double sum[2][kPartWaves]; int32_t at[2][kPartWaves]; };
-__device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a, const RowOut& o, const Params& q, const u32* slices, double aside, int tid, float& x_lo, float& x_hi) {
+__device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a, const RowOut& o, const Params& q, const u32* slices, double aside, int more, int tid, float& x_lo, float& x_hi) {
     const int lane = tid & 63, wave = __builtin_amdgcn_readfirstlane(tid >> 6);
     const Ranges range_of(o);
     const float below = o.ref;
@@ -1400,7 +1400,8 @@ __device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a,
         }
     }
     // a range's weight is about its count times the weight at its middle, and for all of them together the logits lie within an eighth of a range of the middles;
-    // bf16's, which lie on a grid of their own, within 0.3 of one (with an eighth there, 2 of 600 flat rows of 151936 bf16 logits missed their cut)
+    // bf16's, which lie on a grid of their own, within 0.3 of one, and four ranges more (flat rows of 151936 bf16 logits missed their cut with an
+    // eighth in 2 of 600, with 0.3 in 1 of 1400, with two more in 1 of 2800)
     const double limit = count ? (double)(q.k - o.listed) : (double)q.p * o.total - (double)o.listed_q * 0x1p-50;
     const double width = count ? 0.0 : q.inv / (double)range_of.per_unit, step = exp_neg(-width), spare = exp_neg(-aside * width);
     double middle = count ? 1.0 : exp_neg(fmin(((double)range_of.ref - (double)o.top) * q.inv - (PER * tid + 0.5) * width, 0.0));
@@ -1444,6 +1445,8 @@ __device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a,
     b0 = min(min(s.at[0][0], s.at[0][1]), min(s.at[0][2], s.at[0][3]));
     b1 = min(min(min(s.at[1][0], s.at[1][1]), min(s.at[1][2], s.at[1][3])), kRanges - 1);
     const bool good = b0 < kRanges && limit > 0.0;
+    b0 = max(b0 - more, 0);
+    b1 = min(b1 + more, kRanges - 1);
     x_lo = from_key(first_key(range_of.ref, lane, [&](float x) { return range_of(x) <= b1; }));
     x_hi = b0 == 0 ? below : from_key(first_key(range_of.ref, lane, [&](float x) { return range_of(x) < b0; }));
     return good;
@@ -1471,7 +1474,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         int type = o.type;
         __syncthreads();
         if (type >= 0 && type != BY_SHARE) {
-            if (!find_ranges(s, a, o, q, a.slices + (int64_t)i * a.n_parts * (kRanges / 2), sizeof(T) == 2 ? 0.3 : 0.125, tid, x_lo, x_hi)) type = -1;
+            if (!find_ranges(s, a, o, q, a.slices + (int64_t)i * a.n_parts * (kRanges / 2), sizeof(T) == 2 ? 0.3 : 0.125, sizeof(T) == 2 ? 4 : 0, tid, x_lo, x_hi)) type = -1;
             else if (o.x_m >= x_hi) type = BY_SHARE, x_lo = x_hi = o.x_m;          // min-p keeps less
         }
         if (part == 0 && tid == 0) {
@@ -1711,8 +1714,8 @@ Plan plan_of(int rows, int vocab) {
     p.sample_len = f < 0.015 ? 4 : f < 0.03 ? 2 : 1;
     const int groups = kGroups / 4 * std::min(4, std::max(1, p.part_len / kPartWaves / 256));      // (a short run fills a part of a step)
     p.sample_rank = std::min(groups, std::max(1, (int)(groups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
-    // eight times what a wave should find
-    p.list_len = std::max(64, (8 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16);
+    // eight times what a wave should find, but no more than a row's lists may hold together
+    p.list_len = std::max(128, std::min(kList / kPartWaves, (8 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16));
     return p;
 }
 size_t lists_bytes(const Plan& p, int rows) { return (size_t)rows * p.n_parts * kPartWaves * p.list_len * sizeof(u64); }

@@ -90,7 +90,7 @@ def check(x, u, t=None, k=None, p=None, m=None, dtype=None, pad=0, offset=0, mas
 
 
 @pytest.mark.parametrize("kind", ["peaked", "flat", "masked", "ties", "equal", "wide", "zeros"])
-@pytest.mark.parametrize("rows, vocab, dtype, pad, offset", [(16, 500, "f32", 0, 0), (24, 2, "f32", 0, 0), (24, 3, "bf16", 1, 1), (16, 2048, "bf16", 0, 0), (16, 2049, "f32", 3, 0), (16, 3001, "bf16", 7, 8), (16, 4097, "f32", 3, 0),
+@pytest.mark.parametrize("rows, vocab, dtype, pad, offset", [(16, 500, "f32", 0, 0), (24, 2, "f32", 0, 0), (24, 3, "bf16", 1, 1), (16, 1536, "bf16", 0, 0), (16, 1537, "f32", 3, 0), (16, 3001, "bf16", 7, 8), (16, 4097, "f32", 3, 0),
                                                              (16, 9999, "bf16", 1, 3), (16, 32000, "f32", 0, 0), (16, 50257, "f32", 0, 2), (8, 151936, "bf16", 0, 0),
                                                              (8, 151936, "f32", 0, 0)])
 def test_settings(rows, vocab, dtype, pad, offset, kind):
@@ -240,6 +240,26 @@ def test_replayed_and_on_another_stream():
         step()
         torch.cuda.synchronize()
         assert (token.tolist(), kept.tolist(), logp.tolist()) == replayed
+
+
+@pytest.mark.parametrize("rows, vocab", [(65535, 33), (30000, 2100), (4097, 9000)])
+def test_many_rows(rows, vocab):
+    """The first of the largest logits under top-k 1 and under a top-p that keeps one; masks of the same"""
+    import torch
+    import paper_2602_24174_amd as T
+    g = torch.Generator(device="cuda")
+    g.manual_seed(rows)
+    x = torch.randn((rows, vocab), generator=g, device="cuda").round(decimals=1)
+    x[::3, 5] = 40.0
+    want = torch.where(x == x.amax(1, keepdim=True), torch.arange(vocab, device="cuda"), vocab).amin(1).to(torch.int32)
+    token, kept, logp, u = torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.zeros(rows, dtype=torch.int32, device="cuda"), torch.ones(rows, device="cuda"), torch.rand(rows, device="cuda")
+    T.tasc_sample(x, u, token, None, torch.ones(rows, dtype=torch.int32, device="cuda"), None, None, logp, kept)
+    assert torch.equal(token, want) and (kept == 1).all() and (logp == 0).all()
+    T.tasc_sample(x, u, token, torch.full((rows,), 0.7, device="cuda"), None, torch.full((rows,), 1e-9, device="cuda"), None, logp, kept)
+    assert torch.equal(token, want) and (kept == 1).all()
+    out = torch.zeros((rows, 1, vocab), device="cuda")
+    T.tasc_filter_logits(x[:, None], out, None, torch.ones(rows, dtype=torch.int32, device="cuda"))
+    assert ((out[:, 0] > -np.inf).sum(1) == 1).all() and torch.equal(out[:, 0].argmax(1).to(torch.int32), want)
 
 
 def test_no_rows():
