@@ -1389,28 +1389,33 @@ __device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a,
     constexpr int PER = kRanges / kPartThreads;
     static_assert(PER == 8);
     u32 each[PER] = {};
-#pragma unroll 8
-    for (int j = 0; j < a.n_parts; ++j) {
-        const uint4 m = *(const uint4*)(slices + j * (kRanges / 2) + 4 * tid);
-        const u32 two[4] = {m.x, m.y, m.z, m.w};
+    constexpr int AHEAD = 16;
+    for (int j0 = 0; j0 < a.n_parts; j0 += AHEAD) {
+        uint4 m[AHEAD];
 #pragma unroll
-        for (int e = 0; e < 4; ++e) {
-            each[2 * e] += two[e] & 0xFFFF;
-            each[2 * e + 1] += two[e] >> 16;
+        for (int j = 0; j < AHEAD; ++j) m[j] = j0 + j < a.n_parts ? *(const uint4*)(slices + (j0 + j) * (kRanges / 2) + 4 * tid) : uint4{0, 0, 0, 0};
+#pragma unroll
+        for (int j = 0; j < AHEAD; ++j) {
+            const u32 two[4] = {m[j].x, m[j].y, m[j].z, m[j].w};
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                each[2 * e] += two[e] & 0xFFFF;
+                each[2 * e + 1] += two[e] >> 16;
+            }
         }
     }
     // a range's weight is about its count times the weight at its middle, and for all of them together the logits lie within an eighth of a range of the middles;
     // bf16's, which lie on a grid of their own, within 0.3 of one, and four ranges more (flat rows of 151936 bf16 logits missed their cut with an
     // eighth in 2 of 600, with 0.3 in 1 of 1400, with two more in 1 of 2800)
     const double limit = count ? (double)(q.k - o.listed) : (double)q.p * o.total - (double)o.listed_q * 0x1p-50;
-    const double width = count ? 0.0 : q.inv / (double)range_of.per_unit, step = exp_neg(-width), spare = exp_neg(-aside * width);
+    const double width = count ? 0.0 : q.inv / (double)range_of.per_unit, step = exp_neg(-width), spare = exp_neg(-aside * width), over = 1.0 / spare;
     double middle = count ? 1.0 : exp_neg(fmin(((double)range_of.ref - (double)o.top) * q.inv - (PER * tid + 0.5) * width, 0.0));
     double least = 0.0, most = 0.0, v_least[PER], v_most[PER];
 #pragma unroll
     for (int e = 0; e < PER; ++e) {
         const bool rest = !count && PER * tid + e == kRanges - 1;          // (all that is below the others)
         least += v_least[e] = rest ? 0.0 : each[e] * middle * spare;
-        most += v_most[e] = each[e] * middle / spare;
+        most += v_most[e] = each[e] * middle * over;
         middle *= step;
     }
     const double up_least = wave_scan64_dpp(least), up_most = wave_scan64_dpp(most);
@@ -1470,6 +1475,10 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
         const int i = a.wide[1 + item / a.n_parts], part = item % a.n_parts;
         RowOut& o = a.rows[i];
         const Params q = params_of(a, i / a.per);
+        const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
+        const int p0 = part * a.part_len, run = a.part_len / kPartWaves, v_begin = min(p0 + wave * run, a.vocab), v_end = min(v_begin + run, a.vocab);
+        float next[kPer];
+        R::load(row, v_begin, v_end, lane, next);          // (on their way while the ranges are found)
         float x_lo = o.x_m, x_hi = o.x_m;
         int type = o.type;
         __syncthreads();
@@ -1483,16 +1492,12 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
             o.x_hi = x_hi;
         }
         if (type < 0) continue;
-        const T* const row = (const T*)a.logits + (int64_t)i * a.row_stride;
-        const int p0 = part * a.part_len, run = a.part_len / kPartWaves, v_begin = min(p0 + wave * run, a.vocab), v_end = min(v_begin + run, a.vocab);
         const int bits = sum_bits(a.vocab);
         const TableWeight weight(s_pow, o.top, q.inv, bits);
         u64* const lists = a.lists + (int64_t)i * a.n_parts * kPartWaves * a.list_len;
         u64* const list = lists + (part * kPartWaves + wave) * (int64_t)a.list_len;
         u64 sum = 0;
         int above = 0, listed = 0;
-        float next[kPer];
-        R::load(row, v_begin, v_end, lane, next);
         for (int v0 = v_begin; v0 < v_end; v0 += kStep) {
             float x[kPer];
 #pragma unroll
