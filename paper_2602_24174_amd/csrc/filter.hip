@@ -732,7 +732,7 @@ struct __attribute__((aligned(16))) ListShared {
     u64 list[ROOM], weight[ROOM];
     u64 bins[kFinishBins];
     u32 counts[kFinishBins];
-    u64 few_key[kFew], few_q[kFew];
+    u64 few_key[kFew], few_q[kFew], least, most;
     u64 red[kWaves];
     int32_t num[kWaves], few, n, bad;
 };
@@ -765,7 +765,11 @@ __device__ __forceinline__ Found last_item(S& s, int n, u64 lo, u64 hi, u64 limi
         static_assert(kFinishBins == 1 << 9);
         __syncthreads();                                    // (bins and few are still looked at)
         for (int i = tid; i < kFinishBins; i += NT) s.bins[i] = 0;
-        if (tid == 0) s.few = 0;
+        if (tid == 0) {
+            s.few = 0;
+            s.least = ~0ull;
+            s.most = 0;
+        }
         __syncthreads();
 #pragma unroll 4
         for (int i = tid; i < n; i += NT) {
@@ -811,10 +815,18 @@ __device__ __forceinline__ Found last_item(S& s, int n, u64 lo, u64 hi, u64 limi
                 s.few_key[place] = c;
                 s.few_q[place] = q;
             }
+            if (!FEW) {
+                atomicMin(&s.least, c);
+                atomicMax(&s.most, c);
+            }
         }
         __syncthreads();
         const int few = s.few;
-        if (!FEW && few > kFew) continue;
+        if (!FEW && few > kFew) {                           // (equal logits lie far apart from others by their keys, close together by their indices)
+            lo = s.least;
+            hi = s.most;
+            continue;
+        }
         const u64 c = lane < few ? s.few_key[lane] : ~0ull, q = lane < few ? s.few_q[lane] : 0;
         u64 below = 0;
         int rank = 0;
