@@ -599,7 +599,7 @@ tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t ro
  * Sums are of 64 bits, of whole numbers of 2^-36 of the largest weight (vocabularies of 2^24 tokens) to 2^-50 or finer or of fp64 in a fixed order, so a row's outputs depend neither on
  * the order of the work nor on other rows' contents; exponentials are within 2e-13 of themselves.  A row without a distribution (a NaN, +infinity, nothing above -infinity, a temperature below 0 or a NaN as one of its parameters) gives
  * token -1 with a NaN as logprob, 0 kept.
- * The workspace is 16-byte aligned; calls that may overlap need their own.  Rows that keep up to about 500 tokens (of vocabularies beyond 1536) are served from one read of
+ * The workspace is 16-byte aligned; calls that may overlap need their own.  Rows that keep up to about 500 tokens (of vocabularies beyond 1280) are served from one read of
  * their logits; those that keep more are read three times, and a few (a top-k beyond 500 together with a top-p, thousands of equal logits at the border) take
  * a row's workgroup 100 us and more.
  * Limits: rows <= 65535, vocab in [2, 2^24].  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP.

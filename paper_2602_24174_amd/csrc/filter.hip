@@ -23,7 +23,7 @@ constexpr int kThreads = 1024, kWaves = kThreads / 64, kBins = 4096, kWideList =
 constexpr int kListBits = 50;                              // a list's weights: 2^11 of them stay below 2^62
 // a workgroup of k_filter_parts, its waves' shares; lists of a row together, and entries that k_filter_finish takes
 constexpr int kPartThreads = 256, kPartWaves = kPartThreads / 64, kPer = 16, kStep = 64 * kPer;
-constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 1024, kMostParts = 64, kList = 1536, kCloseList = 6144, kGroups = 64, kWanted = 768;
+constexpr int kPart = 16384, kLeastPart = 4096, kFillParts = 1024, kMostParts = 64, kDirect = 1280, kList = 1536, kCloseList = 6144, kGroups = 64, kWanted = 768;
 constexpr int kFinishThreads = 256, kFinishWaves = kFinishThreads / 64, kFinishBins = 512, kFew = 64, kRanges = 2048, kWideGrid = 2048;
 
 // What a part of a row comes to
@@ -627,7 +627,10 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
     if (wave == 0) {
         // the largest bound that so many groups reach, by the upper half of its bits
         const u32 key = key_of(group);
-        const int rank = q.one ? 1 : a.sample_rank;
+        // (in short runs some groups miss lanes: their largest says little; without a whole one everything is listed)
+        const int from = p0 + lane / 16 * run, last = from + R::place(lane / 4 % 4 * 4 + a.sample_len - 1, lane % 4 * 16 + 15);
+        const int there = __popcll(__ballot(last < min(from + run, a.vocab)));
+        const int rank = q.one ? 1 : there == 0 ? kGroups + 1 : (a.sample_rank * there + kGroups - 1) / kGroups;
         u32 at = 0;
         for (u32 bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
             if (__popcll(__ballot(key >= (at | bit))) >= rank) at |= bit;
@@ -1720,7 +1723,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_apply(FilterArgs a) {
 struct Plan { int direct, n_parts, part_len, list_len, sample_len, sample_rank; };
 Plan plan_of(int rows, int vocab) {
     Plan p{};
-    p.direct = vocab <= kList;
+    p.direct = vocab <= kDirect;
     if (p.direct) return p;
     // parts of up to kPart logits; smaller ones, down to kLeastPart, where the rows alone do not fill the chip
     const int most = std::min((vocab - 1) / kLeastPart + 1, kMostParts), least = std::min((vocab - 1) / kPart + 1, kMostParts);
@@ -1729,8 +1732,7 @@ Plan plan_of(int rows, int vocab) {
     // kWanted of the row, a share f of its logits: a group's largest lies among them with probability 1 - (1 - f)^n
     const double f = (double)kWanted / vocab;
     p.sample_len = f < 0.015 ? 4 : f < 0.03 ? 2 : 1;
-    const int groups = kGroups / 4 * std::min(4, std::max(1, p.part_len / kPartWaves / 256));      // (a short run fills a part of a step)
-    p.sample_rank = std::min(groups, std::max(1, (int)(groups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
+    p.sample_rank = std::min(kGroups, std::max(1, (int)(kGroups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
     // eight times what a wave should find, but no more than a row's lists may hold together
     p.list_len = std::max(128, std::min(kList / kPartWaves, (8 * kWanted / (p.n_parts * kPartWaves) + 15) / 16 * 16));
     return p;

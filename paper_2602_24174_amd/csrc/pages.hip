@@ -438,7 +438,7 @@ __global__ __launch_bounds__(kSmallThreads) void k_use_small(UseArgs a) {
 int words_of(int n_pages) { return (n_pages - 1) / 32 + 1; }
 size_t mark_bytes(int n_words) { return (size_t)((n_words + 1) / 2) * 64; }
 int blocks_of(int n_words) { return (n_words - 1) / kBlockWords + 1; }
-constexpr int kSmallWords = 2048, kSmallBatch = 64, kSmallEntries = 1 << 16;
+constexpr int kSmallWords = 1024, kSmallBatch = 64, kSmallEntries = 1 << 14;
 
 struct Array { const char* name; const int32_t* at; int64_t n; };
 bool apart(const Array& x, const Array& y) {

@@ -28,7 +28,7 @@ def test_sample():
                 dict(logits=A + 2), dict(logits=A + 1, dtype=1), dict(ws=10 * A + 8)):
         assert call(**bad) == B.TASC_EINVAL, bad
     assert call(n=need - 1) == B.TASC_ENOMEM and call(ws=None) == B.TASC_ENOMEM
-    assert T.tasc_sample_workspace_bytes(3, 1536) == 0 and call(vocab=1536, ws=None, n=0, dtype=7) == B.TASC_EINVAL
+    assert T.tasc_sample_workspace_bytes(3, 1280) == 0 and call(vocab=1280, ws=None, n=0, dtype=7) == B.TASC_EINVAL
     assert call(rows=0, logits=None, u=None, token=None) == 0
     assert [T.tasc_sample_workspace_bytes(*s) for s in ((0, 100), (65536, 100), (3, 1), (3, (1 << 24) + 1))] == [0] * 4
 
