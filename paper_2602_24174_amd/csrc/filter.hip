@@ -625,11 +625,12 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
     const float group = s_group[lane];
     const float anchor = wave_max_dpp(group);
     if (wave == 0) {
-        // the largest bound that so many groups reach, by the upper half of its bits
-        const u32 key = key_of(group);
-        // (in short runs some groups miss lanes: their largest says little; without a whole one everything is listed)
+        // the largest bound that so many groups reach, by the upper half of its bits (in short runs some groups miss lanes: their largest
+        // says little; without a whole one everything is listed)
         const int from = p0 + lane / 16 * run, last = from + R::place(lane / 4 % 4 * 4 + a.sample_len - 1, lane % 4 * 16 + 15);
-        const int there = __popcll(__ballot(last < min(from + run, a.vocab)));
+        const bool whole_group = last < min(from + run, a.vocab);
+        const u32 key = whole_group || q.one ? key_of(group) : 0;
+        const int there = __popcll(__ballot(whole_group));
         const int rank = q.one ? 1 : there == 0 ? kGroups + 1 : (a.sample_rank * there + kGroups - 1) / kGroups;
         u32 at = 0;
         for (u32 bit = 1u << 31; bit >= 1u << 16; bit >>= 1)
@@ -1730,7 +1731,8 @@ Plan plan_of(int rows, int vocab) {
     p.n_parts = std::max(least, std::min(most, kFillParts / rows));
     p.part_len = ((vocab - 1) / (p.n_parts * kPartWaves) / 16 + 1) * 16 * kPartWaves;    // (waves' runs alike, as whole vectors)
     // kWanted of the row, a share f of its logits: a group's largest lies among them with probability 1 - (1 - f)^n
-    const double f = (double)kWanted / vocab;
+    // (at most a fifth: the least of all groups' largest would now and then be low enough for lists to overflow; 64 rows of 3500: 59 us against 26)
+    const double f = std::min((double)kWanted / vocab, 0.2);
     p.sample_len = f < 0.015 ? 4 : f < 0.03 ? 2 : 1;
     p.sample_rank = std::min(kGroups, std::max(1, (int)(kGroups * (1.0 - pow(1.0 - f, 16.0 * p.sample_len)) + 0.5)));
     // eight times what a wave should find, but no more than a row's lists may hold together
