@@ -3,13 +3,16 @@
 // A row's tokens in the order of their logits (equal ones by index) are whole numbers of 56 bits, `comp`: the logit's bits, turned so that
 // the largest comes first, over the index.  Every filter keeps a prefix of that order, so all of them together come to one last comp, `cut`.
 //
-// k_filter_parts reads every logit once, a workgroup up to 16384 of them: the largest, the sum of the weights where it is wanted, and a list of those
-// above a bound that it takes from a sample, about 900 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and nearly always the
-// cut lies in them.  Rows whose cut does not (flat distributions: thousands of tokens kept) are listed for two kernels that read them again, parts side by
-// side: k_filter_bins sums the weights (or counts) of 512 ranges of values, its last workgroup of a row finds the range in which the cut lies; k_filter_gather
-// lists that range's tokens and sums what is above it, its last workgroup finds the cut and draws.  k_filter_close, a workgroup a row, serves what is left (ties of
-// thousands at the cut, a top-k of thousands and a top-p together): 4096 ranges, of which the one with the cut is sorted if it fits, or cut into 4096 again, by
-// comp, until one token is left.  Rows of up to kList tokens are their own list and need one launch.
+// k_filter_parts reads every logit once: the largest, the sum of the weights where it is wanted, and a list of those above a bound that it takes from a
+// sample, some 768 of a row.  k_filter_finish, a workgroup a row, puts the lists together, and mostly the cut lies in them: the row is done.  Rows whose
+// cut does not (flat distributions: thousands of tokens kept) it lists for three kernels: k_filter_bins counts their logits by 2048 ranges, part by part; in
+// k_filter_gather every workgroup finds the few ranges in which the cut lies from bounds on their weights, lists these ranges' tokens of its part and sums what
+// is above them; k_filter_close, a workgroup a row, finds the cut in those lists.  What is left even then (ties of thousands at the cut, a top-k of thousands
+// together with a top-p) it takes from the row itself: 4096 ranges, of which the one with the cut is sorted if it fits, or cut into 4096 again, until one token is left.
+// Masks: k_filter_apply.  Rows of up to kDirect tokens are their own list and need one launch.  Nothing is waited for between workgroups: a kernel's end orders.
+//
+// Times here are of one MI355X: 1280 rows of 151936 fp32 logits, 140 of them flat, take 264 us, 155 of them the read (79 % of what a plain read of the bytes
+// reaches); one row of 49152, 20 us, all of it latency.
 //
 // Weights are sums of whole numbers, which no order of the work changes: a bin's of 2^-F of the weight at its middle, so that a bin far from the
 // largest is as exact as one next to it, a list's and the draw's of 2^-F of the largest.  Sums over whole rows are fp64 in a fixed order.
@@ -587,6 +590,9 @@ __device__ __forceinline__ float row16_max(float v) {      // of 16 lanes side b
     return up(v, std::integral_constant<int, 0x140>{});
 }
 
+// Bound by the bytes for many rows of fp32, where nothing else is in the way: 778 MB in 155 us (the exponentials of rows with a top-p alone keep the vector units
+// 68 % busy), with the masks filled on the way 350 + 350 MB in 136; by instructions for bf16 (64 rows 15 us: a logit costs what an fp32 one does).  The next step's loads are
+// under way while a step is worked on.
 template <typename T, bool VEC, bool FILL>
 __global__ __launch_bounds__(kPartThreads) void k_filter_parts(FilterArgs a) {
     using R = Run<T, VEC>;
@@ -1102,6 +1108,8 @@ __device__ __forceinline__ double part_total(double sum, double scale, const Row
     return wave_sum64_dpp(sum > 0.0 ? sum * exp_neg(scale - (double)r.top * r.inv) : 0.0);
 }
 
+// A workgroup a row, from its lists.  Bound by its chain: two dependent reads, then for each of top-k and top-p a histogram, its running sums and a comparison of the bin at the
+// cut, about 15 barriers: 10 us for one row, 40 for 1280, five workgroups a compute unit (four, with lists of up to 2048: 12 for one row).
 template <typename T, bool VEC, bool MASK>
 __global__ __launch_bounds__(kFinishThreads) __attribute__((amdgpu_waves_per_eu(5))) void k_filter_finish(FilterArgs a) {
     __shared__ FinishShared s;
@@ -1357,7 +1365,7 @@ struct Ranges {
     __device__ __forceinline__ int operator()(float x) const { return (int)fminf((ref - x) * per_unit, (float)(kRanges - 1)); }
 };
 __device__ __forceinline__ int sum_bits(int n) { return min(kListBits, 61 - (32 - __clz(n))); }      // n weights stay below 2^62
-// Counts of the ranges by part.  Bound by the LDS atomics.
+// Counts of the ranges by part, in 16 bits each.  Bound by the LDS atomics: 140 rows of 151936 20 us.
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
     using R = Run<T, VEC>;
@@ -1474,8 +1482,8 @@ __device__ __forceinline__ bool find_ranges(RangeShared& s, const FilterArgs& a,
 }
 
 // The tokens of the ranges in which the cut may lie, and what lies above them, by part; every workgroup finds the ranges for itself.  Bound by the exponentials of
-// what is kept.  (With a row's last workgroup finding them, and the cut, the fences around that took longer than either kernel's own work: 1280 rows, 140 of
-// them here, 95 + 87 us.)
+// what is kept: 140 rows of 151936 45 us.  (With a row's last workgroup finding the ranges in k_filter_bins, and here the cut, the fences around that took longer than either
+// kernel's own work: 95 + 87 us against 20 + 45 + k_filter_close's 21.)
 template <typename T, bool VEC>
 __global__ __launch_bounds__(kPartThreads) void k_filter_gather(FilterArgs a) {
     using R = Run<T, VEC>;
@@ -1678,7 +1686,8 @@ __device__ __forceinline__ void slow_row(Shared& s, const FilterArgs& a, int i, 
     if (a.logprob) a.logprob[i] = logp;
 }
 
-// The rows that k_filter_gather has read, and those that are left: a workgroup a row
+// The rows that k_filter_gather has read, and those that are left: a workgroup a row.  Bound by its chain, as k_filter_finish: 140 rows 21 us; a row that has to be
+// read again (slow_row) 80 to 250.
 template <typename T, bool VEC, bool MASK>
 __global__ __launch_bounds__(kThreads) void k_filter_close(FilterArgs a) {
     __shared__ union { Shared slow; CloseShared close; } shared;
@@ -1694,7 +1703,8 @@ __global__ __launch_bounds__(kThreads) void k_filter_close(FilterArgs a) {
     slow_row<T, VEC, MASK>(shared.slow, a, i, q, tid);
 }
 
-// In place: what is dropped.  Else, of the rows that were not written from their lists, what is kept.
+// In place: what is dropped.  Else, of the rows that were not written from their lists, what is kept (k_filter_parts has filled the rest).  Bound by the reads:
+// 576 rows of 151936, a ninth of them flat, 35 us.
 template <typename T, bool IN_PLACE>
 __global__ __launch_bounds__(kPartThreads) void k_filter_apply(FilterArgs a) {
     const int i = blockIdx.y, state = a.rows[i].state;
@@ -1720,7 +1730,11 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_apply(FilterArgs a) {
     }
 }
 
-// How a call is cut: parts of kPart logits, up to kMostParts; lists that hold three times what the sample should let through
+// How a call is cut.  Measured with a top-k and a top-p, both ways, us:
+//   one launch (rows are their own lists) | the lists: 1 row, 64, 1280 rows of 1024: 18.8 | 18.8, 21.3 | 20.5, 34.7 | 32.7; of 1280: 14.8 | 19.7, 23.9 | 21.6, 38.2 | 38.3; of
+//     1536: 25.0 | 18.5, 26.7 | 21.3, 41.3 | 34.9; without filters 8.1 | 12.7 and 14.2 | 23.9 (1 and 1280 rows of 1024).
+//   parts as here | of 16384 or more | of 4096, rows of 151936 fp32: 1 row 22.2 | 25.5 | 22.1, 64 rows 30.5 | 31.1 | 31.4, 256 rows 48.2 | 47.7 | 56.4, 1024 rows 154.5 | 154.1 | 172.5.
+//   rows at multiples of 16 bytes | others (RowLoop and Run without VEC): 1280 rows of 151936 fp32 189 | 188, 64 rows bf16 29.0 | 35.9.
 struct Plan { int direct, n_parts, part_len, list_len, sample_len, sample_rank; };
 Plan plan_of(int rows, int vocab) {
     Plan p{};

@@ -116,7 +116,8 @@ struct CopyArgs {
     int32_t n, n_pages, pieces, quads; // of a page: pieces, and 16-byte words of a piece
 };
 constexpr int kCopyThreads = 256, kCopyAhead = 8;
-// Bound by the bytes: a wave has up to 8 KB under way before it writes.
+// Bound by the bytes: a wave has up to 8 KB under way before it writes.  480 copies of 18432-byte pages in 12 layers (106 MB written, the sources' 7 MB read once): 24 us;
+// a few thousand pages of 4608 bytes in 28 layers 35.
 __global__ __launch_bounds__(kCopyThreads) void k_pages_copy(CopyArgs a) {
     const int lane = threadIdx.x & 63;
     const int64_t waves = (int64_t)gridDim.x * (kCopyThreads / 64);
@@ -157,6 +158,7 @@ constexpr int kBlockWords = 256, kUseThreads = 256, kSmallThreads = 1024;
 
 __device__ __forceinline__ int row_pages(const UseArgs& a, int b) { return min(max(a.pages[b], 0), a.max_pages); }
 
+// Times below: 4096 sequences, 2.5 million entries, a pool of 3.7 million pages.  3.7 MB of marks: 2 us
 __global__ __launch_bounds__(kUseThreads) void k_use_clear(UseArgs a) {
     quad* const to = (quad*)a.marks;                       // (two words' pages)
     const int n = (a.n_words + 1) / 2 * 4;
@@ -204,6 +206,7 @@ __device__ __forceinline__ int block_sum(int v, int* s, int tid) {       // of 2
     __syncthreads();
     return v;
 }
+// Marks to bits, and a block of words' sum.  Bound by the launch: 4 us
 __global__ __launch_bounds__(kUseThreads) void k_use_count(UseArgs a) {
     __shared__ int s[kUseThreads / 64];
     const int tid = threadIdx.x, w0 = blockIdx.x * kBlockWords;
@@ -272,6 +275,8 @@ __device__ __forceinline__ int listed_from(const UseArgs& a, int w, u32 bits, in
     return lo >= 32 ? 0 : __popc(lo > 0 ? bits & ~((1u << lo) - 1) : bits);
 }
 
+// Every page to its place, by the sums of all blocks before (each workgroup adds them up itself).  Bound by the scattered runs it writes, 14 MB: 11 us, with blocks of 1024
+// words instead of 256 24.
 template <bool COMPACT>
 __global__ __launch_bounds__(kUseThreads) void k_use_list(UseArgs a) {
     __shared__ int s[kUseThreads / 64];
@@ -341,6 +346,7 @@ __device__ __forceinline__ int moved(const UseArgs& a, int p, u32 bits, int befo
     const int j = listed - 1 - (before + __popc(bits & ((1u << (p & 31)) - 1)));
     return j < a.cap ? a.copy_to[j] : p;
 }
+// A wave a sequence: an entry read, its page's bits and sum, for one that moves the move, and the entry written; bound by these dependent reads.
 __global__ __launch_bounds__(kUseThreads) void k_use_rewrite(UseArgs a, int n_blocks) {
     const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, b = blockIdx.x * (kUseThreads / 64) + wave;
     if (b >= a.batch) return;
@@ -438,6 +444,8 @@ __global__ __launch_bounds__(kSmallThreads) void k_use_small(UseArgs a) {
 int words_of(int n_pages) { return (n_pages - 1) / 32 + 1; }
 size_t mark_bytes(int n_words) { return (size_t)((n_words + 1) / 2) * 64; }
 int blocks_of(int n_words) { return (n_words - 1) / kBlockWords + 1; }
+// Up to these bounds one workgroup does it all.  That | the four launches, us, free (compact): 64 sequences of 64 pages 5.3 | 12.7 (7.8 | 17.7); of 256 9.9 | 13.7 (17.7 | 20.1), in a
+// pool of 32768 11.0 | 13.5 (20.1 | 20.5), of 65536 15.6 | 13.3 (29.5 | 20.9); 256 sequences of 64 12.4 | 13.7 (23.0 | 18.6); 64 of 680 20.6 | 14.4 (41.4 | 25.0).
 constexpr int kSmallWords = 1024, kSmallBatch = 64, kSmallEntries = 1 << 14;
 
 struct Array { const char* name; const int32_t* at; int64_t n; };
