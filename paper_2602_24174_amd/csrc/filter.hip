@@ -1736,13 +1736,14 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_apply(FilterArgs a) {
 //   parts as here | of 16384 or more | of 4096, rows of 151936 fp32: 1 row 22.2 | 25.5 | 22.1, 64 rows 30.5 | 31.1 | 31.4, 256 rows 48.2 | 47.7 | 56.4, 1024 rows 154.5 | 154.1 | 172.5.
 //   rows at multiples of 16 bytes | others (RowLoop and Run without VEC): 1280 rows of 151936 fp32 189 | 188, 64 rows bf16 29.0 | 35.9.
 struct Plan { int direct, n_parts, part_len, list_len, sample_len, sample_rank; };
+int most_parts(int vocab) { return std::min((vocab - 1) / kLeastPart + 1, kMostParts); }
+int least_parts(int vocab) { return std::min((vocab - 1) / kPart + 1, kMostParts); }
 Plan plan_of(int rows, int vocab) {
     Plan p{};
     p.direct = vocab <= kDirect;
     if (p.direct) return p;
     // parts of up to kPart logits; smaller ones, down to kLeastPart, where the rows alone do not fill the chip
-    const int most = std::min((vocab - 1) / kLeastPart + 1, kMostParts), least = std::min((vocab - 1) / kPart + 1, kMostParts);
-    p.n_parts = std::max(least, std::min(most, kFillParts / rows));
+    p.n_parts = std::max(least_parts(vocab), std::min(most_parts(vocab), kFillParts / rows));
     p.part_len = ((vocab - 1) / (p.n_parts * kPartWaves) / 16 + 1) * 16 * kPartWaves;    // (waves' runs alike, as whole vectors)
     // kWanted of the row, a share f of its logits: a group's largest lies among them with probability 1 - (1 - f)^n
     // (at most a fifth: the least of all groups' largest would now and then be low enough for lists to overflow; 64 rows of 3500: 59 us against 26)
@@ -1819,7 +1820,11 @@ tasc_status check_workspace(const char* who, void* workspace, size_t ws_bytes, i
 extern "C" size_t tasc_sample_workspace_bytes(int32_t rows, int32_t vocab) {
     if (rows < 1 || rows > 65535 || vocab < 2 || vocab > 1 << 24) return 0;
     const Plan p = plan_of(rows, vocab);
-    return p.direct ? 0 : parts_bytes(p, rows) + (size_t)rows * sizeof(RowOut) + lists_bytes(p, rows) + slices_bytes(p, rows) + ((size_t)rows + 1) * sizeof(int32_t);
+    if (p.direct) return 0;
+    // so much that fewer rows, in smaller parts, find room, too: of the parts that any number of rows up to this one has, and of their lists
+    const size_t n_parts = std::max(std::min((size_t)rows * most_parts(vocab), (size_t)kFillParts), (size_t)rows * least_parts(vocab));
+    const size_t listed = kPartWaves * std::max(128 * n_parts, std::min(kList / kPartWaves * n_parts, 8 * kWanted / kPartWaves * (size_t)rows + 16 * n_parts));
+    return n_parts * (sizeof(Part) + kRanges / 2 * sizeof(u32)) + listed * sizeof(u64) + (size_t)rows * sizeof(RowOut) + ((size_t)rows + 1) * sizeof(int32_t);
 }
 
 extern "C" tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t rows, int32_t vocab, const float* temperature, const int32_t* top_k,

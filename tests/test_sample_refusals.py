@@ -33,6 +33,12 @@ def test_sample():
     assert [T.tasc_sample_workspace_bytes(*s) for s in ((0, 100), (65536, 100), (3, 1), (3, (1 << 24) + 1))] == [0] * 4
 
 
+@pytest.mark.parametrize("vocab", [1281, 4097, 49152, 151936, 1 << 24])
+def test_a_workspace_for_more_rows_serves_fewer(vocab):
+    sizes = [T.tasc_sample_workspace_bytes(rows, vocab) for rows in list(range(1, 1400)) + [2049, 4096, 65535]]
+    assert sizes == sorted(sizes)
+
+
 def test_filter_logits():
     need = T.tasc_sample_workspace_bytes(9, 5000)
     good = dict(logits=A, dtype=1, stride=5000, batch=3, k=2, vocab=5000, t=2 * A, tk=3 * A, p=4 * A, m=5 * A, out=6 * A, out_stride=5000, kept=9 * A, ws=10 * A, n=need)
