@@ -902,21 +902,28 @@ def tasc_verify_step_sampled(model: Model, s: Session, drafts, k, u, temperature
 
 def tasc_session_filter(s: Session, top_k=None, top_p=None, min_p=None, workspace=None):
     """From the next sampled step on: top_k int32, top_p and min_p fp32 cuda tensors [batch] or None (all None: no filters); the session keeps them.  A workspace
-    made here serves steps of every k and stays with the session (what was in its place may be in use on any stream: it is waited for, once)."""
+    made here serves steps of every k and stays with the session.  Steps on any stream may still use what was in its place, or the filters that the session had
+    before: they are waited for, except where the same tensors are given again."""
     import torch
     who = "session_filter"
     dev, _, _ = _here(None)
     if s._kv_pool.get_device() != dev:
         _refuse(f"{who}: the session is on cuda:{s._kv_pool.get_device()}, the current device is cuda:{dev}")
     _, k, p, m = _filters(who, None, top_k, top_p, min_p, (s.batch,), dev)
+    wait = False
     if workspace is None and (k or p or m):
         if s._filter_workspace is None:
-            s._filter_workspace = torch.empty(tasc_sample_workspace_bytes(s.batch * min(s.max_rows, TASC_MAX_K + 1), s.model.desc.vocab), dtype=torch.uint8, device="cuda")
-            torch.cuda.synchronize()
+            s._filter_workspace = torch.empty(tasc_sample_workspace_bytes(min(s.batch * min(s.max_rows, TASC_MAX_K + 1), 65535), s.model.desc.vocab), dtype=torch.uint8, device="cuda")
+            wait = True
         workspace = s._filter_workspace
     keep, ws, n = _workspace(who, workspace, 0, dev, True)
+    had, has = s._filters or (), (top_k, top_p, min_p, workspace)
+    if wait or any(t is not None and all(t is not x for x in has) for t in had):
+        if torch.cuda.is_current_stream_capturing():
+            _refuse(f"{who}: a call that has to wait for earlier steps cannot be captured")
+        torch.cuda.synchronize()
     _check(lib().tasc_session_filter(s.handle, k, p, m, ws, n))
-    s._filters = top_k, top_p, min_p, workspace
+    s._filters = has
 
 
 def tasc_session_rewind(s: Session, stream=None):

@@ -108,3 +108,33 @@ def test_a_workspace_that_is_too_small():
         T.tasc_verify_step_sampled(rig.model, rig.session, drafts, k, randoms(B, 4))
     T.tasc_session_filter(rig.session)
     T.tasc_verify_step_sampled(rig.model, rig.session, drafts, k, randoms(B, 4))
+
+
+def test_filters_that_are_replaced_while_a_step_is_under_way():
+    """The old filters' memory is free for others only when the steps that were enqueued with them, on whatever stream, have ended"""
+    import torch
+    rig = rig_of("tiled")
+    T, B, k = rig.T, rig.batch, rig.cfg.k
+    u = randoms(B, 8)
+    drafts = torch.zeros((B, k), dtype=torch.int32, device="cuda")
+    accept, emitted = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros((B, k + 1), dtype=torch.int32, device="cuda")
+    scratch = torch.zeros(T.tasc_sampled_scratch_bytes(rig.model, B, k), dtype=torch.uint8, device="cuda")
+    a, b = torch.zeros(1 << 28, dtype=torch.uint8, device="cuda"), torch.zeros(1 << 28, dtype=torch.uint8, device="cuda")
+    T.tasc_session_prefill(rig.model, rig.session, rig.prompts, rig.prompt_off, 12)
+    side = torch.cuda.Stream()
+    outs = []
+    for busy in (False, True):
+        T.tasc_session_rewind(rig.session)
+        T.tasc_session_filter(rig.session, top_k=torch.full((B,), 2, dtype=torch.int32, device="cuda"))
+        torch.cuda.synchronize()
+        for _ in range(50 if busy else 0):                  # (6 ms)
+            T.tasc_calibration_copy(a, b, stream=side.cuda_stream)
+        T.tasc_verify_step_sampled(rig.model, rig.session, drafts, k, u, None, accept, emitted, None, scratch, stream=side.cuda_stream)
+        if busy:
+            T.tasc_session_filter(rig.session)
+            other = [torch.full((B,), 1000, dtype=torch.int32, device="cuda") for _ in range(8)]
+        torch.cuda.synchronize()
+        z = scratch[:B * (k + 1) * rig.cfg.vocab * 4].view(torch.float32).view(B, k + 1, rig.cfg.vocab)
+        assert ((z > float("-inf")).sum(2) == 2).all()
+        outs.append((accept.tolist(), emitted.tolist()))
+    assert outs[0] == outs[1]
