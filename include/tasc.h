@@ -611,7 +611,8 @@ tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t row_stride
 /*
  * The same filters as masked logits: out [batch, k + 1, vocab] is logits where a token is kept, else -infinity, so tasc_accept_sampled over it, with the same
  * temperature, verifies drafts under them.  Parameters are a sequence's ([batch]); out may be logits, with the same stride; kept
- * int32[batch, k + 1], nullable.  A row without a distribution is passed on as it is (0 kept).  vocab, rows and errors as for tasc_sample, k in [0, TASC_MAX_K].
+ * int32[batch, k + 1], nullable.  Logits that are no distribution are passed on as they are, and under a temperature below 0 or a NaN as a parameter nothing is kept, so that
+ * tasc_accept_sampled refuses both (0 kept).  vocab, rows and errors as for tasc_sample, k in [0, TASC_MAX_K].
  */
 tasc_status tasc_filter_logits(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab,
                                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, void* out,

@@ -36,10 +36,11 @@ def sample(logits, u, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
 
 
 def masked(logits, temperature=1.0, top_k=0, top_p=1.0, min_p=0.0):
-    """(logits where kept, else -infinity; tokens kept); a row without a distribution as it is"""
+    """(logits where kept, else -infinity; tokens kept); logits that are no distribution as they are, under parameters that are none nothing is kept"""
     kept = kept_tokens(logits, temperature, top_k, top_p, min_p)
     if kept is None:
-        return np.array(logits), 0
+        good = temperature >= 0 and not np.isnan(top_p) and not np.isnan(min_p)
+        return np.array(logits) if good else np.full_like(np.asarray(logits), -np.inf), 0
     out = np.full_like(np.asarray(logits), -np.inf)
     out[kept] = np.asarray(logits)[kept]
     return out, len(kept)

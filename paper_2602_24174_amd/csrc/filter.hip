@@ -1221,7 +1221,7 @@ __global__ __launch_bounds__(kFinishThreads) __attribute__((amdgpu_waves_per_eu(
                     listed_q = by.listed;
                 }
             }
-            if (by.state == CUT_MANY) {                     // (ties of thousands: the same one after the other)
+            if (by.state == CUT_MANY) {                     // (thousands of tokens at a cut: top-k and top-p one after the other)
                 if (by_count) {
                     if (p.k <= valid) {
                         cut = last_item<false, kFinishThreads>(s, n, lo, hi, (u64)p.k, tid, comp, [](int) { return 1ull; }).key;
@@ -1307,13 +1307,15 @@ __global__ __launch_bounds__(kFinishThreads) __attribute__((amdgpu_waves_per_eu(
     if (MASK) {
         T* const out = (T*)a.out + (int64_t)i * a.out_stride;
         const T none = from_f<T>(-__builtin_inff());
-        if (bad || a.direct) {                              // (a row without a distribution is passed on)
-            if (!bad || !a.in_place)
+        const bool pass = bad && p.good;                    // (its logits are no distribution: they are passed on)
+        if (bad) cut = 0;
+        if (pass || a.direct) {
+            if (!pass || !a.in_place)
                 for (int v = tid; v < a.vocab; v += kFinishThreads) {
                     const T x = row[v];
-                    out[v] = bad || (to_f(x) > -__builtin_inff() && comp_of(to_f(x), v) <= cut) ? x : none;
+                    out[v] = pass || (to_f(x) > -__builtin_inff() && comp_of(to_f(x), v) <= cut) ? x : none;
                 }
-        } else if (!wide && !keep_all && !a.in_place) {
+        } else if (!bad && !wide && !keep_all && !a.in_place) {
             for (int e = tid; e < n; e += kFinishThreads)
                 if (s.list[e] <= cut) out[token_of(s.list[e])] = row[token_of(s.list[e])];
         }
@@ -1322,7 +1324,7 @@ __global__ __launch_bounds__(kFinishThreads) __attribute__((amdgpu_waves_per_eu(
     if (!a.direct) {
         RowOut o{};
         o.cut = cut;
-        o.state = bad ? ROW_BAD : keep_all ? ROW_CUT : !wide ? ROW_DONE : type < 0 ? ROW_SLOW : ROW_WIDE;
+        o.state = bad ? (p.good ? ROW_BAD : ROW_CUT) : keep_all ? ROW_CUT : !wide ? ROW_DONE : type < 0 ? ROW_SLOW : ROW_WIDE;
         o.type = type;
         o.top = r.top;
         o.ref = bound;
