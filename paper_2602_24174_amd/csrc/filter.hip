@@ -1581,15 +1581,17 @@ __device__ __forceinline__ bool close_row(CloseShared& c_s, const FilterArgs& a,
     const int n = read_lists<kThreads>(s, a, i, list_length(a, i, tid), tid, (1ull << 56) - 1);
     if (n < 0) return false;
     u64 cut = (u64)~key_of(x_hi) << 24 | 0xFFFFFF;      // (x_hi itself is above)
-    bool good = true;
+    const u64 over_q = wave_sum_u64(s_part[lane] + s_part[lane + 64] + s_part[lane + 128] + s_part[lane + 192]);
+    const double mass = ceil((double)q.p * o.total * ldexp(1.0, bits));
+    // (where k_filter_gather took min-p for the filter that keeps less, that was by an estimate: the weights from its logit on say whether it is)
+    bool good = o.found != BY_SHARE || o.type != BY_MASS || (double)over_q < mass;
     if (o.found != BY_SHARE) {
         const bool count = o.found == BY_COUNT;
-        const u64 over_q = wave_sum_u64(s_part[lane] + s_part[lane + 64] + s_part[lane + 128] + s_part[lane + 192]);
         u64 mine = 0;
         for (int e = tid; e < n; e += kThreads) mine += s.weight[e] = count ? 1 : weight(logit_of(s.list[e]));
         const u64 listed = block_sum<kThreads>(s, mine, 0, tid).q;
         // what the range may still keep; the cut lies in it if something, and no more than it has
-        const double left = count ? (double)(q.k - n_above) : ceil((double)q.p * o.total * ldexp(1.0, bits)) - (double)over_q;
+        const double left = count ? (double)(q.k - n_above) : mass - (double)over_q;
         good = n > 0 && left >= 1.0 && left <= (double)listed;
         if (good)
             cut = last_item<false, kThreads>(s, n, (u64)~(key_of(x_hi) - 1) << 24, (u64)~key_of(x_lo) << 24 | 0xFFFFFF, (u64)left, tid,

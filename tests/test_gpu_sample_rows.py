@@ -1,0 +1,29 @@
+"""tasc_sample and tasc_filter_logits over rows as masks and vocabularies make them, against their oracle in 64 bits (tokens and counts equal, probabilities within the
+tolerance that test_gpu_sample derives)."""
+import itertools
+
+import numpy as np
+import pytest
+
+from test_gpu_sample import check
+
+pytestmark = pytest.mark.gpu
+f32 = lambda *v: np.array(v, dtype=np.float32)
+
+
+def type_of(name):
+    import torch
+    return torch.bfloat16 if name == "bf16" else torch.float32
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("live", ["uniform", "normal"])
+@pytest.mark.parametrize("mask", [-5e3, -1e4, -1e9])
+@pytest.mark.parametrize("vocab", [50257, 151936])
+def test_top_p_and_min_p_beside_a_finite_mask(vocab, mask, live, dtype):
+    """Masks that are large numbers instead of -infinity stretch the span of a flat row over many temperatures; top-p keeps less than min-p in some rows, more in others"""
+    rng = np.random.default_rng(vocab + int(-mask) % 1000 + len(live))
+    t, p, m = f32(*itertools.product((0.6, 1.0, 1.2), (0.8, 0.9, 0.95), (0.01, 0.05, 0.1))).T.copy()
+    x = rng.uniform(0, 10, (len(t), vocab)) if live == "uniform" else rng.standard_normal((len(t), vocab))
+    x[:, ::97] = mask
+    check(x, rng.random(len(t)).astype(np.float32), t=t, p=p, m=m, dtype=type_of(dtype))
