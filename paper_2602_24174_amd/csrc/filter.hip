@@ -1397,7 +1397,7 @@ __global__ __launch_bounds__(kPartThreads) void k_filter_bins(FilterArgs a) {
                 if (x[e] < below && x[e] > -__builtin_inff()) atomicAdd(&s_bins[range_of(x[e])], 1u);
         }
         __syncthreads();
-        // (16 bits a count: one that does not fit only makes the ranges miss the cut)
+        // (16 bits a count: one that does not fit, of parts beyond 65535 logits, makes the ranges miss the cut, which k_filter_close sees)
         u32* const slices = a.slices + (int64_t)i * a.n_parts * (kRanges / 2);
         for (int e = tid; e < kRanges / 2; e += kPartThreads) slices[part * (kRanges / 2) + e] = min(s_bins[2 * e], 65535u) | min(s_bins[2 * e + 1], 65535u) << 16;
     }
@@ -1583,8 +1583,9 @@ __device__ __forceinline__ bool close_row(CloseShared& c_s, const FilterArgs& a,
     u64 cut = (u64)~key_of(x_hi) << 24 | 0xFFFFFF;      // (x_hi itself is above)
     const u64 over_q = wave_sum_u64(s_part[lane] + s_part[lane + 64] + s_part[lane + 128] + s_part[lane + 192]);
     const double mass = ceil((double)q.p * o.total * ldexp(1.0, bits));
-    // (where k_filter_gather took min-p for the filter that keeps less, that was by an estimate: the weights from its logit on say whether it is)
-    bool good = o.found != BY_SHARE || o.type != BY_MASS || (double)over_q < mass;
+    // (where k_filter_gather took min-p for the filter that keeps less, that was by an estimate, or by counts that may have been cut off: the weights, and the count, from its
+    // logit on say whether it is)
+    bool good = o.found != BY_SHARE || (o.type == BY_MASS ? (double)over_q < mass : o.type != BY_COUNT || n_above <= q.k);
     if (o.found != BY_SHARE) {
         const bool count = o.found == BY_COUNT;
         u64 mine = 0;

@@ -27,3 +27,11 @@ def test_top_p_and_min_p_beside_a_finite_mask(vocab, mask, live, dtype):
     x = rng.uniform(0, 10, (len(t), vocab)) if live == "uniform" else rng.standard_normal((len(t), vocab))
     x[:, ::97] = mask
     check(x, rng.random(len(t)).astype(np.float32), t=t, p=p, m=m, dtype=type_of(dtype))
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+def test_top_k_and_min_p_over_few_logits(dtype):
+    """2^24 tokens of three logits, more of each in a part of the row than 16 bits count: top-k cuts the first logit's tokens, where min-p alone keeps all of them, or the second's"""
+    rng = np.random.default_rng(12)
+    x = rng.integers(0, 3, (2, 1 << 24)) * -0.5
+    check(x, f32(0.4, 0.9), k=np.array([5000000, 8000000], dtype=np.int32), m=f32(0.74, 0.5), dtype=type_of(dtype))
