@@ -111,7 +111,8 @@ __device__ __forceinline__ Params params_of(const FilterArgs& a, int b) {
 
 template <int CTRL, int ROWS = 0xF>
 __device__ __forceinline__ u64 dpp_u64(u64 v) { return __builtin_bit_cast(u64, lane64_dpp<CTRL, ROWS>(__builtin_bit_cast(double, v))); }
-__device__ __forceinline__ u64 of_lane(u64 v, int l) {     // l: the same in all lanes
+// Lane l's value; l is the same in all lanes.  Not for a branch that lane l may not be in: what the compiler copies or loads again there is not lane l's.
+__device__ __forceinline__ u64 of_lane(u64 v, int l) {
     return (u64)(u32)__builtin_amdgcn_readlane((int)(v >> 32), l) << 32 | (u32)__builtin_amdgcn_readlane((int)(u32)v, l);
 }
 __device__ __forceinline__ int wave_sum_int(int v) {
@@ -841,8 +842,9 @@ __device__ __forceinline__ Found last_item(S& s, int n, u64 lo, u64 hi, u64 limi
         u64 below = 0;
         int rank = 0;
         for (int j = 0; j < few; ++j) {
-            const bool less = of_lane(c, j) < c;
-            below += less ? of_lane(q, j) : 0;
+            const u64 c_j = of_lane(c, j), q_j = of_lane(q, j);
+            const bool less = c_j < c;
+            below += less ? q_j : 0;
             rank += less;
         }
         // the last of those that are kept
@@ -959,8 +961,9 @@ __device__ __forceinline__ ListCut list_cut(S& s, int n, u64 lo, u64 hi, int k, 
             below = 0;
             rank = 0;
             for (int j = 0; j < few; ++j) {
-                const bool less = of_lane(key, j) < key;
-                below += less ? of_lane(q, j) : 0;
+                const u64 key_j = of_lane(key, j), q_j = of_lane(q, j);
+                const bool less = key_j < key;
+                below += less ? q_j : 0;
                 rank += less;
             }
         }
