@@ -599,6 +599,8 @@ tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t ro
  * Sums are of 64 bits, of whole numbers of 2^-36 of the largest weight (vocabularies of 2^24 tokens) to 2^-50 or finer or of fp64 in a fixed order, so a row's outputs depend neither on
  * the order of the work nor on other rows' contents; exponentials are within 2e-13 of themselves.  A row without a distribution (a NaN, +infinity, nothing above -infinity, a temperature below 0 or a NaN as one of its parameters) gives
  * token -1 with a NaN as logprob, 0 kept.
+ * token, logprob and kept may each be written over one of the fp32 or int32 arrays [rows] that are read; otherwise nothing that is written, the workspace among it, may overlap
+ * what is read or written beside it (TASC_EINVAL).
  * The workspace is 16-byte aligned; calls that may overlap need their own.  Rows that keep up to about 500 tokens (of vocabularies beyond 1280) are served from one read of
  * their logits; those that keep more are read three times, and a few (a top-k beyond 500 together with a top-p, thousands of equal logits at the border) take
  * a row's workgroup 100 us and more.
@@ -612,7 +614,7 @@ tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t row_stride
  * The same filters as masked logits: out [batch, k + 1, vocab] is logits where a token is kept, else -infinity, so tasc_accept_sampled over it, with the same
  * temperature, verifies drafts under them.  Parameters are a sequence's ([batch]); out may be logits, with the same stride; kept
  * int32[batch, k + 1], nullable.  Logits that are no distribution are passed on as they are, and under a temperature below 0 or a NaN as a parameter nothing is kept, so that
- * tasc_accept_sampled refuses both (0 kept).  vocab, rows and errors as for tasc_sample, k in [0, TASC_MAX_K].
+ * tasc_accept_sampled refuses both (0 kept).  Overlaps, vocab, rows and errors as for tasc_sample, k in [0, TASC_MAX_K].
  */
 tasc_status tasc_filter_logits(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab,
                                const float* temperature, const int32_t* top_k, const float* top_p, const float* min_p, void* out,

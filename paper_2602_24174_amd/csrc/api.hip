@@ -717,6 +717,8 @@ tasc_status sampled_of(const char* who, const tasc_model* m, const tasc_session*
             tasc_set_error("%s: the filters' workspace holds %zu of %zu bytes", who, f.ws_bytes, room);
             return TASC_ENOMEM;
         }
+        const tasc_status rc = tasc_filter_apart(who, p->scratch, need, s->batch, k, m->desc.vocab, p->temperature, f.top_k, f.top_p, f.min_p, p->scratch, need, nullptr, f.workspace);
+        if (rc != TASC_OK) return rc;
     }
     *out = TascSampled{p->temperature, p->u, p->n_u, logprob, (float*)p->scratch, (char*)p->scratch + tasc_sample_logits_bytes(s->batch, k, m->desc.vocab), f};
     return TASC_OK;

@@ -1822,6 +1822,22 @@ tasc_status check_workspace(const char* who, void* workspace, size_t ws_bytes, i
     TASC_REQUIRE(((uintptr_t)workspace & 15) == 0, "%s: the workspace must be 16-byte aligned", who);
     return TASC_OK;
 }
+// What a call reads and writes.  (The workspace holds rows' numbers that kernels go by.  A row's word may be written over one of its own that is read: that is done
+// when all of the row's work is.)
+struct Area { const char* name; const void* at; size_t bytes; bool words; };      // words: one of each row
+template <size_t R, size_t W>
+tasc_status check_apart(const char* who, const Area (&read)[R], const Area (&written)[W]) {
+    auto apart = [](const Area& x, const Area& y) {
+        return !x.at || !y.at || x.bytes == 0 || y.bytes == 0 || (uintptr_t)x.at + x.bytes <= (uintptr_t)y.at || (uintptr_t)y.at + y.bytes <= (uintptr_t)x.at;
+    };
+    for (const Area& w : written) {
+        for (const Area& r : read)
+            TASC_REQUIRE(apart(w, r) || (w.words && r.words && w.at == r.at && w.bytes == r.bytes), "%s: %s and %s overlap", who, w.name, r.name);
+        for (const Area* v = written; v != &w; ++v) TASC_REQUIRE(apart(w, *v), "%s: %s and %s overlap", who, w.name, v->name);
+    }
+    return TASC_OK;
+}
+size_t rows_bytes(int64_t rows, int64_t row_stride, int32_t vocab, tasc_dtype dtype) { return (size_t)((rows - 1) * row_stride + vocab) * (dtype == TASC_F32 ? 4 : 2); }
 
 }  // namespace
 
@@ -1843,8 +1859,25 @@ extern "C" tasc_status tasc_sample(const void* logits, tasc_dtype dtype, int64_t
     TASC_REQUIRE(u && token, "sample: null argument");
     rc = check_workspace("sample", workspace, ws_bytes, rows, vocab);
     if (rc != TASC_OK) return rc;
+    const size_t n = (size_t)rows * 4;
+    const Area read[] = {{"logits", logits, rows_bytes(rows, row_stride, vocab, dtype), false}, {"temperature", temperature, n, true}, {"top_k", top_k, n, true},
+                         {"top_p", top_p, n, true}, {"min_p", min_p, n, true}, {"u", u, n, true}};
+    const Area written[] = {{"token", token, n, true}, {"logprob", logprob, n, true}, {"kept", kept, n, true}, {"workspace", workspace, tasc_sample_workspace_bytes(rows, vocab), false}};
+    rc = check_apart("sample", read, written);
+    if (rc != TASC_OK) return rc;
     const FilterArgs a{logits, row_stride, 1, vocab, temperature, top_k, top_p, min_p, u, token, logprob, kept};
     return dtype == TASC_F32 ? enqueue<float, false>(a, rows, workspace, (hipStream_t)stream) : enqueue<BF16, false>(a, rows, workspace, (hipStream_t)stream);
+}
+
+tasc_status tasc_filter_apart(const char* who, const void* logits, size_t logits_bytes, int32_t batch, int32_t k, int32_t vocab, const float* temperature, const int32_t* top_k,
+                              const float* top_p, const float* min_p, const void* out, size_t out_bytes, const int32_t* kept, const void* workspace) {
+    const size_t n = (size_t)batch * 4;
+    const Area read[] = {{"temperature", temperature, n, true}, {"top_k", top_k, n, true}, {"top_p", top_p, n, true}, {"min_p", min_p, n, true}};
+    const Area written[] = {{"out", out, out_bytes, false}, {"kept", kept, n * (k + 1), true}, {"workspace", workspace, tasc_sample_workspace_bytes(batch * (k + 1), vocab), false}};
+    const tasc_status rc = check_apart(who, read, written);
+    if (rc != TASC_OK || out == logits) return rc;
+    const Area from[] = {{"logits", logits, logits_bytes, false}}, beside[] = {written[1], written[2]};
+    return check_apart(who, from, beside);
 }
 
 extern "C" tasc_status tasc_filter_logits(const void* logits, tasc_dtype dtype, int64_t row_stride, int32_t batch, int32_t k, int32_t vocab, const float* temperature,
@@ -1858,9 +1891,11 @@ extern "C" tasc_status tasc_filter_logits(const void* logits, tasc_dtype dtype, 
     const size_t size = dtype == TASC_F32 ? 4 : 2;
     TASC_REQUIRE(out_stride >= vocab && (uintptr_t)out % size == 0, "filter_logits: rows of %d logits to write lie %lld apart, or are not aligned to their type", vocab,
                  (long long)out_stride);
-    const uintptr_t from = (uintptr_t)logits, to = (uintptr_t)out, from_n = ((rows - 1) * row_stride + vocab) * size, to_n = ((rows - 1) * out_stride + vocab) * size;
+    const uintptr_t from = (uintptr_t)logits, to = (uintptr_t)out, from_n = rows_bytes(rows, row_stride, vocab, dtype), to_n = rows_bytes(rows, out_stride, vocab, dtype);
     TASC_REQUIRE((out == logits && out_stride == row_stride) || from + from_n <= to || to + to_n <= from, "filter_logits: logits and out overlap without being one");
     rc = check_workspace("filter_logits", workspace, ws_bytes, (int32_t)rows, vocab);
+    if (rc != TASC_OK) return rc;
+    rc = tasc_filter_apart("filter_logits", logits, from_n, batch, k, vocab, temperature, top_k, top_p, min_p, out, to_n, kept, workspace);
     if (rc != TASC_OK) return rc;
     const FilterArgs a{logits, row_stride, k + 1, vocab, temperature, top_k, top_p, min_p, nullptr, nullptr, nullptr, kept, out, out_stride};
     return dtype == TASC_F32 ? enqueue<float, true>(a, (int)rows, workspace, (hipStream_t)stream) : enqueue<BF16, true>(a, (int)rows, workspace, (hipStream_t)stream);

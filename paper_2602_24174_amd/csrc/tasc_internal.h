@@ -366,6 +366,9 @@ struct TascVerifyTail {
 // sample.hip: the acceptance of a verify step that samples, from the logits that its forward left
 tasc_status tasc_sample_step(const tasc_session* s, const TascVerifyTail& tail, hipStream_t st);
 size_t tasc_sample_logits_bytes(int32_t batch, int32_t k, int32_t vocab);     // of the scratch: the logits, then the parts
+// filter.hip: refuses arrays of tasc_filter_logits that overlap
+tasc_status tasc_filter_apart(const char* who, const void* logits, size_t logits_bytes, int32_t batch, int32_t k, int32_t vocab, const float* temperature, const int32_t* top_k,
+                              const float* top_p, const float* min_p, const void* out, size_t out_bytes, const int32_t* kept, const void* workspace);
 
 // library-wide options (tasc_config_set)
 // Layout of ONE copy of the small-batch kernels' activation buffers (each written once per launch): byte offsets, strides

@@ -35,3 +35,34 @@ def test_top_k_and_min_p_over_few_logits(dtype):
     rng = np.random.default_rng(12)
     x = rng.integers(0, 3, (2, 1 << 24)) * -0.5
     check(x, f32(0.4, 0.9), k=np.array([5000000, 8000000], dtype=np.int32), m=f32(0.74, 0.5), dtype=type_of(dtype))
+
+
+@pytest.mark.parametrize("vocab", [900, 30000])
+def test_words_of_a_row_over_those_that_it_reads(vocab):
+    """token, logprob and kept in the place of parameters and random numbers: as beside them"""
+    import torch
+    import paper_2602_24174_amd as T
+    from test_gpu_sample import dev, logits_of, settings
+    rng = np.random.default_rng(vocab)
+    rows = 64
+    x, u = dev(logits_of(rng, rows, vocab, "flat").astype(np.float32)), dev(rng.random(rows).astype(np.float32))
+    x[::2, :8] += 9.0                                      # every other row keeps few tokens
+    per = [dev(a) for a in settings(rng, rows)]
+    new = lambda t: torch.zeros(rows, dtype=t, device="cuda")
+    want = new(torch.int32), new(torch.float32), new(torch.int32)
+    T.tasc_sample(x, u, want[0], *per, want[1], want[2])
+    masks, counts = torch.zeros((rows, 1, vocab), device="cuda"), torch.zeros((rows, 1), dtype=torch.int32, device="cuda")
+    T.tasc_filter_logits(x[:, None], masks, *per, counts)
+    for i, name in enumerate(("u", "t", "k", "p", "m")):
+        at = dict(zip(("u", "t", "k", "p", "m"), (u.clone(), *(a.clone() for a in per))))
+        for out in range(3):
+            args = {n: a.clone() for n, a in at.items()}
+            got = [torch.zeros_like(w) for w in want]
+            got[out] = args[name].view(got[out].dtype)
+            T.tasc_sample(x, args["u"], got[0], args["t"], args["k"], args["p"], args["m"], got[1], got[2])
+            assert all(torch.equal(a.view(torch.int32), b.view(torch.int32)) for a, b in zip(got, want)), (name, out)
+        if name != "u":
+            args = {n: a.clone() for n, a in at.items()}
+            out, kept = torch.zeros_like(masks), args[name].view(torch.int32)[:, None]
+            T.tasc_filter_logits(x[:, None], out, args["t"], args["k"], args["p"], args["m"], kept)
+            assert torch.equal(out, masks) and torch.equal(kept, counts), name

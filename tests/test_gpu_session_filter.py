@@ -138,3 +138,29 @@ def test_filters_that_are_replaced_while_a_step_is_under_way():
         assert ((z > float("-inf")).sum(2) == 2).all()
         outs.append((accept.tolist(), emitted.tolist()))
     assert outs[0] == outs[1]
+
+
+def test_filters_that_overlap_what_a_step_writes():
+    """Refused before anything of the step is enqueued"""
+    import torch
+    rig = rig_of("tiled")
+    T, B, k = rig.T, rig.batch, rig.cfg.k
+    u = randoms(B, 4)
+    drafts = torch.zeros((B, k), dtype=torch.int32, device="cuda")
+    ws = torch.zeros(T.tasc_sample_workspace_bytes(B * (k + 1), rig.cfg.vocab), dtype=torch.uint8, device="cuda")
+    scratch = torch.zeros(T.tasc_sampled_scratch_bytes(rig.model, B, k) + ws.numel(), dtype=torch.uint8, device="cuda")       # (room for both)
+    ones = lambda at: at[256:256 + 4 * B].view(torch.int32).fill_(1)
+    accept, emitted = torch.zeros(B, dtype=torch.int32, device="cuda"), torch.zeros((B, k + 1), dtype=torch.int32, device="cuda")
+    step = lambda: T.tasc_verify_step_sampled(rig.model, rig.session, drafts, k, u, None, accept, emitted, None, scratch)
+    T.tasc_session_prefill(rig.model, rig.session, rig.prompts, rig.prompt_off, 4)
+    T.tasc_session_rewind(rig.session)
+    step()
+    want = accept.tolist(), emitted.tolist()
+    T.tasc_session_rewind(rig.session)
+    for top_k, workspace in ((ones(ws), ws), (ones(scratch), ws), (ones(torch.zeros(1024, dtype=torch.uint8, device="cuda")), scratch)):
+        T.tasc_session_filter(rig.session, top_k=top_k, workspace=workspace)
+        with pytest.raises(T.TascError, match="overlap"):
+            step()
+    T.tasc_session_filter(rig.session)
+    step()
+    assert (accept.tolist(), emitted.tolist()) == want

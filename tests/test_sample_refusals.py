@@ -64,3 +64,21 @@ def test_host_tensors_are_refused():
     for call in (lambda: T.tasc_sample(torch.zeros((4, 8)), f, i), lambda: T.tasc_filter_logits(torch.zeros((4, 1, 8)), torch.zeros((4, 1, 8)))):
         with pytest.raises(T.TascError):
             call()
+
+
+def test_arrays_that_overlap():
+    need = T.tasc_sample_workspace_bytes(3, 5000)
+    sample = dict(logits=A, dtype=0, stride=5000, rows=3, vocab=5000, t=2 * A, k=3 * A, p=4 * A, m=5 * A, u=6 * A, token=7 * A, logprob=8 * A, kept=9 * A, ws=10 * A, n=need)
+    masks = dict(logits=A, dtype=0, stride=5000, batch=3, k=0, vocab=5000, t=2 * A, tk=3 * A, p=4 * A, m=5 * A, out=6 * A, out_stride=5000, kept=9 * A, ws=10 * A, n=need)
+    rows = 4 * 15000                                        # bytes of the logits
+    for name, good, written, read in (("tasc_sample", sample, ("token", "logprob", "kept"), ("t", "k", "p", "m", "u")), ("tasc_filter_logits", masks, ("kept",), ("t", "tk", "p", "m"))):
+        bad = [{w: good[r] + 4} for w in written for r in read] + [{w: good[r] - 8} for w in written for r in read]         # (all of it over all of the other is not refused)
+        bad += [{w: good["ws"] + need - 4} for w in written] + [{w: A + rows - 4} for w in written] + [{r: good["ws"] + 64} for r in read]
+        bad += [{w: good[v] + 8} for w in written for v in written if v != w] + [{w: good[v]} for w in written for v in written if v != w]
+        bad += [{"ws": A + 16}, {"ws": A}, {"logits": good["ws"] + need - 16}]
+        if "out" in good:
+            bad += [{"out": good["ws"] + 4096}, {"out": good["ws"] - rows + 4}, {"kept": 6 * A + rows - 4}, {"tk": 6 * A}, {"out": A, "ws": A + 32}, {"out": A, "kept": A + 8}]
+        for kw in bad:
+            assert status(name, *dict(good, **kw).values(), None) == B.TASC_EINVAL, (name, kw)
+    masks.update(k=1, batch=2, kept=3 * A, n=T.tasc_sample_workspace_bytes(4, 5000))        # a count a row over a top-k a sequence
+    assert status("tasc_filter_logits", *masks.values(), None) == B.TASC_EINVAL
