@@ -66,3 +66,42 @@ def test_words_of_a_row_over_those_that_it_reads(vocab):
             out, kept = torch.zeros_like(masks), args[name].view(torch.int32)[:, None]
             T.tasc_filter_logits(x[:, None], out, args["t"], args["k"], args["p"], args["m"], kept)
             assert torch.equal(out, masks) and torch.equal(kept, counts), name
+
+
+def by_index(rng, rows, vocab, kind):
+    """Logits whose level or mask goes by the token's index, as a vocabulary's do"""
+    x = rng.standard_normal((rows, vocab)) * 1.5
+    v = np.arange(vocab)
+    if kind.startswith("falling"):
+        x -= float(kind[7:]) * np.log10(1 + v)
+    elif kind.startswith("below"):                          # live below an index, and one token that ends a text
+        x[:, (v >= int(kind[5:]) * vocab // 151936) & (v != vocab * 9 // 10)] = -np.inf
+    elif kind == "last":                                    # nothing in the parts' first loads
+        x[:, :vocab - vocab // 20] = -np.inf
+    elif kind == "blocks":
+        x[:, v // 3000 % 2 == 0] = -np.inf
+    return x
+
+
+@pytest.mark.parametrize("rows, vocab, dtype", [(1, 151936, "f32"), (24, 151936, "f32"), (64, 151936, "f32"), (24, 151936, "bf16"), (24, 50257, "f32"), (64, 5003, "f32")])
+@pytest.mark.parametrize("kind", ["falling0.5", "falling1", "below20000", "below32000", "below100000", "last", "blocks"])
+def test_logits_that_go_by_the_index(kind, rows, vocab, dtype):
+    rng = np.random.default_rng(rows + vocab + len(kind))
+    x = by_index(rng, rows, vocab, kind)
+    i = np.arange(rows)
+    # a row each without filters, by top-p, by top-k, by both, by all three, by min-p
+    k = np.where(np.isin(i % 6, (2, 3, 4)), rng.choice((5, 40, 100, 1000), rows), 0).astype(np.int32)
+    p = np.where(np.isin(i % 6, (1, 3, 4)), rng.uniform(0.5, 0.98, rows), 1.0).astype(np.float32)
+    m = np.where(np.isin(i % 6, (4, 5)), rng.uniform(0.001, 0.1, rows), 0.0).astype(np.float32)
+    if rows == 1:
+        k[:], p[:] = 100, 0.9
+    check(x, rng.random(rows).astype(np.float32), t=rng.uniform(0.5, 1.5, rows).astype(np.float32), k=k, p=p, m=m, dtype=type_of(dtype), mask=rows < 64)
+
+
+@pytest.mark.parametrize("dtype", ["f32", "bf16"])
+@pytest.mark.parametrize("vocab", [1279, 1280, 1281, 1282])
+@pytest.mark.parametrize("kind", ["peaked", "flat", "masked", "ties", "equal", "wide", "zeros"])
+def test_the_longest_rows_that_are_their_own_lists(kind, vocab, dtype):
+    from test_gpu_sample import logits_of, settings
+    rng = np.random.default_rng(vocab + len(kind))
+    check(logits_of(rng, 16, vocab, kind), rng.random(16).astype(np.float32), *settings(rng, 16), dtype=type_of(dtype))
