@@ -596,14 +596,18 @@ tasc_status tasc_accept_sampled(const void* logits, tasc_dtype dtype, int64_t ro
  *   top_p        fp32[rows], nullable; 1 and more keep all, 0 and less the first;  min_p fp32[rows], nullable; 0 and less keep all
  *   u            fp32[rows] in [0, 1)
  *   token        int32[rows];  logprob fp32[rows], nullable: ln of its share of the kept weights;  kept int32[rows], nullable: tokens kept
- * Sums are of 64 bits, of whole numbers of 2^-36 of the largest weight (vocabularies of 2^24 tokens) to 2^-50 or finer or of fp64 in a fixed order, so a row's outputs depend neither on
- * the order of the work nor on other rows' contents; exponentials are within 2e-13 of themselves.  A row without a distribution (a NaN, +infinity, nothing above -infinity, a temperature below 0 or a NaN as one of its parameters) gives
+ * Sums are of 64 bits, of whole numbers of 2^-36 of the largest weight (vocabularies of 2^24 tokens; 2^-43: of 151936) to 2^-50 or finer or of fp64 in a fixed order, so a row's
+ * outputs depend neither on the order of the work nor on other rows' contents (how many rows a call has may show in logprob's last bits, or where u falls on a border);
+ * exponentials are within 2e-13 of themselves.  A kept token that weighs less than half a unit is never drawn, and missing from the total: of 2^24 tokens such ones may
+ * together weigh up to 2^-13 of the largest, of 151936 2^-26.  A row without a distribution (a NaN, +infinity, nothing above -infinity, a temperature below 0 or a NaN as one of its parameters) gives
  * token -1 with a NaN as logprob, 0 kept.
  * token, logprob and kept may each be written over one of the fp32 or int32 arrays [rows] that are read; otherwise nothing that is written, the workspace among it, may overlap
  * what is read or written beside it (TASC_EINVAL).
- * The workspace is 16-byte aligned; calls that may overlap need their own.  Rows that keep up to about 500 tokens (of vocabularies beyond 1280) are served from one read of
- * their logits; those that keep more are read three times, and a few (a top-k beyond 500 together with a top-p, thousands of equal logits at the border) take
- * a row's workgroup 100 us and more.
+ * The workspace is 16-byte aligned; calls that may overlap need their own.  Of vocabularies beyond 1280 one read of the logits finds a row's largest 200 to 750 if they are spread over
+ * the tokens' indices, 30 to 500, or none, where the logits go by the index (they fall along it; what is not masked lies in a block).  Rows that keep more than that are read
+ * three times.  By one workgroup from end to end, several times, go (80 to 400 us, of 151936): rows under a top-k that one read did not find together with a top-p; with thousands
+ * of equal logits at the border; without a top-k, if a part of the row (a 38th of 151936 where there are few rows, a tenth where there are many) is masked but for a few tokens;
+ * and flat ones under a top-p whose masks are large numbers (-10000) instead of -infinity.
  * Limits: rows <= 65535, vocab in [2, 2^24].  Errors: TASC_EINVAL, TASC_ENOMEM (workspace), TASC_EHIP.
  */
 size_t tasc_sample_workspace_bytes(int32_t rows, int32_t vocab);   /* for tasc_filter_logits, too, with rows = batch * (k + 1) */
